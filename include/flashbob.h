@@ -324,6 +324,98 @@ int32_t attn_bob3_rows(int32_t dtype, int64_t B, int64_t H, int64_t N, int64_t d
                        const void* gdK, const void* gdV, const float* L, const float* D, const float* alpha,
                        void* Qt, void* dOt, float* E, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Attention between sequences of two lengths, with an optional learned bias by
+ * buckets of relative position: cross attention to an encoder's states,
+ * self-attention with a position bias, and the continuation of sequences whose
+ * keys lie in a cache (one new token or several).
+ *
+ * Shapes: query-side matrices (Q, O, dO, gdQ, dQ, Qt, dOt) are [B,H,Nq,d], key-side
+ * ones (K, V, gdK, gdV, dK, dV, Kt, Vt) [B,Hkv,Nk,d], row vectors fp32 [B,H,Nq].  H is
+ * a multiple of Hkv as in the _gqa calls.  Nq and Nk are independent and may be 0
+ * (without keys every row is empty, without queries dK = dV = 0); pointers of empty
+ * matrices are not read.
+ *
+ * Per batch entry b, with key position j and query position s_b + i:
+ *   S_ij = scale q_i . k_j + table[buckets[clamp(j - (s_b + i), -R, R) + R], h]
+ *   key j is valid for query row i if i < q_lens[b], j < kv_lens[b] and, with causal = 1,
+ *   j <= s_b + i.
+ * A row without a valid key (and every row i >= q_lens[b]) is empty: O = 0, L = -inf, D = alpha
+ * = E = 0, its gradients are 0 and it adds nothing to any other.  Keys j >= kv_lens[b] get zero
+ * gradients; neither they nor query rows i >= q_lens[b] are read, so they may hold anything.
+ *
+ * attn_ext (NULL: no lengths, positions from 0, no bias); all pointers are device
+ * memory of the current device:
+ *  q_lens, kv_lens  int32 [B] or NULL (all rows valid).  A value outside 0..Nq (0..Nk)
+ *          counts as the nearer end.
+ *  q_starts  int32 [B] or NULL (0): the position s_b of the first query row; values
+ *          beyond +-2^29 count as those.
+ *  table   [num_buckets, H] in table_dtype (BOB_F32 or BOB_BF16), aligned to its
+ *          type, or NULL: no bias (the other bias fields are then ignored).  An entry of
+ *          -1e30 or less (-inf and the types' lowest values among them) makes its
+ *          bucket's keys invalid.
+ *  buckets int32 [2 max_distance + 1]: the bucket of every step of position from -R
+ *          to R (R = max_distance, 1..1024); steps beyond use the ends.  A bucket outside
+ *          0..num_buckets - 1 counts as the nearer end.  num_buckets is 1..65536.
+ *
+ * Gradients.  dT[c,h] = sum of dS_ij over the pairs of bucket c, over the batch and both
+ * sequences (scale does not enter), in the table's layout and type, summed in fp32.  With a
+ * cotangent gdT (= U_T) on it, Phi gains <dT,U_T>: F_ij gains U_T[bucket,h], and Tt[c,h], the sum of
+ * St_ij over the bucket, is Phi's gradient in the table; every other formula of the calls
+ * above stands.  D here is the exact fp32 sum_j P_ij dP_ij, not do_i . o_i with o_i rounded.
+ *
+ * Workspaces are as those of the *_ws calls: the query gives the size for the same
+ * problem and attn_ext (of which it reads the table's presence and the sizes alone), 0 if
+ * none is needed; a NULL, misaligned (16 bytes) or too small one gives BOB_EINVAL.
+ * Errors as above; BOB_EINVAL also for a bias whose sizes are out of range or whose
+ * buckets are NULL. */
+typedef struct {
+  const int32_t* q_lens;
+  const int32_t* kv_lens;
+  const int32_t* q_starts;
+  const void* table;
+  const int32_t* buckets;
+  int32_t table_dtype;
+  int32_t num_buckets;
+  int32_t max_distance;
+} attn_ext;
+
+/* Forward.  In: Q, K, V.  Out: O, L. */
+int32_t attn_ext_fwd_lse(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
+                         float scale, int32_t causal, const attn_ext* ext, const void* Q, const void* K, const void* V,
+                         void* O, float* L, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* First backward.  In: Q, K, V, O, dO, L.  Out: dQ, dK, dV, D and, with a table, dT (may be
+ * NULL: not wanted). */
+int32_t attn_ext_bwd(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d, float scale,
+                     int32_t causal, const attn_ext* ext, const void* Q, const void* K, const void* V, const void* O,
+                     const void* dO, const float* L, void* dQ, void* dK, void* dV, float* D, void* dT, void* workspace,
+                     int64_t workspace_bytes, void* stream);
+
+/* BoB Pass 1.  In: Q, K, V, O, dO, gdQ, gdK, gdV, gdT (may be NULL: 0), L, D, dQ (required).
+ * Out: Qt, dOt, alpha, E.  D must be attn_ext_bwd's. */
+int32_t attn_ext_pass1_rows(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
+                            float scale, int32_t causal, const attn_ext* ext, const void* Q, const void* K,
+                            const void* V, const void* O, const void* dO, const void* gdQ, const void* gdK,
+                            const void* gdV, const void* gdT, const float* L, const float* D, const void* dQ, void* Qt,
+                            void* dOt, float* alpha, float* E, void* stream);
+
+/* BoB Pass 2, after Pass 1.  In: Q, K, V, dO, gdQ, gdK, gdV, gdT (may be NULL: 0), L, D, alpha, E.
+ * Out: Kt, Vt and, with a table, Tt (may be NULL: not wanted). */
+int32_t attn_ext_pass2_cols(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
+                            float scale, int32_t causal, const attn_ext* ext, const void* Q, const void* K,
+                            const void* V, const void* dO, const void* gdQ, const void* gdK, const void* gdV,
+                            const void* gdT, const float* L, const float* D, const float* alpha, const float* E,
+                            void* Kt, void* Vt, void* Tt, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Workspace bytes of the calls above on the current device (0: none, or the call reports an error). */
+int64_t attn_ext_fwd_workspace_bytes(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,
+                                     int64_t d, int32_t causal, const attn_ext* ext);
+int64_t attn_ext_bwd_workspace_bytes(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,
+                                     int64_t d, int32_t causal, const attn_ext* ext);
+int64_t attn_ext_pass2_workspace_bytes(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,
+                                       int64_t d, int32_t causal, const attn_ext* ext);
+
 /* 1 if (dtype, d) is built into this library, else 0. */
 int32_t bob_supported(int32_t dtype, int64_t d);
 

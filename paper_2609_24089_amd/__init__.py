@@ -90,7 +90,8 @@ def load_library():
     lib.attn_bob_pass2_cols_gqa_noalloc.restype = i32
     lib.bob_scratch_bytes.argtypes = []
     lib.bob_scratch_bytes.restype = i64
-    from . import _fb_torch
+    from . import _fb_torch, ext
+    ext._declare(lib)
     _fb_torch.bind(LIB_PATH)
     _lib, _native = lib, _fb_torch
     return lib
@@ -427,3 +428,6 @@ def bob(Q, K, V, dO, gdQ, gdK, gdV, scale, causal=False, use_dq=True, stream=Non
 
 
 from .autograd import attention  # noqa: E402  (differentiable wrapper; imports the entry points above)
+from .ext import (  # noqa: E402  (attention between sequences of two lengths, with a position bias)
+    AttnExt, attn_ext_bwd, attn_ext_fwd_lse, attn_ext_pass1_rows, attn_ext_pass2_cols, biased_attention,
+    cross_attention, relative_buckets)

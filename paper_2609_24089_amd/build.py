@@ -22,6 +22,12 @@ SOURCES = [
     ("fb_pass1_small.hip", []),
     ("fb_cols_small.hip", []),
     ("fb_passes_d128.hip", ["-mllvm", "-amdgpu-sched-strategy=iterative-ilp"]),
+    ("fb_ext.hip", []),
+    ("fb_ext_fwd.hip", []),
+    ("fb_ext_bwd.hip", []),
+    ("fb_ext_pass1.hip", []),
+    ("fb_ext_pass2.hip", []),
+    ("fb_ext_bob_d128.hip", ["-mllvm", "-amdgpu-sched-strategy=iterative-ilp"]),
 ]
 
 # -packed-fp32-ops keeps hipcc from emitting v_pk_*_f32 (the host pass warns

@@ -1,0 +1,154 @@
+// Host side of the attention between sequences of two lengths (fb_ext_kernels.h): problem,
+// validation, launch forms and the per-(dtype, head dim) launchers, shared by its
+// translation units.  fb_ext.hip holds the C ABI.
+#pragma once
+#include "fb_ext_kernels.h"
+#include "fb_launch.h"
+
+namespace fb {
+
+constexpr int kMaxDistance = 1024;     // R: two tables of 2 (R + 64) + 1 floats beside the largest rings
+constexpr int kMaxBuckets = 1 << 16;
+constexpr int64_t kMaxLds = 160 * 1024;
+
+struct ExtProblem {
+  int32_t dtype;
+  int64_t B, H, Hkv, Nq, Nk, d;
+  float scale;
+  int32_t causal;
+  attn_ext x;   // zeros where the caller gave none
+};
+inline bool has_bias(const ExtProblem& p) { return p.x.table != nullptr; }
+inline int ext_group(const ExtProblem& p) { return (int)(p.H / p.Hkv); }
+inline int64_t ext_width(const ExtProblem& p) { return 2 * (int64_t)p.x.max_distance + 3; }
+
+// How a launch runs: blocks of 16 `blocks` stationary rows, `sets` wave sets, `parts`
+// workgroups a block; folded rows (row kernels).
+struct ExtPlan {
+  int form = 0, blocks = 4, sets = 1, parts = 1;
+  bool fold = false;
+};
+
+inline ExtArgs ext_args(const ExtProblem& p, const ExtPlan& c, int64_t heads, int64_t rows, const void* dir) {
+  ExtArgs a{};
+  a.H = (int)p.H;
+  a.grp = ext_group(p);
+  a.Nq = (int)p.Nq;
+  a.Nk = (int)p.Nk;
+  a.nRB = (int)((rows + 16 * c.blocks - 1) / (16 * c.blocks));
+  a.total = (int)(heads * a.nRB);
+  a.causal = p.causal;
+  a.fold = c.fold ? 1 : 0;
+  a.scale = p.scale;
+  a.nparts = c.parts;
+  a.q_lens = p.x.q_lens;
+  a.kv_lens = p.x.kv_lens;
+  a.q_starts = p.x.q_starts;
+  a.table = p.x.table;
+  a.dir = dir;
+  a.buckets = p.x.buckets;
+  a.table_bf16 = p.x.table_dtype == BOB_BF16 ? 1 : 0;
+  a.num_buckets = p.x.num_buckets;
+  a.R = p.x.max_distance;
+  return a;
+}
+
+// LDS of the bias tables, in bytes.
+inline int64_t ext_steps_bytes(const ExtProblem& p) {
+  return has_bias(p) ? 4 * ((2 * (int64_t)(p.x.max_distance + kStepPad) + 1 + 3) / 4 * 4) : 0;
+}
+
+// Launches (defined per translation unit; instantiated for every (dtype, head dim)).
+template <typename T, int D> ExtPlan ext_fwd_plan(const ExtProblem& p);
+template <typename T, int D>
+int32_t ext_launch_fwd(const ExtProblem& p, const void* Q, const void* K, const void* V, void* O, float* L, float* ws,
+                       hipStream_t s);
+template <typename T, int D> ExtPlan ext_cols_plan(const ExtProblem& p);
+template <typename T, int D>
+int32_t ext_launch_bwd(const ExtProblem& p, const void* Q, const void* K, const void* V, const void* O, const void* dO,
+                       const float* L, void* dQ, void* dK, void* dV, float* Dv, float* parts, float* sums,
+                       hipStream_t s);
+template <typename T, int D>
+int32_t ext_launch_pass1(const ExtProblem& p, const void* Q, const void* K, const void* V, const void* O,
+                         const void* dO, const void* UQ, const void* UK, const void* UV, const void* UT,
+                         const float* L, const float* Dv, const void* dQ, void* Qt, void* dOt, float* alpha, float* E,
+                         hipStream_t s);
+template <typename T, int D> ExtPlan ext_pass2_plan(const ExtProblem& p);
+template <typename T, int D>
+int32_t ext_launch_pass2(const ExtProblem& p, const void* Q, const void* K, const void* V, const void* dO,
+                         const void* UQ, const void* UK, const void* UV, const void* UT, const float* L,
+                         const float* Dv, const float* alpha, const float* E, void* Kt, void* Vt, float* parts,
+                         float* sums, hipStream_t s);
+#define FB_EXT_EACH(M, ...) \
+  M(bf16, 32, __VA_ARGS__) M(bf16, 64, __VA_ARGS__) M(bf16, 128, __VA_ARGS__) M(bf16, 256, __VA_ARGS__) \
+  M(float, 32, __VA_ARGS__) M(float, 64, __VA_ARGS__) M(float, 128, __VA_ARGS__)
+
+// Adds the parts of a column kernel (plane elements each, two planes a part) into X and Y.
+int32_t ext_add_parts(const ExtProblem& p, const float* parts, int nparts, void* X, void* Y, hipStream_t s);
+
+// A kernel's LDS beside its dynamic part, as the runtime tells it.
+template <auto kKernel> int64_t static_lds() {
+  static std::atomic<int> known;
+  return read_once(known, [] {
+    hipFuncAttributes at;
+    if (hipFuncGetAttributes(&at, (const void*)kKernel) != hipSuccess) return 0;
+    return (int)at.sharedSizeBytes + 1;  // 0 is read again
+  });
+}
+
+// ---------------------------------------------------------------------------
+// Row kernels: whole blocks, 64-row blocks in wave sets, 16-row blocks in sets of one wave.
+// Kern<form, bias>::kernel() names the kernel, Kern::shape(form) its shape.
+// ---------------------------------------------------------------------------
+struct ExtShape {
+  int mr, nw, occ, st, ks;
+  constexpr int threads() const { return 64 * nw * ks; }
+  constexpr int blocks() const { return mr * nw; }
+  constexpr bool built() const { return mr > 0; }
+};
+constexpr ExtShape kNotBuilt{0, 1, 1, 2, 1};
+
+// Sets of `tensors` streamed tensors in blocks of nw waves of 16 rows, if more than one fits.
+template <typename T, int D> constexpr ExtShape ext_sets(int nw, int tensors, int extra, int max_waves, int occ) {
+  const SetShape s = set_shape<T, D>(nw, tensors, extra, max_waves, 1);
+  const int lds = s.ks * (2 * tensors * Geo<T, D>::kTileElems * (int)sizeof(T) + extra);
+  // as many waves a SIMD as the workgroups that the LDS holds bring, `occ` at most
+  const int fit = s.ks * nw * (160 * 1024 / lds) / 4;
+  return s.ks > 1 ? ExtShape{1, nw, std::max({1, s.ks * nw / 4, std::min(occ, fit)}), 2, s.ks} : kNotBuilt;
+}
+
+template <typename Kern, int F> Form ext_form_of(const ExtProblem& p, int64_t dynamic, double narrow) {
+  constexpr ExtShape s = Kern::shape(F);
+  if constexpr (s.built()) {
+    const bool bias = has_bias(p);
+    const int64_t lds = bias ? static_lds<Kern::template kernel<F, true>()>() : static_lds<Kern::template kernel<F, false>()>();
+    if (F > 0 && lds + dynamic > kMaxLds) return {};
+    const int fit = bias ? resident_blocks<Kern::template kernel<F, true>()>(s.threads())
+                         : resident_blocks<Kern::template kernel<F, false>()>(s.threads());
+    return {s.blocks(), s.ks, fit, s.threads(), 1, 0.0, F == 0 ? 1.0 : narrow};
+  }
+  return {};
+}
+
+// The current device's dense grids run without the balanced causal order.
+template <typename Kern, int F, typename... Args>
+int32_t ext_go(const ExtProblem& p, dim3 grid, int64_t dynamic, hipStream_t stream, Args... args) {
+  constexpr ExtShape s = Kern::shape(F);
+  if constexpr (s.built()) {
+    (void)hipGetLastError();
+    if (has_bias(p))
+      hipLaunchKernelGGL((Kern::template kernel<F, true>()), grid, dim3(s.threads()), (unsigned)dynamic, stream, args...);
+    else
+      hipLaunchKernelGGL((Kern::template kernel<F, false>()), grid, dim3(s.threads()), 0, stream, args...);
+    return finish_launch();
+  }
+  return BOB_EUNSUPPORTED;
+}
+template <typename Kern, typename... Args>
+int32_t ext_dispatch(int form, const ExtProblem& p, dim3 grid, int64_t dynamic, hipStream_t stream, Args... args) {
+  if (form == 2) return ext_go<Kern, 2>(p, grid, dynamic, stream, args...);
+  if (form == 1) return ext_go<Kern, 1>(p, grid, dynamic, stream, args...);
+  return ext_go<Kern, 0>(p, grid, dynamic, stream, args...);
+}
+
+}  // namespace fb

@@ -1,0 +1,293 @@
+// C ABI of the attention between sequences of two lengths: validation and dispatch, and the
+// kernels that add parts and gather the bias table's gradients.  The entry points are
+// declared (and documented) in include/flashbob.h.
+#include "fb_ext.h"
+
+namespace fb {
+
+// Adds the waves' rows of step sums (StepSums) of head blockIdx.y: workgroup s of S takes
+// rows s, s + S, ... of the head's `rows` and writes one row of `mid` ([H][S][width]).
+__global__ __launch_bounds__(256) void ext_step_rows_kernel(const float* __restrict__ sums, int64_t rows, int width,
+                                                            float* __restrict__ mid) {
+  const float* const head = sums + (int64_t)blockIdx.y * rows * width;
+  float* const out = mid + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * width;
+  for (int x = threadIdx.x; x < width; x += 256) {
+    float v = 0.f;
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) v += head[r * width + x];
+    out[x] = v;
+  }
+}
+
+// Gathers head blockIdx.x's sums by step into its buckets.  Eight lanes share a bucket,
+// each takes every eighth step; the order of the sums is fixed.
+constexpr int kMaxWidth = 2 * kMaxDistance + 3;
+__global__ __launch_bounds__(256) void ext_buckets_kernel(const float* __restrict__ mid, int S, ExtArgs a,
+                                                          void* __restrict__ out) {
+  __shared__ float sum[kMaxWidth];
+  __shared__ int bucket[kMaxWidth];
+  const int width = 2 * a.R + 3;
+  for (int x = threadIdx.x; x < width; x += 256) {
+    float v = 0.f;
+    for (int s = 0; s < S; ++s) v += mid[((int64_t)blockIdx.x * S + s) * width + x];
+    sum[x] = v;
+    // the two sums beyond the steps belong to the buckets of the ends
+    const int step = x <= 2 * a.R ? x : x == 2 * a.R + 1 ? 0 : 2 * a.R;
+    bucket[x] = min(max(a.buckets[step], 0), a.num_buckets - 1);
+  }
+  __syncthreads();
+  const int lane = threadIdx.x & 7;
+  for (int c0 = 0; c0 < a.num_buckets; c0 += 32) {
+    const int c = c0 + (threadIdx.x >> 3);
+    float v = 0.f;
+    for (int x = lane; x < width; x += 8) v += bucket[x] == c ? sum[x] : 0.f;
+    v += __shfl_xor(v, 1);
+    v += __shfl_xor(v, 2);
+    v += __shfl_xor(v, 4);
+    if (lane == 0 && c < a.num_buckets) {
+      const int64_t at = (int64_t)c * a.H + blockIdx.x;
+      if (a.table_bf16 != 0)
+        ((bf16*)out)[at] = (bf16)v;
+      else
+        ((float*)out)[at] = v;
+    }
+  }
+}
+
+int32_t ext_add_parts(const ExtProblem& p, const float* parts, int nparts, void* X, void* Y, hipStream_t s) {
+  const int64_t plane = p.B * p.Hkv * p.Nk * p.d;
+  const unsigned blocks = (unsigned)std::min<int64_t>((plane / 2 + 255) / 256, 8192);
+  (void)hipGetLastError();
+  if (p.dtype == BOB_BF16)
+    hipLaunchKernelGGL(ext_parts_kernel<bf16>, dim3(blocks), dim3(256), 0, s, parts, nparts, plane, (bf16*)X, (bf16*)Y);
+  else
+    hipLaunchKernelGGL(ext_parts_kernel<float>, dim3(blocks), dim3(256), 0, s, parts, nparts, plane, (float*)X,
+                       (float*)Y);
+  return finish_launch();
+}
+
+// Returns BOB_OK to proceed, or an error; sets *empty where there is nothing to compute.
+static int32_t ext_check(const ExtProblem& p, bool* empty) {
+  *empty = false;
+  if (p.dtype != BOB_F32 && p.dtype != BOB_BF16) return BOB_EINVAL;
+  if (p.B < 0 || p.H < 0 || p.Nq < 0 || p.Nk < 0 || p.d < 1) return BOB_EINVAL;
+  if (!std::isfinite(p.scale)) return BOB_EINVAL;
+  if (p.causal != 0 && p.causal != 1) return BOB_EINVAL;
+  if (p.Hkv < 0 || (p.H > 0 && (p.Hkv < 1 || p.H % p.Hkv != 0))) return BOB_EINVAL;
+  if (!supported(p.dtype, p.d)) return BOB_EUNSUPPORTED;
+  auto aligned = [](const void* q, uintptr_t n) { return (reinterpret_cast<uintptr_t>(q) & (n - 1)) == 0; };
+  if (!aligned(p.x.q_lens, 4) || !aligned(p.x.kv_lens, 4) || !aligned(p.x.q_starts, 4)) return BOB_EINVAL;
+  if (has_bias(p)) {
+    if (p.x.table_dtype != BOB_F32 && p.x.table_dtype != BOB_BF16) return BOB_EINVAL;
+    if (!aligned(p.x.table, p.x.table_dtype == BOB_F32 ? 4 : 2)) return BOB_EINVAL;
+    if (p.x.buckets == nullptr || !aligned(p.x.buckets, 4)) return BOB_EINVAL;
+    if (p.x.num_buckets < 1 || p.x.num_buckets > kMaxBuckets) return BOB_EINVAL;
+    if (p.x.max_distance < 1 || p.x.max_distance > kMaxDistance) return BOB_EINVAL;
+  }
+  if (p.H == 0 || (p.B == 0 && !has_bias(p))) {
+    *empty = true;
+    return BOB_OK;
+  }
+  if (p.Nq > kMaxN || p.Nk > kMaxN) return BOB_EINVAL;
+  // 32-bit grids and loop counts: 16-row blocks of every head, and the query tiles of a
+  // group's heads, which one column block streams
+  const int64_t heads = p.B * p.H, rows = std::max(p.Nq, p.Nk);
+  if (p.B > INT32_MAX || p.H > 65535 || heads > INT32_MAX) return BOB_EINVAL;
+  if (heads * ((rows + 15) / 16) > INT32_MAX / 16) return BOB_EINVAL;
+  if (ext_group(p) * p.Nq > INT32_MAX / 2) return BOB_EINVAL;
+  return BOB_OK;
+}
+
+static ExtProblem ext_problem(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
+                              float scale, int32_t causal, const attn_ext* ext) {
+  ExtProblem p{dtype, B, H, Hkv, Nq, Nk, d, scale, causal, attn_ext{}};
+  if (ext != nullptr) p.x = *ext;
+  return p;
+}
+
+#define FB_EXT_DISPATCH(p, FN, ...)                                                   \
+  do {                                                                                \
+    if ((p).dtype == BOB_BF16 && (p).d == 32) return FN<fb::bf16, 32>(__VA_ARGS__);   \
+    if ((p).dtype == BOB_BF16 && (p).d == 64) return FN<fb::bf16, 64>(__VA_ARGS__);   \
+    if ((p).dtype == BOB_BF16 && (p).d == 128) return FN<fb::bf16, 128>(__VA_ARGS__); \
+    if ((p).dtype == BOB_BF16 && (p).d == 256) return FN<fb::bf16, 256>(__VA_ARGS__); \
+    if ((p).dtype == BOB_F32 && (p).d == 32) return FN<float, 32>(__VA_ARGS__);       \
+    if ((p).dtype == BOB_F32 && (p).d == 64) return FN<float, 64>(__VA_ARGS__);       \
+    return FN<float, 128>(__VA_ARGS__);                                               \
+  } while (0)
+
+// Pointers of matrices of `n` rows: aligned, and not NULL unless they are empty.
+static bool ext_ptrs(int64_t n, std::initializer_list<const void*> ptrs) {
+  if (n == 0) return true;
+  return check_ptrs(ptrs) == BOB_OK;
+}
+
+// Workspace of the forward: the parts' sums, references and weights.
+static int64_t fwd_bytes(const ExtProblem& p, const ExtPlan& c) {
+  return c.parts > 1 ? c.parts * p.B * p.H * p.Nq * (p.d + 2) * 4 : 0;
+}
+// Workspace of a column kernel: the parts' fp32 sums, then the waves' rows of step sums and
+// what ext_step_rows_kernel makes of them.
+struct ColBytes {
+  int64_t parts = 0, rows = 0, sums = 0, mid = 0;  // rows: of step sums of one head
+  int S = 1;
+  int64_t all() const { return parts + sums + mid; }
+};
+static ColBytes col_bytes(const ExtProblem& p, const ExtPlan& c) {
+  ColBytes b;
+  if (c.parts > 1) b.parts = (int64_t)c.parts * 2 * p.B * p.Hkv * p.Nk * p.d * 4;
+  if (has_bias(p)) {
+    const int64_t blocks = (p.Nk + 16 * c.blocks - 1) / (16 * c.blocks);
+    const int subs = c.parts > 1 ? c.parts / ext_group(p) : 1;
+    b.rows = p.B * blocks * subs * c.sets;
+    b.S = (int)std::max<int64_t>(1, std::min<int64_t>(64, b.rows));
+    auto pad = [](int64_t n) { return (n + 15) / 16 * 16; };
+    b.sums = pad(b.rows * p.H * ext_width(p) * 4);
+    b.mid = pad(b.S * p.H * ext_width(p) * 4);
+  }
+  return b;
+}
+
+static ExtPlan plan_fwd(const ExtProblem& p) { FB_EXT_DISPATCH(p, ext_fwd_plan, p); }
+static ExtPlan plan_cols(const ExtProblem& p) { FB_EXT_DISPATCH(p, ext_cols_plan, p); }
+static ExtPlan plan_pass2(const ExtProblem& p) { FB_EXT_DISPATCH(p, ext_pass2_plan, p); }
+static int32_t go_fwd(const ExtProblem& p, const void* Q, const void* K, const void* V, void* O, float* L, float* ws,
+                      hipStream_t s) {
+  FB_EXT_DISPATCH(p, ext_launch_fwd, p, Q, K, V, O, L, ws, s);
+}
+static int32_t go_bwd(const ExtProblem& p, const void* Q, const void* K, const void* V, const void* O, const void* dO,
+                      const float* L, void* dQ, void* dK, void* dV, float* D, float* parts, float* sums,
+                      hipStream_t s) {
+  FB_EXT_DISPATCH(p, ext_launch_bwd, p, Q, K, V, O, dO, L, dQ, dK, dV, D, parts, sums, s);
+}
+static int32_t go_pass1(const ExtProblem& p, const void* Q, const void* K, const void* V, const void* O,
+                        const void* dO, const void* UQ, const void* UK, const void* UV, const void* UT, const float* L,
+                        const float* D, const void* dQ, void* Qt, void* dOt, float* alpha, float* E, hipStream_t s) {
+  FB_EXT_DISPATCH(p, ext_launch_pass1, p, Q, K, V, O, dO, UQ, UK, UV, UT, L, D, dQ, Qt, dOt, alpha, E, s);
+}
+static int32_t go_pass2(const ExtProblem& p, const void* Q, const void* K, const void* V, const void* dO,
+                        const void* UQ, const void* UK, const void* UV, const void* UT, const float* L, const float* D,
+                        const float* alpha, const float* E, void* Kt, void* Vt, float* parts, float* sums,
+                        hipStream_t s) {
+  FB_EXT_DISPATCH(p, ext_launch_pass2, p, Q, K, V, dO, UQ, UK, UV, UT, L, D, alpha, E, Kt, Vt, parts, sums, s);
+}
+
+// The rows of step sums -> the table's gradient.
+static int32_t gather_table(const ExtProblem& p, const ColBytes& b, const float* sums, float* mid, void* out,
+                            hipStream_t s) {
+  const int width = (int)ext_width(p);
+  (void)hipGetLastError();
+  hipLaunchKernelGGL(ext_step_rows_kernel, dim3(b.S, (unsigned)p.H), dim3(256), 0, s, sums, b.rows, width, mid);
+  const ExtArgs a = ext_args(p, ExtPlan{}, 0, 0, nullptr);
+  hipLaunchKernelGGL(ext_buckets_kernel, dim3((unsigned)p.H), dim3(256), 0, s, (const float*)mid, b.S, a, out);
+  return finish_launch();
+}
+
+// A table's gradient pointer: not without a table, aligned to its type.
+static bool table_ptr(const ExtProblem& p, const void* t) {
+  if (t == nullptr) return true;
+  return has_bias(p) && (reinterpret_cast<uintptr_t>(t) & (p.x.table_dtype == BOB_F32 ? 3u : 1u)) == 0;
+}
+
+}  // namespace fb
+
+using fb::ExtProblem;
+
+extern "C" {
+
+int32_t attn_ext_fwd_lse(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
+                         float scale, int32_t causal, const attn_ext* ext, const void* Q, const void* K, const void* V,
+                         void* O, float* L, void* workspace, int64_t workspace_bytes, void* stream) {
+  const ExtProblem p = fb::ext_problem(dtype, B, H, Hkv, Nq, Nk, d, scale, causal, ext);
+  bool empty;
+  const int32_t rc = fb::ext_check(p, &empty);
+  if (rc != BOB_OK || empty || B == 0 || Nq == 0) return rc;
+  if (!fb::ext_ptrs(Nq, {Q, O, L}) || !fb::ext_ptrs(Nk, {K, V})) return BOB_EINVAL;
+  const int64_t need = fb::fwd_bytes(p, fb::plan_fwd(p));
+  if (need > 0 && (workspace_bytes < need || !fb::aligned16(workspace))) return BOB_EINVAL;
+  return fb::go_fwd(p, Q, K, V, O, L, (float*)workspace, (hipStream_t)stream);
+}
+
+int32_t attn_ext_bwd(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d, float scale,
+                     int32_t causal, const attn_ext* ext, const void* Q, const void* K, const void* V, const void* O,
+                     const void* dO, const float* L, void* dQ, void* dK, void* dV, float* D, void* dT, void* workspace,
+                     int64_t workspace_bytes, void* stream) {
+  const ExtProblem p = fb::ext_problem(dtype, B, H, Hkv, Nq, Nk, d, scale, causal, ext);
+  bool empty;
+  int32_t rc = fb::ext_check(p, &empty);
+  if (rc != BOB_OK || empty) return rc;
+  if (!fb::ext_ptrs(B * Nq, {Q, O, dO, L, dQ, D}) || !fb::ext_ptrs(B * Nk, {K, V, dK, dV}) || !fb::table_ptr(p, dT))
+    return BOB_EINVAL;
+  const fb::ColBytes b = fb::col_bytes(p, fb::plan_cols(p));
+  const int64_t need = b.all();
+  if (need > 0 && (workspace_bytes < need || !fb::aligned16(workspace))) return BOB_EINVAL;
+  char* const ws = (char*)workspace;
+  float* const sums = dT != nullptr ? (float*)(ws + b.parts) : nullptr;
+  if (B > 0) rc = fb::go_bwd(p, Q, K, V, O, dO, L, dQ, dK, dV, D, (float*)ws, sums, (hipStream_t)stream);
+  if (rc != BOB_OK || dT == nullptr) return rc;
+  return fb::gather_table(p, b, sums, (float*)(ws + b.parts + b.sums), dT, (hipStream_t)stream);
+}
+
+int32_t attn_ext_pass1_rows(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
+                            float scale, int32_t causal, const attn_ext* ext, const void* Q, const void* K,
+                            const void* V, const void* O, const void* dO, const void* gdQ, const void* gdK,
+                            const void* gdV, const void* gdT, const float* L, const float* D, const void* dQ, void* Qt,
+                            void* dOt, float* alpha, float* E, void* stream) {
+  const ExtProblem p = fb::ext_problem(dtype, B, H, Hkv, Nq, Nk, d, scale, causal, ext);
+  bool empty;
+  const int32_t rc = fb::ext_check(p, &empty);
+  if (rc != BOB_OK || empty || B == 0 || Nq == 0) return rc;
+  if (!fb::ext_ptrs(Nq, {Q, O, dO, gdQ, L, D, dQ, Qt, dOt, alpha, E}) || !fb::ext_ptrs(Nk, {K, V, gdK, gdV}) ||
+      !fb::table_ptr(p, gdT))
+    return BOB_EINVAL;
+  return fb::go_pass1(p, Q, K, V, O, dO, gdQ, gdK, gdV, gdT, L, D, dQ, Qt, dOt, alpha, E, (hipStream_t)stream);
+}
+
+int32_t attn_ext_pass2_cols(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
+                            float scale, int32_t causal, const attn_ext* ext, const void* Q, const void* K,
+                            const void* V, const void* dO, const void* gdQ, const void* gdK, const void* gdV,
+                            const void* gdT, const float* L, const float* D, const float* alpha, const float* E,
+                            void* Kt, void* Vt, void* Tt, void* workspace, int64_t workspace_bytes, void* stream) {
+  const ExtProblem p = fb::ext_problem(dtype, B, H, Hkv, Nq, Nk, d, scale, causal, ext);
+  bool empty;
+  int32_t rc = fb::ext_check(p, &empty);
+  if (rc != BOB_OK || empty) return rc;
+  if (!fb::ext_ptrs(B * Nq, {Q, dO, gdQ, L, D, alpha, E}) || !fb::ext_ptrs(B * Nk, {K, V, gdK, gdV, Kt, Vt}) ||
+      !fb::table_ptr(p, gdT) || !fb::table_ptr(p, Tt))
+    return BOB_EINVAL;
+  const fb::ColBytes b = fb::col_bytes(p, fb::plan_pass2(p));
+  const int64_t need = b.all();
+  if (need > 0 && (workspace_bytes < need || !fb::aligned16(workspace))) return BOB_EINVAL;
+  char* const ws = (char*)workspace;
+  float* const sums = Tt != nullptr ? (float*)(ws + b.parts) : nullptr;
+  if (B > 0 && Nk > 0)
+    rc = fb::go_pass2(p, Q, K, V, dO, gdQ, gdK, gdV, gdT, L, D, alpha, E, Kt, Vt, (float*)ws, sums,
+                      (hipStream_t)stream);
+  if (rc != BOB_OK || Tt == nullptr) return rc;
+  return fb::gather_table(p, b, sums, (float*)(ws + b.parts + b.sums), Tt, (hipStream_t)stream);
+}
+
+int64_t attn_ext_fwd_workspace_bytes(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,
+                                     int64_t d, int32_t causal, const attn_ext* ext) {
+  const ExtProblem p = fb::ext_problem(dtype, B, H, Hkv, Nq, Nk, d, 1.0f, causal, ext);
+  bool empty;
+  if (fb::ext_check(p, &empty) != BOB_OK || empty || B == 0 || Nq == 0) return 0;
+  return fb::fwd_bytes(p, fb::plan_fwd(p));
+}
+
+int64_t attn_ext_bwd_workspace_bytes(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,
+                                     int64_t d, int32_t causal, const attn_ext* ext) {
+  const ExtProblem p = fb::ext_problem(dtype, B, H, Hkv, Nq, Nk, d, 1.0f, causal, ext);
+  bool empty;
+  if (fb::ext_check(p, &empty) != BOB_OK || empty) return 0;
+  return fb::col_bytes(p, fb::plan_cols(p)).all();
+}
+
+int64_t attn_ext_pass2_workspace_bytes(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,
+                                       int64_t d, int32_t causal, const attn_ext* ext) {
+  const ExtProblem p = fb::ext_problem(dtype, B, H, Hkv, Nq, Nk, d, 1.0f, causal, ext);
+  bool empty;
+  if (fb::ext_check(p, &empty) != BOB_OK || empty) return 0;
+  return fb::col_bytes(p, fb::plan_pass2(p)).all();
+}
+
+}  // extern "C"

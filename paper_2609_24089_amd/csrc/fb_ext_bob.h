@@ -1,0 +1,102 @@
+// The two BoB passes between sequences of two lengths: their forms and launches, for the
+// translation units that build them.
+#pragma once
+#include "fb_ext.h"
+
+namespace fb {
+
+template <typename T, int D> struct ExtPass1 {
+  static constexpr ExtShape shape(int form) {
+    constexpr Shape w = Cfg<T, D>::kP1;
+    return form == 0   ? ExtShape{w.mr, w.nw, w.occ, w.st, 1}
+           : form == 1 ? ext_sets<T, D>(4, 4, 0, 8, w.occ)
+                       : ext_sets<T, D>(1, 4, 0, 8, w.occ);
+  }
+  template <int F, bool kBias> static __host__ constexpr auto kernel() {
+    constexpr ExtShape s = shape(F);
+    return &ext_pass1_kernel<T, D, s.mr, s.nw, s.occ, s.ks, Cfg<T, D>::kP1.pf, kBias>;
+  }
+};
+template <typename T, int D> struct ExtPass2 {
+  static constexpr int kExtra = 4 * 4 * kBS * (int)sizeof(float) + 1024;
+  static constexpr ExtShape shape(int form) {
+    constexpr Shape w = Cfg<T, D>::kP2;
+    return form == 0   ? ExtShape{w.mr, w.nw, w.occ, w.st, 1}
+           : form == 1 ? (sizeof(T) == 2 && D == 32 ? kNotBuilt : ext_sets<T, D>(4, 3, kExtra, 8, w.occ))
+                       : ext_sets<T, D>(1, 3, kExtra, 8, w.occ);
+  }
+  template <int F, bool kBias> static __host__ constexpr auto kernel() {
+    constexpr ExtShape s = shape(F);
+    return &ext_pass2_kernel<T, D, s.mr, s.nw, s.occ, s.ks, Cfg<T, D>::kP2.pf != 0, kBias>;
+  }
+};
+
+inline int64_t pass2_dynamic(const ExtProblem& p, const ExtShape& s) {
+  return has_bias(p) ? 2 * ext_steps_bytes(p) + (int64_t)s.nw * s.ks * StepSums::kBufFloats * 4 : 0;
+}
+
+template <typename T, int D>
+int32_t ext_launch_pass1(const ExtProblem& p, const void* Q, const void* K, const void* V, const void* O,
+                         const void* dO, const void* UQ, const void* UK, const void* UV, const void* UT,
+                         const float* L, const float* Dv, const void* dQ, void* Qt, void* dOt, float* alpha, float* E,
+                         hipStream_t s) {
+  using R = ExtPass1<T, D>;
+  const int64_t steps = 2 * ext_steps_bytes(p);
+  const FormQuery q{device_cus(), p.B * p.H, p.Nq, std::max<int64_t>((p.Nk + kBS - 1) / kBS, 1), p.causal != 0,
+                    block_us<T>(10, D), kP1Step<T>, merge_us(3, D), kRowMargin};
+  ExtPlan c;
+  c.form = pick_form(q, {ext_form_of<R, 0>(p, steps, 1.0), ext_form_of<R, 1>(p, steps, kP1Step<T>.narrow),
+                         ext_form_of<R, 2>(p, steps, kP1Step<T>.narrow)});
+  c.blocks = R::shape(c.form).blocks();
+  const ExtArgs a = ext_args(p, c, p.B * p.H, p.Nq, UT);
+  return ext_dispatch<R>(c.form, p, dim3(a.total), steps, s, (const T*)Q, (const T*)K, (const T*)V, (const T*)O,
+                         (const T*)dO, (const T*)UQ, (const T*)UK, (const T*)UV, L, Dv, (const T*)dQ, (T*)Qt, (T*)dOt,
+                         alpha, E, a);
+}
+
+template <typename T, int D> ExtPlan ext_pass2_plan(const ExtProblem& p) {
+  using C = ExtPass2<T, D>;
+  const int grp = ext_group(p);
+  ExtPlan c;
+  const bool split = has_bias(p) && grp > 1;
+  const int64_t tiles = std::max<int64_t>((p.Nq + kBS - 1) / kBS, 1) * (split ? 1 : grp);
+  const FormQuery q{device_cus(), p.B * (split ? p.H : p.Hkv), std::max<int64_t>(p.Nk, 1), tiles, p.causal != 0,
+                    block_us<T>(8, D), kP2Step<T>, merge_us(2, D), 1.0};
+  c.form = pick_form(q, {ext_form_of<C, 0>(p, pass2_dynamic(p, C::shape(0)), 1.0),
+                         ext_form_of<C, 1>(p, pass2_dynamic(p, C::shape(1)), kP2Step<T>.narrow),
+                         ext_form_of<C, 2>(p, pass2_dynamic(p, C::shape(2)), kP2Step<T>.narrow)});
+  const ExtShape s = C::shape(c.form);
+  c.blocks = s.blocks();
+  c.sets = s.ks * s.nw;
+  c.parts = split ? grp : 1;
+  return c;
+}
+
+template <typename T, int D>
+int32_t ext_launch_pass2(const ExtProblem& p, const void* Q, const void* K, const void* V, const void* dO,
+                         const void* UQ, const void* UK, const void* UV, const void* UT, const float* L,
+                         const float* Dv, const float* alpha, const float* E, void* Kt, void* Vt, float* parts,
+                         float* sums, hipStream_t s) {
+  using C = ExtPass2<T, D>;
+  const ExtPlan c = ext_pass2_plan<T, D>(p);
+  const ExtArgs a = ext_args(p, c, p.B * p.Hkv, p.Nk, UT);
+  const int32_t rc = ext_dispatch<C>(c.form, p, dim3(a.total, c.parts), pass2_dynamic(p, C::shape(c.form)), s,
+                                     (const T*)Q, (const T*)K, (const T*)V, (const T*)dO, (const T*)UQ, (const T*)UK,
+                                     (const T*)UV, L, Dv, alpha, E, (T*)Kt, (T*)Vt, a, parts, sums);
+  if (rc != BOB_OK || c.parts == 1) return rc;
+  return ext_add_parts(p, parts, c.parts, Kt, Vt, s);
+}
+
+#define FB_EXT_PASS1(T, D, ...)                                                                                      \
+  template int32_t ext_launch_pass1<T, D>(const ExtProblem&, const void*, const void*, const void*, const void*,    \
+                                          const void*, const void*, const void*, const void*, const void*,          \
+                                          const float*, const float*, const void*, void*, void*, float*, float*,    \
+                                          hipStream_t);
+#define FB_EXT_PASS2(T, D, ...)                                                                                     \
+  template ExtPlan ext_pass2_plan<T, D>(const ExtProblem&);                                                         \
+  template int32_t ext_launch_pass2<T, D>(const ExtProblem&, const void*, const void*, const void*, const void*,    \
+                                          const void*, const void*, const void*, const void*, const float*,         \
+                                          const float*, const float*, const float*, void*, void*, float*, float*,   \
+                                          hipStream_t);
+
+}  // namespace fb

@@ -1,0 +1,100 @@
+// The first backward between sequences of two lengths: its forms and launches.
+#include "fb_ext.h"
+
+namespace fb {
+
+template <typename T, int D> struct ExtRowsBwd {
+  static constexpr ExtShape shape(int form) {
+    constexpr Shape w = Cfg<T, D>::kRows;
+    return form == 0   ? ExtShape{w.mr, w.nw, w.occ, w.st, 1}
+           : form == 1 ? ext_sets<T, D>(4, 2, 0, 16, w.occ)
+                       : ext_sets<T, D>(1, 2, 0, 16, w.occ);
+  }
+  template <int F, bool kBias> static __host__ constexpr auto kernel() {
+    constexpr ExtShape s = shape(F);
+    return &ext_bwd_rows_kernel<T, D, s.mr, s.nw, s.occ, s.st, s.ks, kBias>;
+  }
+};
+
+template <typename T, int D> struct ExtColsBwd {
+  static constexpr int kExtra = 4 * 2 * kBS * (int)sizeof(float) + 1024;  // raw and transformed L, D; bias buffers
+  static constexpr ExtShape shape(int form) {
+    constexpr Shape w = Cfg<T, D>::kCols;
+    constexpr int waves = D * (int)sizeof(T) <= 128 ? 16 : 8;
+    return form == 0   ? ExtShape{w.mr, w.nw, w.occ, w.st, 1}
+           : form == 1 ? ext_sets<T, D>(4, 2, kExtra, waves, w.occ)
+                       : ext_sets<T, D>(1, 2, kExtra, waves, w.occ);
+  }
+  template <int F, bool kBias> static __host__ constexpr auto kernel() {
+    constexpr ExtShape s = shape(F);
+    return &ext_bwd_cols_kernel<T, D, s.mr, s.nw, s.occ, s.ks, F == 0 && Cfg<T, D>::kCols.kl != 0, kBias>;
+  }
+};
+
+// Beside the bias, a buffer of step sums for every wave.
+static int64_t cols_dynamic(const ExtProblem& p, const ExtShape& s) {
+  return has_bias(p) ? ext_steps_bytes(p) + (int64_t)s.nw * s.ks * StepSums::kBufFloats * 4 : 0;
+}
+
+template <typename T, int D> ExtPlan ext_rows_plan(const ExtProblem& p) {
+  const int64_t steps = ext_steps_bytes(p);
+  const FormQuery q{device_cus(), p.B * p.H, p.Nq, std::max<int64_t>((p.Nk + kBS - 1) / kBS, 1), p.causal != 0,
+                    block_us<T>(3, D), kRowsStep<T>, merge_us(1, D), kRowMargin};
+  ExtPlan c;
+  c.form = pick_form(q, {ext_form_of<ExtRowsBwd<T, D>, 0>(p, steps, 1.0),
+                         ext_form_of<ExtRowsBwd<T, D>, 1>(p, steps, kRowsStep<T>.narrow),
+                         ext_form_of<ExtRowsBwd<T, D>, 2>(p, steps, kRowsStep<T>.narrow)});
+  const ExtShape s = ExtRowsBwd<T, D>::shape(c.form);
+  c.blocks = s.blocks();
+  c.sets = s.ks;
+  return c;
+}
+
+template <typename T, int D> ExtPlan ext_cols_plan(const ExtProblem& p) {
+  using C = ExtColsBwd<T, D>;
+  const int grp = ext_group(p);
+  ExtPlan c;
+  // with a bias each query head of a group has its own table: one part a head
+  const bool split = has_bias(p) && grp > 1;
+  const int64_t tiles = std::max<int64_t>((p.Nq + kBS - 1) / kBS, 1) * (split ? 1 : grp);
+  const FormQuery q{device_cus(), p.B * (split ? p.H : p.Hkv), std::max<int64_t>(p.Nk, 1), tiles, p.causal != 0,
+                    block_us<T>(4, D), kColsStep<T>, merge_us(2, D), 1.0};
+  c.form = pick_form(q, {ext_form_of<C, 0>(p, cols_dynamic(p, C::shape(0)), 1.0),
+                         ext_form_of<C, 1>(p, cols_dynamic(p, C::shape(1)), kColsStep<T>.narrow),
+                         ext_form_of<C, 2>(p, cols_dynamic(p, C::shape(2)), kColsStep<T>.narrow)});
+  const ExtShape s = C::shape(c.form);
+  c.blocks = s.blocks();
+  c.sets = s.ks * s.nw;  // waves that store step sums
+  c.parts = split ? grp : 1;
+  return c;
+}
+
+template <typename T, int D>
+int32_t ext_launch_bwd(const ExtProblem& p, const void* Q, const void* K, const void* V, const void* O, const void* dO,
+                       const float* L, void* dQ, void* dK, void* dV, float* Dv, float* parts, float* sums,
+                       hipStream_t s) {
+  int32_t rc = BOB_OK;
+  if (p.Nq > 0) {
+    const ExtPlan r = ext_rows_plan<T, D>(p);
+    const ExtArgs a = ext_args(p, r, p.B * p.H, p.Nq, nullptr);
+    rc = ext_dispatch<ExtRowsBwd<T, D>>(r.form, p, dim3(a.total), ext_steps_bytes(p), s, (const T*)Q, (const T*)K,
+                                        (const T*)V, (const T*)O, (const T*)dO, L, (T*)dQ, Dv, a);
+  }
+  if (rc != BOB_OK || p.Nk == 0) return rc;
+  const ExtPlan c = ext_cols_plan<T, D>(p);
+  const ExtArgs a = ext_args(p, c, p.B * p.Hkv, p.Nk, nullptr);
+  rc = ext_dispatch<ExtColsBwd<T, D>>(c.form, p, dim3(a.total, c.parts), cols_dynamic(p, ExtColsBwd<T, D>::shape(c.form)),
+                                      s, (const T*)Q, (const T*)K, (const T*)V, (const T*)dO, L, (const float*)Dv,
+                                      (T*)dK, (T*)dV, a, parts, sums);
+  if (rc != BOB_OK || c.parts == 1) return rc;
+  return ext_add_parts(p, parts, c.parts, dK, dV, s);
+}
+
+#define FB_INST(T, D, ...)                                                                                        \
+  template ExtPlan ext_cols_plan<T, D>(const ExtProblem&);                                                        \
+  template int32_t ext_launch_bwd<T, D>(const ExtProblem&, const void*, const void*, const void*, const void*,    \
+                                        const void*, const float*, void*, void*, void*, float*, float*, float*,   \
+                                        hipStream_t);
+FB_EXT_EACH(FB_INST)
+
+}  // namespace fb

@@ -1,0 +1,66 @@
+// The forward between sequences of two lengths: its forms and launches.
+#include "fb_ext.h"
+
+namespace fb {
+
+template <typename T, int D> struct ExtFwd {
+  static constexpr ExtShape shape(int form) {
+    constexpr Shape w = Cfg<T, D>::kFwd;
+    return form == 0   ? ExtShape{w.mr, w.nw, w.occ, w.st, 1}
+           : form == 1 ? ext_sets<T, D>(4, 2, 0, 16, w.occ)
+                       : ext_sets<T, D>(1, 2, 0, 16, 1);
+  }
+  template <int F, bool kBias> static __host__ constexpr auto kernel() {
+    constexpr ExtShape s = shape(F);
+    return &ext_fwd_kernel<T, D, s.mr, s.nw, s.occ, s.st, s.ks, kBias>;
+  }
+};
+
+template <typename T, int D> ExtPlan ext_fwd_plan(const ExtProblem& p) {
+  ExtPlan c;
+  const int64_t steps = ext_steps_bytes(p);
+  const int grp = ext_group(p);
+  constexpr ExtShape narrow = ExtFwd<T, D>::shape(2);
+  const Form f2 = ext_form_of<ExtFwd<T, D>, 2>(p, steps, kFwdStep<T>.narrow);
+  if (grp > 1 && p.Nq <= 16 && f2.resident > 0)
+    c.fold = ext_form_of<ExtFwd<T, D>, 2>(p, steps * std::min(grp, 16), 1.0).resident > 0;
+  const int64_t rows = c.fold ? grp * p.Nq : p.Nq, heads = p.B * (c.fold ? p.Hkv : p.H);
+  const int64_t tiles = std::max<int64_t>((p.Nk + kBS - 1) / kBS, 1);
+  if (f2.resident > 0 && (c.fold || rows <= 16)) {
+    c.form = 2;
+  } else {
+    const FormQuery q{device_cus(), heads, rows, tiles, p.causal != 0, block_us<T>(2, D), kFwdStep<T>, merge_us(1, D),
+                      kRowMargin};
+    c.form = pick_form(q, {ext_form_of<ExtFwd<T, D>, 0>(p, steps, 1.0),
+                           ext_form_of<ExtFwd<T, D>, 1>(p, steps, kFwdStep<T>.narrow), f2});
+  }
+  const ExtShape s = ExtFwd<T, D>::shape(c.form);
+  c.blocks = s.blocks();
+  c.sets = s.ks;
+  (void)narrow;
+  return c;
+}
+
+template <typename T, int D>
+int32_t ext_launch_fwd(const ExtProblem& p, const void* Q, const void* K, const void* V, void* O, float* L, float* ws,
+                       hipStream_t s) {
+  const ExtPlan c = ext_fwd_plan<T, D>(p);
+  const int64_t rows = c.fold ? ext_group(p) * p.Nq : p.Nq, heads = p.B * (c.fold ? p.Hkv : p.H);
+  const ExtArgs a = ext_args(p, c, heads, rows, nullptr);
+  const int64_t dynamic = ext_steps_bytes(p) * (c.fold ? std::min(ext_group(p), 16) : 1);
+  int32_t rc = ext_dispatch<ExtFwd<T, D>>(c.form, p, dim3(a.total, c.parts), dynamic, s, (const T*)Q, (const T*)K,
+                                          (const T*)V, (T*)O, L, a, ws);
+  if (rc != BOB_OK || c.parts == 1) return rc;
+  const int64_t all = heads * rows;
+  hipLaunchKernelGGL((ext_fwd_join_kernel<T, D>), dim3((unsigned)((all * (D / 4) + 255) / 256)), dim3(256), 0, s, ws,
+                     c.parts, all, a, (T*)O, L);
+  return finish_launch();
+}
+
+#define FB_INST(T, D, ...)                                  \
+  template ExtPlan ext_fwd_plan<T, D>(const ExtProblem&);   \
+  template int32_t ext_launch_fwd<T, D>(const ExtProblem&, const void*, const void*, const void*, void*, float*, float*, \
+                                        hipStream_t);
+FB_EXT_EACH(FB_INST)
+
+}  // namespace fb

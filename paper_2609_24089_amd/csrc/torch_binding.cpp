@@ -12,6 +12,7 @@
 #include <torch/csrc/jit/frontend/tracer.h>
 #include <torch/extension.h>
 
+#include <optional>
 #include <string>
 #include <vector>
 
@@ -31,6 +32,13 @@ struct Api {
   decltype(&::bob_bwd_workspace_bytes) bwd_bytes = nullptr;
   decltype(&::bob_pass2_workspace_bytes) pass2_bytes = nullptr;
   decltype(&::bob_status_string) status = nullptr;
+  decltype(&::attn_ext_fwd_lse) ext_fwd = nullptr;
+  decltype(&::attn_ext_bwd) ext_bwd = nullptr;
+  decltype(&::attn_ext_pass1_rows) ext_pass1 = nullptr;
+  decltype(&::attn_ext_pass2_cols) ext_pass2 = nullptr;
+  decltype(&::attn_ext_fwd_workspace_bytes) ext_fwd_bytes = nullptr;
+  decltype(&::attn_ext_bwd_workspace_bytes) ext_bwd_bytes = nullptr;
+  decltype(&::attn_ext_pass2_workspace_bytes) ext_pass2_bytes = nullptr;
 } api;
 
 // Take the entry points from the library at `path`.
@@ -49,6 +57,13 @@ void bind(const std::string& path) {
   take(a.bwd_bytes, "bob_bwd_workspace_bytes");
   take(a.pass2_bytes, "bob_pass2_workspace_bytes");
   take(a.status, "bob_status_string");
+  take(a.ext_fwd, "attn_ext_fwd_lse");
+  take(a.ext_bwd, "attn_ext_bwd");
+  take(a.ext_pass1, "attn_ext_pass1_rows");
+  take(a.ext_pass2, "attn_ext_pass2_cols");
+  take(a.ext_fwd_bytes, "attn_ext_fwd_workspace_bytes");
+  take(a.ext_bwd_bytes, "attn_ext_bwd_workspace_bytes");
+  take(a.ext_pass2_bytes, "attn_ext_pass2_workspace_bytes");
   api = a;
 }
 
@@ -354,6 +369,233 @@ py::object py_attention(py::handle q, py::handle k, py::handle v, double scale, 
   return py::cast(O);
 }
 
+// ---------------------------------------------------------------------------
+// Attention between sequences of two lengths, with a position bias (ext.py says what
+// the arguments mean).  Undefined tensors stand for arguments that are not given.
+// ---------------------------------------------------------------------------
+struct Extras {
+  Tensor table, buckets, kv_lens, q_lens, q_starts;
+};
+struct ExtDims {
+  int32_t code = 0;
+  int64_t B = 0, H = 0, Hkv = 0, Nq = 0, Nk = 0, d = 0;
+  attn_ext x{};
+};
+
+constexpr int64_t kMaxDistance = 1024, kMaxBuckets = 1 << 16;  // as the library's
+
+// The checks of ext.py; false: not for this path.
+bool ext_check(Refs qside, Refs kside, Refs rows, const Extras& e, ExtDims& m) {
+  const Tensor& q = **qside.begin();
+  const Tensor& k = **kside.begin();
+  if (!plain(q) || !plain(k) || q.dim() != 4 || k.dim() != 4) return false;
+  if (q.scalar_type() == at::kBFloat16)
+    m.code = BOB_BF16;
+  else if (q.scalar_type() == at::kFloat)
+    m.code = BOB_F32;
+  else
+    return false;
+  m.B = q.size(0), m.H = q.size(1), m.Nq = q.size(2), m.d = q.size(3), m.Hkv = k.size(1), m.Nk = k.size(2);
+  if (k.size(0) != m.B || k.size(3) != m.d) return false;
+  if (m.Hkv == 0 ? m.H != 0 : m.H % m.Hkv != 0) return false;
+  auto same = [&](const Tensor& t, const Tensor& like) {
+    return plain(t) && t.sizes() == like.sizes() && t.scalar_type() == q.scalar_type() && t.device() == q.device();
+  };
+  for (const Tensor* t : qside)
+    if (!same(*t, q)) return false;
+  for (const Tensor* t : kside)
+    if (!same(*t, k)) return false;
+  for (const Tensor* t : rows)
+    if (!plain(*t) || t->scalar_type() != at::kFloat || t->sizes() != q.sizes().slice(0, 3) ||
+        t->device() != q.device())
+      return false;
+  auto ints = [&](const Tensor& t) { return plain(t) && t.scalar_type() == at::kInt && t.dim() == 1 && t.device() == q.device(); };
+  auto lens = [&](const Tensor& t) { return !t.defined() || (ints(t) && t.size(0) == m.B); };
+  if (!lens(e.kv_lens) || !lens(e.q_lens) || !lens(e.q_starts) || e.table.defined() != e.buckets.defined()) return false;
+  auto at = [](const Tensor& t) { return t.defined() ? (const int32_t*)t.const_data_ptr() : nullptr; };
+  m.x.q_lens = at(e.q_lens), m.x.kv_lens = at(e.kv_lens), m.x.q_starts = at(e.q_starts);
+  if (e.table.defined()) {
+    const Tensor& t = e.table;
+    if (!plain(t) || t.dim() != 2 || t.size(0) < 1 || t.size(0) > kMaxBuckets || t.size(1) != m.H ||
+        t.device() != q.device() || (t.scalar_type() != at::kFloat && t.scalar_type() != at::kBFloat16))
+      return false;
+    if (!ints(e.buckets) || e.buckets.size(0) % 2 != 1 || e.buckets.size(0) < 3 ||
+        e.buckets.size(0) > 2 * kMaxDistance + 1)
+      return false;
+    m.x.table = t.const_data_ptr();
+    m.x.buckets = at(e.buckets);
+    m.x.table_dtype = t.scalar_type() == at::kFloat ? BOB_F32 : BOB_BF16;
+    m.x.num_buckets = (int32_t)t.size(0);
+    m.x.max_distance = (int32_t)((e.buckets.size(0) - 1) / 2);
+  }
+  return true;
+}
+ExtDims ext_dims_or_throw(Refs qside, Refs kside, Refs rows, const Extras& e) {
+  ExtDims m;
+  TORCH_CHECK_VALUE(ext_check(qside, kside, rows, e, m),
+                    "attention gradients must be contiguous and share the inputs' shape, dtype and device");
+  return m;
+}
+// A cotangent on the table's gradient; undefined: none.
+const void* ext_cotangent(const Tensor& g, const Tensor& table) {
+  if (!g.defined()) return nullptr;
+  TORCH_CHECK_VALUE(plain(g) && g.sizes() == table.sizes() && g.scalar_type() == table.scalar_type() &&
+                        g.device() == table.device(),
+                    "the cotangent on the table's gradient must share the table's shape, dtype and device");
+  return p(g);
+}
+
+Rows2 run_ext_fwd(const ExtDims& m, const Tensor& Q, const Tensor& K, const Tensor& V, double scale, bool causal) {
+  Rows2 r{at::empty_like(Q), rows_like(Q)};
+  const int64_t bytes = api.ext_fwd_bytes(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, causal, &m.x);
+  const Tensor ws = workspace(bytes, Q);
+  ok(api.ext_fwd(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, (float)scale, causal, &m.x, p(Q), p(K), p(V), pm(r.O),
+                 fm(r.L), bytes > 0 ? pm(ws) : nullptr, bytes, stream_of(Q)));
+  return r;
+}
+
+struct ExtBwd {
+  Tensor dQ, dK, dV, D, dT;
+};
+ExtBwd run_ext_bwd(const ExtDims& m, const Tensor& Q, const Tensor& K, const Tensor& V, const Tensor& O,
+                   const Tensor& dO, const Tensor& L, const Extras& e, double scale, bool causal, bool want_table) {
+  ExtBwd r{at::empty_like(Q), at::empty_like(K), at::empty_like(K), rows_like(Q), Tensor()};
+  if (want_table && e.table.defined()) r.dT = at::empty_like(e.table);
+  const int64_t bytes = api.ext_bwd_bytes(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, causal, &m.x);
+  const Tensor ws = workspace(bytes, Q);
+  ok(api.ext_bwd(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, (float)scale, causal, &m.x, p(Q), p(K), p(V), p(O), p(dO),
+                 f(L), pm(r.dQ), pm(r.dK), pm(r.dV), fm(r.D), r.dT.defined() ? pm(r.dT) : nullptr,
+                 bytes > 0 ? pm(ws) : nullptr, bytes, stream_of(Q)));
+  return r;
+}
+
+Tensor given(py::handle h) { return h.is_none() ? Tensor() : THPVariable_Unpack(h.ptr()); }
+bool plain_or_none(std::initializer_list<py::handle> hs) {
+  for (py::handle h : hs)
+    if (!h.is_none() && !THPVariable_CheckExact(h.ptr())) return false;
+  return true;
+}
+
+py::object py_ext_fwd(py::handle q, py::handle k, py::handle v, double scale, bool causal, py::handle table,
+                      py::handle buckets, py::handle kv_lens, py::handle q_lens, py::handle q_starts) {
+  std::vector<Tensor> t;
+  ExtDims m;
+  if (!plain_or_none({table, buckets, kv_lens, q_lens, q_starts}) || !tensors({q, k, v}, t)) return py::none();
+  const Extras e{given(table), given(buckets), given(kv_lens), given(q_lens), given(q_starts)};
+  if (!ext_check({&t[0]}, {&t[1], &t[2]}, {}, e, m)) return py::none();
+  Rows2 r;
+  {
+    py::gil_scoped_release free;
+    c10::OptionalDeviceGuard guard(t[0].device());
+    r = run_ext_fwd(m, t[0], t[1], t[2], scale, causal);
+  }
+  return py::make_tuple(r.O, r.L);
+}
+
+// The functions' arguments that may be missing: apply() takes no undefined tensors.  The
+// table stays the fourth argument, so it is the fourth edge where it is given.
+using Maybe = std::optional<Tensor>;
+Maybe maybe(const Tensor& t) { return t.defined() ? Maybe(t) : Maybe(); }
+Tensor get(const Maybe& t) { return t.has_value() ? *t : Tensor(); }
+
+struct ExtAttentionBackward : torch::autograd::Function<ExtAttentionBackward> {
+  static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& v,
+                               const Maybe& table_, const Tensor& O, const Tensor& L, const Tensor& dO,
+                               const Maybe& buckets_, const Maybe& kv_lens_, const Maybe& q_lens_,
+                               const Maybe& q_starts_, double scale, bool causal, bool want_table) {
+    const Extras e{get(table_), get(buckets_), get(kv_lens_), get(q_lens_), get(q_starts_)};
+    const auto& [table, buckets, kv_lens, q_lens, q_starts] = e;
+    const ExtDims m = ext_dims_or_throw({&q, &O, &dO}, {&k, &v}, {&L}, e);
+    c10::OptionalDeviceGuard guard(q.device());
+    ExtBwd r = run_ext_bwd(m, q, k, v, O, dO, L, e, scale, causal, want_table);
+    ctx->save_for_backward({q, k, v, table, O, L, dO, r.D, r.dQ, buckets, kv_lens, q_lens, q_starts});
+    ctx->saved_data["scale"] = scale;
+    ctx->saved_data["causal"] = causal;
+    variable_list out{r.dQ, r.dK, r.dV};
+    if (r.dT.defined()) out.push_back(r.dT);  // no undefined outputs
+    return out;
+  }
+  static variable_list backward(AutogradContext* ctx, variable_list g) {
+    const variable_list s = ctx->get_saved_variables();
+    const double scale = ctx->saved_data["scale"].toDouble();
+    const bool causal = ctx->saved_data["causal"].toBool();
+    const Tensor &q = s[0], &k = s[1], &v = s[2], &table = s[3], &O = s[4], &L = s[5], &dO = s[6], &D = s[7], &dQ = s[8];
+    const Extras e{table, s[9], s[10], s[11], s[12]};
+    auto cotangent = [](const Tensor& t, const Tensor& like) {
+      return t.defined() ? t.contiguous() : at::zeros_like(like);
+    };
+    const Tensor uq = cotangent(g[0], q), uk = cotangent(g[1], k), uv = cotangent(g[2], v);
+    const Tensor ut = g.size() > 3 && g[3].defined() ? g[3].contiguous() : Tensor();
+    const ExtDims m = ext_dims_or_throw({&q, &O, &dO, &uq, &dQ}, {&k, &v, &uk, &uv}, {&L, &D}, e);
+    c10::OptionalDeviceGuard guard(q.device());
+    at::AutoGradMode no_graph(false);
+    const void* const gT = ext_cotangent(ut, table);
+    const Tensor Qt = at::empty_like(q), dOt = at::empty_like(q), alpha = rows_like(q), E = rows_like(q);
+    ok(api.ext_pass1(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, (float)scale, causal, &m.x, p(q), p(k), p(v), p(O),
+                     p(dO), p(uq), p(uk), p(uv), gT, f(L), f(D), p(dQ), pm(Qt), pm(dOt), fm(alpha), fm(E),
+                     stream_of(q)));
+    const Tensor Kt = at::empty_like(k), Vt = at::empty_like(k);
+    const Tensor Tt = table.defined() && ctx->needs_input_grad(3) ? at::empty_like(table) : Tensor();
+    const int64_t bytes = api.ext_pass2_bytes(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, causal, &m.x);
+    const Tensor ws = workspace(bytes, q);
+    ok(api.ext_pass2(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, (float)scale, causal, &m.x, p(q), p(k), p(v), p(dO),
+                     p(uq), p(uk), p(uv), gT, f(L), f(D), f(alpha), f(E), pm(Kt), pm(Vt),
+                     Tt.defined() ? pm(Tt) : nullptr, bytes > 0 ? pm(ws) : nullptr, bytes, stream_of(q)));
+    return {Qt, Kt, Vt, Tt, Tensor(), Tensor(), dOt, Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+  }
+};
+
+struct ExtAttention : torch::autograd::Function<ExtAttention> {
+  static Tensor forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& v, const Maybe& table_,
+                        const Maybe& buckets_, const Maybe& kv_lens_, const Maybe& q_lens_, const Maybe& q_starts_,
+                        double scale, bool causal) {
+    const Extras e{get(table_), get(buckets_), get(kv_lens_), get(q_lens_), get(q_starts_)};
+    const auto& [table, buckets, kv_lens, q_lens, q_starts] = e;
+    const ExtDims m = ext_dims_or_throw({&q}, {&k, &v}, {}, e);
+    c10::OptionalDeviceGuard guard(q.device());
+    Rows2 r = run_ext_fwd(m, q, k, v, scale, causal);
+    ctx->save_for_backward({q, k, v, table, r.O, r.L, buckets, kv_lens, q_lens, q_starts});
+    ctx->saved_data["scale"] = scale;
+    ctx->saved_data["causal"] = causal;
+    return r.O;
+  }
+  static variable_list backward(AutogradContext* ctx, variable_list g) {
+    const variable_list s = ctx->get_saved_variables();
+    const variable_list d = ExtAttentionBackward::apply(
+        s[0], s[1], s[2], maybe(s[3]), s[4], s[5], g[0].contiguous(), maybe(s[6]), maybe(s[7]), maybe(s[8]), maybe(s[9]),
+        ctx->saved_data["scale"].toDouble(), ctx->saved_data["causal"].toBool(),
+        s[3].defined() && ctx->needs_input_grad(3));
+    return {d[0], d[1], d[2], d.size() > 3 ? d[3] : Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+  }
+};
+
+py::object py_ext_attention(py::handle q, py::handle k, py::handle v, double scale, bool causal, py::handle table,
+                            py::handle buckets, py::handle kv_lens, py::handle q_lens, py::handle q_starts) {
+  std::vector<Tensor> t;
+  ExtDims m;
+  if (!plain_or_none({table, buckets, kv_lens, q_lens, q_starts}) || !tensors({q, k, v}, t)) return py::none();
+  const Extras e{given(table), given(buckets), given(kv_lens), given(q_lens), given(q_starts)};
+  if (!ext_check({&t[0]}, {&t[1], &t[2]}, {}, e, m)) return py::none();
+  if (e.table.defined()) t.push_back(e.table);
+  bool grad = false;
+  for (const Tensor& x : t) {
+    if (x._fw_grad(0).defined()) return py::none();
+    grad |= x.requires_grad();
+  }
+  Tensor O;
+  {
+    py::gil_scoped_release free;
+    if (grad && at::GradMode::is_enabled()) {
+      O = ExtAttention::apply(t[0], t[1], t[2], maybe(e.table), maybe(e.buckets), maybe(e.kv_lens), maybe(e.q_lens),
+                              maybe(e.q_starts), scale, causal);
+    } else {  // a decoding step: nothing to record
+      c10::OptionalDeviceGuard guard(t[0].device());
+      O = run_ext_fwd(m, t[0], t[1], t[2], scale, causal).O;
+    }
+  }
+  return py::cast(O);
+}
+
 }  // namespace
 
 PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
@@ -364,4 +606,6 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
   m.def("pass2", &py_pass2);
   m.def("bob", &py_bob);
   m.def("attention", &py_attention);
+  m.def("ext_fwd", &py_ext_fwd);
+  m.def("ext_attention", &py_ext_attention);
 }
