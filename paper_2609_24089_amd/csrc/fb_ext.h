@@ -130,25 +130,31 @@ template <typename Kern, int F> Form ext_form_of(const ExtProblem& p, int64_t dy
   return {};
 }
 
-// The current device's dense grids run without the balanced causal order.
+// Launches form F of Kern, whose first argument is a.
 template <typename Kern, int F, typename... Args>
-int32_t ext_go(const ExtProblem& p, dim3 grid, int64_t dynamic, hipStream_t stream, Args... args) {
+int32_t ext_go(const ExtProblem& p, dim3 grid, int64_t dynamic, hipStream_t stream, ExtArgs a, Args... args) {
   constexpr ExtShape s = Kern::shape(F);
   if constexpr (s.built()) {
+    if (p.causal != 0 && grid.y == 1) {
+      const int fit = has_bias(p) ? resident_blocks<Kern::template kernel<F, true>()>(s.threads())
+                                  : resident_blocks<Kern::template kernel<F, false>()>(s.threads());
+      a.resident = balanced_order(a.total, fit, device_cus());
+    }
     (void)hipGetLastError();
     if (has_bias(p))
-      hipLaunchKernelGGL((Kern::template kernel<F, true>()), grid, dim3(s.threads()), (unsigned)dynamic, stream, args...);
+      hipLaunchKernelGGL((Kern::template kernel<F, true>()), grid, dim3(s.threads()), (unsigned)dynamic, stream, a, args...);
     else
-      hipLaunchKernelGGL((Kern::template kernel<F, false>()), grid, dim3(s.threads()), 0, stream, args...);
+      hipLaunchKernelGGL((Kern::template kernel<F, false>()), grid, dim3(s.threads()), 0, stream, a, args...);
     return finish_launch();
   }
   return BOB_EUNSUPPORTED;
 }
 template <typename Kern, typename... Args>
-int32_t ext_dispatch(int form, const ExtProblem& p, dim3 grid, int64_t dynamic, hipStream_t stream, Args... args) {
-  if (form == 2) return ext_go<Kern, 2>(p, grid, dynamic, stream, args...);
-  if (form == 1) return ext_go<Kern, 1>(p, grid, dynamic, stream, args...);
-  return ext_go<Kern, 0>(p, grid, dynamic, stream, args...);
+int32_t ext_dispatch(int form, const ExtProblem& p, dim3 grid, int64_t dynamic, hipStream_t stream, const ExtArgs& a,
+                     Args... args) {
+  if (form == 2) return ext_go<Kern, 2>(p, grid, dynamic, stream, a, args...);
+  if (form == 1) return ext_go<Kern, 1>(p, grid, dynamic, stream, a, args...);
+  return ext_go<Kern, 0>(p, grid, dynamic, stream, a, args...);
 }
 
 }  // namespace fb

@@ -5,38 +5,50 @@
 
 namespace fb {
 
+// The sum of rows r0, r0 + by, ... below `rows` of column x, eight loads in flight: the
+// rows are few and far apart, so one load after another was all latency.
+__device__ __forceinline__ float sum_rows(const float* __restrict__ m, int64_t r0, int64_t rows, int64_t by, int width,
+                                          int x) {
+  float v[8];
+#pragma unroll
+  for (int u = 0; u < 8; ++u) v[u] = 0.f;
+  int64_t r = r0;
+  for (; r + 7 * by < rows; r += 8 * by)
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] += m[(r + u * by) * width + x];
+#pragma unroll
+  for (int u = 0; u < 7; ++u)
+    if (r + u * by < rows) v[u] += m[(r + u * by) * width + x];
+  return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+}
+
 // Adds the waves' rows of step sums (StepSums) of head blockIdx.y: workgroup s of S takes
 // rows s, s + S, ... of the head's `rows` and writes one row of `mid` ([H][S][width]).
 __global__ __launch_bounds__(256) void ext_step_rows_kernel(const float* __restrict__ sums, int64_t rows, int width,
                                                             float* __restrict__ mid) {
   const float* const head = sums + (int64_t)blockIdx.y * rows * width;
   float* const out = mid + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * width;
-  for (int x = threadIdx.x; x < width; x += 256) {
-    float v = 0.f;
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) v += head[r * width + x];
-    out[x] = v;
-  }
+  for (int x = threadIdx.x; x < width; x += 256) out[x] = sum_rows(head, blockIdx.x, rows, gridDim.x, width, x);
 }
 
 // Gathers head blockIdx.x's sums by step into its buckets.  Eight lanes share a bucket,
 // each takes every eighth step; the order of the sums is fixed.
 constexpr int kMaxWidth = 2 * kMaxDistance + 3;
-__global__ __launch_bounds__(256) void ext_buckets_kernel(const float* __restrict__ mid, int S, ExtArgs a,
-                                                          void* __restrict__ out) {
+constexpr int kGatherThreads = 512;
+__global__ __launch_bounds__(kGatherThreads) void ext_buckets_kernel(const float* __restrict__ mid, int S, ExtArgs a,
+                                                                     void* __restrict__ out) {
   __shared__ float sum[kMaxWidth];
   __shared__ int bucket[kMaxWidth];
   const int width = 2 * a.R + 3;
-  for (int x = threadIdx.x; x < width; x += 256) {
-    float v = 0.f;
-    for (int s = 0; s < S; ++s) v += mid[((int64_t)blockIdx.x * S + s) * width + x];
-    sum[x] = v;
+  for (int x = threadIdx.x; x < width; x += kGatherThreads) {
     // the two sums beyond the steps belong to the buckets of the ends
     const int step = x <= 2 * a.R ? x : x == 2 * a.R + 1 ? 0 : 2 * a.R;
     bucket[x] = min(max(a.buckets[step], 0), a.num_buckets - 1);
+    sum[x] = sum_rows(mid + (int64_t)blockIdx.x * S * width, 0, S, 1, width, x);
   }
   __syncthreads();
   const int lane = threadIdx.x & 7;
-  for (int c0 = 0; c0 < a.num_buckets; c0 += 32) {
+  for (int c0 = 0; c0 < a.num_buckets; c0 += kGatherThreads / 8) {
     const int c = c0 + (threadIdx.x >> 3);
     float v = 0.f;
     for (int x = lane; x < width; x += 8) v += bucket[x] == c ? sum[x] : 0.f;
@@ -139,7 +151,7 @@ static ColBytes col_bytes(const ExtProblem& p, const ExtPlan& c) {
     const int64_t blocks = (p.Nk + 16 * c.blocks - 1) / (16 * c.blocks);
     const int subs = c.parts > 1 ? c.parts / ext_group(p) : 1;
     b.rows = p.B * blocks * subs * c.sets;
-    b.S = (int)std::max<int64_t>(1, std::min<int64_t>(64, b.rows));
+    b.S = (int)std::max<int64_t>(1, std::min<int64_t>(16, b.rows / 8));
     auto pad = [](int64_t n) { return (n + 15) / 16 * 16; };
     b.sums = pad(b.rows * p.H * ext_width(p) * 4);
     b.mid = pad(b.S * p.H * ext_width(p) * 4);
@@ -178,7 +190,7 @@ static int32_t gather_table(const ExtProblem& p, const ColBytes& b, const float*
   (void)hipGetLastError();
   hipLaunchKernelGGL(ext_step_rows_kernel, dim3(b.S, (unsigned)p.H), dim3(256), 0, s, sums, b.rows, width, mid);
   const ExtArgs a = ext_args(p, ExtPlan{}, 0, 0, nullptr);
-  hipLaunchKernelGGL(ext_buckets_kernel, dim3((unsigned)p.H), dim3(256), 0, s, (const float*)mid, b.S, a, out);
+  hipLaunchKernelGGL(ext_buckets_kernel, dim3((unsigned)p.H), dim3(kGatherThreads), 0, s, (const float*)mid, b.S, a, out);
   return finish_launch();
 }
 

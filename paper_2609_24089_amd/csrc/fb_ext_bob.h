@@ -49,9 +49,9 @@ int32_t ext_launch_pass1(const ExtProblem& p, const void* Q, const void* K, cons
                          ext_form_of<R, 2>(p, steps, kP1Step<T>.narrow)});
   c.blocks = R::shape(c.form).blocks();
   const ExtArgs a = ext_args(p, c, p.B * p.H, p.Nq, UT);
-  return ext_dispatch<R>(c.form, p, dim3(a.total), steps, s, (const T*)Q, (const T*)K, (const T*)V, (const T*)O,
+  return ext_dispatch<R>(c.form, p, dim3(a.total), steps, s, a, (const T*)Q, (const T*)K, (const T*)V, (const T*)O,
                          (const T*)dO, (const T*)UQ, (const T*)UK, (const T*)UV, L, Dv, (const T*)dQ, (T*)Qt, (T*)dOt,
-                         alpha, E, a);
+                         alpha, E);
 }
 
 template <typename T, int D> ExtPlan ext_pass2_plan(const ExtProblem& p) {
@@ -80,9 +80,9 @@ int32_t ext_launch_pass2(const ExtProblem& p, const void* Q, const void* K, cons
   using C = ExtPass2<T, D>;
   const ExtPlan c = ext_pass2_plan<T, D>(p);
   const ExtArgs a = ext_args(p, c, p.B * p.Hkv, p.Nk, UT);
-  const int32_t rc = ext_dispatch<C>(c.form, p, dim3(a.total, c.parts), pass2_dynamic(p, C::shape(c.form)), s,
+  const int32_t rc = ext_dispatch<C>(c.form, p, dim3(a.total, c.parts), pass2_dynamic(p, C::shape(c.form)), s, a,
                                      (const T*)Q, (const T*)K, (const T*)V, (const T*)dO, (const T*)UQ, (const T*)UK,
-                                     (const T*)UV, L, Dv, alpha, E, (T*)Kt, (T*)Vt, a, parts, sums);
+                                     (const T*)UV, L, Dv, alpha, E, (T*)Kt, (T*)Vt, parts, sums);
   if (rc != BOB_OK || c.parts == 1) return rc;
   return ext_add_parts(p, parts, c.parts, Kt, Vt, s);
 }

@@ -77,15 +77,15 @@ int32_t ext_launch_bwd(const ExtProblem& p, const void* Q, const void* K, const 
   if (p.Nq > 0) {
     const ExtPlan r = ext_rows_plan<T, D>(p);
     const ExtArgs a = ext_args(p, r, p.B * p.H, p.Nq, nullptr);
-    rc = ext_dispatch<ExtRowsBwd<T, D>>(r.form, p, dim3(a.total), ext_steps_bytes(p), s, (const T*)Q, (const T*)K,
-                                        (const T*)V, (const T*)O, (const T*)dO, L, (T*)dQ, Dv, a);
+    rc = ext_dispatch<ExtRowsBwd<T, D>>(r.form, p, dim3(a.total), ext_steps_bytes(p), s, a, (const T*)Q, (const T*)K,
+                                        (const T*)V, (const T*)O, (const T*)dO, L, (T*)dQ, Dv);
   }
   if (rc != BOB_OK || p.Nk == 0) return rc;
   const ExtPlan c = ext_cols_plan<T, D>(p);
   const ExtArgs a = ext_args(p, c, p.B * p.Hkv, p.Nk, nullptr);
   rc = ext_dispatch<ExtColsBwd<T, D>>(c.form, p, dim3(a.total, c.parts), cols_dynamic(p, ExtColsBwd<T, D>::shape(c.form)),
-                                      s, (const T*)Q, (const T*)K, (const T*)V, (const T*)dO, L, (const float*)Dv,
-                                      (T*)dK, (T*)dV, a, parts, sums);
+                                      s, a, (const T*)Q, (const T*)K, (const T*)V, (const T*)dO, L, (const float*)Dv,
+                                      (T*)dK, (T*)dV, parts, sums);
   if (rc != BOB_OK || c.parts == 1) return rc;
   return ext_add_parts(p, parts, c.parts, dK, dV, s);
 }

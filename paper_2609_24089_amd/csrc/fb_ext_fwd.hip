@@ -48,8 +48,8 @@ int32_t ext_launch_fwd(const ExtProblem& p, const void* Q, const void* K, const 
   const int64_t rows = c.fold ? ext_group(p) * p.Nq : p.Nq, heads = p.B * (c.fold ? p.Hkv : p.H);
   const ExtArgs a = ext_args(p, c, heads, rows, nullptr);
   const int64_t dynamic = ext_steps_bytes(p) * (c.fold ? std::min(ext_group(p), 16) : 1);
-  int32_t rc = ext_dispatch<ExtFwd<T, D>>(c.form, p, dim3(a.total, c.parts), dynamic, s, (const T*)Q, (const T*)K,
-                                          (const T*)V, (T*)O, L, a, ws);
+  int32_t rc = ext_dispatch<ExtFwd<T, D>>(c.form, p, dim3(a.total, c.parts), dynamic, s, a, (const T*)Q, (const T*)K,
+                                          (const T*)V, (T*)O, L, ws);
   if (rc != BOB_OK || c.parts == 1) return rc;
   const int64_t all = heads * rows;
   hipLaunchKernelGGL((ext_fwd_join_kernel<T, D>), dim3((unsigned)((all * (D / 4) + 255) / 256)), dim3(256), 0, s, ws,

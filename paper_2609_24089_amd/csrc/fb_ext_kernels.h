@@ -43,6 +43,7 @@ struct ExtArgs {
   int fold;            // row kernels: the rows of the grp query heads of a key/value head form one matrix
   float scale;
   int nparts;
+  int resident;        // of balanced_order(): causal grids of a few rounds
   const int32_t* q_lens;    // [B] or null: every row is valid
   const int32_t* kv_lens;
   const int32_t* q_starts;  // [B] or null: 0
@@ -149,49 +150,77 @@ struct ExtRun {
   __device__ __forceinline__ int size() const { return end - begin; }
 };
 
-// What a row kernel's workgroup and wave know of their rows.
-template <int MR, int NW>
+// What a row kernel's workgroup and wave know of their rows.  kFold: the kernel may run
+// folded rows (a.fold); the others keep one lane position instead of one a 16-row block.
+template <int MR, int NW, bool kFold>
 struct ExtRows {
   int b, kvh, head0, rows;   // batch entry, key/value head, first query head, rows of the matrix
   int64_t qrow;              // its first row among all query rows
   int kvis, tiles;           // keys that some row of the workgroup sees, their tiles
   int lo, hi;                // least and largest last valid key over the wave's rows
   int plo, phi;              // least and largest query position of the wave
-  int row[MR], pos[MR], klim[MR];  // the lane's rows, their positions and last valid keys
-  bool ok[MR];
+  int row0, qlen, Nq, start; // the lane's first row; valid rows of the entry, its rows, its first position
+  bool fold, causal;
 
   __device__ __forceinline__ ExtRows(const ExtArgs& a, int rh, int rb, int wl, int j) {
     constexpr int BR = 16 * MR * NW;
-    const int per_entry = a.fold != 0 ? a.H / a.grp : a.H;
+    fold = kFold && a.fold != 0;
+    causal = a.causal != 0;
+    const int per_entry = fold ? a.H / a.grp : a.H;
     b = rh / per_entry;
     const int h = rh - b * per_entry;
-    rows = a.fold != 0 ? a.grp * a.Nq : a.Nq;
-    kvh = a.fold != 0 ? rh : rh / a.grp;
-    head0 = a.fold != 0 ? h * a.grp : h;
+    rows = fold ? a.grp * a.Nq : a.Nq;
+    kvh = fold ? rh : rh / a.grp;
+    head0 = fold ? h * a.grp : h;
     qrow = (int64_t)rh * rows;
     const ExtLens n = ext_lens(a, b);
-    const int row0 = rb * BR + wl * 16 * MR;
+    qlen = n.q;
+    Nq = a.Nq;
+    start = n.start;
+    const int first = rb * BR + wl * 16 * MR;
+    row0 = first + j;
     // the last valid query of the workgroup; folded rows hold every query of each head
-    const int last = a.fold != 0 ? n.q - 1 : min(rb * BR + BR, n.q) - 1;
-    const bool none = a.fold != 0 ? n.q == 0 : n.q <= rb * BR;
-    kvis = none ? 0 : a.causal != 0 ? max(min(n.k, n.start + last + 1), 0) : n.k;
+    const int last = fold ? n.q - 1 : min(rb * BR + BR, n.q) - 1;
+    const bool none = fold ? n.q == 0 : n.q <= rb * BR;
+    kvis = none ? 0 : causal ? max(min(n.k, n.start + last + 1), 0) : n.k;
     tiles = (kvis + kBS - 1) / kBS;
-    plo = n.start + (a.fold != 0 ? 0 : row0);
-    phi = a.fold != 0 ? n.start + a.Nq - 1 : plo + 16 * MR - 1;
-    lo = a.causal != 0 ? min(kvis - 1, plo) : kvis - 1;
-    hi = a.causal != 0 ? min(kvis - 1, phi) : kvis - 1;
-#pragma unroll
-    for (int mb = 0; mb < MR; ++mb) {
-      row[mb] = row0 + 16 * mb + j;
-      const int i = a.fold != 0 ? row[mb] % a.Nq : row[mb];
-      pos[mb] = n.start + i;
-      klim[mb] = a.causal != 0 ? min(kvis - 1, pos[mb]) : kvis - 1;
-      ok[mb] = row[mb] < rows && i < n.q;
-    }
+    plo = n.start + (fold ? 0 : first);
+    phi = fold ? n.start + a.Nq - 1 : plo + 16 * MR - 1;
+    lo = causal ? min(kvis - 1, plo) : kvis - 1;
+    hi = causal ? min(kvis - 1, phi) : kvis - 1;
   }
+  __device__ __forceinline__ int row(int mb) const { return row0 + 16 * mb; }
+  __device__ __forceinline__ int query(int mb) const { return fold ? row(mb) % Nq : row(mb); }
+  __device__ __forceinline__ int pos(int mb) const { return start + query(mb); }
+  __device__ __forceinline__ int klim(int mb) const { return causal ? min(kvis - 1, pos(mb)) : kvis - 1; }  // last valid key
+  __device__ __forceinline__ bool ok(int mb) const { return row(mb) < rows && query(mb) < qlen; }
   // 0: no valid key of the tile at s0, 1: all valid for every row, 2: mixed
   __device__ __forceinline__ int mode(int s0) const { return s0 > hi ? 0 : s0 + kBS - 1 <= lo ? 1 : 2; }
 };
+
+// Which block a workgroup runs.  As map_block, one head's blocks stay on one XCD, whose L2
+// its key/value head's tensors then pass once; but units of heads that share a key/value
+// head go round the XCDs one by one where their number allows it, so that the entries of a
+// ragged batch spread over all of them: in map_block's runs of consecutive heads an XCD
+// got the longest entry's heads and another the shortest's (B8 H16 Nq512 Nk2048 d64, half to
+// full lengths, forward: 46 us in runs).  Causal grids of a few rounds run in
+// map_block_causal's order.  `per`: blocks of one unit.
+__device__ __forceinline__ void ext_map_block(const ExtArgs& a, int per, bool last_heavy, int& head, int& rb) {
+  if (a.resident > 0) {
+    map_block_causal(a.nRB, a.total, a.resident, last_heavy, head, rb);
+    return;
+  }
+  const int units = a.total / per;
+  if (units % kXCDs != 0) {
+    map_block(a.nRB, a.total, head, rb, last_heavy && a.causal != 0);
+    return;
+  }
+  const int xcd = blockIdx.x % kXCDs, i = blockIdx.x / kXCDs;
+  const int u = i / per, at = i - u * per, h = at / a.nRB;
+  head = (u * kXCDs + xcd) * (per / a.nRB) + h;
+  rb = at - h * a.nRB;
+  if (last_heavy && a.causal != 0) rb = a.nRB - 1 - rb;
+}
 
 // Exponents of invalid keys to -inf: x[sb][r] belongs to key s0 + 16 sb + 4 (l >> 4) + r.
 __device__ __forceinline__ void ext_mask1(floatx4 (&x)[2], int s0, int klim) {
@@ -211,8 +240,8 @@ __device__ __forceinline__ void ext_mask1(floatx4 (&x)[2], int s0, int klim) {
 // ===========================================================================
 template <typename T, int D, int MR, int NW, int OCC, int NSTAGE, int KS, bool kBias>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_fwd_kernel(
-    const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, T* __restrict__ O,
-    float* __restrict__ L, ExtArgs a, float* __restrict__ parts) {
+    ExtArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, T* __restrict__ O,
+    float* __restrict__ L, float* __restrict__ parts) {
   using E = Elt<T>;
   using G = Geo<T, D>;
   constexpr int BR = 16 * MR * NW;
@@ -221,18 +250,18 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_fwd_kernel(
   float FB_LDS* const steps = (float FB_LDS*)steps_mem;
 
   int rh, rb;
-  map_block(a.nRB, a.total, rh, rb, a.causal != 0);
+  ext_map_block(a, a.fold != 0 ? a.nRB : a.grp * a.nRB, true, rh, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
   const int wl = KS == 1 ? wave_id() : wave_id() % NW;
-  const ExtRows<MR, NW> rw(a, rh, rb, wl, j);
+  const ExtRows<MR, NW, NW == 1> rw(a, rh, rb, wl, j);
   const int part = blockIdx.y;
   const int64_t kvoff = (int64_t)rw.kvh * a.Nk * D;
 
   u32x4 qf[MR][G::kChunks];
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb)
-    load_stationary<T, D>(qf[mb], Q + rw.qrow * D, rw.ok[mb] ? rw.row[mb] : rw.rows, rw.rows);
+    load_stationary<T, D>(qf[mb], Q + rw.qrow * D, rw.ok(mb) ? rw.row(mb) : rw.rows, rw.rows);
 
   floatx4 acc[G::kNB][MR];
 #pragma unroll
@@ -267,7 +296,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_fwd_kernel(
     }
     if (mode == 2) {
 #pragma unroll
-      for (int mb = 0; mb < MR; ++mb) ext_mask1(e[mb], s0, rw.klim[mb]);
+      for (int mb = 0; mb < MR; ++mb) ext_mask1(e[mb], s0, rw.klim(mb));
     }
 #pragma unroll
     for (int mb = 0; mb < MR; ++mb) {
@@ -285,7 +314,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_fwd_kernel(
         for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
           for (int r = 0; r < 4; ++r) x[sb][r] = __builtin_fmaf(s[sb][mb][r], cf, kb[mb]);
-        if (mode == 2) ext_mask1(x, s0, rw.klim[mb]);
+        if (mode == 2) ext_mask1(x, s0, rw.klim(mb));
         float mx = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 8; ++i) mx = fmaxf(mx, x[i >> 2][i & 3]);
@@ -329,16 +358,16 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_fwd_kernel(
       [&]() {
         if constexpr (kBias) {
           const int n = ext_steps(a);
-          const int h0 = a.fold != 0 ? rb * BR / a.Nq : 0;  // folded: the heads of this block's rows
-          const int h1 = a.fold != 0 ? (min(rb * BR + BR, rw.rows) - 1) / a.Nq : 0;
+          const int h0 = rw.fold ? rb * BR / a.Nq : 0;  // folded: the heads of this block's rows
+          const int h1 = rw.fold ? (min(rb * BR + BR, rw.rows) - 1) / a.Nq : 0;
           ext_fill_steps<true>(a, a.table, rw.head0 + h0, h1 - h0 + 1, steps, KS * NW * 64);
           __syncthreads();
 #pragma unroll
           for (int mb = 0; mb < MR; ++mb) {
-            const int hh = a.fold != 0 ? min(rw.row[mb], rw.rows - 1) / a.Nq - h0 : 0;
+            const int hh = rw.fold ? min(rw.row(mb), rw.rows - 1) / a.Nq - h0 : 0;
             blo[mb] = steps[hh * n];
             bhi[mb] = steps[hh * n + n - 1];
-            tb[mb] = hh * n + a.R + kStepPad - rw.pos[mb];
+            tb[mb] = hh * n + a.R + kStepPad - rw.pos(mb);
           }
         }
       },
@@ -424,8 +453,8 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_fwd_kernel(
     float* const ml = parts + a.nparts * all * D;
 #pragma unroll
     for (int mb = 0; mb < MR; ++mb)
-      if (rw.ok[mb]) {
-        const int64_t at = part * all + rw.qrow + rw.row[mb];
+      if (rw.ok(mb)) {
+        const int64_t at = part * all + rw.qrow + rw.row(mb);
 #pragma unroll
         for (int nb = 0; nb < G::kNB; ++nb)
           if (own.owns(nb)) *(floatx4*)(parts + at * D + 16 * nb + 4 * g) = acc[nb][mb];
@@ -438,9 +467,9 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_fwd_kernel(
   }
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb) {
-    if (rw.row[mb] >= rw.rows) continue;
-    const int64_t at = rw.qrow + rw.row[mb];
-    const bool some = rw.ok[mb] && lt[mb] != 0.f;
+    if (rw.row(mb) >= rw.rows) continue;
+    const int64_t at = rw.qrow + rw.row(mb);
+    const bool some = rw.ok(mb) && lt[mb] != 0.f;
     const float inv = 1.f / lt[mb];
 #pragma unroll
     for (int nb = 0; nb < G::kNB; ++nb)
@@ -485,12 +514,14 @@ __global__ __launch_bounds__(256) void ext_fwd_join_kernel(const float* __restri
 // fp32: the tiles form dP minus do_i . o_i, whose o_i is rounded to the tensors' type, and
 // D_i adds what sum_j P_ij (dP_ij - do_i . o_i) is off zero.  The table's gradient is a
 // sum over many rows of fp32 products, and that rounding of o would be its largest error
-// by far (2^-9 of D a row against 2^-24).
+// by far (2^-8 of D a row against 2^-24).  In dQ it matters where few keys share a row's
+// weight (a row of one key has dQ = 0): a row whose whole weight lies in a set's first tile
+// takes D from that tile.
 // ===========================================================================
 template <typename T, int D, int MR, int NW, int OCC, int NSTAGE, int KS, bool kBias>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
-    const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ O,
-    const T* __restrict__ dO, const float* __restrict__ L, T* __restrict__ dQ, float* __restrict__ Dout, ExtArgs a) {
+    ExtArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ O,
+    const T* __restrict__ dO, const float* __restrict__ L, T* __restrict__ dQ, float* __restrict__ Dout) {
   using E = Elt<T>;
   using G = Geo<T, D>;
   constexpr int BR = 16 * MR * NW;
@@ -499,18 +530,19 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
   float FB_LDS* const steps = (float FB_LDS*)steps_mem;
 
   int rh, rb;
-  map_block(a.nRB, a.total, rh, rb, a.causal != 0);
+  ext_map_block(a, a.grp * a.nRB, true, rh, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
   const int wl = KS == 1 ? wave_id() : wave_id() % NW;
-  const ExtRows<MR, NW> rw(a, rh, rb, wl, j);
+  const ExtRows<MR, NW, false> rw(a, rh, rb, wl, j);
   const int64_t kvoff = (int64_t)rw.kvh * a.Nk * D, qoff = rw.qrow * D;
 
   u32x4 qf[MR][G::kChunks], dof[MR][G::kChunks];
-  float lb[MR], drow[MR], rest[MR];
+  float lb[MR], drow[MR], dout[MR], rest[MR];
+  bool centred = false;
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb) {
-    const int row = rw.ok[mb] ? rw.row[mb] : rw.rows;
+    const int row = rw.ok(mb) ? rw.row(mb) : rw.rows;
     load_stationary<T, D>(qf[mb], Q + qoff, row, rw.rows);
     load_stationary<T, D>(dof[mb], dO + qoff, row, rw.rows);
     u32x4 of[G::kChunks];
@@ -518,9 +550,9 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
     float part = 0.f;
 #pragma unroll
     for (int kk = 0; kk < G::kChunks; ++kk) part += E::dot_chunk(dof[mb][kk], of[kk]);
-    drow[mb] = group_sum(part);
+    drow[mb] = dout[mb] = group_sum(part);
     // an empty row (L = -inf) gets P = 0
-    const float Lr = rw.ok[mb] ? L[rw.qrow + rw.row[mb]] : 0.f;
+    const float Lr = rw.ok(mb) ? L[rw.qrow + rw.row(mb)] : 0.f;
     lb[mb] = Lr == -INFINITY ? INFINITY : Lr * kLog2e;
     rest[mb] = 0.f;
   }
@@ -554,7 +586,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
       },
       [&](int it, int st) {
         const int s0 = min(run.begin + it, rw.tiles - 1) * kBS;
-        const int mode = __builtin_amdgcn_readfirstlane(run.begin + it < run.end ? rw.mode(s0) : 0);
+        const int mode = run.begin + it < run.end ? rw.mode(s0) : 0;
         if (mode == 0) return;
         const T FB_LDS* Ks = (const T FB_LDS*)sm.lds[ks][st];
         const T FB_LDS* Vs = Ks + G::kTileElems;
@@ -597,7 +629,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
           if (ext_side(s0 - rw.phi, s0 + kBS - 1 - rw.plo, a.R) == 0) {
 #pragma unroll
             for (int mb = 0; mb < MR; ++mb) {
-              const float FB_LDS* bias = steps + (a.R + kStepPad + s0 - rw.pos[mb] + 4 * g);
+              const float FB_LDS* bias = steps + (a.R + kStepPad + s0 - rw.pos(mb) + 4 * g);
 #pragma unroll
               for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
@@ -609,9 +641,32 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
 #pragma unroll
           for (int mb = 0; mb < MR; ++mb) {
             floatx4 x[2] = {s[0][mb], s[1][mb]};
-            ext_mask1(x, s0, rw.klim[mb]);
+            ext_mask1(x, s0, rw.klim(mb));
             s[0][mb] = x[0];
             s[1][mb] = x[1];
+          }
+        }
+        if (!centred) {
+          centred = true;
+#pragma unroll
+          for (int mb = 0; mb < MR; ++mb) {
+            float w = 0.f, wd = 0.f;
+#pragma unroll
+            for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const float p = fast_exp2(s[sb][mb][r]);
+                w += p;
+                wd = __builtin_fmaf(p, dp[sb][mb][r], wd);
+              }
+            w = group_sum(w);
+            wd = group_sum(wd);
+            // L and the weights are off by a few 2^-24 of L's size
+            const float by = w > 1.f - 0x1p-16f ? wd / w : 0.f;
+            drow[mb] += by;
+            rest[mb] = g == 0 ? by : 0.f;
+#pragma unroll
+            for (int sb = 0; sb < 2; ++sb) dp[sb][mb] -= by;
           }
         }
 #pragma unroll
@@ -651,13 +706,13 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
   const RowSplit<KS> own{ks, 0};
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb) {
-    if (rw.row[mb] >= rw.rows) continue;
-    const int64_t at = rw.qrow + rw.row[mb];
+    if (rw.row(mb) >= rw.rows) continue;
+    const int64_t at = rw.qrow + rw.row(mb);
 #pragma unroll
     for (int nb = 0; nb < G::kNB; ++nb)
       if (own.owns(nb))
-        E::store4(dQ + at * D + 16 * nb + 4 * g, rw.ok[mb] ? acc[nb][mb] * a.scale : floatx4{0.f, 0.f, 0.f, 0.f});
-    if (g == 0 && ks == 0) Dout[at] = rw.ok[mb] ? drow[mb] + rest[mb] : 0.f;
+        E::store4(dQ + at * D + 16 * nb + 4 * g, rw.ok(mb) ? acc[nb][mb] * a.scale : floatx4{0.f, 0.f, 0.f, 0.f});
+    if (g == 0 && ks == 0) Dout[at] = rw.ok(mb) ? dout[mb] + rest[mb] : 0.f;
   }
 }
 
@@ -896,8 +951,8 @@ __global__ __launch_bounds__(256) void ext_parts_kernel(const float* __restrict_
 // the table's step sums (`sums`, or null).
 template <typename T, int D, int MC, int NW, int OCC, int KS, bool kKL, bool kBias>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_cols_kernel(
-    const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ dO,
-    const float* __restrict__ L, const float* __restrict__ Dv, T* __restrict__ dK, T* __restrict__ dV, ExtArgs a,
+    ExtArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ dO,
+    const float* __restrict__ L, const float* __restrict__ Dv, T* __restrict__ dK, T* __restrict__ dV,
     float* __restrict__ parts, float* __restrict__ sums) {
   using E = Elt<T>;
   using G = Geo<T, D>;
@@ -915,7 +970,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_cols_kernel(
   extern __shared__ float steps_mem[];
 
   int kv, rb;
-  map_block(a.nRB, a.total, kv, rb);
+  ext_map_block(a, a.nRB, false, kv, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
   const int wl = KS == 1 ? wave_id() : wave_id() % NW;
@@ -975,7 +1030,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_cols_kernel(
       },
       [&](int it, int st, int ts, auto&& prep_next) {
         const int s0 = cl.tile(flat(it)) * kBS;
-        const int mode = __builtin_amdgcn_readfirstlane(run.begin + it < run.end ? cl.mode(s0, a.causal != 0) : 0);
+        const int mode = run.begin + it < run.end ? cl.mode(s0, a.causal != 0) : 0;
         if (mode == 0) {
           prep_next();
           return;
@@ -1109,10 +1164,10 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_cols_kernel(
 // ===========================================================================
 template <typename T, int D, int MR, int NW, int OCC, int KS, int kPF, bool kBias>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
-    const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ O,
+    ExtArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ O,
     const T* __restrict__ dO, const T* __restrict__ UQ, const T* __restrict__ UK, const T* __restrict__ UV,
     const float* __restrict__ L, const float* __restrict__ Dv, const T* __restrict__ dQ, T* __restrict__ Qt,
-    T* __restrict__ dOt, float* __restrict__ alpha_out, float* __restrict__ E_out, ExtArgs a) {
+    T* __restrict__ dOt, float* __restrict__ alpha_out, float* __restrict__ E_out) {
   using E = Elt<T>;
   using G = Geo<T, D>;
   constexpr int BR = 16 * MR * NW;
@@ -1123,24 +1178,24 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
   float FB_LDS* const dirs = steps + (kBias ? (ext_steps(a) + 3) & ~3 : 0);
 
   int rh, rb;
-  map_block(a.nRB, a.total, rh, rb, a.causal != 0);
+  ext_map_block(a, a.grp * a.nRB, true, rh, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
   const int wl = KS == 1 ? wave_id() : wave_id() % NW;
-  const ExtRows<MR, NW> rw(a, rh, rb, wl, j);
+  const ExtRows<MR, NW, false> rw(a, rh, rb, wl, j);
   const int64_t kvoff = (int64_t)rw.kvh * a.Nk * D, qoff = rw.qrow * D;
 
   u32x4 qf[MR][G::kChunks], uqf[MR][G::kChunks], dof[MR][G::kChunks];
   float lb[MR], drow[MR];
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb) {
-    const int row = rw.ok[mb] ? rw.row[mb] : rw.rows;
+    const int row = rw.ok(mb) ? rw.row(mb) : rw.rows;
     load_stationary<T, D>(qf[mb], Q + qoff, row, rw.rows);
     load_stationary<T, D>(uqf[mb], UQ + qoff, row, rw.rows);
     load_stationary<T, D>(dof[mb], dO + qoff, row, rw.rows);
-    const float Lr = rw.ok[mb] ? L[rw.qrow + rw.row[mb]] : 0.f;
+    const float Lr = rw.ok(mb) ? L[rw.qrow + rw.row(mb)] : 0.f;
     lb[mb] = Lr == -INFINITY ? INFINITY : Lr * kLog2e;
-    drow[mb] = rw.ok[mb] ? Dv[rw.qrow + rw.row[mb]] : 0.f;
+    drow[mb] = rw.ok(mb) ? Dv[rw.qrow + rw.row(mb)] : 0.f;
   }
   floatx4 aDO[G::kNB][MR], aOM[G::kNB][MR], aB[G::kNB][MR];
 #pragma unroll
@@ -1183,7 +1238,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
       },
       [&](int it, int st) {
         const int s0 = min(run.begin + it, rw.tiles - 1) * kBS;
-        const int mode = __builtin_amdgcn_readfirstlane(run.begin + it < run.end ? rw.mode(s0) : 0);
+        const int mode = run.begin + it < run.end ? rw.mode(s0) : 0;
         if (mode == 0 && (KS == 1 || it > 0)) return;
         const T FB_LDS* Ks = (const T FB_LDS*)sm.lds[ks][st];
         const T FB_LDS* Vs = Ks + G::kTileElems;
@@ -1242,7 +1297,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
           if (side == 0) {
 #pragma unroll
             for (int mb = 0; mb < MR; ++mb) {
-              const int at = a.R + kStepPad + s0 - rw.pos[mb] + 4 * g;
+              const int at = a.R + kStepPad + s0 - rw.pos(mb) + 4 * g;
 #pragma unroll
               for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
@@ -1257,12 +1312,13 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
 #pragma unroll
           for (int mb = 0; mb < MR; ++mb) {
             floatx4 x[2] = {s[0][mb], s[1][mb]};
-            ext_mask1(x, s0, rw.klim[mb]);
+            ext_mask1(x, s0, rw.klim(mb));
             s[0][mb] = x[0];
             s[1][mb] = x[1];
           }
         }
-        if (!centred) {
+        // every wave of a workgroup with sets comes here in its first iteration (a barrier)
+        if (KS > 1 ? it == 0 : !centred) {
           centred = true;
 #pragma unroll
           for (int mb = 0; mb < MR; ++mb) {
@@ -1395,18 +1451,18 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
   const floatx4 zero = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb) {
-    if (rw.row[mb] >= rw.rows) continue;
-    const int64_t at = rw.qrow + rw.row[mb];
+    if (rw.row(mb) >= rw.rows) continue;
+    const int64_t at = rw.qrow + rw.row(mb);
     if (g == 0 && ks == 0) {
       const float al = aref[mb] + alpha[mb];
-      alpha_out[at] = rw.ok[mb] ? al : 0.f;
-      E_out[at] = rw.ok[mb] ? eref[mb] + e0[mb] - al * drow[mb] : 0.f;
+      alpha_out[at] = rw.ok(mb) ? al : 0.f;
+      E_out[at] = rw.ok(mb) ? eref[mb] + e0[mb] - al * drow[mb] : 0.f;
     }
 #pragma unroll
     for (int nb = 0; nb < G::kNB; ++nb) {
       if (!own.owns(nb)) continue;
       const int64_t off = at * D + 16 * nb + 4 * g;
-      if (rw.ok[mb]) {
+      if (rw.ok(mb)) {
         E::store4(dOt + off, aDO[nb][mb] - alpha[mb] * E::load4(O + off));
         E::store4(Qt + off, a.scale * (aOM[nb][mb] - e0[mb] * aB[nb][mb]) - alpha[mb] * E::load4(dQ + off));
       } else {
@@ -1422,10 +1478,10 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
 // ===========================================================================
 template <typename T, int D, int MC, int NW, int OCC, int KS, bool kPF, bool kBias>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass2_kernel(
-    const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ dO,
+    ExtArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ dO,
     const T* __restrict__ UQ, const T* __restrict__ UK, const T* __restrict__ UV, const float* __restrict__ L,
     const float* __restrict__ Dv, const float* __restrict__ alpha_in, const float* __restrict__ E_in,
-    T* __restrict__ Kt, T* __restrict__ Vt, ExtArgs a, float* __restrict__ parts, float* __restrict__ sums) {
+    T* __restrict__ Kt, T* __restrict__ Vt, float* __restrict__ parts, float* __restrict__ sums) {
   using E = Elt<T>;
   using G = Geo<T, D>;
   struct Smem2 {
@@ -1437,7 +1493,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass2_kernel(
   extern __shared__ float steps_mem[];
 
   int kv, rb;
-  map_block(a.nRB, a.total, kv, rb);
+  ext_map_block(a, a.nRB, false, kv, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
   const int wl = KS == 1 ? wave_id() : wave_id() % NW;
@@ -1500,7 +1556,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass2_kernel(
       },
       [&](int it, int st, int ts, auto&& prep_next) {
         const int s0 = cl.tile(flat(it)) * kBS;
-        const int mode = __builtin_amdgcn_readfirstlane(run.begin + it < run.end ? cl.mode(s0, a.causal != 0) : 0);
+        const int mode = run.begin + it < run.end ? cl.mode(s0, a.causal != 0) : 0;
         if (mode == 0) {
           prep_next();
           return;

@@ -508,7 +508,9 @@ struct ExtAttentionBackward : torch::autograd::Function<ExtAttentionBackward> {
     const ExtDims m = ext_dims_or_throw({&q, &O, &dO}, {&k, &v}, {&L}, e);
     c10::OptionalDeviceGuard guard(q.device());
     ExtBwd r = run_ext_bwd(m, q, k, v, O, dO, L, e, scale, causal, want_table);
-    ctx->save_for_backward({q, k, v, table, O, L, dO, r.D, r.dQ, buckets, kv_lens, q_lens, q_starts});
+    // dQ as well: an output, and no path of the second backward
+    ctx->save_for_backward({q, k, v, table, O, L, dO, r.D, r.dQ.detach(), buckets, kv_lens, q_lens, q_starts});
+    ctx->set_materialize_grads(false);
     ctx->saved_data["scale"] = scale;
     ctx->saved_data["causal"] = causal;
     variable_list out{r.dQ, r.dK, r.dV};
@@ -554,7 +556,9 @@ struct ExtAttention : torch::autograd::Function<ExtAttention> {
     const ExtDims m = ext_dims_or_throw({&q}, {&k, &v}, {}, e);
     c10::OptionalDeviceGuard guard(q.device());
     Rows2 r = run_ext_fwd(m, q, k, v, scale, causal);
-    ctx->save_for_backward({q, k, v, table, r.O, r.L, buckets, kv_lens, q_lens, q_starts});
+    // O without its graph: the first backward passes no gradient on to it, and the engine
+    // would run this node's backward on zeros for that
+    ctx->save_for_backward({q, k, v, table, r.O.detach(), r.L, buckets, kv_lens, q_lens, q_starts});
     ctx->saved_data["scale"] = scale;
     ctx->saved_data["causal"] = causal;
     return r.O;

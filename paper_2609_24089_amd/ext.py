@@ -245,7 +245,9 @@ class _ExtFn(torch.autograd.Function):
     def forward(ctx, q, k, v, table, buckets, kv_lens, q_lens, q_starts, scale, causal):
         bias = None if table is None else (table, buckets)
         O, L = attn_ext_fwd_lse(q, k, v, scale, causal, bias, kv_lens, q_lens, q_starts)
-        ctx.save_for_backward(q, k, v, table, buckets, kv_lens, q_lens, q_starts, O, L)
+        # O without its graph: the first backward passes no gradient on to it, and the engine
+        # would run this node's backward on zeros for that
+        ctx.save_for_backward(q, k, v, table, buckets, kv_lens, q_lens, q_starts, O.detach(), L)
         ctx.scale, ctx.causal = scale, causal
         return O
 
@@ -263,7 +265,8 @@ class _ExtBackwardFn(torch.autograd.Function):
         bias = None if table is None else (table, buckets)
         dq, dk, dv, D, dt = attn_ext_bwd(q, k, v, O, dO, L, scale, causal, bias, kv_lens, q_lens, q_starts,
                                          want_table=want_table)
-        ctx.save_for_backward(q, k, v, table, buckets, kv_lens, q_lens, q_starts, O, L, dO, D, dq)
+        ctx.save_for_backward(q, k, v, table, buckets, kv_lens, q_lens, q_starts, O, L, dO, D, dq.detach())
+        ctx.set_materialize_grads(False)
         ctx.scale, ctx.causal = scale, causal
         return dq, dk, dv, dt
 
