@@ -97,8 +97,8 @@ template <auto kKernel> int64_t static_lds() {
 }
 
 // ---------------------------------------------------------------------------
-// Row kernels: whole blocks, 64-row blocks in wave sets, 16-row blocks in sets of one wave.
-// Kern<form, bias>::kernel() names the kernel, Kern::shape(form) its shape.
+// Kernels: whole blocks, and 64-, 32- and 16-row blocks in wave sets.
+// Kern::kernel<form, bias>() names the kernel, Kern::shape(form, bias) its shape.
 // ---------------------------------------------------------------------------
 struct ExtShape {
   int mr, nw, occ, st, ks;
@@ -107,6 +107,8 @@ struct ExtShape {
   constexpr bool built() const { return mr > 0; }
 };
 constexpr ExtShape kNotBuilt{0, 1, 1, 2, 1};
+// Forms: 0 whole blocks, the others blocks of this many waves of 16 rows in wave sets.
+constexpr int kFormWaves[4] = {0, 4, 1, 2};
 
 // Sets of `tensors` streamed tensors in blocks of nw waves of 16 rows, if more than one fits.
 template <typename T, int D> constexpr ExtShape ext_sets(int nw, int tensors, int extra, int max_waves, int occ) {
@@ -118,40 +120,41 @@ template <typename T, int D> constexpr ExtShape ext_sets(int nw, int tensors, in
 }
 
 template <typename Kern, int F> Form ext_form_of(const ExtProblem& p, int64_t dynamic, double narrow) {
-  constexpr ExtShape s = Kern::shape(F);
-  if constexpr (s.built()) {
-    const bool bias = has_bias(p);
-    const int64_t lds = bias ? static_lds<Kern::template kernel<F, true>()>() : static_lds<Kern::template kernel<F, false>()>();
-    if (F > 0 && lds + dynamic > kMaxLds) return {};
-    const int fit = bias ? resident_blocks<Kern::template kernel<F, true>()>(s.threads())
-                         : resident_blocks<Kern::template kernel<F, false>()>(s.threads());
-    return {s.blocks(), s.ks, fit, s.threads(), 1, 0.0, F == 0 ? 1.0 : narrow};
-  }
-  return {};
+  auto form = [&](auto bias) -> Form {
+    constexpr bool kBias = decltype(bias)::value;
+    constexpr ExtShape s = Kern::shape(F, kBias);
+    if constexpr (s.built()) {
+      if (F > 0 && static_lds<Kern::template kernel<F, kBias>()>() + dynamic > kMaxLds) return {};
+      const int fit = resident_blocks<Kern::template kernel<F, kBias>()>(s.threads());
+      return {s.blocks(), s.ks, fit, s.threads(), 1, 0.0, F == 0 ? 1.0 : narrow};
+    }
+    return {};
+  };
+  return has_bias(p) ? form(std::true_type{}) : form(std::false_type{});
 }
 
 // Launches form F of Kern, whose first argument is a.
 template <typename Kern, int F, typename... Args>
 int32_t ext_go(const ExtProblem& p, dim3 grid, int64_t dynamic, hipStream_t stream, ExtArgs a, Args... args) {
-  constexpr ExtShape s = Kern::shape(F);
-  if constexpr (s.built()) {
-    if (p.causal != 0 && grid.y == 1) {
-      const int fit = has_bias(p) ? resident_blocks<Kern::template kernel<F, true>()>(s.threads())
-                                  : resident_blocks<Kern::template kernel<F, false>()>(s.threads());
-      a.resident = balanced_order(a.total, fit, device_cus());
+  auto go = [&](auto bias) -> int32_t {
+    constexpr bool kBias = decltype(bias)::value;
+    constexpr ExtShape s = Kern::shape(F, kBias);
+    if constexpr (s.built()) {
+      constexpr auto kernel = Kern::template kernel<F, kBias>();
+      if (p.causal != 0 && grid.y == 1)
+        a.resident = balanced_order(a.total, resident_blocks<kernel>(s.threads()), device_cus());
+      (void)hipGetLastError();
+      hipLaunchKernelGGL(kernel, grid, dim3(s.threads()), (unsigned)(kBias ? dynamic : 0), stream, a, args...);
+      return finish_launch();
     }
-    (void)hipGetLastError();
-    if (has_bias(p))
-      hipLaunchKernelGGL((Kern::template kernel<F, true>()), grid, dim3(s.threads()), (unsigned)dynamic, stream, a, args...);
-    else
-      hipLaunchKernelGGL((Kern::template kernel<F, false>()), grid, dim3(s.threads()), 0, stream, a, args...);
-    return finish_launch();
-  }
-  return BOB_EUNSUPPORTED;
+    return BOB_EUNSUPPORTED;
+  };
+  return has_bias(p) ? go(std::true_type{}) : go(std::false_type{});
 }
 template <typename Kern, typename... Args>
 int32_t ext_dispatch(int form, const ExtProblem& p, dim3 grid, int64_t dynamic, hipStream_t stream, const ExtArgs& a,
                      Args... args) {
+  if (form == 3) return ext_go<Kern, 3>(p, grid, dynamic, stream, a, args...);
   if (form == 2) return ext_go<Kern, 2>(p, grid, dynamic, stream, a, args...);
   if (form == 1) return ext_go<Kern, 1>(p, grid, dynamic, stream, a, args...);
   return ext_go<Kern, 0>(p, grid, dynamic, stream, a, args...);

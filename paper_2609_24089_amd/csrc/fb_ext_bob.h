@@ -6,27 +6,27 @@
 namespace fb {
 
 template <typename T, int D> struct ExtPass1 {
-  static constexpr ExtShape shape(int form) {
+  static constexpr ExtShape shape(int form, bool bias) {
     constexpr Shape w = Cfg<T, D>::kP1;
     return form == 0   ? ExtShape{w.mr, w.nw, w.occ, w.st, 1}
-           : form == 1 ? ext_sets<T, D>(4, 4, 0, 8, w.occ)
-                       : ext_sets<T, D>(1, 4, 0, 8, w.occ);
+                       : ext_sets<T, D>(kFormWaves[form], 4, 0, 8, w.occ);
   }
   template <int F, bool kBias> static __host__ constexpr auto kernel() {
-    constexpr ExtShape s = shape(F);
+    constexpr ExtShape s = shape(F, kBias);
     return &ext_pass1_kernel<T, D, s.mr, s.nw, s.occ, s.ks, Cfg<T, D>::kP1.pf, kBias>;
   }
 };
 template <typename T, int D> struct ExtPass2 {
   static constexpr int kExtra = 4 * 4 * kBS * (int)sizeof(float) + 1024;
-  static constexpr ExtShape shape(int form) {
+  static constexpr ExtShape shape(int form, bool bias) {
     constexpr Shape w = Cfg<T, D>::kP2;
     return form == 0   ? ExtShape{w.mr, w.nw, w.occ, w.st, 1}
-           : form == 1 ? (sizeof(T) == 2 && D == 32 ? kNotBuilt : ext_sets<T, D>(4, 3, kExtra, 8, w.occ))
-                       : ext_sets<T, D>(1, 3, kExtra, 8, w.occ);
+           : sizeof(T) == 2 && D == 32 && form == 1
+               ? kNotBuilt  // three tensors of two 1 KB blocks do not deal out over four waves
+               : ext_sets<T, D>(kFormWaves[form], 3, kExtra, 8, w.occ);
   }
   template <int F, bool kBias> static __host__ constexpr auto kernel() {
-    constexpr ExtShape s = shape(F);
+    constexpr ExtShape s = shape(F, kBias);
     return &ext_pass2_kernel<T, D, s.mr, s.nw, s.occ, s.ks, Cfg<T, D>::kP2.pf != 0, kBias>;
   }
 };
@@ -46,8 +46,9 @@ int32_t ext_launch_pass1(const ExtProblem& p, const void* Q, const void* K, cons
                     block_us<T>(10, D), kP1Step<T>, merge_us(3, D), kRowMargin};
   ExtPlan c;
   c.form = pick_form(q, {ext_form_of<R, 0>(p, steps, 1.0), ext_form_of<R, 1>(p, steps, kP1Step<T>.narrow),
-                         ext_form_of<R, 2>(p, steps, kP1Step<T>.narrow)});
-  c.blocks = R::shape(c.form).blocks();
+                         ext_form_of<R, 2>(p, steps, kP1Step<T>.narrow),
+                         ext_form_of<R, 3>(p, steps, kP1Step<T>.narrow)});
+  c.blocks = R::shape(c.form, has_bias(p)).blocks();
   const ExtArgs a = ext_args(p, c, p.B * p.H, p.Nq, UT);
   return ext_dispatch<R>(c.form, p, dim3(a.total), steps, s, a, (const T*)Q, (const T*)K, (const T*)V, (const T*)O,
                          (const T*)dO, (const T*)UQ, (const T*)UK, (const T*)UV, L, Dv, (const T*)dQ, (T*)Qt, (T*)dOt,
@@ -62,10 +63,11 @@ template <typename T, int D> ExtPlan ext_pass2_plan(const ExtProblem& p) {
   const int64_t tiles = std::max<int64_t>((p.Nq + kBS - 1) / kBS, 1) * (split ? 1 : grp);
   const FormQuery q{device_cus(), p.B * (split ? p.H : p.Hkv), std::max<int64_t>(p.Nk, 1), tiles, p.causal != 0,
                     block_us<T>(8, D), kP2Step<T>, merge_us(2, D), 1.0};
-  c.form = pick_form(q, {ext_form_of<C, 0>(p, pass2_dynamic(p, C::shape(0)), 1.0),
-                         ext_form_of<C, 1>(p, pass2_dynamic(p, C::shape(1)), kP2Step<T>.narrow),
-                         ext_form_of<C, 2>(p, pass2_dynamic(p, C::shape(2)), kP2Step<T>.narrow)});
-  const ExtShape s = C::shape(c.form);
+  c.form = pick_form(q, {ext_form_of<C, 0>(p, pass2_dynamic(p, C::shape(0, has_bias(p))), 1.0),
+                         ext_form_of<C, 1>(p, pass2_dynamic(p, C::shape(1, has_bias(p))), kP2Step<T>.narrow),
+                         ext_form_of<C, 2>(p, pass2_dynamic(p, C::shape(2, has_bias(p))), kP2Step<T>.narrow),
+                         ext_form_of<C, 3>(p, pass2_dynamic(p, C::shape(3, has_bias(p))), kP2Step<T>.narrow)});
+  const ExtShape s = C::shape(c.form, has_bias(p));
   c.blocks = s.blocks();
   c.sets = s.ks * s.nw;
   c.parts = split ? grp : 1;
@@ -80,7 +82,7 @@ int32_t ext_launch_pass2(const ExtProblem& p, const void* Q, const void* K, cons
   using C = ExtPass2<T, D>;
   const ExtPlan c = ext_pass2_plan<T, D>(p);
   const ExtArgs a = ext_args(p, c, p.B * p.Hkv, p.Nk, UT);
-  const int32_t rc = ext_dispatch<C>(c.form, p, dim3(a.total, c.parts), pass2_dynamic(p, C::shape(c.form)), s, a,
+  const int32_t rc = ext_dispatch<C>(c.form, p, dim3(a.total, c.parts), pass2_dynamic(p, C::shape(c.form, has_bias(p))), s, a,
                                      (const T*)Q, (const T*)K, (const T*)V, (const T*)dO, (const T*)UQ, (const T*)UK,
                                      (const T*)UV, L, Dv, alpha, E, (T*)Kt, (T*)Vt, parts, sums);
   if (rc != BOB_OK || c.parts == 1) return rc;

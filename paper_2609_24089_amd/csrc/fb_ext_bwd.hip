@@ -4,29 +4,30 @@
 namespace fb {
 
 template <typename T, int D> struct ExtRowsBwd {
-  static constexpr ExtShape shape(int form) {
+  static constexpr ExtShape shape(int form, bool bias) {
     constexpr Shape w = Cfg<T, D>::kRows;
     return form == 0   ? ExtShape{w.mr, w.nw, w.occ, w.st, 1}
-           : form == 1 ? ext_sets<T, D>(4, 2, 0, 16, w.occ)
-                       : ext_sets<T, D>(1, 2, 0, 16, w.occ);
+                       : ext_sets<T, D>(kFormWaves[form], 2, 0, 16, w.occ);
   }
   template <int F, bool kBias> static __host__ constexpr auto kernel() {
-    constexpr ExtShape s = shape(F);
+    constexpr ExtShape s = shape(F, kBias);
     return &ext_bwd_rows_kernel<T, D, s.mr, s.nw, s.occ, s.st, s.ks, kBias>;
   }
 };
 
 template <typename T, int D> struct ExtColsBwd {
   static constexpr int kExtra = 4 * 2 * kBS * (int)sizeof(float) + 1024;  // raw and transformed L, D; bias buffers
-  static constexpr ExtShape shape(int form) {
+  static constexpr ExtShape shape(int form, bool bias) {
     constexpr Shape w = Cfg<T, D>::kCols;
     constexpr int waves = D * (int)sizeof(T) <= 128 ? 16 : 8;
-    return form == 0   ? ExtShape{w.mr, w.nw, w.occ, w.st, 1}
-           : form == 1 ? ext_sets<T, D>(4, 2, kExtra, waves, w.occ)
-                       : ext_sets<T, D>(1, 2, kExtra, waves, w.occ);
+    // three waves per SIMD for some spills beside the near tiles: 814 us for 881 with two at
+    // B4 H12 N4096 dense, 462 for 485 causal (first backward)
+    constexpr bool kThree = std::is_same_v<T, bf16> && D == 64;
+    return form == 0   ? ExtShape{w.mr, w.nw, bias && kThree ? 3 : w.occ, w.st, 1}
+                       : ext_sets<T, D>(kFormWaves[form], 2, kExtra, waves, w.occ);
   }
   template <int F, bool kBias> static __host__ constexpr auto kernel() {
-    constexpr ExtShape s = shape(F);
+    constexpr ExtShape s = shape(F, kBias);
     return &ext_bwd_cols_kernel<T, D, s.mr, s.nw, s.occ, s.ks, F == 0 && Cfg<T, D>::kCols.kl != 0, kBias>;
   }
 };
@@ -43,8 +44,9 @@ template <typename T, int D> ExtPlan ext_rows_plan(const ExtProblem& p) {
   ExtPlan c;
   c.form = pick_form(q, {ext_form_of<ExtRowsBwd<T, D>, 0>(p, steps, 1.0),
                          ext_form_of<ExtRowsBwd<T, D>, 1>(p, steps, kRowsStep<T>.narrow),
-                         ext_form_of<ExtRowsBwd<T, D>, 2>(p, steps, kRowsStep<T>.narrow)});
-  const ExtShape s = ExtRowsBwd<T, D>::shape(c.form);
+                         ext_form_of<ExtRowsBwd<T, D>, 2>(p, steps, kRowsStep<T>.narrow),
+                         ext_form_of<ExtRowsBwd<T, D>, 3>(p, steps, kRowsStep<T>.narrow)});
+  const ExtShape s = ExtRowsBwd<T, D>::shape(c.form, has_bias(p));
   c.blocks = s.blocks();
   c.sets = s.ks;
   return c;
@@ -59,10 +61,11 @@ template <typename T, int D> ExtPlan ext_cols_plan(const ExtProblem& p) {
   const int64_t tiles = std::max<int64_t>((p.Nq + kBS - 1) / kBS, 1) * (split ? 1 : grp);
   const FormQuery q{device_cus(), p.B * (split ? p.H : p.Hkv), std::max<int64_t>(p.Nk, 1), tiles, p.causal != 0,
                     block_us<T>(4, D), kColsStep<T>, merge_us(2, D), 1.0};
-  c.form = pick_form(q, {ext_form_of<C, 0>(p, cols_dynamic(p, C::shape(0)), 1.0),
-                         ext_form_of<C, 1>(p, cols_dynamic(p, C::shape(1)), kColsStep<T>.narrow),
-                         ext_form_of<C, 2>(p, cols_dynamic(p, C::shape(2)), kColsStep<T>.narrow)});
-  const ExtShape s = C::shape(c.form);
+  c.form = pick_form(q, {ext_form_of<C, 0>(p, cols_dynamic(p, C::shape(0, has_bias(p))), 1.0),
+                         ext_form_of<C, 1>(p, cols_dynamic(p, C::shape(1, has_bias(p))), kColsStep<T>.narrow),
+                         ext_form_of<C, 2>(p, cols_dynamic(p, C::shape(2, has_bias(p))), kColsStep<T>.narrow),
+                         ext_form_of<C, 3>(p, cols_dynamic(p, C::shape(3, has_bias(p))), kColsStep<T>.narrow)});
+  const ExtShape s = C::shape(c.form, has_bias(p));
   c.blocks = s.blocks();
   c.sets = s.ks * s.nw;  // waves that store step sums
   c.parts = split ? grp : 1;
@@ -83,7 +86,7 @@ int32_t ext_launch_bwd(const ExtProblem& p, const void* Q, const void* K, const 
   if (rc != BOB_OK || p.Nk == 0) return rc;
   const ExtPlan c = ext_cols_plan<T, D>(p);
   const ExtArgs a = ext_args(p, c, p.B * p.Hkv, p.Nk, nullptr);
-  rc = ext_dispatch<ExtColsBwd<T, D>>(c.form, p, dim3(a.total, c.parts), cols_dynamic(p, ExtColsBwd<T, D>::shape(c.form)),
+  rc = ext_dispatch<ExtColsBwd<T, D>>(c.form, p, dim3(a.total, c.parts), cols_dynamic(p, ExtColsBwd<T, D>::shape(c.form, has_bias(p))),
                                       s, a, (const T*)Q, (const T*)K, (const T*)V, (const T*)dO, L, (const float*)Dv,
                                       (T*)dK, (T*)dV, parts, sums);
   if (rc != BOB_OK || c.parts == 1) return rc;

@@ -4,14 +4,13 @@
 namespace fb {
 
 template <typename T, int D> struct ExtFwd {
-  static constexpr ExtShape shape(int form) {
+  static constexpr ExtShape shape(int form, bool bias) {
     constexpr Shape w = Cfg<T, D>::kFwd;
     return form == 0   ? ExtShape{w.mr, w.nw, w.occ, w.st, 1}
-           : form == 1 ? ext_sets<T, D>(4, 2, 0, 16, w.occ)
-                       : ext_sets<T, D>(1, 2, 0, 16, 1);
+                       : ext_sets<T, D>(kFormWaves[form], 2, 0, 16, form == 2 ? 1 : w.occ);
   }
   template <int F, bool kBias> static __host__ constexpr auto kernel() {
-    constexpr ExtShape s = shape(F);
+    constexpr ExtShape s = shape(F, kBias);
     return &ext_fwd_kernel<T, D, s.mr, s.nw, s.occ, s.st, s.ks, kBias>;
   }
 };
@@ -20,7 +19,6 @@ template <typename T, int D> ExtPlan ext_fwd_plan(const ExtProblem& p) {
   ExtPlan c;
   const int64_t steps = ext_steps_bytes(p);
   const int grp = ext_group(p);
-  constexpr ExtShape narrow = ExtFwd<T, D>::shape(2);
   const Form f2 = ext_form_of<ExtFwd<T, D>, 2>(p, steps, kFwdStep<T>.narrow);
   if (grp > 1 && p.Nq <= 16 && f2.resident > 0)
     c.fold = ext_form_of<ExtFwd<T, D>, 2>(p, steps * std::min(grp, 16), 1.0).resident > 0;
@@ -32,12 +30,12 @@ template <typename T, int D> ExtPlan ext_fwd_plan(const ExtProblem& p) {
     const FormQuery q{device_cus(), heads, rows, tiles, p.causal != 0, block_us<T>(2, D), kFwdStep<T>, merge_us(1, D),
                       kRowMargin};
     c.form = pick_form(q, {ext_form_of<ExtFwd<T, D>, 0>(p, steps, 1.0),
-                           ext_form_of<ExtFwd<T, D>, 1>(p, steps, kFwdStep<T>.narrow), f2});
+                           ext_form_of<ExtFwd<T, D>, 1>(p, steps, kFwdStep<T>.narrow), f2,
+                           ext_form_of<ExtFwd<T, D>, 3>(p, steps, kFwdStep<T>.narrow)});
   }
-  const ExtShape s = ExtFwd<T, D>::shape(c.form);
+  const ExtShape s = ExtFwd<T, D>::shape(c.form, has_bias(p));
   c.blocks = s.blocks();
   c.sets = s.ks;
-  (void)narrow;
   return c;
 }
 

@@ -139,6 +139,14 @@ __device__ __forceinline__ void ext_stream(int n, Issue&& issue, Pro&& pro, Body
   }
 }
 
+// A tile's mode in a vector register: the wave indices are scalar, and a branch on a scalar
+// mode made the compiler merge the tile's body with the loop around it and spill hundreds of
+// registers (cross attention's column kernel at d = 128: 2.9 ms for 0.47 ms).
+__device__ __forceinline__ int vector_mode(int mode) {
+  asm volatile("" : "+v"(mode));
+  return mode;
+}
+
 // Run `index` of `count` equal runs over n tiles.
 struct ExtRun {
   int begin, end;
@@ -253,7 +261,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_fwd_kernel(
   ext_map_block(a, a.fold != 0 ? a.nRB : a.grp * a.nRB, true, rh, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
-  const int wl = KS == 1 ? wave_id() : wave_id() % NW;
+  const int wl = __builtin_amdgcn_readfirstlane(KS == 1 ? wave_id() : wave_id() % NW);
   const ExtRows<MR, NW, NW == 1> rw(a, rh, rb, wl, j);
   const int part = blockIdx.y;
   const int64_t kvoff = (int64_t)rw.kvh * a.Nk * D;
@@ -373,7 +381,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_fwd_kernel(
       },
       [&](int it, int st) {
         const int s0 = min(run.begin + it, rw.tiles - 1) * kBS;
-        const int mode = __builtin_amdgcn_readfirstlane(run.begin + it < run.end ? rw.mode(s0) : 0);
+        const int mode = vector_mode(run.begin + it < run.end ? rw.mode(s0) : 0);
         if (mode == 0) return;
         const T FB_LDS* Ks = (const T FB_LDS*)sm.lds[ks][st];
         const T FB_LDS* Vs = Ks + G::kTileElems;
@@ -533,7 +541,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
   ext_map_block(a, a.grp * a.nRB, true, rh, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
-  const int wl = KS == 1 ? wave_id() : wave_id() % NW;
+  const int wl = __builtin_amdgcn_readfirstlane(KS == 1 ? wave_id() : wave_id() % NW);
   const ExtRows<MR, NW, false> rw(a, rh, rb, wl, j);
   const int64_t kvoff = (int64_t)rw.kvh * a.Nk * D, qoff = rw.qrow * D;
 
@@ -586,7 +594,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
       },
       [&](int it, int st) {
         const int s0 = min(run.begin + it, rw.tiles - 1) * kBS;
-        const int mode = run.begin + it < run.end ? rw.mode(s0) : 0;
+        const int mode = vector_mode(run.begin + it < run.end ? rw.mode(s0) : 0);
         if (mode == 0) return;
         const T FB_LDS* Ks = (const T FB_LDS*)sm.lds[ks][st];
         const T FB_LDS* Vs = Ks + G::kTileElems;
@@ -791,16 +799,16 @@ __device__ __forceinline__ void ext_mask_cols(floatx4 (&x)[2][MC], int s0, int t
 struct StepSums {
   static constexpr int kStride = 36, kBufFloats = 16 * kStride;
   float* out;
-  int R, next, top, low;   // step of the carried window's first lane, range stored so far
-  bool carried, stored;
-  float carry, below, above;
+  int R;
+  float carry, below, above;  // the window below the last near tile's; the far sums
+  // The row starts at zero: the loop's first wait for its copies waits for these stores too.
   __device__ __forceinline__ void init(float* row, int r) {
     out = row;
     R = r;
-    carried = stored = false;
-    next = top = low = 0;
     carry = below = above = 0.f;
+    for (int x = lane_id(); x < 2 * R + 1; x += 64) out[x] = 0.f;
   }
+  // The sums of steps at .. at + 31, one a lane; every window is stored once.
   __device__ __forceinline__ void emit(int at, float v) {
     const int l = lane_id(), step = at + l;
     if (l < 32) {
@@ -811,14 +819,14 @@ struct StepSums {
       else
         out[step + R] = v;
     }
-    if (!stored) top = at + 31;
-    stored = true;
-    low = at;
   }
   template <int MC>
   __device__ __forceinline__ void far(const floatx4 (&x)[2][MC], int base, int side) {
-    if (carried) emit(base, carry);
-    carried = false;
+    // the first tile below the near ones: its upper window is what they left
+    if (side < 0 && base + 31 + 16 * MC > -R) {
+      emit(base, carry);
+      carry = 0.f;
+    }
     float sum = 0.f;
 #pragma unroll
     for (int mc = 0; mc < MC; ++mc) {
@@ -832,7 +840,10 @@ struct StepSums {
   }
   template <int MC>
   __device__ __forceinline__ void near(const floatx4 (&x)[2][MC], int base, float FB_LDS* buf) {
-    const int l = lane_id(), g = l >> 4, j = l & 15, cls = l & 31, half = l >> 5;
+    // made anew in every tile: kept over the loop, the addresses below cost 20 registers
+    int l = lane_id();
+    asm volatile("" : "+v"(l));
+    const int g = l >> 4, j = l & 15, cls = l & 31, half = l >> 5;
     // lane l sums the pairs whose step is l mod 32: those at base + cls (up) and at
     // base + cls - 32 (down); the two halves of the wave take eight keys each
     float up = 0.f, down = 0.f;
@@ -852,24 +863,18 @@ struct StepSums {
     }
     up += __shfl_xor(up, 32);
     down += __shfl_xor(down, 32);
-    emit(base, carried ? up + carry : up);
+    emit(base, up + carry);
     carry = down;
-    carried = true;
-    next = base - 32;
   }
-  __device__ __forceinline__ void finish() {
-    if (carried) emit(next, carry);
-    const int l = lane_id();
-    for (int x = l; x < 2 * R + 1; x += 64) {
-      const int step = x - R;
-      if (!stored || step > top || step < low) out[x] = 0.f;
-    }
+  // last: `base` of the last tile of the run (of any tile if the run is empty)
+  __device__ __forceinline__ void finish(int last) {
+    emit(last - 32, carry);
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) {
       below += __shfl_xor(below, m);
       above += __shfl_xor(above, m);
     }
-    if (l == 0) {
+    if (lane_id() == 0) {
       out[2 * R + 1] = below;
       out[2 * R + 2] = above;
     }
@@ -900,7 +905,8 @@ struct ExtColMem {
 __device__ __forceinline__ float* ext_step_row(float* sums, const ExtArgs& a, int qhead, int b, int rb, int sub,
                                                int subs, int waves) {
   const int batch = a.total / a.nRB / (a.H / a.grp);
-  const int64_t row = ((((int64_t)(qhead - b * a.H) * batch + b) * a.nRB + rb) * subs + sub) * waves + wave_id();
+  const int64_t row = ((((int64_t)(qhead - b * a.H) * batch + b) * a.nRB + rb) * subs + sub) * waves +
+                      __builtin_amdgcn_readfirstlane(wave_id());
   return sums + row * (2 * a.R + 3);
 }
 
@@ -973,7 +979,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_cols_kernel(
   ext_map_block(a, a.nRB, false, kv, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
-  const int wl = KS == 1 ? wave_id() : wave_id() % NW;
+  const int wl = __builtin_amdgcn_readfirstlane(KS == 1 ? wave_id() : wave_id() % NW);
   const ExtCols<MC, NW> cl(a, kv, rb, wl);
   const int64_t koff = (int64_t)kv * a.Nk * D;
 
@@ -1030,7 +1036,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_cols_kernel(
       },
       [&](int it, int st, int ts, auto&& prep_next) {
         const int s0 = cl.tile(flat(it)) * kBS;
-        const int mode = run.begin + it < run.end ? cl.mode(s0, a.causal != 0) : 0;
+        const int mode = vector_mode(run.begin + it < run.end ? cl.mode(s0, a.causal != 0) : 0);
         if (mode == 0) {
           prep_next();
           return;
@@ -1141,7 +1147,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_cols_kernel(
         prep_next();
       });
   if constexpr (kBias)
-    if (sums != nullptr) tab.finish();
+    if (sums != nullptr) tab.finish(cl.col0 - (cl.start + cl.tile(max(run.end - 1, 0)) * kBS));
   if constexpr (KS > 1) {
     static_assert(sizeof(sm.lds) >= merge_bytes<KS, NW, G::kNB, MC>(), "set merge buffer");
     merge_sets<KS, NW>(dk, ks, wl, (floatx4 FB_LDS*)&sm.lds[0][0][0]);
@@ -1181,7 +1187,8 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
   ext_map_block(a, a.grp * a.nRB, true, rh, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
-  const int wl = KS == 1 ? wave_id() : wave_id() % NW;
+  // scalar, one set at d = 64 takes 174 registers for 166 and loses its third wave per SIMD
+  const int wl = KS == 1 ? wave_id() : __builtin_amdgcn_readfirstlane(wave_id() % NW);
   const ExtRows<MR, NW, false> rw(a, rh, rb, wl, j);
   const int64_t kvoff = (int64_t)rw.kvh * a.Nk * D, qoff = rw.qrow * D;
 
@@ -1238,7 +1245,8 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
       },
       [&](int it, int st) {
         const int s0 = min(run.begin + it, rw.tiles - 1) * kBS;
-        const int mode = run.begin + it < run.end ? rw.mode(s0) : 0;
+        int mode = run.begin + it < run.end ? rw.mode(s0) : 0;
+        if constexpr (KS > 1) mode = vector_mode(mode);
         if (mode == 0 && (KS == 1 || it > 0)) return;
         const T FB_LDS* Ks = (const T FB_LDS*)sm.lds[ks][st];
         const T FB_LDS* Vs = Ks + G::kTileElems;
@@ -1496,7 +1504,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass2_kernel(
   ext_map_block(a, a.nRB, false, kv, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
-  const int wl = KS == 1 ? wave_id() : wave_id() % NW;
+  const int wl = __builtin_amdgcn_readfirstlane(KS == 1 ? wave_id() : wave_id() % NW);
   const ExtCols<MC, NW> cl(a, kv, rb, wl);
   const int64_t koff = (int64_t)kv * a.Nk * D;
 
@@ -1556,7 +1564,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass2_kernel(
       },
       [&](int it, int st, int ts, auto&& prep_next) {
         const int s0 = cl.tile(flat(it)) * kBS;
-        const int mode = run.begin + it < run.end ? cl.mode(s0, a.causal != 0) : 0;
+        const int mode = vector_mode(run.begin + it < run.end ? cl.mode(s0, a.causal != 0) : 0);
         if (mode == 0) {
           prep_next();
           return;
@@ -1708,7 +1716,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass2_kernel(
         }
       });
   if constexpr (kBias)
-    if (sums != nullptr) tab.finish();
+    if (sums != nullptr) tab.finish(cl.col0 - (cl.start + cl.tile(max(run.end - 1, 0)) * kBS));
   if constexpr (KS > 1) {
     static_assert(sizeof(sm.lds) >= merge_bytes<KS, NW, G::kNB, MC>(), "set merge buffer");
     merge_sets<KS, NW>(aK, ks, wl, (floatx4 FB_LDS*)&sm.lds[0][0][0]);
