@@ -107,8 +107,10 @@ struct ExtShape {
   constexpr bool built() const { return mr > 0; }
 };
 constexpr ExtShape kNotBuilt{0, 1, 1, 2, 1};
-// Forms: 0 whole blocks, the others blocks of this many waves of 16 rows in wave sets.
+// Forms: 0 whole blocks, 1 to 3 blocks of this many waves of 16 rows in wave sets, 4 whole
+// blocks of 32 rows a wave in two sets (with 16 rows a wave those are form 1's).
 constexpr int kFormWaves[4] = {0, 4, 1, 2};
+constexpr int kForms = 5;
 
 // Sets of `tensors` streamed tensors in blocks of nw waves of 16 rows, if more than one fits.
 template <typename T, int D> constexpr ExtShape ext_sets(int nw, int tensors, int extra, int max_waves, int occ) {
@@ -119,6 +121,14 @@ template <typename T, int D> constexpr ExtShape ext_sets(int nw, int tensors, in
   return s.ks > 1 ? ExtShape{1, nw, std::max({1, s.ks * nw / 4, std::min(occ, fit)}), 2, s.ks} : kNotBuilt;
 }
 
+// Whole blocks in two wave sets, two waves per SIMD; `beside` bytes of LDS beside the rings.
+template <typename T, int D> constexpr ExtShape ext_two_sets(const Shape& w, int tensors, int beside) {
+  const int ring = 2 * tensors * Geo<T, D>::kTileElems * (int)sizeof(T);
+  const bool fits = w.mr == 2 && w.nw == 4 && 2 * ring + beside <= 144 * 1024 &&
+                    2 * ring >= w.nw * Geo<T, D>::kNB * w.mr * 1024;
+  return fits ? ExtShape{w.mr, w.nw, 2, 2, 2} : kNotBuilt;
+}
+
 template <typename Kern, int F> Form ext_form_of(const ExtProblem& p, int64_t dynamic, double narrow) {
   auto form = [&](auto bias) -> Form {
     constexpr bool kBias = decltype(bias)::value;
@@ -126,7 +136,7 @@ template <typename Kern, int F> Form ext_form_of(const ExtProblem& p, int64_t dy
     if constexpr (s.built()) {
       if (F > 0 && static_lds<Kern::template kernel<F, kBias>()>() + dynamic > kMaxLds) return {};
       const int fit = resident_blocks<Kern::template kernel<F, kBias>()>(s.threads());
-      return {s.blocks(), s.ks, fit, s.threads(), 1, 0.0, F == 0 ? 1.0 : narrow};
+      return {s.blocks(), s.ks, fit, s.threads(), 1, 0.0, F == 0 || F == 4 ? 1.0 : narrow};
     }
     return {};
   };
@@ -154,10 +164,22 @@ int32_t ext_go(const ExtProblem& p, dim3 grid, int64_t dynamic, hipStream_t stre
 template <typename Kern, typename... Args>
 int32_t ext_dispatch(int form, const ExtProblem& p, dim3 grid, int64_t dynamic, hipStream_t stream, const ExtArgs& a,
                      Args... args) {
+  if (form == 4) return ext_go<Kern, 4>(p, grid, dynamic, stream, a, args...);
   if (form == 3) return ext_go<Kern, 3>(p, grid, dynamic, stream, a, args...);
   if (form == 2) return ext_go<Kern, 2>(p, grid, dynamic, stream, a, args...);
   if (form == 1) return ext_go<Kern, 1>(p, grid, dynamic, stream, a, args...);
   return ext_go<Kern, 0>(p, grid, dynamic, stream, a, args...);
+}
+
+// The form with the least estimated time (pick_form); dynamic(shape): its LDS of the bias.
+template <typename Kern, typename Dynamic>
+int ext_pick(const ExtProblem& p, const FormQuery& q, double narrow, Dynamic&& dynamic) {
+  const bool b = has_bias(p);
+  return pick_form(q, {ext_form_of<Kern, 0>(p, dynamic(Kern::shape(0, b)), 1.0),
+                       ext_form_of<Kern, 1>(p, dynamic(Kern::shape(1, b)), narrow),
+                       ext_form_of<Kern, 2>(p, dynamic(Kern::shape(2, b)), narrow),
+                       ext_form_of<Kern, 3>(p, dynamic(Kern::shape(3, b)), narrow),
+                       ext_form_of<Kern, 4>(p, dynamic(Kern::shape(4, b)), narrow)});
 }
 
 }  // namespace fb

@@ -141,7 +141,7 @@ static int64_t fwd_bytes(const ExtProblem& p, const ExtPlan& c) {
 // what ext_step_rows_kernel makes of them.
 struct ColBytes {
   int64_t parts = 0, rows = 0, sums = 0, mid = 0;  // rows: of step sums of one head
-  int S = 1;
+  int S = 0;  // rows a head that ext_step_rows_kernel makes of them; 0: it does not run
   int64_t all() const { return parts + sums + mid; }
 };
 static ColBytes col_bytes(const ExtProblem& p, const ExtPlan& c) {
@@ -151,7 +151,8 @@ static ColBytes col_bytes(const ExtProblem& p, const ExtPlan& c) {
     const int64_t blocks = (p.Nk + 16 * c.blocks - 1) / (16 * c.blocks);
     const int subs = c.parts > 1 ? c.parts / ext_group(p) : 1;
     b.rows = p.B * blocks * subs * c.sets;
-    b.S = (int)std::max<int64_t>(1, std::min<int64_t>(16, b.rows / 8));
+    // few rows go straight to the gather, for one launch less
+    b.S = b.rows <= 64 ? 0 : (int)std::min<int64_t>(16, b.rows / 8);
     auto pad = [](int64_t n) { return (n + 15) / 16 * 16; };
     b.sums = pad(b.rows * p.H * ext_width(p) * 4);
     b.mid = pad(b.S * p.H * ext_width(p) * 4);
@@ -187,10 +188,12 @@ static int32_t go_pass2(const ExtProblem& p, const void* Q, const void* K, const
 static int32_t gather_table(const ExtProblem& p, const ColBytes& b, const float* sums, float* mid, void* out,
                             hipStream_t s) {
   const int width = (int)ext_width(p);
-  (void)hipGetLastError();
-  hipLaunchKernelGGL(ext_step_rows_kernel, dim3(b.S, (unsigned)p.H), dim3(256), 0, s, sums, b.rows, width, mid);
   const ExtArgs a = ext_args(p, ExtPlan{}, 0, 0, nullptr);
-  hipLaunchKernelGGL(ext_buckets_kernel, dim3((unsigned)p.H), dim3(kGatherThreads), 0, s, (const float*)mid, b.S, a, out);
+  (void)hipGetLastError();
+  if (b.S > 0)
+    hipLaunchKernelGGL(ext_step_rows_kernel, dim3(b.S, (unsigned)p.H), dim3(256), 0, s, sums, b.rows, width, mid);
+  hipLaunchKernelGGL(ext_buckets_kernel, dim3((unsigned)p.H), dim3(kGatherThreads), 0, s, b.S > 0 ? (const float*)mid : sums,
+                     b.S > 0 ? b.S : (int)b.rows, a, out);
   return finish_launch();
 }
 

@@ -9,6 +9,7 @@ template <typename T, int D> struct ExtPass1 {
   static constexpr ExtShape shape(int form, bool bias) {
     constexpr Shape w = Cfg<T, D>::kP1;
     return form == 0   ? ExtShape{w.mr, w.nw, w.occ, w.st, 1}
+           : form == 4 ? ext_two_sets<T, D>(w, 4, 0)
                        : ext_sets<T, D>(kFormWaves[form], 4, 0, 8, w.occ);
   }
   template <int F, bool kBias> static __host__ constexpr auto kernel() {
@@ -21,6 +22,7 @@ template <typename T, int D> struct ExtPass2 {
   static constexpr ExtShape shape(int form, bool bias) {
     constexpr Shape w = Cfg<T, D>::kP2;
     return form == 0   ? ExtShape{w.mr, w.nw, w.occ, w.st, 1}
+           : form == 4 ? ext_two_sets<T, D>(w, 3, 2 * kExtra)
            : sizeof(T) == 2 && D == 32 && form == 1
                ? kNotBuilt  // three tensors of two 1 KB blocks do not deal out over four waves
                : ext_sets<T, D>(kFormWaves[form], 3, kExtra, 8, w.occ);
@@ -45,9 +47,7 @@ int32_t ext_launch_pass1(const ExtProblem& p, const void* Q, const void* K, cons
   const FormQuery q{device_cus(), p.B * p.H, p.Nq, std::max<int64_t>((p.Nk + kBS - 1) / kBS, 1), p.causal != 0,
                     block_us<T>(10, D), kP1Step<T>, merge_us(3, D), kRowMargin};
   ExtPlan c;
-  c.form = pick_form(q, {ext_form_of<R, 0>(p, steps, 1.0), ext_form_of<R, 1>(p, steps, kP1Step<T>.narrow),
-                         ext_form_of<R, 2>(p, steps, kP1Step<T>.narrow),
-                         ext_form_of<R, 3>(p, steps, kP1Step<T>.narrow)});
+  c.form = ext_pick<R>(p, q, kP1Step<T>.narrow, [&](const ExtShape&) { return steps; });
   c.blocks = R::shape(c.form, has_bias(p)).blocks();
   const ExtArgs a = ext_args(p, c, p.B * p.H, p.Nq, UT);
   return ext_dispatch<R>(c.form, p, dim3(a.total), steps, s, a, (const T*)Q, (const T*)K, (const T*)V, (const T*)O,
@@ -63,10 +63,7 @@ template <typename T, int D> ExtPlan ext_pass2_plan(const ExtProblem& p) {
   const int64_t tiles = std::max<int64_t>((p.Nq + kBS - 1) / kBS, 1) * (split ? 1 : grp);
   const FormQuery q{device_cus(), p.B * (split ? p.H : p.Hkv), std::max<int64_t>(p.Nk, 1), tiles, p.causal != 0,
                     block_us<T>(8, D), kP2Step<T>, merge_us(2, D), 1.0};
-  c.form = pick_form(q, {ext_form_of<C, 0>(p, pass2_dynamic(p, C::shape(0, has_bias(p))), 1.0),
-                         ext_form_of<C, 1>(p, pass2_dynamic(p, C::shape(1, has_bias(p))), kP2Step<T>.narrow),
-                         ext_form_of<C, 2>(p, pass2_dynamic(p, C::shape(2, has_bias(p))), kP2Step<T>.narrow),
-                         ext_form_of<C, 3>(p, pass2_dynamic(p, C::shape(3, has_bias(p))), kP2Step<T>.narrow)});
+  c.form = ext_pick<C>(p, q, kP2Step<T>.narrow, [&](const ExtShape& s) { return pass2_dynamic(p, s); });
   const ExtShape s = C::shape(c.form, has_bias(p));
   c.blocks = s.blocks();
   c.sets = s.ks * s.nw;

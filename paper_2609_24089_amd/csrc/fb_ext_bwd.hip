@@ -7,6 +7,7 @@ template <typename T, int D> struct ExtRowsBwd {
   static constexpr ExtShape shape(int form, bool bias) {
     constexpr Shape w = Cfg<T, D>::kRows;
     return form == 0   ? ExtShape{w.mr, w.nw, w.occ, w.st, 1}
+           : form == 4 ? ext_two_sets<T, D>(w, 2, 0)
                        : ext_sets<T, D>(kFormWaves[form], 2, 0, 16, w.occ);
   }
   template <int F, bool kBias> static __host__ constexpr auto kernel() {
@@ -24,11 +25,12 @@ template <typename T, int D> struct ExtColsBwd {
     // B4 H12 N4096 dense, 462 for 485 causal (first backward)
     constexpr bool kThree = std::is_same_v<T, bf16> && D == 64;
     return form == 0   ? ExtShape{w.mr, w.nw, bias && kThree ? 3 : w.occ, w.st, 1}
+           : form == 4 ? ext_two_sets<T, D>(w, 2, 2 * kExtra + (w.kl ? 4 * Geo<T, D>::kTileElems * (int)sizeof(T) : 0))
                        : ext_sets<T, D>(kFormWaves[form], 2, kExtra, waves, w.occ);
   }
   template <int F, bool kBias> static __host__ constexpr auto kernel() {
     constexpr ExtShape s = shape(F, kBias);
-    return &ext_bwd_cols_kernel<T, D, s.mr, s.nw, s.occ, s.ks, F == 0 && Cfg<T, D>::kCols.kl != 0, kBias>;
+    return &ext_bwd_cols_kernel<T, D, s.mr, s.nw, s.occ, s.ks, (F == 0 || F == 4) && Cfg<T, D>::kCols.kl != 0, kBias>;
   }
 };
 
@@ -42,10 +44,7 @@ template <typename T, int D> ExtPlan ext_rows_plan(const ExtProblem& p) {
   const FormQuery q{device_cus(), p.B * p.H, p.Nq, std::max<int64_t>((p.Nk + kBS - 1) / kBS, 1), p.causal != 0,
                     block_us<T>(3, D), kRowsStep<T>, merge_us(1, D), kRowMargin};
   ExtPlan c;
-  c.form = pick_form(q, {ext_form_of<ExtRowsBwd<T, D>, 0>(p, steps, 1.0),
-                         ext_form_of<ExtRowsBwd<T, D>, 1>(p, steps, kRowsStep<T>.narrow),
-                         ext_form_of<ExtRowsBwd<T, D>, 2>(p, steps, kRowsStep<T>.narrow),
-                         ext_form_of<ExtRowsBwd<T, D>, 3>(p, steps, kRowsStep<T>.narrow)});
+  c.form = ext_pick<ExtRowsBwd<T, D>>(p, q, kRowsStep<T>.narrow, [&](const ExtShape&) { return steps; });
   const ExtShape s = ExtRowsBwd<T, D>::shape(c.form, has_bias(p));
   c.blocks = s.blocks();
   c.sets = s.ks;
@@ -61,10 +60,7 @@ template <typename T, int D> ExtPlan ext_cols_plan(const ExtProblem& p) {
   const int64_t tiles = std::max<int64_t>((p.Nq + kBS - 1) / kBS, 1) * (split ? 1 : grp);
   const FormQuery q{device_cus(), p.B * (split ? p.H : p.Hkv), std::max<int64_t>(p.Nk, 1), tiles, p.causal != 0,
                     block_us<T>(4, D), kColsStep<T>, merge_us(2, D), 1.0};
-  c.form = pick_form(q, {ext_form_of<C, 0>(p, cols_dynamic(p, C::shape(0, has_bias(p))), 1.0),
-                         ext_form_of<C, 1>(p, cols_dynamic(p, C::shape(1, has_bias(p))), kColsStep<T>.narrow),
-                         ext_form_of<C, 2>(p, cols_dynamic(p, C::shape(2, has_bias(p))), kColsStep<T>.narrow),
-                         ext_form_of<C, 3>(p, cols_dynamic(p, C::shape(3, has_bias(p))), kColsStep<T>.narrow)});
+  c.form = ext_pick<C>(p, q, kColsStep<T>.narrow, [&](const ExtShape& s) { return cols_dynamic(p, s); });
   const ExtShape s = C::shape(c.form, has_bias(p));
   c.blocks = s.blocks();
   c.sets = s.ks * s.nw;  // waves that store step sums

@@ -7,6 +7,7 @@ template <typename T, int D> struct ExtFwd {
   static constexpr ExtShape shape(int form, bool bias) {
     constexpr Shape w = Cfg<T, D>::kFwd;
     return form == 0   ? ExtShape{w.mr, w.nw, w.occ, w.st, 1}
+           : form == 4 ? ext_two_sets<T, D>(w, 2, 0)
                        : ext_sets<T, D>(kFormWaves[form], 2, 0, 16, form == 2 ? 1 : w.occ);
   }
   template <int F, bool kBias> static __host__ constexpr auto kernel() {
@@ -29,9 +30,7 @@ template <typename T, int D> ExtPlan ext_fwd_plan(const ExtProblem& p) {
   } else {
     const FormQuery q{device_cus(), heads, rows, tiles, p.causal != 0, block_us<T>(2, D), kFwdStep<T>, merge_us(1, D),
                       kRowMargin};
-    c.form = pick_form(q, {ext_form_of<ExtFwd<T, D>, 0>(p, steps, 1.0),
-                           ext_form_of<ExtFwd<T, D>, 1>(p, steps, kFwdStep<T>.narrow), f2,
-                           ext_form_of<ExtFwd<T, D>, 3>(p, steps, kFwdStep<T>.narrow)});
+    c.form = ext_pick<ExtFwd<T, D>>(p, q, kFwdStep<T>.narrow, [&](const ExtShape&) { return steps; });
   }
   const ExtShape s = ExtFwd<T, D>::shape(c.form, has_bias(p));
   c.blocks = s.blocks();

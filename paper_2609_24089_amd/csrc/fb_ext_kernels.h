@@ -107,35 +107,50 @@ __device__ __forceinline__ int ext_side(int lo, int hi, int R) { return hi <= -R
 // ---------------------------------------------------------------------------
 template <int NSTAGE, int LT, bool kBarrier, class Issue, class Pro, class Body>
 __device__ __forceinline__ void ext_stream(int n, Issue&& issue, Pro&& pro, Body&& body) {
-#pragma unroll
-  for (int st = 0; st < NSTAGE - 1; ++st)
-    if (st < n) issue(st, st);
-  pro();
-  wait_copies<true>();
-  __syncthreads();
-  auto step = [&](int k, auto cur) {
-    constexpr int kCur = decltype(cur)::value;
-    constexpr int kNext = kCur == 0 ? NSTAGE - 1 : kCur - 1;
-    const int nx = k + NSTAGE - 1;
-    if (nx < n) issue(nx, kNext);
-    body(k, kCur);
-    // without a barrier the wave's own reads of this stage have to be back before the
-    // next copy into it is issued (lgkmcnt(0), the other counters at their maxima)
-    if constexpr (!kBarrier) __builtin_amdgcn_s_waitcnt(0xc07f);
-    if (NSTAGE > 2 && nx < n)
-      wait_vm<(NSTAGE - 2) * LT>();
-    else
+  static_assert(NSTAGE == 2 || (NSTAGE == 4 && !kBarrier), "ring depth");
+  if constexpr (kBarrier) {
+    if (n > 0) issue(0, 0);
+    pro();
+    wait_copies<true>();
+    __syncthreads();
+    auto step = [&](int k, auto cur) {
+      constexpr int kCur = decltype(cur)::value;
+      if (k + 1 < n) issue(k + 1, 1 - kCur);
+      body(k, kCur);
       wait_copies<true>();
-    if constexpr (kBarrier) __syncthreads();
-  };
-  static_assert(NSTAGE >= 2 && NSTAGE <= 4, "ring depth");
-  for (int k = 0; k < n; k += NSTAGE) {
-    step(k, std::integral_constant<int, 0>{});
-    if (k + 1 < n) step(k + 1, std::integral_constant<int, 1>{});
-    if constexpr (NSTAGE > 2)
-      if (k + 2 < n) step(k + 2, std::integral_constant<int, 2>{});
-    if constexpr (NSTAGE > 3)
-      if (k + 3 < n) step(k + 3, std::integral_constant<int, 3>{});
+      __syncthreads();
+    };
+    for (int k = 0; k < n; k += 2) {
+      step(k, std::integral_constant<int, 0>{});
+      if (k + 1 < n) step(k + 1, std::integral_constant<int, 1>{});
+    }
+  } else {
+    // the whole ring is in flight at the start, and a stage is filled again as soon as its
+    // tile is done: the wave's own reads of it have to be back before (lgkmcnt(0), the other
+    // counters at their maxima)
+#pragma unroll
+    for (int st = 0; st < NSTAGE; ++st)
+      if (st < n) issue(st, st);
+    pro();
+    __syncthreads();
+    auto step = [&](int k, auto cur) {
+      constexpr int kCur = decltype(cur)::value;
+      if (k + NSTAGE - 1 < n)
+        wait_vm<(NSTAGE - 1) * LT>();
+      else
+        wait_copies<true>();
+      body(k, kCur);
+      __builtin_amdgcn_s_waitcnt(0xc07f);
+      if (k + NSTAGE < n) issue(k + NSTAGE, kCur);
+    };
+    for (int k = 0; k < n; k += NSTAGE) {
+      step(k, std::integral_constant<int, 0>{});
+      if (k + 1 < n) step(k + 1, std::integral_constant<int, 1>{});
+      if constexpr (NSTAGE > 2) {
+        if (k + 2 < n) step(k + 2, std::integral_constant<int, 2>{});
+        if (k + 3 < n) step(k + 3, std::integral_constant<int, 3>{});
+      }
+    }
   }
 }
 
@@ -797,15 +812,16 @@ __device__ __forceinline__ void ext_mask_cols(floatx4 (&x)[2][MC], int s0, int t
 // key and first query.  buf: kBufFloats floats of LDS of this wave.  out: 2 R + 3 sums:
 // steps -R .. R, then all below -R, then all above R.
 struct StepSums {
-  static constexpr int kStride = 36, kBufFloats = 16 * kStride;
+  static constexpr int kStride = 76, kBufFloats = 4 * kStride;
   float* out;
   int R;
   float carry, below, above;  // the window below the last near tile's; the far sums
   // The row starts at zero: the loop's first wait for its copies waits for these stores too.
-  __device__ __forceinline__ void init(float* row, int r) {
+  __device__ __forceinline__ void init(float* row, int r, float FB_LDS* buf) {
     out = row;
     R = r;
     carry = below = above = 0.f;
+    for (int x = lane_id(); x < kBufFloats; x += 64) buf[x] = 0.f;  // columns that no tile writes stay so
     for (int x = lane_id(); x < 2 * R + 1; x += 64) out[x] = 0.f;
   }
   // The sums of steps at .. at + 31, one a lane; every window is stored once.
@@ -838,33 +854,40 @@ struct StepSums {
     else
       above += sum;
   }
+  // The sum of a 16x16 block x_r (query 4 g + r, key j) along its diagonals for one lane
+  // group g: same[c] over key - r = c, next[c] over key - r = c - 16.
+  static __device__ __forceinline__ void diagonals(floatx4 x, float& same, float& next) {
+    same = shifted<0x101>(shifted<0x101>(shifted<0x101>(x[3]) + x[2]) + x[1]) + x[0];  // lane c takes lane c + 1
+    next = shifted<0x11f>(x[1]) + (shifted<0x11e>(x[2]) + shifted<0x11d>(x[3]));       // lane c takes c - 15, - 14, - 13
+  }
+  template <int kCtrl> static __device__ __forceinline__ float shifted(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kCtrl, 0xf, 0xf, true));
+  }
+  // A tile with steps of their own sums.  Blocks of equal key - query are added first, each
+  // is summed along its diagonals inside its lane group by shifts in the row of 16 lanes,
+  // and the four groups, whose steps lie 4 apart, meet in LDS: row g of the buffer holds its
+  // 64 sums 4 g to the left, so that lane l finds step l - 32 in one column.  (Summing the
+  // diagonals from a whole tile in LDS, 16 reads and 110 vector instructions for 4 and 35,
+  // took B8 H12 N512 d64, all of it near, 41 us for the column kernel.)
   template <int MC>
   __device__ __forceinline__ void near(const floatx4 (&x)[2][MC], int base, float FB_LDS* buf) {
-    // made anew in every tile: kept over the loop, the addresses below cost 20 registers
     int l = lane_id();
-    asm volatile("" : "+v"(l));
-    const int g = l >> 4, j = l & 15, cls = l & 31, half = l >> 5;
-    // lane l sums the pairs whose step is l mod 32: those at base + cls (up) and at
-    // base + cls - 32 (down); the two halves of the wave take eight keys each
-    float up = 0.f, down = 0.f;
-#pragma unroll
-    for (int mc = 0; mc < MC; ++mc) {
-#pragma unroll
-      for (int sb = 0; sb < 2; ++sb) *(floatx4 FB_LDS*)(buf + kStride * j + 16 * sb + 4 * g) = x[sb][mc];
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int k = 8 * half + u, key = 16 * mc + k;
-        const float v = buf[kStride * k + ((key - cls) & 31)];
-        if (key >= cls)
-          up += v;
-        else
-          down += v;
-      }
-    }
-    up += __shfl_xor(up, 32);
-    down += __shfl_xor(down, 32);
-    emit(base, up + carry);
-    carry = down;
+    asm volatile("" : "+v"(l));  // the addresses are made anew in every tile, not kept
+    float a0, n0, am, nm, a1 = 0.f, n1 = 0.f;
+    diagonals(MC == 2 ? x[0][0] + x[1][MC - 1] : x[0][0], a0, n0);
+    diagonals(x[1][0], am, nm);
+    if constexpr (MC == 2) diagonals(x[0][1], a1, n1);
+    float FB_LDS* const to = buf + (kStride - 4) * (l >> 4) + (l & 15) + 12;  // row g, 4 g to the left
+    to[0] = nm;
+    to[16] = am + n0;
+    to[32] = a0 + n1;
+    if constexpr (MC == 2) to[48] = a1;
+    const float FB_LDS* const from = buf + l + 12;
+    const float sum = (from[0] + from[kStride]) + (from[2 * kStride] + from[3 * kStride]);
+    // lanes 32 .. 63: the upper window, which no later tile meets
+    const float other = __shfl_xor(sum, 32);
+    emit(base, (l < 32 ? other : sum) + carry);
+    carry = sum;
   }
   // last: `base` of the last tile of the run (of any tile if the run is empty)
   __device__ __forceinline__ void finish(int last) {
@@ -893,7 +916,7 @@ struct ExtColMem {
     if constexpr (kBias) {
       const int n = (ext_steps(a) + 3) & ~3;
       dirs = steps + n;
-      buf = steps + (kDir ? 2 : 1) * n + wave_id() * StepSums::kBufFloats;
+      buf = steps + (kDir ? 2 : 1) * n + __builtin_amdgcn_readfirstlane(wave_id()) * StepSums::kBufFloats;
       ext_fill_steps<true>(a, a.table, head, 1, steps, KS * NW * 64);
       if constexpr (kDir) ext_fill_steps<false>(a, a.dir, head, 1, dirs, KS * NW * 64);
     }
@@ -1000,7 +1023,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_cols_kernel(
   const ExtColMem<kBias, KS, NW, false> mem(steps_mem, a, cl.hq - cl.b * a.H);
   StepSums tab;
   if constexpr (kBias)
-    if (sums != nullptr) tab.init(ext_step_row(sums, a, cl.hq, cl.b, rb, cl.sub, cl.subs, KS * NW), a.R);
+    if (sums != nullptr) tab.init(ext_step_row(sums, a, cl.hq, cl.b, rb, cl.sub, cl.subs, KS * NW), a.R, mem.buf);
   floatx4 dk[G::kNB][MC], dv[G::kNB][MC];
 #pragma unroll
   for (int nb = 0; nb < G::kNB; ++nb)
@@ -1520,7 +1543,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass2_kernel(
   const ExtColMem<kBias, KS, NW, true> mem(steps_mem, a, cl.hq - cl.b * a.H);
   StepSums tab;
   if constexpr (kBias)
-    if (sums != nullptr) tab.init(ext_step_row(sums, a, cl.hq, cl.b, rb, cl.sub, cl.subs, KS * NW), a.R);
+    if (sums != nullptr) tab.init(ext_step_row(sums, a, cl.hq, cl.b, rb, cl.sub, cl.subs, KS * NW), a.R, mem.buf);
   floatx4 aK[G::kNB][MC], aV[G::kNB][MC];
 #pragma unroll
   for (int nb = 0; nb < G::kNB; ++nb)
