@@ -151,8 +151,8 @@ int32_t ext_go(const ExtProblem& p, dim3 grid, int64_t dynamic, hipStream_t stre
     constexpr ExtShape s = Kern::shape(F, kBias);
     if constexpr (s.built()) {
       constexpr auto kernel = Kern::template kernel<F, kBias>();
-      if (p.causal != 0 && grid.y == 1)
-        a.resident = balanced_order(a.total, resident_blocks<kernel>(s.threads()), device_cus());
+      a.fit = resident_blocks<kernel>(s.threads());
+      if (p.causal != 0 && grid.y == 1) a.resident = balanced_order(a.total, a.fit, device_cus());
       (void)hipGetLastError();
       hipLaunchKernelGGL(kernel, grid, dim3(s.threads()), (unsigned)(kBias ? dynamic : 0), stream, a, args...);
       return finish_launch();

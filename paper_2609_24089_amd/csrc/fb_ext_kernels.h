@@ -44,6 +44,7 @@ struct ExtArgs {
   float scale;
   int nparts;
   int resident;        // of balanced_order(): causal grids of a few rounds
+  int fit;             // workgroups of the kernel that fit a compute unit
   const int32_t* q_lens;    // [B] or null: every row is valid
   const int32_t* kv_lens;
   const int32_t* q_starts;  // [B] or null: 0
@@ -221,26 +222,55 @@ struct ExtRows {
   __device__ __forceinline__ int mode(int s0) const { return s0 > hi ? 0 : s0 + kBS - 1 <= lo ? 1 : 2; }
 };
 
+// The batch entry with the `rank`-th largest length (equal ones in order), 2 to 64 entries:
+// each lane ranks one.
+__device__ __forceinline__ int entry_of_rank(const int32_t* lens, int entries, int limit, int rank) {
+  const int l = lane_id();
+  const int n = l < entries ? min(max(lens[l], 0), limit) : -1;
+  int above = 0;
+  for (int q = 0; q < entries; ++q) {
+    const int other = __builtin_amdgcn_readlane(n, q);
+    above += other > n || (other == n && q < l) ? 1 : 0;
+  }
+  return __builtin_ctzll(__builtin_amdgcn_ballot_w64(l < entries && above == rank));
+}
+
 // Which block a workgroup runs.  As map_block, one head's blocks stay on one XCD, whose L2
 // its key/value head's tensors then pass once; but units of heads that share a key/value
 // head go round the XCDs one by one where their number allows it, so that the entries of a
-// ragged batch spread over all of them: in map_block's runs of consecutive heads an XCD
-// got the longest entry's heads and another the shortest's (B8 H16 Nq512 Nk2048 d64, half to
-// full lengths, forward: 46 us in runs).  Causal grids of a few rounds run in
-// map_block_causal's order.  `per`: blocks of one unit.
-__device__ __forceinline__ void ext_map_block(const ExtArgs& a, int per, bool last_heavy, int& head, int& rb) {
+// ragged batch spread over all of them (in map_block's runs of consecutive heads an XCD got
+// the longest entry's heads and another the shortest's: 3 to 10% slower on such batches).
+// `lens`: the streamed side's lengths, or null.  With them the longest entries' blocks start
+// first, and in the rounds that become resident together each XCD deals them to its CUs in
+// alternating direction, as map_block_causal does: a CU gets a long block and a short one.
+// Causal grids of a few rounds run in map_block_causal's order.  `per`: blocks of one unit.
+__device__ __forceinline__ void ext_map_block(const ExtArgs& a, int per, bool last_heavy, const int32_t* lens, int limit,
+                                              int& head, int& rb) {
   if (a.resident > 0) {
     map_block_causal(a.nRB, a.total, a.resident, last_heavy, head, rb);
     return;
   }
-  const int units = a.total / per;
+  const int units = a.total / per, entry_units = a.H / a.grp, entries = units / entry_units;
   if (units % kXCDs != 0) {
     map_block(a.nRB, a.total, head, rb, last_heavy && a.causal != 0);
     return;
   }
-  const int xcd = blockIdx.x % kXCDs, i = blockIdx.x / kXCDs;
-  const int u = i / per, at = i - u * per, h = at / a.nRB;
-  head = (u * kXCDs + xcd) * (per / a.nRB) + h;
+  const int xcd = blockIdx.x % kXCDs;
+  int i = blockIdx.x / kXCDs;
+  const bool ranked = lens != nullptr && entries > 1 && entries <= 64;
+  if (ranked) {
+    const int round = i / kCUsPerXCD, first = round * kCUsPerXCD;
+    const int m = min(kCUsPerXCD, a.total / kXCDs - first);
+    if ((round & 1) != 0 && round < a.fit) i = first + m - 1 - (i - first);
+  }
+  int u = i / per;
+  const int at = i - u * per, h = at / a.nRB;
+  u = u * kXCDs + xcd;
+  if (ranked) {
+    const int rank = u / entry_units;
+    u += (entry_of_rank(lens, entries, limit, rank) - rank) * entry_units;
+  }
+  head = u * (per / a.nRB) + h;
   rb = at - h * a.nRB;
   if (last_heavy && a.causal != 0) rb = a.nRB - 1 - rb;
 }
@@ -273,7 +303,8 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_fwd_kernel(
   float FB_LDS* const steps = (float FB_LDS*)steps_mem;
 
   int rh, rb;
-  ext_map_block(a, a.fold != 0 ? a.nRB : a.grp * a.nRB, true, rh, rb);
+  // a few rows a head: every workgroup is resident, whatever the order
+  ext_map_block(a, a.fold != 0 ? a.nRB : a.grp * a.nRB, true, NW == 1 ? nullptr : a.kv_lens, a.Nk, rh, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
   const int wl = __builtin_amdgcn_readfirstlane(KS == 1 ? wave_id() : wave_id() % NW);
@@ -553,7 +584,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
   float FB_LDS* const steps = (float FB_LDS*)steps_mem;
 
   int rh, rb;
-  ext_map_block(a, a.grp * a.nRB, true, rh, rb);
+  ext_map_block(a, a.grp * a.nRB, true, a.kv_lens, a.Nk, rh, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
   const int wl = __builtin_amdgcn_readfirstlane(KS == 1 ? wave_id() : wave_id() % NW);
@@ -999,7 +1030,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_cols_kernel(
   extern __shared__ float steps_mem[];
 
   int kv, rb;
-  ext_map_block(a, a.nRB, false, kv, rb);
+  ext_map_block(a, a.nRB, false, a.q_lens, a.Nq, kv, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
   const int wl = __builtin_amdgcn_readfirstlane(KS == 1 ? wave_id() : wave_id() % NW);
@@ -1207,7 +1238,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
   float FB_LDS* const dirs = steps + (kBias ? (ext_steps(a) + 3) & ~3 : 0);
 
   int rh, rb;
-  ext_map_block(a, a.grp * a.nRB, true, rh, rb);
+  ext_map_block(a, a.grp * a.nRB, true, a.kv_lens, a.Nk, rh, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
   // scalar, one set at d = 64 takes 174 registers for 166 and loses its third wave per SIMD
@@ -1524,7 +1555,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass2_kernel(
   extern __shared__ float steps_mem[];
 
   int kv, rb;
-  ext_map_block(a, a.nRB, false, kv, rb);
+  ext_map_block(a, a.nRB, false, a.q_lens, a.Nq, kv, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
   const int wl = __builtin_amdgcn_readfirstlane(KS == 1 ? wave_id() : wave_id() % NW);
