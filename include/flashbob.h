@@ -398,7 +398,8 @@ int32_t attn_ext_pass1_rows(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, in
                             float scale, int32_t causal, const attn_ext* ext, const void* Q, const void* K,
                             const void* V, const void* O, const void* dO, const void* gdQ, const void* gdK,
                             const void* gdV, const void* gdT, const float* L, const float* D, const void* dQ, void* Qt,
-                            void* dOt, float* alpha, float* E, void* stream);
+                            void* dOt, float* alpha, float* E, void* workspace, int64_t workspace_bytes,
+                            void* stream);
 
 /* BoB Pass 2, after Pass 1.  In: Q, K, V, dO, gdQ, gdK, gdV, gdT (may be NULL: 0), L, D, alpha, E.
  * Out: Kt, Vt and, with a table, Tt (may be NULL: not wanted). */
@@ -413,6 +414,8 @@ int64_t attn_ext_fwd_workspace_bytes(int32_t dtype, int64_t B, int64_t H, int64_
                                      int64_t d, int32_t causal, const attn_ext* ext);
 int64_t attn_ext_bwd_workspace_bytes(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,
                                      int64_t d, int32_t causal, const attn_ext* ext);
+int64_t attn_ext_pass1_workspace_bytes(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,
+                                       int64_t d, int32_t causal, const attn_ext* ext);
 int64_t attn_ext_pass2_workspace_bytes(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,
                                        int64_t d, int32_t causal, const attn_ext* ext);
 

@@ -25,7 +25,7 @@ inline int64_t ext_width(const ExtProblem& p) { return 2 * (int64_t)p.x.max_dist
 // How a launch runs: blocks of 16 `blocks` stationary rows, `sets` wave sets, `parts`
 // workgroups a block; folded rows (row kernels).
 struct ExtPlan {
-  int form = 0, blocks = 4, sets = 1, parts = 1;
+  int form = 0, blocks = 4, sets = 1, waves = 4, parts = 1;
   bool fold = false;
 };
 
@@ -63,16 +63,18 @@ template <typename T, int D> ExtPlan ext_fwd_plan(const ExtProblem& p);
 template <typename T, int D>
 int32_t ext_launch_fwd(const ExtProblem& p, const void* Q, const void* K, const void* V, void* O, float* L, float* ws,
                        hipStream_t s);
+template <typename T, int D> ExtPlan ext_rows_plan(const ExtProblem& p);
 template <typename T, int D> ExtPlan ext_cols_plan(const ExtProblem& p);
 template <typename T, int D>
 int32_t ext_launch_bwd(const ExtProblem& p, const void* Q, const void* K, const void* V, const void* O, const void* dO,
-                       const float* L, void* dQ, void* dK, void* dV, float* Dv, float* parts, float* sums,
+                       const float* L, void* dQ, void* dK, void* dV, float* Dv, float* row_parts, float* parts, float* sums,
                        hipStream_t s);
+template <typename T, int D> ExtPlan ext_pass1_plan(const ExtProblem& p);
 template <typename T, int D>
 int32_t ext_launch_pass1(const ExtProblem& p, const void* Q, const void* K, const void* V, const void* O,
                          const void* dO, const void* UQ, const void* UK, const void* UV, const void* UT,
                          const float* L, const float* Dv, const void* dQ, void* Qt, void* dOt, float* alpha, float* E,
-                         hipStream_t s);
+                         float* parts, hipStream_t s);
 template <typename T, int D> ExtPlan ext_pass2_plan(const ExtProblem& p);
 template <typename T, int D>
 int32_t ext_launch_pass2(const ExtProblem& p, const void* Q, const void* K, const void* V, const void* dO,
@@ -171,15 +173,55 @@ int32_t ext_dispatch(int form, const ExtProblem& p, dim3 grid, int64_t dynamic, 
   return ext_go<Kern, 0>(p, grid, dynamic, stream, a, args...);
 }
 
-// The form with the least estimated time (pick_form); dynamic(shape): its LDS of the bias.
+// The form and the parts with the least estimated time.  dynamic(shape): its LDS of the bias;
+// base: parts that a block has in any case (1, or a group's query heads); others are multiples
+// of `unit`; part_bytes: of fp32 sums that a part of all blocks stores.  A part costs what its
+// sums take to write and to read back at 4 TB/s, all of them the joining launch; only grids
+// of at most two workgroups a compute unit are offered, of four tiles a set or more.  Measured, one part -> chosen: see
+// the launchers.
+constexpr double kJoinUs = 6.0;
 template <typename Kern, typename Dynamic>
-int ext_pick(const ExtProblem& p, const FormQuery& q, double narrow, Dynamic&& dynamic) {
+void ext_pick(const ExtProblem& p, const FormQuery& q, double narrow, Dynamic&& dynamic, int only, int base,
+              int unit, int64_t part_bytes, ExtPlan* c) {
   const bool b = has_bias(p);
-  return pick_form(q, {ext_form_of<Kern, 0>(p, dynamic(Kern::shape(0, b)), 1.0),
-                       ext_form_of<Kern, 1>(p, dynamic(Kern::shape(1, b)), narrow),
-                       ext_form_of<Kern, 2>(p, dynamic(Kern::shape(2, b)), narrow),
-                       ext_form_of<Kern, 3>(p, dynamic(Kern::shape(3, b)), narrow),
-                       ext_form_of<Kern, 4>(p, dynamic(Kern::shape(4, b)), narrow)});
+  const Form forms[kForms] = {ext_form_of<Kern, 0>(p, dynamic(Kern::shape(0, b)), 1.0),
+                              ext_form_of<Kern, 1>(p, dynamic(Kern::shape(1, b)), narrow),
+                              ext_form_of<Kern, 2>(p, dynamic(Kern::shape(2, b)), narrow),
+                              ext_form_of<Kern, 3>(p, dynamic(Kern::shape(3, b)), narrow),
+                              ext_form_of<Kern, 4>(p, dynamic(Kern::shape(4, b)), narrow)};
+  double least = 0;
+  bool found = false, fills = false;
+  c->form = std::max(only, 0);  // an unknown device
+  c->parts = base;
+  for (int i = 0; i < kForms && q.cus > 0; ++i) {
+    Form f = forms[i];
+    if (f.resident == 0 || (only >= 0 && i != only)) continue;
+    const int64_t blocks = q.heads * ((q.N + 16 * f.blocks - 1) / (16 * f.blocks));
+    if (i == 0) fills = f.resident > 1 && blocks * base > q.cus * f.resident;
+    if (i > 0 && only < 0 && fills) continue;
+    for (int m = 0; m <= 16; m = m == 0 ? 1 : 2 * m) {
+      f.parts = m == 0 ? base : unit * m;
+      if (m > 0 && f.parts <= base) continue;
+      const int64_t total = blocks * f.parts;
+      if (m > 0 && (total > 2 * q.cus || q.tiles < (int64_t)4 * f.sets * f.parts)) break;
+      if (total > INT32_MAX / 16 || total * f.threads > (int64_t)UINT32_MAX) continue;
+      double t = form_us(q, f) * (f.parts > base ? 1.08 : i > 0 ? q.margin : 1.0);
+      if (f.parts > 1) t += kJoinUs + 2.0 * f.parts * (double)part_bytes / 4.0e6;
+      if (!found || t < least) {
+        least = t;
+        found = true;
+        c->form = i;
+        c->parts = f.parts;
+      }
+    }
+  }
+  const ExtShape s = Kern::shape(c->form, b);
+  c->blocks = s.blocks();
+  c->sets = s.ks;
+  c->waves = s.ks * s.nw;
 }
+
+// A causal problem whose queries start its keys: the blocks' work grows to the diagonal.
+inline bool triangular(const ExtProblem& p) { return p.causal != 0 && p.Nq == p.Nk; }
 
 }  // namespace fb

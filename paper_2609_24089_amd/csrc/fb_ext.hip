@@ -133,10 +133,14 @@ static bool ext_ptrs(int64_t n, std::initializer_list<const void*> ptrs) {
   return check_ptrs(ptrs) == BOB_OK;
 }
 
-// Workspace of the forward: the parts' sums, references and weights.
-static int64_t fwd_bytes(const ExtProblem& p, const ExtPlan& c) {
-  return c.parts > 1 ? c.parts * p.B * p.H * p.Nq * (p.d + 2) * 4 : 0;
+// Workspace of a row kernel: `floats` of each part and row (the forward's sums, reference and
+// weight; the first backward's sums and D; Pass 1's three sums and four scalars).
+static int64_t row_bytes(const ExtProblem& p, const ExtPlan& c, int64_t floats) {
+  return c.parts > 1 ? (c.parts * p.B * p.H * p.Nq * floats * 4 + 15) / 16 * 16 : 0;
 }
+static int64_t fwd_bytes(const ExtProblem& p, const ExtPlan& c) { return row_bytes(p, c, p.d + 2); }
+static int64_t rows_bytes(const ExtProblem& p, const ExtPlan& c) { return row_bytes(p, c, p.d + 1); }
+static int64_t pass1_bytes(const ExtProblem& p, const ExtPlan& c) { return row_bytes(p, c, 3 * p.d + 4); }
 // Workspace of a column kernel: the parts' fp32 sums, then the waves' rows of step sums and
 // what ext_step_rows_kernel makes of them.
 struct ColBytes {
@@ -150,7 +154,7 @@ static ColBytes col_bytes(const ExtProblem& p, const ExtPlan& c) {
   if (has_bias(p)) {
     const int64_t blocks = (p.Nk + 16 * c.blocks - 1) / (16 * c.blocks);
     const int subs = c.parts > 1 ? c.parts / ext_group(p) : 1;
-    b.rows = p.B * blocks * subs * c.sets;
+    b.rows = p.B * blocks * subs * c.waves;
     // few rows go straight to the gather, for one launch less
     b.S = b.rows <= 64 ? 0 : (int)std::min<int64_t>(16, b.rows / 8);
     auto pad = [](int64_t n) { return (n + 15) / 16 * 16; };
@@ -161,6 +165,8 @@ static ColBytes col_bytes(const ExtProblem& p, const ExtPlan& c) {
 }
 
 static ExtPlan plan_fwd(const ExtProblem& p) { FB_EXT_DISPATCH(p, ext_fwd_plan, p); }
+static ExtPlan plan_rows(const ExtProblem& p) { FB_EXT_DISPATCH(p, ext_rows_plan, p); }
+static ExtPlan plan_pass1(const ExtProblem& p) { FB_EXT_DISPATCH(p, ext_pass1_plan, p); }
 static ExtPlan plan_cols(const ExtProblem& p) { FB_EXT_DISPATCH(p, ext_cols_plan, p); }
 static ExtPlan plan_pass2(const ExtProblem& p) { FB_EXT_DISPATCH(p, ext_pass2_plan, p); }
 static int32_t go_fwd(const ExtProblem& p, const void* Q, const void* K, const void* V, void* O, float* L, float* ws,
@@ -168,14 +174,15 @@ static int32_t go_fwd(const ExtProblem& p, const void* Q, const void* K, const v
   FB_EXT_DISPATCH(p, ext_launch_fwd, p, Q, K, V, O, L, ws, s);
 }
 static int32_t go_bwd(const ExtProblem& p, const void* Q, const void* K, const void* V, const void* O, const void* dO,
-                      const float* L, void* dQ, void* dK, void* dV, float* D, float* parts, float* sums,
-                      hipStream_t s) {
-  FB_EXT_DISPATCH(p, ext_launch_bwd, p, Q, K, V, O, dO, L, dQ, dK, dV, D, parts, sums, s);
+                      const float* L, void* dQ, void* dK, void* dV, float* D, float* row_parts, float* parts,
+                      float* sums, hipStream_t s) {
+  FB_EXT_DISPATCH(p, ext_launch_bwd, p, Q, K, V, O, dO, L, dQ, dK, dV, D, row_parts, parts, sums, s);
 }
 static int32_t go_pass1(const ExtProblem& p, const void* Q, const void* K, const void* V, const void* O,
                         const void* dO, const void* UQ, const void* UK, const void* UV, const void* UT, const float* L,
-                        const float* D, const void* dQ, void* Qt, void* dOt, float* alpha, float* E, hipStream_t s) {
-  FB_EXT_DISPATCH(p, ext_launch_pass1, p, Q, K, V, O, dO, UQ, UK, UV, UT, L, D, dQ, Qt, dOt, alpha, E, s);
+                        const float* D, const void* dQ, void* Qt, void* dOt, float* alpha, float* E, float* parts,
+                        hipStream_t s) {
+  FB_EXT_DISPATCH(p, ext_launch_pass1, p, Q, K, V, O, dO, UQ, UK, UV, UT, L, D, dQ, Qt, dOt, alpha, E, parts, s);
 }
 static int32_t go_pass2(const ExtProblem& p, const void* Q, const void* K, const void* V, const void* dO,
                         const void* UQ, const void* UK, const void* UV, const void* UT, const float* L, const float* D,
@@ -233,11 +240,13 @@ int32_t attn_ext_bwd(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t N
   if (!fb::ext_ptrs(B * Nq, {Q, O, dO, L, dQ, D}) || !fb::ext_ptrs(B * Nk, {K, V, dK, dV}) || !fb::table_ptr(p, dT))
     return BOB_EINVAL;
   const fb::ColBytes b = fb::col_bytes(p, fb::plan_cols(p));
-  const int64_t need = b.all();
+  const int64_t rows = fb::rows_bytes(p, fb::plan_rows(p)), need = rows + b.all();
   if (need > 0 && (workspace_bytes < need || !fb::aligned16(workspace))) return BOB_EINVAL;
-  char* const ws = (char*)workspace;
+  char* const row_ws = (char*)workspace;
+  char* const ws = row_ws + rows;
   float* const sums = dT != nullptr ? (float*)(ws + b.parts) : nullptr;
-  if (B > 0) rc = fb::go_bwd(p, Q, K, V, O, dO, L, dQ, dK, dV, D, (float*)ws, sums, (hipStream_t)stream);
+  if (B > 0)
+    rc = fb::go_bwd(p, Q, K, V, O, dO, L, dQ, dK, dV, D, (float*)row_ws, (float*)ws, sums, (hipStream_t)stream);
   if (rc != BOB_OK || dT == nullptr) return rc;
   return fb::gather_table(p, b, sums, (float*)(ws + b.parts + b.sums), dT, (hipStream_t)stream);
 }
@@ -246,7 +255,8 @@ int32_t attn_ext_pass1_rows(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, in
                             float scale, int32_t causal, const attn_ext* ext, const void* Q, const void* K,
                             const void* V, const void* O, const void* dO, const void* gdQ, const void* gdK,
                             const void* gdV, const void* gdT, const float* L, const float* D, const void* dQ, void* Qt,
-                            void* dOt, float* alpha, float* E, void* stream) {
+                            void* dOt, float* alpha, float* E, void* workspace, int64_t workspace_bytes,
+                            void* stream) {
   const ExtProblem p = fb::ext_problem(dtype, B, H, Hkv, Nq, Nk, d, scale, causal, ext);
   bool empty;
   const int32_t rc = fb::ext_check(p, &empty);
@@ -254,7 +264,10 @@ int32_t attn_ext_pass1_rows(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, in
   if (!fb::ext_ptrs(Nq, {Q, O, dO, gdQ, L, D, dQ, Qt, dOt, alpha, E}) || !fb::ext_ptrs(Nk, {K, V, gdK, gdV}) ||
       !fb::table_ptr(p, gdT))
     return BOB_EINVAL;
-  return fb::go_pass1(p, Q, K, V, O, dO, gdQ, gdK, gdV, gdT, L, D, dQ, Qt, dOt, alpha, E, (hipStream_t)stream);
+  const int64_t need = fb::pass1_bytes(p, fb::plan_pass1(p));
+  if (need > 0 && (workspace_bytes < need || !fb::aligned16(workspace))) return BOB_EINVAL;
+  return fb::go_pass1(p, Q, K, V, O, dO, gdQ, gdK, gdV, gdT, L, D, dQ, Qt, dOt, alpha, E, (float*)workspace,
+                      (hipStream_t)stream);
 }
 
 int32_t attn_ext_pass2_cols(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
@@ -294,7 +307,15 @@ int64_t attn_ext_bwd_workspace_bytes(int32_t dtype, int64_t B, int64_t H, int64_
   const ExtProblem p = fb::ext_problem(dtype, B, H, Hkv, Nq, Nk, d, 1.0f, causal, ext);
   bool empty;
   if (fb::ext_check(p, &empty) != BOB_OK || empty) return 0;
-  return fb::col_bytes(p, fb::plan_cols(p)).all();
+  return fb::rows_bytes(p, fb::plan_rows(p)) + fb::col_bytes(p, fb::plan_cols(p)).all();
+}
+
+int64_t attn_ext_pass1_workspace_bytes(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,
+                                       int64_t d, int32_t causal, const attn_ext* ext) {
+  const ExtProblem p = fb::ext_problem(dtype, B, H, Hkv, Nq, Nk, d, 1.0f, causal, ext);
+  bool empty;
+  if (fb::ext_check(p, &empty) != BOB_OK || empty || B == 0 || Nq == 0) return 0;
+  return fb::pass1_bytes(p, fb::plan_pass1(p));
 }
 
 int64_t attn_ext_pass2_workspace_bytes(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,

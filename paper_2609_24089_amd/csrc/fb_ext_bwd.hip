@@ -40,14 +40,12 @@ static int64_t cols_dynamic(const ExtProblem& p, const ExtShape& s) {
 }
 
 template <typename T, int D> ExtPlan ext_rows_plan(const ExtProblem& p) {
-  const int64_t steps = ext_steps_bytes(p);
-  const FormQuery q{device_cus(), p.B * p.H, p.Nq, std::max<int64_t>((p.Nk + kBS - 1) / kBS, 1), p.causal != 0,
-                    block_us<T>(3, D), kRowsStep<T>, merge_us(1, D), kRowMargin};
   ExtPlan c;
-  c.form = ext_pick<ExtRowsBwd<T, D>>(p, q, kRowsStep<T>.narrow, [&](const ExtShape&) { return steps; });
-  const ExtShape s = ExtRowsBwd<T, D>::shape(c.form, has_bias(p));
-  c.blocks = s.blocks();
-  c.sets = s.ks;
+  const FormQuery q{device_cus(), p.B * p.H, std::max<int64_t>(p.Nq, 1), std::max<int64_t>((p.Nk + kBS - 1) / kBS, 1),
+                    triangular(p), block_us<T>(3, D), kRowsStep<T>, merge_us(1, D), kRowMargin};
+  const int64_t steps = ext_steps_bytes(p);
+  ext_pick<ExtRowsBwd<T, D>>(p, q, kRowsStep<T>.narrow, [&](const ExtShape&) { return steps; }, -1, 1, 1,
+                             p.B * p.H * p.Nq * (D + 1) * 4, &c);
   return c;
 }
 
@@ -56,43 +54,49 @@ template <typename T, int D> ExtPlan ext_cols_plan(const ExtProblem& p) {
   const int grp = ext_group(p);
   ExtPlan c;
   // with a bias each query head of a group has its own table: one part a head
-  const bool split = has_bias(p) && grp > 1;
-  const int64_t tiles = std::max<int64_t>((p.Nq + kBS - 1) / kBS, 1) * (split ? 1 : grp);
-  const FormQuery q{device_cus(), p.B * (split ? p.H : p.Hkv), std::max<int64_t>(p.Nk, 1), tiles, p.causal != 0,
-                    block_us<T>(4, D), kColsStep<T>, merge_us(2, D), 1.0};
-  c.form = ext_pick<C>(p, q, kColsStep<T>.narrow, [&](const ExtShape& s) { return cols_dynamic(p, s); });
-  const ExtShape s = C::shape(c.form, has_bias(p));
-  c.blocks = s.blocks();
-  c.sets = s.ks * s.nw;  // waves that store step sums
-  c.parts = split ? grp : 1;
+  const int base = has_bias(p) ? grp : 1;
+  const FormQuery q{device_cus(), p.B * p.Hkv, std::max<int64_t>(p.Nk, 1),
+                    std::max<int64_t>((p.Nq + kBS - 1) / kBS, 1) * grp, triangular(p), block_us<T>(4, D), kColsStep<T>,
+                    merge_us(2, D), 1.0};
+  ext_pick<C>(p, q, kColsStep<T>.narrow, [&](const ExtShape& s) { return cols_dynamic(p, s); }, -1, base, grp,
+              2 * p.B * p.Hkv * p.Nk * D * 4, &c);
   return c;
 }
 
 template <typename T, int D>
 int32_t ext_launch_bwd(const ExtProblem& p, const void* Q, const void* K, const void* V, const void* O, const void* dO,
-                       const float* L, void* dQ, void* dK, void* dV, float* Dv, float* parts, float* sums,
-                       hipStream_t s) {
+                       const float* L, void* dQ, void* dK, void* dV, float* Dv, float* row_parts, float* parts,
+                       float* sums, hipStream_t s) {
   int32_t rc = BOB_OK;
   if (p.Nq > 0) {
     const ExtPlan r = ext_rows_plan<T, D>(p);
     const ExtArgs a = ext_args(p, r, p.B * p.H, p.Nq, nullptr);
-    rc = ext_dispatch<ExtRowsBwd<T, D>>(r.form, p, dim3(a.total), ext_steps_bytes(p), s, a, (const T*)Q, (const T*)K,
-                                        (const T*)V, (const T*)O, (const T*)dO, L, (T*)dQ, Dv);
+    rc = ext_dispatch<ExtRowsBwd<T, D>>(r.form, p, dim3(a.total, r.parts), ext_steps_bytes(p), s, a, (const T*)Q,
+                                        (const T*)K, (const T*)V, (const T*)O, (const T*)dO, L, (T*)dQ, Dv, row_parts);
+    if (rc == BOB_OK && r.parts > 1) {
+      const int64_t all = p.B * p.H * p.Nq;
+      hipLaunchKernelGGL((ext_bwd_join_kernel<T, D>), dim3((unsigned)((all * (D / 4) + 255) / 256)), dim3(256), 0, s, a,
+                         (const float*)row_parts, all, (T*)dQ, Dv);
+      rc = finish_launch();
+    }
   }
   if (rc != BOB_OK || p.Nk == 0) return rc;
   const ExtPlan c = ext_cols_plan<T, D>(p);
   const ExtArgs a = ext_args(p, c, p.B * p.Hkv, p.Nk, nullptr);
-  rc = ext_dispatch<ExtColsBwd<T, D>>(c.form, p, dim3(a.total, c.parts), cols_dynamic(p, ExtColsBwd<T, D>::shape(c.form, has_bias(p))),
-                                      s, a, (const T*)Q, (const T*)K, (const T*)V, (const T*)dO, L, (const float*)Dv,
-                                      (T*)dK, (T*)dV, parts, sums);
+  rc = ext_dispatch<ExtColsBwd<T, D>>(c.form, p, dim3(a.total, c.parts),
+                                      cols_dynamic(p, ExtColsBwd<T, D>::shape(c.form, has_bias(p))), s, a, (const T*)Q,
+                                      (const T*)K, (const T*)V, (const T*)dO, L, (const float*)Dv, (T*)dK, (T*)dV, parts,
+                                      sums);
   if (rc != BOB_OK || c.parts == 1) return rc;
   return ext_add_parts(p, parts, c.parts, dK, dV, s);
 }
 
 #define FB_INST(T, D, ...)                                                                                        \
+  template ExtPlan ext_rows_plan<T, D>(const ExtProblem&);                                                        \
   template ExtPlan ext_cols_plan<T, D>(const ExtProblem&);                                                        \
   template int32_t ext_launch_bwd<T, D>(const ExtProblem&, const void*, const void*, const void*, const void*,    \
                                         const void*, const float*, void*, void*, void*, float*, float*, float*,   \
+                                        float*,                                                                   \
                                         hipStream_t);
 FB_EXT_EACH(FB_INST)
 

@@ -20,21 +20,16 @@ template <typename T, int D> ExtPlan ext_fwd_plan(const ExtProblem& p) {
   ExtPlan c;
   const int64_t steps = ext_steps_bytes(p);
   const int grp = ext_group(p);
-  const Form f2 = ext_form_of<ExtFwd<T, D>, 2>(p, steps, kFwdStep<T>.narrow);
-  if (grp > 1 && p.Nq <= 16 && f2.resident > 0)
-    c.fold = ext_form_of<ExtFwd<T, D>, 2>(p, steps * std::min(grp, 16), 1.0).resident > 0;
+  const auto few = [&](int64_t dynamic) { return ext_form_of<ExtFwd<T, D>, 2>(p, dynamic, 1.0).resident > 0; };
+  // the query heads of a group together read each key and value once: a few rows a head
+  c.fold = grp > 1 && p.Nq <= 16 && few(steps * std::min(grp, 16));
   const int64_t rows = c.fold ? grp * p.Nq : p.Nq, heads = p.B * (c.fold ? p.Hkv : p.H);
   const int64_t tiles = std::max<int64_t>((p.Nk + kBS - 1) / kBS, 1);
-  if (f2.resident > 0 && (c.fold || rows <= 16)) {
-    c.form = 2;
-  } else {
-    const FormQuery q{device_cus(), heads, rows, tiles, p.causal != 0, block_us<T>(2, D), kFwdStep<T>, merge_us(1, D),
-                      kRowMargin};
-    c.form = ext_pick<ExtFwd<T, D>>(p, q, kFwdStep<T>.narrow, [&](const ExtShape&) { return steps; });
-  }
-  const ExtShape s = ExtFwd<T, D>::shape(c.form, has_bias(p));
-  c.blocks = s.blocks();
-  c.sets = s.ks;
+  const FormQuery q{device_cus(), heads, rows, tiles, triangular(p), block_us<T>(2, D), kFwdStep<T>, merge_us(1, D),
+                    kRowMargin};
+  const int64_t dynamic = steps * (c.fold ? std::min(grp, 16) : 1);
+  ext_pick<ExtFwd<T, D>>(p, q, kFwdStep<T>.narrow, [&](const ExtShape&) { return dynamic; },
+                         c.fold || (rows <= 16 && few(steps)) ? 2 : -1, 1, 1, heads * rows * (D + 2) * 4, &c);
   return c;
 }
 
@@ -49,8 +44,8 @@ int32_t ext_launch_fwd(const ExtProblem& p, const void* Q, const void* K, const 
                                           (const T*)V, (T*)O, L, ws);
   if (rc != BOB_OK || c.parts == 1) return rc;
   const int64_t all = heads * rows;
-  hipLaunchKernelGGL((ext_fwd_join_kernel<T, D>), dim3((unsigned)((all * (D / 4) + 255) / 256)), dim3(256), 0, s, ws,
-                     c.parts, all, a, (T*)O, L);
+  hipLaunchKernelGGL((ext_fwd_join_kernel<T, D>), dim3((unsigned)((all * (D / 4) + 255) / 256)), dim3(256), 0, s, a,
+                     (const float*)ws, all, (T*)O, L);
   return finish_launch();
 }
 

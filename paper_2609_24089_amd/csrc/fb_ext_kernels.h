@@ -174,6 +174,17 @@ struct ExtRun {
   __device__ __forceinline__ int size() const { return end - begin; }
 };
 
+// The parts that split a row block's tiles, of nparts: each set of a part gets four tiles at
+// least, the parts beyond take none.
+__device__ __forceinline__ int ext_parts_of(int tiles, int sets, int nparts) {
+  return min(max(tiles / (4 * sets), 1), nparts);
+}
+// The run of set ks of part `part`.
+__device__ __forceinline__ ExtRun ext_run(int tiles, int part, int split, int ks, int sets) {
+  ExtRun r(tiles, min(part, split) * sets + ks, split * sets);
+  return r;
+}
+
 // What a row kernel's workgroup and wave know of their rows.  kFold: the kernel may run
 // folded rows (a.fold); the others keep one lane position instead of one a 16-row block.
 template <int MR, int NW, bool kFold>
@@ -287,7 +298,7 @@ __device__ __forceinline__ void ext_mask1(floatx4 (&x)[2], int s0, int klim) {
 // ===========================================================================
 // Forward.  As attn_fwd_kernel (online softmax against a lazily moved reference), over the
 // keys of another sequence, with the bias.  A part (gridDim.y of them) takes a run of the
-// key tiles and stores its unnormalised sums, reference and weight instead of O and L;
+// key tiles (none, if the block has few) and stores its unnormalised sums, reference and weight instead of O and L;
 // ext_fwd_join_kernel joins them.  One wave a set (NW = 1) runs without barriers: the form
 // of a few query rows against a long cache, which reads each key and value once.
 // ===========================================================================
@@ -399,8 +410,8 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_fwd_kernel(
 
   const T* const src[2] = {K + kvoff, V + kvoff};
   // every set of a workgroup with barriers runs as long as its first, whose run is the longest
-  const ExtRun run(rw.tiles, part * KS + ks, a.nparts * KS);
-  const ExtRun first(rw.tiles, part * KS, a.nparts * KS);
+  const int split = ext_parts_of(rw.tiles, KS, a.nparts);
+  const ExtRun run = ext_run(rw.tiles, part, split, ks, KS), first = ext_run(rw.tiles, part, split, 0, KS);
   constexpr bool kBarrier = NW > 1;
   const int iters = kBarrier ? first.size() : run.size();
   const TileCopy<T, D, NW, 2> copy(wl);
@@ -536,8 +547,8 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_fwd_kernel(
 // Joins the parts of the forward: every part's sums brought to the largest reference.
 // One thread for four head dims of a row.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void ext_fwd_join_kernel(const float* __restrict__ parts, int nparts, int64_t all,
-                                                           ExtArgs a, T* __restrict__ O, float* __restrict__ L) {
+__global__ __launch_bounds__(256) void ext_fwd_join_kernel(ExtArgs a, const float* __restrict__ parts, int64_t all,
+                                                           T* __restrict__ O, float* __restrict__ L) {
   using E = Elt<T>;
   constexpr int kPer = D / 4;
   const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -546,12 +557,12 @@ __global__ __launch_bounds__(256) void ext_fwd_join_kernel(const float* __restri
   if (row >= all) return;
   const int64_t bh = row / a.Nq;
   const bool ok = (int)(row - bh * a.Nq) < ext_lens(a, (int)(bh / a.H)).q;
-  const float* const ml = parts + nparts * all * D;
+  const float* const ml = parts + a.nparts * all * D;
   floatx4 sum = floatx4{0.f, 0.f, 0.f, 0.f};
   float m = -1e30f, w = 0.f;
   if (ok) {
-    for (int q = 0; q < nparts; ++q) m = fmaxf(m, ml[2 * (q * all + row)]);
-    for (int q = 0; q < nparts; ++q) {
+    for (int q = 0; q < a.nparts; ++q) m = fmaxf(m, ml[2 * (q * all + row)]);
+    for (int q = 0; q < a.nparts; ++q) {
       const int64_t at = q * all + row;
       const float f = fast_exp2(ml[2 * at] - m);
       w = __builtin_fmaf(ml[2 * at + 1], f, w);
@@ -575,7 +586,7 @@ __global__ __launch_bounds__(256) void ext_fwd_join_kernel(const float* __restri
 template <typename T, int D, int MR, int NW, int OCC, int NSTAGE, int KS, bool kBias>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
     ExtArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ O,
-    const T* __restrict__ dO, const float* __restrict__ L, T* __restrict__ dQ, float* __restrict__ Dout) {
+    const T* __restrict__ dO, const float* __restrict__ L, T* __restrict__ dQ, float* __restrict__ Dout, float* __restrict__ parts) {
   using E = Elt<T>;
   using G = Geo<T, D>;
   constexpr int BR = 16 * MR * NW;
@@ -621,7 +632,8 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
   typename E::TFrag dsf[MR];
 
   const T* const src[2] = {K + kvoff, V + kvoff};
-  const ExtRun run(rw.tiles, ks, KS), first(rw.tiles, 0, KS);
+  const int part = blockIdx.y, split = ext_parts_of(rw.tiles, KS, a.nparts);
+  const ExtRun run = ext_run(rw.tiles, part, split, ks, KS), first = ext_run(rw.tiles, part, split, 0, KS);
   constexpr bool kBarrier = NW > 1;
   const TileCopy<T, D, NW, 2> copy(wl);
   float blo = 0.f, bhi = 0.f;
@@ -758,6 +770,20 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
     merge_sets<KS, NW>(acc, ks, wl, (floatx4 FB_LDS*)&sm.lds[0][0][0]);
   }
   const RowSplit<KS> own{ks, 0};
+  if (a.nparts > 1) {
+    const int64_t all = (int64_t)(a.total / a.nRB) * rw.rows;
+    float* const sc = parts + a.nparts * all * D;
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb)
+      if (rw.ok(mb)) {
+        const int64_t at = part * all + rw.qrow + rw.row(mb);
+#pragma unroll
+        for (int nb = 0; nb < G::kNB; ++nb)
+          if (own.owns(nb)) *(floatx4*)(parts + at * D + 16 * nb + 4 * g) = acc[nb][mb];
+        if (g == 0 && ks == 0) sc[at] = (part == 0 ? dout[mb] : 0.f) + rest[mb];
+      }
+    return;
+  }
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb) {
     if (rw.row(mb) >= rw.rows) continue;
@@ -768,6 +794,31 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
         E::store4(dQ + at * D + 16 * nb + 4 * g, rw.ok(mb) ? acc[nb][mb] * a.scale : floatx4{0.f, 0.f, 0.f, 0.f});
     if (g == 0 && ks == 0) Dout[at] = rw.ok(mb) ? dout[mb] + rest[mb] : 0.f;
   }
+}
+
+// Adds the parts of the row side: dQ = tau times the sums, D their scalars' sum.  One
+// thread for four head dims of a row.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void ext_bwd_join_kernel(ExtArgs a, const float* __restrict__ parts, int64_t all,
+                                                           T* __restrict__ dQ, float* __restrict__ Dout) {
+  constexpr int kPer = D / 4;
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = x / kPer;
+  const int dim = 4 * (int)(x % kPer);
+  if (row >= all) return;
+  const int64_t bh = row / a.Nq;
+  floatx4 sum = floatx4{0.f, 0.f, 0.f, 0.f};
+  float d = 0.f;
+  if ((int)(row - bh * a.Nq) < ext_lens(a, (int)(bh / a.H)).q) {
+    const float* const sc = parts + a.nparts * all * D;
+    for (int q = 0; q < a.nparts; ++q) {
+      const int64_t at = q * all + row;
+      sum += *(const floatx4*)(parts + at * D + dim);
+      d += sc[at];
+    }
+  }
+  Elt<T>::store4(dQ + row * D + dim, sum * a.scale);
+  if (dim == 0) Dout[row] = d;
 }
 
 // ===========================================================================
@@ -1227,7 +1278,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
     ExtArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ O,
     const T* __restrict__ dO, const T* __restrict__ UQ, const T* __restrict__ UK, const T* __restrict__ UV,
     const float* __restrict__ L, const float* __restrict__ Dv, const T* __restrict__ dQ, T* __restrict__ Qt,
-    T* __restrict__ dOt, float* __restrict__ alpha_out, float* __restrict__ E_out) {
+    T* __restrict__ dOt, float* __restrict__ alpha_out, float* __restrict__ E_out, float* __restrict__ parts) {
   using E = Elt<T>;
   using G = Geo<T, D>;
   constexpr int BR = 16 * MR * NW;
@@ -1272,14 +1323,16 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
   using AF = typename E::AFrag;
 
   const T* const src[4] = {K + kvoff, V + kvoff, UK + kvoff, UV + kvoff};
-  const ExtRun run(rw.tiles, ks, KS), first(rw.tiles, 0, KS);
+  const int part = blockIdx.y, split = ext_parts_of(rw.tiles, KS, a.nparts);
+  const ExtRun run = ext_run(rw.tiles, part, split, ks, KS), first = ext_run(rw.tiles, part, split, 0, KS);
   constexpr bool kBarrier = NW > 1 || KS > 1;  // the sets meet in the first tile
   const TileCopy<T, D, NW, 4> copy(wl);
   float blo = 0.f, bhi = 0.f, ulo = 0.f, uhi = 0.f;
   float aref[MR], eref[MR];
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb) aref[mb] = eref[mb] = 0.f;
-  bool centred = false;
+  // parts that share a block take their sums from 0: each row of theirs has many keys in view
+  bool centred = split > 1;
   ext_stream<2, tile_loads<T, D, NW, 4>(), kBarrier>(
       kBarrier ? first.size() : run.size(),
       [&](int it, int st) {
@@ -1301,7 +1354,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
         const int s0 = min(run.begin + it, rw.tiles - 1) * kBS;
         int mode = run.begin + it < run.end ? rw.mode(s0) : 0;
         if constexpr (KS > 1) mode = vector_mode(mode);
-        if (mode == 0 && (KS == 1 || it > 0)) return;
+        if (mode == 0 && (KS == 1 || it > 0 || split > 1)) return;
         const T FB_LDS* Ks = (const T FB_LDS*)sm.lds[ks][st];
         const T FB_LDS* Vs = Ks + G::kTileElems;
         const T FB_LDS* UKs = Vs + G::kTileElems;
@@ -1380,7 +1433,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
           }
         }
         // every wave of a workgroup with sets comes here in its first iteration (a barrier)
-        if (KS > 1 ? it == 0 : !centred) {
+        if (KS > 1 ? it == 0 && split == 1 : !centred) {
           centred = true;
 #pragma unroll
           for (int mb = 0; mb < MR; ++mb) {
@@ -1510,6 +1563,25 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
     merge_sets<KS, NW>(aB, ks, wl, buf);
   }
   const RowSplit<KS> own{ks, 0};
+  if (a.nparts > 1) {
+    const int64_t all = (int64_t)(a.total / a.nRB) * rw.rows;
+    float* const sc = parts + a.nparts * all * (3 * D);
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb)
+      if (rw.ok(mb)) {
+        const int64_t at = part * all + rw.qrow + rw.row(mb);
+#pragma unroll
+        for (int nb = 0; nb < G::kNB; ++nb)
+          if (own.owns(nb)) {
+            float* const to = parts + at * (3 * D) + 16 * nb + 4 * g;
+            *(floatx4*)to = aDO[nb][mb];
+            *(floatx4*)(to + D) = aOM[nb][mb];
+            *(floatx4*)(to + 2 * D) = aB[nb][mb];
+          }
+        if (g == 0 && ks == 0) *(floatx4*)(sc + 4 * at) = floatx4{alpha[mb], e0[mb], aref[mb], eref[mb]};
+      }
+    return;
+  }
   const floatx4 zero = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb) {
@@ -1532,6 +1604,46 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
         E::store4(Qt + off, zero);
       }
     }
+  }
+}
+
+// Adds the parts of Pass 1 and finishes its rows.  One thread for four head dims of a row.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void ext_pass1_join_kernel(ExtArgs a, const float* __restrict__ parts, int64_t all,
+                                                             const T* __restrict__ O, const float* __restrict__ Dv,
+                                                             const T* __restrict__ dQ, T* __restrict__ Qt,
+                                                             T* __restrict__ dOt, float* __restrict__ alpha_out,
+                                                             float* __restrict__ E_out) {
+  using E = Elt<T>;
+  constexpr int kPer = D / 4;
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = x / kPer;
+  const int dim = 4 * (int)(x % kPer);
+  if (row >= all) return;
+  const int64_t bh = row / a.Nq, off = row * D + dim;
+  const bool ok = (int)(row - bh * a.Nq) < ext_lens(a, (int)(bh / a.H)).q;
+  const floatx4 zero = floatx4{0.f, 0.f, 0.f, 0.f};
+  floatx4 d = zero, om = zero, b = zero, sc = zero;
+  if (ok) {
+    const float* const scalars = parts + a.nparts * all * (3 * D);
+    for (int q = 0; q < a.nparts; ++q) {
+      const int64_t at = q * all + row;
+      const float* const from = parts + at * (3 * D) + dim;
+      d += *(const floatx4*)from;
+      om += *(const floatx4*)(from + D);
+      b += *(const floatx4*)(from + 2 * D);
+      sc += *(const floatx4*)(scalars + 4 * at);
+    }
+    E::store4(dOt + off, d - sc[0] * E::load4(O + off));
+    E::store4(Qt + off, a.scale * (om - sc[1] * b) - sc[0] * E::load4(dQ + off));
+  } else {
+    E::store4(dOt + off, zero);
+    E::store4(Qt + off, zero);
+  }
+  if (dim == 0) {
+    const float al = sc[2] + sc[0];
+    alpha_out[row] = al;
+    E_out[row] = ok ? sc[3] + sc[1] - al * Dv[row] : 0.f;
   }
 }
 

@@ -60,6 +60,30 @@ struct FormQuery {
   double margin = 1.0;  // by which another unsplit form has to be faster than the whole blocks
 };
 
+// Estimated time of one form, but for its margin and extra_us (the figures are beside
+// pick_form()).
+inline double form_us(const FormQuery& q, const Form& f) {
+  constexpr double kRound = 4.0;
+  const int64_t total = q.heads * ((q.N + 16 * f.blocks - 1) / (16 * f.blocks)) * f.parts;
+  const int64_t shares = (int64_t)f.sets * f.parts;
+  const double share = (double)((q.tiles + shares - 1) / shares);
+  auto step = [&](int64_t workgroups) {
+    const int64_t blocks = std::max<int64_t>(4, workgroups * f.blocks * f.sets);
+    return q.block_us * (q.step.base + q.step.per_block * f.weight * (double)blocks);
+  };
+  const int64_t k = (total + q.cus - 1) / q.cus;  // workgroups of the fullest CU
+  double t;
+  if (q.causal) {
+    const int64_t n = std::min<int64_t>(k, f.resident);
+    const double mean = 0.5 * (share + 1) * total / (double)q.cus / n * step(n);
+    t = std::max(mean, share * step(1));
+  } else {
+    t = share * ((double)(k / f.resident) * step(f.resident) + (k % f.resident != 0 ? step(k % f.resident) : 0));
+  }
+  t += (kRound + q.merge_us * f.blocks * (f.sets - 1)) * (double)((k + f.resident - 1) / f.resident);
+  return t;
+}
+
 // Estimated time of a kernel's forms.  Equal (dense) blocks cost the rounds of
 // the fullest CU, causal ones the larger of the mean load and the heaviest
 // block's steps; a step has at least the four 16-row blocks that occupy every
@@ -79,7 +103,6 @@ struct FormQuery {
 // Returns the index of the form with the least time; 0 if the device is unknown.
 // *chosen (may be null): that form.
 inline int pick_form(const FormQuery& q, std::initializer_list<Form> forms, Form* chosen = nullptr) {
-  constexpr double kRound = 4.0;
   if (chosen != nullptr) *chosen = *forms.begin();
   if (q.cus <= 0) return 0;
   int best = 0, i = -1;
@@ -97,22 +120,7 @@ inline int pick_form(const FormQuery& q, std::initializer_list<Form> forms, Form
     // d = 32 rows in 16-row blocks reach
     const bool launches = total <= INT32_MAX && total * f.threads <= (int64_t)UINT32_MAX;
     if (i > 0 && ((fills && f.parts == 1) || !launches)) continue;
-    const int64_t shares = (int64_t)f.sets * f.parts;
-    const double share = (double)((q.tiles + shares - 1) / shares);
-    auto step = [&](int64_t workgroups) {
-      const int64_t blocks = std::max<int64_t>(4, workgroups * f.blocks * f.sets);
-      return q.block_us * (q.step.base + q.step.per_block * f.weight * (double)blocks);
-    };
-    const int64_t k = (total + q.cus - 1) / q.cus;  // workgroups of the fullest CU
-    double t;
-    if (q.causal) {
-      const int64_t n = std::min<int64_t>(k, f.resident);
-      const double mean = 0.5 * (share + 1) * total / (double)q.cus / n * step(n);
-      t = std::max(mean, share * step(1));
-    } else {
-      t = share * ((double)(k / f.resident) * step(f.resident) + (k % f.resident != 0 ? step(k % f.resident) : 0));
-    }
-    t += (kRound + q.merge_us * f.blocks * (f.sets - 1)) * (double)((k + f.resident - 1) / f.resident);
+    double t = form_us(q, f);
     // splits cost what the estimate does not see (streams of several heads in flight,
     // the reduction's launch): they have to be clearly faster
     if (i > 0) t *= f.parts > 1 ? 1.08 : q.margin;

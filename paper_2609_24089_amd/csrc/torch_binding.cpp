@@ -38,6 +38,7 @@ struct Api {
   decltype(&::attn_ext_pass2_cols) ext_pass2 = nullptr;
   decltype(&::attn_ext_fwd_workspace_bytes) ext_fwd_bytes = nullptr;
   decltype(&::attn_ext_bwd_workspace_bytes) ext_bwd_bytes = nullptr;
+  decltype(&::attn_ext_pass1_workspace_bytes) ext_pass1_bytes = nullptr;
   decltype(&::attn_ext_pass2_workspace_bytes) ext_pass2_bytes = nullptr;
 } api;
 
@@ -63,6 +64,7 @@ void bind(const std::string& path) {
   take(a.ext_pass2, "attn_ext_pass2_cols");
   take(a.ext_fwd_bytes, "attn_ext_fwd_workspace_bytes");
   take(a.ext_bwd_bytes, "attn_ext_bwd_workspace_bytes");
+  take(a.ext_pass1_bytes, "attn_ext_pass1_workspace_bytes");
   take(a.ext_pass2_bytes, "attn_ext_pass2_workspace_bytes");
   api = a;
 }
@@ -533,9 +535,11 @@ struct ExtAttentionBackward : torch::autograd::Function<ExtAttentionBackward> {
     at::AutoGradMode no_graph(false);
     const void* const gT = ext_cotangent(ut, table);
     const Tensor Qt = at::empty_like(q), dOt = at::empty_like(q), alpha = rows_like(q), E = rows_like(q);
+    const int64_t bytes1 = api.ext_pass1_bytes(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, causal, &m.x);
+    const Tensor ws1 = workspace(bytes1, q);
     ok(api.ext_pass1(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, (float)scale, causal, &m.x, p(q), p(k), p(v), p(O),
                      p(dO), p(uq), p(uk), p(uv), gT, f(L), f(D), p(dQ), pm(Qt), pm(dOt), fm(alpha), fm(E),
-                     stream_of(q)));
+                     bytes1 > 0 ? pm(ws1) : nullptr, bytes1, stream_of(q)));
     const Tensor Kt = at::empty_like(k), Vt = at::empty_like(k);
     const Tensor Tt = table.defined() && ctx->needs_input_grad(3) ? at::empty_like(table) : Tensor();
     const int64_t bytes = api.ext_pass2_bytes(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, causal, &m.x);
@@ -565,6 +569,15 @@ struct ExtAttention : torch::autograd::Function<ExtAttention> {
   }
   static variable_list backward(AutogradContext* ctx, variable_list g) {
     const variable_list s = ctx->get_saved_variables();
+    if (!at::GradMode::is_enabled()) {  // no second derivatives asked for: no node for them
+      const Extras e{s[3], s[6], s[7], s[8], s[9]};
+      const Tensor dO = g[0].contiguous();
+      const ExtDims m = ext_dims_or_throw({&s[0], &s[4], &dO}, {&s[1], &s[2]}, {&s[5]}, e);
+      c10::OptionalDeviceGuard guard(s[0].device());
+      const ExtBwd r = run_ext_bwd(m, s[0], s[1], s[2], s[4], dO, s[5], e, ctx->saved_data["scale"].toDouble(),
+                                   ctx->saved_data["causal"].toBool(), s[3].defined() && ctx->needs_input_grad(3));
+      return {r.dQ, r.dK, r.dV, r.dT, Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+    }
     const variable_list d = ExtAttentionBackward::apply(
         s[0], s[1], s[2], maybe(s[3]), s[4], s[5], g[0].contiguous(), maybe(s[6]), maybe(s[7]), maybe(s[8]), maybe(s[9]),
         ctx->saved_data["scale"].toDouble(), ctx->saved_data["causal"].toBool(),

@@ -44,11 +44,11 @@ def _declare(lib):
     shape = [i32] + [i64] * 6
     lib.attn_ext_fwd_lse.argtypes = shape + [f32, i32, ext] + [vp] * 5 + [vp, i64, vp]
     lib.attn_ext_bwd.argtypes = shape + [f32, i32, ext] + [vp] * 11 + [vp, i64, vp]
-    lib.attn_ext_pass1_rows.argtypes = shape + [f32, i32, ext] + [vp] * 16 + [vp]
+    lib.attn_ext_pass1_rows.argtypes = shape + [f32, i32, ext] + [vp] * 16 + [vp, i64, vp]
     lib.attn_ext_pass2_cols.argtypes = shape + [f32, i32, ext] + [vp] * 15 + [vp, i64, vp]
     for name in ("fwd_lse", "bwd", "pass1_rows", "pass2_cols"):
         getattr(lib, "attn_ext_" + name).restype = i32
-    for name in ("fwd", "bwd", "pass2"):
+    for name in ("fwd", "bwd", "pass1", "pass2"):
         fn = getattr(lib, f"attn_ext_{name}_workspace_bytes")
         fn.argtypes = shape + [i32, ext]
         fn.restype = i64
@@ -215,8 +215,10 @@ def attn_ext_pass1_rows(Q, K, V, O, dO, gdQ, gdK, gdV, L, D, dQ, scale, causal=F
     _check_mats(Q, Qt, dOt)
     _check_rows(Q.shape, alpha, E)
     lib = load_library()
+    st = _stream(stream, Q)
+    ws, wp, n = p.workspace(lib.attn_ext_pass1_workspace_bytes, stream)
     _call(Q, lib.attn_ext_pass1_rows, *p.shape, *p.options, _p(Q), _p(K), _p(V), _p(O), _p(dO), _p(gdQ), _p(gdK),
-          _p(gdV), p.cotangent(gdT), _p(L), _p(D), _p(dQ), _p(Qt), _p(dOt), _p(alpha), _p(E), _stream(stream, Q))
+          _p(gdV), p.cotangent(gdT), _p(L), _p(D), _p(dQ), _p(Qt), _p(dOt), _p(alpha), _p(E), wp, n, st)
     return Qt, dOt, alpha, E
 
 

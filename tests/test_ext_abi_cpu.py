@@ -37,7 +37,7 @@ def call(lib, fn, dtype=fb.BOB_BF16, B=1, H=2, Hkv=1, Nq=16, Nk=20, d=64, scale=
             ptrs[i] = ctypes.c_void_p(0)
     for i, v in (bad or {}).items():
         ptrs[i] = ctypes.c_void_p(v)
-    tail = [] if fn == "pass1_rows" else [ctypes.c_void_p(ws), nbytes]
+    tail = [ctypes.c_void_p(ws), nbytes]
     return getattr(lib, "attn_ext_" + fn)(dtype, B, H, Hkv, Nq, Nk, d, ctypes.c_float(scale), causal,
                                           None if ext is None else ctypes.byref(ext), *ptrs, *tail, None)
 

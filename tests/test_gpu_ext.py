@@ -83,6 +83,17 @@ CASES = {
     "cross_token_grouped_f32": dict(B=2, H=20, Hkv=1, Nq=1, Nk=70, d=64, dtype="f32"),
     "rows_before_keys": dict(B=1, H=2, Hkv=2, Nq=80, Nk=60, d=64, bias=(32, 128), causal=True, q_starts=[-37]),
     "keys_behind": dict(B=1, H=2, Hkv=2, Nq=50, Nk=60, d=64, bias=(32, 128), q_starts=[100000]),
+    # few rows against many keys, and few keys against many queries: blocks split over workgroups
+    "split_token": dict(B=1, H=2, Hkv=2, Nq=1, Nk=6000, d=64, kv_lens=[5900]),
+    "split_tokens_grouped": dict(B=3, H=8, Hkv=1, Nq=4, Nk=5000, d=128, bias=(32, 128), causal=True,
+                                 q_starts=[4990, 20, 700], kv_lens=[4994, 24, 704]),
+    "split_rows": dict(B=1, H=2, Hkv=1, Nq=40, Nk=5000, d=64),
+    "split_rows_ragged": dict(B=3, H=1, Hkv=1, Nq=70, Nk=4100, d=128, kv_lens=[4100, 90, 0], q_lens=[70, 70, 20]),
+    "split_rows_chunk": dict(B=2, H=1, Hkv=1, Nq=50, Nk=4000, d=64, bias=(32, 128), causal=True, q_starts=[3950, 0]),
+    "split_rows_f32": dict(B=1, H=1, Hkv=1, Nq=33, Nk=3000, d=64, dtype="f32", bias=(32, 128)),
+    "split_cols": dict(B=1, H=2, Hkv=2, Nq=6000, Nk=40, d=64, q_lens=[5800]),
+    "split_cols_grouped": dict(B=1, H=8, Hkv=2, Nq=1100, Nk=100, d=128),
+    "split_cols_bias": dict(B=1, H=4, Hkv=2, Nq=2100, Nk=64, d=32, bias=(32, 128)),
     "causal_no_bias": dict(B=2, H=2, Hkv=1, Nq=70, Nk=150, d=64, causal=True, q_starts=[80, 0]),
 }
 
@@ -156,6 +167,27 @@ def compare(got, want, c, names):
         assert e <= bar(n, c.get("dtype"), c.get("table_dtype", "f32")), (n, e)
 
 
+@pytest.mark.parametrize("name", [n for n in CASES if n.startswith("split_")])
+def test_split_cases_are_split(name):
+    """The cases above need a workspace, without a bias for the parts' sums alone."""
+    import ctypes
+    import paper_2609_24089_amd as fb
+    c = CASES[name]
+    lib = fb.load_library()
+    table = 1 << 20 if "bias" in c else 0
+    e = fb.AttnExt(None, None, None, table, table, fb.BOB_F32, *c.get("bias", (0, 0)))
+    args = (fb.BOB_F32 if c.get("dtype") == "f32" else fb.BOB_BF16, c["B"], c["H"], c["Hkv"], c["Nq"], c["Nk"], c["d"],
+            int(c.get("causal", False)), ctypes.byref(e))
+    n = {k: getattr(lib, f"attn_ext_{k}_workspace_bytes")(*args) for k in ("fwd", "bwd", "pass1", "pass2")}
+    say("   bytes", n)
+    if "cols" in name:
+        assert n["pass2"] >= 2 * 2 * c["B"] * c["Hkv"] * c["Nk"] * c["d"] * 4
+    if "token" in name:
+        assert n["fwd"] >= 2 * c["B"] * c["H"] * c["Nq"] * c["d"] * 4
+    if "rows" in name:
+        assert n["pass1"] >= 2 * 3 * c["B"] * c["H"] * c["Nq"] * c["d"] * 4
+
+
 @pytest.mark.parametrize("name", CASES)
 def test_every_output(name):
     c = CASES[name]
@@ -192,7 +224,7 @@ def differentiate(xd, c, tau, fn=layer):
     return dict(zip(names, [t.detach() for t in (O, *g, *h)]))
 
 
-LAYERS = ["tile_edges", "f32_d64", "empty_entries", "bias_causal", "bias_grouped", "bias_bf16_table", "cache_chunk",
+LAYERS = ["split_rows_ragged", "split_cols_grouped", "split_cols_bias", "tile_edges", "f32_d64", "empty_entries", "bias_causal", "bias_grouped", "bias_bf16_table", "cache_chunk",
           "cross_tokens_grouped", "cache_tokens_grouped"]
 
 
@@ -273,7 +305,7 @@ def test_gradient_against_differences():
 # ---------------------------------------------------------------------------
 # Padding, masks, memory
 # ---------------------------------------------------------------------------
-@pytest.mark.parametrize("name", ["tile_edges", "empty_entries", "whole_d128_bias", "bias_grouped", "cache_chunk",
+@pytest.mark.parametrize("name", ["split_rows_ragged", "split_cols", "split_tokens_grouped", "tile_edges", "empty_entries", "whole_d128_bias", "bias_grouped", "cache_chunk",
                                   "cross_tokens_grouped", "cache_token_grouped"])
 def test_padding_is_never_read(name):
     """NaN and infinities in padded rows and keys change no output, and padded rows, padded
