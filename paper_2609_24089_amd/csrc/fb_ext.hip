@@ -31,27 +31,32 @@ __global__ __launch_bounds__(256) void ext_step_rows_kernel(const float* __restr
   for (int x = threadIdx.x; x < width; x += 256) out[x] = sum_rows(head, blockIdx.x, rows, gridDim.x, width, x);
 }
 
-// Gathers head blockIdx.x's sums by step into its buckets.  Eight lanes share a bucket,
-// each takes every eighth step; the order of the sums is fixed.
+// Gathers head blockIdx.x's sums by step into its buckets: four groups of 256 threads add
+// every fourth row of a step, then eight lanes share a bucket and take every eighth step each.
+// The order of the sums is fixed.
 constexpr int kMaxWidth = 2 * kMaxDistance + 3;
-constexpr int kGatherThreads = 512;
-__global__ __launch_bounds__(kGatherThreads) void ext_buckets_kernel(const float* __restrict__ mid, int S, ExtArgs a,
+constexpr int kGroups = 4, kGatherThreads = 256 * kGroups;
+__global__ __launch_bounds__(kGatherThreads) void ext_buckets_kernel(const float* __restrict__ rows, int n, ExtArgs a,
                                                                      void* __restrict__ out) {
-  __shared__ float sum[kMaxWidth];
+  __shared__ float sum[kGroups][kMaxWidth];
   __shared__ int bucket[kMaxWidth];
-  const int width = 2 * a.R + 3;
-  for (int x = threadIdx.x; x < width; x += kGatherThreads) {
-    // the two sums beyond the steps belong to the buckets of the ends
-    const int step = x <= 2 * a.R ? x : x == 2 * a.R + 1 ? 0 : 2 * a.R;
-    bucket[x] = min(max(a.buckets[step], 0), a.num_buckets - 1);
-    sum[x] = sum_rows(mid + (int64_t)blockIdx.x * S * width, 0, S, 1, width, x);
+  const int width = 2 * a.R + 3, group = threadIdx.x >> 8;
+  const float* const mine = rows + (int64_t)blockIdx.x * n * width;
+  for (int x = threadIdx.x & 255; x < width; x += 256) {
+    if (group == 0) {
+      // the two sums beyond the steps belong to the buckets of the ends
+      const int step = x <= 2 * a.R ? x : x == 2 * a.R + 1 ? 0 : 2 * a.R;
+      bucket[x] = min(max(a.buckets[step], 0), a.num_buckets - 1);
+    }
+    sum[group][x] = sum_rows(mine, group, n, kGroups, width, x);
   }
   __syncthreads();
   const int lane = threadIdx.x & 7;
   for (int c0 = 0; c0 < a.num_buckets; c0 += kGatherThreads / 8) {
     const int c = c0 + (threadIdx.x >> 3);
     float v = 0.f;
-    for (int x = lane; x < width; x += 8) v += bucket[x] == c ? sum[x] : 0.f;
+    for (int x = lane; x < width; x += 8)
+      if (bucket[x] == c) v += (sum[0][x] + sum[1][x]) + (sum[2][x] + sum[3][x]);
     v += __shfl_xor(v, 1);
     v += __shfl_xor(v, 2);
     v += __shfl_xor(v, 4);
@@ -156,7 +161,7 @@ static ColBytes col_bytes(const ExtProblem& p, const ExtPlan& c) {
     const int subs = c.parts > 1 ? c.parts / ext_group(p) : 1;
     b.rows = p.B * blocks * subs * c.waves;
     // few rows go straight to the gather, for one launch less
-    b.S = b.rows <= 64 ? 0 : (int)std::min<int64_t>(16, b.rows / 8);
+    b.S = b.rows <= 256 ? 0 : (int)std::min<int64_t>(16, b.rows / 8);
     auto pad = [](int64_t n) { return (n + 15) / 16 * 16; };
     b.sums = pad(b.rows * p.H * ext_width(p) * 4);
     b.mid = pad(b.S * p.H * ext_width(p) * 4);
