@@ -105,11 +105,11 @@ static int32_t ext_check(const ExtProblem& p, bool* empty) {
     return BOB_OK;
   }
   if (p.Nq > kMaxN || p.Nk > kMaxN) return BOB_EINVAL;
-  // 32-bit grids and loop counts: 16-row blocks of every head, and the query tiles of a
-  // group's heads, which one column block streams
+  // 2^30 rows of all heads: a launch takes fewer than 2^32 threads, and the whole blocks have
+  // 64 rows or more in 256 threads.  A column block streams a group's query tiles in one loop.
   const int64_t heads = p.B * p.H, rows = std::max(p.Nq, p.Nk);
   if (p.B > INT32_MAX || p.H > 65535 || heads > INT32_MAX) return BOB_EINVAL;
-  if (heads * ((rows + 15) / 16) > INT32_MAX / 16) return BOB_EINVAL;
+  if (heads * ((rows + 63) / 64) >= int64_t(1) << 24) return BOB_EINVAL;
   if (ext_group(p) * p.Nq > INT32_MAX / 2) return BOB_EINVAL;
   return BOB_OK;
 }

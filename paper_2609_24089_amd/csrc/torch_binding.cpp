@@ -12,6 +12,7 @@
 #include <torch/csrc/jit/frontend/tracer.h>
 #include <torch/extension.h>
 
+#include <algorithm>
 #include <optional>
 #include <string>
 #include <vector>
@@ -460,14 +461,18 @@ struct ExtBwd {
   Tensor dQ, dK, dV, D, dT;
 };
 ExtBwd run_ext_bwd(const ExtDims& m, const Tensor& Q, const Tensor& K, const Tensor& V, const Tensor& O,
-                   const Tensor& dO, const Tensor& L, const Extras& e, double scale, bool causal, bool want_table) {
-  ExtBwd r{at::empty_like(Q), at::empty_like(K), at::empty_like(K), rows_like(Q), Tensor()};
+                   const Tensor& dO, const Tensor& L, const Extras& e, double scale, bool causal, bool want_table,
+                   bool keep_D) {
+  ExtBwd r{at::empty_like(Q), at::empty_like(K), at::empty_like(K), keep_D ? rows_like(Q) : Tensor(), Tensor()};
   if (want_table && e.table.defined()) r.dT = at::empty_like(e.table);
   const int64_t bytes = api.ext_bwd_bytes(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, causal, &m.x);
-  const Tensor ws = workspace(bytes, Q);
+  // D lies with the workspace where no second backward reads it
+  const int64_t rows = keep_D ? 0 : (m.B * m.H * m.Nq * 4 + 255) / 256 * 256;
+  const Tensor scratch = workspace(rows + bytes, Q);
+  char* const mem = scratch.defined() ? (char*)pm(scratch) : nullptr;
   ok(api.ext_bwd(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, (float)scale, causal, &m.x, p(Q), p(K), p(V), p(O), p(dO),
-                 f(L), pm(r.dQ), pm(r.dK), pm(r.dV), fm(r.D), r.dT.defined() ? pm(r.dT) : nullptr,
-                 bytes > 0 ? pm(ws) : nullptr, bytes, stream_of(Q)));
+                 f(L), pm(r.dQ), pm(r.dK), pm(r.dV), keep_D ? fm(r.D) : (float*)mem,
+                 r.dT.defined() ? pm(r.dT) : nullptr, mem + rows, bytes, stream_of(Q)));
   return r;
 }
 
@@ -509,7 +514,7 @@ struct ExtAttentionBackward : torch::autograd::Function<ExtAttentionBackward> {
     const auto& [table, buckets, kv_lens, q_lens, q_starts] = e;
     const ExtDims m = ext_dims_or_throw({&q, &O, &dO}, {&k, &v}, {&L}, e);
     c10::OptionalDeviceGuard guard(q.device());
-    ExtBwd r = run_ext_bwd(m, q, k, v, O, dO, L, e, scale, causal, want_table);
+    ExtBwd r = run_ext_bwd(m, q, k, v, O, dO, L, e, scale, causal, want_table, true);
     // dQ as well: an output, and no path of the second backward
     ctx->save_for_backward({q, k, v, table, O, L, dO, r.D, r.dQ.detach(), buckets, kv_lens, q_lens, q_starts});
     ctx->set_materialize_grads(false);
@@ -534,19 +539,22 @@ struct ExtAttentionBackward : torch::autograd::Function<ExtAttentionBackward> {
     c10::OptionalDeviceGuard guard(q.device());
     at::AutoGradMode no_graph(false);
     const void* const gT = ext_cotangent(ut, table);
-    const Tensor Qt = at::empty_like(q), dOt = at::empty_like(q), alpha = rows_like(q), E = rows_like(q);
+    // alpha, E and the workspace of whichever pass runs, in one allocation
+    const int64_t rows = (m.B * m.H * m.Nq * 4 + 255) / 256 * 256;
     const int64_t bytes1 = api.ext_pass1_bytes(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, causal, &m.x);
-    const Tensor ws1 = workspace(bytes1, q);
+    const int64_t bytes2 = api.ext_pass2_bytes(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, causal, &m.x);
+    const Tensor scratch = workspace(2 * rows + std::max(bytes1, bytes2), q);
+    char* const mem = scratch.defined() ? (char*)pm(scratch) : nullptr;
+    float *const alpha = (float*)mem, *const E = (float*)(mem + rows);
+    const Tensor Qt = at::empty_like(q), dOt = at::empty_like(q);
     ok(api.ext_pass1(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, (float)scale, causal, &m.x, p(q), p(k), p(v), p(O),
-                     p(dO), p(uq), p(uk), p(uv), gT, f(L), f(D), p(dQ), pm(Qt), pm(dOt), fm(alpha), fm(E),
-                     bytes1 > 0 ? pm(ws1) : nullptr, bytes1, stream_of(q)));
+                     p(dO), p(uq), p(uk), p(uv), gT, f(L), f(D), p(dQ), pm(Qt), pm(dOt), alpha, E, mem + 2 * rows, bytes1,
+                     stream_of(q)));
     const Tensor Kt = at::empty_like(k), Vt = at::empty_like(k);
     const Tensor Tt = table.defined() && ctx->needs_input_grad(3) ? at::empty_like(table) : Tensor();
-    const int64_t bytes = api.ext_pass2_bytes(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, causal, &m.x);
-    const Tensor ws = workspace(bytes, q);
     ok(api.ext_pass2(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, (float)scale, causal, &m.x, p(q), p(k), p(v), p(dO),
-                     p(uq), p(uk), p(uv), gT, f(L), f(D), f(alpha), f(E), pm(Kt), pm(Vt),
-                     Tt.defined() ? pm(Tt) : nullptr, bytes > 0 ? pm(ws) : nullptr, bytes, stream_of(q)));
+                     p(uq), p(uk), p(uv), gT, f(L), f(D), alpha, E, pm(Kt), pm(Vt), Tt.defined() ? pm(Tt) : nullptr,
+                     mem + 2 * rows, bytes2, stream_of(q)));
     return {Qt, Kt, Vt, Tt, Tensor(), Tensor(), dOt, Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
   }
 };
@@ -575,7 +583,7 @@ struct ExtAttention : torch::autograd::Function<ExtAttention> {
       const ExtDims m = ext_dims_or_throw({&s[0], &s[4], &dO}, {&s[1], &s[2]}, {&s[5]}, e);
       c10::OptionalDeviceGuard guard(s[0].device());
       const ExtBwd r = run_ext_bwd(m, s[0], s[1], s[2], s[4], dO, s[5], e, ctx->saved_data["scale"].toDouble(),
-                                   ctx->saved_data["causal"].toBool(), s[3].defined() && ctx->needs_input_grad(3));
+                                   ctx->saved_data["causal"].toBool(), s[3].defined() && ctx->needs_input_grad(3), false);
       return {r.dQ, r.dK, r.dV, r.dT, Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
     }
     const variable_list d = ExtAttentionBackward::apply(

@@ -2,7 +2,8 @@
 buckets of relative position (the attn_ext_* calls of include/flashbob.h).
 
 `cross_attention` and `biased_attention` are the differentiable layers, with
-first and second derivatives on the HIP path as `attention` has them; the
+first and second derivatives on the HIP path as `attention` has them (third
+ones are not built: the second backward's results carry no graph); the
 attn_ext_* functions are the entry points one by one, under the C names.
 
 Query-side tensors are [B, H, Nq, d], key-side ones [B, Hkv, Nk, d] (H a
