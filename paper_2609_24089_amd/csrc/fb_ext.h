@@ -177,12 +177,14 @@ int32_t ext_dispatch(int form, const ExtProblem& p, dim3 grid, int64_t dynamic, 
 // base: parts that a block has in any case (1, or a group's query heads); others are multiples
 // of `unit`; part_bytes: of fp32 sums that a part of all blocks stores.  A part costs what its
 // sums take to write and to read back at 4 TB/s, all of them the joining launch; only grids
-// of at most two workgroups a compute unit are offered, of four tiles a set or more.  Measured, one part -> chosen: see
+// of at most two workgroups a compute unit are offered, of four tiles a set or more.
+// max_chain: tiles that one accumulator of a column kernel may sum: longer ones drift
+// (SectionSums), so they are split whatever it costs.  Measured, one part -> chosen: see
 // the launchers.
 constexpr double kJoinUs = 6.0;
 template <typename Kern, typename Dynamic>
 void ext_pick(const ExtProblem& p, const FormQuery& q, double narrow, Dynamic&& dynamic, int only, int base,
-              int unit, int64_t part_bytes, ExtPlan* c) {
+              int unit, int64_t part_bytes, ExtPlan* c, int64_t max_chain = int64_t(1) << 40) {
   const bool b = has_bias(p);
   const Form forms[kForms] = {ext_form_of<Kern, 0>(p, dynamic(Kern::shape(0, b)), 1.0),
                               ext_form_of<Kern, 1>(p, dynamic(Kern::shape(1, b)), narrow),
@@ -199,11 +201,14 @@ void ext_pick(const ExtProblem& p, const FormQuery& q, double narrow, Dynamic&& 
     const int64_t blocks = q.heads * ((q.N + 16 * f.blocks - 1) / (16 * f.blocks));
     if (i == 0) fills = f.resident > 1 && blocks * base > q.cus * f.resident;
     if (i > 0 && only < 0 && fills) continue;
+    const auto too_long = [&](int parts) { return q.tiles > max_chain * f.sets * parts; };
     for (int m = 0; m <= 16; m = m == 0 ? 1 : 2 * m) {
       f.parts = m == 0 ? base : unit * m;
       if (m > 0 && f.parts <= base) continue;
       const int64_t total = blocks * f.parts;
-      if (m > 0 && (total > 2 * q.cus || q.tiles < (int64_t)4 * f.sets * f.parts)) break;
+      if (too_long(f.parts) && m < 16) continue;
+      const bool few = total <= 2 * q.cus && q.tiles >= (int64_t)4 * f.sets * f.parts;
+      if (m > 0 && !few && !too_long(base)) break;
       if (total > INT32_MAX / 16 || total * f.threads > (int64_t)UINT32_MAX) continue;
       double t = form_us(q, f) * (f.parts > base ? 1.08 : i > 0 ? q.margin : 1.0);
       if (f.parts > 1) t += kJoinUs + 2.0 * f.parts * (double)part_bytes / 4.0e6;

@@ -74,7 +74,7 @@ template <typename T, int D> ExtPlan ext_pass2_plan(const ExtProblem& p) {
                     std::max<int64_t>((p.Nq + kBS - 1) / kBS, 1) * grp, triangular(p), block_us<T>(8, D), kP2Step<T>,
                     merge_us(2, D), 1.0};
   ext_pick<C>(p, q, kP2Step<T>.narrow, [&](const ExtShape& s) { return pass2_dynamic(p, s); }, -1, base, grp,
-              2 * p.B * p.Hkv * p.Nk * D * 4, &c);
+              2 * p.B * p.Hkv * p.Nk * D * 4, &c, kLongChain);
   return c;
 }
 

@@ -59,7 +59,7 @@ template <typename T, int D> ExtPlan ext_cols_plan(const ExtProblem& p) {
                     std::max<int64_t>((p.Nq + kBS - 1) / kBS, 1) * grp, triangular(p), block_us<T>(4, D), kColsStep<T>,
                     merge_us(2, D), 1.0};
   ext_pick<C>(p, q, kColsStep<T>.narrow, [&](const ExtShape& s) { return cols_dynamic(p, s); }, -1, base, grp,
-              2 * p.B * p.Hkv * p.Nk * D * 4, &c);
+              2 * p.B * p.Hkv * p.Nk * D * 4, &c, kLongChain);
   return c;
 }
 

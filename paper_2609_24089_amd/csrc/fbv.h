@@ -44,6 +44,7 @@ struct ExtArgs {
   float scale;
   int nparts;
   int resident;        // of balanced_order(): causal grids of a few rounds
+  int fit;             // workgroups of the kernel that fit a compute unit
   const int32_t* q_lens;    // [B] or null: every row is valid
   const int32_t* kv_lens;
   const int32_t* q_starts;  // [B] or null: 0
@@ -107,35 +108,50 @@ __device__ __forceinline__ int ext_side(int lo, int hi, int R) { return hi <= -R
 // ---------------------------------------------------------------------------
 template <int NSTAGE, int LT, bool kBarrier, class Issue, class Pro, class Body>
 __device__ __forceinline__ void ext_stream(int n, Issue&& issue, Pro&& pro, Body&& body) {
-#pragma unroll
-  for (int st = 0; st < NSTAGE - 1; ++st)
-    if (st < n) issue(st, st);
-  pro();
-  wait_copies<true>();
-  __syncthreads();
-  auto step = [&](int k, auto cur) {
-    constexpr int kCur = decltype(cur)::value;
-    constexpr int kNext = kCur == 0 ? NSTAGE - 1 : kCur - 1;
-    const int nx = k + NSTAGE - 1;
-    if (nx < n) issue(nx, kNext);
-    body(k, kCur);
-    // without a barrier the wave's own reads of this stage have to be back before the
-    // next copy into it is issued (lgkmcnt(0), the other counters at their maxima)
-    if constexpr (!kBarrier) __builtin_amdgcn_s_waitcnt(0xc07f);
-    if (NSTAGE > 2 && nx < n)
-      wait_vm<(NSTAGE - 2) * LT>();
-    else
+  static_assert(NSTAGE == 2 || (NSTAGE == 4 && !kBarrier), "ring depth");
+  if constexpr (kBarrier) {
+    if (n > 0) issue(0, 0);
+    pro();
+    wait_copies<true>();
+    __syncthreads();
+    auto step = [&](int k, auto cur) {
+      constexpr int kCur = decltype(cur)::value;
+      if (k + 1 < n) issue(k + 1, 1 - kCur);
+      body(k, kCur);
       wait_copies<true>();
-    if constexpr (kBarrier) __syncthreads();
-  };
-  static_assert(NSTAGE >= 2 && NSTAGE <= 4, "ring depth");
-  for (int k = 0; k < n; k += NSTAGE) {
-    step(k, std::integral_constant<int, 0>{});
-    if (k + 1 < n) step(k + 1, std::integral_constant<int, 1>{});
-    if constexpr (NSTAGE > 2)
-      if (k + 2 < n) step(k + 2, std::integral_constant<int, 2>{});
-    if constexpr (NSTAGE > 3)
-      if (k + 3 < n) step(k + 3, std::integral_constant<int, 3>{});
+      __syncthreads();
+    };
+    for (int k = 0; k < n; k += 2) {
+      step(k, std::integral_constant<int, 0>{});
+      if (k + 1 < n) step(k + 1, std::integral_constant<int, 1>{});
+    }
+  } else {
+    // the whole ring is in flight at the start, and a stage is filled again as soon as its
+    // tile is done: the wave's own reads of it have to be back before (lgkmcnt(0), the other
+    // counters at their maxima)
+#pragma unroll
+    for (int st = 0; st < NSTAGE; ++st)
+      if (st < n) issue(st, st);
+    pro();
+    __syncthreads();
+    auto step = [&](int k, auto cur) {
+      constexpr int kCur = decltype(cur)::value;
+      if (k + NSTAGE - 1 < n)
+        wait_vm<(NSTAGE - 1) * LT>();
+      else
+        wait_copies<true>();
+      body(k, kCur);
+      __builtin_amdgcn_s_waitcnt(0xc07f);
+      if (k + NSTAGE < n) issue(k + NSTAGE, kCur);
+    };
+    for (int k = 0; k < n; k += NSTAGE) {
+      step(k, std::integral_constant<int, 0>{});
+      if (k + 1 < n) step(k + 1, std::integral_constant<int, 1>{});
+      if constexpr (NSTAGE > 2) {
+        if (k + 2 < n) step(k + 2, std::integral_constant<int, 2>{});
+        if (k + 3 < n) step(k + 3, std::integral_constant<int, 3>{});
+      }
+    }
   }
 }
 
@@ -157,6 +173,17 @@ struct ExtRun {
   }
   __device__ __forceinline__ int size() const { return end - begin; }
 };
+
+// The parts that split a row block's tiles, of nparts: each set of a part gets four tiles at
+// least, the parts beyond take none.
+__device__ __forceinline__ int ext_parts_of(int tiles, int sets, int nparts) {
+  return min(max(tiles / (4 * sets), 1), nparts);
+}
+// The run of set ks of part `part`.
+__device__ __forceinline__ ExtRun ext_run(int tiles, int part, int split, int ks, int sets) {
+  ExtRun r(tiles, min(part, split) * sets + ks, split * sets);
+  return r;
+}
 
 // What a row kernel's workgroup and wave know of their rows.  kFold: the kernel may run
 // folded rows (a.fold); the others keep one lane position instead of one a 16-row block.
@@ -206,26 +233,55 @@ struct ExtRows {
   __device__ __forceinline__ int mode(int s0) const { return s0 > hi ? 0 : s0 + kBS - 1 <= lo ? 1 : 2; }
 };
 
+// The batch entry with the `rank`-th largest length (equal ones in order), 2 to 64 entries:
+// each lane ranks one.
+__device__ __forceinline__ int entry_of_rank(const int32_t* lens, int entries, int limit, int rank) {
+  const int l = lane_id();
+  const int n = l < entries ? min(max(lens[l], 0), limit) : -1;
+  int above = 0;
+  for (int q = 0; q < entries; ++q) {
+    const int other = __builtin_amdgcn_readlane(n, q);
+    above += other > n || (other == n && q < l) ? 1 : 0;
+  }
+  return __builtin_ctzll(__builtin_amdgcn_ballot_w64(l < entries && above == rank));
+}
+
 // Which block a workgroup runs.  As map_block, one head's blocks stay on one XCD, whose L2
 // its key/value head's tensors then pass once; but units of heads that share a key/value
 // head go round the XCDs one by one where their number allows it, so that the entries of a
-// ragged batch spread over all of them: in map_block's runs of consecutive heads an XCD
-// got the longest entry's heads and another the shortest's (B8 H16 Nq512 Nk2048 d64, half to
-// full lengths, forward: 46 us in runs).  Causal grids of a few rounds run in
-// map_block_causal's order.  `per`: blocks of one unit.
-__device__ __forceinline__ void ext_map_block(const ExtArgs& a, int per, bool last_heavy, int& head, int& rb) {
+// ragged batch spread over all of them (in map_block's runs of consecutive heads an XCD got
+// the longest entry's heads and another the shortest's: 3 to 10% slower on such batches).
+// `lens`: the streamed side's lengths, or null.  With them the longest entries' blocks start
+// first, and in the rounds that become resident together each XCD deals them to its CUs in
+// alternating direction, as map_block_causal does: a CU gets a long block and a short one.
+// Causal grids of a few rounds run in map_block_causal's order.  `per`: blocks of one unit.
+__device__ __forceinline__ void ext_map_block(const ExtArgs& a, int per, bool last_heavy, const int32_t* lens, int limit,
+                                              int& head, int& rb) {
   if (a.resident > 0) {
     map_block_causal(a.nRB, a.total, a.resident, last_heavy, head, rb);
     return;
   }
-  const int units = a.total / per;
+  const int units = a.total / per, entry_units = a.H / a.grp, entries = units / entry_units;
   if (units % kXCDs != 0) {
     map_block(a.nRB, a.total, head, rb, last_heavy && a.causal != 0);
     return;
   }
-  const int xcd = blockIdx.x % kXCDs, i = blockIdx.x / kXCDs;
-  const int u = i / per, at = i - u * per, h = at / a.nRB;
-  head = (u * kXCDs + xcd) * (per / a.nRB) + h;
+  const int xcd = blockIdx.x % kXCDs;
+  int i = blockIdx.x / kXCDs;
+  const bool ranked = lens != nullptr && entries > 1 && entries <= 64;
+  if (ranked) {
+    const int round = i / kCUsPerXCD, first = round * kCUsPerXCD;
+    const int m = min(kCUsPerXCD, a.total / kXCDs - first);
+    if ((round & 1) != 0 && round < a.fit) i = first + m - 1 - (i - first);
+  }
+  int u = i / per;
+  const int at = i - u * per, h = at / a.nRB;
+  u = u * kXCDs + xcd;
+  if (ranked) {
+    const int rank = u / entry_units;
+    u += (entry_of_rank(lens, entries, limit, rank) - rank) * entry_units;
+  }
+  head = u * (per / a.nRB) + h;
   rb = at - h * a.nRB;
   if (last_heavy && a.causal != 0) rb = a.nRB - 1 - rb;
 }
@@ -242,7 +298,7 @@ __device__ __forceinline__ void ext_mask1(floatx4 (&x)[2], int s0, int klim) {
 // ===========================================================================
 // Forward.  As attn_fwd_kernel (online softmax against a lazily moved reference), over the
 // keys of another sequence, with the bias.  A part (gridDim.y of them) takes a run of the
-// key tiles and stores its unnormalised sums, reference and weight instead of O and L;
+// key tiles (none, if the block has few) and stores its unnormalised sums, reference and weight instead of O and L;
 // ext_fwd_join_kernel joins them.  One wave a set (NW = 1) runs without barriers: the form
 // of a few query rows against a long cache, which reads each key and value once.
 // ===========================================================================
@@ -258,7 +314,8 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_fwd_kernel(
   float FB_LDS* const steps = (float FB_LDS*)steps_mem;
 
   int rh, rb;
-  ext_map_block(a, a.fold != 0 ? a.nRB : a.grp * a.nRB, true, rh, rb);
+  // a few rows a head: every workgroup is resident, whatever the order
+  ext_map_block(a, a.fold != 0 ? a.nRB : a.grp * a.nRB, true, NW == 1 ? nullptr : a.kv_lens, a.Nk, rh, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
   const int wl = __builtin_amdgcn_readfirstlane(KS == 1 ? wave_id() : wave_id() % NW);
@@ -353,8 +410,8 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_fwd_kernel(
 
   const T* const src[2] = {K + kvoff, V + kvoff};
   // every set of a workgroup with barriers runs as long as its first, whose run is the longest
-  const ExtRun run(rw.tiles, part * KS + ks, a.nparts * KS);
-  const ExtRun first(rw.tiles, part * KS, a.nparts * KS);
+  const int split = ext_parts_of(rw.tiles, KS, a.nparts);
+  const ExtRun run = ext_run(rw.tiles, part, split, ks, KS), first = ext_run(rw.tiles, part, split, 0, KS);
   constexpr bool kBarrier = NW > 1;
   const int iters = kBarrier ? first.size() : run.size();
   const TileCopy<T, D, NW, 2> copy(wl);
@@ -490,8 +547,8 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_fwd_kernel(
 // Joins the parts of the forward: every part's sums brought to the largest reference.
 // One thread for four head dims of a row.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void ext_fwd_join_kernel(const float* __restrict__ parts, int nparts, int64_t all,
-                                                           ExtArgs a, T* __restrict__ O, float* __restrict__ L) {
+__global__ __launch_bounds__(256) void ext_fwd_join_kernel(ExtArgs a, const float* __restrict__ parts, int64_t all,
+                                                           T* __restrict__ O, float* __restrict__ L) {
   using E = Elt<T>;
   constexpr int kPer = D / 4;
   const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -500,12 +557,12 @@ __global__ __launch_bounds__(256) void ext_fwd_join_kernel(const float* __restri
   if (row >= all) return;
   const int64_t bh = row / a.Nq;
   const bool ok = (int)(row - bh * a.Nq) < ext_lens(a, (int)(bh / a.H)).q;
-  const float* const ml = parts + nparts * all * D;
+  const float* const ml = parts + a.nparts * all * D;
   floatx4 sum = floatx4{0.f, 0.f, 0.f, 0.f};
   float m = -1e30f, w = 0.f;
   if (ok) {
-    for (int q = 0; q < nparts; ++q) m = fmaxf(m, ml[2 * (q * all + row)]);
-    for (int q = 0; q < nparts; ++q) {
+    for (int q = 0; q < a.nparts; ++q) m = fmaxf(m, ml[2 * (q * all + row)]);
+    for (int q = 0; q < a.nparts; ++q) {
       const int64_t at = q * all + row;
       const float f = fast_exp2(ml[2 * at] - m);
       w = __builtin_fmaf(ml[2 * at + 1], f, w);
@@ -529,7 +586,7 @@ __global__ __launch_bounds__(256) void ext_fwd_join_kernel(const float* __restri
 template <typename T, int D, int MR, int NW, int OCC, int NSTAGE, int KS, bool kBias>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
     ExtArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ O,
-    const T* __restrict__ dO, const float* __restrict__ L, T* __restrict__ dQ, float* __restrict__ Dout) {
+    const T* __restrict__ dO, const float* __restrict__ L, T* __restrict__ dQ, float* __restrict__ Dout, float* __restrict__ parts) {
   using E = Elt<T>;
   using G = Geo<T, D>;
   constexpr int BR = 16 * MR * NW;
@@ -538,7 +595,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
   float FB_LDS* const steps = (float FB_LDS*)steps_mem;
 
   int rh, rb;
-  ext_map_block(a, a.grp * a.nRB, true, rh, rb);
+  ext_map_block(a, a.grp * a.nRB, true, a.kv_lens, a.Nk, rh, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
   const int wl = __builtin_amdgcn_readfirstlane(KS == 1 ? wave_id() : wave_id() % NW);
@@ -575,7 +632,8 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
   typename E::TFrag dsf[MR];
 
   const T* const src[2] = {K + kvoff, V + kvoff};
-  const ExtRun run(rw.tiles, ks, KS), first(rw.tiles, 0, KS);
+  const int part = blockIdx.y, split = ext_parts_of(rw.tiles, KS, a.nparts);
+  const ExtRun run = ext_run(rw.tiles, part, split, ks, KS), first = ext_run(rw.tiles, part, split, 0, KS);
   constexpr bool kBarrier = NW > 1;
   const TileCopy<T, D, NW, 2> copy(wl);
   float blo = 0.f, bhi = 0.f;
@@ -712,6 +770,20 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
     merge_sets<KS, NW>(acc, ks, wl, (floatx4 FB_LDS*)&sm.lds[0][0][0]);
   }
   const RowSplit<KS> own{ks, 0};
+  if (a.nparts > 1) {
+    const int64_t all = (int64_t)(a.total / a.nRB) * rw.rows;
+    float* const sc = parts + a.nparts * all * D;
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb)
+      if (rw.ok(mb)) {
+        const int64_t at = part * all + rw.qrow + rw.row(mb);
+#pragma unroll
+        for (int nb = 0; nb < G::kNB; ++nb)
+          if (own.owns(nb)) *(floatx4*)(parts + at * D + 16 * nb + 4 * g) = acc[nb][mb];
+        if (g == 0 && ks == 0) sc[at] = (part == 0 ? dout[mb] : 0.f) + rest[mb];
+      }
+    return;
+  }
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb) {
     if (rw.row(mb) >= rw.rows) continue;
@@ -722,6 +794,31 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
         E::store4(dQ + at * D + 16 * nb + 4 * g, rw.ok(mb) ? acc[nb][mb] * a.scale : floatx4{0.f, 0.f, 0.f, 0.f});
     if (g == 0 && ks == 0) Dout[at] = rw.ok(mb) ? dout[mb] + rest[mb] : 0.f;
   }
+}
+
+// Adds the parts of the row side: dQ = tau times the sums, D their scalars' sum.  One
+// thread for four head dims of a row.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void ext_bwd_join_kernel(ExtArgs a, const float* __restrict__ parts, int64_t all,
+                                                           T* __restrict__ dQ, float* __restrict__ Dout) {
+  constexpr int kPer = D / 4;
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = x / kPer;
+  const int dim = 4 * (int)(x % kPer);
+  if (row >= all) return;
+  const int64_t bh = row / a.Nq;
+  floatx4 sum = floatx4{0.f, 0.f, 0.f, 0.f};
+  float d = 0.f;
+  if ((int)(row - bh * a.Nq) < ext_lens(a, (int)(bh / a.H)).q) {
+    const float* const sc = parts + a.nparts * all * D;
+    for (int q = 0; q < a.nparts; ++q) {
+      const int64_t at = q * all + row;
+      sum += *(const floatx4*)(parts + at * D + dim);
+      d += sc[at];
+    }
+  }
+  Elt<T>::store4(dQ + row * D + dim, sum * a.scale);
+  if (dim == 0) Dout[row] = d;
 }
 
 // ===========================================================================
@@ -797,15 +894,16 @@ __device__ __forceinline__ void ext_mask_cols(floatx4 (&x)[2][MC], int s0, int t
 // key and first query.  buf: kBufFloats floats of LDS of this wave.  out: 2 R + 3 sums:
 // steps -R .. R, then all below -R, then all above R.
 struct StepSums {
-  static constexpr int kStride = 36, kBufFloats = 16 * kStride;
+  static constexpr int kStride = 76, kBufFloats = 4 * kStride;
   float* out;
   int R;
   float carry, below, above;  // the window below the last near tile's; the far sums
   // The row starts at zero: the loop's first wait for its copies waits for these stores too.
-  __device__ __forceinline__ void init(float* row, int r) {
+  __device__ __forceinline__ void init(float* row, int r, float FB_LDS* buf) {
     out = row;
     R = r;
     carry = below = above = 0.f;
+    for (int x = lane_id(); x < kBufFloats; x += 64) buf[x] = 0.f;  // columns that no tile writes stay so
     for (int x = lane_id(); x < 2 * R + 1; x += 64) out[x] = 0.f;
   }
   // The sums of steps at .. at + 31, one a lane; every window is stored once.
@@ -838,32 +936,40 @@ struct StepSums {
     else
       above += sum;
   }
+  // The sum of a 16x16 block x_r (query 4 g + r, key j) along its diagonals for one lane
+  // group g: same[c] over key - r = c, next[c] over key - r = c - 16.
+  static __device__ __forceinline__ void diagonals(floatx4 x, float& same, float& next) {
+    same = shifted<0x101>(shifted<0x101>(shifted<0x101>(x[3]) + x[2]) + x[1]) + x[0];  // lane c takes lane c + 1
+    next = shifted<0x11f>(x[1]) + (shifted<0x11e>(x[2]) + shifted<0x11d>(x[3]));       // lane c takes c - 15, - 14, - 13
+  }
+  template <int kCtrl> static __device__ __forceinline__ float shifted(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kCtrl, 0xf, 0xf, true));
+  }
+  // A tile with steps of their own sums.  Blocks of equal key - query are added first, each
+  // is summed along its diagonals inside its lane group by shifts in the row of 16 lanes,
+  // and the four groups, whose steps lie 4 apart, meet in LDS: row g of the buffer holds its
+  // 64 sums 4 g to the left, so that lane l finds step l - 32 in one column.  (Summing the
+  // diagonals from a whole tile in LDS, 16 reads and 110 vector instructions for 4 and 35,
+  // took B8 H12 N512 d64, all of it near, 41 us for the column kernel.)
   template <int MC>
   __device__ __forceinline__ void near(const floatx4 (&x)[2][MC], int base, float FB_LDS* buf) {
     int l = lane_id();
-    asm volatile("" : "+v"(l));  // the addresses below are made per tile: kept, they cost 20 registers
-    const int g = l >> 4, j = l & 15, cls = l & 31, half = l >> 5;
-    // lane l sums the pairs whose step is l mod 32: those at base + cls (up) and at
-    // base + cls - 32 (down); the two halves of the wave take eight keys each
-    float up = 0.f, down = 0.f;
-#pragma unroll
-    for (int mc = 0; mc < MC; ++mc) {
-#pragma unroll
-      for (int sb = 0; sb < 2; ++sb) *(floatx4 FB_LDS*)(buf + kStride * j + 16 * sb + 4 * g) = x[sb][mc];
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int k = 8 * half + u, key = 16 * mc + k;
-        const float v = buf[kStride * k + ((key - cls) & 31)];
-        if (key >= cls)
-          up += v;
-        else
-          down += v;
-      }
-    }
-    up += __shfl_xor(up, 32);
-    down += __shfl_xor(down, 32);
-    emit(base, up + carry);
-    carry = down;
+    asm volatile("" : "+v"(l));  // the addresses are made anew in every tile, not kept
+    float a0, n0, am, nm, a1 = 0.f, n1 = 0.f;
+    diagonals(MC == 2 ? x[0][0] + x[1][MC - 1] : x[0][0], a0, n0);
+    diagonals(x[1][0], am, nm);
+    if constexpr (MC == 2) diagonals(x[0][1], a1, n1);
+    float FB_LDS* const to = buf + (kStride - 4) * (l >> 4) + (l & 15) + 12;  // row g, 4 g to the left
+    to[0] = nm;
+    to[16] = am + n0;
+    to[32] = a0 + n1;
+    if constexpr (MC == 2) to[48] = a1;
+    const float FB_LDS* const from = buf + l + 12;
+    const float sum = (from[0] + from[kStride]) + (from[2 * kStride] + from[3 * kStride]);
+    // lanes 32 .. 63: the upper window, which no later tile meets
+    const float other = __shfl_xor(sum, 32);
+    emit(base, (l < 32 ? other : sum) + carry);
+    carry = sum;
   }
   // last: `base` of the last tile of the run (of any tile if the run is empty)
   __device__ __forceinline__ void finish(int last) {
@@ -892,7 +998,7 @@ struct ExtColMem {
     if constexpr (kBias) {
       const int n = (ext_steps(a) + 3) & ~3;
       dirs = steps + n;
-      buf = steps + (kDir ? 2 : 1) * n + wave_id() * StepSums::kBufFloats;
+      buf = steps + (kDir ? 2 : 1) * n + __builtin_amdgcn_readfirstlane(wave_id()) * StepSums::kBufFloats;
       ext_fill_steps<true>(a, a.table, head, 1, steps, KS * NW * 64);
       if constexpr (kDir) ext_fill_steps<false>(a, a.dir, head, 1, dirs, KS * NW * 64);
     }
@@ -975,7 +1081,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_cols_kernel(
   extern __shared__ float steps_mem[];
 
   int kv, rb;
-  ext_map_block(a, a.nRB, false, kv, rb);
+  ext_map_block(a, a.nRB, false, a.q_lens, a.Nq, kv, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
   const int wl = __builtin_amdgcn_readfirstlane(KS == 1 ? wave_id() : wave_id() % NW);
@@ -999,7 +1105,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_cols_kernel(
   const ExtColMem<kBias, KS, NW, false> mem(steps_mem, a, cl.hq - cl.b * a.H);
   StepSums tab;
   if constexpr (kBias)
-    if (sums != nullptr) tab.init(ext_step_row(sums, a, cl.hq, cl.b, rb, cl.sub, cl.subs, KS * NW), a.R);
+    if (sums != nullptr) tab.init(ext_step_row(sums, a, cl.hq, cl.b, rb, cl.sub, cl.subs, KS * NW), a.R, mem.buf);
   floatx4 dk[G::kNB][MC], dv[G::kNB][MC];
 #pragma unroll
   for (int nb = 0; nb < G::kNB; ++nb)
@@ -1104,8 +1210,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_cols_kernel(
         }
         if constexpr (kBias) {
           if (side == 0) {
-            int jj = j - 4 * g; asm volatile("" : "+v"(jj));
-            const float FB_LDS* bias = mem.steps + (a.R + kStepPad + base + jj - 19);
+            const float FB_LDS* bias = mem.steps + (a.R + kStepPad + base + j - 4 * g - 19);
 #pragma unroll
             for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
@@ -1173,7 +1278,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
     ExtArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ O,
     const T* __restrict__ dO, const T* __restrict__ UQ, const T* __restrict__ UK, const T* __restrict__ UV,
     const float* __restrict__ L, const float* __restrict__ Dv, const T* __restrict__ dQ, T* __restrict__ Qt,
-    T* __restrict__ dOt, float* __restrict__ alpha_out, float* __restrict__ E_out) {
+    T* __restrict__ dOt, float* __restrict__ alpha_out, float* __restrict__ E_out, float* __restrict__ parts) {
   using E = Elt<T>;
   using G = Geo<T, D>;
   constexpr int BR = 16 * MR * NW;
@@ -1184,7 +1289,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
   float FB_LDS* const dirs = steps + (kBias ? (ext_steps(a) + 3) & ~3 : 0);
 
   int rh, rb;
-  ext_map_block(a, a.grp * a.nRB, true, rh, rb);
+  ext_map_block(a, a.grp * a.nRB, true, a.kv_lens, a.Nk, rh, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
   // scalar, one set at d = 64 takes 174 registers for 166 and loses its third wave per SIMD
@@ -1218,14 +1323,16 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
   using AF = typename E::AFrag;
 
   const T* const src[4] = {K + kvoff, V + kvoff, UK + kvoff, UV + kvoff};
-  const ExtRun run(rw.tiles, ks, KS), first(rw.tiles, 0, KS);
+  const int part = blockIdx.y, split = ext_parts_of(rw.tiles, KS, a.nparts);
+  const ExtRun run = ext_run(rw.tiles, part, split, ks, KS), first = ext_run(rw.tiles, part, split, 0, KS);
   constexpr bool kBarrier = NW > 1 || KS > 1;  // the sets meet in the first tile
   const TileCopy<T, D, NW, 4> copy(wl);
   float blo = 0.f, bhi = 0.f, ulo = 0.f, uhi = 0.f;
   float aref[MR], eref[MR];
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb) aref[mb] = eref[mb] = 0.f;
-  bool centred = false;
+  // parts that share a block take their sums from 0: each row of theirs has many keys in view
+  bool centred = split > 1;
   ext_stream<2, tile_loads<T, D, NW, 4>(), kBarrier>(
       kBarrier ? first.size() : run.size(),
       [&](int it, int st) {
@@ -1247,7 +1354,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
         const int s0 = min(run.begin + it, rw.tiles - 1) * kBS;
         int mode = run.begin + it < run.end ? rw.mode(s0) : 0;
         if constexpr (KS > 1) mode = vector_mode(mode);
-        if (mode == 0 && (KS == 1 || it > 0)) return;
+        if (mode == 0 && (KS == 1 || it > 0 || split > 1)) return;
         const T FB_LDS* Ks = (const T FB_LDS*)sm.lds[ks][st];
         const T FB_LDS* Vs = Ks + G::kTileElems;
         const T FB_LDS* UKs = Vs + G::kTileElems;
@@ -1326,7 +1433,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
           }
         }
         // every wave of a workgroup with sets comes here in its first iteration (a barrier)
-        if (KS > 1 ? it == 0 : !centred) {
+        if (KS > 1 ? it == 0 && split == 1 : !centred) {
           centred = true;
 #pragma unroll
           for (int mb = 0; mb < MR; ++mb) {
@@ -1456,6 +1563,25 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
     merge_sets<KS, NW>(aB, ks, wl, buf);
   }
   const RowSplit<KS> own{ks, 0};
+  if (a.nparts > 1) {
+    const int64_t all = (int64_t)(a.total / a.nRB) * rw.rows;
+    float* const sc = parts + a.nparts * all * (3 * D);
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb)
+      if (rw.ok(mb)) {
+        const int64_t at = part * all + rw.qrow + rw.row(mb);
+#pragma unroll
+        for (int nb = 0; nb < G::kNB; ++nb)
+          if (own.owns(nb)) {
+            float* const to = parts + at * (3 * D) + 16 * nb + 4 * g;
+            *(floatx4*)to = aDO[nb][mb];
+            *(floatx4*)(to + D) = aOM[nb][mb];
+            *(floatx4*)(to + 2 * D) = aB[nb][mb];
+          }
+        if (g == 0 && ks == 0) *(floatx4*)(sc + 4 * at) = floatx4{alpha[mb], e0[mb], aref[mb], eref[mb]};
+      }
+    return;
+  }
   const floatx4 zero = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb) {
@@ -1481,6 +1607,46 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
   }
 }
 
+// Adds the parts of Pass 1 and finishes its rows.  One thread for four head dims of a row.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void ext_pass1_join_kernel(ExtArgs a, const float* __restrict__ parts, int64_t all,
+                                                             const T* __restrict__ O, const float* __restrict__ Dv,
+                                                             const T* __restrict__ dQ, T* __restrict__ Qt,
+                                                             T* __restrict__ dOt, float* __restrict__ alpha_out,
+                                                             float* __restrict__ E_out) {
+  using E = Elt<T>;
+  constexpr int kPer = D / 4;
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = x / kPer;
+  const int dim = 4 * (int)(x % kPer);
+  if (row >= all) return;
+  const int64_t bh = row / a.Nq, off = row * D + dim;
+  const bool ok = (int)(row - bh * a.Nq) < ext_lens(a, (int)(bh / a.H)).q;
+  const floatx4 zero = floatx4{0.f, 0.f, 0.f, 0.f};
+  floatx4 d = zero, om = zero, b = zero, sc = zero;
+  if (ok) {
+    const float* const scalars = parts + a.nparts * all * (3 * D);
+    for (int q = 0; q < a.nparts; ++q) {
+      const int64_t at = q * all + row;
+      const float* const from = parts + at * (3 * D) + dim;
+      d += *(const floatx4*)from;
+      om += *(const floatx4*)(from + D);
+      b += *(const floatx4*)(from + 2 * D);
+      sc += *(const floatx4*)(scalars + 4 * at);
+    }
+    E::store4(dOt + off, d - sc[0] * E::load4(O + off));
+    E::store4(Qt + off, a.scale * (om - sc[1] * b) - sc[0] * E::load4(dQ + off));
+  } else {
+    E::store4(dOt + off, zero);
+    E::store4(Qt + off, zero);
+  }
+  if (dim == 0) {
+    const float al = sc[2] + sc[0];
+    alpha_out[row] = al;
+    E_out[row] = ok ? sc[3] + sc[1] - al * Dv[row] : 0.f;
+  }
+}
+
 // ===========================================================================
 // BoB Pass 2: as bob_pass2_kernel, with the second-order table sums (`sums`, or null).
 // ===========================================================================
@@ -1501,7 +1667,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass2_kernel(
   extern __shared__ float steps_mem[];
 
   int kv, rb;
-  ext_map_block(a, a.nRB, false, kv, rb);
+  ext_map_block(a, a.nRB, false, a.q_lens, a.Nq, kv, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
   const int wl = __builtin_amdgcn_readfirstlane(KS == 1 ? wave_id() : wave_id() % NW);
@@ -1520,7 +1686,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass2_kernel(
   const ExtColMem<kBias, KS, NW, true> mem(steps_mem, a, cl.hq - cl.b * a.H);
   StepSums tab;
   if constexpr (kBias)
-    if (sums != nullptr) tab.init(ext_step_row(sums, a, cl.hq, cl.b, rb, cl.sub, cl.subs, KS * NW), a.R);
+    if (sums != nullptr) tab.init(ext_step_row(sums, a, cl.hq, cl.b, rb, cl.sub, cl.subs, KS * NW), a.R, mem.buf);
   floatx4 aK[G::kNB][MC], aV[G::kNB][MC];
 #pragma unroll
   for (int nb = 0; nb < G::kNB; ++nb)
