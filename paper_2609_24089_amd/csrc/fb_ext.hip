@@ -107,8 +107,9 @@ static int32_t ext_check(const ExtProblem& p, bool* empty) {
   if (p.Nq > kMaxN || p.Nk > kMaxN) return BOB_EINVAL;
   // 2^30 rows of all heads: a launch takes fewer than 2^32 threads, and the whole blocks have
   // 64 rows or more in 256 threads.  A column block streams a group's query tiles in one loop.
+  if (p.B > INT32_MAX || p.H > 65535) return BOB_EINVAL;
   const int64_t heads = p.B * p.H, rows = std::max(p.Nq, p.Nk);
-  if (p.B > INT32_MAX || p.H > 65535 || heads > INT32_MAX) return BOB_EINVAL;
+  if (heads > INT32_MAX) return BOB_EINVAL;
   if (heads * ((rows + 63) / 64) >= int64_t(1) << 24) return BOB_EINVAL;
   if (ext_group(p) * p.Nq > INT32_MAX / 2) return BOB_EINVAL;
   return BOB_OK;

@@ -505,6 +505,22 @@ using Maybe = std::optional<Tensor>;
 Maybe maybe(const Tensor& t) { return t.defined() ? Maybe(t) : Maybe(); }
 Tensor get(const Maybe& t) { return t.has_value() ? *t : Tensor(); }
 
+// The second backward's results, tied to what they depend on: third derivatives are not
+// built, and asking for one has to fail, not to leave out these terms.
+struct ExtSecond : torch::autograd::Function<ExtSecond> {
+  static variable_list forward(AutogradContext* ctx, const Tensor& Qt, const Tensor& Kt, const Tensor& Vt,
+                               const Tensor& dOt, const Maybe& Tt, const Tensor& q, const Tensor& k, const Tensor& v,
+                               const Maybe& table, const Tensor& dO, const Maybe& uq, const Maybe& uk, const Maybe& uv,
+                               const Maybe& ut) {
+    variable_list out{Qt, Kt, Vt, dOt};
+    if (Tt.has_value()) out.push_back(*Tt);
+    return out;
+  }
+  static variable_list backward(AutogradContext* ctx, variable_list g) {
+    TORCH_CHECK_NOT_IMPLEMENTED(false, "third derivatives of cross_attention and biased_attention are not built");
+  }
+};
+
 struct ExtAttentionBackward : torch::autograd::Function<ExtAttentionBackward> {
   static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& v,
                                const Maybe& table_, const Tensor& O, const Tensor& L, const Tensor& dO,
@@ -537,7 +553,7 @@ struct ExtAttentionBackward : torch::autograd::Function<ExtAttentionBackward> {
     const Tensor ut = g.size() > 3 && g[3].defined() ? g[3].contiguous() : Tensor();
     const ExtDims m = ext_dims_or_throw({&q, &O, &dO, &uq, &dQ}, {&k, &v, &uk, &uv}, {&L, &D}, e);
     c10::OptionalDeviceGuard guard(q.device());
-    at::AutoGradMode no_graph(false);
+    const bool graph = at::GradMode::is_enabled();
     const void* const gT = ext_cotangent(ut, table);
     // alpha, E and the workspace of whichever pass runs, in one allocation
     const int64_t rows = (m.B * m.H * m.Nq * 4 + 255) / 256 * 256;
@@ -546,15 +562,21 @@ struct ExtAttentionBackward : torch::autograd::Function<ExtAttentionBackward> {
     const Tensor scratch = workspace(2 * rows + std::max(bytes1, bytes2), q);
     char* const mem = scratch.defined() ? (char*)pm(scratch) : nullptr;
     float *const alpha = (float*)mem, *const E = (float*)(mem + rows);
-    const Tensor Qt = at::empty_like(q), dOt = at::empty_like(q);
+    Tensor Qt = at::empty_like(q), dOt = at::empty_like(q);
     ok(api.ext_pass1(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, (float)scale, causal, &m.x, p(q), p(k), p(v), p(O),
                      p(dO), p(uq), p(uk), p(uv), gT, f(L), f(D), p(dQ), pm(Qt), pm(dOt), alpha, E, mem + 2 * rows, bytes1,
                      stream_of(q)));
-    const Tensor Kt = at::empty_like(k), Vt = at::empty_like(k);
-    const Tensor Tt = table.defined() && ctx->needs_input_grad(3) ? at::empty_like(table) : Tensor();
+    Tensor Kt = at::empty_like(k), Vt = at::empty_like(k);
+    Tensor Tt = table.defined() && ctx->needs_input_grad(3) ? at::empty_like(table) : Tensor();
     ok(api.ext_pass2(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, (float)scale, causal, &m.x, p(q), p(k), p(v), p(dO),
                      p(uq), p(uk), p(uv), gT, f(L), f(D), alpha, E, pm(Kt), pm(Vt), Tt.defined() ? pm(Tt) : nullptr,
                      mem + 2 * rows, bytes2, stream_of(q)));
+    if (graph) {
+      const variable_list r = ExtSecond::apply(Qt, Kt, Vt, dOt, maybe(Tt), q, k, v, maybe(table), dO, maybe(g[0]),
+                                               maybe(g[1]), maybe(g[2]), maybe(ut));
+      Qt = r[0], Kt = r[1], Vt = r[2], dOt = r[3];
+      if (Tt.defined()) Tt = r[4];
+    }
     return {Qt, Kt, Vt, Tt, Tensor(), Tensor(), dOt, Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
   }
 };

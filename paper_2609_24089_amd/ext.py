@@ -3,8 +3,7 @@ buckets of relative position (the attn_ext_* calls of include/flashbob.h).
 
 `cross_attention` and `biased_attention` are the differentiable layers, with
 first and second derivatives on the HIP path as `attention` has them (third
-ones are not built: the second backward's results carry no graph); the
-attn_ext_* functions are the entry points one by one, under the C names.
+ones are not built and raise NotImplementedError); the attn_ext_* functions are the entry points one by one, under the C names.
 
 Query-side tensors are [B, H, Nq, d], key-side ones [B, Hkv, Nk, d] (H a
 multiple of Hkv), contiguous bf16 or fp32 on the ROCm device.  Per batch entry
@@ -282,7 +281,22 @@ class _ExtBackwardFn(torch.autograd.Function):
         Qt, dOt, alpha, E = attn_ext_pass1_rows(q, k, v, O, dO, *cot, L, D, dq, ctx.scale, ctx.causal, **more)
         Kt, Vt, Tt = attn_ext_pass2_cols(q, k, v, dO, *cot, L, D, alpha, E, ctx.scale, ctx.causal,
                                          want_table=ctx.needs_input_grad[3], **more)
+        if torch.is_grad_enabled():
+            Qt, Kt, Vt, dOt, Tt = _ExtSecondFn.apply(Qt, Kt, Vt, dOt, Tt, q, k, v, table, dO, gdq, gdk, gdv, gdt)
         return Qt, Kt, Vt, Tt, None, None, None, None, None, None, dOt, None, None, None
+
+
+class _ExtSecondFn(torch.autograd.Function):
+    """The second backward's results, tied to what they depend on: asking for a
+    third derivative has to fail, not to leave out these terms."""
+
+    @staticmethod
+    def forward(ctx, Qt, Kt, Vt, dOt, Tt, *depends):
+        return Qt, Kt, Vt, dOt, Tt
+
+    @staticmethod
+    def backward(ctx, *g):
+        raise NotImplementedError("third derivatives of cross_attention and biased_attention are not built")
 
 
 def _layer(q, k, v, table, buckets, scale, causal, kv_lens, q_lens, q_starts):

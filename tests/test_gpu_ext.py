@@ -81,6 +81,16 @@ CASES = {
                         kv_lens=[400, 140]),
     "cross_tokens_grouped": dict(B=3, H=32, Hkv=4, Nq=3, Nk=190, d=64, kv_lens=[190, 7, 100]),
     "cross_token_grouped_f32": dict(B=2, H=20, Hkv=1, Nq=1, Nk=70, d=64, dtype="f32"),
+    # the largest distance, with folded heads whose tables fit beside the rings and with more
+    "far_token_grouped": dict(B=2, H=8, Hkv=2, Nq=1, Nk=1500, d=64, bias=(64, 1024), causal=True,
+                              q_starts=[1499, 600], kv_lens=[1500, 601]),
+    "far_token_16_heads": dict(B=1, H=32, Hkv=2, Nq=1, Nk=1300, d=128, bias=(64, 1024), causal=True, q_starts=[1299]),
+    "far_d256": dict(B=1, H=2, Hkv=1, Nq=1100, Nk=40, d=256, bias=(64, 1024), q_starts=[-600]),
+    # ragged batches of up to 64 entries are dealt out by length, larger ones in order
+    "entries_64": dict(B=64, H=2, Hkv=2, Nq=40, Nk=70, d=64, kv_lens=[(37 * b) % 71 for b in range(64)],
+                       q_lens=[(29 * b) % 41 for b in range(64)]),
+    "entries_70": dict(B=70, H=8, Hkv=4, Nq=17, Nk=35, d=32, bias=(8, 20), kv_lens=[(11 * b) % 36 for b in range(70)],
+                       q_lens=[(5 * b) % 18 for b in range(70)]),
     "rows_before_keys": dict(B=1, H=2, Hkv=2, Nq=80, Nk=60, d=64, bias=(32, 128), causal=True, q_starts=[-37]),
     "keys_behind": dict(B=1, H=2, Hkv=2, Nq=50, Nk=60, d=64, bias=(32, 128), q_starts=[100000]),
     # few rows against many keys, and few keys against many queries: blocks split over workgroups
@@ -280,6 +290,52 @@ def test_partial_gradients():
     (h,) = torch.autograd.grad(g, t, xd["UT"])
     zero = {**xd, **{n: torch.zeros_like(xd[n]) for n in ("UQ", "UK", "UV")}}
     assert torch.equal(h, chain(zero, c, 0.125)["Tt"])
+
+
+@pytest.mark.parametrize("name", ["tile_edges", "bias_grouped"])
+def test_third_derivatives_are_refused(name):
+    """The second gradients may be asked for with a graph; their own are refused, through the
+    native functions and through the Python ones."""
+    from paper_2609_24089_amd import ext
+    c = CASES[name]
+    xd = {n: t.cuda() for n, t in make(c, 14).items()}
+    want = chain(xd, c, 0.125)
+
+    def in_python(xd, c, tau, q, k, v, table):
+        return ext._ExtFn.apply(q, k, v, table, xd.get("buckets"), xd.get("kv_lens"), xd.get("q_lens"),
+                                xd.get("q_starts"), tau, c.get("causal", False))
+
+    for fn in (layer, in_python):
+        q, k, v = (xd[n].clone().requires_grad_(True) for n in ("Q", "K", "V"))
+        leaves = [q, k, v] + ([xd["table"].clone().requires_grad_(True)] if "bias" in c else [])
+        O = fn(xd, c, 0.125, q, k, v, leaves[3] if "bias" in c else None)
+        g = torch.autograd.grad(O, leaves, xd["dO"], create_graph=True)
+        u = [xd[n] for n in ("UQ", "UK", "UV", "UT") if n in xd]
+        h = torch.autograd.grad(g, leaves, u, create_graph=True)
+        for n, t in zip(("Qt", "Kt", "Vt", "Tt"), h):
+            assert torch.equal(t, want[n]), n
+            with pytest.raises(NotImplementedError, match="third derivatives"):
+                torch.autograd.grad(t.float().square().sum(), leaves, retain_graph=True, allow_unused=True)
+
+
+def test_two_streams_at_once():
+    """The whole path on two streams at a time, each with its own inputs and workspaces."""
+    jobs = []
+    for name in ("split_cols_bias", "bias_grouped"):
+        c = CASES[name]
+        xd = {n: t.cuda() for n, t in make(c, 15).items()}
+        jobs.append((c, xd, chain(xd, c, 0.125), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for i, (c, xd, _, s) in enumerate(jobs):
+            with torch.cuda.stream(s):
+                got[i].append(chain(xd, c, 0.125))
+    torch.cuda.synchronize()
+    for runs, (_, _, want, _) in zip(got, jobs):
+        for run in runs:
+            for n, t in want.items():
+                assert torch.equal(run[n], t), n
 
 
 def test_gradient_against_differences():
