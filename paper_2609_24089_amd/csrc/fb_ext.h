@@ -103,12 +103,12 @@ template <auto kKernel> int64_t static_lds() {
 // Kern::kernel<form, bias>() names the kernel, Kern::shape(form, bias) its shape.
 // ---------------------------------------------------------------------------
 struct ExtShape {
-  int mr, nw, occ, st, ks;
+  int mr, nw, occ, ks;
   constexpr int threads() const { return 64 * nw * ks; }
   constexpr int blocks() const { return mr * nw; }
   constexpr bool built() const { return mr > 0; }
 };
-constexpr ExtShape kNotBuilt{0, 1, 1, 2, 1};
+constexpr ExtShape kNotBuilt{0, 1, 1, 1};
 // Forms: 0 whole blocks, 1 to 3 blocks of this many waves of 16 rows in wave sets, 4 whole
 // blocks of 32 rows a wave in two sets (with 16 rows a wave those are form 1's).
 constexpr int kFormWaves[4] = {0, 4, 1, 2};
@@ -120,7 +120,7 @@ template <typename T, int D> constexpr ExtShape ext_sets(int nw, int tensors, in
   const int lds = s.ks * (2 * tensors * Geo<T, D>::kTileElems * (int)sizeof(T) + extra);
   // as many waves a SIMD as the workgroups that the LDS holds bring, `occ` at most
   const int fit = s.ks * nw * (160 * 1024 / lds) / 4;
-  return s.ks > 1 ? ExtShape{1, nw, std::max({1, s.ks * nw / 4, std::min(occ, fit)}), 2, s.ks} : kNotBuilt;
+  return s.ks > 1 ? ExtShape{1, nw, std::max({1, s.ks * nw / 4, std::min(occ, fit)}), s.ks} : kNotBuilt;
 }
 
 // Whole blocks in two wave sets, two waves per SIMD; `beside` bytes of LDS beside the rings.
@@ -128,7 +128,7 @@ template <typename T, int D> constexpr ExtShape ext_two_sets(const Shape& w, int
   const int ring = 2 * tensors * Geo<T, D>::kTileElems * (int)sizeof(T);
   const bool fits = w.mr == 2 && w.nw == 4 && 2 * ring + beside <= 144 * 1024 &&
                     2 * ring >= w.nw * Geo<T, D>::kNB * w.mr * 1024;
-  return fits ? ExtShape{w.mr, w.nw, 2, 2, 2} : kNotBuilt;
+  return fits ? ExtShape{w.mr, w.nw, 2, 2} : kNotBuilt;
 }
 
 template <typename Kern, int F> Form ext_form_of(const ExtProblem& p, int64_t dynamic, double narrow) {
@@ -179,8 +179,11 @@ int32_t ext_dispatch(int form, const ExtProblem& p, dim3 grid, int64_t dynamic, 
 // sums take to write and to read back at 4 TB/s, all of them the joining launch; only grids
 // of at most two workgroups a compute unit are offered, of four tiles a set or more.
 // max_chain: tiles that one accumulator of a column kernel may sum: longer ones drift
-// (SectionSums), so they are split whatever it costs.  Measured, one part -> chosen: see
-// the launchers.
+// (SectionSums), so they are split whatever it costs.  Measured, one part -> chosen (us): a
+// token against 16384 keys, bf16 B1 H16 d64 46 -> 24, B1 H32 Hkv4 d128 131 -> 24; fp32 B2 H16
+// N1024 d128 causal Hessian-vector product 617 -> 475.  On 60 drawn problems the choice is 1
+// to 3% slower than the best form and parts on average (worst: the forward 1.29, the row side
+// 1.05, the column side 1.13, the passes 1.34 and 1.27).
 constexpr double kJoinUs = 6.0;
 template <typename Kern, typename Dynamic>
 void ext_pick(const ExtProblem& p, const FormQuery& q, double narrow, Dynamic&& dynamic, int only, int base,

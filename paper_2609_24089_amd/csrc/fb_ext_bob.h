@@ -8,7 +8,7 @@ namespace fb {
 template <typename T, int D> struct ExtPass1 {
   static constexpr ExtShape shape(int form, bool bias) {
     constexpr Shape w = Cfg<T, D>::kP1;
-    return form == 0   ? ExtShape{w.mr, w.nw, w.occ, w.st, 1}
+    return form == 0   ? ExtShape{w.mr, w.nw, w.occ, 1}
            : form == 4 ? ext_two_sets<T, D>(w, 4, 0)
                        : ext_sets<T, D>(kFormWaves[form], 4, 0, 8, w.occ);
   }
@@ -21,7 +21,7 @@ template <typename T, int D> struct ExtPass2 {
   static constexpr int kExtra = 4 * 4 * kBS * (int)sizeof(float) + 1024;
   static constexpr ExtShape shape(int form, bool bias) {
     constexpr Shape w = Cfg<T, D>::kP2;
-    return form == 0   ? ExtShape{w.mr, w.nw, w.occ, w.st, 1}
+    return form == 0   ? ExtShape{w.mr, w.nw, w.occ, 1}
            : form == 4 ? ext_two_sets<T, D>(w, 3, 2 * kExtra)
            : sizeof(T) == 2 && D == 32 && form == 1
                ? kNotBuilt  // three tensors of two 1 KB blocks do not deal out over four waves

@@ -6,13 +6,13 @@ namespace fb {
 template <typename T, int D> struct ExtRowsBwd {
   static constexpr ExtShape shape(int form, bool bias) {
     constexpr Shape w = Cfg<T, D>::kRows;
-    return form == 0   ? ExtShape{w.mr, w.nw, w.occ, w.st, 1}
+    return form == 0   ? ExtShape{w.mr, w.nw, w.occ, 1}
            : form == 4 ? ext_two_sets<T, D>(w, 2, 0)
                        : ext_sets<T, D>(kFormWaves[form], 2, 0, 16, w.occ);
   }
   template <int F, bool kBias> static __host__ constexpr auto kernel() {
     constexpr ExtShape s = shape(F, kBias);
-    return &ext_bwd_rows_kernel<T, D, s.mr, s.nw, s.occ, s.st, s.ks, kBias>;
+    return &ext_bwd_rows_kernel<T, D, s.mr, s.nw, s.occ, s.ks, kBias>;
   }
 };
 
@@ -24,7 +24,7 @@ template <typename T, int D> struct ExtColsBwd {
     // three waves per SIMD for some spills beside the near tiles: 814 us for 881 with two at
     // B4 H12 N4096 dense, 462 for 485 causal (first backward)
     constexpr bool kThree = std::is_same_v<T, bf16> && D == 64;
-    return form == 0   ? ExtShape{w.mr, w.nw, bias && kThree ? 3 : w.occ, w.st, 1}
+    return form == 0   ? ExtShape{w.mr, w.nw, bias && kThree ? 3 : w.occ, 1}
            : form == 4 ? ext_two_sets<T, D>(w, 2, 2 * kExtra + (w.kl ? 4 * Geo<T, D>::kTileElems * (int)sizeof(T) : 0))
                        : ext_sets<T, D>(kFormWaves[form], 2, kExtra, waves, w.occ);
   }

@@ -6,13 +6,13 @@ namespace fb {
 template <typename T, int D> struct ExtFwd {
   static constexpr ExtShape shape(int form, bool bias) {
     constexpr Shape w = Cfg<T, D>::kFwd;
-    return form == 0   ? ExtShape{w.mr, w.nw, w.occ, w.st, 1}
+    return form == 0   ? ExtShape{w.mr, w.nw, w.occ, 1}
            : form == 4 ? ext_two_sets<T, D>(w, 2, 0)
                        : ext_sets<T, D>(kFormWaves[form], 2, 0, 16, form == 2 ? 1 : w.occ);
   }
   template <int F, bool kBias> static __host__ constexpr auto kernel() {
     constexpr ExtShape s = shape(F, kBias);
-    return &ext_fwd_kernel<T, D, s.mr, s.nw, s.occ, s.st, s.ks, kBias>;
+    return &ext_fwd_kernel<T, D, s.mr, s.nw, s.occ, s.ks, kBias>;
   }
 };
 

@@ -102,56 +102,39 @@ __device__ __forceinline__ void ext_fill_steps(const ExtArgs& a, const void* t, 
 __device__ __forceinline__ int ext_side(int lo, int hi, int R) { return hi <= -R ? -1 : lo >= R ? 1 : 0; }
 
 // ---------------------------------------------------------------------------
-// Tile loop of the row kernels: as stream_loop with opaque copies, with any ring depth, a
-// callback that runs while the first tiles are on their way, and (kBarrier false: one wave
+// Tile loop of the row kernels: as stream_loop with opaque copies into a ring of two stages,
+// a callback that runs while the first tiles are on their way, and (kBarrier false: one wave
 // a set, which alone writes and reads its ring) no barrier but the first.
 // ---------------------------------------------------------------------------
-template <int NSTAGE, int LT, bool kBarrier, class Issue, class Pro, class Body>
+template <int LT, bool kBarrier, class Issue, class Pro, class Body>
 __device__ __forceinline__ void ext_stream(int n, Issue&& issue, Pro&& pro, Body&& body) {
-  static_assert(NSTAGE == 2 || (NSTAGE == 4 && !kBarrier), "ring depth");
-  if constexpr (kBarrier) {
-    if (n > 0) issue(0, 0);
-    pro();
-    wait_copies<true>();
-    __syncthreads();
-    auto step = [&](int k, auto cur) {
-      constexpr int kCur = decltype(cur)::value;
+  if (n > 0) issue(0, 0);
+  if (!kBarrier && n > 1) issue(1, 1);
+  pro();
+  if constexpr (kBarrier) wait_copies<true>();
+  __syncthreads();
+  auto step = [&](int k, auto cur) {
+    constexpr int kCur = decltype(cur)::value;
+    if constexpr (kBarrier) {
       if (k + 1 < n) issue(k + 1, 1 - kCur);
       body(k, kCur);
       wait_copies<true>();
       __syncthreads();
-    };
-    for (int k = 0; k < n; k += 2) {
-      step(k, std::integral_constant<int, 0>{});
-      if (k + 1 < n) step(k + 1, std::integral_constant<int, 1>{});
-    }
-  } else {
-    // the whole ring is in flight at the start, and a stage is filled again as soon as its
-    // tile is done: the wave's own reads of it have to be back before (lgkmcnt(0), the other
-    // counters at their maxima)
-#pragma unroll
-    for (int st = 0; st < NSTAGE; ++st)
-      if (st < n) issue(st, st);
-    pro();
-    __syncthreads();
-    auto step = [&](int k, auto cur) {
-      constexpr int kCur = decltype(cur)::value;
-      if (k + NSTAGE - 1 < n)
-        wait_vm<(NSTAGE - 1) * LT>();
+    } else {
+      if (k + 1 < n)
+        wait_vm<LT>();
       else
         wait_copies<true>();
       body(k, kCur);
+      // the stage is filled again as soon as its tile is done: the wave's own reads of it have
+      // to be back before (lgkmcnt(0), the other counters at their maxima)
       __builtin_amdgcn_s_waitcnt(0xc07f);
-      if (k + NSTAGE < n) issue(k + NSTAGE, kCur);
-    };
-    for (int k = 0; k < n; k += NSTAGE) {
-      step(k, std::integral_constant<int, 0>{});
-      if (k + 1 < n) step(k + 1, std::integral_constant<int, 1>{});
-      if constexpr (NSTAGE > 2) {
-        if (k + 2 < n) step(k + 2, std::integral_constant<int, 2>{});
-        if (k + 3 < n) step(k + 3, std::integral_constant<int, 3>{});
-      }
+      if (k + 2 < n) issue(k + 2, kCur);
     }
+  };
+  for (int k = 0; k < n; k += 2) {
+    step(k, std::integral_constant<int, 0>{});
+    if (k + 1 < n) step(k + 1, std::integral_constant<int, 1>{});
   }
 }
 
@@ -301,15 +284,19 @@ __device__ __forceinline__ void ext_mask1(floatx4 (&x)[2], int s0, int klim) {
 // key tiles (none, if the block has few) and stores its unnormalised sums, reference and weight instead of O and L;
 // ext_fwd_join_kernel joins them.  One wave a set (NW = 1) runs without barriers: the form
 // of a few query rows against a long cache, which reads each key and value once.
+// Bound by the keys' and values' bytes for a few rows (B32 H32 Hkv8, one token, up to 4096
+// keys, d128: 403 MB in 77 us, 5.2 TB/s, what a large copy reaches), by MFMA and VALU issue
+// for many (B1 H16 N8192 d128 causal with a bias: 258 us, 1.07 PFLOP/s; d64 0.80 PFLOP/s, where
+// an element's exponential meets half the MFMA work).
 // ===========================================================================
-template <typename T, int D, int MR, int NW, int OCC, int NSTAGE, int KS, bool kBias>
+template <typename T, int D, int MR, int NW, int OCC, int KS, bool kBias>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_fwd_kernel(
     ExtArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, T* __restrict__ O,
     float* __restrict__ L, float* __restrict__ parts) {
   using E = Elt<T>;
   using G = Geo<T, D>;
   constexpr int BR = 16 * MR * NW;
-  __shared__ __attribute__((aligned(16))) RowSmem<T, D, 2, NSTAGE, KS, BR> sm;
+  __shared__ __attribute__((aligned(16))) RowSmem<T, D, 2, 2, KS, BR> sm;
   extern __shared__ float steps_mem[];
   float FB_LDS* const steps = (float FB_LDS*)steps_mem;
 
@@ -415,7 +402,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_fwd_kernel(
   constexpr bool kBarrier = NW > 1;
   const int iters = kBarrier ? first.size() : run.size();
   const TileCopy<T, D, NW, 2> copy(wl);
-  ext_stream<NSTAGE, tile_loads<T, D, NW, 2>(), kBarrier>(
+  ext_stream<tile_loads<T, D, NW, 2>(), kBarrier>(
       iters,
       [&](int it, int st) {
         copy.template issue<true>(src, (T FB_LDS*)sm.lds[ks][st], min(run.begin + it, rw.tiles - 1) * kBS, rw.kvis);
@@ -581,16 +568,17 @@ __global__ __launch_bounds__(256) void ext_fwd_join_kernel(ExtArgs a, const floa
 // sum over many rows of fp32 products, and that rounding of o would be its largest error
 // by far (2^-8 of D a row against 2^-24).  In dQ it matters where few keys share a row's
 // weight (a row of one key has dQ = 0): a row whose whole weight lies in a set's first tile
-// takes D from that tile.
+// takes D from that tile.  MFMA and VALU issue bound it: B4 H16 of 2048 ragged queries and
+// 4096 keys, d128, 326 us (0.96 PFLOP/s); B4 H12 N4096 d64 causal with a bias 175 us (0.89).
 // ===========================================================================
-template <typename T, int D, int MR, int NW, int OCC, int NSTAGE, int KS, bool kBias>
+template <typename T, int D, int MR, int NW, int OCC, int KS, bool kBias>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
     ExtArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ O,
     const T* __restrict__ dO, const float* __restrict__ L, T* __restrict__ dQ, float* __restrict__ Dout, float* __restrict__ parts) {
   using E = Elt<T>;
   using G = Geo<T, D>;
   constexpr int BR = 16 * MR * NW;
-  __shared__ __attribute__((aligned(16))) RowSmem<T, D, 2, NSTAGE, KS, BR> sm;
+  __shared__ __attribute__((aligned(16))) RowSmem<T, D, 2, 2, KS, BR> sm;
   extern __shared__ float steps_mem[];
   float FB_LDS* const steps = (float FB_LDS*)steps_mem;
 
@@ -637,7 +625,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
   constexpr bool kBarrier = NW > 1;
   const TileCopy<T, D, NW, 2> copy(wl);
   float blo = 0.f, bhi = 0.f;
-  ext_stream<NSTAGE, tile_loads<T, D, NW, 2>(), kBarrier>(
+  ext_stream<tile_loads<T, D, NW, 2>(), kBarrier>(
       kBarrier ? first.size() : run.size(),
       [&](int it, int st) {
         copy.template issue<true>(src, (T FB_LDS*)sm.lds[ks][st], min(run.begin + it, rw.tiles - 1) * kBS, rw.kvis);
@@ -1059,7 +1047,9 @@ __global__ __launch_bounds__(256) void ext_parts_kernel(const float* __restrict_
 }
 
 // First backward, column side: as attn_bwd_cols_kernel (its K rows in LDS with kKL), with
-// the table's step sums (`sums`, or null).
+// the table's step sums (`sums`, or null).  Issue bound, a third of the waves' time at the
+// tiles' barriers: B4 H16 of 2048 ragged queries and 4096 keys, d128, 446 us (0.93 PFLOP/s);
+// B4 H12 N4096 d64 causal with a bias 259 us (0.80), dense 732 us, without the bias 656.
 template <typename T, int D, int MC, int NW, int OCC, int KS, bool kKL, bool kBias>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_cols_kernel(
     ExtArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ dO,
@@ -1272,6 +1262,9 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_cols_kernel(
 //   dOt = sum P u_V + sum P F' v - da O,  alpha = alpha* + da,  E = E* + de - alpha D,
 // since Pt - E = w - da (dP - D) - de.  It costs nothing after the first tile: alpha* rides
 // on the fma that scales F, -E* is where the C tile starts.  Wave sets share one estimate.
+// MFMA and VALU issue bound it: B4 H12 N4096 d64 dense with a bias 910 us (1.13 PFLOP/s of the
+// ten contractions), without 898; a wave's chain of LDS reads, MFMA and VALU where the grid
+// leaves one or two waves a SIMD (B2 H8 of 1000 queries and 2047 keys: 53 us, 0.55 PFLOP/s).
 // ===========================================================================
 template <typename T, int D, int MR, int NW, int OCC, int KS, int kPF, bool kBias>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
@@ -1333,7 +1326,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
   for (int mb = 0; mb < MR; ++mb) aref[mb] = eref[mb] = 0.f;
   // parts that share a block take their sums from 0: each row of theirs has many keys in view
   bool centred = split > 1;
-  ext_stream<2, tile_loads<T, D, NW, 4>(), kBarrier>(
+  ext_stream<tile_loads<T, D, NW, 4>(), kBarrier>(
       kBarrier ? first.size() : run.size(),
       [&](int it, int st) {
         copy.template issue<true>(src, (T FB_LDS*)sm.lds[ks][st], min(run.begin + it, rw.tiles - 1) * kBS, rw.kvis);
@@ -1648,7 +1641,9 @@ __global__ __launch_bounds__(256) void ext_pass1_join_kernel(ExtArgs a, const fl
 }
 
 // ===========================================================================
-// BoB Pass 2: as bob_pass2_kernel, with the second-order table sums (`sums`, or null).
+// BoB Pass 2: as bob_pass2_kernel, with the second-order table sums (`sums`, or null).  Bound
+// as Pass 1: B4 H12 N4096 d64 dense with a bias 771 us (1.07 PFLOP/s of the eight
+// contractions), without 688: the near tiles' bias reads and step sums, and registers.
 // ===========================================================================
 template <typename T, int D, int MC, int NW, int OCC, int KS, bool kPF, bool kBias>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass2_kernel(
