@@ -439,13 +439,10 @@ ExtDims ext_dims_or_throw(Refs qside, Refs kside, Refs rows, const Extras& e) {
                     "attention gradients must be contiguous and share the inputs' shape, dtype and device");
   return m;
 }
-// A cotangent on the table's gradient; undefined: none.
-const void* ext_cotangent(const Tensor& g, const Tensor& table) {
-  if (!g.defined()) return nullptr;
-  TORCH_CHECK_VALUE(plain(g) && g.sizes() == table.sizes() && g.scalar_type() == table.scalar_type() &&
-                        g.device() == table.device(),
-                    "the cotangent on the table's gradient must share the table's shape, dtype and device");
-  return p(g);
+// Whether a cotangent on the table's gradient (undefined: none) is like the table.
+bool ext_like_table(const Tensor& g, const Tensor& table) {
+  return !g.defined() || (table.defined() && plain(g) && g.sizes() == table.sizes() &&
+                          g.scalar_type() == table.scalar_type() && g.device() == table.device());
 }
 
 Rows2 run_ext_fwd(const ExtDims& m, const Tensor& Q, const Tensor& K, const Tensor& V, double scale, bool causal) {
@@ -497,6 +494,84 @@ py::object py_ext_fwd(py::handle q, py::handle k, py::handle v, double scale, bo
     r = run_ext_fwd(m, t[0], t[1], t[2], scale, causal);
   }
   return py::make_tuple(r.O, r.L);
+}
+
+// The calls one by one, as ext.py's functions with fresh outputs on the current stream.
+py::object py_ext_bwd(py::handle q, py::handle k, py::handle v, py::handle o, py::handle dO, py::handle L, double scale,
+                      bool causal, py::handle table, py::handle buckets, py::handle kv_lens, py::handle q_lens,
+                      py::handle q_starts, bool want_table) {
+  std::vector<Tensor> t;
+  ExtDims m;
+  if (!plain_or_none({table, buckets, kv_lens, q_lens, q_starts}) || !tensors({q, k, v, o, dO, L}, t)) return py::none();
+  const Extras e{given(table), given(buckets), given(kv_lens), given(q_lens), given(q_starts)};
+  if (!ext_check({&t[0], &t[3], &t[4]}, {&t[1], &t[2]}, {&t[5]}, e, m)) return py::none();
+  ExtBwd r;
+  {
+    py::gil_scoped_release free;
+    c10::OptionalDeviceGuard guard(t[0].device());
+    r = run_ext_bwd(m, t[0], t[1], t[2], t[3], t[4], t[5], e, scale, causal, want_table, true);
+  }
+  return py::make_tuple(r.dQ, r.dK, r.dV, r.D, r.dT.defined() ? py::cast(r.dT) : py::none());
+}
+
+py::object py_ext_pass1(py::handle q, py::handle k, py::handle v, py::handle o, py::handle dO, py::handle uq,
+                        py::handle uk, py::handle uv, py::handle L, py::handle D, py::handle dQ, double scale,
+                        bool causal, py::handle table, py::handle buckets, py::handle ut, py::handle kv_lens,
+                        py::handle q_lens, py::handle q_starts) {
+  std::vector<Tensor> t;
+  ExtDims m;
+  if (!plain_or_none({table, buckets, ut, kv_lens, q_lens, q_starts}) ||
+      !tensors({q, k, v, o, dO, uq, uk, uv, L, D, dQ}, t))
+    return py::none();
+  const Extras e{given(table), given(buckets), given(kv_lens), given(q_lens), given(q_starts)};
+  if (!ext_check({&t[0], &t[3], &t[4], &t[5], &t[10]}, {&t[1], &t[2], &t[6], &t[7]}, {&t[8], &t[9]}, e, m))
+    return py::none();
+  const Tensor gT = given(ut);
+  if (!ext_like_table(gT, e.table)) return py::none();
+  const Tensor& Q = t[0];
+  Tensor Qt, dOt, alpha, E;
+  {
+    py::gil_scoped_release free;
+    c10::OptionalDeviceGuard guard(Q.device());
+    Qt = at::empty_like(Q), dOt = at::empty_like(Q), alpha = rows_like(Q), E = rows_like(Q);
+    const int64_t bytes = api.ext_pass1_bytes(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, causal, &m.x);
+    const Tensor ws = workspace(bytes, Q);
+    ok(api.ext_pass1(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, (float)scale, causal, &m.x, p(Q), p(t[1]), p(t[2]),
+                     p(t[3]), p(t[4]), p(t[5]), p(t[6]), p(t[7]), gT.defined() ? p(gT) : nullptr, f(t[8]), f(t[9]),
+                     p(t[10]), pm(Qt), pm(dOt), fm(alpha), fm(E), bytes > 0 ? pm(ws) : nullptr, bytes, stream_of(Q)));
+  }
+  return py::make_tuple(Qt, dOt, alpha, E);
+}
+
+py::object py_ext_pass2(py::handle q, py::handle k, py::handle v, py::handle dO, py::handle uq, py::handle uk,
+                        py::handle uv, py::handle L, py::handle D, py::handle alpha, py::handle E, double scale,
+                        bool causal, py::handle table, py::handle buckets, py::handle ut, py::handle kv_lens,
+                        py::handle q_lens, py::handle q_starts, bool want_table) {
+  std::vector<Tensor> t;
+  ExtDims m;
+  if (!plain_or_none({table, buckets, ut, kv_lens, q_lens, q_starts}) ||
+      !tensors({q, k, v, dO, uq, uk, uv, L, D, alpha, E}, t))
+    return py::none();
+  const Extras e{given(table), given(buckets), given(kv_lens), given(q_lens), given(q_starts)};
+  if (!ext_check({&t[0], &t[3], &t[4]}, {&t[1], &t[2], &t[5], &t[6]}, {&t[7], &t[8], &t[9], &t[10]}, e, m))
+    return py::none();
+  const Tensor gT = given(ut);
+  if (!ext_like_table(gT, e.table)) return py::none();
+  const Tensor& Q = t[0];
+  Tensor Kt, Vt, Tt;
+  {
+    py::gil_scoped_release free;
+    c10::OptionalDeviceGuard guard(Q.device());
+    Kt = at::empty_like(t[1]), Vt = at::empty_like(t[1]);
+    if (want_table && e.table.defined()) Tt = at::empty_like(e.table);
+    const int64_t bytes = api.ext_pass2_bytes(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, causal, &m.x);
+    const Tensor ws = workspace(bytes, Q);
+    ok(api.ext_pass2(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, (float)scale, causal, &m.x, p(Q), p(t[1]), p(t[2]),
+                     p(t[3]), p(t[4]), p(t[5]), p(t[6]), gT.defined() ? p(gT) : nullptr, f(t[7]), f(t[8]), f(t[9]),
+                     f(t[10]), pm(Kt), pm(Vt), Tt.defined() ? pm(Tt) : nullptr, bytes > 0 ? pm(ws) : nullptr, bytes,
+                     stream_of(Q)));
+  }
+  return py::make_tuple(Kt, Vt, Tt.defined() ? py::cast(Tt) : py::none());
 }
 
 // The functions' arguments that may be missing: apply() takes no undefined tensors.  The
@@ -554,7 +629,9 @@ struct ExtAttentionBackward : torch::autograd::Function<ExtAttentionBackward> {
     const ExtDims m = ext_dims_or_throw({&q, &O, &dO, &uq, &dQ}, {&k, &v, &uk, &uv}, {&L, &D}, e);
     c10::OptionalDeviceGuard guard(q.device());
     const bool graph = at::GradMode::is_enabled();
-    const void* const gT = ext_cotangent(ut, table);
+    TORCH_CHECK_VALUE(ext_like_table(ut, table),
+                      "the cotangent on the table's gradient must share the table's shape, dtype and device");
+    const void* const gT = ut.defined() ? p(ut) : nullptr;
     // alpha, E and the workspace of whichever pass runs, in one allocation
     const int64_t rows = (m.B * m.H * m.Nq * 4 + 255) / 256 * 256;
     const int64_t bytes1 = api.ext_pass1_bytes(m.code, m.B, m.H, m.Hkv, m.Nq, m.Nk, m.d, causal, &m.x);
@@ -654,5 +731,8 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
   m.def("bob", &py_bob);
   m.def("attention", &py_attention);
   m.def("ext_fwd", &py_ext_fwd);
+  m.def("ext_bwd", &py_ext_bwd);
+  m.def("ext_pass1", &py_ext_pass1);
+  m.def("ext_pass2", &py_ext_pass2);
   m.def("ext_attention", &py_ext_attention);
 }

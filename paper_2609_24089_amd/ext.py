@@ -161,12 +161,16 @@ class _Problem:
         return _p(gT)
 
 
+def _bias(bias):
+    table, buckets = (None, None) if bias is None else bias
+    return table, buckets
+
+
 def attn_ext_fwd_lse(Q, K, V, scale, causal=False, bias=None, kv_lens=None, q_lens=None, q_starts=None, out=None,
                      stream=None):
     """Forward: returns (O, L)."""
     if out is None and stream is None:
-        table, buckets = (None, None) if bias is None else bias
-        got = _fast().ext_fwd(Q, K, V, float(scale), bool(causal), table, buckets, kv_lens, q_lens, q_starts)
+        got = _fast().ext_fwd(Q, K, V, float(scale), bool(causal), *_bias(bias), kv_lens, q_lens, q_starts)
         if got is not None:
             return got
     p = _Problem((Q,), (K, V), scale, causal, bias, kv_lens, q_lens, q_starts)
@@ -186,6 +190,11 @@ def attn_ext_bwd(Q, K, V, O, dO, L, scale, causal=False, bias=None, kv_lens=None
                  want_table=True, out=None, stream=None):
     """First backward: returns (dQ, dK, dV, D, dT); dT is None without a bias or
     with want_table=False."""
+    if out is None and stream is None:
+        got = _fast().ext_bwd(Q, K, V, O, dO, L, float(scale), bool(causal), *_bias(bias), kv_lens, q_lens, q_starts,
+                              bool(want_table))
+        if got is not None:
+            return got
     p = _Problem((Q, O, dO), (K, V), scale, causal, bias, kv_lens, q_lens, q_starts)
     _check_rows(Q.shape, L)
     if out is None:
@@ -207,6 +216,11 @@ def attn_ext_bwd(Q, K, V, O, dO, L, scale, causal=False, bias=None, kv_lens=None
 def attn_ext_pass1_rows(Q, K, V, O, dO, gdQ, gdK, gdV, L, D, dQ, scale, causal=False, bias=None, gdT=None,
                         kv_lens=None, q_lens=None, q_starts=None, out=None, stream=None):
     """BoB Pass 1: returns (Qt, dOt, alpha, E).  gdT: the cotangent on dT (None: 0)."""
+    if out is None and stream is None:
+        got = _fast().ext_pass1(Q, K, V, O, dO, gdQ, gdK, gdV, L, D, dQ, float(scale), bool(causal), *_bias(bias), gdT,
+                                kv_lens, q_lens, q_starts)
+        if got is not None:
+            return got
     p = _Problem((Q, O, dO, gdQ, dQ), (K, V, gdK, gdV), scale, causal, bias, kv_lens, q_lens, q_starts)
     _check_rows(Q.shape, L, D)
     if out is None:
@@ -226,6 +240,11 @@ def attn_ext_pass2_cols(Q, K, V, dO, gdQ, gdK, gdV, L, D, alpha, E, scale, causa
                         kv_lens=None, q_lens=None, q_starts=None, want_table=True, out=None, stream=None):
     """BoB Pass 2: returns (Kt, Vt, Tt); Tt is None without a bias or with
     want_table=False."""
+    if out is None and stream is None:
+        got = _fast().ext_pass2(Q, K, V, dO, gdQ, gdK, gdV, L, D, alpha, E, float(scale), bool(causal), *_bias(bias),
+                                gdT, kv_lens, q_lens, q_starts, bool(want_table))
+        if got is not None:
+            return got
     p = _Problem((Q, dO, gdQ), (K, V, gdK, gdV), scale, causal, bias, kv_lens, q_lens, q_starts)
     _check_rows(Q.shape, L, D, alpha, E)
     if out is None:

@@ -261,13 +261,22 @@ def test_layers_equal_the_calls(name):
     again = chain(xd, c, 0.15)  # no atomics: the same bits twice
     for n, t in want.items():
         assert torch.equal(again[n], t), n
-    # into outputs of the caller's, on a stream of the caller's
+    # into outputs of the caller's, on a stream of the caller's: the calls without the native path
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
-    out = (torch.empty_like(want["O"]), torch.empty_like(want["L"]))
-    fb.attn_ext_fwd_lse(xd["Q"], xd["K"], xd["V"], 0.15, out=out, stream=s, **options(xd, c))
+    o, w = options(xd, c), {n: torch.empty_like(t) for n, t in want.items()}
+    Q, K, V, dO, U = xd["Q"], xd["K"], xd["V"], xd["dO"], [xd[n] for n in ("UQ", "UK", "UV")]
+    put = lambda *names: tuple(w.get(n) for n in names)  # noqa: E731
+    torch.cuda.synchronize()
+    fb.attn_ext_fwd_lse(Q, K, V, 0.15, out=put("O", "L"), stream=s, **o)
+    fb.attn_ext_bwd(Q, K, V, w["O"], dO, w["L"], 0.15, out=put("dQ", "dK", "dV", "D", "dT"), stream=s, **o)
+    fb.attn_ext_pass1_rows(Q, K, V, w["O"], dO, *U, w["L"], w["D"], w["dQ"], 0.15, gdT=xd.get("UT"),
+                           out=put("Qt", "dOt", "alpha", "E"), stream=s, **o)
+    fb.attn_ext_pass2_cols(Q, K, V, dO, *U, w["L"], w["D"], w["alpha"], w["E"], 0.15, gdT=xd.get("UT"),
+                           out=put("Kt", "Vt", "Tt"), stream=s, **o)
     s.synchronize()
-    assert torch.equal(out[0], want["O"]) and torch.equal(out[1], want["L"])
+    for n, t in w.items():
+        assert torch.equal(t, want[n]), n
 
 
 def test_partial_gradients():
