@@ -173,9 +173,10 @@ int32_t ext_dispatch(int form, const ExtProblem& p, dim3 grid, int64_t dynamic, 
   return ext_go<Kern, 0>(p, grid, dynamic, stream, a, args...);
 }
 
-// The form and the parts with the least estimated time.  dynamic(shape): its LDS of the bias;
-// base: parts that a block has in any case (1, or a group's query heads); others are multiples
-// of `unit`; part_bytes: of fp32 sums that a part of all blocks stores.  A part costs what its
+// The form (of the bits in `allowed`) and the parts with the least estimated time.
+// dynamic(shape): its LDS of the bias; base: parts that a block has in any case (1, or a
+// group's query heads); others are multiples of `unit`; part_bytes: of fp32 sums that a part
+// of all blocks stores.  A part costs what its
 // sums take to write and to read back at 4 TB/s, all of them the joining launch; only grids
 // of at most two workgroups a compute unit are offered, of four tiles a set or more.
 // max_chain: tiles that one accumulator of a column kernel may sum: longer ones drift
@@ -185,8 +186,9 @@ int32_t ext_dispatch(int form, const ExtProblem& p, dim3 grid, int64_t dynamic, 
 // to 3% slower than the best form and parts on average (worst: the forward 1.29, the row side
 // 1.05, the column side 1.13, the passes 1.34 and 1.27).
 constexpr double kJoinUs = 6.0;
+constexpr unsigned kAnyForm = (1u << kForms) - 1;
 template <typename Kern, typename Dynamic>
-void ext_pick(const ExtProblem& p, const FormQuery& q, double narrow, Dynamic&& dynamic, int only, int base,
+void ext_pick(const ExtProblem& p, const FormQuery& q, double narrow, Dynamic&& dynamic, unsigned allowed, int base,
               int unit, int64_t part_bytes, ExtPlan* c, int64_t max_chain = int64_t(1) << 40) {
   const bool b = has_bias(p);
   const Form forms[kForms] = {ext_form_of<Kern, 0>(p, dynamic(Kern::shape(0, b)), 1.0),
@@ -196,14 +198,14 @@ void ext_pick(const ExtProblem& p, const FormQuery& q, double narrow, Dynamic&& 
                               ext_form_of<Kern, 4>(p, dynamic(Kern::shape(4, b)), narrow)};
   double least = 0;
   bool found = false, fills = false;
-  c->form = std::max(only, 0);  // an unknown device
+  c->form = __builtin_ctz(allowed);  // an unknown device
   c->parts = base;
   for (int i = 0; i < kForms && q.cus > 0; ++i) {
     Form f = forms[i];
-    if (f.resident == 0 || (only >= 0 && i != only)) continue;
+    if (f.resident == 0 || (allowed >> i & 1) == 0) continue;
     const int64_t blocks = q.heads * ((q.N + 16 * f.blocks - 1) / (16 * f.blocks));
     if (i == 0) fills = f.resident > 1 && blocks * base > q.cus * f.resident;
-    if (i > 0 && only < 0 && fills) continue;
+    if (i > 0 && fills) continue;
     const auto too_long = [&](int parts) { return q.tiles > max_chain * f.sets * parts; };
     for (int m = 0; m <= 16; m = m == 0 ? 1 : 2 * m) {
       f.parts = m == 0 ? base : unit * m;

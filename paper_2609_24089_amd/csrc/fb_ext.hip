@@ -162,7 +162,8 @@ static ColBytes col_bytes(const ExtProblem& p, const ExtPlan& c) {
     const int64_t blocks = (p.Nk + 16 * c.blocks - 1) / (16 * c.blocks);
     const int subs = c.parts > 1 ? c.parts / ext_group(p) : 1;
     b.rows = p.B * blocks * subs * c.waves;
-    // few rows go straight to the gather, for one launch less
+    // few rows go straight to the gather, for one launch less: 256 rows of 259 steps 8.0 us for
+    // 5.4 + 4.9
     b.S = b.rows <= 256 ? 0 : (int)std::min<int64_t>(16, b.rows / 8);
     auto pad = [](int64_t n) { return (n + 15) / 16 * 16; };
     b.sums = pad(b.rows * p.H * ext_width(p) * 4);

@@ -42,7 +42,7 @@ template <typename T, int D> ExtPlan ext_pass1_plan(const ExtProblem& p) {
   const FormQuery q{device_cus(), p.B * p.H, std::max<int64_t>(p.Nq, 1), std::max<int64_t>((p.Nk + kBS - 1) / kBS, 1),
                     triangular(p), block_us<T>(10, D), kP1Step<T>, merge_us(3, D), kRowMargin};
   const int64_t steps = 2 * ext_steps_bytes(p);
-  ext_pick<ExtPass1<T, D>>(p, q, kP1Step<T>.narrow, [&](const ExtShape&) { return steps; }, -1, 1, 1,
+  ext_pick<ExtPass1<T, D>>(p, q, kP1Step<T>.narrow, [&](const ExtShape&) { return steps; }, kAnyForm, 1, 1,
                            p.B * p.H * p.Nq * (3 * D + 4) * 4, &c);
   return c;
 }
@@ -73,7 +73,7 @@ template <typename T, int D> ExtPlan ext_pass2_plan(const ExtProblem& p) {
   const FormQuery q{device_cus(), p.B * p.Hkv, std::max<int64_t>(p.Nk, 1),
                     std::max<int64_t>((p.Nq + kBS - 1) / kBS, 1) * grp, triangular(p), block_us<T>(8, D), kP2Step<T>,
                     merge_us(2, D), 1.0};
-  ext_pick<C>(p, q, kP2Step<T>.narrow, [&](const ExtShape& s) { return pass2_dynamic(p, s); }, -1, base, grp,
+  ext_pick<C>(p, q, kP2Step<T>.narrow, [&](const ExtShape& s) { return pass2_dynamic(p, s); }, kAnyForm, base, grp,
               2 * p.B * p.Hkv * p.Nk * D * 4, &c, kLongChain);
   return c;
 }

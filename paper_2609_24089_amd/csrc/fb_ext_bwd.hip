@@ -44,7 +44,7 @@ template <typename T, int D> ExtPlan ext_rows_plan(const ExtProblem& p) {
   const FormQuery q{device_cus(), p.B * p.H, std::max<int64_t>(p.Nq, 1), std::max<int64_t>((p.Nk + kBS - 1) / kBS, 1),
                     triangular(p), block_us<T>(3, D), kRowsStep<T>, merge_us(1, D), kRowMargin};
   const int64_t steps = ext_steps_bytes(p);
-  ext_pick<ExtRowsBwd<T, D>>(p, q, kRowsStep<T>.narrow, [&](const ExtShape&) { return steps; }, -1, 1, 1,
+  ext_pick<ExtRowsBwd<T, D>>(p, q, kRowsStep<T>.narrow, [&](const ExtShape&) { return steps; }, kAnyForm, 1, 1,
                              p.B * p.H * p.Nq * (D + 1) * 4, &c);
   return c;
 }
@@ -58,7 +58,7 @@ template <typename T, int D> ExtPlan ext_cols_plan(const ExtProblem& p) {
   const FormQuery q{device_cus(), p.B * p.Hkv, std::max<int64_t>(p.Nk, 1),
                     std::max<int64_t>((p.Nq + kBS - 1) / kBS, 1) * grp, triangular(p), block_us<T>(4, D), kColsStep<T>,
                     merge_us(2, D), 1.0};
-  ext_pick<C>(p, q, kColsStep<T>.narrow, [&](const ExtShape& s) { return cols_dynamic(p, s); }, -1, base, grp,
+  ext_pick<C>(p, q, kColsStep<T>.narrow, [&](const ExtShape& s) { return cols_dynamic(p, s); }, kAnyForm, base, grp,
               2 * p.B * p.Hkv * p.Nk * D * 4, &c, kLongChain);
   return c;
 }

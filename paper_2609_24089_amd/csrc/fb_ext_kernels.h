@@ -306,7 +306,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_fwd_kernel(
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
   const int wl = __builtin_amdgcn_readfirstlane(KS == 1 ? wave_id() : wave_id() % NW);
-  const ExtRows<MR, NW, NW == 1> rw(a, rh, rb, wl, j);
+  const ExtRows<MR, NW, MR == 1> rw(a, rh, rb, wl, j);
   const int part = blockIdx.y;
   const int64_t kvoff = (int64_t)rw.kvh * a.Nk * D;
 

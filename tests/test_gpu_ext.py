@@ -81,6 +81,17 @@ CASES = {
                         kv_lens=[400, 140]),
     "cross_tokens_grouped": dict(B=3, H=32, Hkv=4, Nq=3, Nk=190, d=64, kv_lens=[190, 7, 100]),
     "cross_token_grouped_f32": dict(B=2, H=20, Hkv=1, Nq=1, Nk=70, d=64, dtype="f32"),
+    # more than 16 rows of a group as one matrix, in blocks of one to four waves a set
+    "tokens_16_grouped": dict(B=8, H=32, Hkv=8, Nq=16, Nk=700, d=128, bias=(32, 128), causal=True,
+                              q_starts=[684, 500, 31, 0, 3, 600, 64, 255], kv_lens=[700, 516, 47, 16, 19, 616, 80, 271],
+                              q_lens=[16, 16, 1, 16, 0, 7, 16, 15]),
+    "tokens_11_grouped": dict(B=6, H=30, Hkv=6, Nq=11, Nk=330, d=64, bias=(16, 40), q_starts=[300, 100, 0, 7, 50, 200]),
+    "tokens_8_grouped_f32": dict(B=3, H=12, Hkv=3, Nq=8, Nk=200, d=64, dtype="f32", kv_lens=[200, 40, 1]),
+    "tokens_12_grouped_d32": dict(B=16, H=64, Hkv=16, Nq=12, Nk=260, d=32),
+    "tokens_9_grouped_d256": dict(B=2, H=16, Hkv=4, Nq=9, Nk=130, d=256, bias=(32, 128), q_lens=[9, 4]),
+    "tokens_32_grouped": dict(B=3, H=12, Hkv=3, Nq=32, Nk=300, d=64, bias=(64, 90), causal=True, q_starts=[268, 0, 111],
+                              kv_lens=[300, 32, 140], q_lens=[32, 32, 29]),
+    "rows_33_grouped": dict(B=3, H=12, Hkv=3, Nq=33, Nk=300, d=64, bias=(64, 90), q_starts=[-10, 0, 111]),
     # the largest distance, with folded heads whose tables fit beside the rings and with more
     "far_token_grouped": dict(B=2, H=8, Hkv=2, Nq=1, Nk=1500, d=64, bias=(64, 1024), causal=True,
                               q_starts=[1499, 600], kv_lens=[1500, 601]),
