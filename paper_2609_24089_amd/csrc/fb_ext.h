@@ -176,16 +176,19 @@ int32_t ext_dispatch(int form, const ExtProblem& p, dim3 grid, int64_t dynamic, 
 // The form (of the bits in `allowed`) and the parts with the least estimated time.
 // dynamic(shape): its LDS of the bias; base: parts that a block has in any case (1, or a
 // group's query heads); others are multiples of `unit`; part_bytes: of fp32 sums that a part
-// of all blocks stores.  A part costs what its
-// sums take to write and to read back at 4 TB/s, all of them the joining launch; only grids
-// of at most two workgroups a compute unit are offered, of four tiles a set or more.
+// of all blocks stores.  A part costs what its sums take to write and to read back at 4 TB/s,
+// all of them the joining launch; grids of at most four rounds (causal ones, whose order
+// balances them: two workgroups a compute unit) and kMaxPartBytes are offered parts of four
+// tiles a set or more.  Beyond two workgroups a unit they even out the last round: bf16 B2 H24
+// Hkv12, 3622 queries, 1426 keys, d64, column side 387 -> 304 us with the row side, Pass 2 429
+// -> 307; Pass 1 of B1 H8, 1301 queries, 5846 keys 121 -> 96; two of 110 shapes lost a tenth.
 // max_chain: tiles that one accumulator of a column kernel may sum: longer ones drift
 // (SectionSums), so they are split whatever it costs.  Measured, one part -> chosen (us): a
 // token against 16384 keys, bf16 B1 H16 d64 46 -> 24, B1 H32 Hkv4 d128 131 -> 24; fp32 B2 H16
-// N1024 d128 causal Hessian-vector product 617 -> 475.  On 60 drawn problems the choice is 1
-// to 3% slower than the best form and parts on average (worst: the forward 1.29, the row side
-// 1.05, the column side 1.13, the passes 1.34 and 1.27).
+// N1024 d128 causal Hessian-vector product 617 -> 475.  On 56 drawn problems the choice was 1
+// to 3% slower than the best form and parts on average before the parts of later rounds.
 constexpr double kJoinUs = 6.0;
+constexpr int64_t kMaxPartBytes = int64_t(128) << 20;
 constexpr unsigned kAnyForm = (1u << kForms) - 1;
 template <typename Kern, typename Dynamic>
 void ext_pick(const ExtProblem& p, const FormQuery& q, double narrow, Dynamic&& dynamic, unsigned allowed, int base,
@@ -212,7 +215,8 @@ void ext_pick(const ExtProblem& p, const FormQuery& q, double narrow, Dynamic&& 
       if (m > 0 && f.parts <= base) continue;
       const int64_t total = blocks * f.parts;
       if (too_long(f.parts) && m < 16) continue;
-      const bool few = total <= 2 * q.cus && q.tiles >= (int64_t)4 * f.sets * f.parts;
+      const int64_t most = q.cus * (q.causal ? 2 : std::max<int64_t>(2, 4 * f.resident));
+      const bool few = total <= most && f.parts * part_bytes <= kMaxPartBytes && q.tiles >= (int64_t)4 * f.sets * f.parts;
       if (m > 0 && !few && !too_long(base)) break;
       if (total > INT32_MAX / 16 || total * f.threads > (int64_t)UINT32_MAX) continue;
       double t = form_us(q, f) * (f.parts > base ? 1.08 : i > 0 ? q.margin : 1.0);
