@@ -14,9 +14,9 @@ def test_hash_ignores_other_units(monkeypatch):
 
 
 def test_hash_follows_its_own_units(monkeypatch):
-    base = bench.kernel_source_hash()
-    for i, (name, flags) in enumerate(build.SOURCES):
-        changed = list(build.SOURCES)
+    base, units = bench.kernel_source_hash(), build.SOURCES
+    for i, (name, flags) in enumerate(units):
+        changed = list(units)
         changed[i] = (name, flags + ["-O1"])
         monkeypatch.setattr(build, "SOURCES", changed)
         assert (bench.kernel_source_hash() != base) == (name in bench.KERNEL_SOURCES), name
