@@ -419,6 +419,28 @@ int64_t attn_ext_pass1_workspace_bytes(int32_t dtype, int64_t B, int64_t H, int6
 int64_t attn_ext_pass2_workspace_bytes(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,
                                        int64_t d, int32_t causal, const attn_ext* ext);
 
+/* The launch that a call makes of this problem on the current device, of which the library
+ * chooses every field; `kernel` names the kernel: the forward, the first backward's row side
+ * (dQ, D) and column side (dK, dV, dT), the two passes.
+ *  rows       query (column kernels: key) rows of a workgroup
+ *  wave_sets  wave sets that share a workgroup's rows and divide the streamed side
+ *  parts      workgroups that share a block of rows and divide the streamed side, joined by a
+ *             second launch
+ *  folded     1: the query rows of a group's heads form one matrix (the forward alone)
+ *  resident   workgroups that one compute unit holds at a time; 0 if the device does not tell
+ * All are 0 where the call does not launch the kernel.  Returns BOB_OK, or the status that
+ * the call would return for the problem (scale and pointers aside). */
+enum { ATTN_EXT_FWD = 0, ATTN_EXT_ROWS = 1, ATTN_EXT_COLS = 2, ATTN_EXT_PASS1 = 3, ATTN_EXT_PASS2 = 4 };
+typedef struct {
+  int32_t rows;
+  int32_t wave_sets;
+  int32_t parts;
+  int32_t folded;
+  int32_t resident;
+} attn_ext_launch;
+int32_t attn_ext_layout(int32_t kernel, int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,
+                        int64_t d, int32_t causal, const attn_ext* ext, attn_ext_launch* launch);
+
 /* 1 if (dtype, d) is built into this library, else 0. */
 int32_t bob_supported(int32_t dtype, int64_t d);
 

@@ -429,5 +429,6 @@ def bob(Q, K, V, dO, gdQ, gdK, gdV, scale, causal=False, use_dq=True, stream=Non
 
 from .autograd import attention  # noqa: E402  (differentiable wrapper; imports the entry points above)
 from .ext import (  # noqa: E402  (attention between sequences of two lengths, with a position bias)
-    AttnExt, attn_ext_bwd, attn_ext_fwd_lse, attn_ext_pass1_rows, attn_ext_pass2_cols, biased_attention,
-    cross_attention, relative_buckets)
+    ATTN_EXT_COLS, ATTN_EXT_FWD, ATTN_EXT_PASS1, ATTN_EXT_PASS2, ATTN_EXT_ROWS, AttnExt, AttnExtLaunch, attn_ext_bwd,
+    attn_ext_fwd_lse, attn_ext_layout, attn_ext_pass1_rows, attn_ext_pass2_cols, biased_attention, cross_attention,
+    relative_buckets)

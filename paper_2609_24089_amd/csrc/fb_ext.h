@@ -26,6 +26,7 @@ inline int64_t ext_width(const ExtProblem& p) { return 2 * (int64_t)p.x.max_dist
 // workgroups a block; folded rows (row kernels).
 struct ExtPlan {
   int form = 0, blocks = 4, sets = 1, waves = 4, parts = 1;
+  int resident = 0;  // workgroups a compute unit, as the estimate takes them
   bool fold = false;
 };
 
@@ -232,6 +233,7 @@ void ext_pick(const ExtProblem& p, const FormQuery& q, double narrow, Dynamic&& 
   const ExtShape s = Kern::shape(c->form, b);
   c->blocks = s.blocks();
   c->sets = s.ks;
+  c->resident = q.cus > 0 ? forms[c->form].resident : 0;
   c->waves = s.ks * s.nw;
 }
 

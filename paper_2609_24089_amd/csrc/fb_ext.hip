@@ -336,4 +336,23 @@ int64_t attn_ext_pass2_workspace_bytes(int32_t dtype, int64_t B, int64_t H, int6
   return fb::col_bytes(p, fb::plan_pass2(p)).all();
 }
 
+int32_t attn_ext_layout(int32_t kernel, int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,
+                        int64_t d, int32_t causal, const attn_ext* ext, attn_ext_launch* launch) {
+  if (kernel < ATTN_EXT_FWD || kernel > ATTN_EXT_PASS2 || launch == nullptr) return BOB_EINVAL;
+  const ExtProblem p = fb::ext_problem(dtype, B, H, Hkv, Nq, Nk, d, 1.0f, causal, ext);
+  bool empty;
+  const int32_t rc = fb::ext_check(p, &empty);
+  if (rc != BOB_OK) return rc;
+  *launch = attn_ext_launch{};
+  const bool columns = kernel == ATTN_EXT_COLS || kernel == ATTN_EXT_PASS2;
+  if (empty || B == 0 || (columns ? Nk : Nq) == 0) return BOB_OK;
+  const fb::ExtPlan c = kernel == ATTN_EXT_FWD     ? fb::plan_fwd(p)
+                        : kernel == ATTN_EXT_ROWS  ? fb::plan_rows(p)
+                        : kernel == ATTN_EXT_COLS  ? fb::plan_cols(p)
+                        : kernel == ATTN_EXT_PASS1 ? fb::plan_pass1(p)
+                                                   : fb::plan_pass2(p);
+  *launch = attn_ext_launch{16 * c.blocks, c.sets, c.parts, c.fold ? 1 : 0, c.resident};
+  return BOB_OK;
+}
+
 }  // extern "C"

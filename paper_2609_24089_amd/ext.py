@@ -23,8 +23,8 @@ import ctypes
 
 import torch
 
-from . import (BOB_BF16, BOB_F32, _call, _check_mats, _check_rows, _dtype_code, _fast, _p, _rows_empty, _stream,
-               load_library)
+from . import (BOB_BF16, BOB_F32, BOB_OK, _call, _check_mats, _check_rows, _dtype_code, _fast, _p, _rows_empty,
+               _stream, load_library, status_string)
 
 MAX_DISTANCE = 1024
 MAX_BUCKETS = 1 << 16
@@ -35,6 +35,17 @@ class AttnExt(ctypes.Structure):
     _fields_ = [("q_lens", ctypes.c_void_p), ("kv_lens", ctypes.c_void_p), ("q_starts", ctypes.c_void_p),
                 ("table", ctypes.c_void_p), ("buckets", ctypes.c_void_p), ("table_dtype", ctypes.c_int32),
                 ("num_buckets", ctypes.c_int32), ("max_distance", ctypes.c_int32)]
+
+
+ATTN_EXT_FWD, ATTN_EXT_ROWS, ATTN_EXT_COLS, ATTN_EXT_PASS1, ATTN_EXT_PASS2 = range(5)
+
+
+class AttnExtLaunch(ctypes.Structure):
+    """attn_ext_launch of include/flashbob.h."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "wave_sets", "parts", "folded", "resident")]
+
+    def __repr__(self):
+        return "AttnExtLaunch(" + ", ".join(f"{n}={getattr(self, n)}" for n, _ in self._fields_) + ")"
 
 
 def _declare(lib):
@@ -52,6 +63,8 @@ def _declare(lib):
         fn = getattr(lib, f"attn_ext_{name}_workspace_bytes")
         fn.argtypes = shape + [i32, ext]
         fn.restype = i64
+    lib.attn_ext_layout.argtypes = [i32] + shape + [i32, ext, ctypes.POINTER(AttnExtLaunch)]
+    lib.attn_ext_layout.restype = i32
 
 
 def relative_buckets(num_buckets, max_distance, bidirectional=True, device=None):
@@ -79,6 +92,24 @@ def relative_buckets(num_buckets, max_distance, bidirectional=True, device=None)
         side.append(x if x < e else e + k)
     after = [n + c for c in side] if bidirectional else [side[0]] * (R + 1)
     return torch.tensor(side[:0:-1] + side[:1] + after[1:], dtype=torch.int32, device=device)
+
+
+def attn_ext_layout(kernel, dtype, B, H, Hkv, Nq, Nk, d, causal=False, bias=None, device=None):
+    """The AttnExtLaunch that kernel ATTN_EXT_FWD, ATTN_EXT_ROWS, ATTN_EXT_COLS,
+    ATTN_EXT_PASS1 or ATTN_EXT_PASS2 runs for this problem on `device` (default:
+    the current device).  bias: (num_buckets, max_distance) of its table, or None."""
+    lib = load_library()
+    code = _dtype_code(torch.empty(0, dtype=dtype))
+    ext, got = AttnExt(), AttnExtLaunch()
+    if bias is not None:  # the query reads the pointers' presence alone
+        ext.table = ext.buckets = 16
+        ext.table_dtype, ext.num_buckets, ext.max_distance = BOB_F32, *bias
+    with torch.cuda.device(device if device is not None else torch.cuda.current_device()):
+        rc = lib.attn_ext_layout(kernel, code, B, H, Hkv, Nq, Nk, d, int(bool(causal)), ctypes.byref(ext),
+                                 ctypes.byref(got))
+    if rc != BOB_OK:
+        raise RuntimeError(status_string(rc))
+    return got
 
 
 def _check_lens(name, t, B, like):
