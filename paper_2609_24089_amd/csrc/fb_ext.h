@@ -37,7 +37,7 @@ inline ExtArgs ext_args(const ExtProblem& p, const ExtPlan& c, int64_t heads, in
   a.Nq = (int)p.Nq;
   a.Nk = (int)p.Nk;
   a.nRB = (int)((rows + 16 * c.blocks - 1) / (16 * c.blocks));
-  a.total = (int)(heads * a.nRB);
+  a.total = a.blocks = (int)(heads * a.nRB);
   a.causal = p.causal;
   a.fold = c.fold ? 1 : 0;
   a.scale = p.scale;
@@ -86,8 +86,45 @@ int32_t ext_launch_pass2(const ExtProblem& p, const void* Q, const void* K, cons
   M(bf16, 32, __VA_ARGS__) M(bf16, 64, __VA_ARGS__) M(bf16, 128, __VA_ARGS__) M(bf16, 256, __VA_ARGS__) \
   M(float, 32, __VA_ARGS__) M(float, 64, __VA_ARGS__) M(float, 128, __VA_ARGS__)
 
-// Adds the parts of a column kernel (plane elements each, two planes a part) into X and Y.
-int32_t ext_add_parts(const ExtProblem& p, const float* parts, int nparts, void* X, void* Y, hipStream_t s);
+// Adds the parts of a column kernel ([nparts][2][a.rows][d]) into X and Y.
+int32_t ext_add_parts(const ExtProblem& p, const ExtArgs& a, const float* parts, void* X, void* Y, hipStream_t s);
+
+// A column kernel in parts keeps its parts' sums in at most kSliceBytes of workspace (or one
+// block's, if that is more): where all blocks' would take more, it runs a slice of consecutive
+// blocks at a time and adds each slice's parts before the next.  4 to 8 thousand workgroups a
+// slice, ten rounds and more, so that a slice's last round costs a few percent of it.  Without
+// slices bf16 B4 H64 Hkv8 N32768 d128 with a bias, whose heads of a group have a part each,
+// took 8.6 GB beside outputs of 0.5.
+constexpr int64_t kSliceBytes = int64_t(512) << 20;
+struct ExtSlices {
+  int64_t blocks, rows;  // of a slice, the last one's may be fewer
+};
+inline ExtSlices ext_slices(const ExtProblem& p, const ExtPlan& c) {
+  const int64_t all = p.B * p.Hkv * p.Nk, blocks = p.B * p.Hkv * ((p.Nk + 16 * c.blocks - 1) / (16 * c.blocks));
+  const int64_t row_bytes = (int64_t)c.parts * 2 * p.d * 4, block_rows = std::min<int64_t>(16 * c.blocks, p.Nk);
+  if (c.parts == 1 || all * row_bytes <= kSliceBytes) return {blocks, all};
+  const int64_t most = std::max<int64_t>(1, kSliceBytes / (block_rows * row_bytes)), count = (blocks + most - 1) / most;
+  const int64_t each = (blocks + count - 1) / count;
+  return {each, std::min(each * block_rows, all)};
+}
+
+// Runs launch(a, grid) for every slice of the column kernel's blocks, and adds its parts.
+template <typename Launch>
+int32_t ext_launch_columns(const ExtProblem& p, const ExtPlan& c, ExtArgs a, float* parts, void* X, void* Y,
+                           hipStream_t s, Launch&& launch) {
+  const int64_t each = ext_slices(p, c).blocks;
+  auto row = [&](int64_t block) { return block / a.nRB * p.Nk + block % a.nRB * (16 * c.blocks); };
+  for (int64_t first = 0; first < a.total; first += each) {
+    a.block0 = (int)first;
+    a.blocks = (int)std::min<int64_t>(each, a.total - first);
+    a.row0 = row(first);
+    a.rows = row(first + a.blocks) - a.row0;
+    int32_t rc = launch(a, dim3(a.blocks, c.parts));
+    if (rc == BOB_OK && c.parts > 1) rc = ext_add_parts(p, a, parts, X, Y, s);
+    if (rc != BOB_OK) return rc;
+  }
+  return BOB_OK;
+}
 
 // A kernel's LDS beside its dynamic part, as the runtime tells it.
 template <auto kKernel> int64_t static_lds() {

@@ -71,15 +71,16 @@ __global__ __launch_bounds__(kGatherThreads) void ext_buckets_kernel(const float
   }
 }
 
-int32_t ext_add_parts(const ExtProblem& p, const float* parts, int nparts, void* X, void* Y, hipStream_t s) {
-  const int64_t plane = p.B * p.Hkv * p.Nk * p.d;
+int32_t ext_add_parts(const ExtProblem& p, const ExtArgs& a, const float* parts, void* X, void* Y, hipStream_t s) {
+  const int64_t plane = a.rows * p.d, first = a.row0 * p.d;
   const unsigned blocks = (unsigned)std::min<int64_t>((plane / 2 + 255) / 256, 8192);
   (void)hipGetLastError();
   if (p.dtype == BOB_BF16)
-    hipLaunchKernelGGL(ext_parts_kernel<bf16>, dim3(blocks), dim3(256), 0, s, parts, nparts, plane, (bf16*)X, (bf16*)Y);
+    hipLaunchKernelGGL(ext_parts_kernel<bf16>, dim3(blocks), dim3(256), 0, s, parts, a.nparts, plane, (bf16*)X + first,
+                       (bf16*)Y + first);
   else
-    hipLaunchKernelGGL(ext_parts_kernel<float>, dim3(blocks), dim3(256), 0, s, parts, nparts, plane, (float*)X,
-                       (float*)Y);
+    hipLaunchKernelGGL(ext_parts_kernel<float>, dim3(blocks), dim3(256), 0, s, parts, a.nparts, plane, (float*)X + first,
+                       (float*)Y + first);
   return finish_launch();
 }
 
@@ -157,7 +158,7 @@ struct ColBytes {
 };
 static ColBytes col_bytes(const ExtProblem& p, const ExtPlan& c) {
   ColBytes b;
-  if (c.parts > 1) b.parts = (int64_t)c.parts * 2 * p.B * p.Hkv * p.Nk * p.d * 4;
+  if (c.parts > 1) b.parts = (int64_t)c.parts * 2 * ext_slices(p, c).rows * p.d * 4;
   if (has_bias(p)) {
     const int64_t blocks = (p.Nk + 16 * c.blocks - 1) / (16 * c.blocks);
     const int subs = c.parts > 1 ? c.parts / ext_group(p) : 1;

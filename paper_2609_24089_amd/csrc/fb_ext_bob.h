@@ -85,12 +85,13 @@ int32_t ext_launch_pass2(const ExtProblem& p, const void* Q, const void* K, cons
                          float* sums, hipStream_t s) {
   using C = ExtPass2<T, D>;
   const ExtPlan c = ext_pass2_plan<T, D>(p);
-  const ExtArgs a = ext_args(p, c, p.B * p.Hkv, p.Nk, UT);
-  const int32_t rc = ext_dispatch<C>(c.form, p, dim3(a.total, c.parts), pass2_dynamic(p, C::shape(c.form, has_bias(p))), s, a,
-                                     (const T*)Q, (const T*)K, (const T*)V, (const T*)dO, (const T*)UQ, (const T*)UK,
-                                     (const T*)UV, L, Dv, alpha, E, (T*)Kt, (T*)Vt, parts, sums);
-  if (rc != BOB_OK || c.parts == 1) return rc;
-  return ext_add_parts(p, parts, c.parts, Kt, Vt, s);
+  const int64_t dynamic = pass2_dynamic(p, C::shape(c.form, has_bias(p)));
+  return ext_launch_columns(p, c, ext_args(p, c, p.B * p.Hkv, p.Nk, UT), parts, Kt, Vt, s,
+                            [&](const ExtArgs& a, dim3 grid) {
+                              return ext_dispatch<C>(c.form, p, grid, dynamic, s, a, (const T*)Q, (const T*)K,
+                                                     (const T*)V, (const T*)dO, (const T*)UQ, (const T*)UK,
+                                                     (const T*)UV, L, Dv, alpha, E, (T*)Kt, (T*)Vt, parts, sums);
+                            });
 }
 
 #define FB_EXT_PASS1(T, D, ...)                                                                                      \

@@ -82,13 +82,14 @@ int32_t ext_launch_bwd(const ExtProblem& p, const void* Q, const void* K, const 
   }
   if (rc != BOB_OK || p.Nk == 0) return rc;
   const ExtPlan c = ext_cols_plan<T, D>(p);
-  const ExtArgs a = ext_args(p, c, p.B * p.Hkv, p.Nk, nullptr);
-  rc = ext_dispatch<ExtColsBwd<T, D>>(c.form, p, dim3(a.total, c.parts),
-                                      cols_dynamic(p, ExtColsBwd<T, D>::shape(c.form, has_bias(p))), s, a, (const T*)Q,
-                                      (const T*)K, (const T*)V, (const T*)dO, L, (const float*)Dv, (T*)dK, (T*)dV, parts,
-                                      sums);
-  if (rc != BOB_OK || c.parts == 1) return rc;
-  return ext_add_parts(p, parts, c.parts, dK, dV, s);
+  using C = ExtColsBwd<T, D>;
+  const int64_t dynamic = cols_dynamic(p, C::shape(c.form, has_bias(p)));
+  return ext_launch_columns(p, c, ext_args(p, c, p.B * p.Hkv, p.Nk, nullptr), parts, dK, dV, s,
+                            [&](const ExtArgs& a, dim3 grid) {
+                              return ext_dispatch<C>(c.form, p, grid, dynamic, s, a, (const T*)Q, (const T*)K,
+                                                     (const T*)V, (const T*)dO, L, (const float*)Dv, (T*)dK, (T*)dV,
+                                                     parts, sums);
+                            });
 }
 
 #define FB_INST(T, D, ...)                                                                                        \

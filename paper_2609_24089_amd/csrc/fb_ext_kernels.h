@@ -38,7 +38,9 @@ constexpr int kStepPad = 64;  // steps of bias kept beyond R on either side
 struct ExtArgs {
   int H, grp;          // query heads of a batch entry, query heads that share a key/value head
   int Nq, Nk;
-  int nRB, total;      // blocks a head, blocks of the grid
+  int nRB, total;      // blocks a head, blocks of the problem
+  int block0, blocks;  // column kernels: those of this launch are block0 .. block0 + blocks - 1
+  int64_t row0, rows;  // and their key rows, counted over all key/value heads
   int causal;
   int fold;            // row kernels: the rows of the grp query heads of a key/value head form one matrix
   float scale;
@@ -267,6 +269,19 @@ __device__ __forceinline__ void ext_map_block(const ExtArgs& a, int per, bool la
   head = u * (per / a.nRB) + h;
   rb = at - h * a.nRB;
   if (last_heavy && a.causal != 0) rb = a.nRB - 1 - rb;
+}
+
+// The block of a column kernel's workgroup.  A slice of the problem's blocks has a run of
+// consecutive ones on each XCD.
+__device__ __forceinline__ void ext_map_cols(const ExtArgs& a, int& head, int& rb) {
+  if (a.blocks == a.total) {
+    ext_map_block(a, a.nRB, false, a.q_lens, a.Nq, head, rb);
+    return;
+  }
+  const int xcd = blockIdx.x % kXCDs, each = a.blocks / kXCDs, more = a.blocks % kXCDs;
+  const int id = a.block0 + xcd * each + min(xcd, more) + blockIdx.x / kXCDs;
+  head = id / a.nRB;
+  rb = id - head * a.nRB;
 }
 
 // Exponents of invalid keys to -inf: x[sb][r] belongs to key s0 + 16 sb + 4 (l >> 4) + r.
@@ -1004,13 +1019,13 @@ __device__ __forceinline__ float* ext_step_row(float* sums, const ExtArgs& a, in
 }
 
 // Stores the two key-side accumulators: to the outputs, or as one part's fp32 sums
-// ([nparts][2][B*Hkv][Nk][D]).  Columns that are no valid key get zeros.
+// ([nparts][2][the launch's key rows][D]).  Columns that are no valid key get zeros.
 template <typename T, int D, int KS, int NB, int MC>
 __device__ __forceinline__ void ext_store_cols(const ExtArgs& a, int kvh, int col0, int klen, int ks,
                                                const floatx4 (&x)[NB][MC], const floatx4 (&y)[NB][MC], float fx, float fy,
                                                T* __restrict__ X, T* __restrict__ Y, float* __restrict__ parts) {
   const int l = lane_id(), g = l >> 4, j = l & 15;
-  const int64_t plane = (int64_t)(a.total / a.nRB) * a.Nk * D;
+  const int64_t plane = a.rows * D, first = a.row0 * D;
   const floatx4 zero = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int mc = 0; mc < MC; ++mc) {
@@ -1022,8 +1037,8 @@ __device__ __forceinline__ void ext_store_cols(const ExtArgs& a, int kvh, int co
       const int64_t off = ((int64_t)kvh * a.Nk + col) * D + 16 * nb + 4 * g;
       const floatx4 vx = col < klen ? x[nb][mc] * fx : zero, vy = col < klen ? y[nb][mc] * fy : zero;
       if (a.nparts > 1) {
-        *(floatx4*)(parts + 2 * blockIdx.y * plane + off) = vx;
-        *(floatx4*)(parts + (2 * blockIdx.y + 1) * plane + off) = vy;
+        *(floatx4*)(parts + 2 * blockIdx.y * plane + off - first) = vx;
+        *(floatx4*)(parts + (2 * blockIdx.y + 1) * plane + off - first) = vy;
       } else {
         Elt<T>::store4(X + off, vx);
         Elt<T>::store4(Y + off, vy);
@@ -1071,7 +1086,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_cols_kernel(
   extern __shared__ float steps_mem[];
 
   int kv, rb;
-  ext_map_block(a, a.nRB, false, a.q_lens, a.Nq, kv, rb);
+  ext_map_cols(a, kv, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
   const int wl = __builtin_amdgcn_readfirstlane(KS == 1 ? wave_id() : wave_id() % NW);
@@ -1662,7 +1677,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass2_kernel(
   extern __shared__ float steps_mem[];
 
   int kv, rb;
-  ext_map_block(a, a.nRB, false, a.q_lens, a.Nq, kv, rb);
+  ext_map_cols(a, kv, rb);
   const int l = lane_id(), g = l >> 4, j = l & 15;
   const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
   const int wl = __builtin_amdgcn_readfirstlane(KS == 1 ? wave_id() : wave_id() % NW);
