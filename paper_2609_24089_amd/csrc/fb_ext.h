@@ -247,16 +247,19 @@ void ext_pick(const ExtProblem& p, const FormQuery& q, double narrow, Dynamic&& 
     const int64_t blocks = q.heads * ((q.N + 16 * f.blocks - 1) / (16 * f.blocks));
     if (i == 0) fills = f.resident > 1 && blocks * base > q.cus * f.resident;
     if (i > 0 && fills) continue;
-    const auto too_long = [&](int parts) { return q.tiles > max_chain * f.sets * parts; };
-    for (int m = 0; m <= 16; m = m == 0 ? 1 : 2 * m) {
-      f.parts = m == 0 ? base : unit * m;
+    const auto too_long = [&](int64_t parts) { return q.tiles > max_chain * f.sets * parts; };
+    for (int64_t m = 0;; m = m == 0 ? 1 : 2 * m) {
+      // 16 parts a unit are enough but for chains that are still too long
+      if (m > 16 && !too_long(unit * (m / 2))) break;
+      f.parts = (int)(m == 0 ? base : unit * m);
       if (m > 0 && f.parts <= base) continue;
       const int64_t total = blocks * f.parts;
-      if (too_long(f.parts) && m < 16) continue;
+      if (too_long(f.parts)) continue;
       const int64_t most = q.cus * (q.causal ? 2 : std::max<int64_t>(2, 4 * f.resident));
       const bool few = total <= most && f.parts * part_bytes <= kMaxPartBytes && q.tiles >= (int64_t)4 * f.sets * f.parts;
       if (m > 0 && !few && !too_long(base)) break;
-      if (total > INT32_MAX / 16 || total * f.threads > (int64_t)UINT32_MAX) continue;
+      // a launch takes fewer than 2^32 threads; slices of parts stay far below
+      if (f.parts == 1 && (total > INT32_MAX / 16 || total * f.threads > (int64_t)UINT32_MAX)) continue;
       double t = form_us(q, f) * (f.parts > base ? 1.08 : i > 0 ? q.margin : 1.0);
       if (f.parts > 1) t += kJoinUs + 2.0 * f.parts * (double)part_bytes / 4.0e6;
       if (!found || t < least) {
