@@ -126,7 +126,7 @@ int32_t ext_launch_columns(const ExtProblem& p, const ExtPlan& c, ExtArgs a, flo
   return BOB_OK;
 }
 
-// A kernel's LDS beside its dynamic part, as the runtime tells it.
+// A kernel's LDS beside its dynamic part, as the runtime tells it, and 1 (0: it does not tell).
 template <auto kKernel> int64_t static_lds() {
   static std::atomic<int> known;
   return read_once(known, [] {
@@ -134,6 +134,13 @@ template <auto kKernel> int64_t static_lds() {
     if (hipFuncGetAttributes(&at, (const void*)kKernel) != hipSuccess) return 0;
     return (int)at.sharedSizeBytes + 1;  // 0 is read again
   });
+}
+
+// Workgroups of kKernel that fit one CU with `dynamic` bytes of LDS beside the kernel's own: the
+// occupancy query knows the registers and the kernel's own LDS alone.
+template <auto kKernel> int ext_resident(int threads, int64_t dynamic) {
+  const int64_t own = std::max<int64_t>(static_lds<kKernel>(), 1) - 1, fit = kMaxLds / std::max<int64_t>(own + dynamic, 1);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(resident_blocks<kKernel>(threads), fit));
 }
 
 // ---------------------------------------------------------------------------
@@ -175,7 +182,7 @@ template <typename Kern, int F> Form ext_form_of(const ExtProblem& p, int64_t dy
     constexpr ExtShape s = Kern::shape(F, kBias);
     if constexpr (s.built()) {
       if (F > 0 && static_lds<Kern::template kernel<F, kBias>()>() + dynamic > kMaxLds) return {};
-      const int fit = resident_blocks<Kern::template kernel<F, kBias>()>(s.threads());
+      const int fit = ext_resident<Kern::template kernel<F, kBias>()>(s.threads(), kBias ? dynamic : 0);
       return {s.blocks(), s.ks, fit, s.threads(), 1, 0.0, F == 0 || F == 4 ? 1.0 : narrow};
     }
     return {};
@@ -191,7 +198,7 @@ int32_t ext_go(const ExtProblem& p, dim3 grid, int64_t dynamic, hipStream_t stre
     constexpr ExtShape s = Kern::shape(F, kBias);
     if constexpr (s.built()) {
       constexpr auto kernel = Kern::template kernel<F, kBias>();
-      a.fit = resident_blocks<kernel>(s.threads());
+      a.fit = ext_resident<kernel>(s.threads(), kBias ? dynamic : 0);
       if (p.causal != 0 && grid.y == 1) a.resident = balanced_order(a.total, a.fit, device_cus());
       (void)hipGetLastError();
       hipLaunchKernelGGL(kernel, grid, dim3(s.threads()), (unsigned)(kBias ? dynamic : 0), stream, a, args...);
