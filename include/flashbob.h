@@ -352,8 +352,10 @@ int32_t attn_bob3_rows(int32_t dtype, int64_t B, int64_t H, int64_t N, int64_t d
  *          beyond +-2^29 count as those.
  *  table   [num_buckets, H] in table_dtype (BOB_F32 or BOB_BF16), aligned to its
  *          type, or NULL: no bias (the other bias fields are then ignored).  An entry of
- *          -1e30 or less (-inf and the types' lowest values among them) makes its
- *          bucket's keys invalid.
+ *          -2^24 or less (-inf, the types' lowest values and the usual -1e9 among
+ *          them) makes its bucket's keys invalid.  Scores are formed in fp32, and
+ *          the backward calls take P from L: it is off by up to 2^-22 of the size
+ *          of the row's largest score, which should stay far below 2^24.
  *  buckets int32 [2 max_distance + 1]: the bucket of every step of position from -R
  *          to R (R = max_distance, 1..1024); steps beyond use the ends.  A bucket outside
  *          0..num_buckets - 1 counts as the nearer end.  num_buckets is 1..65536.

@@ -7,12 +7,12 @@ entry and query head at a time on its valid rows and keys alone, from the defini
   F = tau (U_Q K^T + Q U_K^T) + U_T[bucket],  St = P (Pt - E), Tt[c] = sum of St over c
 
 (the other closed forms are those of bob_oracle.py, which this file shares no code with).
-An entry of -1e30 or less masks its bucket.  A row without a valid key has O = 0, L = -inf
+An entry of -2^24 or less masks its bucket.  A row without a valid key has O = 0, L = -inf
 and no part in anything else.
 """
 import numpy as np
 
-MASKED = -1e30
+MASKED = -2.0 ** 24
 
 
 def _safe(x):

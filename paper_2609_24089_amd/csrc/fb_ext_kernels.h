@@ -81,8 +81,11 @@ __device__ __forceinline__ float ext_table(const ExtArgs& a, const void* t, int 
 
 // The bias of heads head0 .. head0 + heads - 1 at every step, `count` threads of the
 // workgroup at work: dst[hh * steps + R + kStepPad + step].  As an exponent (kExp) it is
-// times log2(e), and an entry of -1e30 or less (-inf and the types' lowest values among
-// them) masks its bucket's keys: the product with log2(e) of a lowest value overflows.
+// times log2(e), and an entry of kMaskedEntry or less masks its bucket's keys.  At that size a
+// score in fp32 has no fraction left: L rounds its logarithm of the weights' sum away, and P,
+// which the backward kernels take from L, would be that sum too large in a row that sees such
+// keys alone; the product with log2(e) of a lowest value overflows.
+constexpr float kMaskedEntry = -16777216.f;
 template <bool kExp>
 __device__ __forceinline__ void ext_fill_steps(const ExtArgs& a, const void* t, int head0, int heads, float FB_LDS* dst,
                                                int count) {
@@ -93,7 +96,7 @@ __device__ __forceinline__ void ext_fill_steps(const ExtArgs& a, const void* t, 
       const int hh = x / steps, at = x - hh * steps - kStepPad;
       const int bucket = min(max(a.buckets[min(max(at, 0), 2 * a.R)], 0), a.num_buckets - 1);
       v = ext_table(a, t, bucket, head0 + hh);
-      if (kExp) v = v <= -1e30f ? -INFINITY : v * kLog2e;
+      if (kExp) v = v <= kMaskedEntry ? -INFINITY : v * kLog2e;
     }
     dst[x] = v;
   }

@@ -17,7 +17,8 @@ padded rows hold is never read.
 bias is a pair (table, buckets): the scores gain
 table[buckets[clamp(j - (q_starts[b] + i), -R, R) + R], h], with table
 [num_buckets, H] in fp32 or bf16 and buckets int32 [2 R + 1] on the device
-(`relative_buckets` makes the usual ones).
+(`relative_buckets` makes the usual ones).  An entry of -2^24 or less (-inf, -1e9)
+masks its bucket's keys.
 """
 import ctypes
 
