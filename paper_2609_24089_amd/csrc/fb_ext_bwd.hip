@@ -24,9 +24,13 @@ template <typename T, int D> struct ExtColsBwd {
     // three waves per SIMD for some spills beside the near tiles: 814 us for 881 with two at
     // B4 H12 N4096 dense, 462 for 485 causal (first backward)
     constexpr bool kThree = std::is_same_v<T, bf16> && D == 64;
-    return form == 0   ? ExtShape{w.mr, w.nw, bias && kThree ? 3 : w.occ, 1}
-           : form == 4 ? ext_two_sets<T, D>(w, 2, 2 * kExtra + (w.kl ? 4 * Geo<T, D>::kTileElems * (int)sizeof(T) : 0))
-                       : ext_sets<T, D>(kFormWaves[form], 2, kExtra, waves, w.occ);
+    const ExtShape s =
+        form == 0   ? ExtShape{w.mr, w.nw, bias && kThree ? 3 : w.occ, 1}
+        : form == 4 ? ext_two_sets<T, D>(w, 2, 2 * kExtra + (w.kl ? 4 * Geo<T, D>::kTileElems * (int)sizeof(T) : 0))
+                    : ext_sets<T, D>(kFormWaves[form], 2, kExtra, waves, w.occ);
+    // one-wave sets that leave no room for their buffers of step sums (16 waves at bf16 d = 32)
+    const int ring = 4 * Geo<T, D>::kTileElems * (int)sizeof(T) + 4 * 2 * kBS * (int)sizeof(float);
+    return bias && form == 2 && s.ks * (ring + StepSums::kBufFloats * 4) > kMaxLds ? kNotBuilt : s;
   }
   template <int F, bool kBias> static __host__ constexpr auto kernel() {
     constexpr ExtShape s = shape(F, kBias);
