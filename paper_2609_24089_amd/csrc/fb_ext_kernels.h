@@ -151,13 +151,21 @@ __device__ __forceinline__ int vector_mode(int mode) {
   return mode;
 }
 
-// Run `index` of `count` equal runs over n tiles.
+// A value that is the same in all lanes of the wave, in a scalar register.
+__device__ __forceinline__ float scalar(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
+}
+
+// Run `index` of `count` equal runs over n tiles.  The division leaves its ends in vector
+// registers: there Pass 1 with a bias at d = 64 took 188 of them for 168 and lost its third wave
+// per SIMD (B4 H12 N4096 dense 1021 us for 967), and at d = 128 it
+// spilled ten in its loop (B2 H16 N4096 1631 us for 1135).
 struct ExtRun {
   int begin, end;
   __device__ __forceinline__ ExtRun(int n, int index, int count) {
     const int per = (n + count - 1) / count;
-    begin = min(index * per, n);
-    end = min(begin + per, n);
+    begin = __builtin_amdgcn_readfirstlane(min(index * per, n));
+    end = __builtin_amdgcn_readfirstlane(min(begin + per, n));
   }
   __device__ __forceinline__ int size() const { return end - begin; }
 };
@@ -1343,7 +1351,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb) aref[mb] = eref[mb] = 0.f;
   // parts that share a block take their sums from 0: each row of theirs has many keys in view
-  bool centred = split > 1;
+  bool centred = false;
   ext_stream<tile_loads<T, D, NW, 4>(), kBarrier>(
       kBarrier ? first.size() : run.size(),
       [&](int it, int st) {
@@ -1355,10 +1363,10 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
           ext_fill_steps<false>(a, a.dir, rw.head0, 1, dirs, KS * NW * 64);
           __syncthreads();
           const int n = ext_steps(a);
-          blo = steps[0];
-          bhi = steps[n - 1];
-          ulo = dirs[0];
-          uhi = dirs[n - 1];
+          blo = scalar(steps[0]);
+          bhi = scalar(steps[n - 1]);
+          ulo = scalar(dirs[0]);
+          uhi = scalar(dirs[n - 1]);
         }
       },
       [&](int it, int st) {
@@ -1444,7 +1452,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
           }
         }
         // every wave of a workgroup with sets comes here in its first iteration (a barrier)
-        if (KS > 1 ? it == 0 && split == 1 : !centred) {
+        if (split == 1 && (KS > 1 ? it == 0 : !centred)) {
           centred = true;
 #pragma unroll
           for (int mb = 0; mb < MR; ++mb) {
