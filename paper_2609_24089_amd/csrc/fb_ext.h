@@ -117,8 +117,8 @@ int32_t ext_launch_columns(const ExtProblem& p, const ExtPlan& c, ExtArgs a, flo
   for (int64_t first = 0; first < a.total; first += each) {
     a.block0 = (int)first;
     a.blocks = (int)std::min<int64_t>(each, a.total - first);
-    a.row0 = row(first);
-    a.rows = row(first + a.blocks) - a.row0;
+    a.row0 = a.blocks < a.total ? row(first) : 0;
+    a.rows = a.blocks < a.total ? row(first + a.blocks) - a.row0 : p.B * p.Hkv * p.Nk;
     int32_t rc = launch(a, dim3(a.blocks, c.parts));
     if (rc == BOB_OK && c.parts > 1) rc = ext_add_parts(p, a, parts, X, Y, s);
     if (rc != BOB_OK) return rc;
@@ -139,8 +139,12 @@ template <auto kKernel> int64_t static_lds() {
 // Workgroups of kKernel that fit one CU with `dynamic` bytes of LDS beside the kernel's own: the
 // occupancy query knows the registers and the kernel's own LDS alone.
 template <auto kKernel> int ext_resident(int threads, int64_t dynamic) {
-  const int64_t own = std::max<int64_t>(static_lds<kKernel>(), 1) - 1, fit = kMaxLds / std::max<int64_t>(own + dynamic, 1);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(resident_blocks<kKernel>(threads), fit));
+  int n = resident_blocks<kKernel>(threads);
+  if (dynamic > 0) {
+    const int64_t each = std::max<int64_t>(static_lds<kKernel>(), 1) - 1 + dynamic;
+    while (n > 1 && n * each > kMaxLds) --n;
+  }
+  return n;
 }
 
 // ---------------------------------------------------------------------------
