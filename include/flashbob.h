@@ -366,7 +366,8 @@ int32_t attn_bob3_rows(int32_t dtype, int64_t B, int64_t H, int64_t N, int64_t d
  * St_ij over the bucket, is Phi's gradient in the table; every other formula of the calls
  * above stands.  D here is the exact fp32 sum_j P_ij dP_ij, not do_i . o_i with o_i rounded.
  *
- * Workspaces are as those of the *_ws calls: the query gives the size for the same
+ * Workspaces are as those of the *_ws calls (the column kernels' fp32 sums take at most
+ * 512 MB of one, or a single block's): the query gives the size for the same
  * problem and attn_ext (of which it reads the table's presence and the sizes alone), 0 if
  * none is needed; a NULL, misaligned (16 bytes) or too small one gives BOB_EINVAL.
  * Errors as above; BOB_EINVAL also for a bias whose sizes are out of range or whose

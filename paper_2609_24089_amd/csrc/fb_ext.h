@@ -232,10 +232,11 @@ int32_t ext_dispatch(int form, const ExtProblem& p, dim3 grid, int64_t dynamic, 
 // Hkv12, 3622 queries, 1426 keys, d64, column side 387 -> 304 us with the row side, Pass 2 429
 // -> 307; Pass 1 of B1 H8, 1301 queries, 5846 keys 121 -> 96; two of 110 shapes lost a tenth.
 // max_chain: tiles that one accumulator of a column kernel may sum: longer ones drift
-// (SectionSums), so they are split whatever it costs.  Measured, one part -> chosen (us): a
-// token against 16384 keys, bf16 B1 H16 d64 46 -> 24, B1 H32 Hkv4 d128 131 -> 24; fp32 B2 H16
-// N1024 d128 causal Hessian-vector product 617 -> 475.  On 56 drawn problems the choice was 1
-// to 3% slower than the best form and parts on average before the parts of later rounds.
+// (SectionSums), so they are split whatever it costs, in slices of kSliceBytes.  Measured, one
+// part -> chosen (us): a token against 16384 keys, bf16 B1 H16 d64 46 -> 24, B1 H32 Hkv4 d128
+// 131 -> 24; fp32 B4 H8 Hkv4, 424 queries, 298 keys, d128 Hessian-vector product 617 -> 475.  On
+// 110 drawn problems the choice is 1 to 4% slower than the best form and parts on average; the
+// worst of 35 us and more are the forward's 1.39 and Pass 1's 1.33.
 constexpr double kJoinUs = 6.0;
 constexpr int64_t kMaxPartBytes = int64_t(128) << 20;
 constexpr unsigned kAnyForm = (1u << kForms) - 1;

@@ -21,11 +21,12 @@
 //    row's maximum or L is.  Long sequences are nearly all of the second kind.
 //  * Table gradients.  A column kernel's wave streams query tiles in order, so the steps
 //    that a tile meets lie in two windows of 32, the upper of which no later tile meets.
-//    Near tiles are summed along their diagonals through LDS (two lanes of one diagonal
-//    class, eight reads each per 16 columns), the upper window is stored, the lower carried
-//    in a register; far tiles add to one sum a side.  Each wave stores its own row of
-//    sums, so there are no atomics and the order is fixed; two small kernels add the rows
-//    and gather the steps into buckets.
+//    A near tile's blocks of equal step are added, summed along their diagonals by shifts
+//    inside a row of 16 lanes, and the four lane groups meet in a small LDS buffer of the
+//    wave's own; the upper window is stored, the lower carried in a register; far tiles add
+//    to one sum a side.  Each wave stores its own row of sums, so there are no atomics and
+//    the order is fixed; one kernel adds the rows and gathers the steps into buckets (from
+//    257 rows a head on after another that adds most of them).
 //  * Sets and parts.  Wave sets (KS) and workgroups (parts) that share stationary rows
 //    take one run of consecutive tiles each.
 #pragma once
@@ -312,8 +313,8 @@ __device__ __forceinline__ void ext_mask1(floatx4 (&x)[2], int s0, int klim) {
 // of a few query rows against a long cache, which reads each key and value once.
 // Bound by the keys' and values' bytes for a few rows (B32 H32 Hkv8, one token, up to 4096
 // keys, d128: 403 MB in 77 us, 5.2 TB/s, what a large copy reaches), by MFMA and VALU issue
-// for many (B1 H16 N8192 d128 causal with a bias: 258 us, 1.07 PFLOP/s; d64 0.80 PFLOP/s, where
-// an element's exponential meets half the MFMA work).
+// for many (B1 H16 N8192 d128 causal with a bias: 262 us, 1.05 PFLOP/s; B4 H12 N4096 d64 0.85 and
+// dense 0.92, where an element's exponential meets half the MFMA work).
 // ===========================================================================
 template <typename T, int D, int MR, int NW, int OCC, int KS, bool kBias>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_fwd_kernel(
@@ -594,8 +595,9 @@ __global__ __launch_bounds__(256) void ext_fwd_join_kernel(ExtArgs a, const floa
 // sum over many rows of fp32 products, and that rounding of o would be its largest error
 // by far (2^-8 of D a row against 2^-24).  In dQ it matters where few keys share a row's
 // weight (a row of one key has dQ = 0): a row whose whole weight lies in a set's first tile
-// takes D from that tile.  MFMA and VALU issue bound it: B4 H16 of 2048 ragged queries and
-// 4096 keys, d128, 326 us (0.96 PFLOP/s); B4 H12 N4096 d64 causal with a bias 175 us (0.89).
+// takes D from that tile.  MFMA and VALU issue bound it (47 and 38% busy at 1.6 waves
+// a SIMD, a quarter of the waves' time in waits): B4 H16 of 2048 ragged queries and 4096 keys,
+// d128, 305 us (1.02 PFLOP/s); B4 H12 N4096 d64 causal with a bias 173 us (0.89).
 // ===========================================================================
 template <typename T, int D, int MR, int NW, int OCC, int KS, bool kBias>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_rows_kernel(
@@ -1073,9 +1075,10 @@ __global__ __launch_bounds__(256) void ext_parts_kernel(const float* __restrict_
 }
 
 // First backward, column side: as attn_bwd_cols_kernel (its K rows in LDS with kKL), with
-// the table's step sums (`sums`, or null).  Issue bound, a third of the waves' time at the
-// tiles' barriers: B4 H16 of 2048 ragged queries and 4096 keys, d128, 446 us (0.93 PFLOP/s);
-// B4 H12 N4096 d64 causal with a bias 259 us (0.80), dense 732 us, without the bias 656.
+// the table's step sums (`sums`, or null).  Waits bound it, a third of
+// the waves' time (copies, barriers and LDS reads at 1.7 waves a SIMD; MFMA 44% and VALU 28% busy):
+// B4 H16 of 2048 ragged queries and 4096 keys, d128, 415 us (1.00 PFLOP/s); B4 H12 N4096 d64
+// causal with a bias 238 us (0.87), without 204; dense 439 us (0.94), without 383.
 template <typename T, int D, int MC, int NW, int OCC, int KS, bool kKL, bool kBias>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_cols_kernel(
     ExtArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ dO,
@@ -1288,9 +1291,9 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_bwd_cols_kernel(
 //   dOt = sum P u_V + sum P F' v - da O,  alpha = alpha* + da,  E = E* + de - alpha D,
 // since Pt - E = w - da (dP - D) - de.  It costs nothing after the first tile: alpha* rides
 // on the fma that scales F, -E* is where the C tile starts.  Wave sets share one estimate.
-// MFMA and VALU issue bound it: B4 H12 N4096 d64 dense with a bias 910 us (1.13 PFLOP/s of the
-// ten contractions), without 898; a wave's chain of LDS reads, MFMA and VALU where the grid
-// leaves one or two waves a SIMD (B2 H8 of 1000 queries and 2047 keys: 53 us, 0.55 PFLOP/s).
+// MFMA and VALU issue bound it: B4 H12 N4096 d64 dense with a bias 963 us (1.07 PFLOP/s of the
+// ten contractions), without 929; a wave's chain of LDS reads, MFMA and VALU where the grid
+// leaves one or two waves a SIMD (B2 H8 of 1000 queries and 2047 keys: 52 us, 0.56 PFLOP/s).
 // ===========================================================================
 template <typename T, int D, int MR, int NW, int OCC, int KS, int kPF, bool kBias>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass1_kernel(
@@ -1668,8 +1671,8 @@ __global__ __launch_bounds__(256) void ext_pass1_join_kernel(ExtArgs a, const fl
 
 // ===========================================================================
 // BoB Pass 2: as bob_pass2_kernel, with the second-order table sums (`sums`, or null).  Bound
-// as Pass 1: B4 H12 N4096 d64 dense with a bias 771 us (1.07 PFLOP/s of the eight
-// contractions), without 688: the near tiles' bias reads and step sums, and registers.
+// as Pass 1: B4 H12 N4096 d64 dense with a bias 792 us (1.04 PFLOP/s of the eight
+// contractions), without 705: the near tiles' bias reads and step sums, and registers.
 // ===========================================================================
 template <typename T, int D, int MC, int NW, int OCC, int KS, bool kPF, bool kBias>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void ext_pass2_kernel(
