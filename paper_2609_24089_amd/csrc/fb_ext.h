@@ -263,6 +263,7 @@ void ext_pick(const ExtProblem& p, const FormQuery& q, double narrow, Dynamic&& 
     for (int64_t m = 0;; m = m == 0 ? 1 : 2 * m) {
       // 16 parts a unit are enough but for chains that are still too long
       if (m > 16 && !too_long(unit * (m / 2))) break;
+      if (m > 0 && unit * m > 65535) break;  // a grid's second dimension
       f.parts = (int)(m == 0 ? base : unit * m);
       if (m > 0 && f.parts <= base) continue;
       const int64_t total = blocks * f.parts;

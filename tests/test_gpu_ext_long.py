@@ -33,6 +33,20 @@ def test_no_chain_passes_the_limit(dt, d, bias):
                     assert -(-each // got.wave_sets) <= CHAIN, (kernel, H, Nq, Nk, got)
 
 
+@pytest.mark.parametrize("bias", [None, (32, 128)])
+def test_no_grid_passes_a_launch(bias):
+    """A grid's second dimension, the parts, ends at 65535; groups of tens of thousands of heads
+    whose tiles already pass a chain."""
+    for kernel in (fb.ATTN_EXT_COLS, fb.ATTN_EXT_PASS2):
+        for H in (65535, 40000, 32768, 20000, 4096):
+            for Nq in (1, 100, 5000, (1 << 30) // H - 1):
+                for Nk in (1, 300):
+                    if H * max(Nk, 64) // 64 >= 1 << 24 or H * ((max(Nq, Nk) + 63) // 64) >= 1 << 24:
+                        continue
+                    got = fb.attn_ext_layout(kernel, torch.bfloat16, 1, H, 1, Nq, Nk, 64, False, bias)
+                    assert 1 <= got.parts <= 65535, (H, Nq, Nk, got)
+
+
 def test_workspaces_of_the_longest_sequences():
     """B1 H16 d64 at 2^22 rows: parts of the whole problem would take 275 GB.  Step sums: a row
     of 5 floats a wave."""
