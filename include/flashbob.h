@@ -444,6 +444,71 @@ typedef struct {
 int32_t attn_ext_layout(int32_t kernel, int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,
                         int64_t d, int32_t causal, const attn_ext* ext, attn_ext_launch* launch);
 
+/* ---------------------------------------------------------------------------
+ * Attention over capped scores, with a bias that falls with distance, and masks by
+ * spans of positions (packed documents, prefixes): shapes, positions, lengths, empty rows,
+ * outputs, workspaces and errors are those of the attn_ext_* calls, and with
+ *   s_ij = scale q_i . k_j,  z_ij = cap tanh(s_ij / cap) - slopes[h] |j - (s_b + i)|
+ * P is the softmax of z over the valid keys.  The first backward's dS is dz (1 - tanh^2), and the
+ * passes take the second derivative of the tanh along; there is no gradient in cap and slopes.
+ *
+ * attn_score (NULL: a plain softmax); all pointers are device memory of the current device:
+ *  q_lens, kv_lens, q_starts  as in attn_ext.
+ *  spans   int32 [B,Nk,4], 16-byte aligned, or NULL.  Entry p of a batch entry holds for position p
+ *          k0, k1, q0, q1: its query sees the keys k0 <= j < k1, and its key is seen by the queries
+ *          of the positions q0 <= i < q1.  The two have to tell the same mask, j in [k0(i), k1(i))
+ *          exactly where i in [q0(j), q1(j)): else the gradients are not those of the output.
+ *          Bounds beyond 0..Nk count as the nearer end; k0 >= k1 is an empty row, as are rows
+ *          whose position lies outside 0..Nk - 1.  With spans `causal` must be 0.  Rows and keys
+ *          that the mask hides from each other enter products with a weight of 0 where they
+ *          share a tile, so they have to be finite.
+ *  slopes  fp32 [H] or NULL (0); with slopes H / Hkv is at most 1024.
+ *  cap     0: none; else 1e-6 to 1e6 (and |scale| up to 1e6). */
+typedef struct {
+  const int32_t* q_lens;
+  const int32_t* kv_lens;
+  const int32_t* q_starts;
+  const int32_t* spans;
+  const float* slopes;
+  float cap;
+} attn_score;
+
+/* Forward.  In: Q, K, V.  Out: O, L. */
+int32_t attn_score_fwd_lse(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
+                           float scale, int32_t causal, const attn_score* score, const void* Q, const void* K,
+                           const void* V, void* O, float* L, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* First backward.  In: Q, K, V, O, dO, L.  Out: dQ, dK, dV, D. */
+int32_t attn_score_bwd(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
+                       float scale, int32_t causal, const attn_score* score, const void* Q, const void* K,
+                       const void* V, const void* O, const void* dO, const float* L, void* dQ, void* dK, void* dV,
+                       float* D, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* BoB Pass 1.  In: Q, K, V, O, dO, gdQ, gdK, gdV, L, D, dQ (required).  Out: Qt, dOt, alpha, E.
+ * D must be attn_score_bwd's. */
+int32_t attn_score_pass1_rows(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
+                              float scale, int32_t causal, const attn_score* score, const void* Q, const void* K,
+                              const void* V, const void* O, const void* dO, const void* gdQ, const void* gdK,
+                              const void* gdV, const float* L, const float* D, const void* dQ, void* Qt, void* dOt,
+                              float* alpha, float* E, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* BoB Pass 2, after Pass 1.  In: Q, K, V, dO, gdQ, gdK, gdV, L, D, alpha, E.  Out: Kt, Vt. */
+int32_t attn_score_pass2_cols(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
+                              float scale, int32_t causal, const attn_score* score, const void* Q, const void* K,
+                              const void* V, const void* dO, const void* gdQ, const void* gdK, const void* gdV,
+                              const float* L, const float* D, const float* alpha, const float* E, void* Kt, void* Vt,
+                              void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Workspace bytes of a call on the current device (0: none, or the call reports an error).  Of
+ * attn_score it reads the presence of the pointers and the cap alone. */
+enum { ATTN_SCORE_FWD = 0, ATTN_SCORE_BWD = 1, ATTN_SCORE_PASS1 = 2, ATTN_SCORE_PASS2 = 3 };
+int64_t attn_score_workspace_bytes(int32_t call, int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq,
+                                   int64_t Nk, int64_t d, int32_t causal, const attn_score* score);
+
+/* As attn_ext_layout (kernels ATTN_EXT_*). */
+int32_t attn_score_layout(int32_t kernel, int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,
+                          int64_t d, int32_t causal, const attn_score* score, attn_ext_launch* launch);
+
 /* 1 if (dtype, d) is built into this library, else 0. */
 int32_t bob_supported(int32_t dtype, int64_t d);
 

@@ -90,8 +90,9 @@ def load_library():
     lib.attn_bob_pass2_cols_gqa_noalloc.restype = i32
     lib.bob_scratch_bytes.argtypes = []
     lib.bob_scratch_bytes.restype = i64
-    from . import _fb_torch, ext
+    from . import _fb_torch, ext, score
     ext._declare(lib)
+    score._declare(lib)
     _fb_torch.bind(LIB_PATH)
     _lib, _native = lib, _fb_torch
     return lib
@@ -432,3 +433,6 @@ from .ext import (  # noqa: E402  (attention between sequences of two lengths, w
     ATTN_EXT_COLS, ATTN_EXT_FWD, ATTN_EXT_PASS1, ATTN_EXT_PASS2, ATTN_EXT_ROWS, AttnExt, AttnExtLaunch, attn_ext_bwd,
     attn_ext_fwd_lse, attn_ext_layout, attn_ext_pass1_rows, attn_ext_pass2_cols, biased_attention, cross_attention,
     relative_buckets)
+from .score import (  # noqa: E402  (attention over capped scores, distance biases and spans)
+    ATTN_SCORE_BWD, ATTN_SCORE_FWD, ATTN_SCORE_PASS1, ATTN_SCORE_PASS2, AttnScore, attention_spans, attn_score_bwd,
+    attn_score_fwd_lse, attn_score_layout, attn_score_pass1_rows, attn_score_pass2_cols, scored_attention)

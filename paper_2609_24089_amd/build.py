@@ -28,6 +28,12 @@ SOURCES = [
     ("fb_ext_pass1.hip", []),
     ("fb_ext_pass2.hip", []),
     ("fb_ext_bob_d128.hip", ["-mllvm", "-amdgpu-sched-strategy=iterative-ilp"]),
+    ("fb_ext_score.hip", []),
+    ("fb_ext_score_fwd.hip", []),
+    ("fb_ext_score_bwd.hip", []),
+    ("fb_ext_score_pass1.hip", []),
+    ("fb_ext_score_pass2.hip", []),
+    ("fb_ext_score_bob_d128.hip", ["-mllvm", "-amdgpu-sched-strategy=iterative-ilp"]),
 ]
 
 # -packed-fp32-ops keeps hipcc from emitting v_pk_*_f32 (the host pass warns

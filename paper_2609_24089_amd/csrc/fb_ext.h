@@ -19,6 +19,8 @@ struct ExtProblem {
   attn_ext x;   // zeros where the caller gave none
 };
 inline bool has_bias(const ExtProblem& p) { return p.x.table != nullptr; }
+// Which of a form's two kernels runs the problem (kBias of the ext kernels).
+inline bool ext_variant(const ExtProblem& p) { return has_bias(p); }
 inline int ext_group(const ExtProblem& p) { return (int)(p.H / p.Hkv); }
 inline int64_t ext_width(const ExtProblem& p) { return 2 * (int64_t)p.x.max_distance + 3; }
 
@@ -86,6 +88,15 @@ int32_t ext_launch_pass2(const ExtProblem& p, const void* Q, const void* K, cons
   M(bf16, 32, __VA_ARGS__) M(bf16, 64, __VA_ARGS__) M(bf16, 128, __VA_ARGS__) M(bf16, 256, __VA_ARGS__) \
   M(float, 32, __VA_ARGS__) M(float, 64, __VA_ARGS__) M(float, 128, __VA_ARGS__)
 
+// The joining launches of the row kernels' parts, for the kernels of either header.
+template <typename T, int D>
+int32_t ext_join_fwd(const ExtArgs& a, const float* parts, int64_t all, void* O, float* L, hipStream_t s);
+template <typename T, int D>
+int32_t ext_join_bwd(const ExtArgs& a, const float* parts, int64_t all, void* dQ, float* Dv, hipStream_t s);
+template <typename T, int D>
+int32_t ext_join_pass1(const ExtArgs& a, const float* parts, int64_t all, const void* O, const float* Dv,
+                       const void* dQ, void* Qt, void* dOt, float* alpha, float* E, hipStream_t s);
+
 // Adds the parts of a column kernel ([nparts][2][a.rows][d]) into X and Y.
 int32_t ext_add_parts(const ExtProblem& p, const ExtArgs& a, const float* parts, void* X, void* Y, hipStream_t s);
 
@@ -109,9 +120,9 @@ inline ExtSlices ext_slices(const ExtProblem& p, const ExtPlan& c) {
 }
 
 // Runs launch(a, grid) for every slice of the column kernel's blocks, and adds its parts.
-template <typename Launch>
-int32_t ext_launch_columns(const ExtProblem& p, const ExtPlan& c, ExtArgs a, float* parts, void* X, void* Y,
-                           hipStream_t s, Launch&& launch) {
+template <typename A, typename Launch>
+int32_t ext_launch_columns(const ExtProblem& p, const ExtPlan& c, A a, float* parts, void* X, void* Y, hipStream_t s,
+                           Launch&& launch) {
   const int64_t each = ext_slices(p, c).blocks;
   auto row = [&](int64_t block) { return block / a.nRB * p.Nk + block % a.nRB * (16 * c.blocks); };
   for (int64_t first = 0; first < a.total; first += each) {
@@ -149,7 +160,7 @@ template <auto kKernel> int ext_resident(int threads, int64_t dynamic) {
 
 // ---------------------------------------------------------------------------
 // Kernels: whole blocks, and 64-, 32- and 16-row blocks in wave sets.
-// Kern::kernel<form, bias>() names the kernel, Kern::shape(form, bias) its shape.
+// Kern::kernel<form, variant>() names the kernel, Kern::shape(form, variant) its shape.
 // ---------------------------------------------------------------------------
 struct ExtShape {
   int mr, nw, occ, ks;
@@ -180,41 +191,40 @@ template <typename T, int D> constexpr ExtShape ext_two_sets(const Shape& w, int
   return fits ? ExtShape{w.mr, w.nw, 2, 2} : kNotBuilt;
 }
 
-template <typename Kern, int F> Form ext_form_of(const ExtProblem& p, int64_t dynamic, double narrow) {
-  auto form = [&](auto bias) -> Form {
-    constexpr bool kBias = decltype(bias)::value;
-    constexpr ExtShape s = Kern::shape(F, kBias);
+template <typename Kern, int F, typename P> Form ext_form_of(const P& p, int64_t dynamic, double narrow) {
+  auto form = [&](auto variant) -> Form {
+    constexpr bool kVariant = decltype(variant)::value;
+    constexpr ExtShape s = Kern::shape(F, kVariant);
     if constexpr (s.built()) {
-      if (F > 0 && static_lds<Kern::template kernel<F, kBias>()>() + dynamic > kMaxLds) return {};
-      const int fit = ext_resident<Kern::template kernel<F, kBias>()>(s.threads(), kBias ? dynamic : 0);
+      if (F > 0 && static_lds<Kern::template kernel<F, kVariant>()>() + dynamic > kMaxLds) return {};
+      const int fit = ext_resident<Kern::template kernel<F, kVariant>()>(s.threads(), dynamic);
       return {s.blocks(), s.ks, fit, s.threads(), 1, 0.0, F == 0 || F == 4 ? 1.0 : narrow};
     }
     return {};
   };
-  return has_bias(p) ? form(std::true_type{}) : form(std::false_type{});
+  return ext_variant(p) ? form(std::true_type{}) : form(std::false_type{});
 }
 
 // Launches form F of Kern, whose first argument is a.
-template <typename Kern, int F, typename... Args>
-int32_t ext_go(const ExtProblem& p, dim3 grid, int64_t dynamic, hipStream_t stream, ExtArgs a, Args... args) {
-  auto go = [&](auto bias) -> int32_t {
-    constexpr bool kBias = decltype(bias)::value;
-    constexpr ExtShape s = Kern::shape(F, kBias);
+template <typename Kern, int F, typename P, typename A, typename... Args>
+int32_t ext_go(const P& p, dim3 grid, int64_t dynamic, hipStream_t stream, A a, Args... args) {
+  auto go = [&](auto variant) -> int32_t {
+    constexpr bool kVariant = decltype(variant)::value;
+    constexpr ExtShape s = Kern::shape(F, kVariant);
     if constexpr (s.built()) {
-      constexpr auto kernel = Kern::template kernel<F, kBias>();
-      a.fit = ext_resident<kernel>(s.threads(), kBias ? dynamic : 0);
+      constexpr auto kernel = Kern::template kernel<F, kVariant>();
+      a.fit = ext_resident<kernel>(s.threads(), dynamic);
       if (p.causal != 0 && grid.y == 1) a.resident = balanced_order(a.total, a.fit, device_cus());
       (void)hipGetLastError();
-      hipLaunchKernelGGL(kernel, grid, dim3(s.threads()), (unsigned)(kBias ? dynamic : 0), stream, a, args...);
+      hipLaunchKernelGGL(kernel, grid, dim3(s.threads()), (unsigned)dynamic, stream, a, args...);
       return finish_launch();
     }
     return BOB_EUNSUPPORTED;
   };
-  return has_bias(p) ? go(std::true_type{}) : go(std::false_type{});
+  return ext_variant(p) ? go(std::true_type{}) : go(std::false_type{});
 }
-template <typename Kern, typename... Args>
-int32_t ext_dispatch(int form, const ExtProblem& p, dim3 grid, int64_t dynamic, hipStream_t stream, const ExtArgs& a,
-                     Args... args) {
+template <typename Kern, typename P, typename A, typename... Args>
+int32_t ext_dispatch(int form, const P& p, dim3 grid, int64_t dynamic, hipStream_t stream, const A& a, Args... args) {
   if (form == 4) return ext_go<Kern, 4>(p, grid, dynamic, stream, a, args...);
   if (form == 3) return ext_go<Kern, 3>(p, grid, dynamic, stream, a, args...);
   if (form == 2) return ext_go<Kern, 2>(p, grid, dynamic, stream, a, args...);
@@ -240,10 +250,10 @@ int32_t ext_dispatch(int form, const ExtProblem& p, dim3 grid, int64_t dynamic, 
 constexpr double kJoinUs = 6.0;
 constexpr int64_t kMaxPartBytes = int64_t(128) << 20;
 constexpr unsigned kAnyForm = (1u << kForms) - 1;
-template <typename Kern, typename Dynamic>
-void ext_pick(const ExtProblem& p, const FormQuery& q, double narrow, Dynamic&& dynamic, unsigned allowed, int base,
+template <typename Kern, typename P, typename Dynamic>
+void ext_pick(const P& p, const FormQuery& q, double narrow, Dynamic&& dynamic, unsigned allowed, int base,
               int unit, int64_t part_bytes, ExtPlan* c, int64_t max_chain = int64_t(1) << 40) {
-  const bool b = has_bias(p);
+  const bool b = ext_variant(p);
   const Form forms[kForms] = {ext_form_of<Kern, 0>(p, dynamic(Kern::shape(0, b)), 1.0),
                               ext_form_of<Kern, 1>(p, dynamic(Kern::shape(1, b)), narrow),
                               ext_form_of<Kern, 2>(p, dynamic(Kern::shape(2, b)), narrow),
@@ -288,6 +298,33 @@ void ext_pick(const ExtProblem& p, const FormQuery& q, double narrow, Dynamic&& 
   c->sets = s.ks;
   c->resident = q.cus > 0 ? forms[c->form].resident : 0;
   c->waves = s.ks * s.nw;
+}
+
+// Returns BOB_OK to proceed, or an error; sets *empty where there is nothing to compute.
+int32_t ext_check(const ExtProblem& p, bool* empty);
+
+// Returns FN<type, head dim>(...) of the problem.
+#define FB_EXT_DISPATCH(p, FN, ...)                                                   \
+  do {                                                                                \
+    if ((p).dtype == BOB_BF16 && (p).d == 32) return FN<fb::bf16, 32>(__VA_ARGS__);   \
+    if ((p).dtype == BOB_BF16 && (p).d == 64) return FN<fb::bf16, 64>(__VA_ARGS__);   \
+    if ((p).dtype == BOB_BF16 && (p).d == 128) return FN<fb::bf16, 128>(__VA_ARGS__); \
+    if ((p).dtype == BOB_BF16 && (p).d == 256) return FN<fb::bf16, 256>(__VA_ARGS__); \
+    if ((p).dtype == BOB_F32 && (p).d == 32) return FN<float, 32>(__VA_ARGS__);       \
+    if ((p).dtype == BOB_F32 && (p).d == 64) return FN<float, 64>(__VA_ARGS__);       \
+    return FN<float, 128>(__VA_ARGS__);                                               \
+  } while (0)
+
+// Pointers of matrices of `n` rows: aligned, and not NULL unless they are empty.
+inline bool ext_ptrs(int64_t n, std::initializer_list<const void*> ptrs) {
+  if (n == 0) return true;
+  return check_ptrs(ptrs) == BOB_OK;
+}
+
+// Workspace of a row kernel: `floats` of each part and row (the forward's sums, reference and
+// weight; the first backward's sums and D; Pass 1's three sums and four scalars).
+inline int64_t ext_row_bytes(const ExtProblem& p, const ExtPlan& c, int64_t floats) {
+  return c.parts > 1 ? (c.parts * p.B * p.H * p.Nq * floats * 4 + 15) / 16 * 16 : 0;
 }
 
 // A causal problem whose queries start its keys: the blocks' work grows to the diagonal.

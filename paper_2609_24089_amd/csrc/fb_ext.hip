@@ -84,8 +84,7 @@ int32_t ext_add_parts(const ExtProblem& p, const ExtArgs& a, const float* parts,
   return finish_launch();
 }
 
-// Returns BOB_OK to proceed, or an error; sets *empty where there is nothing to compute.
-static int32_t ext_check(const ExtProblem& p, bool* empty) {
+int32_t ext_check(const ExtProblem& p, bool* empty) {
   *empty = false;
   if (p.dtype != BOB_F32 && p.dtype != BOB_BF16) return BOB_EINVAL;
   if (p.B < 0 || p.H < 0 || p.Nq < 0 || p.Nk < 0 || p.d < 1) return BOB_EINVAL;
@@ -124,31 +123,9 @@ static ExtProblem ext_problem(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, 
   return p;
 }
 
-#define FB_EXT_DISPATCH(p, FN, ...)                                                   \
-  do {                                                                                \
-    if ((p).dtype == BOB_BF16 && (p).d == 32) return FN<fb::bf16, 32>(__VA_ARGS__);   \
-    if ((p).dtype == BOB_BF16 && (p).d == 64) return FN<fb::bf16, 64>(__VA_ARGS__);   \
-    if ((p).dtype == BOB_BF16 && (p).d == 128) return FN<fb::bf16, 128>(__VA_ARGS__); \
-    if ((p).dtype == BOB_BF16 && (p).d == 256) return FN<fb::bf16, 256>(__VA_ARGS__); \
-    if ((p).dtype == BOB_F32 && (p).d == 32) return FN<float, 32>(__VA_ARGS__);       \
-    if ((p).dtype == BOB_F32 && (p).d == 64) return FN<float, 64>(__VA_ARGS__);       \
-    return FN<float, 128>(__VA_ARGS__);                                               \
-  } while (0)
-
-// Pointers of matrices of `n` rows: aligned, and not NULL unless they are empty.
-static bool ext_ptrs(int64_t n, std::initializer_list<const void*> ptrs) {
-  if (n == 0) return true;
-  return check_ptrs(ptrs) == BOB_OK;
-}
-
-// Workspace of a row kernel: `floats` of each part and row (the forward's sums, reference and
-// weight; the first backward's sums and D; Pass 1's three sums and four scalars).
-static int64_t row_bytes(const ExtProblem& p, const ExtPlan& c, int64_t floats) {
-  return c.parts > 1 ? (c.parts * p.B * p.H * p.Nq * floats * 4 + 15) / 16 * 16 : 0;
-}
-static int64_t fwd_bytes(const ExtProblem& p, const ExtPlan& c) { return row_bytes(p, c, p.d + 2); }
-static int64_t rows_bytes(const ExtProblem& p, const ExtPlan& c) { return row_bytes(p, c, p.d + 1); }
-static int64_t pass1_bytes(const ExtProblem& p, const ExtPlan& c) { return row_bytes(p, c, 3 * p.d + 4); }
+static int64_t fwd_bytes(const ExtProblem& p, const ExtPlan& c) { return ext_row_bytes(p, c, p.d + 2); }
+static int64_t rows_bytes(const ExtProblem& p, const ExtPlan& c) { return ext_row_bytes(p, c, p.d + 1); }
+static int64_t pass1_bytes(const ExtProblem& p, const ExtPlan& c) { return ext_row_bytes(p, c, 3 * p.d + 4); }
 // Workspace of a column kernel: the parts' fp32 sums, then the waves' rows of step sums and
 // what ext_step_rows_kernel makes of them.
 struct ColBytes {

@@ -77,12 +77,7 @@ int32_t ext_launch_bwd(const ExtProblem& p, const void* Q, const void* K, const 
     const ExtArgs a = ext_args(p, r, p.B * p.H, p.Nq, nullptr);
     rc = ext_dispatch<ExtRowsBwd<T, D>>(r.form, p, dim3(a.total, r.parts), ext_steps_bytes(p), s, a, (const T*)Q,
                                         (const T*)K, (const T*)V, (const T*)O, (const T*)dO, L, (T*)dQ, Dv, row_parts);
-    if (rc == BOB_OK && r.parts > 1) {
-      const int64_t all = p.B * p.H * p.Nq;
-      hipLaunchKernelGGL((ext_bwd_join_kernel<T, D>), dim3((unsigned)((all * (D / 4) + 255) / 256)), dim3(256), 0, s, a,
-                         (const float*)row_parts, all, (T*)dQ, Dv);
-      rc = finish_launch();
-    }
+    if (rc == BOB_OK && r.parts > 1) rc = ext_join_bwd<T, D>(a, row_parts, p.B * p.H * p.Nq, dQ, Dv, s);
   }
   if (rc != BOB_OK || p.Nk == 0) return rc;
   const ExtPlan c = ext_cols_plan<T, D>(p);
@@ -96,13 +91,21 @@ int32_t ext_launch_bwd(const ExtProblem& p, const void* Q, const void* K, const 
                             });
 }
 
+template <typename T, int D>
+int32_t ext_join_bwd(const ExtArgs& a, const float* parts, int64_t all, void* dQ, float* Dv, hipStream_t s) {
+  hipLaunchKernelGGL((ext_bwd_join_kernel<T, D>), dim3((unsigned)((all * (D / 4) + 255) / 256)), dim3(256), 0, s, a,
+                     parts, all, (T*)dQ, Dv);
+  return finish_launch();
+}
+
 #define FB_INST(T, D, ...)                                                                                        \
   template ExtPlan ext_rows_plan<T, D>(const ExtProblem&);                                                        \
   template ExtPlan ext_cols_plan<T, D>(const ExtProblem&);                                                        \
   template int32_t ext_launch_bwd<T, D>(const ExtProblem&, const void*, const void*, const void*, const void*,    \
                                         const void*, const float*, void*, void*, void*, float*, float*, float*,   \
                                         float*,                                                                   \
-                                        hipStream_t);
+                                        hipStream_t);                                                             \
+  template int32_t ext_join_bwd<T, D>(const ExtArgs&, const float*, int64_t, void*, float*, hipStream_t);
 FB_EXT_EACH(FB_INST)
 
 }  // namespace fb

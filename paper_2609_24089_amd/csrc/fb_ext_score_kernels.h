@@ -1,0 +1,1434 @@
+// Attention over capped scores, distance biases and masks by spans of positions: forward,
+// first backward and the two BoB passes as gfx950 kernels.
+//
+// The problem is that of fb_ext_kernels.h (two lengths, valid rows of each batch entry,
+// positions past a cache) with, in the place of the bias by buckets,
+//   Z = c tanh(S / c) - m_h |pos_q - pos_k|,  S = tau Q K^T,  P = softmax of Z over valid keys,
+// either term optional (no cap: Z takes S itself), and with the causal mask generalised to
+// spans: per position p of a batch entry the keys k0 .. k1 - 1 that its query sees and the
+// positions q0 .. q1 - 1 whose queries see its key.  Packed documents and prefixes are such
+// masks; each side finds from the spans of its own rows which tiles of the other it meets, so
+// a tile that no row sees is neither loaded nor computed.
+//
+// With t = tanh(S / c), u = dZ/dS = 1 - t^2 and u' = -2 t u / c the identities are those of
+// the uncapped problem with dZ = P (dP - D) for its dS and F = u Fs, Fs = tau (U_Q K^T +
+// Q U_K^T), but where a score's gradient meets the matrices:
+//   dS = u dZ,   St = u P (Pt - E) + u' dZ Fs = P (u (Pt - E) - (2 / c) t (dP - D) F).
+// The distance bias is constant, so it enters Z alone.
+//
+// The kernels keep the skeleton, tiles, sets, parts and folded rows of fb_ext_kernels.h, and
+// the exactness of D and the references of Pass 1 explained there.
+#pragma once
+#include "fb_ext_kernels.h"
+
+namespace fb {
+
+struct ScoreArgs : ExtArgs {
+  const int32_t* spans;  // [B, Nk, 4]: k0, k1, q0, q1 of each position, or null: causal or dense
+  const float* slopes;   // [H] or null: 0
+  float cap_in;          // S / c as an argument of tanh for cap_tanh()
+  float cap_out;         // c log2(e)
+  float cap_k;           // 2 / c
+};
+
+// ---------------------------------------------------------------------------
+// The cap
+// ---------------------------------------------------------------------------
+// tanh of x: bf16 takes y = 2 log2(e) x, as 1 - 2 / (1 + 2^y), off by 2^-23 of 1 (1e-5 of a
+// score of c = 50: P is rounded to bf16 afterwards).  fp32 takes x and is within some 2^-23 of
+// the result: the same for |x| > 0.45, the Taylor series (next term below 2^-25 of x) below.
+template <typename T> __device__ __forceinline__ float cap_tanh(float s, float cap_in);
+template <> __device__ __forceinline__ float cap_tanh<bf16>(float s, float cap_in) {
+  return __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + fast_exp2(s * cap_in)), 1.f);
+}
+template <> __device__ __forceinline__ float cap_tanh<float>(float s, float cap_in) {
+  const float x = s * cap_in;
+  float ax = fabsf(x);
+  ax = ax > 20.f ? 20.f : ax;  // tanh is 1 there; a NaN stays
+  const float d = 1.f + fast_exp2(2.f * kLog2e * ax);
+  float r = __builtin_amdgcn_rcpf(d);
+  r = __builtin_fmaf(r, __builtin_fmaf(-d, r, 1.f), r);
+  const float far = __builtin_copysignf(__builtin_fmaf(-2.f, r, 1.f), x);
+  const float q = x * x;
+  float p = -929569.f / 638512875.f;
+  p = __builtin_fmaf(p, q, 21844.f / 6081075.f);
+  p = __builtin_fmaf(p, q, -1382.f / 155925.f);
+  p = __builtin_fmaf(p, q, 62.f / 2835.f);
+  p = __builtin_fmaf(p, q, -17.f / 315.f);
+  p = __builtin_fmaf(p, q, 2.f / 15.f);
+  p = __builtin_fmaf(p, q, -1.f / 3.f);
+  const float near = __builtin_fmaf(x * q, p, x);
+  return ax < 0.45f ? near : far;
+}
+template <typename T> constexpr float kCapArg = std::is_same_v<T, bf16> ? 2.f * kLog2e : 1.f;  // of cap_in
+
+// ---------------------------------------------------------------------------
+// Spans
+// ---------------------------------------------------------------------------
+struct Interval {
+  int lo, hi;  // lo >= hi: empty
+};
+// The keys that query row `query` of entry b sees, and the query rows that key `key` is seen by.
+__device__ __forceinline__ Interval score_keys(const ScoreArgs& a, const ExtLens& n, int b, int query) {
+  const int pos = n.start + query;
+  Interval v{0, a.causal != 0 ? min(n.k, pos + 1) : n.k};
+  if (a.spans != nullptr) {
+    v.hi = 0;
+    if (pos >= 0 && pos < a.Nk) {
+      const int32_t* const s = a.spans + 4 * ((int64_t)b * a.Nk + pos);
+      v = Interval{max(s[0], 0), min(s[1], n.k)};
+    }
+  }
+  return v;
+}
+__device__ __forceinline__ Interval score_queries(const ScoreArgs& a, const ExtLens& n, int b, int key) {
+  Interval v{a.causal != 0 ? max(key - n.start, 0) : 0, n.q};
+  if (a.spans != nullptr) {
+    const int32_t* const s = a.spans + 4 * ((int64_t)b * a.Nk + key);
+    v = Interval{max(max(s[2], 0) - n.start, 0), min(min(s[3], a.Nk) - n.start, n.q)};
+  }
+  return v;
+}
+
+// What the intervals of several rows have together: some row's from any_lo to any_hi, every
+// row's between all_lo and all_hi.
+struct Reach {
+  int any_lo = INT32_MAX, any_hi = 0, all_lo = 0, all_hi = INT32_MAX;
+  __device__ __forceinline__ void add(Interval v) {
+    if (v.lo < v.hi) {
+      any_lo = min(any_lo, v.lo);
+      any_hi = max(any_hi, v.hi);
+      all_lo = max(all_lo, v.lo);
+      all_hi = min(all_hi, v.hi);
+    } else {
+      all_hi = -1;
+    }
+  }
+  // over the lanes whose index differs in the bits below `lanes`, into scalar registers
+  template <int lanes> __device__ __forceinline__ void join() {
+#pragma unroll
+    for (int m = 1; m < lanes; m *= 2) {
+      any_lo = min(any_lo, __shfl_xor(any_lo, m));
+      any_hi = max(any_hi, __shfl_xor(any_hi, m));
+      all_lo = max(all_lo, __shfl_xor(all_lo, m));
+      all_hi = min(all_hi, __shfl_xor(all_hi, m));
+    }
+    any_lo = __builtin_amdgcn_readfirstlane(any_lo);
+    any_hi = __builtin_amdgcn_readfirstlane(any_hi);
+    all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+    all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+  }
+  // 0: no valid pair of the tile at s0, 1: all valid for every row, 2: mixed
+  __device__ __forceinline__ int mode(int s0) const {
+    return s0 >= any_hi || s0 + kBS <= any_lo ? 0 : s0 >= all_lo && s0 + kBS <= all_hi ? 1 : 2;
+  }
+};
+
+// Exponents outside v to -inf: x[sb][r] belongs to streamed row s0 + 16 sb + 4 (l >> 4) + r.
+__device__ __forceinline__ void score_mask(floatx4& x0, floatx4& x1, int s0, Interval v) {
+  const int first = s0 + 4 * (lane_id() >> 4) - v.lo;
+  const unsigned n = (unsigned)max(v.hi - v.lo, 0);
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    x0[r] = (unsigned)(first + r) < n ? x0[r] : -INFINITY;
+    x1[r] = (unsigned)(first + 16 + r) < n ? x1[r] : -INFINITY;
+  }
+}
+
+// Adds -m |distance| to exponents: `first` is the distance at sb = 0, r = 0, which falls (rows:
+// the keys stream) or grows (columns: the queries stream) by one a streamed row; m in log2 units.
+template <int kSign> __device__ __forceinline__ void score_slope(floatx4& x0, floatx4& x1, int first, float m) {
+  const float d = (float)first;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    x0[r] = __builtin_fmaf(-m, fabsf(d + (float)(kSign * r)), x0[r]);
+    x1[r] = __builtin_fmaf(-m, fabsf(d + (float)(kSign * (16 + r))), x1[r]);
+  }
+}
+
+// What a row kernel's workgroup and wave know of their rows (as ExtRows).
+template <int MR, int NW, bool kFold>
+struct ScoreRows {
+  int b, kvh, head0, rows;
+  int64_t qrow;
+  int t0, tiles, kend;  // first key tile of the workgroup, tiles, keys that some row of it sees
+  Interval keys[MR];    // of the lane's rows
+  Reach reach;          // of the wave's rows
+  int row0, qlen, Nq, start;
+  bool fold;
+
+  __device__ __forceinline__ ScoreRows(const ScoreArgs& a, int rh, int rb, int wl, int j) {
+    constexpr int BR = 16 * MR * NW;
+    fold = kFold && a.fold != 0;
+    const int per_entry = fold ? a.H / a.grp : a.H;
+    b = rh / per_entry;
+    const int h = rh - b * per_entry;
+    rows = fold ? a.grp * a.Nq : a.Nq;
+    kvh = fold ? rh : rh / a.grp;
+    head0 = fold ? h * a.grp : h;
+    qrow = (int64_t)rh * rows;
+    const ExtLens n = ext_lens(a, b);
+    qlen = n.q;
+    Nq = a.Nq;
+    start = n.start;
+    row0 = rb * BR + wl * 16 * MR + j;
+    // folded rows hold every query of each head
+    const int first = fold ? 0 : rb * BR, last = fold ? qlen : min(rb * BR + BR, qlen);
+    Reach all;
+    for (int q = first + lane_id(); q < last; q += 64) all.add(score_keys(a, n, b, q));
+    all.template join<64>();
+    kend = all.any_hi;
+    t0 = all.any_lo < all.any_hi ? all.any_lo / kBS : 0;
+    tiles = (kend + kBS - 1) / kBS - t0;
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb) {
+      keys[mb] = Interval{0, 0};
+      if (ok(mb)) {  // other rows are not stored, whatever they hold
+        keys[mb] = score_keys(a, n, b, query(mb));
+        reach.add(keys[mb]);
+      }
+    }
+    reach.template join<16>();
+  }
+  __device__ __forceinline__ int row(int mb) const { return row0 + 16 * mb; }
+  __device__ __forceinline__ int query(int mb) const { return fold ? row(mb) % Nq : row(mb); }
+  __device__ __forceinline__ int head(int mb) const { return fold ? head0 + min(row(mb), rows - 1) / Nq : head0; }
+  __device__ __forceinline__ int pos(int mb) const { return start + query(mb); }
+  __device__ __forceinline__ bool ok(int mb) const { return row(mb) < rows && query(mb) < qlen; }
+  // the first key of tile i of the run
+  __device__ __forceinline__ int key(int i) const { return (t0 + min(i, tiles - 1)) * kBS; }
+};
+
+// Slope of the lane's row mb in log2 units.
+template <typename Rows> __device__ __forceinline__ float score_row_slope(const ScoreArgs& a, const Rows& rw, int mb) {
+  return a.slopes != nullptr ? a.slopes[rw.head(mb)] * kLog2e : 0.f;
+}
+
+// ===========================================================================
+// Forward, as ext_fwd_kernel.
+// ===========================================================================
+template <typename T, int D, int MR, int NW, int OCC, int KS, bool kCap>
+__global__ __launch_bounds__(KS * NW * 64, OCC) void score_fwd_kernel(
+    ScoreArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, T* __restrict__ O,
+    float* __restrict__ L, float* __restrict__ parts) {
+  using E = Elt<T>;
+  using G = Geo<T, D>;
+  constexpr int BR = 16 * MR * NW;
+  __shared__ __attribute__((aligned(16))) RowSmem<T, D, 2, 2, KS, BR> sm;
+
+  int rh, rb;
+  ext_map_block(a, a.fold != 0 ? a.nRB : a.grp * a.nRB, true, NW == 1 ? nullptr : a.kv_lens, a.Nk, rh, rb);
+  const int l = lane_id(), g = l >> 4, j = l & 15;
+  const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
+  const int wl = __builtin_amdgcn_readfirstlane(KS == 1 ? wave_id() : wave_id() % NW);
+  const ScoreRows<MR, NW, MR == 1> rw(a, rh, rb, wl, j);
+  const int part = blockIdx.y;
+  const int64_t kvoff = (int64_t)rw.kvh * a.Nk * D;
+
+  u32x4 qf[MR][G::kChunks];
+#pragma unroll
+  for (int mb = 0; mb < MR; ++mb)
+    load_stationary<T, D>(qf[mb], Q + rw.qrow * D, rw.ok(mb) ? rw.row(mb) : rw.rows, rw.rows);
+
+  floatx4 acc[G::kNB][MR];
+#pragma unroll
+  for (int nb = 0; nb < G::kNB; ++nb)
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb) acc[nb][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
+  float mrun[MR], lsum[MR], slope[MR];
+  const int sloped = vector_mode(a.slopes != nullptr ? 1 : 0);
+#pragma unroll
+  for (int mb = 0; mb < MR; ++mb) {
+    mrun[mb] = -1e30f;
+    lsum[mb] = 0.f;
+    slope[mb] = score_row_slope(a, rw, mb);
+  }
+  const float c = kCap ? a.cap_out : a.scale * kLog2e;
+  floatx4 s[2][MR];
+  typename E::TFrag pf[MR];
+
+  // s times cf are the scores in log2 units (cf = 1 where a bias went into s)
+  auto softmax_step = [&](int s0, int mode, float cf) {
+    float p[MR][8], ls[MR];
+    bool grown = false;
+    floatx4 e[MR][2];
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb)
+#pragma unroll
+      for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) e[mb][sb][r] = __builtin_fmaf(s[sb][mb][r], cf, -mrun[mb]);
+    if (mode == 2) {
+#pragma unroll
+      for (int mb = 0; mb < MR; ++mb) score_mask(e[mb][0], e[mb][1], s0, rw.keys[mb]);
+    }
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[mb][i] = fast_exp2(e[mb][i >> 2][i & 3]);
+      ls[mb] = ((p[mb][0] + p[mb][1]) + (p[mb][2] + p[mb][3])) + ((p[mb][4] + p[mb][5]) + (p[mb][6] + p[mb][7]));
+      grown |= !(ls[mb] <= kRescaleP);
+    }
+    if (__builtin_amdgcn_ballot_w64(grown) != 0) {
+#pragma unroll
+      for (int mb = 0; mb < MR; ++mb) {
+        if (__builtin_amdgcn_ballot_w64(!(ls[mb] <= kRescaleP)) == 0) continue;
+        floatx4 x[2];
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x[sb][r] = s[sb][mb][r] * cf;
+        if (mode == 2) score_mask(x[0], x[1], s0, rw.keys[mb]);
+        float mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) mx = fmaxf(mx, x[i >> 2][i & 3]);
+        mx = group_max(mx);
+        if (__builtin_amdgcn_ballot_w64(mx > mrun[mb] + kRescaleLog2) != 0) {
+          const float mnew = fmaxf(mrun[mb], mx);
+          const float corr = fast_exp2(mrun[mb] - mnew);
+          mrun[mb] = mnew;
+          lsum[mb] *= corr;
+#pragma unroll
+          for (int nb = 0; nb < G::kNB; ++nb) acc[nb][mb] *= corr;
+        }
+        ls[mb] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          p[mb][i] = fast_exp2(x[i >> 2][i & 3] - mrun[mb]);
+          ls[mb] += p[mb][i];
+        }
+      }
+    }
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb) {
+      lsum[mb] += ls[mb];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) pf[mb].set(i, p[mb][i]);
+    }
+  };
+
+  const T* const src[2] = {K + kvoff, V + kvoff};
+  const int split = ext_parts_of(rw.tiles, KS, a.nparts);
+  const ExtRun run = ext_run(rw.tiles, part, split, ks, KS), first = ext_run(rw.tiles, part, split, 0, KS);
+  constexpr bool kBarrier = NW > 1;
+  const TileCopy<T, D, NW, 2> copy(wl);
+  ext_stream<tile_loads<T, D, NW, 2>(), kBarrier>(
+      kBarrier ? first.size() : run.size(),
+      [&](int it, int st) {
+        copy.template issue<true>(src, (T FB_LDS*)sm.lds[ks][st], rw.key(run.begin + it), rw.kend);
+      },
+      []() {},
+      [&](int it, int st) {
+        const int s0 = rw.key(run.begin + it);
+        const int mode = vector_mode(run.begin + it < run.end ? rw.reach.mode(s0) : 0);
+        if (mode == 0) return;
+        const T FB_LDS* Ks = (const T FB_LDS*)sm.lds[ks][st];
+        const T FB_LDS* Vs = Ks + G::kTileElems;
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+          for (int mb = 0; mb < MR; ++mb) s[sb][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+          for (int kk = 0; kk < G::kChunks; ++kk) {
+            const u32x4 ak = *(const u32x4 FB_LDS*)(Ks + G::chunk_off(16 * sb + j, 4 * kk + g));
+#pragma unroll
+            for (int mb = 0; mb < MR; ++mb) s[sb][mb] = E::mma_chunk(ak, qf[mb][kk], s[sb][mb]);
+          }
+        float cf = c;
+        if constexpr (kCap) {
+#pragma unroll
+          for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+            for (int mb = 0; mb < MR; ++mb)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) s[sb][mb][r] = cap_tanh<T>(s[sb][mb][r], a.cap_in);
+        }
+        if (sloped != 0) {
+          cf = 1.f;
+#pragma unroll
+          for (int mb = 0; mb < MR; ++mb) {
+            s[0][mb] *= c;
+            s[1][mb] *= c;
+            score_slope<-1>(s[0][mb], s[1][mb], rw.pos(mb) - s0 - 4 * g, slope[mb]);
+          }
+        }
+        softmax_step(s0, mode, cf);
+#pragma unroll
+        for (int nb = 0; nb < G::kNB; ++nb) {
+          const typename E::AFrag av = G::load_afrag(Vs, 16 * nb);
+#pragma unroll
+          for (int mb = 0; mb < MR; ++mb) acc[nb][mb] = E::mma_acc(av, pf[mb], acc[nb][mb]);
+        }
+      });
+  float lt[MR];
+#pragma unroll
+  for (int mb = 0; mb < MR; ++mb) lt[mb] = group_sum(lsum[mb]);
+  if constexpr (KS > 1) {
+    // one reference for the sets, then their sums, as in ext_fwd_kernel
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb)
+      if (g == 0) {
+        sm.sc[0][ks][16 * (wl * MR + mb) + j] = mrun[mb];
+        sm.sc[1][ks][16 * (wl * MR + mb) + j] = lt[mb];
+      }
+    __syncthreads();
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb) {
+      const int at = 16 * (wl * MR + mb) + j;
+      float m = sm.sc[0][0][at], sum = 0.f;
+#pragma unroll
+      for (int q = 1; q < KS; ++q) m = fmaxf(m, sm.sc[0][q][at]);
+#pragma unroll
+      for (int q = 0; q < KS; ++q) sum = __builtin_fmaf(sm.sc[1][q][at], fast_exp2(sm.sc[0][q][at] - m), sum);
+      const float corr = fast_exp2(mrun[mb] - m);
+      mrun[mb] = m;
+      lt[mb] = sum;
+#pragma unroll
+      for (int nb = 0; nb < G::kNB; ++nb) acc[nb][mb] *= corr;
+    }
+    static_assert(sizeof(sm.lds) >= merge_bytes<KS, NW, G::kNB, MR>(), "set merge buffer");
+    merge_sets<KS, NW>(acc, ks, wl, (floatx4 FB_LDS*)&sm.lds[0][0][0]);
+  }
+  const RowSplit<KS> own{ks, 0};
+  if (a.nparts > 1) {
+    const int64_t all = (int64_t)(a.total / a.nRB) * rw.rows;
+    float* const ml = parts + a.nparts * all * D;
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb)
+      if (rw.ok(mb)) {
+        const int64_t at = part * all + rw.qrow + rw.row(mb);
+#pragma unroll
+        for (int nb = 0; nb < G::kNB; ++nb)
+          if (own.owns(nb)) *(floatx4*)(parts + at * D + 16 * nb + 4 * g) = acc[nb][mb];
+        if (g == 0 && ks == 0) {
+          ml[2 * at] = mrun[mb];
+          ml[2 * at + 1] = lt[mb];
+        }
+      }
+    return;
+  }
+#pragma unroll
+  for (int mb = 0; mb < MR; ++mb) {
+    if (rw.row(mb) >= rw.rows) continue;
+    const int64_t at = rw.qrow + rw.row(mb);
+    const bool some = rw.ok(mb) && lt[mb] != 0.f;
+    const float inv = 1.f / lt[mb];
+#pragma unroll
+    for (int nb = 0; nb < G::kNB; ++nb)
+      if (own.owns(nb))
+        E::store4(O + at * D + 16 * nb + 4 * g, some ? acc[nb][mb] * inv : floatx4{0.f, 0.f, 0.f, 0.f});
+    if (g == 0 && ks == 0) L[at] = some ? (mrun[mb] + __log2f(lt[mb])) * kLn2 : -INFINITY;
+  }
+}
+
+// The exponent of P from a raw score: s c, or the capped score with its t = tanh, less L
+// (off = -L log2(e)).
+template <typename T, bool kCap>
+__device__ __forceinline__ float score_exponent(const ScoreArgs& a, float s, float c, float off, float& t) {
+  if constexpr (kCap) {
+    t = cap_tanh<T>(s, a.cap_in);
+    return __builtin_fmaf(t, a.cap_out, off);
+  } else {
+    return __builtin_fmaf(s, c, off);
+  }
+}
+__device__ __forceinline__ float cap_slope(float t) { return __builtin_fmaf(-t, t, 1.f); }
+
+// ===========================================================================
+// First backward, row side, as ext_bwd_rows_kernel.  A capped tile's t takes eight registers a
+// 16-row block from the exponent to the gradient of the score.
+// ===========================================================================
+template <typename T, int D, int MR, int NW, int OCC, int KS, bool kCap>
+__global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_rows_kernel(
+    ScoreArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ O,
+    const T* __restrict__ dO, const float* __restrict__ L, T* __restrict__ dQ, float* __restrict__ Dout,
+    float* __restrict__ parts) {
+  using E = Elt<T>;
+  using G = Geo<T, D>;
+  constexpr int BR = 16 * MR * NW;
+  __shared__ __attribute__((aligned(16))) RowSmem<T, D, 2, 2, KS, BR> sm;
+
+  int rh, rb;
+  ext_map_block(a, a.grp * a.nRB, true, a.kv_lens, a.Nk, rh, rb);
+  const int l = lane_id(), g = l >> 4, j = l & 15;
+  const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
+  const int wl = __builtin_amdgcn_readfirstlane(KS == 1 ? wave_id() : wave_id() % NW);
+  const ScoreRows<MR, NW, false> rw(a, rh, rb, wl, j);
+  const int64_t kvoff = (int64_t)rw.kvh * a.Nk * D, qoff = rw.qrow * D;
+
+  u32x4 qf[MR][G::kChunks], dof[MR][G::kChunks];
+  float lb[MR], drow[MR], dout[MR], rest[MR];
+  const int sloped = vector_mode(a.slopes != nullptr ? 1 : 0);
+  const float slope = score_row_slope(a, rw, 0);
+  bool centred = false;
+#pragma unroll
+  for (int mb = 0; mb < MR; ++mb) {
+    const int row = rw.ok(mb) ? rw.row(mb) : rw.rows;
+    load_stationary<T, D>(qf[mb], Q + qoff, row, rw.rows);
+    load_stationary<T, D>(dof[mb], dO + qoff, row, rw.rows);
+    u32x4 of[G::kChunks];
+    load_stationary<T, D>(of, O + qoff, row, rw.rows);
+    float part = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < G::kChunks; ++kk) part += E::dot_chunk(dof[mb][kk], of[kk]);
+    drow[mb] = dout[mb] = group_sum(part);
+    // an empty row (L = -inf) gets P = 0
+    const float Lr = rw.ok(mb) ? L[rw.qrow + rw.row(mb)] : 0.f;
+    lb[mb] = Lr == -INFINITY ? INFINITY : Lr * kLog2e;
+    rest[mb] = 0.f;
+  }
+
+  floatx4 acc[G::kNB][MR];
+#pragma unroll
+  for (int nb = 0; nb < G::kNB; ++nb)
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb) acc[nb][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const float c = a.scale * kLog2e;
+  floatx4 s[2][MR], dp[2][MR], t[kCap ? 2 : 1][kCap ? MR : 1];
+  typename E::TFrag dsf[MR];
+
+  const T* const src[2] = {K + kvoff, V + kvoff};
+  const int part = blockIdx.y, split = ext_parts_of(rw.tiles, KS, a.nparts);
+  const ExtRun run = ext_run(rw.tiles, part, split, ks, KS), first = ext_run(rw.tiles, part, split, 0, KS);
+  constexpr bool kBarrier = NW > 1;
+  const TileCopy<T, D, NW, 2> copy(wl);
+  ext_stream<tile_loads<T, D, NW, 2>(), kBarrier>(
+      kBarrier ? first.size() : run.size(),
+      [&](int it, int st) {
+        copy.template issue<true>(src, (T FB_LDS*)sm.lds[ks][st], rw.key(run.begin + it), rw.kend);
+      },
+      []() {},
+      [&](int it, int st) {
+        const int s0 = rw.key(run.begin + it);
+        const int mode = vector_mode(run.begin + it < run.end ? rw.reach.mode(s0) : 0);
+        if (mode == 0) return;
+        const T FB_LDS* Ks = (const T FB_LDS*)sm.lds[ks][st];
+        const T FB_LDS* Vs = Ks + G::kTileElems;
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+          for (int mb = 0; mb < MR; ++mb) {
+            s[sb][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
+            dp[sb][mb] = floatx4{-drow[mb], -drow[mb], -drow[mb], -drow[mb]};
+          }
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+          for (int kk = 0; kk < G::kChunks; ++kk) {
+            const int off = G::chunk_off(16 * sb + j, 4 * kk + g);
+            const u32x4 ak = *(const u32x4 FB_LDS*)(Ks + off);
+            const u32x4 av = *(const u32x4 FB_LDS*)(Vs + off);
+#pragma unroll
+            for (int mb = 0; mb < MR; ++mb) {
+              s[sb][mb] = E::mma_chunk(ak, qf[mb][kk], s[sb][mb]);
+              dp[sb][mb] = E::mma_chunk(av, dof[mb][kk], dp[sb][mb]);
+            }
+          }
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+          for (int mb = 0; mb < MR; ++mb)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              float tr = 0.f;
+              s[sb][mb][r] = score_exponent<T, kCap>(a, s[sb][mb][r], c, -lb[mb], tr);
+              if constexpr (kCap) t[sb][mb][r] = tr;
+            }
+        if (sloped != 0) {
+#pragma unroll
+          for (int mb = 0; mb < MR; ++mb) score_slope<-1>(s[0][mb], s[1][mb], rw.pos(mb) - s0 - 4 * g, slope);
+        }
+        if (mode == 2) {
+#pragma unroll
+          for (int mb = 0; mb < MR; ++mb) score_mask(s[0][mb], s[1][mb], s0, rw.keys[mb]);
+        }
+        // the first tile, and those where a row's span begins
+        if (!centred || s0 <= rw.reach.all_lo) {
+          centred = true;
+#pragma unroll
+          for (int mb = 0; mb < MR; ++mb) {
+            float w = 0.f, wd = 0.f;
+#pragma unroll
+            for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const float p = fast_exp2(s[sb][mb][r]);
+                w += p;
+                wd = __builtin_fmaf(p, dp[sb][mb][r], wd);
+              }
+            w = group_sum(w);
+            wd = group_sum(wd);
+            // L and the weights are off by a few 2^-24 of L's size
+            const float by = w > 1.f - 0x1p-16f ? wd / w : 0.f;
+            drow[mb] += by;
+            rest[mb] += g == 0 ? by : 0.f;
+#pragma unroll
+            for (int sb = 0; sb < 2; ++sb) dp[sb][mb] -= by;
+          }
+        }
+#pragma unroll
+        for (int mb = 0; mb < MR; ++mb)
+#pragma unroll
+          for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float dz = fast_exp2(s[sb][mb][r]) * dp[sb][mb][r];
+              rest[mb] += dz;
+              if constexpr (kCap)
+                dsf[mb].set(4 * sb + r, dz * cap_slope(t[sb][mb][r]));
+              else
+                dsf[mb].set(4 * sb + r, dz);
+            }
+#pragma unroll
+        for (int nb = 0; nb < G::kNB; ++nb) {
+          const typename E::AFrag ak = G::load_afrag(Ks, 16 * nb);
+#pragma unroll
+          for (int mb = 0; mb < MR; ++mb) acc[nb][mb] = E::mma_acc(ak, dsf[mb], acc[nb][mb]);
+        }
+      });
+#pragma unroll
+  for (int mb = 0; mb < MR; ++mb) rest[mb] = group_sum(rest[mb]);
+  if constexpr (KS > 1) {
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb)
+      if (g == 0) sm.sc[0][ks][16 * (wl * MR + mb) + j] = rest[mb];
+    __syncthreads();
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb) {
+      const int at = 16 * (wl * MR + mb) + j;
+      rest[mb] = sm.sc[0][0][at];
+#pragma unroll
+      for (int q = 1; q < KS; ++q) rest[mb] += sm.sc[0][q][at];
+    }
+    static_assert(sizeof(sm.lds) >= merge_bytes<KS, NW, G::kNB, MR>(), "set merge buffer");
+    merge_sets<KS, NW>(acc, ks, wl, (floatx4 FB_LDS*)&sm.lds[0][0][0]);
+  }
+  const RowSplit<KS> own{ks, 0};
+  if (a.nparts > 1) {
+    const int64_t all = (int64_t)(a.total / a.nRB) * rw.rows;
+    float* const sc = parts + a.nparts * all * D;
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb)
+      if (rw.ok(mb)) {
+        const int64_t at = part * all + rw.qrow + rw.row(mb);
+#pragma unroll
+        for (int nb = 0; nb < G::kNB; ++nb)
+          if (own.owns(nb)) *(floatx4*)(parts + at * D + 16 * nb + 4 * g) = acc[nb][mb];
+        if (g == 0 && ks == 0) sc[at] = (part == 0 ? dout[mb] : 0.f) + rest[mb];
+      }
+    return;
+  }
+#pragma unroll
+  for (int mb = 0; mb < MR; ++mb) {
+    if (rw.row(mb) >= rw.rows) continue;
+    const int64_t at = rw.qrow + rw.row(mb);
+#pragma unroll
+    for (int nb = 0; nb < G::kNB; ++nb)
+      if (own.owns(nb))
+        E::store4(dQ + at * D + 16 * nb + 4 * g, rw.ok(mb) ? acc[nb][mb] * a.scale : floatx4{0.f, 0.f, 0.f, 0.f});
+    if (g == 0 && ks == 0) Dout[at] = rw.ok(mb) ? dout[mb] + rest[mb] : 0.f;
+  }
+}
+
+// ===========================================================================
+// Column kernels
+// ===========================================================================
+
+// What a column kernel's workgroup and wave know of their columns (as ExtCols).
+template <int MC, int NW>
+struct ScoreCols {
+  int b, kvh, hq, heads, sub, subs;
+  int t0, per_head;  // first query tile, query tiles a head
+  int qlen, klen, start;
+  int col0;
+  Interval rows[MC];  // query rows that see the lane's columns
+  Reach reach;        // of the wave's columns
+  __device__ __forceinline__ ScoreCols(const ScoreArgs& a, int kv, int rb, int wl) {
+    constexpr int BC = 16 * MC * NW;
+    const int per_entry = a.H / a.grp;
+    kvh = kv;
+    b = kv / per_entry;
+    const int split = a.nparts > 1;
+    subs = split ? a.nparts / a.grp : 1;
+    const int part = blockIdx.y;
+    heads = split ? 1 : a.grp;
+    hq = kv * a.grp + (split ? part / subs : 0);
+    sub = split ? part % subs : 0;
+    const ExtLens n = ext_lens(a, b);
+    qlen = n.q;
+    klen = n.k;
+    start = n.start;
+    col0 = rb * BC + wl * 16 * MC;
+    Reach all;
+    for (int col = rb * BC + lane_id(); col < min(rb * BC + BC, klen); col += 64) all.add(score_queries(a, n, b, col));
+    all.template join<64>();
+    t0 = all.any_lo < all.any_hi ? all.any_lo / kBS : 0;
+    per_head = (all.any_hi + kBS - 1) / kBS - t0;
+#pragma unroll
+    for (int mc = 0; mc < MC; ++mc) {
+      const int col = col0 + 16 * mc + (lane_id() & 15);
+      rows[mc] = Interval{0, 0};
+      if (col < klen) {  // other columns are stored as zeros
+        rows[mc] = score_queries(a, n, b, col);
+        reach.add(rows[mc]);
+      }
+    }
+    reach.template join<16>();
+  }
+  __device__ __forceinline__ int count() const { return heads * per_head; }
+  __device__ __forceinline__ int qhead(int f) const { return heads == 1 ? hq : hq + f / per_head; }
+  __device__ __forceinline__ int tile(int f) const { return t0 + (heads == 1 ? f : f % per_head); }
+};
+
+// The slopes of a key/value head's query heads in LDS, in log2 units, for all waves after the
+// next barrier.
+__device__ __forceinline__ void score_fill_slopes(const ScoreArgs& a, int kv, float FB_LDS* dst, int count) {
+  if (a.slopes == nullptr) return;
+  for (int x = threadIdx.x; x < a.grp; x += count) dst[x] = a.slopes[kv * a.grp % a.H + x] * kLog2e;
+}
+
+// First backward, column side, as ext_bwd_cols_kernel.
+template <typename T, int D, int MC, int NW, int OCC, int KS, bool kKL, bool kCap>
+__global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_cols_kernel(
+    ScoreArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ dO,
+    const float* __restrict__ L, const float* __restrict__ Dv, T* __restrict__ dK, T* __restrict__ dV,
+    float* __restrict__ parts) {
+  using E = Elt<T>;
+  using G = Geo<T, D>;
+  struct Smem {
+    T lds[KS][2][2 * G::kTileElems];
+    float rawsc[KS][2][2 * kBS];
+    float tsc[KS][2][2 * kBS];
+  };
+  constexpr int kWPT = kBS / (16 * MC);  // waves per stationary K tile
+  static_assert(!kKL || (kBS % (16 * MC) == 0 && NW % kWPT == 0), "stationary K in LDS: 32-row tiles");
+  struct SmemK : Smem {
+    T kst[NW / kWPT][G::kTileElems];
+  };
+  __shared__ __attribute__((aligned(16))) std::conditional_t<kKL, SmemK, Smem> sm;
+  extern __shared__ float slope_mem[];
+  float FB_LDS* const slopes = (float FB_LDS*)slope_mem;
+
+  int kv, rb;
+  ext_map_cols(a, kv, rb);
+  const int l = lane_id(), g = l >> 4, j = l & 15;
+  const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
+  const int wl = __builtin_amdgcn_readfirstlane(KS == 1 ? wave_id() : wave_id() % NW);
+  const ScoreCols<MC, NW> cl(a, kv, rb, wl);
+  const int64_t koff = (int64_t)kv * a.Nk * D;
+
+  u32x4 kf[kKL ? 1 : MC][G::kChunks], vf[MC][G::kChunks];
+#pragma unroll
+  for (int mc = 0; mc < MC; ++mc) {
+    if constexpr (!kKL) load_stationary<T, D>(kf[mc], K + koff, cl.col0 + 16 * mc + j, cl.klen);
+    load_stationary<T, D>(vf[mc], V + koff, cl.col0 + 16 * mc + j, cl.klen);
+  }
+  if constexpr (kKL) {
+    // read by waves with a valid column alone, which lies in the tile
+    if (ks == 0 && wl % kWPT == 0 && cl.col0 < cl.klen) {
+      const TileCopy<T, D, 1, 1> kc(0);
+      const T* const ksrc[1] = {K + koff};
+      kc.template issue<true>(ksrc, (T FB_LDS*)sm.kst[wl / kWPT], cl.col0, cl.klen);
+    }
+  }
+  score_fill_slopes(a, kv, slopes, KS * NW * 64);
+  const int sloped = vector_mode(a.slopes != nullptr ? 1 : 0);
+  floatx4 dk[G::kNB][MC], dv[G::kNB][MC];
+#pragma unroll
+  for (int nb = 0; nb < G::kNB; ++nb)
+#pragma unroll
+    for (int mc = 0; mc < MC; ++mc) dk[nb][mc] = dv[nb][mc] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const float c = a.scale * kLog2e;
+  floatx4 s[2][MC], dp[2][MC], t[kCap ? 2 : 1][kCap ? MC : 1];
+  typename E::TFrag pf[MC], dsf[MC];
+
+  const int n = cl.count();
+  const ExtRun run(n, cl.sub * KS + ks, cl.subs * KS), first(n, cl.sub * KS, cl.subs * KS);
+  auto flat = [&](int it) { return min(run.begin + it, n - 1); };
+  const TileCopy<T, D, NW, 2> copy(wl);
+  stream_loop_rs<2, tile_loads<T, D, NW, 2>(), 1, true>(
+      0, first.size(), __builtin_amdgcn_readfirstlane(wl) == 0,
+      [&](int it, int rs) {
+        const int64_t qs = (int64_t)cl.qhead(flat(it)) * a.Nq;
+        issue_scalar_pair<true>((float FB_LDS*)sm.rawsc[ks][rs], L + qs, Dv + qs, cl.tile(flat(it)) * kBS, cl.qlen);
+      },
+      [&](int it, int st) {
+        const int64_t qo = (int64_t)cl.qhead(flat(it)) * a.Nq * D;
+        const T* const src[2] = {Q + qo, dO + qo};
+        copy.template issue<true>(src, (T FB_LDS*)sm.lds[ks][st], cl.tile(flat(it)) * kBS, cl.qlen);
+      },
+      [&](int, int rs, int ts) {
+        if (l < kBS) {
+          const float FB_LDS* raw = (const float FB_LDS*)sm.rawsc[ks][rs];
+          float FB_LDS* to = (float FB_LDS*)sm.tsc[ks][ts];
+          const float Lr = raw[l];
+          to[l] = Lr == -INFINITY ? -INFINITY : -Lr * kLog2e;  // an empty row: P = 0
+          to[kBS + l] = -raw[kBS + l];
+        }
+      },
+      [&](int it, int st, int ts, auto&& prep_next) {
+        const int s0 = cl.tile(flat(it)) * kBS;
+        const int mode = vector_mode(run.begin + it < run.end ? cl.reach.mode(s0) : 0);
+        if (mode == 0) {
+          prep_next();
+          return;
+        }
+        const T FB_LDS* Qs = (const T FB_LDS*)sm.lds[ks][st];
+        const T FB_LDS* dOs = Qs + G::kTileElems;
+        const float FB_LDS* Ts = (const float FB_LDS*)sm.tsc[ks][ts];
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb) {
+          const floatx4 t1 = *(const floatx4 FB_LDS*)(Ts + kBS + 16 * sb + 4 * g);
+#pragma unroll
+          for (int mc = 0; mc < MC; ++mc) {
+            s[sb][mc] = floatx4{0.f, 0.f, 0.f, 0.f};
+            dp[sb][mc] = t1;
+          }
+        }
+        __builtin_amdgcn_s_setprio(1);
+        if constexpr (kKL) {
+          const T FB_LDS* Ks = (const T FB_LDS*)sm.kst[wl / kWPT];
+          const int r0 = 16 * MC * (wl % kWPT);
+#pragma unroll
+          for (int kk = 0; kk < G::kChunks; ++kk) {
+            u32x4 kfr[MC];
+#pragma unroll
+            for (int mc = 0; mc < MC; ++mc)
+              kfr[mc] = *(const u32x4 FB_LDS*)(Ks + G::chunk_off(r0 + 16 * mc + j, 4 * kk + g));
+#pragma unroll
+            for (int sb = 0; sb < 2; ++sb) {
+              const int off = G::chunk_off(16 * sb + j, 4 * kk + g);
+              const u32x4 aq = *(const u32x4 FB_LDS*)(Qs + off);
+              const u32x4 ado = *(const u32x4 FB_LDS*)(dOs + off);
+#pragma unroll
+              for (int mc = 0; mc < MC; ++mc) {
+                s[sb][mc] = E::mma_chunk(aq, kfr[mc], s[sb][mc]);
+                dp[sb][mc] = E::mma_chunk(ado, vf[mc][kk], dp[sb][mc]);
+              }
+            }
+          }
+        } else {
+#pragma unroll
+          for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+            for (int kk = 0; kk < G::kChunks; ++kk) {
+              const int off = G::chunk_off(16 * sb + j, 4 * kk + g);
+              const u32x4 aq = *(const u32x4 FB_LDS*)(Qs + off);
+              const u32x4 ado = *(const u32x4 FB_LDS*)(dOs + off);
+#pragma unroll
+              for (int mc = 0; mc < MC; ++mc) {
+                s[sb][mc] = E::mma_chunk(aq, kf[mc][kk], s[sb][mc]);
+                dp[sb][mc] = E::mma_chunk(ado, vf[mc][kk], dp[sb][mc]);
+              }
+            }
+        }
+        __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb) {
+          const floatx4 off = *(const floatx4 FB_LDS*)(Ts + 16 * sb + 4 * g);
+#pragma unroll
+          for (int mc = 0; mc < MC; ++mc)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              float tr = 0.f;
+              s[sb][mc][r] = score_exponent<T, kCap>(a, s[sb][mc][r], c, off[r], tr);
+              if constexpr (kCap) t[sb][mc][r] = tr;
+            }
+        }
+        if (sloped != 0) {
+          const float m = slopes[cl.qhead(flat(it)) - kv * a.grp];
+#pragma unroll
+          for (int mc = 0; mc < MC; ++mc)
+            score_slope<1>(s[0][mc], s[1][mc], cl.start + s0 + 4 * g - (cl.col0 + 16 * mc + j), m);
+        }
+        if (mode == 2) {
+#pragma unroll
+          for (int mc = 0; mc < MC; ++mc) score_mask(s[0][mc], s[1][mc], s0, cl.rows[mc]);
+        }
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int mc = 0; mc < MC; ++mc) {
+              const float p = fast_exp2(s[sb][mc][r]);
+              pf[mc].set(4 * sb + r, p);
+              if constexpr (kCap)
+                dsf[mc].set(4 * sb + r, p * dp[sb][mc][r] * cap_slope(t[sb][mc][r]));
+              else
+                dsf[mc].set(4 * sb + r, p * dp[sb][mc][r]);
+            }
+#pragma unroll
+        for (int nb = 0; nb < G::kNB; ++nb) {
+          const typename E::AFrag ado = G::load_afrag(dOs, 16 * nb);
+          const typename E::AFrag aq = G::load_afrag(Qs, 16 * nb);
+#pragma unroll
+          for (int mc = 0; mc < MC; ++mc) {
+            dv[nb][mc] = E::mma_acc(ado, pf[mc], dv[nb][mc]);
+            dk[nb][mc] = E::mma_acc(aq, dsf[mc], dk[nb][mc]);
+          }
+        }
+        prep_next();
+      });
+  if constexpr (KS > 1) {
+    static_assert(sizeof(sm.lds) >= merge_bytes<KS, NW, G::kNB, MC>(), "set merge buffer");
+    merge_sets<KS, NW>(dk, ks, wl, (floatx4 FB_LDS*)&sm.lds[0][0][0]);
+    merge_sets<KS, NW>(dv, ks, wl, (floatx4 FB_LDS*)&sm.lds[0][0][0]);
+  }
+  ext_store_cols<T, D, KS>(a, kv, cl.col0, cl.klen, ks, dk, dv, a.scale, 1.f, dK, dV, parts);
+}
+
+// ===========================================================================
+// BoB Pass 1, as ext_pass1_kernel.  Capped, the sums that meet K carry u: with F' = F - alpha*
+// and w = C + F' (dP - D) - E* the epilogue's
+//   Qt = tau (sum P (u w - (2 / c) t (dP - D) F) k + sum u P (dP - D) u_K - de sum u P k) - da dQ
+// needs one more operand, u P, beside P, which stays with u_V.
+// ===========================================================================
+template <typename T, int D, int MR, int NW, int OCC, int KS, int kPF, bool kCap>
+__global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
+    ScoreArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ O,
+    const T* __restrict__ dO, const T* __restrict__ UQ, const T* __restrict__ UK, const T* __restrict__ UV,
+    const float* __restrict__ L, const float* __restrict__ Dv, const T* __restrict__ dQ, T* __restrict__ Qt,
+    T* __restrict__ dOt, float* __restrict__ alpha_out, float* __restrict__ E_out, float* __restrict__ parts) {
+  using E = Elt<T>;
+  using G = Geo<T, D>;
+  constexpr int BR = 16 * MR * NW;
+  __shared__ __attribute__((aligned(16))) RowSmem<T, D, 4, 2, KS, BR> sm;
+  __shared__ float ref_mem[KS == 1 ? 1 : 5 * KS * BR];
+
+  int rh, rb;
+  ext_map_block(a, a.grp * a.nRB, true, a.kv_lens, a.Nk, rh, rb);
+  const int l = lane_id(), g = l >> 4, j = l & 15;
+  const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
+  const int wl = KS == 1 ? wave_id() : __builtin_amdgcn_readfirstlane(wave_id() % NW);
+  const ScoreRows<MR, NW, false> rw(a, rh, rb, wl, j);
+  const int64_t kvoff = (int64_t)rw.kvh * a.Nk * D, qoff = rw.qrow * D;
+
+  u32x4 qf[MR][G::kChunks], uqf[MR][G::kChunks], dof[MR][G::kChunks];
+  float lb[MR], drow[MR];
+  const int sloped = vector_mode(a.slopes != nullptr ? 1 : 0);
+  const float slope = score_row_slope(a, rw, 0);
+#pragma unroll
+  for (int mb = 0; mb < MR; ++mb) {
+    const int row = rw.ok(mb) ? rw.row(mb) : rw.rows;
+    load_stationary<T, D>(qf[mb], Q + qoff, row, rw.rows);
+    load_stationary<T, D>(uqf[mb], UQ + qoff, row, rw.rows);
+    load_stationary<T, D>(dof[mb], dO + qoff, row, rw.rows);
+    const float Lr = rw.ok(mb) ? L[rw.qrow + rw.row(mb)] : 0.f;
+    lb[mb] = Lr == -INFINITY ? INFINITY : Lr * kLog2e;
+    drow[mb] = rw.ok(mb) ? Dv[rw.qrow + rw.row(mb)] : 0.f;
+  }
+  floatx4 aDO[G::kNB][MR], aOM[G::kNB][MR], aB[G::kNB][MR];
+#pragma unroll
+  for (int nb = 0; nb < G::kNB; ++nb)
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb) aDO[nb][mb] = aOM[nb][mb] = aB[nb][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
+  float alpha[MR], e0[MR];
+#pragma unroll
+  for (int mb = 0; mb < MR; ++mb) alpha[mb] = e0[mb] = 0.f;
+  const float c = a.scale * kLog2e;
+  floatx4 s[2][MR], dp[2][MR], f[2][MR], cc[2][MR], t[kCap ? 2 : 1][kCap ? MR : 1];
+  typename E::TFrag fP[MR], fPF[MR], fPPt[MR], fPdd[MR], fPu[kCap ? MR : 1];
+  using AF = typename E::AFrag;
+
+  const T* const src[4] = {K + kvoff, V + kvoff, UK + kvoff, UV + kvoff};
+  const int part = blockIdx.y, split = ext_parts_of(rw.tiles, KS, a.nparts);
+  const ExtRun run = ext_run(rw.tiles, part, split, ks, KS), first = ext_run(rw.tiles, part, split, 0, KS);
+  constexpr bool kBarrier = NW > 1 || KS > 1;  // the sets meet in the first tile
+  const TileCopy<T, D, NW, 4> copy(wl);
+  float aref[MR], eref[MR];
+#pragma unroll
+  for (int mb = 0; mb < MR; ++mb) aref[mb] = eref[mb] = 0.f;
+  bool centred = false;
+  ext_stream<tile_loads<T, D, NW, 4>(), kBarrier>(
+      kBarrier ? first.size() : run.size(),
+      [&](int it, int st) {
+        copy.template issue<true>(src, (T FB_LDS*)sm.lds[ks][st], rw.key(run.begin + it), rw.kend);
+      },
+      []() {},
+      [&](int it, int st) {
+        const int s0 = rw.key(run.begin + it);
+        int mode = run.begin + it < run.end ? rw.reach.mode(s0) : 0;
+        if constexpr (KS > 1) mode = vector_mode(mode);
+        if (mode == 0 && (KS == 1 || it > 0 || split > 1)) return;
+        const T FB_LDS* Ks = (const T FB_LDS*)sm.lds[ks][st];
+        const T FB_LDS* Vs = Ks + G::kTileElems;
+        const T FB_LDS* UKs = Vs + G::kTileElems;
+        const T FB_LDS* UVs = UKs + G::kTileElems;
+        if constexpr (std::is_same_v<T, bf16> && D == 128) __builtin_amdgcn_iglp_opt(3);
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+          for (int mb = 0; mb < MR; ++mb) {
+            s[sb][mb] = f[sb][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
+            cc[sb][mb] = floatx4{-eref[mb], -eref[mb], -eref[mb], -eref[mb]};
+            dp[sb][mb] = floatx4{-drow[mb], -drow[mb], -drow[mb], -drow[mb]};
+          }
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+          for (int kk = 0; kk < G::kChunks; ++kk) {
+            const int off = G::chunk_off(16 * sb + j, 4 * kk + g);
+            const u32x4 ak = *(const u32x4 FB_LDS*)(Ks + off), av = *(const u32x4 FB_LDS*)(Vs + off);
+            const u32x4 auk = *(const u32x4 FB_LDS*)(UKs + off), auv = *(const u32x4 FB_LDS*)(UVs + off);
+#pragma unroll
+            for (int mb = 0; mb < MR; ++mb) {
+              s[sb][mb] = E::mma_chunk(ak, qf[mb][kk], s[sb][mb]);        // S^T = K Q^T
+              dp[sb][mb] = E::mma_chunk(av, dof[mb][kk], dp[sb][mb]);     // (dP - D)^T
+              f[sb][mb] = E::mma_chunk(ak, uqf[mb][kk], f[sb][mb]);       // (U_Q K^T)^T
+              f[sb][mb] = E::mma_chunk(auk, qf[mb][kk], f[sb][mb]);       // + (Q U_K^T)^T
+              cc[sb][mb] = E::mma_chunk(auv, dof[mb][kk], cc[sb][mb]);    // C^T - E* = U_V dO^T - E*
+            }
+          }
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+          for (int mb = 0; mb < MR; ++mb)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              float tr = 0.f;
+              s[sb][mb][r] = score_exponent<T, kCap>(a, s[sb][mb][r], c, -lb[mb], tr);
+              if constexpr (kCap) t[sb][mb][r] = tr;
+              const float by = kCap ? a.scale * cap_slope(tr) : a.scale;
+              f[sb][mb][r] = __builtin_fmaf(f[sb][mb][r], by, -aref[mb]);
+            }
+        AF cur[4];
+        auto load_frags = [&](int nb) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) cur[x] = G::load_afrag(Ks + x * G::kTileElems, 16 * nb);
+        };
+        if constexpr (kPF != 0) load_frags(0);
+        if (sloped != 0) {
+#pragma unroll
+          for (int mb = 0; mb < MR; ++mb) score_slope<-1>(s[0][mb], s[1][mb], rw.pos(mb) - s0 - 4 * g, slope);
+        }
+        if (mode == 2) {
+#pragma unroll
+          for (int mb = 0; mb < MR; ++mb) score_mask(s[0][mb], s[1][mb], s0, rw.keys[mb]);
+        }
+        // The estimate of the first tile, which the sets share (a barrier: every wave of a workgroup
+        // with sets comes here in its first iteration), and that of a row whose span begins in a
+        // later tile: its sums are 0 until then.  Where other sets or parts sum the row's further
+        // tiles about 0, only rows that lie in this tile whole have one.
+        const bool shared = split == 1 && (KS > 1 ? it == 0 : !centred);
+        if (shared || s0 <= rw.reach.all_lo) {
+          centred = true;
+#pragma unroll
+          for (int mb = 0; mb < MR; ++mb) {
+            float w = 0.f, wf = 0.f, wd = 0.f, wc = 0.f, wfd = 0.f;  // sums of P, P F, P (dP - D), P C, P F (dP - D)
+            if (mode != 0) {
+#pragma unroll
+              for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                  const float p = fast_exp2(s[sb][mb][r]), pf = p * f[sb][mb][r];
+                  w += p;
+                  wf += pf;
+                  wd = __builtin_fmaf(p, dp[sb][mb][r], wd);
+                  wc = __builtin_fmaf(p, cc[sb][mb][r], wc);
+                  wfd = __builtin_fmaf(pf, dp[sb][mb][r], wfd);
+                }
+            }
+            w = group_sum(w);
+            wf = group_sum(wf);
+            wd = group_sum(wd);
+            wc = group_sum(wc);
+            wfd = group_sum(wfd);
+            if (KS > 1 && shared) {
+              float FB_LDS* at = (float FB_LDS*)ref_mem + 16 * (wl * MR + mb) + j;
+              if (g == 0) {
+                at[(5 * ks + 0) * BR] = w;
+                at[(5 * ks + 1) * BR] = wf;
+                at[(5 * ks + 2) * BR] = wd;
+                at[(5 * ks + 3) * BR] = wc;
+                at[(5 * ks + 4) * BR] = wfd;
+              }
+              __syncthreads();
+              w = wf = wd = wc = wfd = 0.f;
+#pragma unroll
+              for (int q = 0; q < KS; ++q) {
+                w += at[(5 * q + 0) * BR];
+                wf += at[(5 * q + 1) * BR];
+                wd += at[(5 * q + 2) * BR];
+                wc += at[(5 * q + 3) * BR];
+                wfd += at[(5 * q + 4) * BR];
+              }
+            }
+            // rows without weight here (or of NaN) keep the reference 0
+            const bool begins = rw.keys[mb].lo >= s0;
+            const bool set = w > 0.f && (shared || (begins && ((KS == 1 && split == 1) || rw.keys[mb].hi <= s0 + kBS)));
+            const float by_f = set ? wf / w : 0.f, by_c = set ? (wc + (wfd - by_f * wd)) / w : 0.f;
+            aref[mb] += by_f;
+            eref[mb] += by_c;
+#pragma unroll
+            for (int sb = 0; sb < 2; ++sb) {
+              f[sb][mb] -= by_f;
+              cc[sb][mb] -= by_c;
+            }
+          }
+        }
+        if (KS > 1 && mode == 0) return;
+#pragma unroll
+        for (int mb = 0; mb < MR; ++mb)
+#pragma unroll
+          for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float p = fast_exp2(s[sb][mb][r]);
+              const float dd = dp[sb][mb][r];
+              const float pf = p * f[sb][mb][r];
+              const float w = __builtin_fmaf(f[sb][mb][r], dd, cc[sb][mb][r]);
+              const float ppt = p * w;
+              const int i = 4 * sb + r;
+              alpha[mb] += pf;
+              e0[mb] += ppt;
+              fP[mb].set(i, p);
+              fPF[mb].set(i, pf);
+              if constexpr (kCap) {
+                const float tr = t[sb][mb][r], pu = p * cap_slope(tr);
+                fPu[mb].set(i, pu);
+                fPdd[mb].set(i, pu * dd);
+                // P (u w - (2 / c) t (dP - D) F)
+                fPPt[mb].set(i, __builtin_fmaf(pu, w, -a.cap_k * tr * (p * dd) * (f[sb][mb][r] + aref[mb])));
+              } else {
+                fPPt[mb].set(i, ppt);
+                fPdd[mb].set(i, p * dd);
+              }
+            }
+#pragma unroll
+        for (int nb = 0; nb < G::kNB; ++nb) {
+          AF ak, av, auk, auv;
+          if constexpr (kPF != 0) {
+            ak = cur[0];
+            av = cur[1];
+            auk = cur[2];
+            auv = cur[3];
+            if (nb + 1 < G::kNB) load_frags(nb + 1);
+          } else {
+            ak = G::load_afrag(Ks, 16 * nb);
+            av = G::load_afrag(Vs, 16 * nb);
+            auk = G::load_afrag(UKs, 16 * nb);
+            auv = G::load_afrag(UVs, 16 * nb);
+          }
+#pragma unroll
+          for (int mb = 0; mb < MR; ++mb) {
+            aB[nb][mb] = E::mma_acc(ak, kCap ? fPu[mb] : fP[mb], aB[nb][mb]);
+            aOM[nb][mb] = E::mma_acc(ak, fPPt[mb], aOM[nb][mb]);
+            aOM[nb][mb] = E::mma_acc(auk, fPdd[mb], aOM[nb][mb]);
+            aDO[nb][mb] = E::mma_acc(auv, fP[mb], aDO[nb][mb]);
+            aDO[nb][mb] = E::mma_acc(av, fPF[mb], aDO[nb][mb]);
+          }
+        }
+      });
+#pragma unroll
+  for (int mb = 0; mb < MR; ++mb) {
+    alpha[mb] = group_sum(alpha[mb]);
+    e0[mb] = group_sum(e0[mb]);
+  }
+  if constexpr (KS > 1) {
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb)
+      if (g == 0) {
+        const int at = 16 * (wl * MR + mb) + j;
+        sm.sc[0][ks][at] = alpha[mb];
+        sm.sc[1][ks][at] = e0[mb];
+        ref_mem[(2 * ks + 0) * BR + at] = aref[mb];
+        ref_mem[(2 * ks + 1) * BR + at] = eref[mb];
+      }
+    __syncthreads();
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb) {
+      const int at = 16 * (wl * MR + mb) + j;
+      alpha[mb] = sm.sc[0][0][at];
+      e0[mb] = sm.sc[1][0][at];
+      // a row's reference is the same in all sets, or that of one and 0 in the others
+      aref[mb] = ref_mem[at];
+      eref[mb] = ref_mem[BR + at];
+#pragma unroll
+      for (int q = 1; q < KS; ++q) {
+        alpha[mb] += sm.sc[0][q][at];
+        e0[mb] += sm.sc[1][q][at];
+        const float ar = ref_mem[2 * q * BR + at], er = ref_mem[(2 * q + 1) * BR + at];
+        aref[mb] = ar != 0.f ? ar : aref[mb];
+        eref[mb] = er != 0.f ? er : eref[mb];
+      }
+    }
+    static_assert(sizeof(sm.lds) >= merge_bytes<KS, NW, G::kNB, MR>(), "set merge buffer");
+    floatx4 FB_LDS* buf = (floatx4 FB_LDS*)&sm.lds[0][0][0];
+    merge_sets<KS, NW>(aDO, ks, wl, buf);
+    merge_sets<KS, NW>(aOM, ks, wl, buf);
+    merge_sets<KS, NW>(aB, ks, wl, buf);
+  }
+  const RowSplit<KS> own{ks, 0};
+  if (a.nparts > 1) {
+    const int64_t all = (int64_t)(a.total / a.nRB) * rw.rows;
+    float* const sc = parts + a.nparts * all * (3 * D);
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb)
+      if (rw.ok(mb)) {
+        const int64_t at = part * all + rw.qrow + rw.row(mb);
+#pragma unroll
+        for (int nb = 0; nb < G::kNB; ++nb)
+          if (own.owns(nb)) {
+            float* const to = parts + at * (3 * D) + 16 * nb + 4 * g;
+            *(floatx4*)to = aDO[nb][mb];
+            *(floatx4*)(to + D) = aOM[nb][mb];
+            *(floatx4*)(to + 2 * D) = aB[nb][mb];
+          }
+        // of the parts of a row one at most has a reference: the join adds them
+        if (g == 0 && ks == 0) *(floatx4*)(sc + 4 * at) = floatx4{alpha[mb], e0[mb], aref[mb], eref[mb]};
+      }
+    return;
+  }
+  const floatx4 zero = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int mb = 0; mb < MR; ++mb) {
+    if (rw.row(mb) >= rw.rows) continue;
+    const int64_t at = rw.qrow + rw.row(mb);
+    if (g == 0 && ks == 0) {
+      const float al = aref[mb] + alpha[mb];
+      alpha_out[at] = rw.ok(mb) ? al : 0.f;
+      E_out[at] = rw.ok(mb) ? eref[mb] + e0[mb] - al * drow[mb] : 0.f;
+    }
+#pragma unroll
+    for (int nb = 0; nb < G::kNB; ++nb) {
+      if (!own.owns(nb)) continue;
+      const int64_t off = at * D + 16 * nb + 4 * g;
+      if (rw.ok(mb)) {
+        E::store4(dOt + off, aDO[nb][mb] - alpha[mb] * E::load4(O + off));
+        E::store4(Qt + off, a.scale * (aOM[nb][mb] - e0[mb] * aB[nb][mb]) - alpha[mb] * E::load4(dQ + off));
+      } else {
+        E::store4(dOt + off, zero);
+        E::store4(Qt + off, zero);
+      }
+    }
+  }
+}
+
+// ===========================================================================
+// BoB Pass 2, as ext_pass2_kernel.
+// ===========================================================================
+template <typename T, int D, int MC, int NW, int OCC, int KS, bool kPF, bool kCap>
+__global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass2_kernel(
+    ScoreArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ dO,
+    const T* __restrict__ UQ, const T* __restrict__ UK, const T* __restrict__ UV, const float* __restrict__ L,
+    const float* __restrict__ Dv, const float* __restrict__ alpha_in, const float* __restrict__ E_in,
+    T* __restrict__ Kt, T* __restrict__ Vt, float* __restrict__ parts) {
+  using E = Elt<T>;
+  using G = Geo<T, D>;
+  struct Smem2 {
+    T lds[KS][2][3 * G::kTileElems];
+    float rawsc[KS][2][4 * kBS];
+    float tsc[KS][2][4 * kBS];
+  };
+  __shared__ __attribute__((aligned(16))) Smem2 sm;
+  extern __shared__ float slope_mem[];
+  float FB_LDS* const slopes = (float FB_LDS*)slope_mem;
+
+  int kv, rb;
+  ext_map_cols(a, kv, rb);
+  const int l = lane_id(), g = l >> 4, j = l & 15;
+  const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id() / NW);
+  const int wl = __builtin_amdgcn_readfirstlane(KS == 1 ? wave_id() : wave_id() % NW);
+  const ScoreCols<MC, NW> cl(a, kv, rb, wl);
+  const int64_t koff = (int64_t)kv * a.Nk * D;
+
+  u32x4 kf[MC][G::kChunks], vf[MC][G::kChunks], ukf[MC][G::kChunks], uvf[MC][G::kChunks];
+#pragma unroll
+  for (int mc = 0; mc < MC; ++mc) {
+    const int col = cl.col0 + 16 * mc + j;
+    load_stationary<T, D>(kf[mc], K + koff, col, cl.klen);
+    load_stationary<T, D>(vf[mc], V + koff, col, cl.klen);
+    load_stationary<T, D>(ukf[mc], UK + koff, col, cl.klen);
+    load_stationary<T, D>(uvf[mc], UV + koff, col, cl.klen);
+  }
+  score_fill_slopes(a, kv, slopes, KS * NW * 64);
+  const int sloped = vector_mode(a.slopes != nullptr ? 1 : 0);
+  floatx4 aK[G::kNB][MC], aV[G::kNB][MC];
+#pragma unroll
+  for (int nb = 0; nb < G::kNB; ++nb)
+#pragma unroll
+    for (int mc = 0; mc < MC; ++mc) aK[nb][mc] = aV[nb][mc] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const float c = a.scale * kLog2e;
+  floatx4 s[2][MC], dp[2][MC], f[2][MC], cc[2][MC];
+  typename E::TFrag fPh[MC], fSt[MC], fdS[MC];
+
+  // Transformed row scalars: T0 = -L log2e, T1 = -D (the dP tile's start), T2 = -alpha,
+  // T3 = -(alpha D + E) (the C tile's start).  With h = F - alpha:
+  //   P h = p h,  P (Pt - E) = p (h (dP - D) + C - (alpha D + E)),  dZ = p (dP - D).
+  const int n = cl.count();
+  const ExtRun run(n, cl.sub * KS + ks, cl.subs * KS), first(n, cl.sub * KS, cl.subs * KS);
+  auto flat = [&](int it) { return min(run.begin + it, n - 1); };
+  const TileCopy<T, D, NW, 3> copy(wl);
+  stream_loop_rs<2, tile_loads<T, D, NW, 3>(), 2, true>(
+      0, first.size(), __builtin_amdgcn_readfirstlane(wl) == 0,
+      [&](int it, int rs) {
+        const int64_t qs = (int64_t)cl.qhead(flat(it)) * a.Nq;
+        const int s0 = cl.tile(flat(it)) * kBS;
+        float FB_LDS* dst = (float FB_LDS*)sm.rawsc[ks][rs];
+        issue_scalar_pair<true>(dst, L + qs, Dv + qs, s0, cl.qlen);
+        issue_scalar_pair<true>(dst + 2 * kBS, alpha_in + qs, E_in + qs, s0, cl.qlen);
+      },
+      [&](int it, int st) {
+        const int64_t qo = (int64_t)cl.qhead(flat(it)) * a.Nq * D;
+        const T* const src[3] = {Q + qo, UQ + qo, dO + qo};
+        copy.template issue<true>(src, (T FB_LDS*)sm.lds[ks][st], cl.tile(flat(it)) * kBS, cl.qlen);
+      },
+      [&](int, int rs, int ts) {
+        if (l < kBS) {
+          const float FB_LDS* raw = (const float FB_LDS*)sm.rawsc[ks][rs];
+          float FB_LDS* to = (float FB_LDS*)sm.tsc[ks][ts];
+          const float Lr = raw[l], Dr = raw[kBS + l], ar = raw[2 * kBS + l], Er = raw[3 * kBS + l];
+          to[l] = Lr == -INFINITY ? -INFINITY : -Lr * kLog2e;
+          to[kBS + l] = -Dr;
+          to[2 * kBS + l] = -ar;
+          to[3 * kBS + l] = -__builtin_fmaf(ar, Dr, Er);
+        }
+      },
+      [&](int it, int st, int ts, auto&& prep_next) {
+        const int s0 = cl.tile(flat(it)) * kBS;
+        const int mode = vector_mode(run.begin + it < run.end ? cl.reach.mode(s0) : 0);
+        if (mode == 0) {
+          prep_next();
+          return;
+        }
+        const T FB_LDS* Qs = (const T FB_LDS*)sm.lds[ks][st];
+        const T FB_LDS* UQs = Qs + G::kTileElems;
+        const T FB_LDS* dOs = UQs + G::kTileElems;
+        const float FB_LDS* Ts = (const float FB_LDS*)sm.tsc[ks][ts];
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb) {
+          const floatx4 t1 = *(const floatx4 FB_LDS*)(Ts + kBS + 16 * sb + 4 * g);
+          const floatx4 t3 = *(const floatx4 FB_LDS*)(Ts + 3 * kBS + 16 * sb + 4 * g);
+#pragma unroll
+          for (int mc = 0; mc < MC; ++mc) {
+            s[sb][mc] = f[sb][mc] = floatx4{0.f, 0.f, 0.f, 0.f};
+            dp[sb][mc] = t1;
+            cc[sb][mc] = t3;
+          }
+        }
+        auto score_step = [&](int sb, int kk, u32x4 aq, u32x4 auq, u32x4 ado) {
+#pragma unroll
+          for (int mc = 0; mc < MC; ++mc) {
+            s[sb][mc] = E::mma_chunk(aq, kf[mc][kk], s[sb][mc]);        // S = Q K^T
+            dp[sb][mc] = E::mma_chunk(ado, vf[mc][kk], dp[sb][mc]);     // dP - D
+            f[sb][mc] = E::mma_chunk(auq, kf[mc][kk], f[sb][mc]);       // U_Q K^T
+            f[sb][mc] = E::mma_chunk(aq, ukf[mc][kk], f[sb][mc]);       //  + Q U_K^T
+            cc[sb][mc] = E::mma_chunk(ado, uvf[mc][kk], cc[sb][mc]);    // C - (alpha D + E)
+          }
+        };
+        auto read_step = [&](int sb, int kk, u32x4 (&o)[3]) {
+          const int off = G::chunk_off(16 * sb + j, 4 * kk + g);
+          o[0] = *(const u32x4 FB_LDS*)(Qs + off);
+          o[1] = *(const u32x4 FB_LDS*)(UQs + off);
+          o[2] = *(const u32x4 FB_LDS*)(dOs + off);
+        };
+        __builtin_amdgcn_s_setprio(1);
+        if constexpr (kPF) {
+          constexpr int kSteps = 2 * G::kChunks;
+          u32x4 nx[3];
+          read_step(0, 0, nx);
+#pragma unroll
+          for (int q = 0; q < kSteps; ++q) {
+            const u32x4 aq = nx[0], auq = nx[1], ado = nx[2];
+            if (q + 1 < kSteps) read_step((q + 1) / G::kChunks, (q + 1) % G::kChunks, nx);
+            score_step(q / G::kChunks, q % G::kChunks, aq, auq, ado);
+          }
+        } else {
+#pragma unroll
+          for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+            for (int kk = 0; kk < G::kChunks; ++kk) {
+              u32x4 o[3];
+              read_step(sb, kk, o);
+              score_step(sb, kk, o[0], o[1], o[2]);
+            }
+        }
+        __builtin_amdgcn_s_setprio(0);
+        prep_next();
+        floatx4 t[kCap ? 2 : 1][kCap ? MC : 1];
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb) {
+          const floatx4 off = *(const floatx4 FB_LDS*)(Ts + 16 * sb + 4 * g);
+#pragma unroll
+          for (int mc = 0; mc < MC; ++mc)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              float tr = 0.f;
+              s[sb][mc][r] = score_exponent<T, kCap>(a, s[sb][mc][r], c, off[r], tr);
+              if constexpr (kCap) t[sb][mc][r] = tr;
+              f[sb][mc][r] *= kCap ? a.scale * cap_slope(tr) : a.scale;
+            }
+        }
+        typename E::AFrag cur[3];
+        if constexpr (kPF) {
+#pragma unroll
+          for (int x = 0; x < 3; ++x) cur[x] = G::load_afrag(Qs + x * G::kTileElems, 0);
+        }
+        if (sloped != 0) {
+          const float m = slopes[cl.qhead(flat(it)) - kv * a.grp];
+#pragma unroll
+          for (int mc = 0; mc < MC; ++mc)
+            score_slope<1>(s[0][mc], s[1][mc], cl.start + s0 + 4 * g - (cl.col0 + 16 * mc + j), m);
+        }
+        if (mode == 2) {
+#pragma unroll
+          for (int mc = 0; mc < MC; ++mc) score_mask(s[0][mc], s[1][mc], s0, cl.rows[mc]);
+        }
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb) {
+          const floatx4 t2 = *(const floatx4 FB_LDS*)(Ts + 2 * kBS + 16 * sb + 4 * g);
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int mc = 0; mc < MC; ++mc) {
+              const float p = fast_exp2(s[sb][mc][r]);
+              const float h = f[sb][mc][r] + t2[r], dd = dp[sb][mc][r];
+              const float w = __builtin_fmaf(h, dd, cc[sb][mc][r]);
+              const int i = 4 * sb + r;
+              fPh[mc].set(i, p * h);
+              if constexpr (kCap) {
+                const float tr = t[sb][mc][r], pu = p * cap_slope(tr);
+                fSt[mc].set(i, __builtin_fmaf(pu, w, -a.cap_k * tr * (p * dd) * f[sb][mc][r]));
+                fdS[mc].set(i, pu * dd);
+              } else {
+                fSt[mc].set(i, p * w);
+                fdS[mc].set(i, p * dd);
+              }
+            }
+        }
+#pragma unroll
+        for (int nb = 0; nb < G::kNB; ++nb) {
+          typename E::AFrag aq, auq, ado;
+          if constexpr (kPF) {
+            aq = cur[0];
+            auq = cur[1];
+            ado = cur[2];
+            if (nb + 1 < G::kNB) {
+#pragma unroll
+              for (int x = 0; x < 3; ++x) cur[x] = G::load_afrag(Qs + x * G::kTileElems, 16 * (nb + 1));
+            }
+          } else {
+            aq = G::load_afrag(Qs, 16 * nb);
+            auq = G::load_afrag(UQs, 16 * nb);
+            ado = G::load_afrag(dOs, 16 * nb);
+          }
+#pragma unroll
+          for (int mc = 0; mc < MC; ++mc) {
+            aV[nb][mc] = E::mma_acc(ado, fPh[mc], aV[nb][mc]);
+            aK[nb][mc] = E::mma_acc(aq, fSt[mc], aK[nb][mc]);
+            aK[nb][mc] = E::mma_acc(auq, fdS[mc], aK[nb][mc]);
+          }
+        }
+      });
+  if constexpr (KS > 1) {
+    static_assert(sizeof(sm.lds) >= merge_bytes<KS, NW, G::kNB, MC>(), "set merge buffer");
+    merge_sets<KS, NW>(aK, ks, wl, (floatx4 FB_LDS*)&sm.lds[0][0][0]);
+    merge_sets<KS, NW>(aV, ks, wl, (floatx4 FB_LDS*)&sm.lds[0][0][0]);
+  }
+  ext_store_cols<T, D, KS>(a, kv, cl.col0, cl.klen, ks, aK, aV, a.scale, 1.f, Kt, Vt, parts);
+}
+
+}  // namespace fb
