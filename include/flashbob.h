@@ -509,6 +509,73 @@ int64_t attn_score_workspace_bytes(int32_t call, int32_t dtype, int64_t B, int64
 int32_t attn_score_layout(int32_t kernel, int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,
                           int64_t d, int32_t causal, const attn_score* score, attn_ext_launch* launch);
 
+/* ---------------------------------------------------------------------------
+ * Heads of an attention from a projection's output: each head vector of the queries and keys is
+ * divided by its root mean square and multiplied by a weight (optional, for queries and keys
+ * apart), then the pairs of its first 2 `pairs` elements are rotated by angles of position:
+ *   y = R(n) (w x / sqrt(mean(x^2) + eps)),  R turns pair i by freqs[i] positions[axes[i], b, n]
+ * radians, counterclockwise.  Pair i is elements (i, i + pairs) or, interleaved, (2 i, 2 i + 1); the
+ * others stay.  Statistics and angles are fp32 (the angle's whole turns leave it in fp64, so
+ * far positions are as exact as near ones); matrices are rounded once.
+ *
+ * A tensor of head vectors [B,heads,N,d] is an attn_heads: element (b,h,n,i) lies at
+ * b stride_b + h stride_h + n stride_n + i; data is 16-byte aligned and the strides (any sign, 0
+ * too in inputs) multiples of 16 bytes.  So a projection's [B,N,heads,d] is read where it lies
+ * and an output may be a slot of a cache.  Outputs must not overlap each other; one may be the
+ * input of the same vectors in the same strides.  H or Hkv may be 0 (its tensors are not read).
+ * d is 32, 64, 128 or 256 for both types.  H + Hkv is at most 65535, B N at most 2^31.
+ *
+ * attn_rotary; all pointers are device memory of the current device:
+ *  positions  int32 [num_axes,B,N];  freqs fp64 [pairs];  axes int32 [pairs], NULL with one
+ *             axis (an axis outside 0..num_axes - 1 counts as the nearer end).  Not read if pairs is 0.
+ *  pairs      a multiple of 8, at most d / 2.
+ *  q_weight, k_weight  [d] in weight_dtype, 16-byte aligned, or NULL: no norm.
+ * Returns as above; BOB_EINVAL also where one of these rules is broken. */
+typedef struct {
+  void* data;
+  int64_t stride_b, stride_h, stride_n;
+} attn_heads;
+typedef struct {
+  const int32_t* positions;
+  const double* freqs;
+  const int32_t* axes;
+  int32_t num_axes;
+  int32_t pairs;
+  int32_t interleaved;
+  const void* q_weight;
+  const void* k_weight;
+  int32_t weight_dtype;
+  float eps;
+} attn_rotary;
+
+/* Forward.  In: Q, K.  Out: Qr, Kr.  inverse = 1 rotates back (without weights alone). */
+int32_t attn_rotary_fwd(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t N, int64_t d, int32_t inverse,
+                        const attn_rotary* rotary, const attn_heads* Q, const attn_heads* K, const attn_heads* Qr,
+                        const attn_heads* Kr, void* stream);
+
+/* Backward.  In: Q, K (with a weight), dQr, dKr.  Out: dQ, dK and the weights' gradients dWq, dWk (NULL: not
+ * wanted), summed in fp32 in a fixed order.  The workspace, for the weights' gradients, has
+ * attn_rotary_workspace_bytes and is 16-byte aligned. */
+int32_t attn_rotary_bwd(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t N, int64_t d,
+                        const attn_rotary* rotary, const attn_heads* Q, const attn_heads* K, const attn_heads* dQr,
+                        const attn_heads* dKr, const attn_heads* dQ, const attn_heads* dK, void* dWq, void* dWk,
+                        void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Backward of the backward: the gradients of <dQ,gdQ> + <dK,gdK> + <dWq,gdWq> + <dWk,gdWk>.
+ * In: Q, K, dQr, dKr (with a weight), gdQ, gdK, gdWq, gdWk (16-byte aligned; each may be NULL: 0).
+ * Out: Qt, Kt (with a weight; without one they are 0 and not written), dQrt, dKrt, and Wqt, Wkt (NULL:
+ * not wanted). */
+int32_t attn_rotary_bwd2(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t N, int64_t d,
+                         const attn_rotary* rotary, const attn_heads* Q, const attn_heads* K, const attn_heads* dQr,
+                         const attn_heads* dKr, const attn_heads* gdQ, const attn_heads* gdK, const void* gdWq,
+                         const void* gdWk, const attn_heads* Qt, const attn_heads* Kt, const attn_heads* dQrt,
+                         const attn_heads* dKrt, void* Wqt, void* Wkt, void* workspace, int64_t workspace_bytes,
+                         void* stream);
+
+/* Workspace bytes of the two calls above where they sum a weight's gradient. */
+int64_t attn_rotary_workspace_bytes(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t N, int64_t d,
+                                    const attn_rotary* rotary);
+
 /* 1 if (dtype, d) is built into this library, else 0. */
 int32_t bob_supported(int32_t dtype, int64_t d);
 

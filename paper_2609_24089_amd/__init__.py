@@ -90,9 +90,10 @@ def load_library():
     lib.attn_bob_pass2_cols_gqa_noalloc.restype = i32
     lib.bob_scratch_bytes.argtypes = []
     lib.bob_scratch_bytes.restype = i64
-    from . import _fb_torch, ext, score
+    from . import _fb_torch, ext, rotary, score
     ext._declare(lib)
     score._declare(lib)
+    rotary._declare(lib)
     _fb_torch.bind(LIB_PATH)
     _lib, _native = lib, _fb_torch
     return lib
@@ -436,3 +437,6 @@ from .ext import (  # noqa: E402  (attention between sequences of two lengths, w
 from .score import (  # noqa: E402  (attention over capped scores, distance biases and spans)
     ATTN_SCORE_BWD, ATTN_SCORE_FWD, ATTN_SCORE_PASS1, ATTN_SCORE_PASS2, AttnScore, attention_spans, attn_score_bwd,
     attn_score_fwd_lse, attn_score_layout, attn_score_pass1_rows, attn_score_pass2_cols, scored_attention)
+from .rotary import (  # noqa: E402  (normalised, rotated heads)
+    AttnHeads, AttnRotary, attn_rotary_bwd, attn_rotary_bwd2, attn_rotary_fwd, rotary_attention, rotary_frequencies,
+    rotate_heads)

@@ -28,6 +28,7 @@ SOURCES = [
     ("fb_ext_pass1.hip", []),
     ("fb_ext_pass2.hip", []),
     ("fb_ext_bob_d128.hip", ["-mllvm", "-amdgpu-sched-strategy=iterative-ilp"]),
+    ("fb_ext_rotary.hip", []),
     ("fb_ext_score.hip", []),
     ("fb_ext_score_fwd.hip", []),
     ("fb_ext_score_bwd.hip", []),

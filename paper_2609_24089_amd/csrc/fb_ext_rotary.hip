@@ -1,0 +1,577 @@
+// Normalised, rotated heads: each head vector of the queries and keys divided by its root mean
+// square and multiplied by a weight (optional), then rotated by the angles of its position,
+// forward, backward and the backward of that, and the C ABI.
+//
+// Per vector x of d elements with weight w, g = R^T dy (R: the rotation), a = w g, u the
+// cotangent on dx, uw that on dw, and xh = r x, r = (mean x^2 + eps)^-1/2:
+//   y  = R (w xh)
+//   dx = r (a - (a.xh) xh / d),  dw = sum g xh
+//   the gradients of <dx, u> + <dw, uw>, with A = a.u, B = a.xh, C = u.xh, S = (uw g).xh:
+//   xt = r uw g - r ((r A + S) xh + r C a + r B u) / d + 3 r^2 B C xh / d^2
+//   wt = sum (r g u - r C g xh / d)
+//   gt = r w u - r C w xh / d + uw xh,  dyt = R gt
+// Without a weight y = R x, dx = R^T dy and dyt = R u.
+//
+// Everything is bound by memory: each call reads and writes every vector once, whatever the
+// layout (strides of batch entry, head and token), so the way from a projection's [B,N,heads,d]
+// to an attention's [B,heads,N,d] is part of it.  d / 16 lanes share a vector: a lane holds
+// eight pairs, whose halves are two runs of eight elements (neighbours paired: one run of 16), so
+// it loads 16 bytes at a time and a rotation needs no other lane.  A lane keeps its token and
+// goes through heads, for which the cosines and sines are made once.
+#include "fb_ext.h"
+
+namespace fb {
+
+// Tensor of head vectors: element strides of batch entry, head and token.
+struct Heads {
+  void* data;
+  int64_t b, h, n;
+};
+
+struct RotaryArgs {
+  int B, N, H[2];         // H: heads of the queries, of the keys
+  int chunk, chunks[2];   // heads a workgroup goes through; workgroups that cover the heads
+  int pairs, num_axes;
+  const int32_t* positions;  // [num_axes, B, N]
+  const double* freqs;       // [pairs]: radians a position
+  const int32_t* axes;       // [pairs] or null: axis 0
+  const void* w[2];          // [d] or null: no norm
+  const void* uw[2];         // cotangents on dw, or null: 0
+  int w_bf16;
+  float eps, sign;           // of the angles: -1 rotates back
+  // x; y (forward) or dx; dy; u; x~; dy~
+  Heads x[2], out[2], dy[2], u[2], xt[2], dyt[2];
+  float* sums;               // [chunks of both][gridDim.x][d]: sums of dw or wt, or null
+};
+
+constexpr int kRotaryThreads = 256;
+constexpr double kTurns = 0.15915494309189535;  // 1 / (2 pi)
+
+// Sum over the d / 16 lanes (a power of two up to 16) that share a vector: all of them get it.
+template <int LPV> __device__ __forceinline__ float vector_sum(float v) {
+  auto add = [&](auto ctrl) {
+    v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, 0xf,
+                                                               0xf, true));
+  };
+  if constexpr (LPV >= 2) add(std::integral_constant<int, 0xb1>{});   // quad_perm 1,0,3,2
+  if constexpr (LPV >= 4) add(std::integral_constant<int, 0x4e>{});   // quad_perm 2,3,0,1
+  if constexpr (LPV >= 8) add(std::integral_constant<int, 0x141>{});  // row_half_mirror
+  if constexpr (LPV >= 16) add(std::integral_constant<int, 0x140>{}); // row_mirror
+  return v;
+}
+
+// Where a lane's two runs of eight elements lie in a vector, and whether they are rotated.
+struct LanePairs {
+  int a, b;     // first elements
+  bool turned;
+  int pair;     // first pair
+};
+template <bool kNeighbours> __device__ __forceinline__ LanePairs lane_pairs(int p, int pairs) {
+  LanePairs l;
+  l.turned = 8 * p < pairs;
+  l.pair = 8 * p;
+  if (kNeighbours || !l.turned) {
+    l.a = 16 * p;
+    l.b = 16 * p + 8;
+  } else {
+    l.a = 8 * p;
+    l.b = pairs + 8 * p;
+  }
+  return l;
+}
+
+template <typename T> __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    const bf16x8 v = __builtin_bit_cast(bf16x8, *(const u32x4*)p);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
+  } else {
+    const floatx4 v0 = *(const floatx4*)p, v1 = *(const floatx4*)(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = v0[i], x[4 + i] = v1[i];
+  }
+}
+template <typename T> __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    bf16x8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (bf16)x[i];
+    *(u32x4*)p = __builtin_bit_cast(u32x4, v);
+  } else {
+    *(floatx4*)p = floatx4{x[0], x[1], x[2], x[3]};
+    *(floatx4*)(p + 4) = floatx4{x[4], x[5], x[6], x[7]};
+  }
+}
+
+// The lane's 16 elements as pairs (a[i], b[i]).
+struct Pairs {
+  float a[8], b[8];
+};
+// Neighbours come as elements 0 .. 7 and 8 .. 15.
+__device__ __forceinline__ Pairs from_neighbours(const Pairs& e) {
+  Pairs p;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    p.a[i] = e.a[2 * i], p.b[i] = e.a[2 * i + 1];
+    p.a[4 + i] = e.b[2 * i], p.b[4 + i] = e.b[2 * i + 1];
+  }
+  return p;
+}
+__device__ __forceinline__ Pairs to_neighbours(const Pairs& p) {
+  Pairs e;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    e.a[2 * i] = p.a[i], e.a[2 * i + 1] = p.b[i];
+    e.b[2 * i] = p.a[4 + i], e.b[2 * i + 1] = p.b[4 + i];
+  }
+  return e;
+}
+template <typename T, bool kNeighbours> __device__ __forceinline__ Pairs load_pairs(const T* v, const LanePairs& l) {
+  Pairs p;
+  load8(v + l.a, p.a);
+  load8(v + l.b, p.b);
+  return kNeighbours ? from_neighbours(p) : p;
+}
+template <typename T, bool kNeighbours>
+__device__ __forceinline__ void store_pairs(T* v, const LanePairs& l, const Pairs& x) {
+  const Pairs p = kNeighbours ? to_neighbours(x) : x;
+  store8(v + l.a, p.a);
+  store8(v + l.b, p.b);
+}
+template <bool kNeighbours>
+__device__ __forceinline__ Pairs load_weight(const void* w, int w_bf16, const LanePairs& l) {
+  if (w_bf16 != 0) return load_pairs<bf16, kNeighbours>((const bf16*)w, l);
+  return load_pairs<float, kNeighbours>((const float*)w, l);
+}
+
+// x turned by the angles (sign 1) or back (-1).
+__device__ __forceinline__ Pairs turn(const Pairs& x, const Pairs& cs, float sign) {
+  Pairs y;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float s = sign * cs.b[i];
+    y.a[i] = __builtin_fmaf(x.a[i], cs.a[i], -(x.b[i] * s));
+    y.b[i] = __builtin_fmaf(x.a[i], s, x.b[i] * cs.a[i]);
+  }
+  return y;
+}
+template <class F> __device__ __forceinline__ Pairs each(F&& f) {
+  Pairs y;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    y.a[i] = f([i](const Pairs& p) { return p.a[i]; });
+    y.b[i] = f([i](const Pairs& p) { return p.b[i]; });
+  }
+  return y;
+}
+template <int LPV> __device__ __forceinline__ float dot(const Pairs& x, const Pairs& y) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s = __builtin_fmaf(x.a[i], y.a[i], __builtin_fmaf(x.b[i], y.b[i], s));
+  return vector_sum<LPV>(s);
+}
+
+// kMode 0: y (or, with sign -1 and no weights, x from y); 1: dx, dw; 2: x~, dy~, w~.
+template <typename T, int D, int kMode, bool kNeighbours>
+__global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a) {
+  constexpr int LPV = D / 16, kSlots = kRotaryThreads / LPV;
+  const int slot = threadIdx.x / LPV, p = threadIdx.x % LPV;
+  const int k = (int)blockIdx.y < a.chunks[0] ? 0 : 1;  // queries or keys
+  const int h0 = ((int)blockIdx.y - (k == 0 ? 0 : a.chunks[0])) * a.chunk, h1 = min(h0 + a.chunk, a.H[k]);
+  const LanePairs l = lane_pairs<kNeighbours>(p, a.pairs);
+  const bool norm = a.w[k] != nullptr;
+  Pairs w, uw, sum;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w.a[i] = w.b[i] = 1.f, uw.a[i] = uw.b[i] = sum.a[i] = sum.b[i] = 0.f;
+  if (norm) {
+    w = load_weight<kNeighbours>(a.w[k], a.w_bf16, l);
+    if (kMode == 2 && a.uw[k] != nullptr) uw = load_weight<kNeighbours>(a.uw[k], a.w_bf16, l);
+  }
+  const int64_t tokens = (int64_t)a.B * a.N;
+  for (int64_t t0 = (int64_t)blockIdx.x * kSlots; t0 < tokens; t0 += (int64_t)gridDim.x * kSlots) {
+    const int64_t t = min(t0 + slot, tokens - 1);
+    const bool live = t0 + slot < tokens;
+    const int64_t b = t / a.N, n = t - b * a.N;
+    Pairs cs;  // cosines and sines
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      cs.a[i] = 1.f;
+      cs.b[i] = 0.f;
+      if (l.turned) {
+        // the angle in turns, without its whole ones, in 64 bits: far positions keep their fraction
+        const int axis = a.axes != nullptr ? min(max(a.axes[l.pair + i], 0), a.num_axes - 1) : 0;
+        const double turns = a.freqs[l.pair + i] * kTurns * (double)a.positions[(int64_t)axis * tokens + t];
+        sincospif(2.f * (float)(turns - rint(turns)), &cs.b[i], &cs.a[i]);
+        cs.b[i] *= a.sign;
+      }
+    }
+    auto at = [&](const Heads& v, int h) { return (T*)v.data + b * v.b + h * v.h + n * v.n; };
+    for (int h = h0; h < h1; ++h) {
+      if constexpr (kMode == 0) {
+        Pairs x = load_pairs<T, kNeighbours>(at(a.x[k], h), l);
+        if (norm) {
+          const float r = rsqrtf(dot<LPV>(x, x) * (1.f / D) + a.eps);
+          x = each([&](auto of) { return of(x) * r * of(w); });
+        }
+        if (live) store_pairs<T, kNeighbours>(at(a.out[k], h), l, turn(x, cs, 1.f));
+      } else if constexpr (kMode == 1) {
+        const Pairs g = turn(load_pairs<T, kNeighbours>(at(a.dy[k], h), l), cs, -1.f);
+        if (!norm) {
+          if (live) store_pairs<T, kNeighbours>(at(a.out[k], h), l, g);
+          continue;
+        }
+        Pairs x = load_pairs<T, kNeighbours>(at(a.x[k], h), l);
+        const float r = rsqrtf(dot<LPV>(x, x) * (1.f / D) + a.eps);
+        x = each([&](auto of) { return of(x) * r; });
+        const Pairs aw = each([&](auto of) { return of(w) * of(g); });
+        const float B = dot<LPV>(aw, x) * (1.f / D);
+        if (live) {
+          sum = each([&](auto of) { return __builtin_fmaf(of(g), of(x), of(sum)); });
+          store_pairs<T, kNeighbours>(at(a.out[k], h), l,
+                                      each([&](auto of) { return r * __builtin_fmaf(-B, of(x), of(aw)); }));
+        }
+      } else {
+        Pairs u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u.a[i] = u.b[i] = 0.f;
+        if (a.u[k].data != nullptr) u = load_pairs<T, kNeighbours>(at(a.u[k], h), l);
+        if (!norm) {
+          if (live) store_pairs<T, kNeighbours>(at(a.dyt[k], h), l, turn(u, cs, 1.f));
+          continue;
+        }
+        const Pairs g = turn(load_pairs<T, kNeighbours>(at(a.dy[k], h), l), cs, -1.f);
+        Pairs x = load_pairs<T, kNeighbours>(at(a.x[k], h), l);
+        const float r = rsqrtf(dot<LPV>(x, x) * (1.f / D) + a.eps);
+        x = each([&](auto of) { return of(x) * r; });
+        const Pairs aw = each([&](auto of) { return of(w) * of(g); });
+        const Pairs ug = each([&](auto of) { return of(uw) * of(g); });
+        const float A = dot<LPV>(aw, u) * (1.f / D), B = dot<LPV>(aw, x) * (1.f / D);
+        const float C = dot<LPV>(u, x) * (1.f / D), S = dot<LPV>(ug, x) * (1.f / D);
+        const float by_x = __builtin_fmaf(3.f * r, B * C, -__builtin_fmaf(r, A, S));
+        if (live) {
+          sum = each([&](auto of) { return __builtin_fmaf(r * of(g), __builtin_fmaf(-C, of(x), of(u)), of(sum)); });
+          store_pairs<T, kNeighbours>(at(a.xt[k], h), l, each([&](auto of) {
+                                        const float m = __builtin_fmaf(C, of(aw), B * of(u));
+                                        return r * (of(ug) + __builtin_fmaf(by_x, of(x), -r * m));
+                                      }));
+          const Pairs gt = each([&](auto of) {
+            return __builtin_fmaf(r * of(w), __builtin_fmaf(-C, of(x), of(u)), of(uw) * of(x));
+          });
+          store_pairs<T, kNeighbours>(at(a.dyt[k], h), l, turn(gt, cs, 1.f));
+        }
+      }
+    }
+  }
+  if constexpr (kMode != 0) {
+    if (a.sums == nullptr || !norm) return;
+    // the workgroup's sums in one row
+    __shared__ float rows[kSlots][D];
+    Pairs e = kNeighbours ? to_neighbours(sum) : sum;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      rows[slot][l.a + i] = e.a[i];
+      rows[slot][l.b + i] = e.b[i];
+    }
+    __syncthreads();
+    float* const to = a.sums + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * D;
+    for (int x = threadIdx.x; x < D; x += kRotaryThreads) {
+      float v = 0.f;
+#pragma unroll
+      for (int s = 0; s < kSlots; ++s) v += rows[s][x];
+      to[x] = v;
+    }
+  }
+}
+
+// Adds the workgroups' rows of sums: 16 columns of the queries' (blockIdx.y 0) or keys' weight a
+// workgroup, 16 threads a column.
+__global__ __launch_bounds__(256) void rotary_sums_kernel(const float* __restrict__ sums, int d, int64_t rows_q,
+                                                          int64_t rows_k, void* out_q, void* out_k, int w_bf16) {
+  __shared__ float part[16][17];
+  void* const out = blockIdx.y == 0 ? out_q : out_k;
+  if (out == nullptr) return;
+  const int64_t first = blockIdx.y == 0 ? 0 : rows_q, n = blockIdx.y == 0 ? rows_q : rows_k;
+  const int x = threadIdx.x & 15, y = threadIdx.x >> 4, col = blockIdx.x * 16 + x;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int64_t r = y; r < n; r += 64)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (r + 16 * i < n) v[i] += sums[(first + r + 16 * i) * d + col];
+  part[y][x] = (v[0] + v[1]) + (v[2] + v[3]);
+  __syncthreads();
+  if (threadIdx.x < 16) {
+    float s = 0.f;
+    for (int i = 0; i < 16; ++i) s += part[i][threadIdx.x];
+    const int at = blockIdx.x * 16 + threadIdx.x;
+    if (w_bf16 != 0)
+      ((bf16*)out)[at] = (bf16)s;
+    else
+      ((float*)out)[at] = s;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Host
+// ---------------------------------------------------------------------------
+struct RotaryProblem {
+  int32_t dtype;
+  int64_t B, H, Hkv, N, d;
+  attn_rotary r;
+};
+
+// Returns BOB_OK to proceed, or an error; sets *empty where there are no vectors.
+static int32_t rotary_check(const RotaryProblem& p, bool* empty) {
+  *empty = false;
+  if (p.dtype != BOB_F32 && p.dtype != BOB_BF16) return BOB_EINVAL;
+  if (p.B < 0 || p.H < 0 || p.Hkv < 0 || p.N < 0) return BOB_EINVAL;
+  if (p.d != 32 && p.d != 64 && p.d != 128 && p.d != 256) return BOB_EUNSUPPORTED;
+  if (p.r.pairs < 0 || p.r.pairs % 8 != 0 || 2 * (int64_t)p.r.pairs > p.d) return BOB_EINVAL;
+  if (p.r.interleaved != 0 && p.r.interleaved != 1) return BOB_EINVAL;
+  auto aligned = [](const void* q, uintptr_t n) { return (reinterpret_cast<uintptr_t>(q) & (n - 1)) == 0; };
+  if (p.r.q_weight != nullptr || p.r.k_weight != nullptr) {
+    if (p.r.weight_dtype != BOB_F32 && p.r.weight_dtype != BOB_BF16) return BOB_EINVAL;
+    if (!aligned(p.r.q_weight, 16) || !aligned(p.r.k_weight, 16)) return BOB_EINVAL;
+    if (!(p.r.eps >= 0.f) || !std::isfinite(p.r.eps)) return BOB_EINVAL;
+  }
+  if (p.B == 0 || p.N == 0 || p.H + p.Hkv == 0) {
+    *empty = true;
+    return BOB_OK;
+  }
+  if (p.r.pairs > 0) {
+    if (p.r.num_axes < 1 || p.r.positions == nullptr || p.r.freqs == nullptr) return BOB_EINVAL;
+    if (!aligned(p.r.positions, 4) || !aligned(p.r.freqs, 8) || !aligned(p.r.axes, 4)) return BOB_EINVAL;
+    if (p.r.num_axes > 1 && p.r.axes == nullptr) return BOB_EINVAL;
+  }
+  // a launch has one block a group of tokens and fewer than 2^16 chunks of heads
+  if (p.N > kMaxN || p.B > INT32_MAX || p.B * p.N > (int64_t(1) << 31) || p.H > 65535 || p.Hkv > 65535 ||
+      p.H + p.Hkv > 65535)
+    return BOB_EINVAL;
+  return BOB_OK;
+}
+
+// How a launch runs: groups of tokens, heads a workgroup.
+struct RotaryPlan {
+  int64_t groups;
+  int chunk, chunks[2];
+  int64_t rows(int k) const { return groups * chunks[k]; }
+};
+// As many workgroups as keep the device's memory busy (kEnough), then more heads a workgroup, for
+// which the angles are made once.  Calls that sum a weight's gradient have about kMaxSums
+// rows of sums; a launch takes fewer than 2^32 threads (kMaxBlocks: 2^31).  Workgroups go on
+// to further groups of tokens.
+constexpr int64_t kEnough = 2048, kMaxSums = 1024, kMaxBlocks = int64_t(1) << 23;
+static RotaryPlan rotary_plan(const RotaryProblem& p, bool sums) {
+  RotaryPlan c;
+  const int64_t slots = kRotaryThreads / (p.d / 16), all = (p.B * p.N + slots - 1) / slots;
+  auto set = [&](int chunk) {
+    c.chunk = chunk;
+    c.chunks[0] = (int)((p.H + chunk - 1) / chunk);
+    c.chunks[1] = (int)((p.Hkv + chunk - 1) / chunk);
+  };
+  int chunk = 8;
+  for (set(chunk); chunk > 1 && all * (c.chunks[0] + c.chunks[1]) < kEnough; set(chunk)) chunk /= 2;
+  c.groups = std::min(all, std::max<int64_t>(1, (sums ? kMaxSums : kMaxBlocks) / (c.chunks[0] + c.chunks[1])));
+  return c;
+}
+static int64_t rotary_bytes(const RotaryProblem& p) {
+  if (p.r.q_weight == nullptr && p.r.k_weight == nullptr) return 0;
+  const RotaryPlan c = rotary_plan(p, true);
+  return (c.rows(0) + c.rows(1)) * p.d * 4;
+}
+
+// A tensor of head vectors of `heads` heads: present, aligned, in strides that keep 16 bytes.
+static bool heads_ok(const RotaryProblem& p, int64_t heads, const attn_heads* v, bool required) {
+  if (heads == 0) return true;
+  if (v == nullptr || v->data == nullptr) return !required;
+  const int64_t unit = p.dtype == BOB_BF16 ? 8 : 4;
+  return aligned16(v->data) && v->stride_b % unit == 0 && v->stride_h % unit == 0 && v->stride_n % unit == 0;
+}
+static Heads heads_of(const attn_heads* v) {
+  return v == nullptr ? Heads{} : Heads{v->data, v->stride_b, v->stride_h, v->stride_n};
+}
+
+static RotaryArgs rotary_args(const RotaryProblem& p, const RotaryPlan& c) {
+  RotaryArgs a{};
+  a.B = (int)p.B;
+  a.N = (int)p.N;
+  a.H[0] = (int)p.H;
+  a.H[1] = (int)p.Hkv;
+  a.chunk = c.chunk;
+  a.chunks[0] = c.chunks[0];
+  a.chunks[1] = c.chunks[1];
+  a.pairs = p.r.pairs;
+  a.num_axes = p.r.num_axes;
+  a.positions = p.r.positions;
+  a.freqs = p.r.freqs;
+  a.axes = p.r.axes;
+  a.w[0] = p.r.q_weight;
+  a.w[1] = p.r.k_weight;
+  a.w_bf16 = p.r.weight_dtype == BOB_BF16 ? 1 : 0;
+  a.eps = p.r.eps;
+  a.sign = 1.f;
+  return a;
+}
+
+template <int kMode> static int32_t rotary_launch(const RotaryProblem& p, const RotaryPlan& c, const RotaryArgs& a,
+                                                  hipStream_t s) {
+  const dim3 grid((unsigned)c.groups, (unsigned)(c.chunks[0] + c.chunks[1]));
+  (void)hipGetLastError();
+  auto go = [&](auto type, auto dim) {
+    using T = decltype(type);
+    constexpr int D = decltype(dim)::value;
+    if (p.r.interleaved != 0)
+      hipLaunchKernelGGL((rotary_kernel<T, D, kMode, true>), grid, dim3(kRotaryThreads), 0, s, a);
+    else
+      hipLaunchKernelGGL((rotary_kernel<T, D, kMode, false>), grid, dim3(kRotaryThreads), 0, s, a);
+  };
+  auto dims = [&](auto type) {
+    if (p.d == 32) go(type, std::integral_constant<int, 32>{});
+    if (p.d == 64) go(type, std::integral_constant<int, 64>{});
+    if (p.d == 128) go(type, std::integral_constant<int, 128>{});
+    if (p.d == 256) go(type, std::integral_constant<int, 256>{});
+  };
+  if (p.dtype == BOB_BF16)
+    dims(bf16{});
+  else
+    dims(float{});
+  return finish_launch();
+}
+
+// The workgroups' sums -> the weights' gradients.
+static int32_t rotary_gather(const RotaryProblem& p, const RotaryPlan& c, const float* sums, void* out_q, void* out_k,
+                             hipStream_t s) {
+  hipLaunchKernelGGL(rotary_sums_kernel, dim3((unsigned)(p.d / 16), 2), dim3(256), 0, s, sums, (int)p.d, c.rows(0),
+                     c.rows(1), out_q, out_k, p.r.weight_dtype == BOB_BF16 ? 1 : 0);
+  return finish_launch();
+}
+
+static RotaryProblem rotary_problem(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t N, int64_t d,
+                                    const attn_rotary* r) {
+  RotaryProblem p{dtype, B, H, Hkv, N, d, attn_rotary{}};
+  if (r != nullptr) p.r = *r;
+  return p;
+}
+// A weight's gradient: not without the weight, aligned to its type.
+static bool weight_ptr(const RotaryProblem& p, const void* weight, const void* grad, uintptr_t align) {
+  if (grad == nullptr) return true;
+  return weight != nullptr && (reinterpret_cast<uintptr_t>(grad) & (align - 1)) == 0;
+}
+
+}  // namespace fb
+
+using fb::RotaryProblem;
+
+extern "C" {
+
+int32_t attn_rotary_fwd(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t N, int64_t d, int32_t inverse,
+                        const attn_rotary* rotary, const attn_heads* Q, const attn_heads* K, const attn_heads* Qr,
+                        const attn_heads* Kr, void* stream) {
+  const RotaryProblem p = fb::rotary_problem(dtype, B, H, Hkv, N, d, rotary);
+  bool empty;
+  const int32_t rc = fb::rotary_check(p, &empty);
+  if (rc != BOB_OK) return rc;
+  if (rotary == nullptr || (inverse != 0 && inverse != 1)) return BOB_EINVAL;
+  if (inverse != 0 && (p.r.q_weight != nullptr || p.r.k_weight != nullptr)) return BOB_EINVAL;
+  if (empty) return BOB_OK;
+  if (!fb::heads_ok(p, H, Q, true) || !fb::heads_ok(p, Hkv, K, true) || !fb::heads_ok(p, H, Qr, true) ||
+      !fb::heads_ok(p, Hkv, Kr, true))
+    return BOB_EINVAL;
+  const fb::RotaryPlan c = fb::rotary_plan(p, false);
+  fb::RotaryArgs a = fb::rotary_args(p, c);
+  a.sign = inverse != 0 ? -1.f : 1.f;
+  a.x[0] = fb::heads_of(Q);
+  a.x[1] = fb::heads_of(K);
+  a.out[0] = fb::heads_of(Qr);
+  a.out[1] = fb::heads_of(Kr);
+  return fb::rotary_launch<0>(p, c, a, (hipStream_t)stream);
+}
+
+int32_t attn_rotary_bwd(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t N, int64_t d,
+                        const attn_rotary* rotary, const attn_heads* Q, const attn_heads* K, const attn_heads* dQr,
+                        const attn_heads* dKr, const attn_heads* dQ, const attn_heads* dK, void* dWq, void* dWk,
+                        void* workspace, int64_t workspace_bytes, void* stream) {
+  const RotaryProblem p = fb::rotary_problem(dtype, B, H, Hkv, N, d, rotary);
+  bool empty;
+  int32_t rc = fb::rotary_check(p, &empty);
+  if (rc != BOB_OK) return rc;
+  const uintptr_t align = p.r.weight_dtype == BOB_F32 ? 4 : 2;
+  if (rotary == nullptr || !fb::weight_ptr(p, p.r.q_weight, dWq, align) ||
+      !fb::weight_ptr(p, p.r.k_weight, dWk, align))
+    return BOB_EINVAL;
+  const bool sums = dWq != nullptr || dWk != nullptr;
+  if (empty && !sums) return BOB_OK;
+  fb::RotaryPlan c{};
+  if (!empty) {
+    if (!fb::heads_ok(p, H, Q, p.r.q_weight != nullptr) || !fb::heads_ok(p, Hkv, K, p.r.k_weight != nullptr) ||
+        !fb::heads_ok(p, H, dQr, true) || !fb::heads_ok(p, Hkv, dKr, true) || !fb::heads_ok(p, H, dQ, true) ||
+        !fb::heads_ok(p, Hkv, dK, true))
+      return BOB_EINVAL;
+    if (sums && (workspace_bytes < fb::rotary_bytes(p) || !fb::aligned16(workspace))) return BOB_EINVAL;
+    c = fb::rotary_plan(p, sums);
+    fb::RotaryArgs a = fb::rotary_args(p, c);
+    a.x[0] = fb::heads_of(Q);
+    a.x[1] = fb::heads_of(K);
+    a.dy[0] = fb::heads_of(dQr);
+    a.dy[1] = fb::heads_of(dKr);
+    a.out[0] = fb::heads_of(dQ);
+    a.out[1] = fb::heads_of(dK);
+    a.sums = sums ? (float*)workspace : nullptr;
+    rc = fb::rotary_launch<1>(p, c, a, (hipStream_t)stream);
+  }
+  return rc == BOB_OK && sums ? fb::rotary_gather(p, c, (const float*)workspace, dWq, dWk, (hipStream_t)stream) : rc;
+}
+
+int32_t attn_rotary_bwd2(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t N, int64_t d,
+                         const attn_rotary* rotary, const attn_heads* Q, const attn_heads* K, const attn_heads* dQr,
+                         const attn_heads* dKr, const attn_heads* gdQ, const attn_heads* gdK, const void* gdWq,
+                         const void* gdWk, const attn_heads* Qt, const attn_heads* Kt, const attn_heads* dQrt,
+                         const attn_heads* dKrt, void* Wqt, void* Wkt, void* workspace, int64_t workspace_bytes,
+                         void* stream) {
+  const RotaryProblem p = fb::rotary_problem(dtype, B, H, Hkv, N, d, rotary);
+  bool empty;
+  int32_t rc = fb::rotary_check(p, &empty);
+  if (rc != BOB_OK) return rc;
+  const uintptr_t align = p.r.weight_dtype == BOB_F32 ? 4 : 2;
+  if (rotary == nullptr || !fb::weight_ptr(p, p.r.q_weight, Wqt, align) ||
+      !fb::weight_ptr(p, p.r.k_weight, Wkt, align) || !fb::weight_ptr(p, p.r.q_weight, gdWq, 16) ||
+      !fb::weight_ptr(p, p.r.k_weight, gdWk, 16))
+    return BOB_EINVAL;
+  const bool sums = Wqt != nullptr || Wkt != nullptr;
+  if (empty && !sums) return BOB_OK;
+  fb::RotaryPlan c{};
+  if (!empty) {
+    const bool nq = p.r.q_weight != nullptr, nk = p.r.k_weight != nullptr;
+    if (!fb::heads_ok(p, H, Q, nq) || !fb::heads_ok(p, Hkv, K, nk) || !fb::heads_ok(p, H, dQr, nq) ||
+        !fb::heads_ok(p, Hkv, dKr, nk) || !fb::heads_ok(p, H, gdQ, false) || !fb::heads_ok(p, Hkv, gdK, false) ||
+        !fb::heads_ok(p, H, Qt, nq) || !fb::heads_ok(p, Hkv, Kt, nk) || !fb::heads_ok(p, H, dQrt, true) ||
+        !fb::heads_ok(p, Hkv, dKrt, true))
+      return BOB_EINVAL;
+    if (sums && (workspace_bytes < fb::rotary_bytes(p) || !fb::aligned16(workspace))) return BOB_EINVAL;
+    c = fb::rotary_plan(p, sums);
+    fb::RotaryArgs a = fb::rotary_args(p, c);
+    a.x[0] = fb::heads_of(Q);
+    a.x[1] = fb::heads_of(K);
+    a.dy[0] = fb::heads_of(dQr);
+    a.dy[1] = fb::heads_of(dKr);
+    a.u[0] = fb::heads_of(gdQ);
+    a.u[1] = fb::heads_of(gdK);
+    a.uw[0] = gdWq;
+    a.uw[1] = gdWk;
+    a.xt[0] = fb::heads_of(Qt);
+    a.xt[1] = fb::heads_of(Kt);
+    a.dyt[0] = fb::heads_of(dQrt);
+    a.dyt[1] = fb::heads_of(dKrt);
+    a.sums = sums ? (float*)workspace : nullptr;
+    rc = fb::rotary_launch<2>(p, c, a, (hipStream_t)stream);
+  }
+  return rc == BOB_OK && sums ? fb::rotary_gather(p, c, (const float*)workspace, Wqt, Wkt, (hipStream_t)stream) : rc;
+}
+
+int64_t attn_rotary_workspace_bytes(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t N, int64_t d,
+                                    const attn_rotary* rotary) {
+  const RotaryProblem p = fb::rotary_problem(dtype, B, H, Hkv, N, d, rotary);
+  bool empty;
+  return fb::rotary_check(p, &empty) != BOB_OK || empty ? 0 : fb::rotary_bytes(p);
+}
+
+}  // extern "C"
