@@ -452,6 +452,10 @@ int32_t attn_ext_layout(int32_t kernel, int32_t dtype, int64_t B, int64_t H, int
  * P is the softmax of z over the valid keys.  The first backward's dS is dz (1 - tanh^2), and the
  * passes take the second derivative of the tanh along; there is no gradient in cap and slopes.
  *
+ * Orest [B,H,Nq,d] in the matrices' type is what rounding O to it left: O + Orest is the output in
+ * twice the bits.  The calls that read O take it too (NULL: 0): D, and the terms of dQ, Qt and dOt that
+ * cancel in rows whose weight lies on few keys, are then not off by O's rounding.
+ *
  * attn_score (NULL: a plain softmax); all pointers are device memory of the current device:
  *  q_lens, kv_lens, q_starts  as in attn_ext.
  *  spans   int32 [B,Nk,4], 16-byte aligned, or NULL.  Entry p of a batch entry holds for position p
@@ -473,24 +477,25 @@ typedef struct {
   float cap;
 } attn_score;
 
-/* Forward.  In: Q, K, V.  Out: O, L. */
+/* Forward.  In: Q, K, V.  Out: O, Orest (may be NULL: not wanted), L. */
 int32_t attn_score_fwd_lse(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
                            float scale, int32_t causal, const attn_score* score, const void* Q, const void* K,
-                           const void* V, void* O, float* L, void* workspace, int64_t workspace_bytes, void* stream);
+                           const void* V, void* O, void* Orest, float* L, void* workspace, int64_t workspace_bytes,
+                           void* stream);
 
-/* First backward.  In: Q, K, V, O, dO, L.  Out: dQ, dK, dV, D. */
+/* First backward.  In: Q, K, V, O, Orest, dO, L.  Out: dQ, dK, dV, D. */
 int32_t attn_score_bwd(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
                        float scale, int32_t causal, const attn_score* score, const void* Q, const void* K,
-                       const void* V, const void* O, const void* dO, const float* L, void* dQ, void* dK, void* dV,
-                       float* D, void* workspace, int64_t workspace_bytes, void* stream);
+                       const void* V, const void* O, const void* Orest, const void* dO, const float* L, void* dQ,
+                       void* dK, void* dV, float* D, void* workspace, int64_t workspace_bytes, void* stream);
 
-/* BoB Pass 1.  In: Q, K, V, O, dO, gdQ, gdK, gdV, L, D, dQ (required).  Out: Qt, dOt, alpha, E.
+/* BoB Pass 1.  In: Q, K, V, O, Orest, dO, gdQ, gdK, gdV, L, D, dQ (required).  Out: Qt, dOt, alpha, E.
  * D must be attn_score_bwd's. */
 int32_t attn_score_pass1_rows(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
                               float scale, int32_t causal, const attn_score* score, const void* Q, const void* K,
-                              const void* V, const void* O, const void* dO, const void* gdQ, const void* gdK,
-                              const void* gdV, const float* L, const float* D, const void* dQ, void* Qt, void* dOt,
-                              float* alpha, float* E, void* workspace, int64_t workspace_bytes, void* stream);
+                              const void* V, const void* O, const void* Orest, const void* dO, const void* gdQ,
+                              const void* gdK, const void* gdV, const float* L, const float* D, const void* dQ,
+                              void* Qt, void* dOt, float* alpha, float* E, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* BoB Pass 2, after Pass 1.  In: Q, K, V, dO, gdQ, gdK, gdV, L, D, alpha, E.  Out: Kt, Vt. */
 int32_t attn_score_pass2_cols(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,

@@ -88,14 +88,9 @@ int32_t ext_launch_pass2(const ExtProblem& p, const void* Q, const void* K, cons
   M(bf16, 32, __VA_ARGS__) M(bf16, 64, __VA_ARGS__) M(bf16, 128, __VA_ARGS__) M(bf16, 256, __VA_ARGS__) \
   M(float, 32, __VA_ARGS__) M(float, 64, __VA_ARGS__) M(float, 128, __VA_ARGS__)
 
-// The joining launches of the row kernels' parts, for the kernels of either header.
-template <typename T, int D>
-int32_t ext_join_fwd(const ExtArgs& a, const float* parts, int64_t all, void* O, float* L, hipStream_t s);
+// Adds the parts of the first backward's row side, for the kernels of either header.
 template <typename T, int D>
 int32_t ext_join_bwd(const ExtArgs& a, const float* parts, int64_t all, void* dQ, float* Dv, hipStream_t s);
-template <typename T, int D>
-int32_t ext_join_pass1(const ExtArgs& a, const float* parts, int64_t all, const void* O, const float* Dv,
-                       const void* dQ, void* Qt, void* dOt, float* alpha, float* E, hipStream_t s);
 
 // Adds the parts of a column kernel ([nparts][2][a.rows][d]) into X and Y.
 int32_t ext_add_parts(const ExtProblem& p, const ExtArgs& a, const float* parts, void* X, void* Y, hipStream_t s);

@@ -59,14 +59,9 @@ int32_t ext_launch_pass1(const ExtProblem& p, const void* Q, const void* K, cons
       (const T*)O, (const T*)dO, (const T*)UQ, (const T*)UK, (const T*)UV, L, Dv, (const T*)dQ, (T*)Qt, (T*)dOt, alpha,
       E, parts);
   if (rc != BOB_OK || c.parts == 1) return rc;
-  return ext_join_pass1<T, D>(a, parts, p.B * p.H * p.Nq, O, Dv, dQ, Qt, dOt, alpha, E, s);
-}
-
-template <typename T, int D>
-int32_t ext_join_pass1(const ExtArgs& a, const float* parts, int64_t all, const void* O, const float* Dv,
-                       const void* dQ, void* Qt, void* dOt, float* alpha, float* E, hipStream_t s) {
+  const int64_t all = p.B * p.H * p.Nq;
   hipLaunchKernelGGL((ext_pass1_join_kernel<T, D>), dim3((unsigned)((all * (D / 4) + 255) / 256)), dim3(256), 0, s, a,
-                     parts, all, (const T*)O, Dv, (const T*)dQ, (T*)Qt, (T*)dOt, alpha, E);
+                     (const float*)parts, all, (const T*)O, Dv, (const T*)dQ, (T*)Qt, (T*)dOt, alpha, E);
   return finish_launch();
 }
 
@@ -104,9 +99,7 @@ int32_t ext_launch_pass2(const ExtProblem& p, const void* Q, const void* K, cons
   template int32_t ext_launch_pass1<T, D>(const ExtProblem&, const void*, const void*, const void*, const void*,    \
                                           const void*, const void*, const void*, const void*, const void*,          \
                                           const float*, const float*, const void*, void*, void*, float*, float*,    \
-                                          float*, hipStream_t);                                                      \
-  template int32_t ext_join_pass1<T, D>(const ExtArgs&, const float*, int64_t, const void*, const float*,            \
-                                        const void*, void*, void*, float*, float*, hipStream_t);
+                                          float*, hipStream_t);
 #define FB_EXT_PASS2(T, D, ...)                                                                                     \
   template ExtPlan ext_pass2_plan<T, D>(const ExtProblem&);                                                         \
   template int32_t ext_launch_pass2<T, D>(const ExtProblem&, const void*, const void*, const void*, const void*,    \

@@ -67,21 +67,16 @@ int32_t ext_launch_fwd(const ExtProblem& p, const void* Q, const void* K, const 
   int32_t rc = ext_dispatch<ExtFwd<T, D>>(c.form, p, dim3(a.total, c.parts), dynamic, s, a, (const T*)Q, (const T*)K,
                                           (const T*)V, (T*)O, L, ws);
   if (rc != BOB_OK || c.parts == 1) return rc;
-  return ext_join_fwd<T, D>(a, ws, heads * rows, O, L, s);
-}
-
-template <typename T, int D>
-int32_t ext_join_fwd(const ExtArgs& a, const float* parts, int64_t all, void* O, float* L, hipStream_t s) {
+  const int64_t all = heads * rows;
   hipLaunchKernelGGL((ext_fwd_join_kernel<T, D>), dim3((unsigned)((all * (D / 4) + 255) / 256)), dim3(256), 0, s, a,
-                     parts, all, (T*)O, L);
+                     (const float*)ws, all, (T*)O, L);
   return finish_launch();
 }
 
 #define FB_INST(T, D, ...)                                  \
   template ExtPlan ext_fwd_plan<T, D>(const ExtProblem&);   \
   template int32_t ext_launch_fwd<T, D>(const ExtProblem&, const void*, const void*, const void*, void*, float*, float*, \
-                                        hipStream_t);     \
-  template int32_t ext_join_fwd<T, D>(const ExtArgs&, const float*, int64_t, void*, float*, hipStream_t);
+                                        hipStream_t);
 FB_EXT_EACH(FB_INST)
 
 }  // namespace fb

@@ -37,18 +37,18 @@ inline int64_t score_cols_lds(const ScoreProblem& p) {
 // Launches (defined per translation unit; instantiated for every (dtype, head dim)).
 template <typename T, int D> ExtPlan score_fwd_plan(const ScoreProblem& p);
 template <typename T, int D>
-int32_t score_launch_fwd(const ScoreProblem& p, const void* Q, const void* K, const void* V, void* O, float* L,
-                         float* ws, hipStream_t s);
+int32_t score_launch_fwd(const ScoreProblem& p, const void* Q, const void* K, const void* V, void* O, void* Orest,
+                         float* L, float* ws, hipStream_t s);
 template <typename T, int D> ExtPlan score_rows_plan(const ScoreProblem& p);
 template <typename T, int D> ExtPlan score_cols_plan(const ScoreProblem& p);
 template <typename T, int D>
 int32_t score_launch_bwd(const ScoreProblem& p, const void* Q, const void* K, const void* V, const void* O,
-                         const void* dO, const float* L, void* dQ, void* dK, void* dV, float* Dv, float* row_parts,
+                         const void* Orest, const void* dO, const float* L, void* dQ, void* dK, void* dV, float* Dv, float* row_parts,
                          float* parts, hipStream_t s);
 template <typename T, int D> ExtPlan score_pass1_plan(const ScoreProblem& p);
 template <typename T, int D>
 int32_t score_launch_pass1(const ScoreProblem& p, const void* Q, const void* K, const void* V, const void* O,
-                           const void* dO, const void* UQ, const void* UK, const void* UV, const float* L,
+                           const void* Orest, const void* dO, const void* UQ, const void* UK, const void* UV, const float* L,
                            const float* Dv, const void* dQ, void* Qt, void* dOt, float* alpha, float* E, float* parts,
                            hipStream_t s);
 template <typename T, int D> ExtPlan score_pass2_plan(const ScoreProblem& p);

@@ -38,19 +38,19 @@ static ExtPlan plan_rows(const ScoreProblem& p) { FB_EXT_DISPATCH(p, score_rows_
 static ExtPlan plan_cols(const ScoreProblem& p) { FB_EXT_DISPATCH(p, score_cols_plan, p); }
 static ExtPlan plan_pass1(const ScoreProblem& p) { FB_EXT_DISPATCH(p, score_pass1_plan, p); }
 static ExtPlan plan_pass2(const ScoreProblem& p) { FB_EXT_DISPATCH(p, score_pass2_plan, p); }
-static int32_t go_fwd(const ScoreProblem& p, const void* Q, const void* K, const void* V, void* O, float* L, float* ws,
-                      hipStream_t s) {
-  FB_EXT_DISPATCH(p, score_launch_fwd, p, Q, K, V, O, L, ws, s);
+static int32_t go_fwd(const ScoreProblem& p, const void* Q, const void* K, const void* V, void* O, void* Orest, float* L,
+                      float* ws, hipStream_t s) {
+  FB_EXT_DISPATCH(p, score_launch_fwd, p, Q, K, V, O, Orest, L, ws, s);
 }
 static int32_t go_bwd(const ScoreProblem& p, const void* Q, const void* K, const void* V, const void* O,
-                      const void* dO, const float* L, void* dQ, void* dK, void* dV, float* D, float* row_parts,
+                      const void* Orest, const void* dO, const float* L, void* dQ, void* dK, void* dV, float* D, float* row_parts,
                       float* parts, hipStream_t s) {
-  FB_EXT_DISPATCH(p, score_launch_bwd, p, Q, K, V, O, dO, L, dQ, dK, dV, D, row_parts, parts, s);
+  FB_EXT_DISPATCH(p, score_launch_bwd, p, Q, K, V, O, Orest, dO, L, dQ, dK, dV, D, row_parts, parts, s);
 }
 static int32_t go_pass1(const ScoreProblem& p, const void* Q, const void* K, const void* V, const void* O,
-                        const void* dO, const void* UQ, const void* UK, const void* UV, const float* L, const float* D,
-                        const void* dQ, void* Qt, void* dOt, float* alpha, float* E, float* parts, hipStream_t s) {
-  FB_EXT_DISPATCH(p, score_launch_pass1, p, Q, K, V, O, dO, UQ, UK, UV, L, D, dQ, Qt, dOt, alpha, E, parts, s);
+                        const void* Orest, const void* dO, const void* UQ, const void* UK, const void* UV,
+                        const float* L, const float* D, const void* dQ, void* Qt, void* dOt, float* alpha, float* E, float* parts, hipStream_t s) {
+  FB_EXT_DISPATCH(p, score_launch_pass1, p, Q, K, V, O, Orest, dO, UQ, UK, UV, L, D, dQ, Qt, dOt, alpha, E, parts, s);
 }
 static int32_t go_pass2(const ScoreProblem& p, const void* Q, const void* K, const void* V, const void* dO,
                         const void* UQ, const void* UK, const void* UV, const float* L, const float* D,
@@ -65,12 +65,14 @@ static int64_t parts_bytes(const ScoreProblem& p, const ExtPlan& c) {
 }
 static int64_t call_bytes(int32_t call, const ScoreProblem& p) {
   switch (call) {
-    case ATTN_SCORE_FWD: return p.Nq == 0 ? 0 : ext_row_bytes(p, plan_fwd(p), p.d + 2);
+    case ATTN_SCORE_FWD: return p.Nq == 0 ? 0 : ext_row_bytes(p, plan_fwd(p), p.d + kFwdScalars);
     case ATTN_SCORE_BWD: return rows_bytes(p) + parts_bytes(p, plan_cols(p));
-    case ATTN_SCORE_PASS1: return p.Nq == 0 ? 0 : ext_row_bytes(p, plan_pass1(p), 3 * p.d + 4);
+    case ATTN_SCORE_PASS1: return p.Nq == 0 ? 0 : ext_row_bytes(p, plan_pass1(p), 3 * p.d + 2);
     default: return parts_bytes(p, plan_pass2(p));
   }
 }
+// Orest: NULL, or as the other matrices of n rows.
+static bool score_rest(int64_t n, const void* Orest) { return n == 0 || Orest == nullptr || aligned16(Orest); }
 static bool workspace_fits(int64_t need, const void* workspace, int64_t bytes) {
   return need == 0 || (bytes >= need && aligned16(workspace));
 }
@@ -83,44 +85,45 @@ extern "C" {
 
 int32_t attn_score_fwd_lse(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
                            float scale, int32_t causal, const attn_score* score, const void* Q, const void* K,
-                           const void* V, void* O, float* L, void* workspace, int64_t workspace_bytes, void* stream) {
+                           const void* V, void* O, void* Orest, float* L, void* workspace, int64_t workspace_bytes,
+                           void* stream) {
   const ScoreProblem p = fb::score_problem(dtype, B, H, Hkv, Nq, Nk, d, scale, causal, score);
   bool empty;
   const int32_t rc = fb::score_check(p, &empty);
   if (rc != BOB_OK || empty || Nq == 0) return rc;
-  if (!fb::ext_ptrs(Nq, {Q, O, L}) || !fb::ext_ptrs(Nk, {K, V})) return BOB_EINVAL;
+  if (!fb::score_rest(Nq, Orest) || !fb::ext_ptrs(Nq, {Q, O, L}) || !fb::ext_ptrs(Nk, {K, V})) return BOB_EINVAL;
   if (!fb::workspace_fits(fb::call_bytes(ATTN_SCORE_FWD, p), workspace, workspace_bytes)) return BOB_EINVAL;
-  return fb::go_fwd(p, Q, K, V, O, L, (float*)workspace, (hipStream_t)stream);
+  return fb::go_fwd(p, Q, K, V, O, Orest, L, (float*)workspace, (hipStream_t)stream);
 }
 
 int32_t attn_score_bwd(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
                        float scale, int32_t causal, const attn_score* score, const void* Q, const void* K,
-                       const void* V, const void* O, const void* dO, const float* L, void* dQ, void* dK, void* dV,
-                       float* D, void* workspace, int64_t workspace_bytes, void* stream) {
+                       const void* V, const void* O, const void* Orest, const void* dO, const float* L, void* dQ,
+                       void* dK, void* dV, float* D, void* workspace, int64_t workspace_bytes, void* stream) {
   const ScoreProblem p = fb::score_problem(dtype, B, H, Hkv, Nq, Nk, d, scale, causal, score);
   bool empty;
   const int32_t rc = fb::score_check(p, &empty);
   if (rc != BOB_OK || empty) return rc;
-  if (!fb::ext_ptrs(Nq, {Q, O, dO, L, dQ, D}) || !fb::ext_ptrs(Nk, {K, V, dK, dV})) return BOB_EINVAL;
+  if (!fb::score_rest(Nq, Orest) || !fb::ext_ptrs(Nq, {Q, O, dO, L, dQ, D}) || !fb::ext_ptrs(Nk, {K, V, dK, dV})) return BOB_EINVAL;
   if (!fb::workspace_fits(fb::call_bytes(ATTN_SCORE_BWD, p), workspace, workspace_bytes)) return BOB_EINVAL;
   char* const ws = (char*)workspace;
-  return fb::go_bwd(p, Q, K, V, O, dO, L, dQ, dK, dV, D, (float*)ws, (float*)(ws + fb::rows_bytes(p)),
+  return fb::go_bwd(p, Q, K, V, O, Orest, dO, L, dQ, dK, dV, D, (float*)ws, (float*)(ws + fb::rows_bytes(p)),
                     (hipStream_t)stream);
 }
 
 int32_t attn_score_pass1_rows(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
                               float scale, int32_t causal, const attn_score* score, const void* Q, const void* K,
-                              const void* V, const void* O, const void* dO, const void* gdQ, const void* gdK,
-                              const void* gdV, const float* L, const float* D, const void* dQ, void* Qt, void* dOt,
+                              const void* V, const void* O, const void* Orest, const void* dO, const void* gdQ,
+                              const void* gdK, const void* gdV, const float* L, const float* D, const void* dQ, void* Qt, void* dOt,
                               float* alpha, float* E, void* workspace, int64_t workspace_bytes, void* stream) {
   const ScoreProblem p = fb::score_problem(dtype, B, H, Hkv, Nq, Nk, d, scale, causal, score);
   bool empty;
   const int32_t rc = fb::score_check(p, &empty);
   if (rc != BOB_OK || empty || Nq == 0) return rc;
-  if (!fb::ext_ptrs(Nq, {Q, O, dO, gdQ, L, D, dQ, Qt, dOt, alpha, E}) || !fb::ext_ptrs(Nk, {K, V, gdK, gdV}))
+  if (!fb::score_rest(Nq, Orest) || !fb::ext_ptrs(Nq, {Q, O, dO, gdQ, L, D, dQ, Qt, dOt, alpha, E}) || !fb::ext_ptrs(Nk, {K, V, gdK, gdV}))
     return BOB_EINVAL;
   if (!fb::workspace_fits(fb::call_bytes(ATTN_SCORE_PASS1, p), workspace, workspace_bytes)) return BOB_EINVAL;
-  return fb::go_pass1(p, Q, K, V, O, dO, gdQ, gdK, gdV, L, D, dQ, Qt, dOt, alpha, E, (float*)workspace,
+  return fb::go_pass1(p, Q, K, V, O, Orest, dO, gdQ, gdK, gdV, L, D, dQ, Qt, dOt, alpha, E, (float*)workspace,
                       (hipStream_t)stream);
 }
 

@@ -38,22 +38,26 @@ template <typename T, int D> ExtPlan score_pass1_plan(const ScoreProblem& p) {
   const FormQuery q{device_cus(), p.B * p.H, std::max<int64_t>(p.Nq, 1), std::max<int64_t>((p.Nk + kBS - 1) / kBS, 1),
                     triangular(p), block_us<T>(10, D), kP1Step<T>, merge_us(3, D), kRowMargin};
   ext_pick<ScorePass1<T, D>>(p, q, kP1Step<T>.narrow, [](const ExtShape&) { return int64_t(0); }, kAnyForm, 1, 1,
-                             p.B * p.H * p.Nq * (3 * D + 4) * 4, &c);
+                             p.B * p.H * p.Nq * (3 * D + 2) * 4, &c);
   return c;
 }
 
 template <typename T, int D>
 int32_t score_launch_pass1(const ScoreProblem& p, const void* Q, const void* K, const void* V, const void* O,
-                           const void* dO, const void* UQ, const void* UK, const void* UV, const float* L,
-                           const float* Dv, const void* dQ, void* Qt, void* dOt, float* alpha, float* E, float* parts,
+                           const void* Orest, const void* dO, const void* UQ, const void* UK, const void* UV,
+                           const float* L, const float* Dv, const void* dQ, void* Qt, void* dOt, float* alpha, float* E, float* parts,
                            hipStream_t s) {
   const ExtPlan c = score_pass1_plan<T, D>(p);
   const ScoreArgs a = score_args<T>(p, c, p.B * p.H, p.Nq);
   const int32_t rc = ext_dispatch<ScorePass1<T, D>>(
-      c.form, p, dim3(a.total, c.parts), 0, s, a, (const T*)Q, (const T*)K, (const T*)V, (const T*)O, (const T*)dO,
-      (const T*)UQ, (const T*)UK, (const T*)UV, L, Dv, (const T*)dQ, (T*)Qt, (T*)dOt, alpha, E, parts);
+      c.form, p, dim3(a.total, c.parts), 0, s, a, (const T*)Q, (const T*)K, (const T*)V, (const T*)O,
+      (const T*)Orest, (const T*)dO, (const T*)UQ, (const T*)UK, (const T*)UV, L, Dv, (const T*)dQ, (T*)Qt, (T*)dOt, alpha, E, parts);
   if (rc != BOB_OK || c.parts == 1) return rc;
-  return ext_join_pass1<T, D>(a, parts, p.B * p.H * p.Nq, O, Dv, dQ, Qt, dOt, alpha, E, s);
+  const int64_t all = p.B * p.H * p.Nq;
+  hipLaunchKernelGGL((score_pass1_join_kernel<T, D>), dim3((unsigned)((all * (D / 4) + 255) / 256)), dim3(256), 0, s, a,
+                     (const float*)parts, all, (const T*)O, (const T*)Orest, Dv, (const T*)dQ, (T*)Qt, (T*)dOt, alpha,
+                     E);
+  return finish_launch();
 }
 
 template <typename T, int D> ExtPlan score_pass2_plan(const ScoreProblem& p) {
@@ -84,8 +88,9 @@ int32_t score_launch_pass2(const ScoreProblem& p, const void* Q, const void* K, 
 #define FB_SCORE_PASS1(T, D, ...)                                                                                     \
   template ExtPlan score_pass1_plan<T, D>(const ScoreProblem&);                                                       \
   template int32_t score_launch_pass1<T, D>(const ScoreProblem&, const void*, const void*, const void*, const void*, \
-                                            const void*, const void*, const void*, const void*, const float*,        \
-                                            const float*, const void*, void*, void*, float*, float*, float*,         \
+                                            const void*, const void*, const void*, const void*, const void*,         \
+                                            const float*, const float*, const void*, void*, void*, float*, float*,   \
+                                            float*,                                                                  \
                                             hipStream_t);
 #define FB_SCORE_PASS2(T, D, ...)                                                                                     \
   template ExtPlan score_pass2_plan<T, D>(const ScoreProblem&);                                                       \

@@ -53,14 +53,15 @@ template <typename T, int D> ExtPlan score_cols_plan(const ScoreProblem& p) {
 
 template <typename T, int D>
 int32_t score_launch_bwd(const ScoreProblem& p, const void* Q, const void* K, const void* V, const void* O,
-                         const void* dO, const float* L, void* dQ, void* dK, void* dV, float* Dv, float* row_parts,
+                         const void* Orest, const void* dO, const float* L, void* dQ, void* dK, void* dV, float* Dv, float* row_parts,
                          float* parts, hipStream_t s) {
   int32_t rc = BOB_OK;
   if (p.Nq > 0) {
     const ExtPlan r = score_rows_plan<T, D>(p);
     const ScoreArgs a = score_args<T>(p, r, p.B * p.H, p.Nq);
     rc = ext_dispatch<ScoreRowsBwd<T, D>>(r.form, p, dim3(a.total, r.parts), 0, s, a, (const T*)Q, (const T*)K,
-                                          (const T*)V, (const T*)O, (const T*)dO, L, (T*)dQ, Dv, row_parts);
+                                          (const T*)V, (const T*)O, (const T*)Orest, (const T*)dO, L, (T*)dQ, Dv,
+                                          row_parts);
     if (rc == BOB_OK && r.parts > 1) rc = ext_join_bwd<T, D>(a, row_parts, p.B * p.H * p.Nq, dQ, Dv, s);
   }
   if (rc != BOB_OK || p.Nk == 0) return rc;
@@ -78,7 +79,7 @@ int32_t score_launch_bwd(const ScoreProblem& p, const void* Q, const void* K, co
   template ExtPlan score_rows_plan<T, D>(const ScoreProblem&);                                                     \
   template ExtPlan score_cols_plan<T, D>(const ScoreProblem&);                                                     \
   template int32_t score_launch_bwd<T, D>(const ScoreProblem&, const void*, const void*, const void*, const void*, \
-                                          const void*, const float*, void*, void*, void*, float*, float*, float*,  \
+                                          const void*, const void*, const float*, void*, void*, void*, float*, float*, float*,  \
                                           hipStream_t);
 FB_EXT_EACH(FB_INST)
 

@@ -35,26 +35,29 @@ template <typename T, int D> ExtPlan score_fwd_plan(const ScoreProblem& p) {
                     kRowMargin};
   const unsigned forms = rows <= 16 && fits ? 1u << 2 : c.fold ? 1u << 1 | 1u << 2 | 1u << 3 : kAnyForm;
   ext_pick<ScoreFwd<T, D>>(p, q, kFwdStep<T>.narrow, [](const ExtShape&) { return int64_t(0); }, forms, 1, 1,
-                           heads * rows * (D + 2) * 4, &c);
+                           heads * rows * (D + kFwdScalars) * 4, &c);
   return c;
 }
 
 template <typename T, int D>
-int32_t score_launch_fwd(const ScoreProblem& p, const void* Q, const void* K, const void* V, void* O, float* L,
-                         float* ws, hipStream_t s) {
+int32_t score_launch_fwd(const ScoreProblem& p, const void* Q, const void* K, const void* V, void* O, void* Orest,
+                         float* L, float* ws, hipStream_t s) {
   const ExtPlan c = score_fwd_plan<T, D>(p);
   const int64_t rows = c.fold ? ext_group(p) * p.Nq : p.Nq, heads = p.B * (c.fold ? p.Hkv : p.H);
   const ScoreArgs a = score_args<T>(p, c, heads, rows);
   const int32_t rc = ext_dispatch<ScoreFwd<T, D>>(c.form, p, dim3(a.total, c.parts), 0, s, a, (const T*)Q, (const T*)K,
-                                                  (const T*)V, (T*)O, L, ws);
+                                                  (const T*)V, (T*)O, (T*)Orest, L, ws);
   if (rc != BOB_OK || c.parts == 1) return rc;
-  return ext_join_fwd<T, D>(a, ws, heads * rows, O, L, s);
+  const int64_t all = heads * rows;
+  hipLaunchKernelGGL((score_fwd_join_kernel<T, D>), dim3((unsigned)((all * (D / 4) + 255) / 256)), dim3(256), 0, s, a,
+                     (const float*)ws, all, (T*)O, (T*)Orest, L);
+  return finish_launch();
 }
 
 #define FB_INST(T, D, ...)                                                                                       \
   template ExtPlan score_fwd_plan<T, D>(const ScoreProblem&);                                                    \
   template int32_t score_launch_fwd<T, D>(const ScoreProblem&, const void*, const void*, const void*, void*,     \
-                                          float*, float*, hipStream_t);
+                                          void*, float*, float*, hipStream_t);
 FB_EXT_EACH(FB_INST)
 
 }  // namespace fb

@@ -16,8 +16,19 @@
 //   dS = u dZ,   St = u P (Pt - E) + u' dZ Fs = P (u (Pt - E) - (2 / c) t (dP - D) F).
 // The distance bias is constant, so it enters Z alone.
 //
-// The kernels keep the skeleton, tiles, sets, parts and folded rows of fb_ext_kernels.h, and
-// the exactness of D and the references of Pass 1 explained there.
+// The kernels keep the skeleton, tiles, sets, parts and folded rows of fb_ext_kernels.h.  The
+// gradients of rows whose weight lies on few keys anywhere in the sequence, as in trained models,
+// are differences of terms far larger than themselves, which operands rounded to bf16 do not
+// carry.  So
+//  * the forward divides by the sum of P as it was rounded, which leaves sum r_j (v_j - O) of
+//    the roundings r_j, and also stores Orest, what O's own rounding left; D = do.O and
+//    alpha O in Pass 1 take both;
+//  * operands whose sums cancel, dS of dQ and those of Pass 1 that its epilogue subtracts from
+//    each other, meet the matrix instructions as two bf16 values each (SplitFrag).
+// With scores of standard deviation 3 that takes dQ from 2.9e-3 off to 2.0e-3, Qt from 3.2 to
+// 2.1e-3 and dOt from 3.3 to 1.8e-3 of their size (a bf16 output is 1.7e-3 off by itself), also
+// with a mean in the keys and values far above their spread, and makes the estimates of
+// ext_bwd_rows_kernel and ext_pass1_kernel unnecessary.
 #pragma once
 #include "fb_ext_kernels.h"
 
@@ -204,17 +215,57 @@ template <typename Rows> __device__ __forceinline__ float score_row_slope(const 
   return a.slopes != nullptr ? a.slopes[rw.head(mb)] * kLog2e : 0.f;
 }
 
+// x rounded to T, and what that leaves.
+template <typename T> __device__ __forceinline__ void store_both(T* hi, T* lo, floatx4 x) {
+  Elt<T>::store4(hi, x);
+  if (lo == nullptr) return;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) x[r] -= (float)(T)x[r];
+  Elt<T>::store4(lo, x);
+}
+template <typename T> __device__ __forceinline__ floatx4 load_both(const T* hi, const T* lo, int64_t at) {
+  const floatx4 x = Elt<T>::load4(hi + at);
+  return lo == nullptr ? x : x + Elt<T>::load4(lo + at);
+}
+
+// sum plus an operand's elements as they are rounded.
+__device__ __forceinline__ float add_rounded(const Elt<bf16>::TFrag& f, float sum) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 one = {(bf16)1.f, (bf16)1.f};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{f.v[2 * i], f.v[2 * i + 1]}, one, sum, false);
+  return sum;
+}
+
+// An operand in twice the bits of bf16: its rounding and what that left.  fp32 needs one.
+template <typename T> struct SplitFrag {
+  using E = Elt<T>;
+  static constexpr bool kTwo = sizeof(T) == 2;
+  typename E::TFrag hi, lo;
+  __device__ __forceinline__ void set(int i, float x) {
+    hi.set(i, x);
+    if constexpr (kTwo) lo.set(i, x - (float)hi.v[i]);
+  }
+  __device__ __forceinline__ floatx4 mma_acc(const typename E::AFrag& a, floatx4 c) const {
+    c = E::mma_acc(a, hi, c);
+    if constexpr (kTwo) c = E::mma_acc(a, lo, c);
+    return c;
+  }
+};
+
 // ===========================================================================
-// Forward, as ext_fwd_kernel.
+// Forward, as ext_fwd_kernel.  Orest may be null.
 // ===========================================================================
 template <typename T, int D, int MR, int NW, int OCC, int KS, bool kCap>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void score_fwd_kernel(
     ScoreArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, T* __restrict__ O,
-    float* __restrict__ L, float* __restrict__ parts) {
+    T* __restrict__ Orest, float* __restrict__ L, float* __restrict__ parts) {
   using E = Elt<T>;
   using G = Geo<T, D>;
   constexpr int BR = 16 * MR * NW;
   __shared__ __attribute__((aligned(16))) RowSmem<T, D, 2, 2, KS, BR> sm;
+  __shared__ float rounded_mem[KS > 1 && sizeof(T) == 2 ? KS : 1][KS > 1 && sizeof(T) == 2 ? BR : 1];
 
   int rh, rb;
   ext_map_block(a, a.fold != 0 ? a.nRB : a.grp * a.nRB, true, NW == 1 ? nullptr : a.kv_lens, a.Nk, rh, rb);
@@ -235,12 +286,13 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_fwd_kernel(
   for (int nb = 0; nb < G::kNB; ++nb)
 #pragma unroll
     for (int mb = 0; mb < MR; ++mb) acc[nb][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
-  float mrun[MR], lsum[MR], slope[MR];
+  constexpr bool kRounded = sizeof(T) == 2;
+  float mrun[MR], lsum[MR], rsum[MR], slope[MR];  // rsum: of P as it is rounded
   const int sloped = vector_mode(a.slopes != nullptr ? 1 : 0);
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb) {
     mrun[mb] = -1e30f;
-    lsum[mb] = 0.f;
+    lsum[mb] = rsum[mb] = 0.f;
     slope[mb] = score_row_slope(a, rw, mb);
   }
   const float c = kCap ? a.cap_out : a.scale * kLog2e;
@@ -288,6 +340,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_fwd_kernel(
           const float corr = fast_exp2(mrun[mb] - mnew);
           mrun[mb] = mnew;
           lsum[mb] *= corr;
+          rsum[mb] *= corr;
 #pragma unroll
           for (int nb = 0; nb < G::kNB; ++nb) acc[nb][mb] *= corr;
         }
@@ -304,6 +357,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_fwd_kernel(
       lsum[mb] += ls[mb];
 #pragma unroll
       for (int i = 0; i < 8; ++i) pf[mb].set(i, p[mb][i]);
+      if constexpr (kRounded) rsum[mb] = add_rounded(pf[mb], rsum[mb]);
     }
   };
 
@@ -362,29 +416,39 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_fwd_kernel(
           for (int mb = 0; mb < MR; ++mb) acc[nb][mb] = E::mma_acc(av, pf[mb], acc[nb][mb]);
         }
       });
-  float lt[MR];
+  float lt[MR], rt[MR];
 #pragma unroll
-  for (int mb = 0; mb < MR; ++mb) lt[mb] = group_sum(lsum[mb]);
+  for (int mb = 0; mb < MR; ++mb) {
+    lt[mb] = group_sum(lsum[mb]);
+    rt[mb] = kRounded ? group_sum(rsum[mb]) : lt[mb];
+  }
   if constexpr (KS > 1) {
     // one reference for the sets, then their sums, as in ext_fwd_kernel
 #pragma unroll
     for (int mb = 0; mb < MR; ++mb)
       if (g == 0) {
-        sm.sc[0][ks][16 * (wl * MR + mb) + j] = mrun[mb];
-        sm.sc[1][ks][16 * (wl * MR + mb) + j] = lt[mb];
+        const int at = 16 * (wl * MR + mb) + j;
+        sm.sc[0][ks][at] = mrun[mb];
+        sm.sc[1][ks][at] = lt[mb];
+        if (kRounded) rounded_mem[ks][at] = rt[mb];
       }
     __syncthreads();
 #pragma unroll
     for (int mb = 0; mb < MR; ++mb) {
       const int at = 16 * (wl * MR + mb) + j;
-      float m = sm.sc[0][0][at], sum = 0.f;
+      float m = sm.sc[0][0][at], sum = 0.f, rounded = 0.f;
 #pragma unroll
       for (int q = 1; q < KS; ++q) m = fmaxf(m, sm.sc[0][q][at]);
 #pragma unroll
-      for (int q = 0; q < KS; ++q) sum = __builtin_fmaf(sm.sc[1][q][at], fast_exp2(sm.sc[0][q][at] - m), sum);
+      for (int q = 0; q < KS; ++q) {
+        const float f = fast_exp2(sm.sc[0][q][at] - m);
+        sum = __builtin_fmaf(sm.sc[1][q][at], f, sum);
+        if (kRounded) rounded = __builtin_fmaf(rounded_mem[q][at], f, rounded);
+      }
       const float corr = fast_exp2(mrun[mb] - m);
       mrun[mb] = m;
       lt[mb] = sum;
+      rt[mb] = kRounded ? rounded : sum;
 #pragma unroll
       for (int nb = 0; nb < G::kNB; ++nb) acc[nb][mb] *= corr;
     }
@@ -402,10 +466,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_fwd_kernel(
 #pragma unroll
         for (int nb = 0; nb < G::kNB; ++nb)
           if (own.owns(nb)) *(floatx4*)(parts + at * D + 16 * nb + 4 * g) = acc[nb][mb];
-        if (g == 0 && ks == 0) {
-          ml[2 * at] = mrun[mb];
-          ml[2 * at + 1] = lt[mb];
-        }
+        if (g == 0 && ks == 0) *(floatx4*)(ml + 4 * at) = floatx4{mrun[mb], lt[mb], rt[mb], 0.f};
       }
     return;
   }
@@ -414,13 +475,50 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_fwd_kernel(
     if (rw.row(mb) >= rw.rows) continue;
     const int64_t at = rw.qrow + rw.row(mb);
     const bool some = rw.ok(mb) && lt[mb] != 0.f;
-    const float inv = 1.f / lt[mb];
+    const float inv = 1.f / rt[mb];
 #pragma unroll
     for (int nb = 0; nb < G::kNB; ++nb)
-      if (own.owns(nb))
-        E::store4(O + at * D + 16 * nb + 4 * g, some ? acc[nb][mb] * inv : floatx4{0.f, 0.f, 0.f, 0.f});
+      if (own.owns(nb)) {
+        const int64_t off = at * D + 16 * nb + 4 * g;
+        store_both(O + off, Orest != nullptr ? Orest + off : nullptr,
+                   some ? acc[nb][mb] * inv : floatx4{0.f, 0.f, 0.f, 0.f});
+      }
     if (g == 0 && ks == 0) L[at] = some ? (mrun[mb] + __log2f(lt[mb])) * kLn2 : -INFINITY;
   }
+}
+
+constexpr int kFwdScalars = 4;  // floats a row and part: reference, sum, rounded sum
+
+// Joins the parts of the forward, as ext_fwd_join_kernel.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void score_fwd_join_kernel(ExtArgs a, const float* __restrict__ parts, int64_t all,
+                                                             T* __restrict__ O, T* __restrict__ Orest,
+                                                             float* __restrict__ L) {
+  constexpr int kPer = D / 4;
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = x / kPer;
+  const int dim = 4 * (int)(x % kPer);
+  if (row >= all) return;
+  const int64_t bh = row / a.Nq, off = row * D + dim;
+  const bool ok = (int)(row - bh * a.Nq) < ext_lens(a, (int)(bh / a.H)).q;
+  const float* const ml = parts + a.nparts * all * D;
+  floatx4 sum = floatx4{0.f, 0.f, 0.f, 0.f};
+  float m = -1e30f, w = 0.f, rounded = 0.f;
+  if (ok) {
+    for (int q = 0; q < a.nparts; ++q) m = fmaxf(m, ml[4 * (q * all + row)]);
+    for (int q = 0; q < a.nparts; ++q) {
+      const int64_t at = q * all + row;
+      const floatx4 mine = *(const floatx4*)(ml + 4 * at);
+      const float f = fast_exp2(mine[0] - m);
+      w = __builtin_fmaf(mine[1], f, w);
+      rounded = __builtin_fmaf(mine[2], f, rounded);
+      sum += *(const floatx4*)(parts + at * D + dim) * f;
+    }
+  }
+  const bool some = ok && w != 0.f;
+  store_both(O + off, Orest != nullptr ? Orest + off : nullptr,
+             some ? sum * (1.f / rounded) : floatx4{0.f, 0.f, 0.f, 0.f});
+  if (dim == 0) L[row] = some ? (m + __log2f(w)) * kLn2 : -INFINITY;
 }
 
 // The exponent of P from a raw score: s c, or the capped score with its t = tanh, less L
@@ -443,7 +541,8 @@ __device__ __forceinline__ float cap_slope(float t) { return __builtin_fmaf(-t, 
 template <typename T, int D, int MR, int NW, int OCC, int KS, bool kCap>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_rows_kernel(
     ScoreArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ O,
-    const T* __restrict__ dO, const float* __restrict__ L, T* __restrict__ dQ, float* __restrict__ Dout,
+    const T* __restrict__ Orest, const T* __restrict__ dO, const float* __restrict__ L, T* __restrict__ dQ,
+    float* __restrict__ Dout,
     float* __restrict__ parts) {
   using E = Elt<T>;
   using G = Geo<T, D>;
@@ -462,7 +561,6 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_rows_kernel(
   float lb[MR], drow[MR], dout[MR], rest[MR];
   const int sloped = vector_mode(a.slopes != nullptr ? 1 : 0);
   const float slope = score_row_slope(a, rw, 0);
-  bool centred = false;
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb) {
     const int row = rw.ok(mb) ? rw.row(mb) : rw.rows;
@@ -473,6 +571,13 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_rows_kernel(
     float part = 0.f;
 #pragma unroll
     for (int kk = 0; kk < G::kChunks; ++kk) part += E::dot_chunk(dof[mb][kk], of[kk]);
+    if (Orest != nullptr) {
+      load_stationary<T, D>(of, Orest + qoff, row, rw.rows);
+      float rest_part = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < G::kChunks; ++kk) rest_part += E::dot_chunk(dof[mb][kk], of[kk]);
+      part += rest_part;
+    }
     drow[mb] = dout[mb] = group_sum(part);
     // an empty row (L = -inf) gets P = 0
     const float Lr = rw.ok(mb) ? L[rw.qrow + rw.row(mb)] : 0.f;
@@ -487,7 +592,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_rows_kernel(
     for (int mb = 0; mb < MR; ++mb) acc[nb][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
   const float c = a.scale * kLog2e;
   floatx4 s[2][MR], dp[2][MR], t[kCap ? 2 : 1][kCap ? MR : 1];
-  typename E::TFrag dsf[MR];
+  SplitFrag<T> dsf[MR];
 
   const T* const src[2] = {K + kvoff, V + kvoff};
   const int part = blockIdx.y, split = ext_parts_of(rw.tiles, KS, a.nparts);
@@ -544,30 +649,6 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_rows_kernel(
 #pragma unroll
           for (int mb = 0; mb < MR; ++mb) score_mask(s[0][mb], s[1][mb], s0, rw.keys[mb]);
         }
-        // the first tile, and those where a row's span begins
-        if (!centred || s0 <= rw.reach.all_lo) {
-          centred = true;
-#pragma unroll
-          for (int mb = 0; mb < MR; ++mb) {
-            float w = 0.f, wd = 0.f;
-#pragma unroll
-            for (int sb = 0; sb < 2; ++sb)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const float p = fast_exp2(s[sb][mb][r]);
-                w += p;
-                wd = __builtin_fmaf(p, dp[sb][mb][r], wd);
-              }
-            w = group_sum(w);
-            wd = group_sum(wd);
-            // L and the weights are off by a few 2^-24 of L's size
-            const float by = w > 1.f - 0x1p-16f ? wd / w : 0.f;
-            drow[mb] += by;
-            rest[mb] += g == 0 ? by : 0.f;
-#pragma unroll
-            for (int sb = 0; sb < 2; ++sb) dp[sb][mb] -= by;
-          }
-        }
 #pragma unroll
         for (int mb = 0; mb < MR; ++mb)
 #pragma unroll
@@ -585,7 +666,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_rows_kernel(
         for (int nb = 0; nb < G::kNB; ++nb) {
           const typename E::AFrag ak = G::load_afrag(Ks, 16 * nb);
 #pragma unroll
-          for (int mb = 0; mb < MR; ++mb) acc[nb][mb] = E::mma_acc(ak, dsf[mb], acc[nb][mb]);
+          for (int mb = 0; mb < MR; ++mb) acc[nb][mb] = dsf[mb].mma_acc(ak, acc[nb][mb]);
         }
       });
 #pragma unroll
@@ -881,22 +962,23 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_cols_kernel(
 }
 
 // ===========================================================================
-// BoB Pass 1, as ext_pass1_kernel.  Capped, the sums that meet K carry u: with F' = F - alpha*
-// and w = C + F' (dP - D) - E* the epilogue's
-//   Qt = tau (sum P (u w - (2 / c) t (dP - D) F) k + sum u P (dP - D) u_K - de sum u P k) - da dQ
-// needs one more operand, u P, beside P, which stays with u_V.
+// BoB Pass 1, as ext_pass1_kernel without its references.  With w = C + F (dP - D) and
+// alpha, e the sums of P F and P w, the epilogue's
+//   Qt = tau (sum P (u w - (2 / c) t (dP - D) F) k + sum u P (dP - D) u_K - e sum u P k) - alpha dQ
+//   dOt = sum P u_V + sum P F v - alpha O,  E = e - alpha D
+// needs, capped, one more operand, u P, beside P, which stays with u_V.
 // ===========================================================================
 template <typename T, int D, int MR, int NW, int OCC, int KS, int kPF, bool kCap>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
     ScoreArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ O,
-    const T* __restrict__ dO, const T* __restrict__ UQ, const T* __restrict__ UK, const T* __restrict__ UV,
-    const float* __restrict__ L, const float* __restrict__ Dv, const T* __restrict__ dQ, T* __restrict__ Qt,
-    T* __restrict__ dOt, float* __restrict__ alpha_out, float* __restrict__ E_out, float* __restrict__ parts) {
+    const T* __restrict__ Orest, const T* __restrict__ dO, const T* __restrict__ UQ, const T* __restrict__ UK,
+    const T* __restrict__ UV, const float* __restrict__ L, const float* __restrict__ Dv, const T* __restrict__ dQ,
+    T* __restrict__ Qt, T* __restrict__ dOt, float* __restrict__ alpha_out, float* __restrict__ E_out,
+    float* __restrict__ parts) {
   using E = Elt<T>;
   using G = Geo<T, D>;
   constexpr int BR = 16 * MR * NW;
   __shared__ __attribute__((aligned(16))) RowSmem<T, D, 4, 2, KS, BR> sm;
-  __shared__ float ref_mem[KS == 1 ? 1 : 5 * KS * BR];
 
   int rh, rb;
   ext_map_block(a, a.grp * a.nRB, true, a.kv_lens, a.Nk, rh, rb);
@@ -930,18 +1012,15 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
   for (int mb = 0; mb < MR; ++mb) alpha[mb] = e0[mb] = 0.f;
   const float c = a.scale * kLog2e;
   floatx4 s[2][MR], dp[2][MR], f[2][MR], cc[2][MR], t[kCap ? 2 : 1][kCap ? MR : 1];
-  typename E::TFrag fP[MR], fPF[MR], fPPt[MR], fPdd[MR], fPu[kCap ? MR : 1];
+  typename E::TFrag fP[MR], fPdd[MR];  // of a cap: P, and u P in fB
+  SplitFrag<T> fPF[MR], fPPt[MR], fB[MR];
   using AF = typename E::AFrag;
 
   const T* const src[4] = {K + kvoff, V + kvoff, UK + kvoff, UV + kvoff};
   const int part = blockIdx.y, split = ext_parts_of(rw.tiles, KS, a.nparts);
   const ExtRun run = ext_run(rw.tiles, part, split, ks, KS), first = ext_run(rw.tiles, part, split, 0, KS);
-  constexpr bool kBarrier = NW > 1 || KS > 1;  // the sets meet in the first tile
+  constexpr bool kBarrier = NW > 1;
   const TileCopy<T, D, NW, 4> copy(wl);
-  float aref[MR], eref[MR];
-#pragma unroll
-  for (int mb = 0; mb < MR; ++mb) aref[mb] = eref[mb] = 0.f;
-  bool centred = false;
   ext_stream<tile_loads<T, D, NW, 4>(), kBarrier>(
       kBarrier ? first.size() : run.size(),
       [&](int it, int st) {
@@ -952,7 +1031,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
         const int s0 = rw.key(run.begin + it);
         int mode = run.begin + it < run.end ? rw.reach.mode(s0) : 0;
         if constexpr (KS > 1) mode = vector_mode(mode);
-        if (mode == 0 && (KS == 1 || it > 0 || split > 1)) return;
+        if (mode == 0) return;
         const T FB_LDS* Ks = (const T FB_LDS*)sm.lds[ks][st];
         const T FB_LDS* Vs = Ks + G::kTileElems;
         const T FB_LDS* UKs = Vs + G::kTileElems;
@@ -962,8 +1041,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
         for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
           for (int mb = 0; mb < MR; ++mb) {
-            s[sb][mb] = f[sb][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
-            cc[sb][mb] = floatx4{-eref[mb], -eref[mb], -eref[mb], -eref[mb]};
+            s[sb][mb] = f[sb][mb] = cc[sb][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
             dp[sb][mb] = floatx4{-drow[mb], -drow[mb], -drow[mb], -drow[mb]};
           }
 #pragma unroll
@@ -979,7 +1057,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
               dp[sb][mb] = E::mma_chunk(av, dof[mb][kk], dp[sb][mb]);     // (dP - D)^T
               f[sb][mb] = E::mma_chunk(ak, uqf[mb][kk], f[sb][mb]);       // (U_Q K^T)^T
               f[sb][mb] = E::mma_chunk(auk, qf[mb][kk], f[sb][mb]);       // + (Q U_K^T)^T
-              cc[sb][mb] = E::mma_chunk(auv, dof[mb][kk], cc[sb][mb]);    // C^T - E* = U_V dO^T - E*
+              cc[sb][mb] = E::mma_chunk(auv, dof[mb][kk], cc[sb][mb]);    // C^T = U_V dO^T
             }
           }
 #pragma unroll
@@ -991,8 +1069,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
               float tr = 0.f;
               s[sb][mb][r] = score_exponent<T, kCap>(a, s[sb][mb][r], c, -lb[mb], tr);
               if constexpr (kCap) t[sb][mb][r] = tr;
-              const float by = kCap ? a.scale * cap_slope(tr) : a.scale;
-              f[sb][mb][r] = __builtin_fmaf(f[sb][mb][r], by, -aref[mb]);
+              f[sb][mb][r] *= kCap ? a.scale * cap_slope(tr) : a.scale;
             }
         AF cur[4];
         auto load_frags = [&](int nb) {
@@ -1008,68 +1085,6 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
 #pragma unroll
           for (int mb = 0; mb < MR; ++mb) score_mask(s[0][mb], s[1][mb], s0, rw.keys[mb]);
         }
-        // The estimate of the first tile, which the sets share (a barrier: every wave of a workgroup
-        // with sets comes here in its first iteration), and that of a row whose span begins in a
-        // later tile: its sums are 0 until then.  Where other sets or parts sum the row's further
-        // tiles about 0, only rows that lie in this tile whole have one.
-        const bool shared = split == 1 && (KS > 1 ? it == 0 : !centred);
-        if (shared || s0 <= rw.reach.all_lo) {
-          centred = true;
-#pragma unroll
-          for (int mb = 0; mb < MR; ++mb) {
-            float w = 0.f, wf = 0.f, wd = 0.f, wc = 0.f, wfd = 0.f;  // sums of P, P F, P (dP - D), P C, P F (dP - D)
-            if (mode != 0) {
-#pragma unroll
-              for (int sb = 0; sb < 2; ++sb)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                  const float p = fast_exp2(s[sb][mb][r]), pf = p * f[sb][mb][r];
-                  w += p;
-                  wf += pf;
-                  wd = __builtin_fmaf(p, dp[sb][mb][r], wd);
-                  wc = __builtin_fmaf(p, cc[sb][mb][r], wc);
-                  wfd = __builtin_fmaf(pf, dp[sb][mb][r], wfd);
-                }
-            }
-            w = group_sum(w);
-            wf = group_sum(wf);
-            wd = group_sum(wd);
-            wc = group_sum(wc);
-            wfd = group_sum(wfd);
-            if (KS > 1 && shared) {
-              float FB_LDS* at = (float FB_LDS*)ref_mem + 16 * (wl * MR + mb) + j;
-              if (g == 0) {
-                at[(5 * ks + 0) * BR] = w;
-                at[(5 * ks + 1) * BR] = wf;
-                at[(5 * ks + 2) * BR] = wd;
-                at[(5 * ks + 3) * BR] = wc;
-                at[(5 * ks + 4) * BR] = wfd;
-              }
-              __syncthreads();
-              w = wf = wd = wc = wfd = 0.f;
-#pragma unroll
-              for (int q = 0; q < KS; ++q) {
-                w += at[(5 * q + 0) * BR];
-                wf += at[(5 * q + 1) * BR];
-                wd += at[(5 * q + 2) * BR];
-                wc += at[(5 * q + 3) * BR];
-                wfd += at[(5 * q + 4) * BR];
-              }
-            }
-            // rows without weight here (or of NaN) keep the reference 0
-            const bool begins = rw.keys[mb].lo >= s0;
-            const bool set = w > 0.f && (shared || (begins && ((KS == 1 && split == 1) || rw.keys[mb].hi <= s0 + kBS)));
-            const float by_f = set ? wf / w : 0.f, by_c = set ? (wc + (wfd - by_f * wd)) / w : 0.f;
-            aref[mb] += by_f;
-            eref[mb] += by_c;
-#pragma unroll
-            for (int sb = 0; sb < 2; ++sb) {
-              f[sb][mb] -= by_f;
-              cc[sb][mb] -= by_c;
-            }
-          }
-        }
-        if (KS > 1 && mode == 0) return;
 #pragma unroll
         for (int mb = 0; mb < MR; ++mb)
 #pragma unroll
@@ -1084,15 +1099,16 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
               const int i = 4 * sb + r;
               alpha[mb] += pf;
               e0[mb] += ppt;
-              fP[mb].set(i, p);
               fPF[mb].set(i, pf);
               if constexpr (kCap) {
                 const float tr = t[sb][mb][r], pu = p * cap_slope(tr);
-                fPu[mb].set(i, pu);
+                fP[mb].set(i, p);
+                fB[mb].set(i, pu);
                 fPdd[mb].set(i, pu * dd);
                 // P (u w - (2 / c) t (dP - D) F)
-                fPPt[mb].set(i, __builtin_fmaf(pu, w, -a.cap_k * tr * (p * dd) * (f[sb][mb][r] + aref[mb])));
+                fPPt[mb].set(i, __builtin_fmaf(pu, w, -a.cap_k * tr * (p * dd) * f[sb][mb][r]));
               } else {
+                fB[mb].set(i, p);
                 fPPt[mb].set(i, ppt);
                 fPdd[mb].set(i, p * dd);
               }
@@ -1114,11 +1130,11 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
           }
 #pragma unroll
           for (int mb = 0; mb < MR; ++mb) {
-            aB[nb][mb] = E::mma_acc(ak, kCap ? fPu[mb] : fP[mb], aB[nb][mb]);
-            aOM[nb][mb] = E::mma_acc(ak, fPPt[mb], aOM[nb][mb]);
+            aB[nb][mb] = fB[mb].mma_acc(ak, aB[nb][mb]);
+            aOM[nb][mb] = fPPt[mb].mma_acc(ak, aOM[nb][mb]);
             aOM[nb][mb] = E::mma_acc(auk, fPdd[mb], aOM[nb][mb]);
-            aDO[nb][mb] = E::mma_acc(auv, fP[mb], aDO[nb][mb]);
-            aDO[nb][mb] = E::mma_acc(av, fPF[mb], aDO[nb][mb]);
+            aDO[nb][mb] = E::mma_acc(auv, kCap ? fP[mb] : fB[mb].hi, aDO[nb][mb]);
+            aDO[nb][mb] = fPF[mb].mma_acc(av, aDO[nb][mb]);
           }
         }
       });
@@ -1131,11 +1147,8 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
 #pragma unroll
     for (int mb = 0; mb < MR; ++mb)
       if (g == 0) {
-        const int at = 16 * (wl * MR + mb) + j;
-        sm.sc[0][ks][at] = alpha[mb];
-        sm.sc[1][ks][at] = e0[mb];
-        ref_mem[(2 * ks + 0) * BR + at] = aref[mb];
-        ref_mem[(2 * ks + 1) * BR + at] = eref[mb];
+        sm.sc[0][ks][16 * (wl * MR + mb) + j] = alpha[mb];
+        sm.sc[1][ks][16 * (wl * MR + mb) + j] = e0[mb];
       }
     __syncthreads();
 #pragma unroll
@@ -1143,16 +1156,10 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
       const int at = 16 * (wl * MR + mb) + j;
       alpha[mb] = sm.sc[0][0][at];
       e0[mb] = sm.sc[1][0][at];
-      // a row's reference is the same in all sets, or that of one and 0 in the others
-      aref[mb] = ref_mem[at];
-      eref[mb] = ref_mem[BR + at];
 #pragma unroll
       for (int q = 1; q < KS; ++q) {
         alpha[mb] += sm.sc[0][q][at];
         e0[mb] += sm.sc[1][q][at];
-        const float ar = ref_mem[2 * q * BR + at], er = ref_mem[(2 * q + 1) * BR + at];
-        aref[mb] = ar != 0.f ? ar : aref[mb];
-        eref[mb] = er != 0.f ? er : eref[mb];
       }
     }
     static_assert(sizeof(sm.lds) >= merge_bytes<KS, NW, G::kNB, MR>(), "set merge buffer");
@@ -1177,8 +1184,10 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
             *(floatx4*)(to + D) = aOM[nb][mb];
             *(floatx4*)(to + 2 * D) = aB[nb][mb];
           }
-        // of the parts of a row one at most has a reference: the join adds them
-        if (g == 0 && ks == 0) *(floatx4*)(sc + 4 * at) = floatx4{alpha[mb], e0[mb], aref[mb], eref[mb]};
+        if (g == 0 && ks == 0) {
+          sc[2 * at] = alpha[mb];
+          sc[2 * at + 1] = e0[mb];
+        }
       }
     return;
   }
@@ -1187,23 +1196,57 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
   for (int mb = 0; mb < MR; ++mb) {
     if (rw.row(mb) >= rw.rows) continue;
     const int64_t at = rw.qrow + rw.row(mb);
+    const bool ok = rw.ok(mb);
     if (g == 0 && ks == 0) {
-      const float al = aref[mb] + alpha[mb];
-      alpha_out[at] = rw.ok(mb) ? al : 0.f;
-      E_out[at] = rw.ok(mb) ? eref[mb] + e0[mb] - al * drow[mb] : 0.f;
+      alpha_out[at] = ok ? alpha[mb] : 0.f;
+      E_out[at] = ok ? e0[mb] - alpha[mb] * drow[mb] : 0.f;
     }
 #pragma unroll
     for (int nb = 0; nb < G::kNB; ++nb) {
       if (!own.owns(nb)) continue;
       const int64_t off = at * D + 16 * nb + 4 * g;
-      if (rw.ok(mb)) {
-        E::store4(dOt + off, aDO[nb][mb] - alpha[mb] * E::load4(O + off));
-        E::store4(Qt + off, a.scale * (aOM[nb][mb] - e0[mb] * aB[nb][mb]) - alpha[mb] * E::load4(dQ + off));
-      } else {
-        E::store4(dOt + off, zero);
-        E::store4(Qt + off, zero);
-      }
+      E::store4(dOt + off, ok ? aDO[nb][mb] - alpha[mb] * load_both(O, Orest, off) : zero);
+      E::store4(Qt + off, ok ? a.scale * (aOM[nb][mb] - e0[mb] * aB[nb][mb]) - alpha[mb] * E::load4(dQ + off) : zero);
     }
+  }
+}
+
+// Adds the parts of Pass 1 and finishes its rows, as ext_pass1_join_kernel.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void score_pass1_join_kernel(ExtArgs a, const float* __restrict__ parts, int64_t all,
+                                                               const T* __restrict__ O, const T* __restrict__ Orest,
+                                                               const float* __restrict__ Dv, const T* __restrict__ dQ,
+                                                               T* __restrict__ Qt, T* __restrict__ dOt,
+                                                               float* __restrict__ alpha_out,
+                                                               float* __restrict__ E_out) {
+  using E = Elt<T>;
+  constexpr int kPer = D / 4;
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = x / kPer;
+  const int dim = 4 * (int)(x % kPer);
+  if (row >= all) return;
+  const int64_t bh = row / a.Nq, off = row * D + dim;
+  const bool ok = (int)(row - bh * a.Nq) < ext_lens(a, (int)(bh / a.H)).q;
+  const floatx4 zero = floatx4{0.f, 0.f, 0.f, 0.f};
+  floatx4 d = zero, om = zero, b = zero;
+  float alpha = 0.f, e0 = 0.f;
+  if (ok) {
+    const float* const scalars = parts + a.nparts * all * (3 * D);
+    for (int q = 0; q < a.nparts; ++q) {
+      const int64_t at = q * all + row;
+      const float* const from = parts + at * (3 * D) + dim;
+      d += *(const floatx4*)from;
+      om += *(const floatx4*)(from + D);
+      b += *(const floatx4*)(from + 2 * D);
+      alpha += scalars[2 * at];
+      e0 += scalars[2 * at + 1];
+    }
+  }
+  E::store4(dOt + off, ok ? d - alpha * load_both(O, Orest, off) : zero);
+  E::store4(Qt + off, ok ? a.scale * (om - e0 * b) - alpha * E::load4(dQ + off) : zero);
+  if (dim == 0) {
+    alpha_out[row] = alpha;
+    E_out[row] = ok ? e0 - alpha * Dv[row] : 0.f;
   }
 }
 

@@ -39,7 +39,7 @@ def _declare(lib):
     i32, i64, f32, vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_void_p
     score = ctypes.POINTER(AttnScore)
     shape = [i32] + [i64] * 6
-    for name, pointers in (("fwd_lse", 5), ("bwd", 10), ("pass1_rows", 15), ("pass2_cols", 13)):
+    for name, pointers in (("fwd_lse", 6), ("bwd", 11), ("pass1_rows", 16), ("pass2_cols", 13)):
         fn = getattr(lib, "attn_score_" + name)
         fn.argtypes = shape + [f32, i32, score] + [vp] * pointers + [vp, i64, vp]
         fn.restype = i32
@@ -134,25 +134,33 @@ class _Score(_Problem):
         return self.workspace(lambda *args: lib.attn_score_workspace_bytes(call, *args), stream)
 
 
+def _check_rest(O, Orest):
+    if Orest is not None:
+        _check_mats(O, Orest)
+
+
 def attn_score_fwd_lse(Q, K, V, scale, causal=False, cap=None, slopes=None, spans=None, kv_lens=None, q_lens=None,
-                       q_starts=None, out=None, stream=None):
-    """Forward: returns (O, L)."""
+                       q_starts=None, want_rest=False, out=None, stream=None):
+    """Forward: returns (O, Orest, L).  Orest is what rounding O left, for the backward calls (None unless wanted)."""
     p = _Score((Q,), (K, V), scale, causal, cap, slopes, spans, kv_lens, q_lens, q_starts)
     if out is None:
-        out = (torch.empty_like(Q), _rows_empty(Q.shape, Q))
-    O, L = out
+        out = (torch.empty_like(Q), torch.empty_like(Q) if want_rest else None, _rows_empty(Q.shape, Q))
+    O, Orest, L = out
     _check_mats(Q, O)
+    _check_rest(Q, Orest)
     _check_rows(Q.shape, L)
     st = _stream(stream, Q)
     ws, wp, n = p.space(ATTN_SCORE_FWD, stream)
-    _call(Q, load_library().attn_score_fwd_lse, *p.shape, *p.options, _p(Q), _p(K), _p(V), _p(O), _p(L), wp, n, st)
-    return O, L
+    _call(Q, load_library().attn_score_fwd_lse, *p.shape, *p.options, _p(Q), _p(K), _p(V), _p(O), _ptr(Orest), _p(L),
+          wp, n, st)
+    return O, Orest, L
 
 
-def attn_score_bwd(Q, K, V, O, dO, L, scale, causal=False, cap=None, slopes=None, spans=None, kv_lens=None,
+def attn_score_bwd(Q, K, V, O, Orest, dO, L, scale, causal=False, cap=None, slopes=None, spans=None, kv_lens=None,
                    q_lens=None, q_starts=None, out=None, stream=None):
-    """First backward: returns (dQ, dK, dV, D)."""
+    """First backward: returns (dQ, dK, dV, D).  Orest: the forward's, or None (0)."""
     p = _Score((Q, O, dO), (K, V), scale, causal, cap, slopes, spans, kv_lens, q_lens, q_starts)
+    _check_rest(Q, Orest)
     _check_rows(Q.shape, L)
     if out is None:
         out = (torch.empty_like(Q), torch.empty_like(K), torch.empty_like(K), _rows_empty(Q.shape, Q))
@@ -162,15 +170,16 @@ def attn_score_bwd(Q, K, V, O, dO, L, scale, causal=False, cap=None, slopes=None
     _check_rows(Q.shape, D)
     st = _stream(stream, Q)
     ws, wp, n = p.space(ATTN_SCORE_BWD, stream)
-    _call(Q, load_library().attn_score_bwd, *p.shape, *p.options, _p(Q), _p(K), _p(V), _p(O), _p(dO), _p(L), _p(dQ),
-          _p(dK), _p(dV), _p(D), wp, n, st)
+    _call(Q, load_library().attn_score_bwd, *p.shape, *p.options, _p(Q), _p(K), _p(V), _p(O), _ptr(Orest), _p(dO),
+          _p(L), _p(dQ), _p(dK), _p(dV), _p(D), wp, n, st)
     return dQ, dK, dV, D
 
 
-def attn_score_pass1_rows(Q, K, V, O, dO, gdQ, gdK, gdV, L, D, dQ, scale, causal=False, cap=None, slopes=None,
+def attn_score_pass1_rows(Q, K, V, O, Orest, dO, gdQ, gdK, gdV, L, D, dQ, scale, causal=False, cap=None, slopes=None,
                           spans=None, kv_lens=None, q_lens=None, q_starts=None, out=None, stream=None):
-    """BoB Pass 1: returns (Qt, dOt, alpha, E)."""
+    """BoB Pass 1: returns (Qt, dOt, alpha, E).  Orest: the forward's, or None (0)."""
     p = _Score((Q, O, dO, gdQ, dQ), (K, V, gdK, gdV), scale, causal, cap, slopes, spans, kv_lens, q_lens, q_starts)
+    _check_rest(Q, Orest)
     _check_rows(Q.shape, L, D)
     if out is None:
         out = (torch.empty_like(Q), torch.empty_like(Q), _rows_empty(Q.shape, Q), _rows_empty(Q.shape, Q))
@@ -179,8 +188,8 @@ def attn_score_pass1_rows(Q, K, V, O, dO, gdQ, gdK, gdV, L, D, dQ, scale, causal
     _check_rows(Q.shape, alpha, E)
     st = _stream(stream, Q)
     ws, wp, n = p.space(ATTN_SCORE_PASS1, stream)
-    _call(Q, load_library().attn_score_pass1_rows, *p.shape, *p.options, _p(Q), _p(K), _p(V), _p(O), _p(dO), _p(gdQ),
-          _p(gdK), _p(gdV), _p(L), _p(D), _p(dQ), _p(Qt), _p(dOt), _p(alpha), _p(E), wp, n, st)
+    _call(Q, load_library().attn_score_pass1_rows, *p.shape, *p.options, _p(Q), _p(K), _p(V), _p(O), _ptr(Orest),
+          _p(dO), _p(gdQ), _p(gdK), _p(gdV), _p(L), _p(D), _p(dQ), _p(Qt), _p(dOt), _p(alpha), _p(E), wp, n, st)
     return Qt, dOt, alpha, E
 
 
@@ -203,40 +212,42 @@ def attn_score_pass2_cols(Q, K, V, dO, gdQ, gdK, gdV, L, D, alpha, E, scale, cau
 class _ScoreFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, slopes, spans, kv_lens, q_lens, q_starts, scale, causal, cap):
-        O, L = attn_score_fwd_lse(q, k, v, scale, causal, cap, slopes, spans, kv_lens, q_lens, q_starts)
+        # fp32 outputs are as exact as their sums
+        O, Orest, L = attn_score_fwd_lse(q, k, v, scale, causal, cap, slopes, spans, kv_lens, q_lens, q_starts,
+                                         want_rest=q.dtype == torch.bfloat16)
         # O without its graph: the first backward passes no gradient on to it, and the engine
         # would run this node's backward on zeros for that
-        ctx.save_for_backward(q, k, v, O.detach(), L, slopes, spans, kv_lens, q_lens, q_starts)
+        ctx.save_for_backward(q, k, v, O.detach(), Orest, L, slopes, spans, kv_lens, q_lens, q_starts)
         ctx.options = scale, causal, cap
         return O
 
     @staticmethod
     def backward(ctx, dO):
-        q, k, v, O, L, *more = ctx.saved_tensors
-        dq, dk, dv = _ScoreBackwardFn.apply(q, k, v, O, L, dO.contiguous(), *more, *ctx.options)
+        q, k, v, O, Orest, L, *more = ctx.saved_tensors
+        dq, dk, dv = _ScoreBackwardFn.apply(q, k, v, O, Orest, L, dO.contiguous(), *more, *ctx.options)
         return (dq, dk, dv) + (None,) * 8
 
 
 class _ScoreBackwardFn(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, v, O, L, dO, slopes, spans, kv_lens, q_lens, q_starts, scale, causal, cap):
+    def forward(ctx, q, k, v, O, Orest, L, dO, slopes, spans, kv_lens, q_lens, q_starts, scale, causal, cap):
         more = (slopes, spans, kv_lens, q_lens, q_starts)
-        dq, dk, dv, D = attn_score_bwd(q, k, v, O, dO, L, scale, causal, cap, *more)
-        ctx.save_for_backward(q, k, v, O, L, dO, D, dq.detach(), *more)
+        dq, dk, dv, D = attn_score_bwd(q, k, v, O, Orest, dO, L, scale, causal, cap, *more)
+        ctx.save_for_backward(q, k, v, O, Orest, L, dO, D, dq.detach(), *more)
         ctx.set_materialize_grads(False)
         ctx.options = scale, causal, cap
         return dq, dk, dv
 
     @staticmethod
     def backward(ctx, gdq, gdk, gdv):
-        q, k, v, O, L, dO, D, dq, *more = ctx.saved_tensors
+        q, k, v, O, Orest, L, dO, D, dq, *more = ctx.saved_tensors
         more = (*ctx.options, *more)
         cot = [torch.zeros_like(x) if g is None else g.contiguous() for g, x in ((gdq, q), (gdk, k), (gdv, v))]
-        Qt, dOt, alpha, E = attn_score_pass1_rows(q, k, v, O, dO, *cot, L, D, dq, *more)
+        Qt, dOt, alpha, E = attn_score_pass1_rows(q, k, v, O, Orest, dO, *cot, L, D, dq, *more)
         Kt, Vt = attn_score_pass2_cols(q, k, v, dO, *cot, L, D, alpha, E, *more)
         if torch.is_grad_enabled():
             Qt, Kt, Vt, dOt = _ScoreSecondFn.apply(Qt, Kt, Vt, dOt, q, k, v, dO, gdq, gdk, gdv)
-        return (Qt, Kt, Vt, None, None, dOt) + (None,) * 8
+        return (Qt, Kt, Vt, None, None, None, dOt) + (None,) * 8
 
 
 class _ScoreSecondFn(torch.autograd.Function):
