@@ -272,5 +272,11 @@ def scored_attention(q, k, v, scale=None, causal=False, cap=None, slopes=None, s
     values lie in a cache of kv_lens rows.  scale defaults to 1/sqrt(d)."""
     if scale is None:
         scale = q.shape[-1] ** -0.5
+    if not torch.compiler.is_compiling() and (cap is None or cap):
+        # the same functions in C++ (csrc/torch_binding.cpp); None for calls it does not take
+        O = _fast().scored_attention(q, k, v, float(scale), bool(causal), float(cap or 0), slopes, spans, kv_lens, q_lens,
+                                     q_starts)
+        if O is not None:
+            return O
     _Score((q,), (k, v), scale, causal, cap, slopes, spans, kv_lens, q_lens, q_starts)
     return _ScoreFn.apply(q, k, v, slopes, spans, kv_lens, q_lens, q_starts, float(scale), bool(causal), cap)

@@ -178,3 +178,306 @@ def test_layers_equal_the_calls(name):
     again = chain(xd, c)  # no atomics: the same bits twice
     for n, t in want.items():
         assert torch.equal(again[n], t), n
+
+
+def in_python(t, xd, c):
+    """The layer's functions without the native ones."""
+    from paper_2609_24089_amd import rotary
+    more, il = (xd["positions"], xd["freqs"], xd["axes"]), c.get("interleaved", False)
+    if "wq" not in t and "wk" not in t:
+        return rotary._RotateFn.apply(t["q"], t["k"], *more, il, False, (False, False))
+    return rotary._RotaryFn.apply(t["q"], t["k"], t.get("wq"), t.get("wk"), *more, 1e-6, il)
+
+
+@pytest.mark.parametrize("name", ["d64_half", "f32_d64", "no_norm", "keys_normed", "axes_3", "packed"])
+def test_native_and_python_functions_agree(name):
+    """Bit for bit; the first gradients with and without a graph, in the inputs' order of heads and tokens."""
+    import paper_2609_24089_amd as fb
+    c = CASES[name]
+    xd = placed(make(c, 24), c)
+    names = [n for n in ("q", "k", "wq", "wk") if n in xd]
+    runs = []
+    for fn in (in_python, None):
+        for graph in (False, True):
+            t = {n: xd[n].detach().requires_grad_(True) for n in names}
+            y = in_python(t, xd, c) if fn else fb.rotate_heads(
+                t["q"], t["k"], xd["positions"], (xd["freqs"], xd["axes"]), t.get("wq"), t.get("wk"),
+                interleaved=c.get("interleaved", False))
+            up = [xd[n].clone().requires_grad_(True) for n in ("gq", "gk")]
+            g = torch.autograd.grad(y, list(t.values()), up, create_graph=graph)
+            for a, n in zip(g, ("q", "k")):
+                assert (a.stride(1) < a.stride(2)) == (xd[n].stride(1) < xd[n].stride(2)), n
+            h = torch.autograd.grad(g, up + list(t.values()), [xd["u" + n] for n in names],
+                                    allow_unused=True) if graph else ()
+            runs.append((*y, *g, *h))
+    for run in runs[1:]:
+        for a, b in zip(run, runs[1]):
+            assert (a is None) == (b is None) and (a is None or torch.equal(a, b))
+    for a, b in zip(runs[0], runs[1]):
+        assert torch.equal(a, b)
+
+
+def test_no_norm_derivatives_of_any_order():
+    """The rotation is linear: its third derivative in the upstream gradient is itself again."""
+    import paper_2609_24089_amd as fb
+    c = CASES["no_norm"]
+    xd = placed(make(c, 25), c)
+    for layer in (lambda t: fb.rotate_heads(t["q"], t["k"], xd["positions"], (xd["freqs"], xd["axes"])),
+                  lambda t: in_python(t, xd, c)):
+        t = {n: xd[n].detach().requires_grad_(True) for n in ("q", "k")}
+        up = [xd[n].clone().requires_grad_(True) for n in ("gq", "gk")]
+        y = layer(t)
+        g = torch.autograd.grad(y, list(t.values()), up, create_graph=True)
+        u = [xd[n].clone().requires_grad_(True) for n in ("uq", "uk")]
+        h = torch.autograd.grad(g, up, u, create_graph=True)
+        third = torch.autograd.grad(h, u, [xd["gq"], xd["gk"]])
+        for a, b in zip(third, g):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_third_derivatives_of_norms_are_refused(native):
+    import paper_2609_24089_amd as fb
+    c = CASES["d128"]
+    xd = placed(make(c, 26), c)
+    t = {n: xd[n].detach().requires_grad_(True) for n in ("q", "k", "wq", "wk")}
+    y = fb.rotate_heads(t["q"], t["k"], xd["positions"], (xd["freqs"], xd["axes"]), t["wq"], t["wk"]) if native else \
+        in_python(t, xd, c)
+    leaves = list(t.values())
+    g = torch.autograd.grad(y, leaves, [xd["gq"], xd["gk"]], create_graph=True)
+    h = torch.autograd.grad(g, leaves, [xd[n] for n in ("uq", "uk", "uwq", "uwk")], create_graph=True)
+    for a in h:
+        with pytest.raises(NotImplementedError, match="third derivatives"):
+            torch.autograd.grad(a.float().square().sum(), leaves, retain_graph=True, allow_unused=True)
+
+
+def test_partial_gradients():
+    """Frozen weights, a frozen input, and an upstream gradient for the queries alone."""
+    import paper_2609_24089_amd as fb
+    c = CASES["d64_half"]
+    xd = placed(make(c, 27), c)
+    want = chain(xd, c)
+    q = xd["q"].detach().requires_grad_(True)
+    w = xd["wk"].clone().requires_grad_(True)
+    rot = (xd["freqs"], xd["axes"])
+    y = fb.rotate_heads(q, xd["k"], xd["positions"], rot, xd["wq"], xd["wk"])
+    (g,) = torch.autograd.grad(y, q, [xd["gq"], xd["gk"]])
+    assert torch.equal(g, want["dq"])
+    y = fb.rotate_heads(xd["q"], xd["k"], xd["positions"], rot, xd["wq"], w)
+    (g,) = torch.autograd.grad(y[1], w, xd["gk"])
+    assert torch.equal(g, want["dwk"])
+    y = fb.rotate_heads(q, xd["k"], xd["positions"], rot, xd["wq"], w)
+    (g,) = torch.autograd.grad(y[0], q, xd["gq"], create_graph=True)
+    (h,) = torch.autograd.grad(g, q, xd["uq"])
+    alone = fb.attn_rotary_bwd2(xd["q"], xd["k"], xd["gq"], torch.zeros_like(xd["gk"]), xd["uq"], None,
+                                **options(xd, c))[0]
+    assert torch.equal(h, alone)
+    # an upstream gradient that is one number everywhere (strides of 0)
+    y = fb.rotate_heads(q, xd["k"], xd["positions"], rot, xd["wq"], w)
+    (a,) = torch.autograd.grad(y[0].sum(), q)
+    (b,) = torch.autograd.grad(fb.rotate_heads(q, xd["k"], xd["positions"], rot, xd["wq"], w)[0], q,
+                               torch.ones_like(xd["gq"]))
+    assert torch.equal(a, b)
+
+
+def test_into_a_cache():
+    """The keys go straight to the slots of a cache, and nothing else of it changes."""
+    import paper_2609_24089_amd as fb
+    c = CASES["tokens"]
+    xd = placed(make(c, 28), c)
+    cache = torch.full((c["B"], c["Hkv"], 50, c["d"]), 7.0, dtype=torch.bfloat16, device="cuda")
+    q = torch.empty(c["B"], c["H"], 1, c["d"], dtype=torch.bfloat16, device="cuda")
+    fb.attn_rotary_fwd(xd["q"], xd["k"], out=(q, cache[:, :, 33:34]), **options(xd, c))
+    want = chain(xd, c)
+    assert torch.equal(cache[:, :, 33:34], want["k"]) and torch.equal(q, want["q"])
+    cache[:, :, 33] = 7.0
+    assert (cache == 7.0).all()
+    # over their own input, on a stream of the caller's
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    mine = [xd[n].clone(memory_format=torch.preserve_format) for n in ("q", "k")]
+    torch.cuda.synchronize()
+    fb.attn_rotary_fwd(*mine, out=mine, stream=s, **options(xd, c))
+    s.synchronize()
+    assert torch.equal(mine[0], want["q"]) and torch.equal(mine[1], want["k"])
+
+
+def test_gradient_against_differences():
+    """fp32 against central differences in float64 sums, steps of 2^-7: the third-order term is below 1e-3 of the
+    slope."""
+    import paper_2609_24089_amd as fb
+    c = dict(B=1, H=2, Hkv=2, N=30, d=32, dtype="f32")
+    xd = placed(make(c, 29), c)
+    got = chain(xd, c)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    for n, other in (("q", "dq"), ("wq", "dwq"), ("k", "dk")):
+        u = torch.randn(xd[n].shape, generator=gen, device="cuda")
+        ends = []
+        for step in (2.0 ** -7, -2.0 ** -7):
+            y = {**xd, n: xd[n] + step * u}
+            r = fb.attn_rotary_fwd(y["q"], y["k"], **options(y, c))
+            ends.append(sum(float((a.double() * xd[g].double()).sum()) for a, g in zip(r, ("gq", "gk"))))
+        slope, exact = (ends[0] - ends[1]) * 2.0 ** 6, float((got[other].double() * u.double()).sum())
+        assert abs(slope - exact) <= 2e-3 * max(1.0, abs(exact)), n
+
+
+def test_empty_problems():
+    import paper_2609_24089_amd as fb
+    for B, N, H, Hkv in ((0, 5, 2, 1), (2, 0, 2, 1), (2, 3, 0, 0)):
+        c = dict(B=B, H=H, Hkv=Hkv, N=N, d=64)
+        got = chain(placed(make(c, 30), c), c)
+        for n, t in got.items():
+            assert not t.any(), n
+        assert got["dwq"].shape == (64,)
+
+
+def test_offsets_past_32_bits():
+    """More than 2^31 elements of queries: the last tokens equal the same ones alone."""
+    import paper_2609_24089_amd as fb
+    B, N, H, d = 5, 60000, 60, 128
+    assert B * N * H * d > 2 ** 31
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    q = torch.empty(B, N, H, d, dtype=torch.bfloat16, device="cuda").normal_(generator=gen).transpose(1, 2)
+    k = torch.empty(B, N, 1, d, dtype=torch.bfloat16, device="cuda").normal_(generator=gen).transpose(1, 2)
+    w = torch.rand(d, device="cuda") + 0.5
+    pos = torch.arange(N, dtype=torch.int32, device="cuda").expand(B, N).contiguous()
+    rot = fb.rotary_frequencies(d, device="cuda")
+    y = fb.rotate_heads(q, k, pos, rot, w, w)
+    tail = fb.rotate_heads(q[-1:, :, -9:], k[-1:, :, -9:], pos[-1:, -9:].contiguous(), rot, w, w)
+    assert torch.equal(y[0][-1:, :, -9:], tail[0]) and torch.equal(y[1][-1:, :, -9:], tail[1])
+
+
+def test_captured_and_replayed():
+    """A training step captured and replayed on changing inputs, with eager work between; equal bit for bit."""
+    import paper_2609_24089_amd as fb
+    c = CASES["d128"]
+    xd = placed(make(c, 31), c)
+    names = ("q", "k", "wq", "wk")
+    leaves = [xd[n].detach().requires_grad_(True) for n in names]
+
+    def train():
+        y = fb.rotate_heads(leaves[0], leaves[1], xd["positions"], (xd["freqs"], xd["axes"]), leaves[2], leaves[3])
+        return (*y, *torch.autograd.grad(y, leaves, [xd["gq"], xd["gk"]]))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        train()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = train()
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    for _ in range(4):
+        with torch.no_grad():
+            for t in (*leaves, xd["gq"]):
+                t.copy_(torch.randn(t.shape, generator=gen, device="cuda"))
+            xd["positions"].add_(7)
+        graph.replay()
+        want = train()
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b)
+
+
+def test_refusals_of_the_layer():
+    import paper_2609_24089_amd as fb
+    q = torch.zeros(2, 4, 5, 64, device="cuda", dtype=torch.bfloat16)
+    k = torch.zeros(2, 2, 5, 64, device="cuda", dtype=torch.bfloat16)
+    pos, rot = torch.zeros(2, 5, device="cuda", dtype=torch.int32), fb.rotary_frequencies(64, device="cuda")
+    w = torch.ones(64, device="cuda")
+    good = dict(q=q, k=k, positions=pos, rotary=rot, q_weight=w, k_weight=w)
+    fb.rotate_heads(**good)
+    for bad in (dict(k=k[:, :, :4]), dict(k=k.float()), dict(q=q[..., :48], k=k[..., :48]), dict(positions=pos.long()),
+                dict(positions=pos[:, :4]), dict(positions=pos.cpu()), dict(positions=torch.stack([pos, pos]), rotary=(rot[0], None)),
+                dict(rotary=(rot[0].float(), rot[1])), dict(rotary=(rot[0][:12], None)), dict(rotary=(rot[0], rot[1][:8])),
+                dict(rotary=fb.rotary_frequencies(128, device="cuda")), dict(q_weight=w[:32]), dict(q_weight=w.cpu()),
+                dict(eps=-1.0), dict(q=q.cpu(), k=k.cpu())):
+        with pytest.raises((ValueError, TypeError)):
+            fb.rotate_heads(**{**good, **bad})
+    for bad in (dict(q_weight=w.half(), k_weight=w.half()), dict(k_weight=w.bfloat16()), dict(q=q.half(), k=k.half())):
+        with pytest.raises(TypeError):
+            fb.rotate_heads(**{**good, **bad})
+    # outputs that overlap themselves or are not aligned; copies on another stream
+    with pytest.raises(ValueError):
+        fb.attn_rotary_fwd(q, k, pos, *rot, out=(q[:, :1].expand(2, 4, 5, 64), k))
+    odd = torch.zeros(2 * 4 * 5 * 64 + 1, device="cuda", dtype=torch.bfloat16)[1:].view(2, 4, 5, 64)
+    with pytest.raises(ValueError):
+        fb.attn_rotary_fwd(q, k, pos, *rot, out=(odd, torch.empty_like(k)))
+    with pytest.raises(ValueError, match="stream"):
+        fb.attn_rotary_fwd(odd, k, pos, *rot, stream=torch.cuda.Stream())
+    with pytest.raises(ValueError):
+        fb.attn_rotary_fwd(q, k, pos, *rot, q_weight=w, inverse=True)
+
+
+def test_a_layer_from_projections_to_output():
+    """The operators as a model uses them: packed documents, a projection, normalised and rotated heads, capped
+    attention with a distance bias, a loss, its gradients and a Hessian-vector product, in fp32 against torch operations
+    in float64; and the last token again through a cache."""
+    import paper_2609_24089_amd as fb
+    torch.manual_seed(0)
+    B, N, H, Hkv, d, cap = 2, 75, 4, 2, 32, 4.0
+    width = 48
+    ids = torch.tensor([[0] * 30 + [1] * 45, [0] * 10 + [1] * 1 + [2] * 50 + [-1] * 14], dtype=torch.int32, device="cuda")
+    spans = fb.attention_spans(B, N, ids, prefix_lens=torch.tensor([5, 0], dtype=torch.int32, device="cuda"))
+    first = torch.stack([torch.searchsorted(r, r) for r in torch.where(ids < 0, 9, ids)])
+    pos = (torch.arange(N, device="cuda") - first).to(torch.int32)
+    rot = fb.rotary_frequencies(d, device="cuda")
+    slopes = torch.tensor([0.5, 0.25, 0.1, 0.0], device="cuda")
+    x = torch.randn(B, N, width, device="cuda")
+    p = [(torch.randn(width, (H + 2 * Hkv) * d, device="cuda") / 7).requires_grad_(True),
+         (1 + 0.2 * torch.randn(d, device="cuda")).requires_grad_(True),
+         (1 + 0.2 * torch.randn(d, device="cuda")).requires_grad_(True),
+         (torch.randn(H * d, width, device="cuda") / 12).requires_grad_(True)]
+
+    def model(w, wq, wk, wo):
+        heads = (x @ w).unflatten(2, (H + 2 * Hkv, d)).transpose(1, 2)
+        q, k, v = heads[:, :H], heads[:, H:H + Hkv], heads[:, H + Hkv:]
+        o = fb.rotary_attention(q, k, v, pos, rot, wq, wk, cap=cap, slopes=slopes, spans=spans)
+        return o.transpose(1, 2).flatten(2) @ wo
+
+    keep = (ids >= 0)[:, :, None]
+    y = model(*p)
+    loss = ((y * keep) ** 2).sum() / 100
+    g = torch.autograd.grad(loss, p, create_graph=True)
+    dirs = [torch.randn_like(t) for t in p]
+    hv = torch.autograd.grad(sum((a * b).sum() for a, b in zip(g, dirs)), p)
+
+    def plain(w, wq, wk, wo):
+        heads = (x.double() @ w).unflatten(2, (H + 2 * Hkv, d)).transpose(1, 2)
+        angle = pos.double()[:, None, :, None] * rot[0]
+
+        def made(t, weight):
+            t = t / torch.sqrt(t.square().mean(-1, keepdim=True) + 1e-6) * weight
+            a, b = t.chunk(2, -1)
+            return torch.cat([a * angle.cos() - b * angle.sin(), a * angle.sin() + b * angle.cos()], -1)
+
+        q, k = made(heads[:, :H], wq), made(heads[:, H:H + Hkv], wk).repeat_interleave(H // Hkv, 1)
+        v = heads[:, H + Hkv:].repeat_interleave(H // Hkv, 1)
+        at = torch.arange(N, device="cuda")
+        s = spans.long()
+        ok = (at >= s[:, :, 0, None]) & (at < s[:, :, 1, None])
+        z = cap * torch.tanh(q @ k.transpose(-1, -2) * d ** -0.5 / cap)
+        z = z - slopes.double()[:, None, None] * (at[:, None] - at).abs()
+        z = torch.where(ok.any(-1)[:, None, :, None], z.masked_fill(~ok[:, None], float("-inf")), 0.0)
+        o = torch.softmax(z, -1) * ok.any(-1)[:, None, :, None] @ v
+        return o.transpose(1, 2).flatten(2) @ wo
+
+    wide = [t.detach().double().requires_grad_(True) for t in p]
+    y64 = plain(*wide)
+    g64 = torch.autograd.grad(((y64 * keep) ** 2).sum() / 100, wide, create_graph=True)
+    hv64 = torch.autograd.grad(sum((a * b.double()).sum() for a, b in zip(g64, dirs)), wide)
+    # the fp32 model rounds each of its ten products and sums at 2^-24 of terms that cancel by at most a hundred: 1e-4
+    errs = [float((a.double() - b).norm() / b.norm()) for a, b in zip((y * keep, *g, *hv), (y64 * keep, *g64, *hv64))]
+    say("   output, gradients and products", [f"{e:.0e}" for e in errs])
+    assert max(errs) <= 1e-4
+    # the last token of entry 0, from a cache: no documents' first keys but its own document's
+    with torch.no_grad():
+        heads = (x @ p[0]).unflatten(2, (H + 2 * Hkv, d)).transpose(1, 2)
+        q, k = fb.rotate_heads(heads[:, :H], heads[:, H:H + Hkv], pos, rot, p[1], p[2])
+        last = torch.full((B,), N - 1, dtype=torch.int32, device="cuda")
+        o = fb.scored_attention(q[:, :, -1:].contiguous(), k, heads[:, H + Hkv:].contiguous(), cap=cap, slopes=slopes,
+                                spans=spans, q_starts=last)
+        one = o.transpose(1, 2).flatten(2) @ p[3]
+        assert nrel(one[0, 0].double().cpu().numpy(), y[0, -1].detach().double().cpu().numpy()) <= 2e-5
+        assert not o[1].any()  # padding
