@@ -16,8 +16,8 @@
 // layout (strides of batch entry, head and token), so the way from a projection's [B,N,heads,d]
 // to an attention's [B,heads,N,d] is part of it.  d / 16 lanes share a vector: a lane holds
 // eight pairs, whose halves are two runs of eight elements (neighbours paired: one run of 16), so
-// it loads 16 bytes at a time and a rotation needs no other lane.  A lane keeps its token and
-// goes through heads, for which the cosines and sines are made once.
+// it loads 16 bytes at a time and a rotation needs no other lane.  A workgroup makes the cosines
+// and sines of its tokens once for all heads of the queries or keys.
 #include "fb_ext.h"
 
 namespace fb {
@@ -30,7 +30,7 @@ struct Heads {
 
 struct RotaryArgs {
   int B, N, H[2];         // H: heads of the queries, of the keys
-  int chunk, chunks[2];   // heads a workgroup goes through; workgroups that cover the heads
+  int tokens;             // a workgroup takes at a time: a power of two up to kMaxTokens
   int pairs, num_axes;
   const int32_t* positions;  // [num_axes, B, N]
   const double* freqs;       // [pairs]: radians a position
@@ -41,10 +41,10 @@ struct RotaryArgs {
   float eps, sign;           // of the angles: -1 rotates back
   // x; y (forward) or dx; dy; u; x~; dy~
   Heads x[2], out[2], dy[2], u[2], xt[2], dyt[2];
-  float* sums;               // [chunks of both][gridDim.x][d]: sums of dw or wt, or null
+  float* sums;               // [2][gridDim.x][d]: sums of dw or wt, or null
 };
 
-constexpr int kRotaryThreads = 256;
+constexpr int kRotaryThreads = 256, kMaxTokens = 16;
 constexpr double kTurns = 0.15915494309189535;  // 1 / (2 pi)
 
 // Sum over the d / 16 lanes (a power of two up to 16) that share a vector: all of them get it.
@@ -171,14 +171,88 @@ template <int LPV> __device__ __forceinline__ float dot(const Pairs& x, const Pa
   return vector_sum<LPV>(s);
 }
 
-// kMode 0: y (or, with sign -1 and no weights, x from y); 1: dx, dw; 2: x~, dy~, w~.
+// The cosines and sines of the workgroup's tokens: four floats between tokens keep the lanes of
+// different tokens on different banks.
+template <int D> struct AngleMem {
+  static constexpr int kStride = D / 2 + 4;
+  float cs[2][kMaxTokens][kStride];
+};
+
+// One vector's work; kMode 0: y (or, with sign -1 and no weights, x from y); 1: dx, dw; 2: x~, dy~, w~.
+template <typename T, int D, int kMode, bool kNeighbours>
+__device__ __forceinline__ void rotary_vector(const RotaryArgs& a, int k, int64_t b, int h, int64_t n,
+                                              const LanePairs& l, const Pairs& cs, bool norm, const Pairs& w,
+                                              const Pairs& uw, Pairs& sum) {
+  constexpr int LPV = D / 16;
+  auto at = [&](const Heads& v) { return (T*)v.data + b * v.b + h * v.h + n * v.n; };
+  if constexpr (kMode == 0) {
+    Pairs x = load_pairs<T, kNeighbours>(at(a.x[k]), l);
+    if (norm) {
+      const float r = rsqrtf(dot<LPV>(x, x) * (1.f / D) + a.eps);
+      x = each([&](auto of) { return of(x) * r * of(w); });
+    }
+    store_pairs<T, kNeighbours>(at(a.out[k]), l, turn(x, cs, 1.f));
+  } else if constexpr (kMode == 1) {
+    Pairs g = load_pairs<T, kNeighbours>(at(a.dy[k]), l);
+    if (!norm) {
+      store_pairs<T, kNeighbours>(at(a.out[k]), l, turn(g, cs, -1.f));
+      return;
+    }
+    Pairs x = load_pairs<T, kNeighbours>(at(a.x[k]), l);
+    g = turn(g, cs, -1.f);
+    const float r = rsqrtf(dot<LPV>(x, x) * (1.f / D) + a.eps);
+    x = each([&](auto of) { return of(x) * r; });
+    const Pairs aw = each([&](auto of) { return of(w) * of(g); });
+    const float B = dot<LPV>(aw, x) * (1.f / D);
+    sum = each([&](auto of) { return __builtin_fmaf(of(g), of(x), of(sum)); });
+    store_pairs<T, kNeighbours>(at(a.out[k]), l,
+                                each([&](auto of) { return r * __builtin_fmaf(-B, of(x), of(aw)); }));
+  } else {
+    Pairs u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u.a[i] = u.b[i] = 0.f;
+    if (a.u[k].data != nullptr) u = load_pairs<T, kNeighbours>(at(a.u[k]), l);
+    if (!norm) {
+      store_pairs<T, kNeighbours>(at(a.dyt[k]), l, turn(u, cs, 1.f));
+      return;
+    }
+    Pairs g = load_pairs<T, kNeighbours>(at(a.dy[k]), l);
+    Pairs x = load_pairs<T, kNeighbours>(at(a.x[k]), l);
+    g = turn(g, cs, -1.f);
+    const float r = rsqrtf(dot<LPV>(x, x) * (1.f / D) + a.eps);
+    x = each([&](auto of) { return of(x) * r; });
+    const Pairs aw = each([&](auto of) { return of(w) * of(g); });
+    const Pairs ug = each([&](auto of) { return of(uw) * of(g); });
+    const float A = dot<LPV>(aw, u) * (1.f / D), B = dot<LPV>(aw, x) * (1.f / D);
+    const float C = dot<LPV>(u, x) * (1.f / D), S = dot<LPV>(ug, x) * (1.f / D);
+    const float by_x = __builtin_fmaf(3.f * r, B * C, -__builtin_fmaf(r, A, S));
+    sum = each([&](auto of) { return __builtin_fmaf(r * of(g), __builtin_fmaf(-C, of(x), of(u)), of(sum)); });
+    store_pairs<T, kNeighbours>(at(a.xt[k]), l, each([&](auto of) {
+                                  const float m = __builtin_fmaf(C, of(aw), B * of(u));
+                                  return r * (of(ug) + __builtin_fmaf(by_x, of(x), -r * m));
+                                }));
+    const Pairs gt = each([&](auto of) {
+      return __builtin_fmaf(r * of(w), __builtin_fmaf(-C, of(x), of(u)), of(uw) * of(x));
+    });
+    store_pairs<T, kNeighbours>(at(a.dyt[k]), l, turn(gt, cs, 1.f));
+  }
+}
+
+// A workgroup takes a.tokens tokens at a time, for which it makes the angles once, and shares the
+// heads of each out over 256 / (d / 16) / tokens slots of d / 16 lanes.
 template <typename T, int D, int kMode, bool kNeighbours>
 __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a) {
   constexpr int LPV = D / 16, kSlots = kRotaryThreads / LPV;
+  __shared__ union Mem {
+    AngleMem<D> angles;
+    float rows[kMode == 0 ? 1 : kSlots][D];
+  } mem;
   const int slot = threadIdx.x / LPV, p = threadIdx.x % LPV;
-  const int k = (int)blockIdx.y < a.chunks[0] ? 0 : 1;  // queries or keys
-  const int h0 = ((int)blockIdx.y - (k == 0 ? 0 : a.chunks[0])) * a.chunk, h1 = min(h0 + a.chunk, a.H[k]);
+  const int token = slot % a.tokens, hs = slot / a.tokens, head_slots = kSlots / a.tokens;
   const LanePairs l = lane_pairs<kNeighbours>(p, a.pairs);
+  const int64_t tokens = (int64_t)a.B * a.N;
+  // blockIdx.y: the queries' heads, then the keys'
+  const int k = blockIdx.y;
   const bool norm = a.w[k] != nullptr;
   Pairs w, uw, sum;
 #pragma unroll
@@ -187,121 +261,76 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a) {
     w = load_weight<kNeighbours>(a.w[k], a.w_bf16, l);
     if (kMode == 2 && a.uw[k] != nullptr) uw = load_weight<kNeighbours>(a.uw[k], a.w_bf16, l);
   }
-  const int64_t tokens = (int64_t)a.B * a.N;
-  for (int64_t t0 = (int64_t)blockIdx.x * kSlots; t0 < tokens; t0 += (int64_t)gridDim.x * kSlots) {
-    const int64_t t = min(t0 + slot, tokens - 1);
-    const bool live = t0 + slot < tokens;
-    const int64_t b = t / a.N, n = t - b * a.N;
-    Pairs cs;  // cosines and sines
+  for (int64_t t0 = (int64_t)blockIdx.x * a.tokens; t0 < tokens; t0 += (int64_t)gridDim.x * a.tokens) {
+    for (int x = threadIdx.x; x < a.tokens * a.pairs; x += kRotaryThreads) {
+      const int tk = x / a.pairs, pair = x - tk * a.pairs;
+      const int axis = a.axes != nullptr ? min(max(a.axes[pair], 0), a.num_axes - 1) : 0;
+      // the angle in turns, without its whole ones, in 64 bits: far positions keep their fraction
+      const double turns = a.freqs[pair] * kTurns * (double)a.positions[(int64_t)axis * tokens + min(t0 + tk, tokens - 1)];
+      float s, c;
+      sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
+      mem.angles.cs[0][tk][pair] = c;
+      mem.angles.cs[1][tk][pair] = a.sign * s;
+    }
+    __syncthreads();
+    Pairs cs;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      cs.a[i] = 1.f;
-      cs.b[i] = 0.f;
-      if (l.turned) {
-        // the angle in turns, without its whole ones, in 64 bits: far positions keep their fraction
-        const int axis = a.axes != nullptr ? min(max(a.axes[l.pair + i], 0), a.num_axes - 1) : 0;
-        const double turns = a.freqs[l.pair + i] * kTurns * (double)a.positions[(int64_t)axis * tokens + t];
-        sincospif(2.f * (float)(turns - rint(turns)), &cs.b[i], &cs.a[i]);
-        cs.b[i] *= a.sign;
-      }
+      cs.a[i] = l.turned ? mem.angles.cs[0][token][l.pair + i] : 1.f;
+      cs.b[i] = l.turned ? mem.angles.cs[1][token][l.pair + i] : 0.f;
     }
-    auto at = [&](const Heads& v, int h) { return (T*)v.data + b * v.b + h * v.h + n * v.n; };
-    for (int h = h0; h < h1; ++h) {
-      if constexpr (kMode == 0) {
-        Pairs x = load_pairs<T, kNeighbours>(at(a.x[k], h), l);
-        if (norm) {
-          const float r = rsqrtf(dot<LPV>(x, x) * (1.f / D) + a.eps);
-          x = each([&](auto of) { return of(x) * r * of(w); });
-        }
-        if (live) store_pairs<T, kNeighbours>(at(a.out[k], h), l, turn(x, cs, 1.f));
-      } else if constexpr (kMode == 1) {
-        const Pairs g = turn(load_pairs<T, kNeighbours>(at(a.dy[k], h), l), cs, -1.f);
-        if (!norm) {
-          if (live) store_pairs<T, kNeighbours>(at(a.out[k], h), l, g);
-          continue;
-        }
-        Pairs x = load_pairs<T, kNeighbours>(at(a.x[k], h), l);
-        const float r = rsqrtf(dot<LPV>(x, x) * (1.f / D) + a.eps);
-        x = each([&](auto of) { return of(x) * r; });
-        const Pairs aw = each([&](auto of) { return of(w) * of(g); });
-        const float B = dot<LPV>(aw, x) * (1.f / D);
-        if (live) {
-          sum = each([&](auto of) { return __builtin_fmaf(of(g), of(x), of(sum)); });
-          store_pairs<T, kNeighbours>(at(a.out[k], h), l,
-                                      each([&](auto of) { return r * __builtin_fmaf(-B, of(x), of(aw)); }));
-        }
-      } else {
-        Pairs u;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) u.a[i] = u.b[i] = 0.f;
-        if (a.u[k].data != nullptr) u = load_pairs<T, kNeighbours>(at(a.u[k], h), l);
-        if (!norm) {
-          if (live) store_pairs<T, kNeighbours>(at(a.dyt[k], h), l, turn(u, cs, 1.f));
-          continue;
-        }
-        const Pairs g = turn(load_pairs<T, kNeighbours>(at(a.dy[k], h), l), cs, -1.f);
-        Pairs x = load_pairs<T, kNeighbours>(at(a.x[k], h), l);
-        const float r = rsqrtf(dot<LPV>(x, x) * (1.f / D) + a.eps);
-        x = each([&](auto of) { return of(x) * r; });
-        const Pairs aw = each([&](auto of) { return of(w) * of(g); });
-        const Pairs ug = each([&](auto of) { return of(uw) * of(g); });
-        const float A = dot<LPV>(aw, u) * (1.f / D), B = dot<LPV>(aw, x) * (1.f / D);
-        const float C = dot<LPV>(u, x) * (1.f / D), S = dot<LPV>(ug, x) * (1.f / D);
-        const float by_x = __builtin_fmaf(3.f * r, B * C, -__builtin_fmaf(r, A, S));
-        if (live) {
-          sum = each([&](auto of) { return __builtin_fmaf(r * of(g), __builtin_fmaf(-C, of(x), of(u)), of(sum)); });
-          store_pairs<T, kNeighbours>(at(a.xt[k], h), l, each([&](auto of) {
-                                        const float m = __builtin_fmaf(C, of(aw), B * of(u));
-                                        return r * (of(ug) + __builtin_fmaf(by_x, of(x), -r * m));
-                                      }));
-          const Pairs gt = each([&](auto of) {
-            return __builtin_fmaf(r * of(w), __builtin_fmaf(-C, of(x), of(u)), of(uw) * of(x));
-          });
-          store_pairs<T, kNeighbours>(at(a.dyt[k], h), l, turn(gt, cs, 1.f));
-        }
-      }
+    __syncthreads();
+    const int64_t t = t0 + token;
+    if (t < tokens) {
+      const int64_t b = t / a.N, n = t - b * a.N;
+      for (int h = hs; h < a.H[k]; h += head_slots)
+        rotary_vector<T, D, kMode, kNeighbours>(a, k, b, h, n, l, cs, norm, w, uw, sum);
     }
   }
   if constexpr (kMode != 0) {
     if (a.sums == nullptr || !norm) return;
     // the workgroup's sums in one row
-    __shared__ float rows[kSlots][D];
     Pairs e = kNeighbours ? to_neighbours(sum) : sum;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      rows[slot][l.a + i] = e.a[i];
-      rows[slot][l.b + i] = e.b[i];
+      mem.rows[slot][l.a + i] = e.a[i];
+      mem.rows[slot][l.b + i] = e.b[i];
     }
     __syncthreads();
     float* const to = a.sums + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * D;
     for (int x = threadIdx.x; x < D; x += kRotaryThreads) {
       float v = 0.f;
 #pragma unroll
-      for (int s = 0; s < kSlots; ++s) v += rows[s][x];
+      for (int s = 0; s < kSlots; ++s) v += mem.rows[s][x];
       to[x] = v;
     }
   }
 }
 
 // Adds the workgroups' rows of sums: 16 columns of the queries' (blockIdx.y 0) or keys' weight a
-// workgroup, 16 threads a column.
-__global__ __launch_bounds__(256) void rotary_sums_kernel(const float* __restrict__ sums, int d, int64_t rows_q,
-                                                          int64_t rows_k, void* out_q, void* out_k, int w_bf16) {
-  __shared__ float part[16][17];
+// workgroup, 64 threads a column with eight loads in flight each, for all of it is latency
+// (1024 rows: 16 threads a column 14 us).
+constexpr int kSumThreads = 1024;
+__global__ __launch_bounds__(kSumThreads) void rotary_sums_kernel(const float* __restrict__ sums, int d, int rows,
+                                                                  void* out_q, void* out_k, int w_bf16) {
+  __shared__ float part[64][17];
   void* const out = blockIdx.y == 0 ? out_q : out_k;
   if (out == nullptr) return;
-  const int64_t first = blockIdx.y == 0 ? 0 : rows_q, n = blockIdx.y == 0 ? rows_q : rows_k;
   const int x = threadIdx.x & 15, y = threadIdx.x >> 4, col = blockIdx.x * 16 + x;
-  float v[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int64_t r = y; r < n; r += 64)
+  const float* const from = sums + (int64_t)blockIdx.y * rows * d + col;
+  float v[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (r + 16 * i < n) v[i] += sums[(first + r + 16 * i) * d + col];
-  part[y][x] = (v[0] + v[1]) + (v[2] + v[3]);
+  for (int i = 0; i < 8; ++i) v[i] = 0.f;
+  for (int r = y; r < rows; r += 512)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (r + 64 * i < rows) v[i] += from[(int64_t)(r + 64 * i) * d];
+  part[y][x] = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
   __syncthreads();
   if (threadIdx.x < 16) {
     float s = 0.f;
-    for (int i = 0; i < 16; ++i) s += part[i][threadIdx.x];
+#pragma unroll
+    for (int i = 0; i < 64; ++i) s += part[i][threadIdx.x];
     const int at = blockIdx.x * 16 + threadIdx.x;
     if (w_bf16 != 0)
       ((bf16*)out)[at] = (bf16)s;
@@ -342,41 +371,33 @@ static int32_t rotary_check(const RotaryProblem& p, bool* empty) {
     if (!aligned(p.r.positions, 4) || !aligned(p.r.freqs, 8) || !aligned(p.r.axes, 4)) return BOB_EINVAL;
     if (p.r.num_axes > 1 && p.r.axes == nullptr) return BOB_EINVAL;
   }
-  // a launch has one block a group of tokens and fewer than 2^16 chunks of heads
   if (p.N > kMaxN || p.B > INT32_MAX || p.B * p.N > (int64_t(1) << 31) || p.H > 65535 || p.Hkv > 65535 ||
       p.H + p.Hkv > 65535)
     return BOB_EINVAL;
   return BOB_OK;
 }
 
-// How a launch runs: groups of tokens, heads a workgroup.
+// How a launch runs: tokens a workgroup takes at a time, workgroups for the queries and as many
+// for the keys.
 struct RotaryPlan {
+  int tokens;
   int64_t groups;
-  int chunk, chunks[2];
-  int64_t rows(int k) const { return groups * chunks[k]; }
 };
-// As many workgroups as keep the device's memory busy (kEnough), then more heads a workgroup, for
-// which the angles are made once.  Calls that sum a weight's gradient have about kMaxSums
-// rows of sums; a launch takes fewer than 2^32 threads (kMaxBlocks: 2^31).  Workgroups go on
-// to further groups of tokens.
-constexpr int64_t kEnough = 2048, kMaxSums = 1024, kMaxBlocks = int64_t(1) << 23;
+// As many tokens at a time as leave kEnough workgroups.  Calls that sum a weight's gradient have at most kMaxSums
+// rows of sums a weight; a launch takes fewer than 2^32 threads (kMaxBlocks: 2^31).  Workgroups go on to further
+// tokens.
+constexpr int64_t kEnough = 1024, kMaxSums = 1024, kMaxBlocks = int64_t(1) << 22;
 static RotaryPlan rotary_plan(const RotaryProblem& p, bool sums) {
   RotaryPlan c;
-  const int64_t slots = kRotaryThreads / (p.d / 16), all = (p.B * p.N + slots - 1) / slots;
-  auto set = [&](int chunk) {
-    c.chunk = chunk;
-    c.chunks[0] = (int)((p.H + chunk - 1) / chunk);
-    c.chunks[1] = (int)((p.Hkv + chunk - 1) / chunk);
-  };
-  int chunk = 8;
-  for (set(chunk); chunk > 1 && all * (c.chunks[0] + c.chunks[1]) < kEnough; set(chunk)) chunk /= 2;
-  c.groups = std::min(all, std::max<int64_t>(1, (sums ? kMaxSums : kMaxBlocks) / (c.chunks[0] + c.chunks[1])));
+  const int64_t all = p.B * p.N;
+  c.tokens = std::min<int>(kMaxTokens, kRotaryThreads / (int)(p.d / 16));
+  while (c.tokens > 1 && all < kEnough * c.tokens) c.tokens /= 2;
+  c.groups = std::min((all + c.tokens - 1) / c.tokens, sums ? kMaxSums : kMaxBlocks);
   return c;
 }
 static int64_t rotary_bytes(const RotaryProblem& p) {
   if (p.r.q_weight == nullptr && p.r.k_weight == nullptr) return 0;
-  const RotaryPlan c = rotary_plan(p, true);
-  return (c.rows(0) + c.rows(1)) * p.d * 4;
+  return 2 * rotary_plan(p, true).groups * p.d * 4;
 }
 
 // A tensor of head vectors of `heads` heads: present, aligned, in strides that keep 16 bytes.
@@ -396,9 +417,7 @@ static RotaryArgs rotary_args(const RotaryProblem& p, const RotaryPlan& c) {
   a.N = (int)p.N;
   a.H[0] = (int)p.H;
   a.H[1] = (int)p.Hkv;
-  a.chunk = c.chunk;
-  a.chunks[0] = c.chunks[0];
-  a.chunks[1] = c.chunks[1];
+  a.tokens = c.tokens;
   a.pairs = p.r.pairs;
   a.num_axes = p.r.num_axes;
   a.positions = p.r.positions;
@@ -414,7 +433,7 @@ static RotaryArgs rotary_args(const RotaryProblem& p, const RotaryPlan& c) {
 
 template <int kMode> static int32_t rotary_launch(const RotaryProblem& p, const RotaryPlan& c, const RotaryArgs& a,
                                                   hipStream_t s) {
-  const dim3 grid((unsigned)c.groups, (unsigned)(c.chunks[0] + c.chunks[1]));
+  const dim3 grid((unsigned)c.groups, 2);
   (void)hipGetLastError();
   auto go = [&](auto type, auto dim) {
     using T = decltype(type);
@@ -440,8 +459,8 @@ template <int kMode> static int32_t rotary_launch(const RotaryProblem& p, const 
 // The workgroups' sums -> the weights' gradients.
 static int32_t rotary_gather(const RotaryProblem& p, const RotaryPlan& c, const float* sums, void* out_q, void* out_k,
                              hipStream_t s) {
-  hipLaunchKernelGGL(rotary_sums_kernel, dim3((unsigned)(p.d / 16), 2), dim3(256), 0, s, sums, (int)p.d, c.rows(0),
-                     c.rows(1), out_q, out_k, p.r.weight_dtype == BOB_BF16 ? 1 : 0);
+  hipLaunchKernelGGL(rotary_sums_kernel, dim3((unsigned)(p.d / 16), 2), dim3(kSumThreads), 0, s, sums, (int)p.d,
+                     (int)c.groups, out_q, out_k, p.r.weight_dtype == BOB_BF16 ? 1 : 0);
   return finish_launch();
 }
 
