@@ -27,6 +27,9 @@ ScoreArgs score_args(const ScoreProblem& p, const ExtPlan& c, int64_t heads, int
     a.cap_in = (float)((double)p.scale / p.cap * kCapArg<T>);
     a.cap_out = p.cap * kLog2e;
     a.cap_k = 2.f / p.cap;
+    const double x = (double)p.scale / p.cap;  // of a score of Q K^T = 1; 0: every tile is near
+    a.cap_near = x != 0 ? (float)std::min(kCapNear / std::fabs(x), 1e30) : 1e30f;
+    for (int i = 0; i < 5; ++i) a.cap_poly[i] = (float)(kCapPoly[i] * std::pow(x, 2 * i + 1));
   }
   return a;
 }

@@ -8,21 +8,28 @@ namespace fb {
 template <typename T, int D> struct ScorePass1 {
   static constexpr ExtShape shape(int form, bool capped) {
     constexpr Shape w = Cfg<T, D>::kP1;
-    return form == 0   ? ExtShape{w.mr, w.nw, w.occ, 1}
+    constexpr bool kThreeWaves = std::is_same_v<T, bf16> && D == 64;  // 168 registers
+    return form == 0   ? ExtShape{w.mr, w.nw, kThreeWaves ? 3 : w.occ, 1}
            : form == 4 ? ext_two_sets<T, D>(w, 4, 0)
                        : ext_sets<T, D>(kFormWaves[form], 4, 0, 8, w.occ);
   }
   template <int F, bool kCap> static __host__ constexpr auto kernel() {
     constexpr ExtShape s = shape(F, kCap);
-    return &score_pass1_kernel<T, D, s.mr, s.nw, s.occ, s.ks, Cfg<T, D>::kP1.pf, kCap>;
+    // fragments read ahead (bf16 d = 128) where the registers hold them: with a cap, or in sets, they
+    // spilled hundreds (B2 H16 N2048 causal with a cap 1300 us for 245)
+    constexpr int pf = F == 0 && !kCap ? Cfg<T, D>::kP1.pf : 0;
+    return &score_pass1_kernel<T, D, s.mr, s.nw, s.occ, s.ks, pf, kCap>;
   }
 };
 template <typename T, int D> struct ScorePass2 {
   static constexpr int kExtra = 4 * 4 * kBS * (int)sizeof(float) + 1024;
   static constexpr ExtShape shape(int form, bool capped) {
+    // 16 columns a wave, three waves per SIMD, where a cap's tanh spilled 63 registers of the 32
+    // columns' 256 (B4 H12 N4096 causal 750 us)
+    constexpr bool kNarrow = std::is_same_v<T, bf16> && D == 64;
     constexpr Shape w = Cfg<T, D>::kP2;
-    return form == 0   ? ExtShape{w.mr, w.nw, w.occ, 1}
-           : form == 4 ? ext_two_sets<T, D>(w, 3, 2 * kExtra)
+    return form == 0   ? capped && kNarrow ? ExtShape{1, 4, 3, 1} : ExtShape{w.mr, w.nw, w.occ, 1}
+           : form == 4 ? capped && kNarrow ? kNotBuilt : ext_two_sets<T, D>(w, 3, 2 * kExtra)
            : sizeof(T) == 2 && D == 32 && form == 1
                ? kNotBuilt  // three tensors of two 1 KB blocks do not deal out over four waves
                : ext_sets<T, D>(kFormWaves[form], 3, kExtra, 8, w.occ);

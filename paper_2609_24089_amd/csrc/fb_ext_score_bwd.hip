@@ -3,10 +3,13 @@
 
 namespace fb {
 
+// Three waves per SIMD (168 registers) for whole blocks at bf16 d = 64.
+template <typename T, int D> constexpr bool kThreeWaves = std::is_same_v<T, bf16> && D == 64;
+
 template <typename T, int D> struct ScoreRowsBwd {
   static constexpr ExtShape shape(int form, bool capped) {
     constexpr Shape w = Cfg<T, D>::kRows;
-    return form == 0   ? ExtShape{w.mr, w.nw, w.occ, 1}
+    return form == 0   ? ExtShape{w.mr, w.nw, kThreeWaves<T, D> ? 3 : w.occ, 1}
            : form == 4 ? ext_two_sets<T, D>(w, 2, 0)
                        : ext_sets<T, D>(kFormWaves[form], 2, 0, 16, w.occ);
   }
@@ -21,9 +24,11 @@ template <typename T, int D> struct ScoreColsBwd {
   static constexpr ExtShape shape(int form, bool capped) {
     constexpr Shape w = Cfg<T, D>::kCols;
     constexpr int waves = D * (int)sizeof(T) <= 128 ? 16 : 8;
-    return form == 0   ? ExtShape{w.mr, w.nw, w.occ, 1}
+    return form == 0   ? ExtShape{w.mr, w.nw, kThreeWaves<T, D> ? 3 : w.occ, 1}
            : form == 4 ? ext_two_sets<T, D>(w, 2, 2 * kExtra + (w.kl ? 4 * Geo<T, D>::kTileElems * (int)sizeof(T) : 0))
-                       : ext_sets<T, D>(kFormWaves[form], 2, kExtra, waves, w.occ);
+           : form == 1 && D == 256
+               ? kNotBuilt  // spilled 127 registers
+               : ext_sets<T, D>(kFormWaves[form], 2, kExtra, waves, w.occ);
   }
   template <int F, bool kCap> static __host__ constexpr auto kernel() {
     constexpr ExtShape s = shape(F, kCap);

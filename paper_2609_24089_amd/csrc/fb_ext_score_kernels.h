@@ -40,6 +40,8 @@ struct ScoreArgs : ExtArgs {
   float cap_in;          // S / c as an argument of tanh for cap_tanh()
   float cap_out;         // c log2(e)
   float cap_k;           // 2 / c
+  float cap_near;        // |Q K^T| up to which the tanh is cap_poly's
+  float cap_poly[5];     // t = s (p0 + p1 s^2 + ... + p4 s^8), s = Q K^T
 };
 
 // ---------------------------------------------------------------------------
@@ -72,6 +74,49 @@ template <> __device__ __forceinline__ float cap_tanh<float>(float s, float cap_
   return ax < 0.45f ? near : far;
 }
 template <typename T> constexpr float kCapArg = std::is_same_v<T, bf16> ? 2.f * kLog2e : 1.f;  // of cap_in
+
+// tanh on |x| <= kCapNear by an odd polynomial, off by 1.1e-6 at most (the least for five terms;
+// 5e-5 of a score of c = 50, where P is rounded to 2^-9).  Scores of trained models lie far below
+// their cap, so whole tiles take it: 6 instructions an element for two transcendentals, at a
+// quarter of the rate, and three others.  cap_near and cap_poly are this in terms of Q K^T.
+constexpr double kCapNear = 0.9;
+constexpr double kCapPoly[5] = {0.9999867425076748, -0.3329870630439696, 0.13076785780676703, -0.04593852969671257,
+                                0.009843491590824895};
+
+// t = tanh(S / c) of a tile of raw scores.
+template <typename T, int A, int B>
+__device__ __forceinline__ void cap_tile(const ScoreArgs& a, const floatx4 (&s)[A][B], floatx4 (&t)[A][B]) {
+  if constexpr (sizeof(T) == 2) {
+    float most = 0.f;
+#pragma unroll
+    for (int x = 0; x < A; ++x)
+#pragma unroll
+      for (int y = 0; y < B; ++y)
+#pragma unroll
+        for (int r = 0; r < 4; r += 2) most = fmaxf(most, fmaxf(fabsf(s[x][y][r]), fabsf(s[x][y][r + 1])));
+    if (__builtin_amdgcn_ballot_w64(most > a.cap_near) == 0) {
+#pragma unroll
+      for (int x = 0; x < A; ++x)
+#pragma unroll
+        for (int y = 0; y < B; ++y)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float v = s[x][y][r], q = v * v;
+            float p = __builtin_fmaf(q, a.cap_poly[4], a.cap_poly[3]);
+            p = __builtin_fmaf(q, p, a.cap_poly[2]);
+            p = __builtin_fmaf(q, p, a.cap_poly[1]);
+            t[x][y][r] = v * __builtin_fmaf(q, p, a.cap_poly[0]);
+          }
+      return;
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < A; ++x)
+#pragma unroll
+    for (int y = 0; y < B; ++y)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) t[x][y][r] = cap_tanh<T>(s[x][y][r], a.cap_in);
+}
 
 // ---------------------------------------------------------------------------
 // Spans
@@ -146,15 +191,20 @@ __device__ __forceinline__ void score_mask(floatx4& x0, floatx4& x1, int s0, Int
   }
 }
 
-// Adds -m |distance| to exponents: `first` is the distance at sb = 0, r = 0, which falls (rows:
-// the keys stream) or grows (columns: the queries stream) by one a streamed row; m in log2 units.
-template <int kSign> __device__ __forceinline__ void score_slope(floatx4& x0, floatx4& x1, int first, float m) {
+// -m |distance| of a tile's two halves, a 16-row block of the stationary side: `first` is the
+// distance at sb = 0, r = 0, kSign its step along the streamed side (rows: the keys stream).
+// Uncapped scores start their MFMA there, with m in units of Q K^T; capped ones add it.
+template <int kSign> __device__ __forceinline__ floatx4 score_distance(int sb, int first, float m) {
   const float d = (float)first;
+  floatx4 x;
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    x0[r] = __builtin_fmaf(-m, fabsf(d + (float)(kSign * r)), x0[r]);
-    x1[r] = __builtin_fmaf(-m, fabsf(d + (float)(kSign * (16 + r))), x1[r]);
-  }
+  for (int r = 0; r < 4; ++r) x[r] = -m * fabsf(d + (float)(kSign * (16 * sb + r)));
+  return x;
+}
+// log2(e) tau, or something of no effect that can be divided by where tau is 0.
+__device__ __forceinline__ float score_scale(float scale) {
+  const float c = scale * kLog2e;
+  return fabsf(c) < 1e-30f ? 1e-30f : c;
 }
 
 // What a row kernel's workgroup and wave know of their rows (as ExtRows).
@@ -208,11 +258,43 @@ struct ScoreRows {
   __device__ __forceinline__ bool ok(int mb) const { return row(mb) < rows && query(mb) < qlen; }
   // the first key of tile i of the run
   __device__ __forceinline__ int key(int i) const { return (t0 + min(i, tiles - 1)) * kBS; }
+  // The same in the forward's order under a distance bias: from the tile of the workgroup's last
+  // query (`peak`, from outward()) down, then those behind it upward.  Scores fall with distance,
+  // so the running maximum is found at once; from the first key on it grew in every tile (B1 H16
+  // N8192 d128 causal 690 us).
+  __device__ __forceinline__ int outward(const ScoreArgs& a, int rb) const {
+    if (a.slopes == nullptr) return -1;
+    const int last = start + (fold ? qlen : min((rb + 1) * 16 * MR * NW, qlen)) - 1;
+    return min(max(last, 0) / kBS - t0, tiles - 1);
+  }
+  __device__ __forceinline__ int key(int i, int peak) const {
+    const int at = min(i, tiles - 1);
+    return (t0 + (at <= peak ? peak - at : at)) * kBS;
+  }
 };
 
-// Slope of the lane's row mb in log2 units.
-template <typename Rows> __device__ __forceinline__ float score_row_slope(const ScoreArgs& a, const Rows& rw, int mb) {
-  return a.slopes != nullptr ? a.slopes[rw.head(mb)] * kLog2e : 0.f;
+// The slope of a row kernel's lane, of one head (folded rows have one row a lane): in log2 units
+// for capped scores, else in units of Q K^T.
+template <bool kCap, typename Rows>
+__device__ __forceinline__ float score_row_slope(const ScoreArgs& a, const Rows& rw, float c) {
+  if (a.slopes == nullptr) return 0.f;
+  const float m = a.slopes[rw.head(0)] * kLog2e;
+  return kCap ? m : m / c;
+}
+// Where the scores of rows mb of the tile at s0 start.
+template <bool kCap, int MR, typename Rows>
+__device__ __forceinline__ void score_row_start(const ScoreArgs& a, const Rows& rw, int s0, float slope,
+                                                floatx4 (&s)[2][MR]) {
+#pragma unroll
+  for (int mb = 0; mb < MR; ++mb) s[0][mb] = s[1][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
+  if (!kCap && a.slopes != nullptr) {
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb) {
+      const int first = rw.pos(mb) - s0 - 4 * (lane_id() >> 4);
+      s[0][mb] = score_distance<-1>(0, first, slope);
+      s[1][mb] = score_distance<-1>(1, first, slope);
+    }
+  }
 }
 
 // x rounded to T, and what that leaves.
@@ -287,29 +369,29 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_fwd_kernel(
 #pragma unroll
     for (int mb = 0; mb < MR; ++mb) acc[nb][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
   constexpr bool kRounded = sizeof(T) == 2;
-  float mrun[MR], lsum[MR], rsum[MR], slope[MR];  // rsum: of P as it is rounded
-  const int sloped = vector_mode(a.slopes != nullptr ? 1 : 0);
+  float mrun[MR], lsum[MR], rsum[MR];  // rsum: of P as it is rounded
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb) {
     mrun[mb] = -1e30f;
     lsum[mb] = rsum[mb] = 0.f;
-    slope[mb] = score_row_slope(a, rw, mb);
   }
-  const float c = kCap ? a.cap_out : a.scale * kLog2e;
+  const float c = kCap ? a.cap_out : score_scale(a.scale);
+  const float slope = score_row_slope<kCap>(a, rw, c);
   floatx4 s[2][MR];
   typename E::TFrag pf[MR];
 
-  // s times cf are the scores in log2 units (cf = 1 where a bias went into s)
+  // s times cf are the scores in log2 units (1 where a bias went into capped ones)
   auto softmax_step = [&](int s0, int mode, float cf) {
     float p[MR][8], ls[MR];
     bool grown = false;
     floatx4 e[MR][2];
 #pragma unroll
-    for (int mb = 0; mb < MR; ++mb)
+    for (int mb = 0; mb < MR; ++mb) {
 #pragma unroll
       for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
         for (int r = 0; r < 4; ++r) e[mb][sb][r] = __builtin_fmaf(s[sb][mb][r], cf, -mrun[mb]);
+    }
     if (mode == 2) {
 #pragma unroll
       for (int mb = 0; mb < MR; ++mb) score_mask(e[mb][0], e[mb][1], s0, rw.keys[mb]);
@@ -362,26 +444,23 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_fwd_kernel(
   };
 
   const T* const src[2] = {K + kvoff, V + kvoff};
-  const int split = ext_parts_of(rw.tiles, KS, a.nparts);
+  const int split = ext_parts_of(rw.tiles, KS, a.nparts), peak = rw.outward(a, rb);
   const ExtRun run = ext_run(rw.tiles, part, split, ks, KS), first = ext_run(rw.tiles, part, split, 0, KS);
   constexpr bool kBarrier = NW > 1;
   const TileCopy<T, D, NW, 2> copy(wl);
   ext_stream<tile_loads<T, D, NW, 2>(), kBarrier>(
       kBarrier ? first.size() : run.size(),
       [&](int it, int st) {
-        copy.template issue<true>(src, (T FB_LDS*)sm.lds[ks][st], rw.key(run.begin + it), rw.kend);
+        copy.template issue<true>(src, (T FB_LDS*)sm.lds[ks][st], rw.key(run.begin + it, peak), rw.kend);
       },
       []() {},
       [&](int it, int st) {
-        const int s0 = rw.key(run.begin + it);
+        const int s0 = rw.key(run.begin + it, peak);
         const int mode = vector_mode(run.begin + it < run.end ? rw.reach.mode(s0) : 0);
         if (mode == 0) return;
         const T FB_LDS* Ks = (const T FB_LDS*)sm.lds[ks][st];
         const T FB_LDS* Vs = Ks + G::kTileElems;
-#pragma unroll
-        for (int sb = 0; sb < 2; ++sb)
-#pragma unroll
-          for (int mb = 0; mb < MR; ++mb) s[sb][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
+        score_row_start<kCap>(a, rw, s0, slope, s);
 #pragma unroll
         for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
@@ -392,20 +471,15 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_fwd_kernel(
           }
         float cf = c;
         if constexpr (kCap) {
+          cap_tile<T>(a, s, s);
+          if (a.slopes != nullptr) {
+            cf = 1.f;
 #pragma unroll
-          for (int sb = 0; sb < 2; ++sb)
+            for (int mb = 0; mb < MR; ++mb) {
+              const int first = rw.pos(mb) - s0 - 4 * g;
 #pragma unroll
-            for (int mb = 0; mb < MR; ++mb)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) s[sb][mb][r] = cap_tanh<T>(s[sb][mb][r], a.cap_in);
-        }
-        if (sloped != 0) {
-          cf = 1.f;
-#pragma unroll
-          for (int mb = 0; mb < MR; ++mb) {
-            s[0][mb] *= c;
-            s[1][mb] *= c;
-            score_slope<-1>(s[0][mb], s[1][mb], rw.pos(mb) - s0 - 4 * g, slope[mb]);
+              for (int sb = 0; sb < 2; ++sb) s[sb][mb] = s[sb][mb] * c + score_distance<-1>(sb, first, slope);
+            }
           }
         }
         softmax_step(s0, mode, cf);
@@ -521,18 +595,33 @@ __global__ __launch_bounds__(256) void score_fwd_join_kernel(ExtArgs a, const fl
   if (dim == 0) L[row] = some ? (m + __log2f(w)) * kLn2 : -INFINITY;
 }
 
-// The exponent of P from a raw score: s c, or the capped score with its t = tanh, less L
-// (off = -L log2(e)).
-template <typename T, bool kCap>
-__device__ __forceinline__ float score_exponent(const ScoreArgs& a, float s, float c, float off, float& t) {
-  if constexpr (kCap) {
-    t = cap_tanh<T>(s, a.cap_in);
-    return __builtin_fmaf(t, a.cap_out, off);
-  } else {
-    return __builtin_fmaf(s, c, off);
+__device__ __forceinline__ float cap_slope(float t) { return __builtin_fmaf(-t, t, 1.f); }
+
+// A row kernel's raw scores -> the exponents of P: capped (t = tanh), less L.
+template <typename T, bool kCap, int MR, int A, int B, typename Rows>
+__device__ __forceinline__ void score_row_exponents(const ScoreArgs& a, const Rows& rw, float slope, float c, int s0,
+                                                    const float (&lb)[MR], floatx4 (&s)[2][MR], floatx4 (&t)[A][B]) {
+  if constexpr (kCap) cap_tile<T>(a, s, t);
+#pragma unroll
+  for (int mb = 0; mb < MR; ++mb)
+#pragma unroll
+    for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if constexpr (kCap)
+          s[sb][mb][r] = __builtin_fmaf(t[sb][mb][r], c, -lb[mb]);
+        else
+          s[sb][mb][r] = __builtin_fmaf(s[sb][mb][r], c, -lb[mb]);
+      }
+  if (kCap && a.slopes != nullptr) {
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb) {
+      const int first = rw.pos(mb) - s0 - 4 * (lane_id() >> 4);
+#pragma unroll
+      for (int sb = 0; sb < 2; ++sb) s[sb][mb] += score_distance<-1>(sb, first, slope);
+    }
   }
 }
-__device__ __forceinline__ float cap_slope(float t) { return __builtin_fmaf(-t, t, 1.f); }
 
 // ===========================================================================
 // First backward, row side, as ext_bwd_rows_kernel.  A capped tile's t takes eight registers a
@@ -559,8 +648,6 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_rows_kernel(
 
   u32x4 qf[MR][G::kChunks], dof[MR][G::kChunks];
   float lb[MR], drow[MR], dout[MR], rest[MR];
-  const int sloped = vector_mode(a.slopes != nullptr ? 1 : 0);
-  const float slope = score_row_slope(a, rw, 0);
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb) {
     const int row = rw.ok(mb) ? rw.row(mb) : rw.rows;
@@ -590,7 +677,8 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_rows_kernel(
   for (int nb = 0; nb < G::kNB; ++nb)
 #pragma unroll
     for (int mb = 0; mb < MR; ++mb) acc[nb][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
-  const float c = a.scale * kLog2e;
+  const float c = kCap ? a.cap_out : score_scale(a.scale);
+  const float slope = score_row_slope<kCap>(a, rw, c);
   floatx4 s[2][MR], dp[2][MR], t[kCap ? 2 : 1][kCap ? MR : 1];
   SplitFrag<T> dsf[MR];
 
@@ -611,13 +699,11 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_rows_kernel(
         if (mode == 0) return;
         const T FB_LDS* Ks = (const T FB_LDS*)sm.lds[ks][st];
         const T FB_LDS* Vs = Ks + G::kTileElems;
+        score_row_start<kCap>(a, rw, s0, slope, s);
 #pragma unroll
         for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
-          for (int mb = 0; mb < MR; ++mb) {
-            s[sb][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
-            dp[sb][mb] = floatx4{-drow[mb], -drow[mb], -drow[mb], -drow[mb]};
-          }
+          for (int mb = 0; mb < MR; ++mb) dp[sb][mb] = floatx4{-drow[mb], -drow[mb], -drow[mb], -drow[mb]};
 #pragma unroll
         for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
@@ -631,20 +717,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_rows_kernel(
               dp[sb][mb] = E::mma_chunk(av, dof[mb][kk], dp[sb][mb]);
             }
           }
-#pragma unroll
-        for (int sb = 0; sb < 2; ++sb)
-#pragma unroll
-          for (int mb = 0; mb < MR; ++mb)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              float tr = 0.f;
-              s[sb][mb][r] = score_exponent<T, kCap>(a, s[sb][mb][r], c, -lb[mb], tr);
-              if constexpr (kCap) t[sb][mb][r] = tr;
-            }
-        if (sloped != 0) {
-#pragma unroll
-          for (int mb = 0; mb < MR; ++mb) score_slope<-1>(s[0][mb], s[1][mb], rw.pos(mb) - s0 - 4 * g, slope);
-        }
+        score_row_exponents<T, kCap>(a, rw, slope, c, s0, lb, s, t);
         if (mode == 2) {
 #pragma unroll
           for (int mb = 0; mb < MR; ++mb) score_mask(s[0][mb], s[1][mb], s0, rw.keys[mb]);
@@ -723,7 +796,7 @@ struct ScoreCols {
   int b, kvh, hq, heads, sub, subs;
   int t0, per_head;  // first query tile, query tiles a head
   int qlen, klen, start;
-  int col0;
+  int col0;           // first column of the wave
   Interval rows[MC];  // query rows that see the lane's columns
   Reach reach;        // of the wave's columns
   __device__ __forceinline__ ScoreCols(const ScoreArgs& a, int kv, int rb, int wl) {
@@ -763,11 +836,75 @@ struct ScoreCols {
   __device__ __forceinline__ int tile(int f) const { return t0 + (heads == 1 ? f : f % per_head); }
 };
 
-// The slopes of a key/value head's query heads in LDS, in log2 units, for all waves after the
-// next barrier.
-__device__ __forceinline__ void score_fill_slopes(const ScoreArgs& a, int kv, float FB_LDS* dst, int count) {
-  if (a.slopes == nullptr) return;
-  for (int x = threadIdx.x; x < a.grp; x += count) dst[x] = a.slopes[kv * a.grp % a.H + x] * kLog2e;
+// The slopes of a key/value head's query heads in log2 units: in LDS, and that of a workgroup with
+// one head in a register (read from LDS in every tile it held up the first MFMA).
+struct ColSlopes {
+  const float FB_LDS* all;
+  float one = 0.f;
+  template <typename Cols>
+  __device__ __forceinline__ ColSlopes(const ScoreArgs& a, const Cols& cl, float* mem, int threads) {
+    float FB_LDS* const to = (float FB_LDS*)mem;
+    all = to;
+    if (a.slopes == nullptr) return;
+    const float* const from = a.slopes + cl.kvh * a.grp % a.H;
+    one = from[cl.hq - cl.kvh * a.grp] * kLog2e;
+    for (int x = threadIdx.x; x < a.grp; x += threads) to[x] = from[x] * kLog2e;
+    __syncthreads();
+  }
+};
+
+// The slope of tile f's head, as score_row_slope().
+template <bool kCap, typename Cols>
+__device__ __forceinline__ float score_col_slope(const ScoreArgs& a, const Cols& cl, const ColSlopes& slopes, int f,
+                                                 float c) {
+  if (a.slopes == nullptr) return 0.f;
+  const float m = cl.heads == 1 ? slopes.one : scalar(slopes.all[cl.qhead(f) - cl.kvh * a.grp]);
+  return kCap ? m : m / c;
+}
+// The distance of the lane's first query of the tile at s0 from column block mc's key.
+template <typename Cols> __device__ __forceinline__ int score_col_first(const Cols& cl, int s0, int mc) {
+  const int l = lane_id();
+  return cl.start + s0 + 4 * (l >> 4) - (cl.col0 + 16 * mc + (l & 15));
+}
+template <bool kCap, int MC, typename Cols>
+__device__ __forceinline__ void score_col_start(const ScoreArgs& a, const Cols& cl, int s0, float slope,
+                                                floatx4 (&s)[2][MC]) {
+#pragma unroll
+  for (int mc = 0; mc < MC; ++mc) s[0][mc] = s[1][mc] = floatx4{0.f, 0.f, 0.f, 0.f};
+  if (!kCap && a.slopes != nullptr) {
+#pragma unroll
+    for (int mc = 0; mc < MC; ++mc) {
+      const int first = score_col_first(cl, s0, mc);
+      s[0][mc] = score_distance<1>(0, first, slope);
+      s[1][mc] = score_distance<1>(1, first, slope);
+    }
+  }
+}
+
+// A column kernel's raw scores -> the exponents of P; off: the row scalars.
+template <typename T, bool kCap, int MC, int A, int B, typename Cols>
+__device__ __forceinline__ void score_col_exponents(const ScoreArgs& a, const Cols& cl, float slope, float c, int s0,
+                                                    const float FB_LDS* off, floatx4 (&s)[2][MC], floatx4 (&t)[A][B]) {
+  if constexpr (kCap) cap_tile<T>(a, s, t);
+#pragma unroll
+  for (int sb = 0; sb < 2; ++sb) {
+    const floatx4 o = *(const floatx4 FB_LDS*)(off + 16 * sb + 4 * (lane_id() >> 4));
+#pragma unroll
+    for (int mc = 0; mc < MC; ++mc)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if constexpr (kCap)
+          s[sb][mc][r] = __builtin_fmaf(t[sb][mc][r], c, o[r]);
+        else
+          s[sb][mc][r] = __builtin_fmaf(s[sb][mc][r], c, o[r]);
+      }
+  }
+  if (kCap && a.slopes != nullptr) {
+#pragma unroll
+    for (int mc = 0; mc < MC; ++mc)
+#pragma unroll
+      for (int sb = 0; sb < 2; ++sb) s[sb][mc] += score_distance<1>(sb, score_col_first(cl, s0, mc), slope);
+  }
 }
 
 // First backward, column side, as ext_bwd_cols_kernel.
@@ -790,7 +927,6 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_cols_kernel(
   };
   __shared__ __attribute__((aligned(16))) std::conditional_t<kKL, SmemK, Smem> sm;
   extern __shared__ float slope_mem[];
-  float FB_LDS* const slopes = (float FB_LDS*)slope_mem;
 
   int kv, rb;
   ext_map_cols(a, kv, rb);
@@ -814,14 +950,13 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_cols_kernel(
       kc.template issue<true>(ksrc, (T FB_LDS*)sm.kst[wl / kWPT], cl.col0, cl.klen);
     }
   }
-  score_fill_slopes(a, kv, slopes, KS * NW * 64);
-  const int sloped = vector_mode(a.slopes != nullptr ? 1 : 0);
+  const ColSlopes slopes(a, cl, slope_mem, KS * NW * 64);
   floatx4 dk[G::kNB][MC], dv[G::kNB][MC];
 #pragma unroll
   for (int nb = 0; nb < G::kNB; ++nb)
 #pragma unroll
     for (int mc = 0; mc < MC; ++mc) dk[nb][mc] = dv[nb][mc] = floatx4{0.f, 0.f, 0.f, 0.f};
-  const float c = a.scale * kLog2e;
+  const float c = kCap ? a.cap_out : score_scale(a.scale);
   floatx4 s[2][MC], dp[2][MC], t[kCap ? 2 : 1][kCap ? MC : 1];
   typename E::TFrag pf[MC], dsf[MC];
 
@@ -859,12 +994,13 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_cols_kernel(
         const T FB_LDS* Qs = (const T FB_LDS*)sm.lds[ks][st];
         const T FB_LDS* dOs = Qs + G::kTileElems;
         const float FB_LDS* Ts = (const float FB_LDS*)sm.tsc[ks][ts];
+        const float slope = score_col_slope<kCap>(a, cl, slopes, flat(it), c);
+        score_col_start<kCap>(a, cl, s0, slope, s);
 #pragma unroll
         for (int sb = 0; sb < 2; ++sb) {
           const floatx4 t1 = *(const floatx4 FB_LDS*)(Ts + kBS + 16 * sb + 4 * g);
 #pragma unroll
           for (int mc = 0; mc < MC; ++mc) {
-            s[sb][mc] = floatx4{0.f, 0.f, 0.f, 0.f};
             dp[sb][mc] = t1;
           }
         }
@@ -906,24 +1042,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_cols_kernel(
             }
         }
         __builtin_amdgcn_s_setprio(0);
-#pragma unroll
-        for (int sb = 0; sb < 2; ++sb) {
-          const floatx4 off = *(const floatx4 FB_LDS*)(Ts + 16 * sb + 4 * g);
-#pragma unroll
-          for (int mc = 0; mc < MC; ++mc)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              float tr = 0.f;
-              s[sb][mc][r] = score_exponent<T, kCap>(a, s[sb][mc][r], c, off[r], tr);
-              if constexpr (kCap) t[sb][mc][r] = tr;
-            }
-        }
-        if (sloped != 0) {
-          const float m = slopes[cl.qhead(flat(it)) - kv * a.grp];
-#pragma unroll
-          for (int mc = 0; mc < MC; ++mc)
-            score_slope<1>(s[0][mc], s[1][mc], cl.start + s0 + 4 * g - (cl.col0 + 16 * mc + j), m);
-        }
+        score_col_exponents<T, kCap>(a, cl, slope, c, s0, Ts, s, t);
         if (mode == 2) {
 #pragma unroll
           for (int mc = 0; mc < MC; ++mc) score_mask(s[0][mc], s[1][mc], s0, cl.rows[mc]);
@@ -990,8 +1109,6 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
 
   u32x4 qf[MR][G::kChunks], uqf[MR][G::kChunks], dof[MR][G::kChunks];
   float lb[MR], drow[MR];
-  const int sloped = vector_mode(a.slopes != nullptr ? 1 : 0);
-  const float slope = score_row_slope(a, rw, 0);
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb) {
     const int row = rw.ok(mb) ? rw.row(mb) : rw.rows;
@@ -1010,7 +1127,8 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
   float alpha[MR], e0[MR];
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb) alpha[mb] = e0[mb] = 0.f;
-  const float c = a.scale * kLog2e;
+  const float c = kCap ? a.cap_out : score_scale(a.scale);
+  const float slope = score_row_slope<kCap>(a, rw, c);
   floatx4 s[2][MR], dp[2][MR], f[2][MR], cc[2][MR], t[kCap ? 2 : 1][kCap ? MR : 1];
   typename E::TFrag fP[MR], fPdd[MR];  // of a cap: P, and u P in fB
   SplitFrag<T> fPF[MR], fPPt[MR], fB[MR];
@@ -1037,11 +1155,12 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
         const T FB_LDS* UKs = Vs + G::kTileElems;
         const T FB_LDS* UVs = UKs + G::kTileElems;
         if constexpr (std::is_same_v<T, bf16> && D == 128) __builtin_amdgcn_iglp_opt(3);
+        score_row_start<kCap>(a, rw, s0, slope, s);
 #pragma unroll
         for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
           for (int mb = 0; mb < MR; ++mb) {
-            s[sb][mb] = f[sb][mb] = cc[sb][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
+            f[sb][mb] = cc[sb][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
             dp[sb][mb] = floatx4{-drow[mb], -drow[mb], -drow[mb], -drow[mb]};
           }
 #pragma unroll
@@ -1060,16 +1179,17 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
               cc[sb][mb] = E::mma_chunk(auv, dof[mb][kk], cc[sb][mb]);    // C^T = U_V dO^T
             }
           }
+        score_row_exponents<T, kCap>(a, rw, slope, c, s0, lb, s, t);
 #pragma unroll
         for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
           for (int mb = 0; mb < MR; ++mb)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              float tr = 0.f;
-              s[sb][mb][r] = score_exponent<T, kCap>(a, s[sb][mb][r], c, -lb[mb], tr);
-              if constexpr (kCap) t[sb][mb][r] = tr;
-              f[sb][mb][r] *= kCap ? a.scale * cap_slope(tr) : a.scale;
+              if constexpr (kCap)
+                f[sb][mb][r] *= a.scale * cap_slope(t[sb][mb][r]);
+              else
+                f[sb][mb][r] *= a.scale;
             }
         AF cur[4];
         auto load_frags = [&](int nb) {
@@ -1077,10 +1197,6 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
           for (int x = 0; x < 4; ++x) cur[x] = G::load_afrag(Ks + x * G::kTileElems, 16 * nb);
         };
         if constexpr (kPF != 0) load_frags(0);
-        if (sloped != 0) {
-#pragma unroll
-          for (int mb = 0; mb < MR; ++mb) score_slope<-1>(s[0][mb], s[1][mb], rw.pos(mb) - s0 - 4 * g, slope);
-        }
         if (mode == 2) {
 #pragma unroll
           for (int mb = 0; mb < MR; ++mb) score_mask(s[0][mb], s[1][mb], s0, rw.keys[mb]);
@@ -1268,7 +1384,6 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass2_kernel(
   };
   __shared__ __attribute__((aligned(16))) Smem2 sm;
   extern __shared__ float slope_mem[];
-  float FB_LDS* const slopes = (float FB_LDS*)slope_mem;
 
   int kv, rb;
   ext_map_cols(a, kv, rb);
@@ -1287,14 +1402,13 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass2_kernel(
     load_stationary<T, D>(ukf[mc], UK + koff, col, cl.klen);
     load_stationary<T, D>(uvf[mc], UV + koff, col, cl.klen);
   }
-  score_fill_slopes(a, kv, slopes, KS * NW * 64);
-  const int sloped = vector_mode(a.slopes != nullptr ? 1 : 0);
+  const ColSlopes slopes(a, cl, slope_mem, KS * NW * 64);
   floatx4 aK[G::kNB][MC], aV[G::kNB][MC];
 #pragma unroll
   for (int nb = 0; nb < G::kNB; ++nb)
 #pragma unroll
     for (int mc = 0; mc < MC; ++mc) aK[nb][mc] = aV[nb][mc] = floatx4{0.f, 0.f, 0.f, 0.f};
-  const float c = a.scale * kLog2e;
+  const float c = kCap ? a.cap_out : score_scale(a.scale);
   floatx4 s[2][MC], dp[2][MC], f[2][MC], cc[2][MC];
   typename E::TFrag fPh[MC], fSt[MC], fdS[MC];
 
@@ -1341,13 +1455,15 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass2_kernel(
         const T FB_LDS* UQs = Qs + G::kTileElems;
         const T FB_LDS* dOs = UQs + G::kTileElems;
         const float FB_LDS* Ts = (const float FB_LDS*)sm.tsc[ks][ts];
+        const float slope = score_col_slope<kCap>(a, cl, slopes, flat(it), c);
+        score_col_start<kCap>(a, cl, s0, slope, s);
 #pragma unroll
         for (int sb = 0; sb < 2; ++sb) {
           const floatx4 t1 = *(const floatx4 FB_LDS*)(Ts + kBS + 16 * sb + 4 * g);
           const floatx4 t3 = *(const floatx4 FB_LDS*)(Ts + 3 * kBS + 16 * sb + 4 * g);
 #pragma unroll
           for (int mc = 0; mc < MC; ++mc) {
-            s[sb][mc] = f[sb][mc] = floatx4{0.f, 0.f, 0.f, 0.f};
+            f[sb][mc] = floatx4{0.f, 0.f, 0.f, 0.f};
             dp[sb][mc] = t1;
             cc[sb][mc] = t3;
           }
@@ -1392,29 +1508,22 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass2_kernel(
         __builtin_amdgcn_s_setprio(0);
         prep_next();
         floatx4 t[kCap ? 2 : 1][kCap ? MC : 1];
+        score_col_exponents<T, kCap>(a, cl, slope, c, s0, Ts, s, t);
 #pragma unroll
-        for (int sb = 0; sb < 2; ++sb) {
-          const floatx4 off = *(const floatx4 FB_LDS*)(Ts + 16 * sb + 4 * g);
+        for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
           for (int mc = 0; mc < MC; ++mc)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              float tr = 0.f;
-              s[sb][mc][r] = score_exponent<T, kCap>(a, s[sb][mc][r], c, off[r], tr);
-              if constexpr (kCap) t[sb][mc][r] = tr;
-              f[sb][mc][r] *= kCap ? a.scale * cap_slope(tr) : a.scale;
+              if constexpr (kCap)
+                f[sb][mc][r] *= a.scale * cap_slope(t[sb][mc][r]);
+              else
+                f[sb][mc][r] *= a.scale;
             }
-        }
         typename E::AFrag cur[3];
         if constexpr (kPF) {
 #pragma unroll
           for (int x = 0; x < 3; ++x) cur[x] = G::load_afrag(Qs + x * G::kTileElems, 0);
-        }
-        if (sloped != 0) {
-          const float m = slopes[cl.qhead(flat(it)) - kv * a.grp];
-#pragma unroll
-          for (int mc = 0; mc < MC; ++mc)
-            score_slope<1>(s[0][mc], s[1][mc], cl.start + s0 + 4 * g - (cl.col0 + 16 * mc + j), m);
         }
         if (mode == 2) {
 #pragma unroll
