@@ -14,10 +14,12 @@
 //
 // Everything is bound by memory: each call reads and writes every vector once, whatever the
 // layout (strides of batch entry, head and token), so the way from a projection's [B,N,heads,d]
-// to an attention's [B,heads,N,d] is part of it.  d / 16 lanes share a vector: a lane holds
-// eight pairs, whose halves are two runs of eight elements (neighbours paired: one run of 16), so
-// it loads 16 bytes at a time and a rotation needs no other lane.  A workgroup makes the cosines
-// and sines of its tokens once for all heads of the queries or keys.
+// to an attention's [B,heads,N,d] is part of it.  A lane holds two runs of 16 bytes of a vector:
+// a run of pairs' first halves and that of their second ones (neighbours paired: two runs of whole
+// pairs, half a vector apart), so a rotation needs no other lane, and the lanes of a vector read
+// and write neighbouring runs (in runs of 16 elements a lane fp32 B8 H6 N1395 d64 of neighbours
+// took 33 us forward).  A workgroup makes the cosines and sines of its tokens once for all heads
+// of the queries or keys.
 #include "fb_ext.h"
 
 namespace fb {
@@ -47,7 +49,11 @@ struct RotaryArgs {
 constexpr int kRotaryThreads = 256, kMaxTokens = 16;
 constexpr double kTurns = 0.15915494309189535;  // 1 / (2 pi)
 
-// Sum over the d / 16 lanes (a power of two up to 16) that share a vector: all of them get it.
+// Elements of a run, and lanes that share a vector (2 to 32).
+template <typename T> constexpr int kRun = 16 / sizeof(T);
+template <typename T, int D> constexpr int kLanes = D / (2 * kRun<T>);
+
+// Sum over the LPV lanes that share a vector: all of them get it.
 template <int LPV> __device__ __forceinline__ float vector_sum(float v) {
   auto add = [&](auto ctrl) {
     v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, 0xf,
@@ -57,117 +63,148 @@ template <int LPV> __device__ __forceinline__ float vector_sum(float v) {
   if constexpr (LPV >= 4) add(std::integral_constant<int, 0x4e>{});   // quad_perm 2,3,0,1
   if constexpr (LPV >= 8) add(std::integral_constant<int, 0x141>{});  // row_half_mirror
   if constexpr (LPV >= 16) add(std::integral_constant<int, 0x140>{}); // row_mirror
+  if constexpr (LPV >= 32) v += __shfl_xor(v, 16);
   return v;
 }
 
-// Where a lane's two runs of eight elements lie in a vector, and whether they are rotated.
+// Where a lane's two runs lie in a vector, and the pair of each of its elements: E / 2 pairs from
+// pair[0] and as many from pair[1] (halves apart: E in a row).  turned: whether those are rotated.
 struct LanePairs {
-  int a, b;     // first elements
-  bool turned;
-  int pair;     // first pair
+  int a, b;
+  int pair[2];
+  bool turned[2];
 };
-template <bool kNeighbours> __device__ __forceinline__ LanePairs lane_pairs(int p, int pairs) {
+template <typename T, int D, bool kNeighbours> __device__ __forceinline__ LanePairs lane_pairs(int p, int pairs) {
+  constexpr int E = kRun<T>;
   LanePairs l;
-  l.turned = 8 * p < pairs;
-  l.pair = 8 * p;
-  if (kNeighbours || !l.turned) {
-    l.a = 16 * p;
-    l.b = 16 * p + 8;
+  if (kNeighbours) {
+    l.a = E * p;
+    l.b = D / 2 + E * p;
+    l.pair[0] = l.a / 2;
+    l.pair[1] = l.b / 2;
   } else {
-    l.a = 8 * p;
-    l.b = pairs + 8 * p;
+    const bool turned = E * p < pairs;
+    l.a = turned ? E * p : 2 * E * p;
+    l.b = turned ? pairs + E * p : 2 * E * p + E;
+    l.pair[0] = E * p;
+    l.pair[1] = E * p + E / 2;
   }
+  l.turned[0] = l.pair[0] < pairs;
+  l.turned[1] = l.pair[1] < pairs;
   return l;
 }
 
-template <typename T> __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
+template <typename T> __device__ __forceinline__ void unpack(u32x4 raw, float (&x)[kRun<T>]) {
   if constexpr (sizeof(T) == 2) {
-    const bf16x8 v = __builtin_bit_cast(bf16x8, *(const u32x4*)p);
+    const bf16x8 v = __builtin_bit_cast(bf16x8, raw);
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
   } else {
-    const floatx4 v0 = *(const floatx4*)p, v1 = *(const floatx4*)(p + 4);
+    const floatx4 v = __builtin_bit_cast(floatx4, raw);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = v0[i], x[4 + i] = v1[i];
+    for (int i = 0; i < 4; ++i) x[i] = v[i];
   }
 }
-template <typename T> __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
+// Element i of the run: of(i).
+template <typename T, class F> __device__ __forceinline__ void store_run(T* p, F&& of) {
   if constexpr (sizeof(T) == 2) {
     bf16x8 v;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (bf16)x[i];
+    for (int i = 0; i < 8; ++i) v[i] = (bf16)of(i);
     *(u32x4*)p = __builtin_bit_cast(u32x4, v);
   } else {
-    *(floatx4*)p = floatx4{x[0], x[1], x[2], x[3]};
-    *(floatx4*)(p + 4) = floatx4{x[4], x[5], x[6], x[7]};
+    *(floatx4*)p = floatx4{of(0), of(1), of(2), of(3)};
   }
 }
 
-// The lane's 16 elements as pairs (a[i], b[i]).
-struct Pairs {
-  float a[8], b[8];
+// The lane's elements as E pairs (a[i], b[i]).
+template <int E> struct Pairs {
+  float a[E], b[E];
 };
-// Neighbours come as elements 0 .. 7 and 8 .. 15.
-__device__ __forceinline__ Pairs from_neighbours(const Pairs& e) {
-  Pairs p;
+// Neighbours come as the elements of the two runs.
+template <int E> __device__ __forceinline__ Pairs<E> from_neighbours(const Pairs<E>& e) {
+  Pairs<E> p;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < E / 2; ++i) {
     p.a[i] = e.a[2 * i], p.b[i] = e.a[2 * i + 1];
-    p.a[4 + i] = e.b[2 * i], p.b[4 + i] = e.b[2 * i + 1];
+    p.a[E / 2 + i] = e.b[2 * i], p.b[E / 2 + i] = e.b[2 * i + 1];
   }
   return p;
 }
-__device__ __forceinline__ Pairs to_neighbours(const Pairs& p) {
-  Pairs e;
+template <int E> __device__ __forceinline__ Pairs<E> to_neighbours(const Pairs<E>& p) {
+  Pairs<E> e;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < E / 2; ++i) {
     e.a[2 * i] = p.a[i], e.a[2 * i + 1] = p.b[i];
-    e.b[2 * i] = p.a[4 + i], e.b[2 * i + 1] = p.b[4 + i];
+    e.b[2 * i] = p.a[E / 2 + i], e.b[2 * i + 1] = p.b[E / 2 + i];
   }
   return e;
 }
-template <typename T, bool kNeighbours> __device__ __forceinline__ Pairs load_pairs(const T* v, const LanePairs& l) {
-  Pairs p;
-  load8(v + l.a, p.a);
-  load8(v + l.b, p.b);
-  return kNeighbours ? from_neighbours(p) : p;
-}
+// The pairs of a run as it lies in memory: a load on its way.
+template <typename T> struct RawPairs {
+  u32x4 a, b;
+  __device__ __forceinline__ void load(const T* v, const LanePairs& l) {
+    a = *(const u32x4*)(v + l.a);
+    b = *(const u32x4*)(v + l.b);
+  }
+  template <bool kNeighbours> __device__ __forceinline__ Pairs<kRun<T>> pairs() const {
+    Pairs<kRun<T>> p;
+    unpack<T>(a, p.a);
+    unpack<T>(b, p.b);
+    if constexpr (kNeighbours) return from_neighbours(p);
+    return p;
+  }
+};
 template <typename T, bool kNeighbours>
-__device__ __forceinline__ void store_pairs(T* v, const LanePairs& l, const Pairs& x) {
-  const Pairs p = kNeighbours ? to_neighbours(x) : x;
-  store8(v + l.a, p.a);
-  store8(v + l.b, p.b);
+__device__ __forceinline__ void store_pairs(T* v, const LanePairs& l, const Pairs<kRun<T>>& x) {
+  if constexpr (kNeighbours) {
+    store_run(v + l.a, [&](int i) { return i % 2 == 0 ? x.a[i / 2] : x.b[i / 2]; });
+    store_run(v + l.b, [&](int i) { return i % 2 == 0 ? x.a[(kRun<T> + i) / 2] : x.b[(kRun<T> + i) / 2]; });
+  } else {
+    store_run(v + l.a, [&](int i) { return x.a[i]; });
+    store_run(v + l.b, [&](int i) { return x.b[i]; });
+  }
 }
-template <bool kNeighbours>
-__device__ __forceinline__ Pairs load_weight(const void* w, int w_bf16, const LanePairs& l) {
-  if (w_bf16 != 0) return load_pairs<bf16, kNeighbours>((const bf16*)w, l);
-  return load_pairs<float, kNeighbours>((const float*)w, l);
+// The lane's elements of a weight, whose type may be another than the heads'.
+template <int E, bool kNeighbours>
+__device__ __forceinline__ Pairs<E> load_weight(const void* w, int w_bf16, const LanePairs& l) {
+  Pairs<E> p;
+  auto load = [&](auto w) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) p.a[i] = (float)w[l.a + i], p.b[i] = (float)w[l.b + i];
+  };
+  if (w_bf16 != 0)
+    load((const bf16*)w);
+  else
+    load((const float*)w);
+  if constexpr (kNeighbours) return from_neighbours(p);
+  return p;
 }
 
 // x turned by the angles (sign 1) or back (-1).
-__device__ __forceinline__ Pairs turn(const Pairs& x, const Pairs& cs, float sign) {
-  Pairs y;
+template <int E> __device__ __forceinline__ Pairs<E> turn(const Pairs<E>& x, const Pairs<E>& cs, float sign) {
+  Pairs<E> y;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < E; ++i) {
     const float s = sign * cs.b[i];
     y.a[i] = __builtin_fmaf(x.a[i], cs.a[i], -(x.b[i] * s));
     y.b[i] = __builtin_fmaf(x.a[i], s, x.b[i] * cs.a[i]);
   }
   return y;
 }
-template <class F> __device__ __forceinline__ Pairs each(F&& f) {
-  Pairs y;
+template <int E, class F> __device__ __forceinline__ Pairs<E> each(F&& f) {
+  Pairs<E> y;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    y.a[i] = f([i](const Pairs& p) { return p.a[i]; });
-    y.b[i] = f([i](const Pairs& p) { return p.b[i]; });
+  for (int i = 0; i < E; ++i) {
+    y.a[i] = f([i](const Pairs<E>& p) { return p.a[i]; });
+    y.b[i] = f([i](const Pairs<E>& p) { return p.b[i]; });
   }
   return y;
 }
-template <int LPV> __device__ __forceinline__ float dot(const Pairs& x, const Pairs& y) {
+template <int LPV, int E> __device__ __forceinline__ float dot(const Pairs<E>& x, const Pairs<E>& y) {
   float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) s = __builtin_fmaf(x.a[i], y.a[i], __builtin_fmaf(x.b[i], y.b[i], s));
+  for (int i = 0; i < E; ++i) s = __builtin_fmaf(x.a[i], y.a[i], __builtin_fmaf(x.b[i], y.b[i], s));
   return vector_sum<LPV>(s);
 }
 
@@ -178,60 +215,74 @@ template <int D> struct AngleMem {
   float cs[2][kMaxTokens][kStride];
 };
 
+// What one vector's work reads.
+template <typename T> struct VectorIn {
+  RawPairs<T> x, g, u;
+};
+template <typename T, int kMode>
+__device__ __forceinline__ void load_vector(const RotaryArgs& a, int k, int64_t b, int h, int64_t n, const LanePairs& l,
+                                            bool norm, VectorIn<T>& v) {
+  auto at = [&](const Heads& t) { return (const T*)t.data + b * t.b + h * t.h + n * t.n; };
+  if (kMode == 0 || norm) v.x.load(at(a.x[k]), l);
+  if (kMode == 1 || (kMode == 2 && norm)) v.g.load(at(a.dy[k]), l);
+  if (kMode == 2 && a.u[k].data != nullptr) v.u.load(at(a.u[k]), l);
+}
+
 // One vector's work; kMode 0: y (or, with sign -1 and no weights, x from y); 1: dx, dw; 2: x~, dy~, w~.
 template <typename T, int D, int kMode, bool kNeighbours>
 __device__ __forceinline__ void rotary_vector(const RotaryArgs& a, int k, int64_t b, int h, int64_t n,
-                                              const LanePairs& l, const Pairs& cs, bool norm, const Pairs& w,
-                                              const Pairs& uw, Pairs& sum) {
-  constexpr int LPV = D / 16;
-  auto at = [&](const Heads& v) { return (T*)v.data + b * v.b + h * v.h + n * v.n; };
+                                              const LanePairs& l, const Pairs<kRun<T>>& cs, bool norm,
+                                              const Pairs<kRun<T>>& w,
+                                              const Pairs<kRun<T>>& uw, const VectorIn<T>& v,
+                                              Pairs<kRun<T>>& sum) {
+  constexpr int LPV = kLanes<T, D>, E = kRun<T>;
+  auto at = [&](const Heads& t) { return (T*)t.data + b * t.b + h * t.h + n * t.n; };
   if constexpr (kMode == 0) {
-    Pairs x = load_pairs<T, kNeighbours>(at(a.x[k]), l);
+    Pairs<E> x = v.x.template pairs<kNeighbours>();
     if (norm) {
       const float r = rsqrtf(dot<LPV>(x, x) * (1.f / D) + a.eps);
-      x = each([&](auto of) { return of(x) * r * of(w); });
+      x = each<E>([&](auto of) { return of(x) * r * of(w); });
     }
     store_pairs<T, kNeighbours>(at(a.out[k]), l, turn(x, cs, 1.f));
   } else if constexpr (kMode == 1) {
-    Pairs g = load_pairs<T, kNeighbours>(at(a.dy[k]), l);
+    Pairs<E> g = v.g.template pairs<kNeighbours>();
     if (!norm) {
       store_pairs<T, kNeighbours>(at(a.out[k]), l, turn(g, cs, -1.f));
       return;
     }
-    Pairs x = load_pairs<T, kNeighbours>(at(a.x[k]), l);
+    Pairs<E> x = v.x.template pairs<kNeighbours>();
     g = turn(g, cs, -1.f);
     const float r = rsqrtf(dot<LPV>(x, x) * (1.f / D) + a.eps);
-    x = each([&](auto of) { return of(x) * r; });
-    const Pairs aw = each([&](auto of) { return of(w) * of(g); });
+    x = each<E>([&](auto of) { return of(x) * r; });
+    const Pairs<E> aw = each<E>([&](auto of) { return of(w) * of(g); });
     const float B = dot<LPV>(aw, x) * (1.f / D);
-    sum = each([&](auto of) { return __builtin_fmaf(of(g), of(x), of(sum)); });
+    sum = each<E>([&](auto of) { return __builtin_fmaf(of(g), of(x), of(sum)); });
     store_pairs<T, kNeighbours>(at(a.out[k]), l,
-                                each([&](auto of) { return r * __builtin_fmaf(-B, of(x), of(aw)); }));
+                                each<E>([&](auto of) { return r * __builtin_fmaf(-B, of(x), of(aw)); }));
   } else {
-    Pairs u;
+    Pairs<E> u;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) u.a[i] = u.b[i] = 0.f;
-    if (a.u[k].data != nullptr) u = load_pairs<T, kNeighbours>(at(a.u[k]), l);
+    for (int i = 0; i < E; ++i) u.a[i] = u.b[i] = 0.f;
+    if (a.u[k].data != nullptr) u = v.u.template pairs<kNeighbours>();
     if (!norm) {
       store_pairs<T, kNeighbours>(at(a.dyt[k]), l, turn(u, cs, 1.f));
       return;
     }
-    Pairs g = load_pairs<T, kNeighbours>(at(a.dy[k]), l);
-    Pairs x = load_pairs<T, kNeighbours>(at(a.x[k]), l);
+    Pairs<E> g = v.g.template pairs<kNeighbours>(), x = v.x.template pairs<kNeighbours>();
     g = turn(g, cs, -1.f);
     const float r = rsqrtf(dot<LPV>(x, x) * (1.f / D) + a.eps);
-    x = each([&](auto of) { return of(x) * r; });
-    const Pairs aw = each([&](auto of) { return of(w) * of(g); });
-    const Pairs ug = each([&](auto of) { return of(uw) * of(g); });
+    x = each<E>([&](auto of) { return of(x) * r; });
+    const Pairs<E> aw = each<E>([&](auto of) { return of(w) * of(g); });
+    const Pairs<E> ug = each<E>([&](auto of) { return of(uw) * of(g); });
     const float A = dot<LPV>(aw, u) * (1.f / D), B = dot<LPV>(aw, x) * (1.f / D);
     const float C = dot<LPV>(u, x) * (1.f / D), S = dot<LPV>(ug, x) * (1.f / D);
     const float by_x = __builtin_fmaf(3.f * r, B * C, -__builtin_fmaf(r, A, S));
-    sum = each([&](auto of) { return __builtin_fmaf(r * of(g), __builtin_fmaf(-C, of(x), of(u)), of(sum)); });
-    store_pairs<T, kNeighbours>(at(a.xt[k]), l, each([&](auto of) {
+    sum = each<E>([&](auto of) { return __builtin_fmaf(r * of(g), __builtin_fmaf(-C, of(x), of(u)), of(sum)); });
+    store_pairs<T, kNeighbours>(at(a.xt[k]), l, each<E>([&](auto of) {
                                   const float m = __builtin_fmaf(C, of(aw), B * of(u));
                                   return r * (of(ug) + __builtin_fmaf(by_x, of(x), -r * m));
                                 }));
-    const Pairs gt = each([&](auto of) {
+    const Pairs<E> gt = each<E>([&](auto of) {
       return __builtin_fmaf(r * of(w), __builtin_fmaf(-C, of(x), of(u)), of(uw) * of(x));
     });
     store_pairs<T, kNeighbours>(at(a.dyt[k]), l, turn(gt, cs, 1.f));
@@ -239,29 +290,35 @@ __device__ __forceinline__ void rotary_vector(const RotaryArgs& a, int k, int64_
 }
 
 // A workgroup takes a.tokens tokens at a time, for which it makes the angles once, and shares the
-// heads of each out over 256 / (d / 16) / tokens slots of d / 16 lanes.
+// heads of each out over 256 / LPV / tokens slots of LPV lanes.
 template <typename T, int D, int kMode, bool kNeighbours>
 __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a) {
-  constexpr int LPV = D / 16, kSlots = kRotaryThreads / LPV;
+  constexpr int LPV = kLanes<T, D>, E = kRun<T>, kSlots = kRotaryThreads / LPV;
   __shared__ union Mem {
     AngleMem<D> angles;
     float rows[kMode == 0 ? 1 : kSlots][D];
   } mem;
   const int slot = threadIdx.x / LPV, p = threadIdx.x % LPV;
   const int token = slot % a.tokens, hs = slot / a.tokens, head_slots = kSlots / a.tokens;
-  const LanePairs l = lane_pairs<kNeighbours>(p, a.pairs);
+  const LanePairs l = lane_pairs<T, D, kNeighbours>(p, a.pairs);
   const int64_t tokens = (int64_t)a.B * a.N;
   // blockIdx.y: the queries' heads, then the keys'
   const int k = blockIdx.y;
   const bool norm = a.w[k] != nullptr;
-  Pairs w, uw, sum;
+  Pairs<E> w, uw, sum;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w.a[i] = w.b[i] = 1.f, uw.a[i] = uw.b[i] = sum.a[i] = sum.b[i] = 0.f;
+  for (int i = 0; i < E; ++i) w.a[i] = w.b[i] = 1.f, uw.a[i] = uw.b[i] = sum.a[i] = sum.b[i] = 0.f;
   if (norm) {
-    w = load_weight<kNeighbours>(a.w[k], a.w_bf16, l);
-    if (kMode == 2 && a.uw[k] != nullptr) uw = load_weight<kNeighbours>(a.uw[k], a.w_bf16, l);
+    w = load_weight<E, kNeighbours>(a.w[k], a.w_bf16, l);
+    if (kMode == 2 && a.uw[k] != nullptr) uw = load_weight<E, kNeighbours>(a.uw[k], a.w_bf16, l);
   }
   for (int64_t t0 = (int64_t)blockIdx.x * a.tokens; t0 < tokens; t0 += (int64_t)gridDim.x * a.tokens) {
+    // a vector is on its way while the angles, or the one before it, are worked on
+    const int64_t t = t0 + token;
+    const unsigned b = (unsigned)t / (unsigned)a.N, n = (unsigned)t - b * (unsigned)a.N;  // t < 2^31, or not used
+    const int heads = t < tokens ? a.H[k] : 0;
+    VectorIn<T> v;
+    if (hs < heads) load_vector<T, kMode>(a, k, b, hs, n, l, norm, v);
     for (int x = threadIdx.x; x < a.tokens * a.pairs; x += kRotaryThreads) {
       const int tk = x / a.pairs, pair = x - tk * a.pairs;
       const int axis = a.axes != nullptr ? min(max(a.axes[pair], 0), a.num_axes - 1) : 0;
@@ -273,26 +330,27 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a) {
       mem.angles.cs[1][tk][pair] = a.sign * s;
     }
     __syncthreads();
-    Pairs cs;
+    Pairs<E> cs;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      cs.a[i] = l.turned ? mem.angles.cs[0][token][l.pair + i] : 1.f;
-      cs.b[i] = l.turned ? mem.angles.cs[1][token][l.pair + i] : 0.f;
+    for (int i = 0; i < E; ++i) {
+      const int half = i / (E / 2), pair = l.pair[half] + i % (E / 2);
+      cs.a[i] = l.turned[half] ? mem.angles.cs[0][token][pair] : 1.f;
+      cs.b[i] = l.turned[half] ? mem.angles.cs[1][token][pair] : 0.f;
     }
     __syncthreads();
-    const int64_t t = t0 + token;
-    if (t < tokens) {
-      const int64_t b = t / a.N, n = t - b * a.N;
-      for (int h = hs; h < a.H[k]; h += head_slots)
-        rotary_vector<T, D, kMode, kNeighbours>(a, k, b, h, n, l, cs, norm, w, uw, sum);
+    for (int h = hs; h < heads; h += head_slots) {
+      const VectorIn<T> now = v;
+      if (h + head_slots < heads) load_vector<T, kMode>(a, k, b, h + head_slots, n, l, norm, v);
+      rotary_vector<T, D, kMode, kNeighbours>(a, k, b, h, n, l, cs, norm, w, uw, now, sum);
     }
   }
   if constexpr (kMode != 0) {
     if (a.sums == nullptr || !norm) return;
     // the workgroup's sums in one row
-    Pairs e = kNeighbours ? to_neighbours(sum) : sum;
+    Pairs<E> e = sum;
+    if constexpr (kNeighbours) e = to_neighbours(sum);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < E; ++i) {
       mem.rows[slot][l.a + i] = e.a[i];
       mem.rows[slot][l.b + i] = e.b[i];
     }
@@ -383,16 +441,22 @@ struct RotaryPlan {
   int tokens;
   int64_t groups;
 };
-// As many tokens at a time as leave kEnough workgroups.  Calls that sum a weight's gradient have at most kMaxSums
-// rows of sums a weight; a launch takes fewer than 2^32 threads (kMaxBlocks: 2^31).  Workgroups go on to further
-// tokens.
+// At least as many tokens at a time as leave no slot without a head (bf16 B2 H12 N2047 d64, whose
+// 32 slots met 12 heads: 12.8 us forward), and more while kEnough workgroups are left.  Calls
+// that sum a weight's gradient have at most kMaxSums rows of sums a weight, in workgroups that go
+// on to as many further tokens as each other; a launch takes fewer than 2^32 threads.
 constexpr int64_t kEnough = 1024, kMaxSums = 1024, kMaxBlocks = int64_t(1) << 22;
 static RotaryPlan rotary_plan(const RotaryProblem& p, bool sums) {
   RotaryPlan c;
   const int64_t all = p.B * p.N;
-  c.tokens = std::min<int>(kMaxTokens, kRotaryThreads / (int)(p.d / 16));
-  while (c.tokens > 1 && all < kEnough * c.tokens) c.tokens /= 2;
-  c.groups = std::min((all + c.tokens - 1) / c.tokens, sums ? kMaxSums : kMaxBlocks);
+  const int slots = kRotaryThreads / ((int)p.d / (p.dtype == BOB_BF16 ? 16 : 8)), most = std::min(kMaxTokens, slots);
+  auto groups = [&] { return (all + c.tokens - 1) / c.tokens; };
+  c.tokens = 1;
+  while (c.tokens < most && slots / (2 * c.tokens) >= std::max(p.H, p.Hkv)) c.tokens *= 2;
+  while (c.tokens < most && all >= 2 * kEnough * c.tokens) c.tokens *= 2;
+  while (sums && c.tokens < most && groups() > kMaxSums) c.tokens *= 2;
+  const int64_t limit = sums ? kMaxSums : kMaxBlocks, each = (groups() + limit - 1) / limit;
+  c.groups = (groups() + each - 1) / std::max<int64_t>(each, 1);
   return c;
 }
 static int64_t rotary_bytes(const RotaryProblem& p) {

@@ -980,8 +980,8 @@ Tensor made_readable(const Tensor& t) {
 }
 bool tokens_first(const Tensor& t) { return t.stride(1) < t.stride(2); }
 Tensor heads_empty(const Tensor& t, bool first) {
-  return first ? at::empty({t.size(0), t.size(2), t.size(1), t.size(3)}, t.options()).transpose(1, 2)
-               : at::empty(t.sizes(), t.options());
+  const int64_t H = t.size(1), N = t.size(2), d = t.size(3);
+  return first ? at::empty_strided(t.sizes(), {N * H * d, d, H * d, 1}, t.options()) : at::empty(t.sizes(), t.options());
 }
 attn_heads heads(const Tensor& t) {
   if (!t.defined()) return attn_heads{};
