@@ -191,15 +191,17 @@ __device__ __forceinline__ void score_mask(floatx4& x0, floatx4& x1, int s0, Int
   }
 }
 
-// -m |distance| of a tile's two halves, a 16-row block of the stationary side: `first` is the
-// distance at sb = 0, r = 0, kSign its step along the streamed side (rows: the keys stream).
-// Uncapped scores start their MFMA there, with m in units of Q K^T; capped ones add it.
-template <int kSign> __device__ __forceinline__ floatx4 score_distance(int sb, int first, float m) {
+// x[sb] - m |distance|, of a tile and a 16-row block of the stationary side: `first` is the distance
+// at sb = 0, r = 0, kSign its step along the streamed side (rows: the keys stream).  m is in units
+// of Q K^T, or of the cap, so that the scores' factor and L meet them in one operation.
+template <int kSign>
+__device__ __forceinline__ void score_distance(floatx4& x0, floatx4& x1, int first, float m) {
   const float d = (float)first;
-  floatx4 x;
 #pragma unroll
-  for (int r = 0; r < 4; ++r) x[r] = -m * fabsf(d + (float)(kSign * (16 * sb + r)));
-  return x;
+  for (int r = 0; r < 4; ++r) {
+    x0[r] = __builtin_fmaf(-m, fabsf(d + (float)(kSign * r)), x0[r]);
+    x1[r] = __builtin_fmaf(-m, fabsf(d + (float)(kSign * (16 + r))), x1[r]);
+  }
 }
 // log2(e) tau, or something of no effect that can be divided by where tau is 0.
 __device__ __forceinline__ float score_scale(float scale) {
@@ -273,28 +275,20 @@ struct ScoreRows {
   }
 };
 
-// The slope of a row kernel's lane, of one head (folded rows have one row a lane): in log2 units
-// for capped scores, else in units of Q K^T.
-template <bool kCap, typename Rows>
+// The slope of a row kernel's lane, of one head (folded rows have one row a lane); c: the scores'
+// factor.
+template <typename Rows>
 __device__ __forceinline__ float score_row_slope(const ScoreArgs& a, const Rows& rw, float c) {
   if (a.slopes == nullptr) return 0.f;
-  const float m = a.slopes[rw.head(0)] * kLog2e;
-  return kCap ? m : m / c;
+  return a.slopes[rw.head(0)] * kLog2e / c;
 }
-// Where the scores of rows mb of the tile at s0 start.
-template <bool kCap, int MR, typename Rows>
-__device__ __forceinline__ void score_row_start(const ScoreArgs& a, const Rows& rw, int s0, float slope,
-                                                floatx4 (&s)[2][MR]) {
+template <int MR, typename Rows>
+__device__ __forceinline__ void score_row_distance(const ScoreArgs& a, const Rows& rw, int s0, float slope,
+                                                   floatx4 (&s)[2][MR]) {
+  if (a.slopes == nullptr) return;
 #pragma unroll
-  for (int mb = 0; mb < MR; ++mb) s[0][mb] = s[1][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
-  if (!kCap && a.slopes != nullptr) {
-#pragma unroll
-    for (int mb = 0; mb < MR; ++mb) {
-      const int first = rw.pos(mb) - s0 - 4 * (lane_id() >> 4);
-      s[0][mb] = score_distance<-1>(0, first, slope);
-      s[1][mb] = score_distance<-1>(1, first, slope);
-    }
-  }
+  for (int mb = 0; mb < MR; ++mb)
+    score_distance<-1>(s[0][mb], s[1][mb], rw.pos(mb) - s0 - 4 * (lane_id() >> 4), slope);
 }
 
 // x rounded to T, and what that leaves.
@@ -320,14 +314,33 @@ __device__ __forceinline__ float add_rounded(const Elt<bf16>::TFrag& f, float su
   return sum;
 }
 
-// An operand in twice the bits of bf16: its rounding and what that left.  fp32 needs one.
+// {-1, 0} and {0, -1} as bf16 pairs, in a register: as the instruction's own constant the
+// assembler writes {-1, 0} as -1.0, which the instruction reads as {0, -1}.
+template <int kAt> __device__ __forceinline__ auto minus_one() {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  unsigned bits = kAt == 0 ? 0x0000bf80u : 0xbf800000u;
+  asm("" : "+s"(bits));
+  return __builtin_bit_cast(bf16x2, bits);
+}
+// An operand in twice the bits of bf16: its rounding and what that left, x - hi in one dot
+// product of two (subtracting the unpacked value takes two instructions).  fp32 needs one.
+// Elements are set in ascending order.
 template <typename T> struct SplitFrag {
   using E = Elt<T>;
   static constexpr bool kTwo = sizeof(T) == 2;
   typename E::TFrag hi, lo;
+  float before;  // element i - 1
   __device__ __forceinline__ void set(int i, float x) {
     hi.set(i, x);
-    if constexpr (kTwo) lo.set(i, x - (float)hi.v[i]);
+    if constexpr (kTwo) {
+      typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+      if (i % 2 != 0) {
+        const bf16x2 pair = {hi.v[i - 1], hi.v[i]};
+        lo.set(i - 1, __builtin_amdgcn_fdot2_f32_bf16(pair, minus_one<0>(), before, false));
+        lo.set(i, __builtin_amdgcn_fdot2_f32_bf16(pair, minus_one<1>(), x, false));
+      }
+      before = x;
+    }
   }
   __device__ __forceinline__ floatx4 mma_acc(const typename E::AFrag& a, floatx4 c) const {
     c = E::mma_acc(a, hi, c);
@@ -376,12 +389,12 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_fwd_kernel(
     lsum[mb] = rsum[mb] = 0.f;
   }
   const float c = kCap ? a.cap_out : score_scale(a.scale);
-  const float slope = score_row_slope<kCap>(a, rw, c);
+  const float slope = score_row_slope(a, rw, c);
   floatx4 s[2][MR];
   typename E::TFrag pf[MR];
 
-  // s times cf are the scores in log2 units (1 where a bias went into capped ones)
-  auto softmax_step = [&](int s0, int mode, float cf) {
+  // s times c are the scores in log2 units
+  auto softmax_step = [&](int s0, int mode) {
     float p[MR][8], ls[MR];
     bool grown = false;
     floatx4 e[MR][2];
@@ -390,7 +403,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_fwd_kernel(
 #pragma unroll
       for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) e[mb][sb][r] = __builtin_fmaf(s[sb][mb][r], cf, -mrun[mb]);
+        for (int r = 0; r < 4; ++r) e[mb][sb][r] = __builtin_fmaf(s[sb][mb][r], c, -mrun[mb]);
     }
     if (mode == 2) {
 #pragma unroll
@@ -411,7 +424,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_fwd_kernel(
 #pragma unroll
         for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) x[sb][r] = s[sb][mb][r] * cf;
+          for (int r = 0; r < 4; ++r) x[sb][r] = s[sb][mb][r] * c;
         if (mode == 2) score_mask(x[0], x[1], s0, rw.keys[mb]);
         float mx = -INFINITY;
 #pragma unroll
@@ -460,7 +473,8 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_fwd_kernel(
         if (mode == 0) return;
         const T FB_LDS* Ks = (const T FB_LDS*)sm.lds[ks][st];
         const T FB_LDS* Vs = Ks + G::kTileElems;
-        score_row_start<kCap>(a, rw, s0, slope, s);
+#pragma unroll
+        for (int x = 0; x < MR; ++x) s[0][x] = s[1][x] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
@@ -469,20 +483,9 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_fwd_kernel(
 #pragma unroll
             for (int mb = 0; mb < MR; ++mb) s[sb][mb] = E::mma_chunk(ak, qf[mb][kk], s[sb][mb]);
           }
-        float cf = c;
-        if constexpr (kCap) {
-          cap_tile<T>(a, s, s);
-          if (a.slopes != nullptr) {
-            cf = 1.f;
-#pragma unroll
-            for (int mb = 0; mb < MR; ++mb) {
-              const int first = rw.pos(mb) - s0 - 4 * g;
-#pragma unroll
-              for (int sb = 0; sb < 2; ++sb) s[sb][mb] = s[sb][mb] * c + score_distance<-1>(sb, first, slope);
-            }
-          }
-        }
-        softmax_step(s0, mode, cf);
+        if constexpr (kCap) cap_tile<T>(a, s, s);
+        score_row_distance(a, rw, s0, slope, s);
+        softmax_step(s0, mode);
 #pragma unroll
         for (int nb = 0; nb < G::kNB; ++nb) {
           const typename E::AFrag av = G::load_afrag(Vs, 16 * nb);
@@ -601,26 +604,18 @@ __device__ __forceinline__ float cap_slope(float t) { return __builtin_fmaf(-t, 
 template <typename T, bool kCap, int MR, int A, int B, typename Rows>
 __device__ __forceinline__ void score_row_exponents(const ScoreArgs& a, const Rows& rw, float slope, float c, int s0,
                                                     const float (&lb)[MR], floatx4 (&s)[2][MR], floatx4 (&t)[A][B]) {
-  if constexpr (kCap) cap_tile<T>(a, s, t);
+  if constexpr (kCap) {
+    cap_tile<T>(a, s, t);
+#pragma unroll
+    for (int mb = 0; mb < MR; ++mb) s[0][mb] = t[0][mb], s[1][mb] = t[1][mb];
+  }
+  score_row_distance(a, rw, s0, slope, s);
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb)
 #pragma unroll
     for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        if constexpr (kCap)
-          s[sb][mb][r] = __builtin_fmaf(t[sb][mb][r], c, -lb[mb]);
-        else
-          s[sb][mb][r] = __builtin_fmaf(s[sb][mb][r], c, -lb[mb]);
-      }
-  if (kCap && a.slopes != nullptr) {
-#pragma unroll
-    for (int mb = 0; mb < MR; ++mb) {
-      const int first = rw.pos(mb) - s0 - 4 * (lane_id() >> 4);
-#pragma unroll
-      for (int sb = 0; sb < 2; ++sb) s[sb][mb] += score_distance<-1>(sb, first, slope);
-    }
-  }
+      for (int r = 0; r < 4; ++r) s[sb][mb][r] = __builtin_fmaf(s[sb][mb][r], c, -lb[mb]);
 }
 
 // ===========================================================================
@@ -678,7 +673,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_rows_kernel(
 #pragma unroll
     for (int mb = 0; mb < MR; ++mb) acc[nb][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
   const float c = kCap ? a.cap_out : score_scale(a.scale);
-  const float slope = score_row_slope<kCap>(a, rw, c);
+  const float slope = score_row_slope(a, rw, c);
   floatx4 s[2][MR], dp[2][MR], t[kCap ? 2 : 1][kCap ? MR : 1];
   SplitFrag<T> dsf[MR];
 
@@ -699,7 +694,8 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_rows_kernel(
         if (mode == 0) return;
         const T FB_LDS* Ks = (const T FB_LDS*)sm.lds[ks][st];
         const T FB_LDS* Vs = Ks + G::kTileElems;
-        score_row_start<kCap>(a, rw, s0, slope, s);
+#pragma unroll
+        for (int x = 0; x < MR; ++x) s[0][x] = s[1][x] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
@@ -836,74 +832,58 @@ struct ScoreCols {
   __device__ __forceinline__ int tile(int f) const { return t0 + (heads == 1 ? f : f % per_head); }
 };
 
-// The slopes of a key/value head's query heads in log2 units: in LDS, and that of a workgroup with
+// The slopes of a key/value head's query heads, as score_row_slope(): in LDS, and that of a workgroup with
 // one head in a register (read from LDS in every tile it held up the first MFMA).
 struct ColSlopes {
   const float FB_LDS* all;
   float one = 0.f;
   template <typename Cols>
-  __device__ __forceinline__ ColSlopes(const ScoreArgs& a, const Cols& cl, float* mem, int threads) {
+  __device__ __forceinline__ ColSlopes(const ScoreArgs& a, const Cols& cl, float* mem, int threads, float c) {
     float FB_LDS* const to = (float FB_LDS*)mem;
     all = to;
     if (a.slopes == nullptr) return;
     const float* const from = a.slopes + cl.kvh * a.grp % a.H;
-    one = from[cl.hq - cl.kvh * a.grp] * kLog2e;
-    for (int x = threadIdx.x; x < a.grp; x += threads) to[x] = from[x] * kLog2e;
+    one = from[cl.hq - cl.kvh * a.grp] * kLog2e / c;
+    for (int x = threadIdx.x; x < a.grp; x += threads) to[x] = from[x] * kLog2e / c;
     __syncthreads();
   }
 };
 
-// The slope of tile f's head, as score_row_slope().
-template <bool kCap, typename Cols>
-__device__ __forceinline__ float score_col_slope(const ScoreArgs& a, const Cols& cl, const ColSlopes& slopes, int f,
-                                                 float c) {
+// The slope of tile f's head.
+template <typename Cols>
+__device__ __forceinline__ float score_col_slope(const ScoreArgs& a, const Cols& cl, const ColSlopes& slopes, int f) {
   if (a.slopes == nullptr) return 0.f;
-  const float m = cl.heads == 1 ? slopes.one : scalar(slopes.all[cl.qhead(f) - cl.kvh * a.grp]);
-  return kCap ? m : m / c;
+  return cl.heads == 1 ? slopes.one : scalar(slopes.all[cl.qhead(f) - cl.kvh * a.grp]);
 }
-// The distance of the lane's first query of the tile at s0 from column block mc's key.
-template <typename Cols> __device__ __forceinline__ int score_col_first(const Cols& cl, int s0, int mc) {
+template <int MC, typename Cols>
+__device__ __forceinline__ void score_col_distance(const ScoreArgs& a, const Cols& cl, int s0, float slope,
+                                                   floatx4 (&s)[2][MC]) {
+  if (a.slopes == nullptr) return;
   const int l = lane_id();
-  return cl.start + s0 + 4 * (l >> 4) - (cl.col0 + 16 * mc + (l & 15));
-}
-template <bool kCap, int MC, typename Cols>
-__device__ __forceinline__ void score_col_start(const ScoreArgs& a, const Cols& cl, int s0, float slope,
-                                                floatx4 (&s)[2][MC]) {
 #pragma unroll
-  for (int mc = 0; mc < MC; ++mc) s[0][mc] = s[1][mc] = floatx4{0.f, 0.f, 0.f, 0.f};
-  if (!kCap && a.slopes != nullptr) {
-#pragma unroll
-    for (int mc = 0; mc < MC; ++mc) {
-      const int first = score_col_first(cl, s0, mc);
-      s[0][mc] = score_distance<1>(0, first, slope);
-      s[1][mc] = score_distance<1>(1, first, slope);
-    }
-  }
+  for (int mc = 0; mc < MC; ++mc)
+    score_distance<1>(s[0][mc], s[1][mc], cl.start + s0 + 4 * (l >> 4) - (cl.col0 + 16 * mc + (l & 15)), slope);
 }
 
-// A column kernel's raw scores -> the exponents of P; off: the row scalars.
+// A column kernel's raw scores -> the exponents of P; off: the row scalars.  Uncapped scores have
+// their distance before the first MFMA (after the last one bf16 d = 64 spilled, and Pass 2 of B4 H12
+// N4096 took 433 us for 409).
 template <typename T, bool kCap, int MC, int A, int B, typename Cols>
 __device__ __forceinline__ void score_col_exponents(const ScoreArgs& a, const Cols& cl, float slope, float c, int s0,
                                                     const float FB_LDS* off, floatx4 (&s)[2][MC], floatx4 (&t)[A][B]) {
-  if constexpr (kCap) cap_tile<T>(a, s, t);
+  if constexpr (kCap) {
+    cap_tile<T>(a, s, t);
+#pragma unroll
+    for (int mc = 0; mc < MC; ++mc) s[0][mc] = t[0][mc], s[1][mc] = t[1][mc];
+    score_col_distance(a, cl, s0, slope, s);
+  }
 #pragma unroll
   for (int sb = 0; sb < 2; ++sb) {
     const floatx4 o = *(const floatx4 FB_LDS*)(off + 16 * sb + 4 * (lane_id() >> 4));
 #pragma unroll
     for (int mc = 0; mc < MC; ++mc)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        if constexpr (kCap)
-          s[sb][mc][r] = __builtin_fmaf(t[sb][mc][r], c, o[r]);
-        else
-          s[sb][mc][r] = __builtin_fmaf(s[sb][mc][r], c, o[r]);
-      }
-  }
-  if (kCap && a.slopes != nullptr) {
-#pragma unroll
-    for (int mc = 0; mc < MC; ++mc)
-#pragma unroll
-      for (int sb = 0; sb < 2; ++sb) s[sb][mc] += score_distance<1>(sb, score_col_first(cl, s0, mc), slope);
+      for (int r = 0; r < 4; ++r) s[sb][mc][r] = __builtin_fmaf(s[sb][mc][r], c, o[r]);
   }
 }
 
@@ -950,13 +930,13 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_cols_kernel(
       kc.template issue<true>(ksrc, (T FB_LDS*)sm.kst[wl / kWPT], cl.col0, cl.klen);
     }
   }
-  const ColSlopes slopes(a, cl, slope_mem, KS * NW * 64);
+  const float c = kCap ? a.cap_out : score_scale(a.scale);
+  const ColSlopes slopes(a, cl, slope_mem, KS * NW * 64, c);
   floatx4 dk[G::kNB][MC], dv[G::kNB][MC];
 #pragma unroll
   for (int nb = 0; nb < G::kNB; ++nb)
 #pragma unroll
     for (int mc = 0; mc < MC; ++mc) dk[nb][mc] = dv[nb][mc] = floatx4{0.f, 0.f, 0.f, 0.f};
-  const float c = kCap ? a.cap_out : score_scale(a.scale);
   floatx4 s[2][MC], dp[2][MC], t[kCap ? 2 : 1][kCap ? MC : 1];
   typename E::TFrag pf[MC], dsf[MC];
 
@@ -994,8 +974,10 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_cols_kernel(
         const T FB_LDS* Qs = (const T FB_LDS*)sm.lds[ks][st];
         const T FB_LDS* dOs = Qs + G::kTileElems;
         const float FB_LDS* Ts = (const float FB_LDS*)sm.tsc[ks][ts];
-        const float slope = score_col_slope<kCap>(a, cl, slopes, flat(it), c);
-        score_col_start<kCap>(a, cl, s0, slope, s);
+        const float slope = score_col_slope(a, cl, slopes, flat(it));
+#pragma unroll
+        for (int x = 0; x < MC; ++x) s[0][x] = s[1][x] = floatx4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (!kCap) score_col_distance(a, cl, s0, slope, s);
 #pragma unroll
         for (int sb = 0; sb < 2; ++sb) {
           const floatx4 t1 = *(const floatx4 FB_LDS*)(Ts + kBS + 16 * sb + 4 * g);
@@ -1128,7 +1110,7 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
 #pragma unroll
   for (int mb = 0; mb < MR; ++mb) alpha[mb] = e0[mb] = 0.f;
   const float c = kCap ? a.cap_out : score_scale(a.scale);
-  const float slope = score_row_slope<kCap>(a, rw, c);
+  const float slope = score_row_slope(a, rw, c);
   floatx4 s[2][MR], dp[2][MR], f[2][MR], cc[2][MR], t[kCap ? 2 : 1][kCap ? MR : 1];
   typename E::TFrag fP[MR], fPdd[MR];  // of a cap: P, and u P in fB
   SplitFrag<T> fPF[MR], fPPt[MR], fB[MR];
@@ -1155,7 +1137,8 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
         const T FB_LDS* UKs = Vs + G::kTileElems;
         const T FB_LDS* UVs = UKs + G::kTileElems;
         if constexpr (std::is_same_v<T, bf16> && D == 128) __builtin_amdgcn_iglp_opt(3);
-        score_row_start<kCap>(a, rw, s0, slope, s);
+#pragma unroll
+        for (int x = 0; x < MR; ++x) s[0][x] = s[1][x] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
@@ -1402,13 +1385,13 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass2_kernel(
     load_stationary<T, D>(ukf[mc], UK + koff, col, cl.klen);
     load_stationary<T, D>(uvf[mc], UV + koff, col, cl.klen);
   }
-  const ColSlopes slopes(a, cl, slope_mem, KS * NW * 64);
+  const float c = kCap ? a.cap_out : score_scale(a.scale);
+  const ColSlopes slopes(a, cl, slope_mem, KS * NW * 64, c);
   floatx4 aK[G::kNB][MC], aV[G::kNB][MC];
 #pragma unroll
   for (int nb = 0; nb < G::kNB; ++nb)
 #pragma unroll
     for (int mc = 0; mc < MC; ++mc) aK[nb][mc] = aV[nb][mc] = floatx4{0.f, 0.f, 0.f, 0.f};
-  const float c = kCap ? a.cap_out : score_scale(a.scale);
   floatx4 s[2][MC], dp[2][MC], f[2][MC], cc[2][MC];
   typename E::TFrag fPh[MC], fSt[MC], fdS[MC];
 
@@ -1455,8 +1438,10 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass2_kernel(
         const T FB_LDS* UQs = Qs + G::kTileElems;
         const T FB_LDS* dOs = UQs + G::kTileElems;
         const float FB_LDS* Ts = (const float FB_LDS*)sm.tsc[ks][ts];
-        const float slope = score_col_slope<kCap>(a, cl, slopes, flat(it), c);
-        score_col_start<kCap>(a, cl, s0, slope, s);
+        const float slope = score_col_slope(a, cl, slopes, flat(it));
+#pragma unroll
+        for (int x = 0; x < MC; ++x) s[0][x] = s[1][x] = floatx4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (!kCap) score_col_distance(a, cl, s0, slope, s);
 #pragma unroll
         for (int sb = 0; sb < 2; ++sb) {
           const floatx4 t1 = *(const floatx4 FB_LDS*)(Ts + kBS + 16 * sb + 4 * g);
