@@ -468,7 +468,7 @@ def test_a_layer_from_projections_to_output():
     g64 = torch.autograd.grad(((y64 * keep) ** 2).sum() / 100, wide, create_graph=True)
     hv64 = torch.autograd.grad(sum((a * b.double()).sum() for a, b in zip(g64, dirs)), wide)
     # the fp32 model rounds each of its ten products and sums at 2^-24 of terms that cancel by at most a hundred: 1e-4
-    errs = [float((a.double() - b).norm() / b.norm()) for a, b in zip((y * keep, *g, *hv), (y64 * keep, *g64, *hv64))]
+    errs = [float(((a.double() - b).norm() / b.norm()).detach()) for a, b in zip((y * keep, *g, *hv), (y64 * keep, *g64, *hv64))]
     say("   output, gradients and products", [f"{e:.0e}" for e in errs])
     assert max(errs) <= 1e-4
     # the last token of entry 0, from a cache: no documents' first keys but its own document's
