@@ -24,11 +24,14 @@ ScoreArgs score_args(const ScoreProblem& p, const ExtPlan& c, int64_t heads, int
   a.spans = p.spans;
   a.slopes = p.slopes;
   if (p.cap > 0.f) {
-    a.cap_in = (float)((double)p.scale / p.cap * kCapArg<T>);
     a.cap_out = p.cap * kLog2e;
     a.cap_k = 2.f / p.cap;
-    const double x = (double)p.scale / p.cap;  // of a score of Q K^T = 1; 0: every tile is near
-    a.cap_near = x != 0 ? (float)std::min(kCapNear / std::fabs(x), 1e30) : 1e30f;
+    // x: S / c of a score of Q K^T = 1, taken into the polynomial while its powers stay in fp32
+    double x = (double)p.scale / p.cap;
+    a.cap_pre = std::fabs(x) >= 1e-4 && std::fabs(x) <= 1e4 ? 1.f : (float)x;
+    x = a.cap_pre == 1.f ? x : 1.0;
+    a.cap_in = (float)(x * kCapArg<T>);
+    a.cap_near = (float)(kCapNear / std::fabs(x));
     for (int i = 0; i < 5; ++i) a.cap_poly[i] = (float)(kCapPoly[i] * std::pow(x, 2 * i + 1));
   }
   return a;

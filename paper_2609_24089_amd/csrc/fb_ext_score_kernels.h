@@ -37,11 +37,12 @@ namespace fb {
 struct ScoreArgs : ExtArgs {
   const int32_t* spans;  // [B, Nk, 4]: k0, k1, q0, q1 of each position, or null: causal or dense
   const float* slopes;   // [H] or null: 0
-  float cap_in;          // S / c as an argument of tanh for cap_tanh()
+  float cap_pre;         // what Q K^T is multiplied by first: 1, or S / c where that is very small or large
+  float cap_in;          // from there to an argument of tanh for cap_tanh()
   float cap_out;         // c log2(e)
   float cap_k;           // 2 / c
-  float cap_near;        // |Q K^T| up to which the tanh is cap_poly's
-  float cap_poly[5];     // t = s (p0 + p1 s^2 + ... + p4 s^8), s = Q K^T
+  float cap_near;        // up to here the tanh is cap_poly's
+  float cap_poly[5];     // t = s (p0 + p1 s^2 + ... + p4 s^8)
 };
 
 // ---------------------------------------------------------------------------
@@ -83,9 +84,15 @@ constexpr double kCapNear = 0.9;
 constexpr double kCapPoly[5] = {0.9999867425076748, -0.3329870630439696, 0.13076785780676703, -0.04593852969671257,
                                 0.009843491590824895};
 
-// t = tanh(S / c) of a tile of raw scores.
+// t = tanh(S / c) of a tile of raw scores, which it may overwrite.
 template <typename T, int A, int B>
-__device__ __forceinline__ void cap_tile(const ScoreArgs& a, const floatx4 (&s)[A][B], floatx4 (&t)[A][B]) {
+__device__ __forceinline__ void cap_tile(const ScoreArgs& a, floatx4 (&s)[A][B], floatx4 (&t)[A][B]) {
+  if (a.cap_pre != 1.f) {
+#pragma unroll
+    for (int x = 0; x < A; ++x)
+#pragma unroll
+      for (int y = 0; y < B; ++y) s[x][y] *= a.cap_pre;
+  }
   if constexpr (sizeof(T) == 2) {
     float most = 0.f;
 #pragma unroll

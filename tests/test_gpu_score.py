@@ -435,6 +435,22 @@ def test_extreme_scores():
         assert nrel(L.double().cpu().numpy(), want["L"]) <= 1e-5, (tau, more)
 
 
+@pytest.mark.parametrize("cap", [1e-6, 1e-4, 1e6])
+@pytest.mark.parametrize("scale", [1.0, 0.0, 1e-7])
+def test_caps_far_from_the_scores(cap, scale):
+    """Scores that are 0 or far beyond their cap, and caps far beyond the scores."""
+    c = dict(B=1, H=2, Hkv=1, Nq=40, Nk=70, d=64, cap=cap, kv_lens=[67])
+    x = make(c, 77)
+    x["Q"][:, :, ::3] = 0
+    got = chain({n: t.cuda() for n, t in x.items()}, c, scale)
+    want = reference(x, c, scale)
+    for n in ("O", "L", "D", "dV", "dOt", "Vt"):
+        a, b = got[n].double().cpu().numpy(), want[n]
+        assert nrel(a, b) <= bar(n, "bf16"), n
+    for n in ("dQ", "dK", "Qt", "Kt", "alpha", "E"):
+        assert np.all(np.isfinite(got[n].double().cpu().numpy())), n
+
+
 def test_offsets_past_32_bits():
     """A key/value cache of more than 2^31 elements: the last entry's last keys, under spans and slopes."""
     import paper_2609_24089_amd as fb
