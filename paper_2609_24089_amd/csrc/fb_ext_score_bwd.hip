@@ -3,13 +3,16 @@
 
 namespace fb {
 
-// Three waves per SIMD (168 registers) for whole blocks at bf16 d = 64.
-template <typename T, int D> constexpr bool kThreeWaves = std::is_same_v<T, bf16> && D == 64;
+// Whole blocks at bf16 d = 64: 16 rows a wave and five waves per SIMD on the row side, three (168
+// registers) on the column side.  With 32 rows and three waves the row side of B4 H12 N4096 took,
+// causal with a cap, 287 us for 277, and under packed documents 74 for 63; the forward (151 for 147
+// us) and the column side (271 for 232) were slower with 16.
+template <typename T, int D> constexpr bool kNarrowHeads = std::is_same_v<T, bf16> && D == 64;
 
 template <typename T, int D> struct ScoreRowsBwd {
   static constexpr ExtShape shape(int form, bool capped) {
     constexpr Shape w = Cfg<T, D>::kRows;
-    return form == 0   ? ExtShape{w.mr, w.nw, kThreeWaves<T, D> ? 3 : w.occ, 1}
+    return form == 0   ? kNarrowHeads<T, D> ? ExtShape{1, 4, 4, 1} : ExtShape{w.mr, w.nw, w.occ, 1}
            : form == 4 ? ext_two_sets<T, D>(w, 2, 0)
                        : ext_sets<T, D>(kFormWaves[form], 2, 0, 16, w.occ);
   }
@@ -24,7 +27,7 @@ template <typename T, int D> struct ScoreColsBwd {
   static constexpr ExtShape shape(int form, bool capped) {
     constexpr Shape w = Cfg<T, D>::kCols;
     constexpr int waves = D * (int)sizeof(T) <= 128 ? 16 : 8;
-    return form == 0   ? ExtShape{w.mr, w.nw, kThreeWaves<T, D> ? 3 : w.occ, 1}
+    return form == 0   ? ExtShape{w.mr, w.nw, kNarrowHeads<T, D> ? 3 : w.occ, 1}
            : form == 4 ? ext_two_sets<T, D>(w, 2, 2 * kExtra + (w.kl ? 4 * Geo<T, D>::kTileElems * (int)sizeof(T) : 0))
            : form == 1 && D == 256
                ? kNotBuilt  // spilled 127 registers

@@ -9,7 +9,7 @@ import torch
 
 import paper_2609_24089_amd as fb
 from tests.parity_util import say
-from tests.test_gpu_ext_forms import COLS, DT, FORMS, FWD, KERNELS, OUTS, PASS2
+from tests.test_gpu_ext_forms import COLS, DT, FORMS, FWD, KERNELS, OUTS, PASS2, ROWS
 from tests.test_gpu_ext_rows import compare_rows
 from tests.test_gpu_score import chain
 
@@ -22,6 +22,8 @@ def built(kernel, dt, d, cap):
     """(rows of a workgroup, wave sets) of every kernel that is built."""
     if (kernel, dt, d) == (COLS, "bf16", 256):
         return {(128, 1), (32, 2), (16, 2)}
+    if (kernel, dt, d) == (ROWS, "bf16", 64):
+        return {(128, 2), (64, 1), (64, 4), (32, 8), (16, 8)}
     if (kernel, dt, d) == (PASS2, "bf16", 64) and cap:
         return {(64, 2), (64, 1), (32, 4), (16, 4)}
     return set(FORMS[kernel, dt, d])
