@@ -296,7 +296,7 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a) {
   constexpr int LPV = kLanes<T, D>, E = kRun<T>, kSlots = kRotaryThreads / LPV;
   __shared__ union Mem {
     AngleMem<D> angles;
-    float rows[kMode == 0 ? 1 : kSlots][D];
+    float rows[kMode == 0 ? 1 : kSlots][D + 4];  // four more: slots on different banks
   } mem;
   const int slot = threadIdx.x / LPV, p = threadIdx.x % LPV;
   const int token = slot % a.tokens, hs = slot / a.tokens, head_slots = kSlots / a.tokens;
@@ -357,10 +357,10 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a) {
     __syncthreads();
     float* const to = a.sums + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * D;
     for (int x = threadIdx.x; x < D; x += kRotaryThreads) {
-      float v = 0.f;
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int s = 0; s < kSlots; ++s) v += mem.rows[s][x];
-      to[x] = v;
+      for (int s = 0; s < kSlots; ++s) v[s & 3] += mem.rows[s][x];
+      to[x] = (v[0] + v[1]) + (v[2] + v[3]);
     }
   }
 }
