@@ -495,7 +495,8 @@ int32_t attn_score_pass1_rows(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, 
                               float scale, int32_t causal, const attn_score* score, const void* Q, const void* K,
                               const void* V, const void* O, const void* Orest, const void* dO, const void* gdQ,
                               const void* gdK, const void* gdV, const float* L, const float* D, const void* dQ,
-                              void* Qt, void* dOt, float* alpha, float* E, void* workspace, int64_t workspace_bytes, void* stream);
+                              void* Qt, void* dOt, float* alpha, float* E, void* workspace, int64_t workspace_bytes,
+                              void* stream);
 
 /* BoB Pass 2, after Pass 1.  In: Q, K, V, dO, gdQ, gdK, gdV, L, D, alpha, E.  Out: Kt, Vt. */
 int32_t attn_score_pass2_cols(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,

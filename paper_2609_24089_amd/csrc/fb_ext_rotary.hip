@@ -290,7 +290,9 @@ __device__ __forceinline__ void rotary_vector(const RotaryArgs& a, int k, int64_
 }
 
 // A workgroup takes a.tokens tokens at a time, for which it makes the angles once, and shares the
-// heads of each out over 256 / LPV / tokens slots of LPV lanes.
+// heads of each out over 256 / LPV / tokens slots of LPV lanes.  bf16, 16384 tokens, 16 + 8 heads of
+// 128: forward 37 us (5.5 TB/s), backward 62 (4.9 TB/s, with the weights' sums); 4094 tokens, 12 + 12
+// heads of 64: 10, 16 and 25 us, a chain of position, angles, vector and store a workgroup.
 template <typename T, int D, int kMode, bool kNeighbours>
 __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a) {
   constexpr int LPV = kLanes<T, D>, E = kRun<T>, kSlots = kRotaryThreads / LPV;

@@ -49,14 +49,14 @@ template <typename T, int D> ExtPlan score_rows_plan(const ScoreProblem& p);
 template <typename T, int D> ExtPlan score_cols_plan(const ScoreProblem& p);
 template <typename T, int D>
 int32_t score_launch_bwd(const ScoreProblem& p, const void* Q, const void* K, const void* V, const void* O,
-                         const void* Orest, const void* dO, const float* L, void* dQ, void* dK, void* dV, float* Dv, float* row_parts,
-                         float* parts, hipStream_t s);
+                         const void* Orest, const void* dO, const float* L, void* dQ, void* dK, void* dV, float* Dv,
+                         float* row_parts, float* parts, hipStream_t s);
 template <typename T, int D> ExtPlan score_pass1_plan(const ScoreProblem& p);
 template <typename T, int D>
 int32_t score_launch_pass1(const ScoreProblem& p, const void* Q, const void* K, const void* V, const void* O,
-                           const void* Orest, const void* dO, const void* UQ, const void* UK, const void* UV, const float* L,
-                           const float* Dv, const void* dQ, void* Qt, void* dOt, float* alpha, float* E, float* parts,
-                           hipStream_t s);
+                           const void* Orest, const void* dO, const void* UQ, const void* UK, const void* UV,
+                           const float* L, const float* Dv, const void* dQ, void* Qt, void* dOt, float* alpha,
+                           float* E, float* parts, hipStream_t s);
 template <typename T, int D> ExtPlan score_pass2_plan(const ScoreProblem& p);
 template <typename T, int D>
 int32_t score_launch_pass2(const ScoreProblem& p, const void* Q, const void* K, const void* V, const void* dO,

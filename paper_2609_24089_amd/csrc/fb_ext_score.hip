@@ -38,18 +38,19 @@ static ExtPlan plan_rows(const ScoreProblem& p) { FB_EXT_DISPATCH(p, score_rows_
 static ExtPlan plan_cols(const ScoreProblem& p) { FB_EXT_DISPATCH(p, score_cols_plan, p); }
 static ExtPlan plan_pass1(const ScoreProblem& p) { FB_EXT_DISPATCH(p, score_pass1_plan, p); }
 static ExtPlan plan_pass2(const ScoreProblem& p) { FB_EXT_DISPATCH(p, score_pass2_plan, p); }
-static int32_t go_fwd(const ScoreProblem& p, const void* Q, const void* K, const void* V, void* O, void* Orest, float* L,
-                      float* ws, hipStream_t s) {
+static int32_t go_fwd(const ScoreProblem& p, const void* Q, const void* K, const void* V, void* O, void* Orest,
+                      float* L, float* ws, hipStream_t s) {
   FB_EXT_DISPATCH(p, score_launch_fwd, p, Q, K, V, O, Orest, L, ws, s);
 }
 static int32_t go_bwd(const ScoreProblem& p, const void* Q, const void* K, const void* V, const void* O,
-                      const void* Orest, const void* dO, const float* L, void* dQ, void* dK, void* dV, float* D, float* row_parts,
-                      float* parts, hipStream_t s) {
+                      const void* Orest, const void* dO, const float* L, void* dQ, void* dK, void* dV, float* D,
+                      float* row_parts, float* parts, hipStream_t s) {
   FB_EXT_DISPATCH(p, score_launch_bwd, p, Q, K, V, O, Orest, dO, L, dQ, dK, dV, D, row_parts, parts, s);
 }
 static int32_t go_pass1(const ScoreProblem& p, const void* Q, const void* K, const void* V, const void* O,
                         const void* Orest, const void* dO, const void* UQ, const void* UK, const void* UV,
-                        const float* L, const float* D, const void* dQ, void* Qt, void* dOt, float* alpha, float* E, float* parts, hipStream_t s) {
+                        const float* L, const float* D, const void* dQ, void* Qt, void* dOt, float* alpha,
+                        float* E, float* parts, hipStream_t s) {
   FB_EXT_DISPATCH(p, score_launch_pass1, p, Q, K, V, O, Orest, dO, UQ, UK, UV, L, D, dQ, Qt, dOt, alpha, E, parts, s);
 }
 static int32_t go_pass2(const ScoreProblem& p, const void* Q, const void* K, const void* V, const void* dO,
@@ -104,7 +105,8 @@ int32_t attn_score_bwd(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t
   bool empty;
   const int32_t rc = fb::score_check(p, &empty);
   if (rc != BOB_OK || empty) return rc;
-  if (!fb::score_rest(Nq, Orest) || !fb::ext_ptrs(Nq, {Q, O, dO, L, dQ, D}) || !fb::ext_ptrs(Nk, {K, V, dK, dV})) return BOB_EINVAL;
+  if (!fb::score_rest(Nq, Orest) || !fb::ext_ptrs(Nq, {Q, O, dO, L, dQ, D}) || !fb::ext_ptrs(Nk, {K, V, dK, dV}))
+    return BOB_EINVAL;
   if (!fb::workspace_fits(fb::call_bytes(ATTN_SCORE_BWD, p), workspace, workspace_bytes)) return BOB_EINVAL;
   char* const ws = (char*)workspace;
   return fb::go_bwd(p, Q, K, V, O, Orest, dO, L, dQ, dK, dV, D, (float*)ws, (float*)(ws + fb::rows_bytes(p)),
@@ -114,13 +116,15 @@ int32_t attn_score_bwd(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t
 int32_t attn_score_pass1_rows(int32_t dtype, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
                               float scale, int32_t causal, const attn_score* score, const void* Q, const void* K,
                               const void* V, const void* O, const void* Orest, const void* dO, const void* gdQ,
-                              const void* gdK, const void* gdV, const float* L, const float* D, const void* dQ, void* Qt, void* dOt,
-                              float* alpha, float* E, void* workspace, int64_t workspace_bytes, void* stream) {
+                              const void* gdK, const void* gdV, const float* L, const float* D, const void* dQ,
+                              void* Qt, void* dOt, float* alpha, float* E, void* workspace, int64_t workspace_bytes,
+                              void* stream) {
   const ScoreProblem p = fb::score_problem(dtype, B, H, Hkv, Nq, Nk, d, scale, causal, score);
   bool empty;
   const int32_t rc = fb::score_check(p, &empty);
   if (rc != BOB_OK || empty || Nq == 0) return rc;
-  if (!fb::score_rest(Nq, Orest) || !fb::ext_ptrs(Nq, {Q, O, dO, gdQ, L, D, dQ, Qt, dOt, alpha, E}) || !fb::ext_ptrs(Nk, {K, V, gdK, gdV}))
+  if (!fb::score_rest(Nq, Orest) || !fb::ext_ptrs(Nq, {Q, O, dO, gdQ, L, D, dQ, Qt, dOt, alpha, E}) ||
+      !fb::ext_ptrs(Nk, {K, V, gdK, gdV}))
     return BOB_EINVAL;
   if (!fb::workspace_fits(fb::call_bytes(ATTN_SCORE_PASS1, p), workspace, workspace_bytes)) return BOB_EINVAL;
   return fb::go_pass1(p, Q, K, V, O, Orest, dO, gdQ, gdK, gdV, L, D, dQ, Qt, dOt, alpha, E, (float*)workspace,

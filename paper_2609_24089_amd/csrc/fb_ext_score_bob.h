@@ -52,13 +52,14 @@ template <typename T, int D> ExtPlan score_pass1_plan(const ScoreProblem& p) {
 template <typename T, int D>
 int32_t score_launch_pass1(const ScoreProblem& p, const void* Q, const void* K, const void* V, const void* O,
                            const void* Orest, const void* dO, const void* UQ, const void* UK, const void* UV,
-                           const float* L, const float* Dv, const void* dQ, void* Qt, void* dOt, float* alpha, float* E, float* parts,
-                           hipStream_t s) {
+                           const float* L, const float* Dv, const void* dQ, void* Qt, void* dOt, float* alpha,
+                           float* E, float* parts, hipStream_t s) {
   const ExtPlan c = score_pass1_plan<T, D>(p);
   const ScoreArgs a = score_args<T>(p, c, p.B * p.H, p.Nq);
   const int32_t rc = ext_dispatch<ScorePass1<T, D>>(
       c.form, p, dim3(a.total, c.parts), 0, s, a, (const T*)Q, (const T*)K, (const T*)V, (const T*)O,
-      (const T*)Orest, (const T*)dO, (const T*)UQ, (const T*)UK, (const T*)UV, L, Dv, (const T*)dQ, (T*)Qt, (T*)dOt, alpha, E, parts);
+      (const T*)Orest, (const T*)dO, (const T*)UQ, (const T*)UK, (const T*)UV, L, Dv, (const T*)dQ, (T*)Qt, (T*)dOt,
+      alpha, E, parts);
   if (rc != BOB_OK || c.parts == 1) return rc;
   const int64_t all = p.B * p.H * p.Nq;
   hipLaunchKernelGGL((score_pass1_join_kernel<T, D>), dim3((unsigned)((all * (D / 4) + 255) / 256)), dim3(256), 0, s, a,

@@ -61,8 +61,8 @@ template <typename T, int D> ExtPlan score_cols_plan(const ScoreProblem& p) {
 
 template <typename T, int D>
 int32_t score_launch_bwd(const ScoreProblem& p, const void* Q, const void* K, const void* V, const void* O,
-                         const void* Orest, const void* dO, const float* L, void* dQ, void* dK, void* dV, float* Dv, float* row_parts,
-                         float* parts, hipStream_t s) {
+                         const void* Orest, const void* dO, const float* L, void* dQ, void* dK, void* dV, float* Dv,
+                         float* row_parts, float* parts, hipStream_t s) {
   int32_t rc = BOB_OK;
   if (p.Nq > 0) {
     const ExtPlan r = score_rows_plan<T, D>(p);
@@ -87,8 +87,8 @@ int32_t score_launch_bwd(const ScoreProblem& p, const void* Q, const void* K, co
   template ExtPlan score_rows_plan<T, D>(const ScoreProblem&);                                                     \
   template ExtPlan score_cols_plan<T, D>(const ScoreProblem&);                                                     \
   template int32_t score_launch_bwd<T, D>(const ScoreProblem&, const void*, const void*, const void*, const void*, \
-                                          const void*, const void*, const float*, void*, void*, void*, float*, float*, float*,  \
-                                          hipStream_t);
+                                          const void*, const void*, const float*, void*, void*, void*, float*, float*,     \
+                                          float*, hipStream_t);
 FB_EXT_EACH(FB_INST)
 
 }  // namespace fb

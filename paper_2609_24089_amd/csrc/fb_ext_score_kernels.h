@@ -357,7 +357,11 @@ template <typename T> struct SplitFrag {
 };
 
 // ===========================================================================
-// Forward, as ext_fwd_kernel.  Orest may be null.
+// Forward, as ext_fwd_kernel.  Orest may be null.  Bound by MFMA and VALU issue for many rows: B1
+// H16 N8192 d128 causal with slopes 283 us, 0.97 PFLOP/s, the two busy for 84% of the cycles; a cap
+// takes 13 VALU operations an element for 7 (B4 H16 Hkv8 N4096 d128 causal 398 us for 320).  For a
+// few rows by the keys' and values' bytes: B16 H16 Hkv4, one token, up to 4096 keys, d128, 87 MB in
+// 21 us.
 // ===========================================================================
 template <typename T, int D, int MR, int NW, int OCC, int KS, bool kCap>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void score_fwd_kernel(
@@ -627,7 +631,9 @@ __device__ __forceinline__ void score_row_exponents(const ScoreArgs& a, const Ro
 
 // ===========================================================================
 // First backward, row side, as ext_bwd_rows_kernel.  A capped tile's t takes eight registers a
-// 16-row block from the exponent to the gradient of the score.
+// 16-row block from the exponent to the gradient of the score.  dS meets K as two bf16 values:
+// four contractions a tile for three.  Bound by MFMA (43% of the cycles) and VALU issue (62%),
+// which overlap little: B4 H16 Hkv8 N4096 d128 causal 525 us, with a cap 631.
 // ===========================================================================
 template <typename T, int D, int MR, int NW, int OCC, int KS, bool kCap>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_rows_kernel(
@@ -894,7 +900,8 @@ __device__ __forceinline__ void score_col_exponents(const ScoreArgs& a, const Co
   }
 }
 
-// First backward, column side, as ext_bwd_cols_kernel.
+// First backward, column side, as ext_bwd_cols_kernel (P and dS are summed over queries whose
+// roundings do not cancel: one bf16 value each).  Bound as the row side: 600 us there, with a cap 700.
 template <typename T, int D, int MC, int NW, int OCC, int KS, bool kKL, bool kCap>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_cols_kernel(
     ScoreArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ dO,
@@ -1074,7 +1081,10 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_cols_kernel(
 // alpha, e the sums of P F and P w, the epilogue's
 //   Qt = tau (sum P (u w - (2 / c) t (dP - D) F) k + sum u P (dP - D) u_K - e sum u P k) - alpha dQ
 //   dOt = sum P u_V + sum P F v - alpha O,  E = e - alpha D
-// needs, capped, one more operand, u P, beside P, which stays with u_V.
+// needs, capped, one more operand, u P, beside P, which stays with u_V.  P F, u P and Pt's operand
+// meet their matrices as two bf16 values each: thirteen contractions a tile for ten.  Bound by MFMA
+// and by a wave's chain of LDS reads, MFMA and exponentials at two or three waves a SIMD: B2 H16
+// N2048 d128 causal 220 us with slopes, 250 with a cap; B4 H12 N4096 d64 610 and 740.
 // ===========================================================================
 template <typename T, int D, int MR, int NW, int OCC, int KS, int kPF, bool kCap>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
@@ -1357,7 +1367,8 @@ __global__ __launch_bounds__(256) void score_pass1_join_kernel(ExtArgs a, const 
 }
 
 // ===========================================================================
-// BoB Pass 2, as ext_pass2_kernel.
+// BoB Pass 2, as ext_pass2_kernel.  Bound as Pass 1: B2 H16 N2048 d128 causal 160 us with slopes,
+// 183 with a cap; B4 H12 N4096 d64 430 and 570.
 // ===========================================================================
 template <typename T, int D, int MC, int NW, int OCC, int KS, bool kPF, bool kCap>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass2_kernel(
