@@ -32,7 +32,7 @@ ScoreArgs score_args(const ScoreProblem& p, const ExtPlan& c, int64_t heads, int
     x = a.cap_pre == 1.f ? x : 1.0;
     a.cap_in = (float)(x * kCapArg<T>);
     a.cap_near = (float)(kCapNear / std::fabs(x));
-    for (int i = 0; i < 5; ++i) a.cap_poly[i] = (float)(kCapPoly[i] * std::pow(x, 2 * i + 1));
+    for (int i = 0; i < 4; ++i) a.cap_poly[i] = (float)(kCapPoly[i] * std::pow(x, 2 * i + 1));
   }
   return a;
 }

@@ -42,7 +42,7 @@ struct ScoreArgs : ExtArgs {
   float cap_out;         // c log2(e)
   float cap_k;           // 2 / c
   float cap_near;        // up to here the tanh is cap_poly's
-  float cap_poly[5];     // t = s (p0 + p1 s^2 + ... + p4 s^8)
+  float cap_poly[4];     // t = s (p0 + p1 s^2 + p2 s^4 + p3 s^6)
 };
 
 // ---------------------------------------------------------------------------
@@ -76,13 +76,14 @@ template <> __device__ __forceinline__ float cap_tanh<float>(float s, float cap_
 }
 template <typename T> constexpr float kCapArg = std::is_same_v<T, bf16> ? 2.f * kLog2e : 1.f;  // of cap_in
 
-// tanh on |x| <= kCapNear by an odd polynomial, off by 1.1e-6 at most (the least for five terms;
+// tanh on |x| <= kCapNear by an odd polynomial, off by 1.1e-6 at most (the least for four terms;
 // 5e-5 of a score of c = 50, where P is rounded to 2^-9).  Scores of trained models lie far below
-// their cap, so whole tiles take it: 6 instructions an element for two transcendentals, at a
-// quarter of the rate, and three others.  cap_near and cap_poly are this in terms of Q K^T.
-constexpr double kCapNear = 0.9;
-constexpr double kCapPoly[5] = {0.9999867425076748, -0.3329870630439696, 0.13076785780676703, -0.04593852969671257,
-                                0.009843491590824895};
+// their cap, so whole tiles take it: 5 instructions an element for two transcendentals, at a
+// quarter of the rate, and three others.  (A fifth term reaches 0.9 for a sixth instruction: a
+// training pass of B4 H16 Hkv8 N4096 d128 causal 1497 us for 1470.)  cap_near and cap_poly are this
+// in terms of Q K^T.
+constexpr double kCapNear = 0.65;
+constexpr double kCapPoly[4] = {0.9999839352347103, -0.332806913691474, 0.12861559355416782, -0.03767224489906605};
 
 // t = tanh(S / c) of a tile of raw scores, which it may overwrite.
 template <typename T, int A, int B>
@@ -109,8 +110,7 @@ __device__ __forceinline__ void cap_tile(const ScoreArgs& a, floatx4 (&s)[A][B],
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const float v = s[x][y][r], q = v * v;
-            float p = __builtin_fmaf(q, a.cap_poly[4], a.cap_poly[3]);
-            p = __builtin_fmaf(q, p, a.cap_poly[2]);
+            float p = __builtin_fmaf(q, a.cap_poly[3], a.cap_poly[2]);
             p = __builtin_fmaf(q, p, a.cap_poly[1]);
             t[x][y][r] = v * __builtin_fmaf(q, p, a.cap_poly[0]);
           }
@@ -359,7 +359,7 @@ template <typename T> struct SplitFrag {
 // ===========================================================================
 // Forward, as ext_fwd_kernel.  Orest may be null.  Bound by MFMA and VALU issue for many rows: B1
 // H16 N8192 d128 causal with slopes 283 us, 0.97 PFLOP/s, the two busy for 84% of the cycles; a cap
-// takes 13 VALU operations an element for 7 (B4 H16 Hkv8 N4096 d128 causal 398 us for 320).  For a
+// takes 12 VALU operations an element for 7 (B4 H16 Hkv8 N4096 d128 causal 387 us for 320).  For a
 // few rows by the keys' and values' bytes: B16 H16 Hkv4, one token, up to 4096 keys, d128, 87 MB in
 // 21 us.
 // ===========================================================================
@@ -633,7 +633,7 @@ __device__ __forceinline__ void score_row_exponents(const ScoreArgs& a, const Ro
 // First backward, row side, as ext_bwd_rows_kernel.  A capped tile's t takes eight registers a
 // 16-row block from the exponent to the gradient of the score.  dS meets K as two bf16 values:
 // four contractions a tile for three.  Bound by MFMA (43% of the cycles) and VALU issue (62%),
-// which overlap little: B4 H16 Hkv8 N4096 d128 causal 525 us, with a cap 631.
+// which overlap little: B4 H16 Hkv8 N4096 d128 causal 525 us, with a cap 616.
 // ===========================================================================
 template <typename T, int D, int MR, int NW, int OCC, int KS, bool kCap>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_rows_kernel(
@@ -901,7 +901,7 @@ __device__ __forceinline__ void score_col_exponents(const ScoreArgs& a, const Co
 }
 
 // First backward, column side, as ext_bwd_cols_kernel (P and dS are summed over queries whose
-// roundings do not cancel: one bf16 value each).  Bound as the row side: 600 us there, with a cap 700.
+// roundings do not cancel: one bf16 value each).  Bound as the row side: 600 us there, with a cap 685.
 template <typename T, int D, int MC, int NW, int OCC, int KS, bool kKL, bool kCap>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_cols_kernel(
     ScoreArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ dO,

@@ -41,6 +41,8 @@ CASES = {
     "keys_alone": dict(B=2, H=0, Hkv=3, N=20, d=64),
     "queries_alone": dict(B=2, H=3, Hkv=0, N=20, d=64),
     "large": dict(B=3, H=16, Hkv=8, N=1500, d=128),
+    "sums_in_rounds": dict(B=4, H=2, Hkv=1, N=5000, d=32),
+    "sums_in_rounds_f32": dict(B=2, H=1, Hkv=2, N=5000, d=256, dtype="f32", interleaved=True),
     "head_major": dict(B=2, H=4, Hkv=2, N=90, d=64, order="heads"),
     "packed": dict(B=2, H=4, Hkv=2, N=90, d=64, order="packed"),
     "unaligned": dict(B=2, H=4, Hkv=2, N=90, d=64, order="unaligned"),
