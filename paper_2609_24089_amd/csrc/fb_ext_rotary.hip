@@ -18,7 +18,7 @@
 // a run of pairs' first halves and that of their second ones (neighbours paired: two runs of whole
 // pairs, half a vector apart), so a rotation needs no other lane, and the lanes of a vector read
 // and write neighbouring runs (in runs of 16 elements a lane fp32 B8 H6 N1395 d64 of neighbours
-// took 33 us forward).  A workgroup makes the cosines and sines of its tokens once for all heads
+// took 33 us forward for 24).  A workgroup makes the cosines and sines of its tokens once for all heads
 // of the queries or keys.
 #include "fb_ext.h"
 
@@ -369,7 +369,7 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a) {
 
 // Adds the workgroups' rows of sums: 16 columns of the queries' (blockIdx.y 0) or keys' weight a
 // workgroup, 64 threads a column with eight loads in flight each, for all of it is latency
-// (1024 rows: 16 threads a column 14 us).
+// (1024 rows: 16 threads a column 14 us for 7).
 constexpr int kSumThreads = 1024;
 __global__ __launch_bounds__(kSumThreads) void rotary_sums_kernel(const float* __restrict__ sums, int d, int rows,
                                                                   void* out_q, void* out_k, int w_bf16) {
@@ -444,7 +444,7 @@ struct RotaryPlan {
   int64_t groups;
 };
 // At least as many tokens at a time as leave no slot without a head (bf16 B2 H12 N2047 d64, whose
-// 32 slots met 12 heads: 12.8 us forward), and more while kEnough workgroups are left.  Calls
+// 32 slots met 12 heads: 12.8 us forward for 10), and more while kEnough workgroups are left.  Calls
 // that sum a weight's gradient have at most kMaxSums rows of sums a weight, in workgroups that go
 // on to as many further tokens as each other; a launch takes fewer than 2^32 threads.
 constexpr int64_t kEnough = 1024, kMaxSums = 1024, kMaxBlocks = int64_t(1) << 22;

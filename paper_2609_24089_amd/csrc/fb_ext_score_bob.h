@@ -25,7 +25,7 @@ template <typename T, int D> struct ScorePass2 {
   static constexpr int kExtra = 4 * 4 * kBS * (int)sizeof(float) + 1024;
   static constexpr ExtShape shape(int form, bool capped) {
     // 16 columns a wave, three waves per SIMD, where a cap's tanh spilled 63 registers of the 32
-    // columns' 256 (B4 H12 N4096 causal 750 us)
+    // columns' 256 (B4 H12 N4096 causal 750 us for 520)
     constexpr bool kNarrow = std::is_same_v<T, bf16> && D == 64;
     constexpr Shape w = Cfg<T, D>::kP2;
     return form == 0   ? capped && kNarrow ? ExtShape{1, 4, 3, 1} : ExtShape{w.mr, w.nw, w.occ, 1}
