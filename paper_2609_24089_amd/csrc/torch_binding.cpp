@@ -1120,7 +1120,7 @@ struct RotaryBackward : torch::autograd::Function<RotaryBackward> {
     ctx->set_materialize_grads(false);
     ctx->saved_data["eps"] = eps;
     ctx->saved_data["interleaved"] = interleaved;
-    ctx->saved_data["wq"] = r[2].defined();
+    ctx->saved_data["wq"] = r[2].defined();  // which outputs follow dQ and dK, and so which cotangents
     ctx->saved_data["wk"] = r[3].defined();
     variable_list out{r[0], r[1]};  // no undefined outputs
     if (r[2].defined()) out.push_back(r[2]);
@@ -1148,17 +1148,19 @@ struct RotaryBackward : torch::autograd::Function<RotaryBackward> {
     const RotaryDims m = rotary_dims_or_throw(q, k, e, {&gq, &uq}, {&gk, &uk});
     c10::OptionalDeviceGuard guard(q.device());
     const bool nq = e.q_weight.defined(), nk = e.k_weight.defined();
-    // x~, w~ and the upstream gradients' cotangents; the weights' alone where their gradients were taken
+    // x~, w~ and the upstream gradients' cotangents.  A weight has its term where this pass asks for it, whether or not
+    // the first one took the weight's gradient: dQ and dK depend on the weights by themselves
+    const bool want_q = nq && ctx->needs_input_grad(2), want_k = nk && ctx->needs_input_grad(nq ? 3 : 2);
     Tensor Qt = nq ? heads_empty(q, tokens_first(q)) : Tensor(), Kt = nk ? heads_empty(k, tokens_first(k)) : Tensor();
-    Tensor Wqt = wq ? at::empty_like(e.q_weight) : Tensor(), Wkt = wk ? at::empty_like(e.k_weight) : Tensor();
+    Tensor Wqt = want_q ? at::empty_like(e.q_weight) : Tensor(), Wkt = want_k ? at::empty_like(e.k_weight) : Tensor();
     Tensor gqt = heads_empty(q, false), gkt = heads_empty(k, false);
-    const int64_t bytes = wq || wk ? api.rotary_bytes(m.code, m.B, m.H, m.Hkv, m.N, m.d, &m.r) : 0;
+    const int64_t bytes = want_q || want_k ? api.rotary_bytes(m.code, m.B, m.H, m.Hkv, m.N, m.d, &m.r) : 0;
     const Tensor ws = workspace(bytes, q);
     const attn_heads in[6] = {heads(q), heads(k), heads(gq), heads(gk), heads(uq), heads(uk)};
     const attn_heads out[4] = {heads(Qt), heads(Kt), heads(gqt), heads(gkt)};
     ok(api.rotary_bwd2(m.code, m.B, m.H, m.Hkv, m.N, m.d, &m.r, &in[0], &in[1], &in[2], &in[3], &in[4], &in[5],
                        uwq.defined() ? p(uwq) : nullptr, uwk.defined() ? p(uwk) : nullptr, &out[0], &out[1], &out[2],
-                       &out[3], wq ? pm(Wqt) : nullptr, wk ? pm(Wkt) : nullptr, bytes > 0 ? pm(ws) : nullptr, bytes,
+                       &out[3], want_q ? pm(Wqt) : nullptr, want_k ? pm(Wkt) : nullptr, bytes > 0 ? pm(ws) : nullptr, bytes,
                        stream_of(q)));
     if (graph) {
       std::vector<Tensor> all;
