@@ -1109,10 +1109,9 @@ struct RotarySecond : torch::autograd::Function<RotarySecond> {
 
 struct RotaryBackward : torch::autograd::Function<RotaryBackward> {
   static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Maybe& q_weight,
-                               const Maybe& k_weight, const Tensor& gq_, const Tensor& gk_, const Tensor& positions,
+                               const Maybe& k_weight, const Tensor& gq, const Tensor& gk, const Tensor& positions,
                                const Tensor& freqs, const Maybe& axes, double eps, bool interleaved, bool want) {
     const RotaryExtras e{positions, freqs, get(axes), get(q_weight), get(k_weight), eps, interleaved};
-    const Tensor gq = made_readable(gq_), gk = made_readable(gk_);
     const RotaryDims m = rotary_dims_or_throw(q, k, e, {&gq}, {&gk});
     c10::OptionalDeviceGuard guard(q.device());
     const variable_list r = run_rotary_bwd(m, e, q, k, gq, gk, want);
@@ -1199,16 +1198,17 @@ struct Rotary : torch::autograd::Function<Rotary> {
     // the edges of the weights that are given follow those of q and k
     const bool nq = e.q_weight.defined(), nk = e.k_weight.defined();
     const bool want = (nq && ctx->needs_input_grad(2)) || (nk && ctx->needs_input_grad(nq ? 3 : 2));
+    // copies that the kernels can read are made here, where they have a graph: RotaryBackward keeps them
+    const Tensor gq = made_readable(g[0]), gk = made_readable(g[1]);
     variable_list out(9);
     if (!at::GradMode::is_enabled()) {
-      const Tensor gq = made_readable(g[0]), gk = made_readable(g[1]);
       const RotaryDims m = rotary_dims_or_throw(s[0], s[1], e, {&gq}, {&gk});
       c10::OptionalDeviceGuard guard(s[0].device());
       const variable_list r = run_rotary_bwd(m, e, s[0], s[1], gq, gk, want);
       for (int i = 0; i < 4; ++i) out[i] = r[i];
       return out;
     }
-    const variable_list r = RotaryBackward::apply(s[0], s[1], maybe(e.q_weight), maybe(e.k_weight), g[0], g[1], s[4],
+    const variable_list r = RotaryBackward::apply(s[0], s[1], maybe(e.q_weight), maybe(e.k_weight), gq, gk, s[4],
                                                   s[5], maybe(e.axes), e.eps, e.interleaved, want);
     out[0] = r[0], out[1] = r[1];
     if (want && nq) out[2] = r[2];
