@@ -767,7 +767,7 @@ bool score_check(Refs qside, Refs kside, Refs rows, const ScoreExtras& e, ScoreD
   if (e.slopes.defined()) {
     const Tensor& t = e.slopes;
     if (!plain(t) || t.scalar_type() != at::kFloat || t.dim() != 1 || t.size(0) != m.H || t.device() != q.device() ||
-        (t.requires_grad() && at::GradMode::is_enabled()))
+        (t.requires_grad() && at::GradMode::is_enabled()) || t._fw_grad(0).defined())
       return false;
     m.s.slopes = f(t);
   }
@@ -1005,7 +1005,9 @@ bool rotary_check(const Tensor& q, const Tensor& k, const RotaryExtras& e, Rotar
   auto here = [&](const Tensor& t, at::ScalarType type, int64_t dim) {
     return plain(t) && t.scalar_type() == type && t.dim() == dim && t.device() == q.device();
   };
-  if (!here(e.freqs, at::kDouble, 1) || e.freqs.size(0) % 8 != 0 || 2 * e.freqs.size(0) > m.d) return false;
+  if (!here(e.freqs, at::kDouble, 1) || e.freqs.size(0) % 8 != 0 || 2 * e.freqs.size(0) > m.d ||
+      (e.freqs.requires_grad() && at::GradMode::is_enabled()) || e.freqs._fw_grad(0).defined())
+    return false;
   if (e.axes.defined() && (!here(e.axes, at::kInt, 1) || e.axes.size(0) != e.freqs.size(0))) return false;
   const Tensor& t = e.positions;
   const int64_t dim = t.defined() ? t.dim() : 0;

@@ -8,17 +8,17 @@ linear, and differentiable any number of times; third derivatives of the norms r
 Queries q [B, H, N, d] and keys k [B, Hkv, N, d] may have any strides whose last is 1; a projection's [B, N, H, d] is
 passed as its transpose(1, 2).  (Where data or strides are not multiples of 16 bytes the layer copies them first.)
 The results are contiguous.  With a weight [d] (fp32 or bf16) each head vector x becomes w x / sqrt(mean(x^2) + eps)
-first.  `rotary` is a pair (freqs, axes): freqs fp64 [pairs], the radians a position, and axes int32 [pairs], the axis of
-the positions that turns each pair (`rotary_frequencies` makes the usual ones); positions are int32 [axes, B, N], or
-[B, N] with one axis.  The pairs, a multiple of 8, are those of the first 2 pairs elements: (i, i + pairs) or,
-interleaved, (2 i, 2 i + 1); further elements are not rotated.  Angles are formed in fp64.
+first.  `rotary` is a pair (freqs, axes): freqs fp64 [pairs], the radians a position, which have no gradient, and axes
+int32 [pairs], the axis of the positions that turns each pair (`rotary_frequencies` makes the usual ones); positions are
+int32 [axes, B, N], or [B, N] with one axis.  The pairs, a multiple of 8, are those of the first 2 pairs elements: (i, i +
+pairs) or, interleaved, (2 i, 2 i + 1); further elements are not rotated.  Angles are formed in fp64.
 """
 import ctypes
 
 import torch
 
 from . import BOB_BF16, BOB_F32, _call, _dtype_code, _fast, _p, _stream, load_library
-from .score import scored_attention
+from .score import has_tangent, scored_attention
 
 HEAD_DIMS = (32, 64, 128, 256)
 
@@ -329,6 +329,8 @@ def rotate_heads(q, k, positions, rotary, q_weight=None, k_weight=None, eps=1e-6
         if y is not None:
             return y
     _Rotary(q, k, positions, freqs, axes, q_weight, k_weight, eps, interleaved)
+    if freqs.requires_grad and torch.is_grad_enabled() or has_tangent(freqs):
+        raise ValueError("freqs have no gradient; detach them")
     if q_weight is None and k_weight is None:
         return _RotateFn.apply(q, k, positions, freqs, axes, bool(interleaved), False, (False, False))
     return _RotaryFn.apply(q, k, q_weight, k_weight, positions, freqs, axes, float(eps), bool(interleaved))

@@ -105,6 +105,11 @@ def attn_score_layout(kernel, dtype, B, H, Hkv, Nq, Nk, d, causal=False, cap=Non
     return got
 
 
+def has_tangent(t):
+    """Whether t is a dual tensor of the current forward-mode level."""
+    return torch.autograd.forward_ad.unpack_dual(t).tangent is not None
+
+
 class _Score(_Problem):
     """Checked shapes of one call and its attn_score."""
 
@@ -118,7 +123,7 @@ class _Score(_Problem):
             if slopes.dtype != torch.float32 or tuple(slopes.shape) != (H,) or not slopes.is_contiguous() or \
                     slopes.device != q.device:
                 raise ValueError("slopes must be a contiguous fp32 [H] tensor on the device of the matrices")
-            if slopes.requires_grad and torch.is_grad_enabled():
+            if slopes.requires_grad and torch.is_grad_enabled() or has_tangent(slopes):
                 raise ValueError("slopes have no gradient; detach them")
         if spans is not None:
             if spans.dtype != torch.int32 or tuple(spans.shape) != (B, Nk, 4) or not spans.is_contiguous() or \
