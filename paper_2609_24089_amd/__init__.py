@@ -195,10 +195,10 @@ def _check_groups(qside, kside):
     return B, H, Hkv, N, d
 
 
-def _check_rows(shape, *vs):
+def _check_rows(like, *vs):
     for v in vs:
-        if v.dtype != torch.float32 or tuple(v.shape) != tuple(shape[:3]) or not v.is_contiguous():
-            raise ValueError("row vectors must be contiguous float32 [B, H, N]")
+        if v.dtype != torch.float32 or v.shape != like.shape[:3] or not v.is_contiguous() or v.device != like.device:
+            raise ValueError("row vectors must be contiguous float32 [B, H, N] on the device of the matrices")
 
 
 def _p(t):
@@ -254,7 +254,7 @@ def attn_fwd_lse(Q, K, V, scale, causal=False, out=None, stream=None):
         out = (torch.empty_like(Q), _rows_empty(Q.shape, Q))
     O, L = out
     _check_mats(Q, O)
-    _check_rows(Q.shape, L)
+    _check_rows(Q, L)
     lib = load_library()
     ptrs = (_p(Q), _p(K), _p(V), _p(O), _p(L), _stream(stream, Q))
     if Hkv == H:
@@ -272,13 +272,13 @@ def attn_bwd(Q, K, V, O, dO, L, scale, causal=False, out=None, stream=None, colu
         if got is not None:
             return got
     B, H, Hkv, N, d = _check_groups((Q, O, dO), (K, V))
-    _check_rows(Q.shape, L)
+    _check_rows(Q, L)
     if out is None:
         out = (torch.empty_like(Q), torch.empty_like(K), torch.empty_like(K), _rows_empty(Q.shape, Q))
     dQ, dK, dV, D = out
     _check_mats(Q, dQ)
     _check_mats(K, dK, dV)
-    _check_rows(Q.shape, D)
+    _check_rows(Q, D)
     lib = load_library()
     code, c = _dtype_code(Q), int(bool(causal))
     ptrs = (_p(Q), _p(K), _p(V), _p(O), _p(dO), _p(L), _p(dQ), _p(dK), _p(dV), _p(D))
@@ -302,12 +302,12 @@ def attn_bob_pass1_rows(Q, K, V, O, dO, gdQ, gdK, gdV, L, D, scale, causal=False
     B, H, Hkv, N, d = _check_groups((Q, O, dO, gdQ), (K, V, gdK, gdV))
     if dQ is not None:
         _check_mats(Q, dQ)
-    _check_rows(Q.shape, L, D)
+    _check_rows(Q, L, D)
     if out is None:
         out = (torch.empty_like(Q), torch.empty_like(Q), _rows_empty(Q.shape, Q), _rows_empty(Q.shape, Q))
     Qt, dOt, alpha, E = out
     _check_mats(Q, Qt, dOt)
-    _check_rows(Q.shape, alpha, E)
+    _check_rows(Q, alpha, E)
     lib = load_library()
     ptrs = (_p(Q), _p(K), _p(V), _p(O), _p(dO), _p(gdQ), _p(gdK), _p(gdV), _p(L), _p(D),
             None if dQ is None else _p(dQ), _p(Qt), _p(dOt), _p(alpha), _p(E), _stream(stream, Q))
@@ -328,7 +328,7 @@ def attn_bob_pass2_cols(Q, K, V, dO, gdQ, gdK, gdV, L, D, alpha, E, scale, causa
         if got is not None:
             return got
     B, H, Hkv, N, d = _check_groups((Q, dO, gdQ), (K, V, gdK, gdV))
-    _check_rows(Q.shape, L, D, alpha, E)
+    _check_rows(Q, L, D, alpha, E)
     if out is None:
         out = (torch.empty_like(K), torch.empty_like(K))
     Kt, Vt = out
@@ -351,7 +351,7 @@ def attn_bob_pass2_cols_noalloc(Q, K, V, dO, gdQ, gdK, gdV, L, D, alpha, E, scal
     no device memory (pass `out` to allocate nothing here either).  Calls that
     overlap on one device race on that buffer.  Returns (Kt, Vt)."""
     B, H, Hkv, N, d = _check_groups((Q, dO, gdQ), (K, V, gdK, gdV))
-    _check_rows(Q.shape, L, D, alpha, E)
+    _check_rows(Q, L, D, alpha, E)
     if out is None:
         out = (torch.empty_like(K), torch.empty_like(K))
     Kt, Vt = out
@@ -367,9 +367,9 @@ def attn_bob_pass2_cols_noalloc(Q, K, V, dO, gdQ, gdK, gdV, L, D, alpha, E, scal
 def attn_bob3_alpha_rows(Q, K, gdQ, gdK, L, scale, causal=False, out=None, stream=None):
     """Three-pass control schedule, sweep 1: returns alpha."""
     B, H, N, d = _check_mats(Q, K, gdQ, gdK)
-    _check_rows(Q.shape, L)
+    _check_rows(Q, L)
     alpha = _rows_empty(Q.shape, Q) if out is None else out
-    _check_rows(Q.shape, alpha)
+    _check_rows(Q, alpha)
     lib = load_library()
     _call(Q, lib.attn_bob3_alpha_rows, _dtype_code(Q), B, H, N, d, float(scale), int(bool(causal)),
           _p(Q), _p(K), _p(gdQ), _p(gdK), _p(L), _p(alpha), _stream(stream, Q))
@@ -379,12 +379,12 @@ def attn_bob3_alpha_rows(Q, K, gdQ, gdK, L, scale, causal=False, out=None, strea
 def attn_bob3_rows(Q, K, V, dO, gdQ, gdK, gdV, L, D, alpha, scale, causal=False, out=None, stream=None):
     """Three-pass control schedule, sweep 2: returns (Qt, dOt, E)."""
     B, H, N, d = _check_mats(Q, K, V, dO, gdQ, gdK, gdV)
-    _check_rows(Q.shape, L, D, alpha)
+    _check_rows(Q, L, D, alpha)
     if out is None:
         out = (torch.empty_like(Q), torch.empty_like(Q), _rows_empty(Q.shape, Q))
     Qt, dOt, E = out
     _check_mats(Q, Qt, dOt)
-    _check_rows(Q.shape, E)
+    _check_rows(Q, E)
     lib = load_library()
     _call(Q, lib.attn_bob3_rows, _dtype_code(Q), B, H, N, d, float(scale), int(bool(causal)),
           _p(Q), _p(K), _p(V), _p(dO), _p(gdQ), _p(gdK), _p(gdV), _p(L), _p(D), _p(alpha),

@@ -210,7 +210,7 @@ def attn_ext_fwd_lse(Q, K, V, scale, causal=False, bias=None, kv_lens=None, q_le
         out = (torch.empty_like(Q), _rows_empty(Q.shape, Q))
     O, L = out
     _check_mats(Q, O)
-    _check_rows(Q.shape, L)
+    _check_rows(Q, L)
     lib = load_library()
     st = _stream(stream, Q)
     ws, wp, n = p.workspace(lib.attn_ext_fwd_workspace_bytes, stream)
@@ -228,14 +228,14 @@ def attn_ext_bwd(Q, K, V, O, dO, L, scale, causal=False, bias=None, kv_lens=None
         if got is not None:
             return got
     p = _Problem((Q, O, dO), (K, V), scale, causal, bias, kv_lens, q_lens, q_starts)
-    _check_rows(Q.shape, L)
+    _check_rows(Q, L)
     if out is None:
         out = (torch.empty_like(Q), torch.empty_like(K), torch.empty_like(K), _rows_empty(Q.shape, Q),
                torch.empty_like(p.table) if p.table is not None and want_table else None)
     dQ, dK, dV, D, dT = out
     _check_mats(Q, dQ)
     _check_mats(K, dK, dV)
-    _check_rows(Q.shape, D)
+    _check_rows(Q, D)
     tp = p.cotangent(dT)
     lib = load_library()
     st = _stream(stream, Q)
@@ -254,12 +254,12 @@ def attn_ext_pass1_rows(Q, K, V, O, dO, gdQ, gdK, gdV, L, D, dQ, scale, causal=F
         if got is not None:
             return got
     p = _Problem((Q, O, dO, gdQ, dQ), (K, V, gdK, gdV), scale, causal, bias, kv_lens, q_lens, q_starts)
-    _check_rows(Q.shape, L, D)
+    _check_rows(Q, L, D)
     if out is None:
         out = (torch.empty_like(Q), torch.empty_like(Q), _rows_empty(Q.shape, Q), _rows_empty(Q.shape, Q))
     Qt, dOt, alpha, E = out
     _check_mats(Q, Qt, dOt)
-    _check_rows(Q.shape, alpha, E)
+    _check_rows(Q, alpha, E)
     lib = load_library()
     st = _stream(stream, Q)
     ws, wp, n = p.workspace(lib.attn_ext_pass1_workspace_bytes, stream)
@@ -278,7 +278,7 @@ def attn_ext_pass2_cols(Q, K, V, dO, gdQ, gdK, gdV, L, D, alpha, E, scale, causa
         if got is not None:
             return got
     p = _Problem((Q, dO, gdQ), (K, V, gdK, gdV), scale, causal, bias, kv_lens, q_lens, q_starts)
-    _check_rows(Q.shape, L, D, alpha, E)
+    _check_rows(Q, L, D, alpha, E)
     if out is None:
         out = (torch.empty_like(K), torch.empty_like(K),
                torch.empty_like(p.table) if p.table is not None and want_table else None)

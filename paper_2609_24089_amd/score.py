@@ -153,7 +153,7 @@ def attn_score_fwd_lse(Q, K, V, scale, causal=False, cap=None, slopes=None, span
     O, Orest, L = out
     _check_mats(Q, O)
     _check_rest(Q, Orest)
-    _check_rows(Q.shape, L)
+    _check_rows(Q, L)
     st = _stream(stream, Q)
     ws, wp, n = p.space(ATTN_SCORE_FWD, stream)
     _call(Q, load_library().attn_score_fwd_lse, *p.shape, *p.options, _p(Q), _p(K), _p(V), _p(O), _ptr(Orest), _p(L),
@@ -166,13 +166,13 @@ def attn_score_bwd(Q, K, V, O, Orest, dO, L, scale, causal=False, cap=None, slop
     """First backward: returns (dQ, dK, dV, D).  Orest: the forward's, or None (0)."""
     p = _Score((Q, O, dO), (K, V), scale, causal, cap, slopes, spans, kv_lens, q_lens, q_starts)
     _check_rest(Q, Orest)
-    _check_rows(Q.shape, L)
+    _check_rows(Q, L)
     if out is None:
         out = (torch.empty_like(Q), torch.empty_like(K), torch.empty_like(K), _rows_empty(Q.shape, Q))
     dQ, dK, dV, D = out
     _check_mats(Q, dQ)
     _check_mats(K, dK, dV)
-    _check_rows(Q.shape, D)
+    _check_rows(Q, D)
     st = _stream(stream, Q)
     ws, wp, n = p.space(ATTN_SCORE_BWD, stream)
     _call(Q, load_library().attn_score_bwd, *p.shape, *p.options, _p(Q), _p(K), _p(V), _p(O), _ptr(Orest), _p(dO),
@@ -185,12 +185,12 @@ def attn_score_pass1_rows(Q, K, V, O, Orest, dO, gdQ, gdK, gdV, L, D, dQ, scale,
     """BoB Pass 1: returns (Qt, dOt, alpha, E).  Orest: the forward's, or None (0)."""
     p = _Score((Q, O, dO, gdQ, dQ), (K, V, gdK, gdV), scale, causal, cap, slopes, spans, kv_lens, q_lens, q_starts)
     _check_rest(Q, Orest)
-    _check_rows(Q.shape, L, D)
+    _check_rows(Q, L, D)
     if out is None:
         out = (torch.empty_like(Q), torch.empty_like(Q), _rows_empty(Q.shape, Q), _rows_empty(Q.shape, Q))
     Qt, dOt, alpha, E = out
     _check_mats(Q, Qt, dOt)
-    _check_rows(Q.shape, alpha, E)
+    _check_rows(Q, alpha, E)
     st = _stream(stream, Q)
     ws, wp, n = p.space(ATTN_SCORE_PASS1, stream)
     _call(Q, load_library().attn_score_pass1_rows, *p.shape, *p.options, _p(Q), _p(K), _p(V), _p(O), _ptr(Orest),
@@ -202,7 +202,7 @@ def attn_score_pass2_cols(Q, K, V, dO, gdQ, gdK, gdV, L, D, alpha, E, scale, cau
                           spans=None, kv_lens=None, q_lens=None, q_starts=None, out=None, stream=None):
     """BoB Pass 2: returns (Kt, Vt)."""
     p = _Score((Q, dO, gdQ), (K, V, gdK, gdV), scale, causal, cap, slopes, spans, kv_lens, q_lens, q_starts)
-    _check_rows(Q.shape, L, D, alpha, E)
+    _check_rows(Q, L, D, alpha, E)
     if out is None:
         out = (torch.empty_like(K), torch.empty_like(K))
     Kt, Vt = out
