@@ -181,6 +181,12 @@ class _Rotary:
                              "strides in multiples of 16 bytes")
         return t
 
+    def gradient(self, name, t, weight):
+        """An output of the caller's for a weight's gradient."""
+        if t is not None and (weight is None or t.shape != weight.shape or t.dtype != weight.dtype or
+                              t.device != weight.device or not t.is_contiguous()):
+            raise ValueError(f"{name} must be like its weight")
+
     def vector(self, name, t, weight):
         """A cotangent like a weight."""
         if t is None:
@@ -224,9 +230,7 @@ def attn_rotary_bwd(Q, K, dQr, dKr, positions, freqs, axes=None, q_weight=None, 
                                            for w in (q_weight, k_weight)]
     dQ, dK, dWq, dWk = out
     p.into("dQ", dQ, Q), p.into("dK", dK, K)
-    for name, t, w in (("dWq", dWq, q_weight), ("dWk", dWk, k_weight)):
-        if t is not None and (w is None or t.shape != w.shape or t.dtype != w.dtype or not t.is_contiguous()):
-            raise ValueError(f"{name} must be like its weight")
+    p.gradient("dWq", dWq, q_weight), p.gradient("dWk", dWk, k_weight)
     st = _stream(stream, Q)
     ws, wp, n = p.workspace() if dWq is not None or dWk is not None else (None, None, 0)
     _call(Q, load_library().attn_rotary_bwd, *p.shape, p.ref, _heads(Q), _heads(K), _heads(dQr), _heads(dKr),
