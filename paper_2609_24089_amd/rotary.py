@@ -88,9 +88,8 @@ def _tokens_first(x):
 
 def _empty(x, tokens_first):
     B, H, N, d = x.shape
-    if tokens_first:
-        return torch.empty(B, N, H, d, dtype=x.dtype, device=x.device).transpose(1, 2)
-    return torch.empty(B, H, N, d, dtype=x.dtype, device=x.device)
+    # x's own method: of its subclass
+    return x.new_empty(B, N, H, d).transpose(1, 2) if tokens_first else x.new_empty(B, H, N, d)
 
 
 def _like(x):
@@ -211,7 +210,7 @@ def attn_rotary_fwd(Q, K, positions, freqs, axes=None, q_weight=None, k_weight=N
         raise ValueError("inverse takes no weights")
     Q, K = p.side("Q", Q, Q), p.side("K", K, K)
     if out is None:
-        out = [torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (Q, K)]
+        out = [_empty(x, False) for x in (Q, K)]
     Qr, Kr = p.into("Qr", out[0], Q), p.into("Kr", out[1], K)
     _call(Q, load_library().attn_rotary_fwd, *p.shape, int(bool(inverse)), p.ref, _heads(Q), _heads(K), _heads(Qr),
           _heads(Kr), _stream(stream, Q))
@@ -248,7 +247,7 @@ def attn_rotary_bwd2(Q, K, dQr, dKr, gdQ, gdK, positions, freqs, axes=None, q_we
     gdQ, gdK = p.side("gdQ", gdQ, Q), p.side("gdK", gdK, K)
     gdWq, gdWk = p.vector("gdWq", gdWq, q_weight), p.vector("gdWk", gdWk, k_weight)
     Qt, Kt = (None if w is None else _like(x) for x, w in zip(order, (q_weight, k_weight)))
-    dQrt, dKrt = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (Q, K))
+    dQrt, dKrt = (_empty(x, False) for x in (Q, K))
     Wqt, Wkt = (None if w is None or not want_weights else torch.empty_like(w) for w in (q_weight, k_weight))
     st = _stream(stream, Q)
     ws, wp, n = p.workspace() if Wqt is not None or Wkt is not None else (None, None, 0)
