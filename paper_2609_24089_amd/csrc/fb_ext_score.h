@@ -31,8 +31,11 @@ ScoreArgs score_args(const ScoreProblem& p, const ExtPlan& c, int64_t heads, int
     a.cap_pre = std::fabs(x) >= 1e-4 && std::fabs(x) <= 1e4 ? 1.f : (float)x;
     x = a.cap_pre == 1.f ? x : 1.0;
     a.cap_in = (float)(x * kCapArg<T>);
-    a.cap_near = (float)(kCapNear / std::fabs(x));
-    for (int i = 0; i < 4; ++i) a.cap_poly[i] = (float)(kCapPoly[i] * std::pow(x, 2 * i + 1));
+    const bool far = p.cap > kCapMinimax;
+    const double(&poly)[4] = far ? kCapTaylor : kCapPoly;
+    a.cap_far = far ? 1 : 0;
+    a.cap_near = (float)((far ? kCapNearFar : kCapNear) / std::fabs(x));
+    for (int i = 0; i < 4; ++i) a.cap_poly[i] = (float)(poly[i] * std::pow(x, 2 * i + 1));
   }
   return a;
 }

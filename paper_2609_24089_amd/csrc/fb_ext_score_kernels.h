@@ -42,13 +42,14 @@ struct ScoreArgs : ExtArgs {
   float cap_out;         // c log2(e)
   float cap_k;           // 2 / c
   float cap_near;        // up to here the tanh is cap_poly's
+  int cap_far;           // 1: a tile beyond cap_near has its elements up to it from cap_poly too
   float cap_poly[4];     // t = s (p0 + p1 s^2 + p2 s^4 + p3 s^6)
 };
 
 // ---------------------------------------------------------------------------
 // The cap
 // ---------------------------------------------------------------------------
-// tanh of x: bf16 takes y = 2 log2(e) x, as 1 - 2 / (1 + 2^y), off by 2^-23 of 1 (1e-5 of a
+// tanh of x: bf16 takes y = 2 log2(e) x, as 1 - 2 / (1 + 2^y), off by some 2^-23 of 1 (1e-5 of a
 // score of c = 50: P is rounded to bf16 afterwards).  fp32 takes x and is within some 2^-23 of
 // the result: the same for |x| > 0.45, the Taylor series (next term below 2^-25 of x) below.
 template <typename T> __device__ __forceinline__ float cap_tanh(float s, float cap_in);
@@ -76,14 +77,24 @@ template <> __device__ __forceinline__ float cap_tanh<float>(float s, float cap_
 }
 template <typename T> constexpr float kCapArg = std::is_same_v<T, bf16> ? 2.f * kLog2e : 1.f;  // of cap_in
 
-// tanh on |x| <= kCapNear by an odd polynomial, off by 1.1e-6 at most (the least for four terms;
-// 5e-5 of a score of c = 50, where P is rounded to 2^-9).  Scores of trained models lie far below
-// their cap, so whole tiles take it: 5 instructions an element for two transcendentals, at a
-// quarter of the rate, and three others.  (A fifth term reaches 0.9 for a sixth instruction: a
-// training pass of B4 H16 Hkv8 N4096 d128 causal 1497 us for 1470.)  cap_near and cap_poly are this
-// in terms of Q K^T.
-constexpr double kCapNear = 0.65;
+// tanh on |x| <= kCapNear by an odd polynomial, off by 1.14e-6 at most (the least for four terms;
+// 6e-5 of a score of c = 50, where P is rounded to 2^-9).  Where scores lie far below their cap whole
+// tiles take it: 5 instructions an element for two transcendentals, at a quarter of the rate, and
+// three others.  (A fifth term reaches 0.9 for a sixth instruction: a training pass of B4 H16 Hkv8
+// N4096 d128 causal 1497 us for 1470.)  cap_near and cap_poly are this in terms of Q K^T.
+// Which of the two a pair's score meets goes by its wave's tile, so forward, row side and column side
+// may differ in it; what either is off by, times c, has to stay below P's rounding.  Caps up to
+// kCapMinimax leave 1.2e-4 of a score.  Farther ones take the Taylor series, off by 2^-24 of the
+// *result* up to kCapNearFar, in every tile: beyond it the other is off by 2^-20 of the result at most.
+constexpr double kCapNear = 0.65, kCapNearFar = 0.2, kCapMinimax = 100.0;
 constexpr double kCapPoly[4] = {0.9999839352347103, -0.332806913691474, 0.12861559355416782, -0.03767224489906605};
+constexpr double kCapTaylor[4] = {1.0, -1.0 / 3, 2.0 / 15, -17.0 / 315};
+__device__ __forceinline__ float cap_series(const ScoreArgs& a, float v) {
+  const float q = v * v;
+  float p = __builtin_fmaf(q, a.cap_poly[3], a.cap_poly[2]);
+  p = __builtin_fmaf(q, p, a.cap_poly[1]);
+  return v * __builtin_fmaf(q, p, a.cap_poly[0]);
+}
 
 // t = tanh(S / c) of a tile of raw scores, which it may overwrite.
 template <typename T, int A, int B>
@@ -108,11 +119,18 @@ __device__ __forceinline__ void cap_tile(const ScoreArgs& a, floatx4 (&s)[A][B],
 #pragma unroll
         for (int y = 0; y < B; ++y)
 #pragma unroll
+          for (int r = 0; r < 4; ++r) t[x][y][r] = cap_series(a, s[x][y][r]);
+      return;
+    }
+    if (a.cap_far != 0) {
+#pragma unroll
+      for (int x = 0; x < A; ++x)
+#pragma unroll
+        for (int y = 0; y < B; ++y)
+#pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float v = s[x][y][r], q = v * v;
-            float p = __builtin_fmaf(q, a.cap_poly[3], a.cap_poly[2]);
-            p = __builtin_fmaf(q, p, a.cap_poly[1]);
-            t[x][y][r] = v * __builtin_fmaf(q, p, a.cap_poly[0]);
+            const float v = s[x][y][r];
+            t[x][y][r] = fabsf(v) <= a.cap_near ? cap_series(a, v) : cap_tanh<T>(v, a.cap_in);
           }
       return;
     }
