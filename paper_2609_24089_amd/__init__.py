@@ -238,6 +238,16 @@ def _column_workspace(query, code, B, H, Hkv, N, d, causal, columns, like, strea
     return ws, nbytes
 
 
+def _has_tangent(t):
+    """Whether t is a dual tensor of the current forward-mode level."""
+    return t is not None and torch.autograd.forward_ad.unpack_dual(t).tangent is not None
+
+
+def _differentiated(*grads):
+    """Whether what becomes of these gradients is differentiated in its turn, by a graph or by forward-mode tangents."""
+    return torch.is_grad_enabled() or any(_has_tangent(g) for g in grads)
+
+
 def _rows_empty(shape, like):
     return torch.empty(tuple(shape[:3]), dtype=torch.float32, device=like.device)
 

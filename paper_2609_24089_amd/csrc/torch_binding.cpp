@@ -103,6 +103,15 @@ bool outside_modes() {
   return !c10::impl::tls_local_dispatch_key_set().included_.has_any(kWrapped) && !torch::jit::tracer::isTracing();
 }
 
+// Whether what becomes of the gradients g is differentiated in its turn: by a graph, or by forward-mode tangents of
+// theirs.  A backward's node for its own derivatives is left out only where neither is so.
+bool differentiated(const torch::autograd::variable_list& g) {
+  if (at::GradMode::is_enabled()) return true;
+  for (const Tensor& t : g)
+    if (t.defined() && t._fw_grad(0).defined()) return true;
+  return false;
+}
+
 bool plain(const Tensor& t) {
   return t.defined() && t.is_cuda() && t.layout() == c10::kStrided && !t.key_set().has_any(kWrapped) &&
          t.is_contiguous() && !t.is_neg() && !t.is_conj();
@@ -646,7 +655,7 @@ struct ExtAttentionBackward : torch::autograd::Function<ExtAttentionBackward> {
     const Tensor ut = g.size() > 3 && g[3].defined() ? g[3].contiguous() : Tensor();
     const ExtDims m = ext_dims_or_throw({&q, &O, &dO, &uq, &dQ}, {&k, &v, &uk, &uv}, {&L, &D}, e);
     c10::OptionalDeviceGuard guard(q.device());
-    const bool graph = at::GradMode::is_enabled();
+    const bool graph = differentiated(g);
     TORCH_CHECK_VALUE(ext_like_table(ut, table),
                       "the cotangent on the table's gradient must share the table's shape, dtype and device");
     const void* const gT = ut.defined() ? p(ut) : nullptr;
@@ -694,7 +703,7 @@ struct ExtAttention : torch::autograd::Function<ExtAttention> {
   }
   static variable_list backward(AutogradContext* ctx, variable_list g) {
     const variable_list s = ctx->get_saved_variables();
-    if (!at::GradMode::is_enabled()) {  // no second derivatives asked for: no node for them
+    if (!differentiated(g)) {  // no second derivatives asked for: no node for them
       const Extras e{s[3], s[6], s[7], s[8], s[9]};
       const Tensor dO = g[0].contiguous();
       const ExtDims m = ext_dims_or_throw({&s[0], &s[4], &dO}, {&s[1], &s[2]}, {&s[5]}, e);
@@ -864,7 +873,7 @@ struct ScoreAttentionBackward : torch::autograd::Function<ScoreAttentionBackward
     const Tensor uq = cotangent(g[0], q), uk = cotangent(g[1], k), uv = cotangent(g[2], v);
     const ScoreDims m = score_dims_or_throw({&q, &O, &dO, &uq, &dQ}, {&k, &v, &uk, &uv}, {&L, &D}, e);
     c10::OptionalDeviceGuard guard(q.device());
-    const bool graph = at::GradMode::is_enabled();
+    const bool graph = differentiated(g);
     // alpha, E and the workspace of whichever pass runs, in one allocation
     const int64_t rows = (m.B * m.H * m.Nq * 4 + 255) / 256 * 256;
     const int64_t bytes1 = m.bytes(ATTN_SCORE_PASS1, e.causal), bytes2 = m.bytes(ATTN_SCORE_PASS2, e.causal);
@@ -908,7 +917,7 @@ struct ScoreAttention : torch::autograd::Function<ScoreAttention> {
     const ScoreExtras e = kept_options(ctx, &s[6]);
     const Tensor dO = g[0].contiguous();
     variable_list out(11);
-    if (!at::GradMode::is_enabled()) {  // no second derivatives asked for: no node for them
+    if (!differentiated(g)) {  // no second derivatives asked for: no node for them
       const ScoreDims m = score_dims_or_throw({&s[0], &s[3], &dO}, {&s[1], &s[2]}, {&s[5]}, e);
       c10::OptionalDeviceGuard guard(s[0].device());
       const Bwd r = run_score_bwd(m, s[0], s[1], s[2], {s[3], s[4], s[5]}, dO, e, false);
@@ -1133,7 +1142,7 @@ struct RotaryBackward : torch::autograd::Function<RotaryBackward> {
     const Tensor &q = s[0], &k = s[1], &gq = s[4], &gk = s[5];
     const RotaryExtras e{s[6], s[7], s[8], s[2], s[3], ctx->saved_data["eps"].toDouble(),
                          ctx->saved_data["interleaved"].toBool()};
-    const bool graph = at::GradMode::is_enabled(), wq = ctx->saved_data["wq"].toBool(),
+    const bool graph = differentiated(g), wq = ctx->saved_data["wq"].toBool(),
                wk = ctx->saved_data["wk"].toBool();
     auto heads_or_none = [](const Tensor& t) { return t.defined() ? made_readable(t) : t; };
     const Tensor uq = heads_or_none(g[0]), uk = heads_or_none(g[1]);
@@ -1203,7 +1212,7 @@ struct Rotary : torch::autograd::Function<Rotary> {
     // copies that the kernels can read are made here, where they have a graph: RotaryBackward keeps them
     const Tensor gq = made_readable(g[0]), gk = made_readable(g[1]);
     variable_list out(9);
-    if (!at::GradMode::is_enabled()) {
+    if (!differentiated(g)) {
       const RotaryDims m = rotary_dims_or_throw(s[0], s[1], e, {&gq}, {&gk});
       c10::OptionalDeviceGuard guard(s[0].device());
       const variable_list r = run_rotary_bwd(m, e, s[0], s[1], gq, gk, want);

@@ -24,8 +24,8 @@ import ctypes
 
 import torch
 
-from . import (BOB_BF16, BOB_F32, BOB_OK, _call, _check_mats, _check_rows, _dtype_code, _fast, _p, _rows_empty,
-               _stream, load_library, status_string)
+from . import (BOB_BF16, BOB_F32, BOB_OK, _call, _check_mats, _check_rows, _differentiated, _dtype_code, _fast, _p,
+               _rows_empty, _stream, load_library, status_string)
 
 MAX_DISTANCE = 1024
 MAX_BUCKETS = 1 << 16
@@ -332,7 +332,7 @@ class _ExtBackwardFn(torch.autograd.Function):
         Qt, dOt, alpha, E = attn_ext_pass1_rows(q, k, v, O, dO, *cot, L, D, dq, ctx.scale, ctx.causal, **more)
         Kt, Vt, Tt = attn_ext_pass2_cols(q, k, v, dO, *cot, L, D, alpha, E, ctx.scale, ctx.causal,
                                          want_table=ctx.needs_input_grad[3], **more)
-        if torch.is_grad_enabled():
+        if _differentiated(gdq, gdk, gdv, gdt):
             Qt, Kt, Vt, dOt, Tt = _ExtSecondFn.apply(Qt, Kt, Vt, dOt, Tt, q, k, v, table, dO, gdq, gdk, gdv, gdt)
         return Qt, Kt, Vt, Tt, None, None, None, None, None, None, dOt, None, None, None
 

@@ -17,8 +17,9 @@ import ctypes
 
 import torch
 
-from . import BOB_BF16, BOB_F32, _call, _dtype_code, _fast, _p, _stream, load_library
-from .score import has_tangent, scored_attention
+from . import (BOB_BF16, BOB_F32, _call, _differentiated, _dtype_code, _fast, _has_tangent, _p, _stream,
+               load_library)
+from .score import scored_attention
 
 HEAD_DIMS = (32, 64, 128, 256)
 
@@ -303,7 +304,7 @@ class _RotaryBackwardFn(torch.autograd.Function):
         Qt, Kt, gqt, gkt, Wqt, Wkt = attn_rotary_bwd2(q, k, gq, gk, uq, uk, *more, q_weight, k_weight, *ctx.options,
                                                       gdWq=uwq, gdWk=uwk, want_weights=want)
         out = (Qt, Kt, Wqt, Wkt, gqt, gkt)
-        if torch.is_grad_enabled():
+        if _differentiated(uq, uk, uwq, uwk):
             out = _RotarySecondFn.apply(*out, q, k, q_weight, k_weight, gq, gk, uq, uk, uwq, uwk)
         return (*out,) + (None,) * 6
 
@@ -332,7 +333,7 @@ def rotate_heads(q, k, positions, rotary, q_weight=None, k_weight=None, eps=1e-6
         if y is not None:
             return y
     _Rotary(q, k, positions, freqs, axes, q_weight, k_weight, eps, interleaved)
-    if freqs.requires_grad and torch.is_grad_enabled() or has_tangent(freqs):
+    if freqs.requires_grad and torch.is_grad_enabled() or _has_tangent(freqs):
         raise ValueError("freqs have no gradient; detach them")
     if q_weight is None and k_weight is None:
         return _RotateFn.apply(q, k, positions, freqs, axes, bool(interleaved), False, (False, False))

@@ -20,8 +20,8 @@ import ctypes
 
 import torch
 
-from . import (BOB_OK, _call, _check_mats, _check_rows, _dtype_code, _fast, _p, _rows_empty, _stream, load_library,
-               status_string)
+from . import (BOB_OK, _call, _check_mats, _check_rows, _differentiated, _dtype_code, _fast, _has_tangent, _p, _rows_empty,
+               _stream, load_library, status_string)
 from .ext import AttnExtLaunch, _Problem, _ptr
 
 ATTN_SCORE_FWD, ATTN_SCORE_BWD, ATTN_SCORE_PASS1, ATTN_SCORE_PASS2 = range(4)
@@ -105,11 +105,6 @@ def attn_score_layout(kernel, dtype, B, H, Hkv, Nq, Nk, d, causal=False, cap=Non
     return got
 
 
-def has_tangent(t):
-    """Whether t is a dual tensor of the current forward-mode level."""
-    return torch.autograd.forward_ad.unpack_dual(t).tangent is not None
-
-
 class _Score(_Problem):
     """Checked shapes of one call and its attn_score."""
 
@@ -123,7 +118,7 @@ class _Score(_Problem):
             if slopes.dtype != torch.float32 or tuple(slopes.shape) != (H,) or not slopes.is_contiguous() or \
                     slopes.device != q.device:
                 raise ValueError("slopes must be a contiguous fp32 [H] tensor on the device of the matrices")
-            if slopes.requires_grad and torch.is_grad_enabled() or has_tangent(slopes):
+            if slopes.requires_grad and torch.is_grad_enabled() or _has_tangent(slopes):
                 raise ValueError("slopes have no gradient; detach them")
         if spans is not None:
             if spans.dtype != torch.int32 or tuple(spans.shape) != (B, Nk, 4) or not spans.is_contiguous() or \
@@ -250,7 +245,7 @@ class _ScoreBackwardFn(torch.autograd.Function):
         cot = [torch.zeros_like(x) if g is None else g.contiguous() for g, x in ((gdq, q), (gdk, k), (gdv, v))]
         Qt, dOt, alpha, E = attn_score_pass1_rows(q, k, v, O, Orest, dO, *cot, L, D, dq, *more)
         Kt, Vt = attn_score_pass2_cols(q, k, v, dO, *cot, L, D, alpha, E, *more)
-        if torch.is_grad_enabled():
+        if _differentiated(gdq, gdk, gdv):
             Qt, Kt, Vt, dOt = _ScoreSecondFn.apply(Qt, Kt, Vt, dOt, q, k, v, dO, gdq, gdk, gdv)
         return (Qt, Kt, Vt, None, None, None, dOt) + (None,) * 8
 
