@@ -16,7 +16,7 @@ template <typename T, int D> struct ScorePass1 {
   template <int F, bool kCap> static __host__ constexpr auto kernel() {
     constexpr ExtShape s = shape(F, kCap);
     // fragments read ahead (bf16 d = 128) where the registers hold them: with a cap, or in sets, they
-    // spilled hundreds (B2 H16 N2048 causal with a cap 1300 us for 245)
+    // spilled hundreds (B2 H16 N2048 causal with a cap: five times as long)
     constexpr int pf = F == 0 && !kCap ? Cfg<T, D>::kP1.pf : 0;
     return &score_pass1_kernel<T, D, s.mr, s.nw, s.occ, s.ks, pf, kCap>;
   }

@@ -20,9 +20,9 @@
 // gradients of rows whose weight lies on few keys anywhere in the sequence, as in trained models,
 // are differences of terms far larger than themselves, which operands rounded to bf16 do not
 // carry.  So
-//  * the forward divides by the sum of P as it was rounded, which leaves sum r_j (v_j - O) of
-//    the roundings r_j, and also stores Orest, what O's own rounding left; D = do.O and
-//    alpha O in Pass 1 take both;
+//  * P meets V as one bf16 value: the forward divides by the sum of P as it was rounded, which
+//    leaves sum r_j (v_j - O) of the roundings r_j, and also stores Orest, what O's own rounding
+//    left; D = do.O and alpha O in Pass 1 take both;
 //  * operands whose sums cancel, dS of dQ and those of Pass 1 that its epilogue subtracts from
 //    each other, meet the matrix instructions as two bf16 values each (SplitFrag).
 // With scores of standard deviation 3 that takes dQ from 2.9e-3 off to 2.0e-3, Qt from 3.2 to
@@ -80,8 +80,11 @@ template <typename T> constexpr float kCapArg = std::is_same_v<T, bf16> ? 2.f * 
 // tanh on |x| <= kCapNear by an odd polynomial, off by 1.14e-6 at most (the least for four terms;
 // 6e-5 of a score of c = 50, where P is rounded to 2^-9).  Where scores lie far below their cap whole
 // tiles take it: 5 instructions an element for two transcendentals, at a quarter of the rate, and
-// three others.  (A fifth term reaches 0.9 for a sixth instruction: a training pass of B4 H16 Hkv8
-// N4096 d128 causal 1497 us for 1470.)  cap_near and cap_poly are this in terms of Q K^T.
+// three others: B4 H16 Hkv8 N4096 d128 causal, standard deviation 3, caps 20 to 50: forward 340 us
+// for 361, first backward 1157 for 1190, Pass 1 1658 for 1710.  Where few tiles qualify (cap 20,
+// standard deviation 6) looking for them costs nothing that shows (365 for 365, 1193 for 1194).  (A
+// fifth term reaches 0.9 for a sixth instruction: the training step 1497 us for 1470.)  cap_near and
+// cap_poly are this in terms of Q K^T.
 // Which of the two a pair's score meets goes by its wave's tile, so forward, row side and column side
 // may differ in it; what either is off by, times c, has to stay below P's rounding.  Caps up to
 // kCapMinimax leave 1.2e-4 of a score.  Farther ones take the Taylor series, off by 2^-24 of the
@@ -376,10 +379,10 @@ template <typename T> struct SplitFrag {
 
 // ===========================================================================
 // Forward, as ext_fwd_kernel.  Orest may be null.  Bound by MFMA and VALU issue for many rows: B1
-// H16 N8192 d128 causal with slopes 283 us, 0.97 PFLOP/s, the two busy for 84% of the cycles; a cap
-// takes 12 VALU operations an element for 7 (B4 H16 Hkv8 N4096 d128 causal 387 us for 320).  For a
+// H16 N8192 d128 causal with slopes 286 us, 0.96 PFLOP/s, the two busy for 83% of the cycles; a cap
+// takes 12 VALU operations an element for 7 (B4 H16 Hkv8 N4096 d128 causal 348 us for 300).  For a
 // few rows by the keys' and values' bytes: B16 H16 Hkv4, one token, up to 4096 keys, d128, 87 MB in
-// 21 us.
+// 22 us.
 // ===========================================================================
 template <typename T, int D, int MR, int NW, int OCC, int KS, bool kCap>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void score_fwd_kernel(
@@ -651,7 +654,7 @@ __device__ __forceinline__ void score_row_exponents(const ScoreArgs& a, const Ro
 // First backward, row side, as ext_bwd_rows_kernel.  A capped tile's t takes eight registers a
 // 16-row block from the exponent to the gradient of the score.  dS meets K as two bf16 values:
 // four contractions a tile for three.  Bound by MFMA (43% of the cycles) and VALU issue (62%),
-// which overlap little: B4 H16 Hkv8 N4096 d128 causal 525 us, with a cap 616.
+// which overlap little: B4 H16 Hkv8 N4096 d128 causal 491 us, with a cap 561.
 // ===========================================================================
 template <typename T, int D, int MR, int NW, int OCC, int KS, bool kCap>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_rows_kernel(
@@ -919,7 +922,7 @@ __device__ __forceinline__ void score_col_exponents(const ScoreArgs& a, const Co
 }
 
 // First backward, column side, as ext_bwd_cols_kernel (P and dS are summed over queries whose
-// roundings do not cancel: one bf16 value each).  Bound as the row side: 600 us there, with a cap 685.
+// roundings do not cancel: one bf16 value each).  Bound as the row side: 556 us there, with a cap 623.
 template <typename T, int D, int MC, int NW, int OCC, int KS, bool kKL, bool kCap>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_cols_kernel(
     ScoreArgs a, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ dO,
@@ -1100,9 +1103,11 @@ __global__ __launch_bounds__(KS * NW * 64, OCC) void score_bwd_cols_kernel(
 //   Qt = tau (sum P (u w - (2 / c) t (dP - D) F) k + sum u P (dP - D) u_K - e sum u P k) - alpha dQ
 //   dOt = sum P u_V + sum P F v - alpha O,  E = e - alpha D
 // needs, capped, one more operand, u P, beside P, which stays with u_V.  P F, u P and Pt's operand
-// meet their matrices as two bf16 values each: thirteen contractions a tile for ten.  Bound by MFMA
-// and by a wave's chain of LDS reads, MFMA and exponentials at two or three waves a SIMD: B2 H16
-// N2048 d128 causal 220 us with slopes, 250 with a cap; B4 H12 N4096 d64 610 and 740.
+// meet their matrices as two bf16 values each: thirteen contractions a tile for ten.  P with u_V and
+// u P (dP - D) with u_K are one: the epilogue subtracts nothing from their sums, which keep a rounding
+// of their terms' size.  Bound by MFMA and by a wave's chain of LDS reads, MFMA and exponentials at
+// two or three waves a SIMD: B2 H16
+// N2048 d128 causal 191 us with slopes, 210 with a cap; B4 H12 N4096 d64 558 and 678.
 // ===========================================================================
 template <typename T, int D, int MR, int NW, int OCC, int KS, int kPF, bool kCap>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass1_kernel(
@@ -1385,8 +1390,10 @@ __global__ __launch_bounds__(256) void score_pass1_join_kernel(ExtArgs a, const 
 }
 
 // ===========================================================================
-// BoB Pass 2, as ext_pass2_kernel.  Bound as Pass 1: B2 H16 N2048 d128 causal 160 us with slopes,
-// 183 with a cap; B4 H12 N4096 d64 430 and 570.
+// BoB Pass 2, as ext_pass2_kernel.  Its operands already hold the differences (h = F - alpha, C -
+// (alpha D + E)) and are summed over queries, whose roundings do not cancel: one bf16 value each.
+// Bound as Pass 1: B2 H16 N2048 d128 causal 139 us with slopes, 154 with a cap; B4 H12 N4096 d64 396
+// and 528.
 // ===========================================================================
 template <typename T, int D, int MC, int NW, int OCC, int KS, bool kPF, bool kCap>
 __global__ __launch_bounds__(KS * NW * 64, OCC) void score_pass2_kernel(

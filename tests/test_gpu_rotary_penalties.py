@@ -103,3 +103,34 @@ def test_heads_of_a_gradient_by_the_weights(fn):
                                                      gdWk=xd["uwk"], **options(xd, c))
     for a, b in zip(h, (hq, hk, hwq, hwk, hgq, hgk)):
         assert torch.equal(a, b)
+
+
+def test_captured_and_replayed():
+    """The weights' part of a penalty's gradient captured and replayed on changing inputs, with eager work between."""
+    c, x, xd, t = start("d128", 44)
+
+    def step():
+        y = native(t, xd, c)
+        g = torch.autograd.grad(y, [t["q"], t["k"]], [xd["gq"], xd["gk"]], create_graph=True)
+        h = torch.autograd.grad(g, list(t.values()), [xd["uq"], xd["uk"]])
+        return [a.detach() for a in (*y, *g, *h)]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    for _ in range(4):
+        with torch.no_grad():
+            for a in (*t.values(), xd["gq"], xd["uk"]):
+                a.copy_(torch.randn(a.shape, generator=gen, device="cuda"))
+            xd["positions"].add_(7)
+        graph.replay()
+        want = step()
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b)
