@@ -108,6 +108,11 @@ def _fast():
     return _native
 
 
+def _uncompiled(layer, *args):
+    """layer(*args) outside the graph that torch.compile is tracing, which has no place for ctypes and raw streams."""
+    return torch.compiler.disable(layer)(*args)
+
+
 def status_string(rc):
     return load_library().bob_status_string(int(rc)).decode()
 
@@ -210,6 +215,8 @@ def _stream(stream, like):
     tensors' device.  The library launches on the current HIP device, which
     _call sets to the tensors' device, so the stream must belong to it too."""
     if stream is None:
+        if torch.compiler.is_compiling():
+            return _uncompiled(_stream, None, like)
         return ctypes.c_void_p(torch.cuda.current_stream(like.device).cuda_stream)
     if stream.device != like.device:
         raise ValueError(f"stream is on {stream.device} but the tensors are on {like.device}")

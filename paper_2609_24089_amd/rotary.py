@@ -18,7 +18,7 @@ import ctypes
 import torch
 
 from . import (BOB_BF16, BOB_F32, _call, _differentiated, _dtype_code, _fast, _has_tangent, _p, _stream,
-               load_library)
+               _uncompiled, load_library)
 from .score import scored_attention
 
 HEAD_DIMS = (32, 64, 128, 256)
@@ -327,11 +327,12 @@ def rotate_heads(q, k, positions, rotary, q_weight=None, k_weight=None, eps=1e-6
     contiguous (q [B, H, N, d], k [B, Hkv, N, d]), with first and second derivatives for q, k and the weights on the HIP
     path.  The rotary pair and positions are as at the head of this file."""
     freqs, axes = rotary
-    if not torch.compiler.is_compiling():
-        # the same functions in C++ (csrc/torch_binding.cpp); None for calls it does not take
-        y = _fast().rotate_heads(q, k, positions, freqs, axes, q_weight, k_weight, float(eps), bool(interleaved))
-        if y is not None:
-            return y
+    if torch.compiler.is_compiling():
+        return _uncompiled(rotate_heads, q, k, positions, rotary, q_weight, k_weight, eps, interleaved)
+    # the same functions in C++ (csrc/torch_binding.cpp); None for calls it does not take
+    y = _fast().rotate_heads(q, k, positions, freqs, axes, q_weight, k_weight, float(eps), bool(interleaved))
+    if y is not None:
+        return y
     _Rotary(q, k, positions, freqs, axes, q_weight, k_weight, eps, interleaved)
     if freqs.requires_grad and torch.is_grad_enabled() or _has_tangent(freqs):
         raise ValueError("freqs have no gradient; detach them")

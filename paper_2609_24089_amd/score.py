@@ -21,7 +21,7 @@ import ctypes
 import torch
 
 from . import (BOB_OK, _call, _check_mats, _check_rows, _differentiated, _dtype_code, _fast, _has_tangent, _p, _rows_empty,
-               _stream, load_library, status_string)
+               _stream, _uncompiled, load_library, status_string)
 from .ext import AttnExtLaunch, _Problem, _ptr
 
 ATTN_SCORE_FWD, ATTN_SCORE_BWD, ATTN_SCORE_PASS1, ATTN_SCORE_PASS2 = range(4)
@@ -272,7 +272,9 @@ def scored_attention(q, k, v, scale=None, causal=False, cap=None, slopes=None, s
     values lie in a cache of kv_lens rows.  scale defaults to 1/sqrt(d)."""
     if scale is None:
         scale = q.shape[-1] ** -0.5
-    if not torch.compiler.is_compiling() and (cap is None or cap):
+    if torch.compiler.is_compiling():
+        return _uncompiled(scored_attention, q, k, v, scale, causal, cap, slopes, spans, kv_lens, q_lens, q_starts)
+    if cap is None or cap:
         # the same functions in C++ (csrc/torch_binding.cpp); None for calls it does not take
         O = _fast().scored_attention(q, k, v, float(scale), bool(causal), float(cap or 0), slopes, spans, kv_lens, q_lens,
                                      q_starts)
