@@ -27,6 +27,20 @@ def test_every_output(cap, scale, loud, dtype):
     compare(chain({n: t.cuda() for n, t in x.items()}, c, scale), reference(x, c, scale), c, OUTS)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", ["late", "saturated"])
+def test_derivatives_at_hard_scores(name, dtype):
+    """Scores that grow along the keys, so that the forward's reference moves late, far below their cap; and scores of
+    standard deviation 240 under a cap of 5, of which one in thirty has a derivative."""
+    cap, tau = (1000.0, 0.125) if name == "late" else (5.0, 30.0)
+    c = dict(B=1, H=2, Hkv=2, Nq=90, Nk=400, d=64, cap=cap, dtype=dtype)
+    x = make(c, 82)
+    if name == "late":
+        x["K"] = (x["K"].float() * 0.1 + 0.05 * torch.linspace(-40.0, 40.0, 400)[:, None]).to(x["K"].dtype)
+    say(f"[cap] {name} {dtype}")
+    compare(chain({n: t.cuda() for n, t in x.items()}, c, tau), reference(x, c, tau), c, OUTS)
+
+
 def two_tiles(c, seed):
     """All scores of the ordinary rows lie near 0.111 of the cap (c x0, spread 1); row 5 has scores of 0.82 of the cap
     with the first 32 keys and near 0 with the others, so its tile of the first keys is one with scores close to the
